@@ -383,6 +383,177 @@ NTC_API ntc_status ntc_kmeans_map(const float *h_features, uint32_t n, uint32_t 
                                   const uint32_t *h_init, uint32_t max_iters, uint32_t *h_map,
                                   double *h_centroids, uint32_t *iters_run);
 
+/* ------------------------------------------------------------ routed experts
+ *
+ * Experts whose assignment is learned: a router gives every token (a texel's
+ * latent features, or any other row) top_k of num_experts experts and their
+ * weights, the (token, slot) entries are ordered by expert, each expert's rows go
+ * through its linear layers and the token's rows are blended.  The paper fixes
+ * the map c(i) before training (Sec. 3.3); these calls are its trainable
+ * counterpart, with decoders of any width, and have no paper counterpart.
+ *
+ * The calls keep no state and need no context.  Every pointer is a device
+ * pointer unless named h_*; matrices are row-major with a leading dimension in
+ * elements; calls are asynchronous on cuda_stream (a cudaStream_t) and may be
+ * captured in a graph.  Outputs must not overlap inputs.  Indices that come
+ * from device memory (ids, rows, place, offsets) are checked by the kernels: no
+ * value of theirs leads outside the buffers. */
+
+typedef enum { NTC_TYPE_FP32 = 0, NTC_TYPE_FP16 = 1, NTC_TYPE_BF16 = 2 } ntc_type;
+
+#define NTC_MAX_EXPERTS 1024u
+#define NTC_MAX_TOP_K 32u
+#define NTC_SCORE_SOFTMAX 0u
+#define NTC_SCORE_SIGMOID 1u
+
+/* Routing.  For the logits l of a token: s = softmax(l) or sigmoid(l); each
+ * expert's choice value is c = s + bias (fp32).  With num_groups > 1 the experts
+ * form that many groups of consecutive experts; a group's value is the sum of
+ * its two largest c (of its only one), the top_groups groups of the largest
+ * value stay, ties to the lower group.  ids are the top_k experts of the largest
+ * c, in descending order, ties to the lower index; weights are
+ * scale * s_j / (renormalize ? sum of the chosen s : 1), without the bias.
+ * A logit of -inf or NaN masks its expert out (s = 0, never chosen); +inf counts
+ * as the largest finite value.  Where fewer than top_k experts are left, the
+ * remaining ids are -1 and their weights 0; where the chosen s sum to 0 the
+ * renormalized weights are 0.  Scores and sums are fp32. */
+typedef struct {
+  uint32_t num_experts; /* 1 .. NTC_MAX_EXPERTS                              */
+  uint32_t top_k;       /* 1 .. min(NTC_MAX_TOP_K, the kept groups' experts) */
+  uint32_t num_groups;  /* divides num_experts; 1 = no groups; at most 32    */
+  uint32_t top_groups;  /* 1 .. num_groups                                   */
+  uint32_t score;       /* NTC_SCORE_SOFTMAX or NTC_SCORE_SIGMOID            */
+  uint32_t renormalize; /* 0 or 1                                            */
+  float scale;          /* finite                                            */
+  ntc_type type;        /* of the logits and of their gradient               */
+} ntc_route_desc;
+
+/* logits[n][ld_logits >= num_experts]; bias[num_experts] fp32 or NULL; out:
+ * ids[n][top_k] int32, weights[n][top_k] fp32. */
+NTC_API ntc_status ntc_route(const ntc_route_desc *desc, size_t n, const void *logits, size_t ld_logits,
+                             const float *bias, int32_t *ids, float *weights, void *cuda_stream);
+
+/* The gradient of the logits, dlogits[n][num_experts] (contiguous, desc->type),
+ * for the gradient dweights[n][top_k] (fp32) of the weights of ids[n][top_k] as
+ * ntc_route returned them (an id outside 0..num_experts-1 contributes nothing;
+ * a repeated id contributes each time).  The choice itself and the bias have no
+ * gradient.  Masked logits get 0.  desc's groups are not read. */
+NTC_API ntc_status ntc_route_backward(const ntc_route_desc *desc, size_t n, const void *logits,
+                                      size_t ld_logits, const int32_t *ids, const float *dweights,
+                                      void *dlogits, void *cuda_stream);
+
+/* The stable order of n = tokens * top_k entries by expert.  ids[n]: expert of
+ * each entry; an id outside 0..num_experts-1 belongs to no expert and comes
+ * after all.  out: rows[n] = token (entry / top_k) of each ordered entry,
+ * place[n] = ordered position of each entry, offsets[num_experts + 1] = first
+ * position of each expert; positions from offsets[num_experts] on belong to no
+ * expert.  int32; n < 2^31.  workspace: ntc_expert_order_workspace bytes
+ * (16-byte aligned; may be NULL when that is 0). */
+NTC_API size_t ntc_expert_order_workspace(size_t n, uint32_t num_experts);
+NTC_API ntc_status ntc_expert_order(const int32_t *ids, size_t n, uint32_t top_k, uint32_t num_experts,
+                                    int32_t *rows, int32_t *place, int32_t *offsets, void *workspace,
+                                    size_t workspace_bytes, void *cuda_stream);
+
+#define NTC_ACT_NONE 0u
+#define NTC_ACT_RELU 1u
+#define NTC_ACT_LEAKY 2u /* leaky_slope * z for z <= 0 */
+#define NTC_ACT_GELU 3u  /* z * Phi(z), Phi the normal distribution function */
+#define NTC_ACT_SILU 4u  /* z / (1 + exp(-z)) */
+
+/* One linear layer of every expert.  For a position i of expert e
+ * (offsets[e] <= i < offsets[e + 1]):
+ *   z_i = W_e x_r + b_e,  r = rows[i] (i without rows);   y_i = act(z_i) + residual_i
+ * and rows of y (and z) of no expert are 0.  Without offsets there is one expert
+ * that has every position.  fp16 or bf16 operands, fp32 accumulation and
+ * epilogue, one rounding at the end; an index of rows outside 0..num_x_rows-1
+ * reads a row of zeros.
+ * Any width, stride and alignment is taken; where TMA cannot read an operand
+ * (address not a multiple of 16 bytes, or leading dimension not of 8 elements)
+ * the call copies it into the workspace first. */
+typedef struct {
+  ntc_type type;        /* NTC_TYPE_FP16 or NTC_TYPE_BF16: x, w, y, z, residual */
+  uint32_t in_dim;      /* K, 1 .. 2^20                                        */
+  uint32_t out_dim;     /* N, 1 .. 2^20                                        */
+  uint32_t num_experts; /* E, 1 .. NTC_MAX_EXPERTS; 1 without offsets          */
+  uint32_t activation;  /* NTC_ACT_*                                           */
+  float leaky_slope;    /* finite                                              */
+  uint64_t num_rows;    /* positions: rows of y, z, residual, rows[]           */
+  uint64_t num_x_rows;  /* rows of x; equal to num_rows without rows           */
+  uint64_t ld_x;        /* >= in_dim                                           */
+  uint64_t ld_w;        /* >= in_dim                                           */
+  uint64_t stride_w;    /* elements from one expert's weights to the next's    */
+  uint64_t ld_y;        /* >= out_dim; of y, or of dy in the backward call     */
+  uint64_t ld_z;        /* >= out_dim                                          */
+  uint64_t ld_residual; /* >= out_dim                                          */
+} ntc_linear_desc;
+
+/* Bytes of workspace for a call with this descriptor and these operands (16-byte
+ * aligned when not 0); 0 for a descriptor the call would refuse. */
+NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, const void *w);
+
+/* x[num_x_rows][ld_x], w[E][N][ld_w], bias[E][N] fp32 (contiguous) or NULL,
+ * residual[num_rows][ld_residual] or NULL, rows[num_rows] int32 or NULL,
+ * offsets[E + 1] int32 (non-decreasing) or NULL; out: y[num_rows][ld_y] and,
+ * unless NULL, z[num_rows][ld_z]. */
+NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void *x, const int32_t *rows,
+                              const int32_t *offsets, const void *w, const float *bias, const void *residual,
+                              void *y, void *z, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Gradients of ntc_linear for dy[num_rows][ld_y], with z as the forward call
+ * stored it (may be NULL with NTC_ACT_NONE): dz = dy * act'(z), then
+ *   dx_i = W_e^T dz_i (a row per position, contiguous [num_rows][K]; rows of no
+ *   expert 0; ntc_combine without weights sums a token's),
+ *   dw_e = sum_i dz_i x_{rows[i]}^T (contiguous [E][N][K]), db_e = sum_i dz_i
+ *   (fp32 [E][N]).  Any of dx, dw, db may be NULL; x may be NULL without dw,
+ * w without dx.  dz is rounded to the operands' type for the two products and
+ * summed for db before that rounding.  dx, dw in the operands' type.  act'(0) is
+ * 0 (ReLU) or leaky_slope.  The sums' order is fixed: equal calls give equal bits. */
+NTC_API size_t ntc_linear_backward_workspace(const ntc_linear_desc *desc, const void *dy, const void *x,
+                                             const void *w);
+NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, const void *dy, const void *z, const void *x,
+                                       const int32_t *rows, const int32_t *offsets, const void *w, void *dx,
+                                       void *dw, float *db, void *workspace, size_t workspace_bytes,
+                                       void *cuda_stream);
+
+/* Whether a kernel of ntc_linear or ntc_linear_backward gave up one of its
+ * bounded waits (200 ms each) on the current device since the last call of
+ * this: NTC_ERR_CUDA then (results since are invalid), and the record is
+ * cleared.  Synchronises the stream. */
+NTC_API ntc_status ntc_linear_status(void *cuda_stream);
+
+/* The blend: out_t = residual_t + sum_j weights[t][j] * y[place[t][j]] over j <
+ * top_k, in fp32, rounded once.  An entry whose place is outside
+ * 0..live-1 (live = offsets[num_experts], or num_rows without offsets) is left
+ * out, whatever its weight and row hold. */
+typedef struct {
+  ntc_type type;        /* NTC_TYPE_*: y, residual, out and their gradients */
+  uint32_t dim;         /* columns, 1 .. 2^20                               */
+  uint32_t top_k;       /* 1 .. NTC_MAX_TOP_K                               */
+  uint32_t num_experts; /* 1 .. NTC_MAX_EXPERTS; where offsets[] ends       */
+  uint64_t num_tokens;  /* rows of out                                      */
+  uint64_t num_rows;    /* rows of y                                        */
+  uint64_t ld_y;        /* >= dim                                           */
+  uint64_t ld_out;      /* >= dim; of out, or of dout in the backward call  */
+  uint64_t ld_residual; /* >= dim                                           */
+} ntc_combine_desc;
+
+/* place[num_tokens][top_k] int32; weights[num_tokens][top_k] fp32 or NULL (all
+ * 1: with a linear layer's dx for y this is the gradient of its gathered
+ * input); residual[num_tokens][ld_residual] or NULL. */
+NTC_API ntc_status ntc_combine(const ntc_combine_desc *desc, const void *y, const int32_t *place,
+                               const float *weights, const int32_t *offsets, const void *residual, void *out,
+                               void *cuda_stream);
+
+/* Gradients for dout[num_tokens][ld_out]: dy[place[t][j]] = weights[t][j] * dout_t
+ * (contiguous [num_rows][dim]) and dweights[t][j] = <dout_t, y[place[t][j]]>
+ * (fp32).  An entry left out of the blend gives dweights 0; its row of dy is 0
+ * where its place is inside 0..num_rows-1.  place must name every row of dy
+ * exactly once for all of dy to be written (as ntc_expert_order's does).  dy or
+ * dweights may be NULL.  The residual's gradient is dout itself. */
+NTC_API ntc_status ntc_combine_backward(const ntc_combine_desc *desc, const void *dout, const void *y,
+                                        const int32_t *place, const float *weights, const int32_t *offsets,
+                                        void *dy, float *dweights, void *cuda_stream);
+
 /* Human-readable message of the last failed call on this host thread (no
  * paper counterpart). */
 NTC_API const char *ntc_last_error(void);

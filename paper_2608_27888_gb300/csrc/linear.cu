@@ -1,0 +1,991 @@
+// Linear layers of many experts and their gradients, on one tcgen05 product.
+//
+//   forward   y_i  = act(W_e x_{r(i)} + b_e) + residual_i    contraction over K
+//   kDx       dx_i = W_e^T dz_i                               contraction over N
+//   kDw       dw_e = sum_i dz_i x_{r(i)}^T                    contraction over e's rows
+//
+// One persistent CTA per SM.  A tile is 128 rows of one expert times BN columns;
+// its operands come in chunks of 64 of the contraction (128 bytes, the swizzle's
+// width) through a ring of shared-memory stages:
+//   warp 0       issues the TMA copies.  Gathered rows (x through rows[]) come by
+//                tile::gather4, four rows an instruction, all lanes issuing; rows
+//                past an expert's end get an index outside the matrix, which TMA
+//                fills with zeros -- so an expert may end anywhere in a tile, and
+//                anywhere in a chunk of kDw's contraction.
+//   warp 1       issues the MMAs (M = 128, N = BN) into one of two TMEM
+//                accumulators.
+//   warps 4..11  the epilogue of one accumulator while the other is filled: 16
+//                columns at a time through a warp's own shared memory, so that
+//                global memory sees 32-byte runs of a row, not one row a lane.
+// A weight matrix [N][K] is read as it lies: K-major in the forward product,
+// MN-major (the descriptors' transpose bits) in kDx; kDw takes both operands
+// MN-major.  Nothing is transposed in memory.
+#include "experts.cuh"
+#include "tcgen05.cuh"
+
+#include <cuda.h>
+
+using namespace ntc;
+
+namespace {
+
+enum Mode { kForward = 0, kDx = 1, kDw = 2 };
+
+constexpr int kThreads = 384;
+constexpr int kEpilogueWarps = 8;
+constexpr uint32_t kRows = 128;   // rows of a tile
+constexpr uint32_t kChunk = 64;   // contraction elements of a stage
+constexpr uint32_t kBand = 16;    // row tiles that are walked together (reuse in L2)
+constexpr uint32_t kABytes = kRows * 128;
+constexpr uint32_t kRing = 196608;  // bytes of all stages
+constexpr uint32_t kStageCols = 16;  // columns of the epilogue's staging
+constexpr uint32_t kMaxStages = 8;
+
+constexpr uint32_t stage_bytes(int BN) { return kABytes + (uint32_t)BN * 128; }
+constexpr uint32_t stages(int BN) {
+  return kRing / stage_bytes(BN) < kMaxStages ? kRing / stage_bytes(BN) : kMaxStages;
+}
+
+struct Shared {
+  uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+  uint32_t tmem, quit;
+  int32_t off[NTC_MAX_EXPERTS + 2];       // first row of each expert; [E]: of no expert; [E + 1]: the end
+  uint32_t tile[NTC_MAX_EXPERTS + 2];     // first row tile of each expert (and of no expert); the total
+};
+constexpr size_t kSharedBytes = 1024 + kRing + kEpilogueWarps * 32 * kStageCols * 4 + sizeof(Shared);
+static_assert(kSharedBytes <= 232448, "shared memory of one CTA");
+
+struct Args {
+  const int32_t *rows, *offsets;
+  const float *bias;
+  const void *residual;
+  void *out, *z;
+  uint64_t ld_out, ld_z, ld_residual;
+  uint32_t num_experts, num_rows, x_rows;
+  uint32_t width;      // columns of the output
+  uint32_t height;     // kDw: rows of one expert's output
+  uint32_t depth;      // contraction length (not kDw: there it is the expert's rows)
+  uint32_t activation;
+  float slope;
+  uint32_t bf16, vec_out, vec_z, vec_residual;
+  unsigned int *status;
+};
+
+__device__ unsigned int g_linear_status;
+
+// ------------------------------------------------------------------ PTX
+
+__device__ __forceinline__ void expect_tx(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, int32_t y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n" ::"r"(dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, int32_t y, int32_t e) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n" ::"r"(
+          dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(e)
+      : "memory");
+}
+// Four rows of 64 columns from column x on; the map's box is one row high.
+__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, const int32_t (&r)[4]) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], "
+      "[%2];\n" ::"r"(dst),
+      "l"(map), "r"(bar), "r"(x), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+      : "memory");
+}
+// D[tmem] (+)= A[smem] x B[smem]
+__device__ __forceinline__ void umma_ss(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                        uint32_t accum) {
+  asm volatile(
+      "{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %6, 0;\nmov.b64 a, {%1, %2};\nmov.b64 b, {%3, %4};\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}\n" ::"r"(d),
+      "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accum)
+      : "memory");
+}
+
+// Descriptor words of a 128-byte-swizzled operand: 8-row groups 1,024 bytes apart
+// (K-major: rows of the matrix; MN-major: rows of the contraction); MN-major
+// operands wider than 64 continue `block` bytes further on.
+__device__ __forceinline__ uint32_t sw128_lo(uint32_t addr, uint32_t block) {
+  return ((addr >> 4) & 0x3FFFu) | ((block >> 4) << 16);
+}
+constexpr uint32_t kSw128Hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+
+// ------------------------------------------------------------ waits
+
+// A bounded wait.  The first one that gives up sets the status word and the
+// CTA's quit flag, which ends the others'.
+struct Waiter {
+  volatile uint32_t *quit;
+  unsigned int *status;
+  __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = global_ns();
+    while (!mbar_try_wait(bar, parity)) {
+      if (*quit) return false;
+      if (global_ns() - t0 > kWaitLimitNs) {
+        *quit = 1;
+        atomicOr(status, 1u);
+        return false;
+      }
+    }
+    return true;
+  }
+};
+
+// ------------------------------------------------------------ tiles
+
+struct Tile {
+  uint32_t e;         // expert; num_experts: rows of no expert
+  uint32_t row;       // first row: of the matrix (kDw: of the expert's output)
+  uint32_t rows;      // rows inside, at most 128
+  uint32_t col;       // first column
+  uint32_t depth;     // contraction length; 0: the tile is zeros
+  uint32_t begin;     // kDw: first row of the contraction
+};
+
+// Experts' rows and row tiles, from offsets that are only trusted to lie
+// anywhere: they are held inside 0..num_rows, an expert that ends before it begins
+// has no rows.  Called by the whole CTA; ends with a barrier.
+__device__ __forceinline__ void make_table(int32_t *off, uint32_t *tile, const int32_t *offsets, uint32_t E, uint32_t num_rows) {
+  for (uint32_t e = threadIdx.x; e <= E; e += blockDim.x)
+    off[e] = offsets ? offset_at(offsets, e, (int32_t)num_rows) : e ? (int32_t)num_rows : 0;
+  if (threadIdx.x == 0) off[E + 1] = (int32_t)num_rows;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    const uint32_t lane = threadIdx.x;
+    uint32_t base = 0;
+    for (uint32_t e0 = 0; e0 <= E; e0 += 32) {
+      const uint32_t e = e0 + lane;
+      const uint32_t mine = e <= E ? ((uint32_t)max(off[e + 1] - off[e], 0) + kRows - 1) / kRows : 0u;
+      uint32_t in = mine;
+#pragma unroll
+      for (int s = 1; s < 32; s <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, in, s);
+        if (lane >= (uint32_t)s) in += o;
+      }
+      if (e <= E) tile[e] = base + in - mine;
+      base += __shfl_sync(0xFFFFFFFFu, in, 31);
+    }
+    if (lane == 0) tile[E + 1] = base;
+  }
+  __syncthreads();
+}
+
+// The bucket that row tile q lies in: the last e with tile[e] <= q and a tile of its own.
+__device__ __forceinline__ uint32_t bucket_of_tile(const uint32_t *tile, uint32_t E, uint32_t q) {
+  uint32_t lo = 0, hi = E + 1;  // tile[lo] <= q < tile[hi]
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (tile[mid] <= q) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+template <int MODE, int BN>
+struct Tiles {
+  const Args &a;
+  const Shared &s;
+  uint32_t cols, row_tiles;
+  uint64_t total;
+  __device__ __forceinline__ Tiles(const Args &args, const Shared &sh) : a(args), s(sh) {
+    cols = (a.width + BN - 1) / BN;
+    row_tiles = (a.height + kRows - 1) / kRows;
+    total = MODE == kDw ? (uint64_t)a.num_experts * row_tiles * cols : (uint64_t)s.tile[a.num_experts + 1] * cols;
+  }
+  // Within an expert: bands of kBand row tiles, columns inside a band, rows inside
+  // a column, so that the CTAs at work at one time share operands.
+  __device__ __forceinline__ Tile at(uint64_t t) const {
+    Tile o;
+    uint32_t many, r;
+    if constexpr (MODE == kDw) {
+      const uint64_t per = (uint64_t)row_tiles * cols;
+      o.e = (uint32_t)(t / per);
+      r = (uint32_t)(t - o.e * per);
+      many = row_tiles;
+    } else {
+      o.e = bucket_of_tile(s.tile, a.num_experts, (uint32_t)(t / cols));
+      r = (uint32_t)(t - (uint64_t)s.tile[o.e] * cols);
+      many = s.tile[o.e + 1] - s.tile[o.e];
+    }
+    const uint32_t band = r / (kBand * cols), in = r - band * kBand * cols;
+    const uint32_t high = min(kBand, many - band * kBand);
+    const uint32_t row = (band * kBand + in % high) * kRows;
+    o.col = in / high * BN;
+    const uint32_t begin = (uint32_t)s.off[o.e], count = (uint32_t)max(s.off[o.e + 1] - s.off[o.e], 0);
+    if constexpr (MODE == kDw) {
+      o.row = row;
+      o.rows = min(kRows, a.height - row);
+      o.begin = begin;
+      o.depth = count;
+    } else {
+      o.row = begin + row;
+      o.rows = min(kRows, count - row);
+      o.begin = 0;
+      o.depth = o.e < a.num_experts ? a.depth : 0u;
+    }
+    return o;
+  }
+};
+
+// ------------------------------------------------------------ epilogue
+
+__device__ __forceinline__ void activate(uint32_t act, float slope, float (&v)[8]) {
+  if (act == NTC_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];  // NaN stays
+  } else if (act == NTC_ACT_LEAKY) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = v[i] > 0.0f ? v[i] : slope * v[i];
+  } else if (act == NTC_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.5f * v[i] * (1.0f + erff(v[i] * 0.70710678f));
+  } else if (act == NTC_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __fdividef(v[i], 1.0f + __expf(-v[i]));
+  }
+}
+
+__device__ __forceinline__ void load8(const void *p, uint64_t at, int n, bool vec, bool bf16, float (&v)[8]) {
+  if (bf16) load_vec<__nv_bfloat16>((const __nv_bfloat16 *)p + at, n, vec, v);
+  else load_vec<__half>((const __half *)p + at, n, vec, v);
+}
+__device__ __forceinline__ void store8(void *p, uint64_t at, int n, bool vec, bool bf16, const float (&v)[8]) {
+  if (bf16) store_vec<__nv_bfloat16>((__nv_bfloat16 *)p + at, n, vec, v);
+  else store_vec<__half>((__half *)p + at, n, vec, v);
+}
+
+// Offset of 16-byte piece c (0..3) of row r in a warp's staging, 64 bytes a row:
+// the pieces of two rows are mixed so that eight lanes meet eight banks' groups
+// both when lanes hold rows and when they hold pieces.
+__device__ __forceinline__ uint32_t staged(uint32_t r, uint32_t c) {
+  return (r >> 1) * 128 + (((((r & 1) << 2) | c) ^ ((r >> 1) & 3)) << 4);
+}
+
+// ------------------------------------------------------------ the kernel
+
+template <int MODE, int BN>
+__global__ void __launch_bounds__(kThreads, 1)
+    k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_ag,
+             const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_bg, const Args a) {
+  constexpr uint32_t kStages = stages(BN), kStage = stage_bytes(BN);
+  extern __shared__ uint8_t raw[];
+  uint8_t *ring = raw + (1024 - (saddr(raw) & 1023)) % 1024;
+  uint8_t *staging = ring + kRing;
+  Shared &s = *reinterpret_cast<Shared *>(staging + kEpilogueWarps * 32 * kStageCols * 4);
+  const uint32_t warp = uniform(threadIdx.x / 32), lane = threadIdx.x & 31;
+
+  if (threadIdx.x == 0) {
+    for (uint32_t i = 0; i < kStages; ++i) {
+      mbar_init(saddr(&s.full[i]), 1);
+      mbar_init(saddr(&s.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(saddr(&s.acc_full[i]), 1);
+      mbar_init(saddr(&s.acc_empty[i]), kEpilogueWarps);
+    }
+    mbar_init(saddr(&s.drain), 1);
+    s.quit = 0;
+    mbar_init_fence();
+  }
+  if (warp == 2) tmem_alloc(saddr(&s.tmem));
+  pdl_wait();
+  make_table(s.off, s.tile, a.offsets, a.num_experts, a.num_rows);
+  fence_after();
+  const uint32_t tmem = s.tmem;
+  const Waiter wait{&s.quit, a.status};
+  const Tiles<MODE, BN> tiles(a, s);
+
+  if (warp == 0) {
+    uint32_t issued = 0;
+    bool ok = true;
+    for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
+      const Tile o = tiles.at(t);
+      const uint32_t chunks = (o.depth + kChunk - 1) / kChunk;
+      int32_t idx[4];
+      if (MODE == kForward && a.rows) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t r = lane * 4 + i;
+          const int32_t at = r < o.rows ? (int32_t)ld_word((const uint32_t *)a.rows + o.row + r) : -1;
+          idx[i] = (uint32_t)at < a.x_rows ? at : (int32_t)a.x_rows;
+        }
+      }
+      for (uint32_t c = 0; c < chunks; ++c, ++issued) {
+        const uint32_t st = issued % kStages;
+        if (MODE == kDw) {  // the rows of this chunk; past the expert's end: none
+          const uint32_t r0 = c * kChunk + (lane & 15) * 4;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool in = r0 + i < o.depth;
+            const int32_t at = !in ? -1 : a.rows ? (int32_t)ld_word((const uint32_t *)a.rows + o.begin + r0 + i)
+                                                 : (int32_t)(o.begin + r0 + i);
+            idx[i] = (uint32_t)at < a.x_rows ? at : (int32_t)a.x_rows;
+          }
+        }
+        ok = wait(saddr(&s.empty[st]), ((issued / kStages) & 1) ^ 1);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        const uint32_t bar = saddr(&s.full[st]);
+        const uint32_t sa = saddr(ring) + st * kStage, sb = sa + kABytes;
+        if constexpr (MODE != kDw) {
+          const uint32_t pieces = MODE == kForward && a.rows ? (o.rows + 3) / 4 : (o.rows + 31) / 32;
+          const uint32_t bytes = pieces * (MODE == kForward && a.rows ? 512u : 4096u);
+          if (lane == 0) expect_tx(bar, bytes + BN * 128);
+          __syncwarp();
+          if (MODE == kForward && a.rows) {
+            if (lane < pieces) tma_gather4(sa + lane * 512, &map_ag, bar, (int32_t)(c * kChunk), idx);
+          } else if (lane < pieces) {
+            tma_2d(sa + lane * 4096, &map_a, bar, (int32_t)(c * kChunk), (int32_t)(o.row + lane * 32));
+          }
+          if constexpr (MODE == kForward) {
+            if (lane == 0) tma_3d(sb, &map_b, bar, (int32_t)(c * kChunk), (int32_t)o.col, (int32_t)o.e);
+          } else {
+            if (lane < BN / 64)
+              tma_3d(sb + lane * 8192, &map_b, bar, (int32_t)(o.col + lane * 64), (int32_t)(c * kChunk), (int32_t)o.e);
+          }
+        } else {
+          const bool whole = (c + 1) * kChunk <= o.depth;
+          if (lane == 0) expect_tx(bar, kABytes + BN * 128);
+          __syncwarp();
+          const uint32_t g = lane & 15, half = lane >> 4;
+          if (whole) {
+            if (lane < 2)
+              tma_2d(sa + lane * 8192, &map_a, bar, (int32_t)(o.row + lane * 64), (int32_t)(o.begin + c * kChunk));
+          } else {
+            int32_t own[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint32_t r = c * kChunk + g * 4 + i;
+              own[i] = (int32_t)(r < o.depth ? o.begin + r : a.num_rows);
+            }
+            tma_gather4(sa + half * 8192 + g * 512, &map_ag, bar, (int32_t)(o.row + half * 64), own);
+          }
+          if (whole && !a.rows) {
+            if (lane < BN / 64)
+              tma_2d(sb + lane * 8192, &map_b, bar, (int32_t)(o.col + lane * 64), (int32_t)(o.begin + c * kChunk));
+          } else {
+#pragma unroll
+            for (uint32_t j = half; j < BN / 64; j += 2)
+              tma_gather4(sb + j * 8192 + g * 512, &map_bg, bar, (int32_t)(o.col + j * 64), idx);
+          }
+        }
+      }
+    }
+    pdl_trigger();
+    if (!ok)  // the copies in flight land before the CTA ends
+      for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
+        mbar_wait(saddr(&s.full[j % kStages]), (j / kStages) & 1);
+  } else if (warp == 1) {
+    const uint32_t idesc = (1u << 4) | (a.bf16 << 7) | (a.bf16 << 10) | ((MODE == kDw ? 1u : 0u) << 15) |
+                           ((MODE != kForward ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((kRows >> 4) << 24);
+    // 16 of the contraction: 32 bytes along a K-major row, 16 rows of an MN-major block
+    constexpr uint32_t kStepA = MODE == kDw ? 2048 >> 4 : 32 >> 4, kStepB = MODE != kForward ? 2048 >> 4 : 32 >> 4;
+    uint32_t used = 0, acc = 0;
+    bool ok = true, any = false;
+    for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
+      const Tile o = tiles.at(t);
+      if (o.depth == 0) continue;
+      const uint32_t chunks = (o.depth + kChunk - 1) / kChunk;
+      ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.acc_empty[acc & 1]), ((acc >> 1) & 1) ^ 1));
+      if (!ok) break;
+      fence_after();
+      const uint32_t d = uniform(tmem + (acc & 1) * BN);
+      for (uint32_t c = 0; c < chunks; ++c, ++used) {
+        const uint32_t st = used % kStages;
+        ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.full[st]), (used / kStages) & 1));
+        if (!ok) break;
+        fence_after();
+        any = true;
+        const uint32_t sa = saddr(ring) + st * kStage;
+        const uint32_t alo = uniform(sw128_lo(sa, 8192)), blo = uniform(sw128_lo(sa + kABytes, 8192));
+        if (elect_one()) {
+#pragma unroll
+          for (uint32_t k = 0; k < kChunk / 16; ++k)
+            umma_ss(d, alo + k * kStepA, kSw128Hi, blo + k * kStepB, kSw128Hi, idesc, (c | k) != 0);
+          umma_commit(saddr(&s.empty[st]));
+          if (c + 1 == chunks) umma_commit(saddr(&s.acc_full[acc & 1]));
+        }
+        __syncwarp();
+      }
+      ++acc;
+    }
+    if (!ok && any) {
+      if (elect_one()) umma_commit(saddr(&s.drain));
+      __syncwarp();
+      mbar_wait(saddr(&s.drain), 0);
+    }
+  } else if (warp >= 4) {
+    const uint32_t w = warp - 4, quarter = warp & 3;
+    const uint32_t part = (w >> 2) * (BN / 2);  // each set of four warps takes half of the columns
+    uint8_t *mine = staging + w * 32 * kStageCols * 4;
+    const uint32_t base = saddr(mine);
+    const bool bf16 = a.bf16;
+    uint32_t acc = 0;
+    for (uint64_t t = blockIdx.x; t < tiles.total; t += gridDim.x) {
+      const Tile o = tiles.at(t);
+      const bool zero = o.depth == 0;
+      if (!zero) {
+        if (!__all_sync(0xFFFFFFFFu, wait(saddr(&s.acc_full[acc & 1]), (acc >> 1) & 1))) break;
+        fence_after();
+      }
+      const int32_t high = (int32_t)o.rows - (int32_t)(quarter * 32);  // rows of this warp inside
+      const uint64_t row0 = (MODE == kDw ? (uint64_t)o.e * a.height : 0) + o.row + quarter * 32;
+      if (high > 0) {
+        for (uint32_t c0 = part; c0 < part + BN / 2 && o.col + c0 < a.width; c0 += kStageCols) {
+          if (!zero) {
+            uint32_t r[16];
+            tmem_ld16(tmem + ((quarter * 32) << 16) + (acc & 1) * BN + c0, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q)
+              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(base + staged(lane, q)), "r"(r[4 * q]),
+                           "r"(r[4 * q + 1]), "r"(r[4 * q + 2]), "r"(r[4 * q + 3])
+                           : "memory");
+            __syncwarp();
+          }
+          const uint32_t col = o.col + c0 + (lane & 1) * 8;
+          const int n = min(8, (int)a.width - (int)col);
+          if (n > 0) {
+            float b[8];
+            if (MODE == kForward && a.bias && !zero) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) b[i] = i < n ? a.bias[(uint64_t)o.e * a.width + col + i] : 0.0f;
+            } else {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+            }
+#pragma unroll
+            for (uint32_t it = 0; it < 2; ++it) {
+              const uint32_t rl = (lane >> 1) + 16 * it;
+              if ((int32_t)rl < high) {
+                float v[8];
+                if (zero) {
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+                } else {
+                  const float4 f = *reinterpret_cast<const float4 *>(mine + staged(rl, (lane & 1) * 2));
+                  const float4 g = *reinterpret_cast<const float4 *>(mine + staged(rl, (lane & 1) * 2 + 1));
+                  v[0] = f.x + b[0], v[1] = f.y + b[1], v[2] = f.z + b[2], v[3] = f.w + b[3];
+                  v[4] = g.x + b[4], v[5] = g.y + b[5], v[6] = g.z + b[6], v[7] = g.w + b[7];
+                }
+                if constexpr (MODE == kForward) {
+                  if (a.z) store8(a.z, (row0 + rl) * a.ld_z + col, n, a.vec_z, bf16, v);
+                  if (!zero) {
+                    activate(a.activation, a.slope, v);
+                    if (a.residual) {
+                      float x[8];
+                      load8(a.residual, (row0 + rl) * a.ld_residual + col, n, a.vec_residual, bf16, x);
+#pragma unroll
+                      for (int i = 0; i < 8; ++i) v[i] += x[i];
+                    }
+                  }
+                }
+                store8(a.out, (row0 + rl) * a.ld_out + col, n, a.vec_out, bf16, v);
+              }
+            }
+          }
+          __syncwarp();
+        }
+      }
+      if (!zero) {
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(saddr(&s.acc_empty[acc & 1]));
+        ++acc;
+      }
+    }
+  }
+  fence_before();
+  __syncthreads();
+  if (warp == 2) {
+    fence_after();
+    tmem_dealloc(tmem);
+  }
+}
+
+// ------------------------------------------------------------ dz, db, copies
+
+__device__ __forceinline__ float act_slope(uint32_t act, float slope, float z) {
+  switch (act) {
+    case NTC_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
+    case NTC_ACT_LEAKY: return z > 0.0f ? 1.0f : slope;
+    case NTC_ACT_GELU:
+      return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
+    case NTC_ACT_SILU: {
+      const float s = 1.0f / (1.0f + expf(-z));
+      return s * (1.0f + z * (1.0f - s));
+    }
+    default: return 1.0f;
+  }
+}
+
+struct DzArgs {
+  const void *dy, *z;
+  const int32_t *offsets;
+  void *dz;       // or NULL: dy is the operand as it is
+  float *part;    // [row tile][pitch] sums of dz over the tile's rows, or NULL
+  uint64_t ld_dy, ld_z;
+  uint32_t num_experts, num_rows, width, pitch, activation;
+  float slope;
+  uint32_t bf16, vec_dy, vec_z;
+};
+
+constexpr int kDzThreads = 256;
+constexpr uint32_t kDzCols = 256;  // columns of one CTA: 32 pieces of 8; its 8 warps take every eighth row
+
+struct TableShared {
+  int32_t off[NTC_MAX_EXPERTS + 2];
+  uint32_t tile[NTC_MAX_EXPERTS + 2];
+};
+
+// dz = dy act'(z), rounded for the two products, and its column sums per row
+// tile before that rounding.  One pass over dy and z, HBM-bound.
+__global__ void __launch_bounds__(kDzThreads) k_dz(const DzArgs a) {
+  extern __shared__ uint8_t raw[];
+  TableShared &s = *reinterpret_cast<TableShared *>(raw);
+  __shared__ float sums[8][kDzCols];
+  pdl_wait();
+  pdl_trigger();
+  make_table(s.off, s.tile, a.offsets, a.num_experts, a.num_rows);
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const uint32_t col = blockIdx.x * kDzCols + lane * 8;
+  const int n = min(8, (int)a.width - (int)col);
+  const uint32_t total = s.tile[a.num_experts];
+  for (uint32_t q = blockIdx.y; q < total; q += gridDim.y) {
+    const uint32_t e = bucket_of_tile(s.tile, a.num_experts, q);
+    const uint32_t row = (uint32_t)s.off[e] + (q - s.tile[e]) * kRows;
+    const uint32_t rows = min(kRows, (uint32_t)s.off[e + 1] - row);
+    float sum[8] = {};
+    if (n > 0) {
+#pragma unroll 4
+      for (uint32_t r = warp; r < rows; r += 8) {
+        float g[8], z[8];
+        load8(a.dy, (uint64_t)(row + r) * a.ld_dy + col, n, a.vec_dy, a.bf16, g);
+        if (a.activation != NTC_ACT_NONE) {
+          load8(a.z, (uint64_t)(row + r) * a.ld_z + col, n, a.vec_z, a.bf16, z);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) g[i] *= act_slope(a.activation, a.slope, z[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += g[i];
+        if (a.dz) store8(a.dz, (uint64_t)(row + r) * a.pitch + col, 8, true, a.bf16, g);  // pads: 0
+      }
+    }
+    if (a.part) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sums[warp][lane * 8 + i] = sum[i];
+      __syncthreads();
+      const uint32_t c = blockIdx.x * kDzCols + threadIdx.x;
+      if (c < a.width) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) v += sums[w][threadIdx.x];
+        a.part[(uint64_t)q * a.pitch + c] = v;
+      }
+    }
+  }
+}
+
+// db_e = the sums of e's row tiles, in a fixed order: eight slices of the tiles,
+// then the slices.
+__global__ void __launch_bounds__(kDzThreads)
+    k_db(const float *part, const int32_t *offsets, uint32_t E, uint32_t num_rows, uint32_t width, uint32_t pitch, float *db) {
+  extern __shared__ uint8_t raw[];
+  TableShared &s = *reinterpret_cast<TableShared *>(raw);
+  __shared__ float sums[8][32];
+  pdl_wait();
+  pdl_trigger();
+  make_table(s.off, s.tile, offsets, E, num_rows);
+  const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
+  const uint32_t c = blockIdx.x * 32 + lane;
+  for (uint32_t e = blockIdx.y; e < E; e += gridDim.y) {
+    const uint32_t a = s.tile[e], z = s.tile[e + 1], slice = (z - a + 7) / 8;
+    const uint32_t from = min(a + warp * slice, z), to = min(from + slice, z);
+    float v = 0.0f;
+    if (c < width) {
+#pragma unroll 8
+      for (uint32_t q = from; q < to; ++q) v += part[(uint64_t)q * pitch + c];
+    }
+    __syncthreads();
+    sums[warp][lane] = v;
+    __syncthreads();
+    if (warp == 0 && c < width) {
+      float t = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) t += sums[w][lane];
+      db[(uint64_t)e * width + c] = t;
+    }
+  }
+}
+
+// A matrix TMA cannot read, copied to rows of `pitch` elements (the pads hold 0).
+__global__ void __launch_bounds__(256)
+    k_pack(const uint16_t *src, uint64_t ld, uint64_t stride, uint32_t cols, uint32_t rows, uint64_t total, uint16_t *dst,
+           uint32_t pitch) {
+  pdl_wait();
+  pdl_trigger();
+  const uint32_t pieces = pitch / 8;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (uint64_t)gridDim.x * 256) {
+    const uint64_t row = i / pieces;  // of all matrices
+    const uint32_t c = (uint32_t)(i - row * pieces) * 8;
+    const uint64_t m = row / rows;
+    const uint16_t *p = src + m * stride + (row - m * rows) * ld + c;
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t lo = c + 2 * j < cols ? p[2 * j] : 0u, hi = c + 2 * j + 1 < cols ? p[2 * j + 1] : 0u;
+      w[j] = lo | (hi << 16);
+    }
+    *reinterpret_cast<uint4 *>(dst + row * pitch + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// ------------------------------------------------------------ host
+
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static const EncodeTiled fn = [] {
+    void *p = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return (EncodeTiled)p;
+  }();
+  return fn;
+}
+
+// A matrix operand as TMA reads it.
+struct Operand {
+  const void *p;
+  uint64_t cols, rows, ld;       // elements
+  uint64_t many = 1, stride = 0;  // matrices and the elements between them
+};
+
+// dims 2 or 3; box of box_cols x box_rows (x 1)
+bool make_map(CUtensorMap *m, const Operand &o, int dims, uint32_t box_cols, uint32_t box_rows) {
+  const EncodeTiled fn = encode_tiled();
+  if (!fn) return false;
+  const cuuint64_t size[3] = {o.cols, o.rows, o.many};
+  const cuuint64_t step[2] = {o.ld * 2, o.many > 1 ? o.stride * 2 : o.ld * o.rows * 2};
+  const cuuint32_t box[3] = {box_cols, box_rows, 1}, ones[3] = {1, 1, 1};
+  return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, (cuuint32_t)dims, const_cast<void *>(o.p), size, step, box, ones,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+unsigned int *status_word() {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<unsigned int *> known[kMaxDevices];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;
+  unsigned int *p = known[dev].load(std::memory_order_acquire);
+  if (!p) {
+    void *q = nullptr;
+    if (cudaGetSymbolAddress(&q, g_linear_status) != cudaSuccess) return nullptr;
+    p = (unsigned int *)q;
+    known[dev].store(p, std::memory_order_release);
+  }
+  return p;
+}
+
+template <int MODE, int BN>
+cudaError_t launch_tile(const Operand &A, const Operand &B, Args a, uint64_t tiles_bound, int sms, cudaStream_t st) {
+  CUtensorMap ma, mag, mb, mbg;
+  bool ok = make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 32) && make_map(&mag, A, 2, 64, 1);
+  if (MODE == kDw) ok = ok && make_map(&mb, B, 2, 64, 64) && make_map(&mbg, B, 2, 64, 1);
+  else ok = ok && make_map(&mb, B, 3, 64, MODE == kForward ? BN : 64);
+  if (!ok) return cudaErrorInvalidValue;
+  if (MODE != kDw) mbg = mb;
+  static std::atomic<uint64_t> allowed{0};  // devices that know of the kernel's shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !((allowed.load() >> dev) & 1)) {
+    e = cudaFuncSetAttribute(k_linear<MODE, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes);
+    if (e != cudaSuccess) return e;
+    if (dev < 64) allowed.fetch_or(1ull << dev);
+  }
+  const unsigned grid = (unsigned)std::min<uint64_t>(tiles_bound, (uint64_t)sms);
+  return launch_pdl(k_linear<MODE, BN>, grid, kThreads, kSharedBytes, st, ma, mag, mb, mbg, a);
+}
+
+// Row tiles of num_rows rows in num_experts segments (and those of no expert), at most.
+uint64_t row_tiles_bound(uint64_t num_rows, uint64_t num_experts) {
+  return std::min<uint64_t>(num_rows, (num_rows + kRows - 1) / kRows + num_experts);
+}
+
+// The width of a tile: the widest whose tiles still fill the SMs.
+template <int MODE>
+cudaError_t launch_product(const Operand &A, const Operand &B, const Args &a, cudaStream_t st) {
+  const int sms = sm_count();
+  const uint64_t high = MODE == kDw ? (uint64_t)a.num_experts * ((a.height + kRows - 1) / kRows)
+                                    : row_tiles_bound(a.num_rows, a.num_experts);
+  if (high == 0) return cudaSuccess;
+  const auto tiles = [&](uint32_t bn) { return high * ((a.width + bn - 1) / bn); };
+  if (tiles(256) >= (uint64_t)sms) return launch_tile<MODE, 256>(A, B, a, tiles(256), sms, st);
+  if (tiles(128) >= (uint64_t)sms) return launch_tile<MODE, 128>(A, B, a, tiles(128), sms, st);
+  return launch_tile<MODE, 64>(A, B, a, tiles(64), sms, st);
+}
+
+// ------------------------------------------------------------ workspaces
+
+uint64_t round8(uint64_t x) { return (x + 7) / 8 * 8; }
+uint64_t round256(uint64_t x) { return (x + 255) / 256 * 256; }
+
+bool tma_reads(const void *p, uint64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+bool x_packs(const ntc_linear_desc &d, const void *x) { return !tma_reads(x, d.ld_x); }
+bool w_packs(const ntc_linear_desc &d, const void *w) {
+  return !tma_reads(w, d.ld_w) || (d.num_experts > 1 && d.stride_w % 8);
+}
+bool dz_writes(const ntc_linear_desc &d, const void *dy) { return d.activation != NTC_ACT_NONE || !tma_reads(dy, d.ld_y); }
+uint64_t x_bytes(const ntc_linear_desc &d) { return round256(d.num_x_rows * round8(d.in_dim) * 2); }
+uint64_t w_bytes(const ntc_linear_desc &d) { return round256((uint64_t)d.num_experts * d.out_dim * round8(d.in_dim) * 2); }
+uint64_t dz_bytes(const ntc_linear_desc &d) { return round256(d.num_rows * round8(d.out_dim) * 2); }
+uint64_t part_bytes(const ntc_linear_desc &d) {
+  return round256(row_tiles_bound(d.num_rows, d.num_experts) * round8(d.out_dim) * 4);
+}
+
+ntc_status check(const ntc_linear_desc *d) {
+  if (!d) return op_fail(NTC_ERR_INVALID_ARG, "null descriptor");
+  if (d->type != NTC_TYPE_FP16 && d->type != NTC_TYPE_BF16) {
+    if (d->type == NTC_TYPE_FP32) return op_fail(NTC_ERR_UNSUPPORTED, "linear layers take fp16 or bf16 operands");
+    return op_fail(NTC_ERR_INVALID_ARG, "unknown type");
+  }
+  if (d->in_dim < 1 || d->in_dim > (1u << 20)) return op_fail(NTC_ERR_INVALID_ARG, "in_dim must be in 1..2^20");
+  if (d->out_dim < 1 || d->out_dim > (1u << 20)) return op_fail(NTC_ERR_INVALID_ARG, "out_dim must be in 1..2^20");
+  if (d->num_experts < 1 || d->num_experts > NTC_MAX_EXPERTS)
+    return op_fail(NTC_ERR_INVALID_ARG, "num_experts must be in 1..1024");
+  if (d->activation > NTC_ACT_SILU) return op_fail(NTC_ERR_INVALID_ARG, "unknown activation");
+  if (!(d->leaky_slope - d->leaky_slope == 0.0f)) return op_fail(NTC_ERR_INVALID_ARG, "leaky_slope must be finite");
+  if (d->num_rows > INT_MAX - 256 || d->num_x_rows > INT_MAX - 256)
+    return op_fail(NTC_ERR_INVALID_ARG, "rows must be below 2^31 - 256");
+  if (d->ld_x < d->in_dim || d->ld_w < d->in_dim) return op_fail(NTC_ERR_INVALID_ARG, "ld_x or ld_w is below in_dim");
+  if (d->ld_y < d->out_dim || d->ld_z < d->out_dim || d->ld_residual < d->out_dim)
+    return op_fail(NTC_ERR_INVALID_ARG, "ld_y, ld_z or ld_residual is below out_dim");
+  constexpr uint64_t kMost = 1ull << 38;  // TMA's strides: below 2^40 bytes
+  if (d->ld_x > kMost || d->ld_w > kMost || d->ld_y > kMost || d->ld_z > kMost || d->ld_residual > kMost ||
+      d->stride_w > kMost)
+    return op_fail(NTC_ERR_UNSUPPORTED, "a leading dimension or stride exceeds 2^38 elements");
+  if (d->num_experts > 1 && d->stride_w < (uint64_t)(d->out_dim - 1) * d->ld_w + d->in_dim)
+    return op_fail(NTC_ERR_INVALID_ARG, "stride_w is below one expert's weights");
+  return NTC_OK;
+}
+
+ntc_status check_rows(const ntc_linear_desc &d, const int32_t *rows, const int32_t *offsets) {
+  if (!offsets && d.num_experts != 1) return op_fail(NTC_ERR_INVALID_ARG, "several experts need offsets");
+  if (!rows && d.num_x_rows != d.num_rows) return op_fail(NTC_ERR_INVALID_ARG, "without rows, num_x_rows is num_rows");
+  if (d.num_rows && !d.num_x_rows) return op_fail(NTC_ERR_INVALID_ARG, "x has no rows");
+  if (((uintptr_t)rows | (uintptr_t)offsets) & 3)
+    return op_fail(NTC_ERR_INVALID_ARG, "rows or offsets is not aligned to 4 bytes");
+  return NTC_OK;
+}
+
+ntc_status check_workspace(const void *p, size_t have, size_t need) {
+  if (have < need || (need && !p))
+    return op_fail(NTC_ERR_INVALID_ARG, "the workspace has %zu bytes, %zu are needed", have, need);
+  if (need && ((uintptr_t)p & 15)) return op_fail(NTC_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+  return NTC_OK;
+}
+
+cudaError_t pack(const void *src, uint64_t ld, uint64_t stride, uint32_t cols, uint64_t rows, uint64_t many, void *dst,
+                 cudaStream_t st) {
+  const uint32_t pitch = (uint32_t)round8(cols);
+  const uint64_t total = rows * many * (pitch / 8);
+  const unsigned grid = (unsigned)std::min<uint64_t>((total + 255) / 256, (uint64_t)sm_count() * 32);
+  return launch_pdl(k_pack, grid, 256, 0, st, (const uint16_t *)src, ld, stride, cols, (uint32_t)rows, total,
+                    (uint16_t *)dst, pitch);
+}
+
+// The operands x and w, through the workspace where TMA cannot read them.
+cudaError_t operand_x(const ntc_linear_desc &d, const void *x, uint8_t *&ws, Operand *o, cudaStream_t st) {
+  *o = Operand{x, d.in_dim, d.num_x_rows, d.ld_x};
+  if (!x_packs(d, x)) return cudaSuccess;
+  const cudaError_t e = pack(x, d.ld_x, 0, d.in_dim, d.num_x_rows, 1, ws, st);
+  *o = Operand{ws, d.in_dim, d.num_x_rows, round8(d.in_dim)};
+  ws += x_bytes(d);
+  return e;
+}
+cudaError_t operand_w(const ntc_linear_desc &d, const void *w, uint8_t *&ws, Operand *o, cudaStream_t st) {
+  *o = Operand{w, d.in_dim, d.out_dim, d.ld_w, d.num_experts, d.stride_w};
+  if (!w_packs(d, w)) return cudaSuccess;
+  const cudaError_t e = pack(w, d.ld_w, d.stride_w, d.in_dim, d.out_dim, d.num_experts, ws, st);
+  const uint64_t p = round8(d.in_dim);
+  *o = Operand{ws, d.in_dim, d.out_dim, p, d.num_experts, p * d.out_dim};
+  ws += w_bytes(d);
+  return e;
+}
+
+}  // namespace
+
+extern "C" NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, const void *w) {
+  if (check(desc)) return 0;
+  return (x_packs(*desc, x) ? x_bytes(*desc) : 0) + (w_packs(*desc, w) ? w_bytes(*desc) : 0);
+}
+
+extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void *x, const int32_t *rows,
+                                         const int32_t *offsets, const void *w, const float *bias, const void *residual,
+                                         void *y, void *z, void *workspace, size_t workspace_bytes, void *cuda_stream) {
+  if (ntc_status s = check(desc)) return s;
+  const ntc_linear_desc &d = *desc;
+  if (ntc_status s = check_rows(d, rows, offsets)) return s;
+  if (d.num_rows == 0) return NTC_OK;
+  if (!x || !w || !y) return op_fail(NTC_ERR_INVALID_ARG, "null device pointer");
+  if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)y | (uintptr_t)z | (uintptr_t)residual) & 1)
+    return op_fail(NTC_ERR_INVALID_ARG, "a buffer is not aligned to its element (2 bytes)");
+  if ((uintptr_t)bias & 3) return op_fail(NTC_ERR_INVALID_ARG, "bias is not aligned to 4 bytes");
+  if (ntc_status s = check_workspace(workspace, workspace_bytes, ntc_linear_workspace(desc, x, w))) return s;
+  unsigned int *status = status_word();
+  if (!status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  uint8_t *ws = (uint8_t *)workspace;
+  Operand X, W;
+  cudaError_t e = operand_x(d, x, ws, &X, st);
+  if (e == cudaSuccess) e = operand_w(d, w, ws, &W, st);
+  if (e != cudaSuccess) return op_cuda(e, "ntc_linear");
+  Args a{};
+  a.rows = rows;
+  a.offsets = offsets;
+  a.bias = bias;
+  a.residual = residual;
+  a.out = y;
+  a.z = z;
+  a.ld_out = d.ld_y;
+  a.ld_z = d.ld_z;
+  a.ld_residual = d.ld_residual;
+  a.num_experts = d.num_experts;
+  a.num_rows = (uint32_t)d.num_rows;
+  a.x_rows = (uint32_t)d.num_x_rows;
+  a.width = d.out_dim;
+  a.depth = d.in_dim;
+  a.activation = d.activation;
+  a.slope = d.leaky_slope;
+  a.bf16 = d.type == NTC_TYPE_BF16;
+  a.vec_out = rows_are_vec(y, d.ld_y, 2);
+  a.vec_z = z && rows_are_vec(z, d.ld_z, 2);
+  a.vec_residual = residual && rows_are_vec(residual, d.ld_residual, 2);
+  a.status = status;
+  return op_cuda(launch_product<kForward>(X, W, a, st), "ntc_linear");
+}
+
+extern "C" NTC_API size_t ntc_linear_backward_workspace(const ntc_linear_desc *desc, const void *dy, const void *x,
+                                                        const void *w) {
+  if (check(desc)) return 0;
+  return (dz_writes(*desc, dy) ? dz_bytes(*desc) : 0) + (x_packs(*desc, x) ? x_bytes(*desc) : 0) +
+         (w_packs(*desc, w) ? w_bytes(*desc) : 0) + part_bytes(*desc);
+}
+
+extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, const void *dy, const void *z,
+                                                  const void *x, const int32_t *rows, const int32_t *offsets,
+                                                  const void *w, void *dx, void *dw, float *db, void *workspace,
+                                                  size_t workspace_bytes, void *cuda_stream) {
+  if (ntc_status s = check(desc)) return s;
+  const ntc_linear_desc &d = *desc;
+  if (ntc_status s = check_rows(d, rows, offsets)) return s;
+  if (!dx && !dw && !db) return NTC_OK;
+  if (d.num_rows && (!dy || (!z && d.activation != NTC_ACT_NONE) || (dx && !w) || (dw && !x)))
+    return op_fail(NTC_ERR_INVALID_ARG, "null device pointer");
+  if (((uintptr_t)dy | (uintptr_t)z | (uintptr_t)x | (uintptr_t)w | (uintptr_t)dx | (uintptr_t)dw) & 1)
+    return op_fail(NTC_ERR_INVALID_ARG, "a buffer is not aligned to its element (2 bytes)");
+  if ((uintptr_t)db & 3) return op_fail(NTC_ERR_INVALID_ARG, "db is not aligned to 4 bytes");
+  if (ntc_status s = check_workspace(workspace, workspace_bytes, ntc_linear_backward_workspace(desc, dy, x, w))) return s;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  const char *what = "ntc_linear_backward";
+  cudaError_t e = cudaSuccess;
+  if (d.num_rows == 0) {  // sums of nothing
+    if (dw) e = cudaMemsetAsync(dw, 0, (size_t)d.num_experts * d.out_dim * d.in_dim * 2, st);
+    if (e == cudaSuccess && db) e = cudaMemsetAsync(db, 0, (size_t)d.num_experts * d.out_dim * 4, st);
+    return op_cuda(e, what);
+  }
+  unsigned int *status = status_word();
+  if (!status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
+  uint8_t *ws = (uint8_t *)workspace;
+  float *part = (float *)ws;
+  ws += part_bytes(d);
+  const bool writes = dz_writes(d, dy);
+  void *dz = nullptr;
+  Operand Z{dy, d.out_dim, d.num_rows, d.ld_y};
+  if (writes) {
+    dz = ws;
+    Z = Operand{dz, d.out_dim, d.num_rows, round8(d.out_dim)};
+    ws += dz_bytes(d);
+  }
+  if ((writes && (dx || dw)) || db) {
+    DzArgs k{};
+    k.dy = dy;
+    k.z = z;
+    k.offsets = offsets;
+    k.dz = dx || dw ? dz : nullptr;
+    k.part = db ? part : nullptr;
+    k.ld_dy = d.ld_y;
+    k.ld_z = d.ld_z;
+    k.num_experts = d.num_experts;
+    k.num_rows = (uint32_t)d.num_rows;
+    k.width = d.out_dim;
+    k.pitch = (uint32_t)round8(d.out_dim);
+    k.activation = d.activation;
+    k.slope = d.leaky_slope;
+    k.bf16 = d.type == NTC_TYPE_BF16;
+    k.vec_dy = rows_are_vec(dy, d.ld_y, 2);
+    k.vec_z = z && rows_are_vec(z, d.ld_z, 2);
+    const unsigned cols = (d.out_dim + kDzCols - 1) / kDzCols;
+    const unsigned high = (unsigned)std::min<uint64_t>(row_tiles_bound(d.num_rows, d.num_experts),
+                                                       std::max(1u, (unsigned)sm_count() * 8 / cols));
+    e = launch_pdl(k_dz, dim3(cols, high), kDzThreads, sizeof(TableShared), st, k);
+    if (e == cudaSuccess && db)
+      e = launch_pdl(k_db, dim3((d.out_dim + 31) / 32, std::min(d.num_experts, 1024u)), kDzThreads, sizeof(TableShared), st,
+                     (const float *)part, offsets, d.num_experts, (uint32_t)d.num_rows, d.out_dim, k.pitch, db);
+  }
+  Args a{};
+  a.offsets = offsets;
+  a.num_experts = d.num_experts;
+  a.num_rows = (uint32_t)d.num_rows;
+  a.width = d.in_dim;
+  a.bf16 = d.type == NTC_TYPE_BF16;
+  a.ld_out = d.in_dim;
+  a.status = status;
+  if (e == cudaSuccess && dx) {
+    Operand W;
+    e = operand_w(d, w, ws, &W, st);
+    a.out = dx;
+    a.depth = d.out_dim;
+    a.vec_out = rows_are_vec(dx, d.in_dim, 2);
+    if (e == cudaSuccess) e = launch_product<kDx>(Z, W, a, st);
+  }
+  if (e == cudaSuccess && dw) {
+    Operand X;
+    e = operand_x(d, x, ws, &X, st);
+    a.out = dw;
+    a.rows = rows;
+    a.x_rows = (uint32_t)d.num_x_rows;
+    a.height = d.out_dim;
+    a.vec_out = rows_are_vec(dw, d.in_dim, 2);
+    if (e == cudaSuccess) e = launch_product<kDw>(Z, X, a, st);
+  }
+  return op_cuda(e, what);
+}
+
+extern "C" NTC_API ntc_status ntc_linear_status(void *cuda_stream) {
+  unsigned int *p = status_word();
+  if (!p) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  unsigned int v = 0;
+  cudaError_t e = cudaMemcpyAsync(&v, p, 4, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e == cudaSuccess && v) e = cudaMemsetAsync(p, 0, 4, st);
+  if (e == cudaSuccess && v) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return op_cuda(e, "ntc_linear_status");
+  return v ? op_fail(NTC_ERR_CUDA, "a kernel gave up a bounded wait: results since the last check are invalid") : NTC_OK;
+}
