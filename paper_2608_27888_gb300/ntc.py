@@ -454,267 +454,15 @@ class Decoder:
         return ntc_stage_times(self.ctx)
 
 
-# ------------------------------------------------- routed experts, on torch tensors
-#
-# Each function allocates its outputs and workspace with torch and makes the one
-# library call of its name.  `stream` (default: the current stream) is where the
-# call is queued and where those allocations live; tensors of another stream are the
-# caller's to order, as for any torch call.  Matrices may have any row stride; their
-# last dimension is contiguous.
-
-def _on(stream):
-    """A context that makes `stream` current (nothing to do for None)."""
-    import contextlib
-    import torch
-    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+# The routed-expert calls on torch tensors live in experts.py, which imports torch;
+# they are names of this module that are looked up when first used.
+_EXPERTS = ("route", "route_backward", "expert_order", "linear", "linear_backward", "combine", "combine_backward")
 
 
-def _types():
-    import torch
-    return {torch.float32: NTC_TYPE_FP32, torch.float16: NTC_TYPE_FP16, torch.bfloat16: NTC_TYPE_BF16}
-
-
-_TYPE_OF = None
-
-
-def _type_of(t, name):
-    global _TYPE_OF
-    if _TYPE_OF is None:
-        _TYPE_OF = _types()
-    try:
-        return _TYPE_OF[t.dtype]
-    except KeyError:
-        raise ValueError(f"{name} must be float32, float16 or bfloat16, not {t.dtype}") from None
-
-
-def _matrix(t, name, rows, cols, dtype, device):
-    """The row stride of a [rows, cols] matrix argument, after its checks."""
-    if t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be {dtype} on {device}, not {t.dtype} on {t.device}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name} must have shape [{rows}, {cols}], not {list(t.shape)}")
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name} must be contiguous along its last dimension")
-    ld = t.stride(0) if rows > 1 else cols
-    if ld < cols:
-        raise ValueError(f"{name} has overlapping rows")
-    return ld
-
-
-def _array(t, name, shape, dtype, device):
-    """The address of a contiguous array argument of this shape (None stays None), after its checks."""
-    if t is None:
-        return None
-    if t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be {dtype} on {device}, not {t.dtype} on {t.device}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} must have shape {list(shape)}, not {list(t.shape)}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
-
-
-def _cuda(t, name):
-    import torch
-    if t.device.type != "cuda":
-        raise ValueError(f"{name} must be a CUDA tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, which is not the current device")
-    return t.device
-
-
-def _choice(table, key, name):
-    try:
-        return table[key]
-    except (KeyError, TypeError):
-        raise ValueError(f"{name} must be one of {', '.join(table)}, not {key!r}") from None
-
-
-def _workspace(bytes_, device):
-    import torch
-    return torch.empty(bytes_, dtype=torch.uint8, device=device) if bytes_ else None
-
-
-def route(logits, top_k: int, *, bias=None, score: str = "softmax", groups: int = 1, top_groups: int = 1,
-          renormalize: bool = True, scale: float = 1.0, stream=None):
-    """ids [n, top_k] int32 and weights [n, top_k] fp32 of each row of logits [n, experts]: see ntc_route."""
-    import torch
-    dev = _cuda(logits, "logits")
-    if logits.dim() != 2:
-        raise ValueError(f"logits must have two dimensions, not {logits.dim()}")
-    n, E = logits.shape
-    d = ntc_route_desc(E, top_k, groups, top_groups, _choice(SCORES, score, "score"), bool(renormalize), scale,
-                       _type_of(logits, "logits"))
-    ld = _matrix(logits, "logits", n, E, logits.dtype, dev)
-    b = _array(bias, "bias", (E,), torch.float32, dev)
-    with _on(stream):
-        ids = torch.empty((n, max(0, top_k)), dtype=torch.int32, device=dev)
-        weights = torch.empty((n, max(0, top_k)), dtype=torch.float32, device=dev)
-        ntc_route(d, n, logits.data_ptr(), ld, b, ids.data_ptr(), weights.data_ptr(), _stream(stream))
-    return ids, weights
-
-
-def route_backward(logits, ids, dweights, *, score: str = "softmax", renormalize: bool = True, scale: float = 1.0,
-                   stream=None):
-    """The gradient of route's logits for the gradient of its weights: see ntc_route_backward."""
-    import torch
-    dev = _cuda(logits, "logits")
-    if logits.dim() != 2 or ids.dim() != 2:
-        raise ValueError("logits and ids must have two dimensions")
-    (n, E), k = logits.shape, ids.shape[1]
-    d = ntc_route_desc(E, k, 1, 1, _choice(SCORES, score, "score"), bool(renormalize), scale,
-                       _type_of(logits, "logits"))
-    ld = _matrix(logits, "logits", n, E, logits.dtype, dev)
-    i = _array(ids, "ids", (n, k), torch.int32, dev)
-    g = _array(dweights, "dweights", (n, k), torch.float32, dev)
-    with _on(stream):
-        out = torch.empty((n, E), dtype=logits.dtype, device=dev)
-        ntc_route_backward(d, n, logits.data_ptr(), ld, i, g, out.data_ptr(), _stream(stream))
-    return out
-
-
-def expert_order(ids, num_experts: int, *, stream=None):
-    """rows [n * k], place [n, k] and offsets [num_experts + 1] (int32) of ids [n, k]: see ntc_expert_order."""
-    import torch
-    dev = _cuda(ids, "ids")
-    if ids.dim() != 2:
-        raise ValueError(f"ids must have two dimensions, not {ids.dim()}")
-    n, k = ids.shape
-    i = _array(ids, "ids", (n, k), torch.int32, dev)
-    with _on(stream):
-        rows = torch.empty(n * k, dtype=torch.int32, device=dev)
-        place = torch.empty((n, k), dtype=torch.int32, device=dev)
-        offsets = torch.empty(max(0, num_experts) + 1, dtype=torch.int32, device=dev)
-        size = ntc_expert_order_workspace(n * k, num_experts)
-        ws = _workspace(size, dev)
-        ntc_expert_order(i, n * k, k, num_experts, rows.data_ptr(), place.data_ptr(), offsets.data_ptr(), _ptr(ws), size,
-                         _stream(stream))
-    return rows, place, offsets
-
-
-def _linear_operands(x, w, rows, offsets, activation, leaky_slope, num_rows):
-    """The descriptor of a linear call, and the addresses of rows and offsets."""
-    import torch
-    dev = _cuda(x, "x")
-    if w.dim() == 2:
-        w = w[None]
-    if x.dim() != 2 or w.dim() != 3:
-        raise ValueError("x must have two dimensions, w two or three")
-    E, N, K = w.shape
-    if w.dtype != x.dtype or w.device != dev:
-        raise ValueError(f"w must be {x.dtype} on {dev}, not {w.dtype} on {w.device}")
-    if K > 1 and w.stride(2) != 1:
-        raise ValueError("w must be contiguous along its last dimension")
-    ldw = w.stride(1) if N > 1 else K
-    step = w.stride(0) if E > 1 else N * ldw
-    ldx = _matrix(x, "x", x.shape[0], K, x.dtype, dev)
-    r = _array(rows, "rows", (num_rows,), torch.int32, dev)
-    o = _array(offsets, "offsets", (E + 1,), torch.int32, dev)
-    d = ntc_linear_desc(_type_of(x, "x"), K, N, E, _choice(ACTIVATIONS, activation, "activation"), leaky_slope, num_rows,
-                        x.shape[0], ldx, ldw, step, N, N, N)
-    return d, w, r, o, dev
-
-
-def linear(x, w, bias=None, *, rows=None, offsets=None, activation: str = "none", leaky_slope: float = 0.01,
-           residual=None, save: bool = False, stream=None):
-    """act(x[rows] w^T + bias) + residual, with each expert's weights for its rows: see ntc_linear.
-
-    x [n, K]; w [E, N, K] (or [N, K]); bias fp32 [E, N] (or [N]); rows int32: the row of x of each row of the
-    result (default: the same); offsets int32 [E + 1]: where each expert's rows begin; residual [rows, N].
-    save=True also returns the input of the activation, which linear_backward takes as z."""
-    import torch
-    m = x.shape[0] if rows is None else rows.shape[0]
-    d, w, r, o, dev = _linear_operands(x, w, rows, offsets, activation, leaky_slope, m)
-    E, N = d.num_experts, d.out_dim
-    if bias is not None and bias.dim() == 1 and E == 1:
-        bias = bias[None]
-    b = _array(bias, "bias", (E, N), torch.float32, dev)
-    if residual is not None:
-        d.ld_residual = _matrix(residual, "residual", m, N, x.dtype, dev)
-    with _on(stream):
-        y = torch.empty((m, N), dtype=x.dtype, device=dev)
-        z = torch.empty((m, N), dtype=x.dtype, device=dev) if save else None
-        size = ntc_linear_workspace(d, x.data_ptr(), w.data_ptr())
-        ws = _workspace(size, dev)
-        ntc_linear(d, x.data_ptr(), r, o, w.data_ptr(), b, _ptr(residual), y.data_ptr(), _ptr(z), _ptr(ws), size,
-                   _stream(stream))
-    return (y, z) if save else y
-
-
-def linear_backward(dy, x, w, *, z=None, rows=None, offsets=None, activation: str = "none", leaky_slope: float = 0.01,
-                    need=("dx", "dw", "db"), stream=None):
-    """(dx, dw, db) of linear for the gradient dy of its result: see ntc_linear_backward.
-
-    z is what linear(save=True) returned beside the result (not needed without an activation).  dx has a row per
-    row of dy; where rows gathered x, combine(dx, place, None, offsets) sums a token's.  Gradients that `need`
-    does not name are None."""
-    import torch
-    m = dy.shape[0]
-    d, w, r, o, dev = _linear_operands(x, w, rows, offsets, activation, leaky_slope, m)
-    E, N, K = d.num_experts, d.out_dim, d.in_dim
-    d.ld_y = _matrix(dy, "dy", m, N, x.dtype, dev)
-    if activation == "none":
-        z = None
-    elif z is None:
-        raise ValueError(f"activation {activation!r} needs z")
-    else:
-        d.ld_z = _matrix(z, "z", m, N, x.dtype, dev)
-    for name in need:
-        _choice({"dx": 0, "dw": 0, "db": 0}, name, "need")
-    with _on(stream):
-        dx = torch.empty((m, K), dtype=x.dtype, device=dev) if "dx" in need else None
-        dw = torch.empty((E, N, K), dtype=x.dtype, device=dev) if "dw" in need else None
-        db = torch.empty((E, N), dtype=torch.float32, device=dev) if "db" in need else None
-        size = ntc_linear_backward_workspace(d, dy.data_ptr(), x.data_ptr(), w.data_ptr())
-        ws = _workspace(size, dev)
-        ntc_linear_backward(d, dy.data_ptr(), _ptr(z), x.data_ptr(), r, o, w.data_ptr(), _ptr(dx), _ptr(dw), _ptr(db),
-                            _ptr(ws), size, _stream(stream))
-    return dx, dw, db
-
-
-def _combine_desc(y, place, offsets, dim):
-    dev = _cuda(y, "y")
-    if y.dim() != 2 or place.dim() != 2:
-        raise ValueError("y and place must have two dimensions")
-    T, k = place.shape
-    E = offsets.shape[0] - 1 if offsets is not None and offsets.dim() == 1 else 1
-    ld = _matrix(y, "y", y.shape[0], dim, y.dtype, dev)
-    return ntc_combine_desc(_type_of(y, "y"), dim, k, E, T, y.shape[0], ld, dim, dim), dev
-
-
-def combine(y, place, weights=None, offsets=None, *, residual=None, stream=None):
-    """residual + the sum of y[place[t, j]] times weights[t, j] (1 without weights): see ntc_combine.
-
-    Places from offsets[-1] on (rows of no expert) are left out."""
-    import torch
-    D = y.shape[1]
-    d, dev = _combine_desc(y, place, offsets, D)
-    T, k = place.shape
-    p = _array(place, "place", (T, k), torch.int32, dev)
-    g = _array(weights, "weights", (T, k), torch.float32, dev)
-    o = _array(offsets, "offsets", (d.num_experts + 1,), torch.int32, dev)
-    if residual is not None:
-        d.ld_residual = _matrix(residual, "residual", T, D, y.dtype, dev)
-    with _on(stream):
-        out = torch.empty((T, D), dtype=y.dtype, device=dev)
-        ntc_combine(d, y.data_ptr(), p, g, o, _ptr(residual), out.data_ptr(), _stream(stream))
-    return out
-
-
-def combine_backward(dout, y, place, weights=None, offsets=None, *, need=("dy", "dweights"), stream=None):
-    """(dy, dweights) of combine for the gradient dout of its result: see ntc_combine_backward."""
-    import torch
-    D = y.shape[1]
-    d, dev = _combine_desc(y, place, offsets, D)
-    T, k = place.shape
-    p = _array(place, "place", (T, k), torch.int32, dev)
-    g = _array(weights, "weights", (T, k), torch.float32, dev)
-    o = _array(offsets, "offsets", (d.num_experts + 1,), torch.int32, dev)
-    d.ld_out = _matrix(dout, "dout", T, D, y.dtype, dev)
-    for name in need:
-        _choice({"dy": 0, "dweights": 0}, name, "need")
-    with _on(stream):
-        dy = torch.empty((y.shape[0], D), dtype=y.dtype, device=dev) if "dy" in need else None
-        dw = torch.empty((T, k), dtype=torch.float32, device=dev) if "dweights" in need else None
-        ntc_combine_backward(d, dout.data_ptr(), y.data_ptr(), p, g, o, _ptr(dy), _ptr(dw), _stream(stream))
-    return dy, dw
+def __getattr__(name):
+    if name in _EXPERTS:
+        from . import experts
+        for n in _EXPERTS:
+            globals()[n] = getattr(experts, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -167,24 +167,37 @@ def test_combine_pointer_refusals():
 
 def test_the_python_functions_check_their_tensors():
     import torch
-    with pytest.raises(ValueError, match="CUDA tensor"):
-        ntc.route(torch.zeros(2, 8), 2)
-    with pytest.raises(ValueError, match="CUDA tensor"):
-        ntc.linear(torch.zeros(2, 8), torch.zeros(4, 8))
-    with pytest.raises(ValueError, match="CUDA tensor"):
-        ntc.combine(torch.zeros(2, 8), torch.zeros(2, 1, dtype=torch.int32))
-    with pytest.raises(ValueError, match="CUDA tensor"):
-        ntc.expert_order(torch.zeros(2, 1, dtype=torch.int32), 2)
+    from paper_2608_27888_gb300 import experts
+    for call in (lambda: ntc.route(torch.zeros(2, 8), 2), lambda: ntc.linear(torch.zeros(2, 8), torch.zeros(4, 8)),
+                 lambda: ntc.combine(torch.zeros(2, 8), torch.zeros(2, 1, dtype=torch.int32)),
+                 lambda: ntc.expert_order(torch.zeros(2, 1, dtype=torch.int32), 2)):
+        with pytest.raises(ValueError, match="CUDA tensor"):
+            call()
     cpu = torch.device("cpu")
     with pytest.raises(ValueError, match="shape"):
-        ntc._array(torch.zeros(3), "bias", (4,), torch.float32, cpu)
+        experts._array(torch.zeros(3), "bias", (4,), torch.float32, cpu)
     with pytest.raises(ValueError, match="float32"):
-        ntc._array(torch.zeros(4).half(), "bias", (4,), torch.float32, cpu)
+        experts._array(torch.zeros(4).half(), "bias", (4,), torch.float32, cpu)
     with pytest.raises(ValueError, match="contiguous"):
-        ntc._array(torch.zeros(8)[::2], "bias", (4,), torch.float32, cpu)
+        experts._array(torch.zeros(8)[::2], "bias", (4,), torch.float32, cpu)
     with pytest.raises(ValueError, match="last dimension"):
-        ntc._matrix(torch.zeros(4, 3).t(), "x", 3, 4, torch.float32, cpu)
+        experts._matrix(torch.zeros(4, 3).t(), "x", 3, 4, torch.float32, cpu)
     with pytest.raises(ValueError, match="overlapping"):
-        ntc._matrix(torch.zeros(1, 4).expand(3, 4), "x", 3, 4, torch.float32, cpu)
+        experts._matrix(torch.zeros(1, 4).expand(3, 4), "x", 3, 4, torch.float32, cpu)
     with pytest.raises(ValueError, match="must be one of"):
-        ntc._choice(ntc.ACTIVATIONS, "tanh", "activation")
+        experts._choice(ntc.ACTIVATIONS, "tanh", "activation")
+    with pytest.raises(ValueError, match="out of range"):
+        experts._pack(experts._ROUTE, -1, 1, 1, 1, 0, True, 1.0, 0)
+    with pytest.raises(ValueError, match="two or three"):
+        experts._operands(torch.zeros(2, 3), torch.zeros(3), cpu)
+    with pytest.raises(AttributeError):
+        ntc.no_such_name
+
+
+def test_packed_descriptors_are_the_structures():
+    """experts.py packs the descriptors with struct: the same bytes as the ctypes structures."""
+    from paper_2608_27888_gb300 import experts
+    for layout, cls in ((experts._ROUTE, ntc.ntc_route_desc), (experts._LINEAR, ntc.ntc_linear_desc),
+                        (experts._COMBINE, ntc.ntc_combine_desc)):
+        values = [1.5 if t is ctypes.c_float else i + 3 for i, (_, t) in enumerate(cls._fields_)]
+        assert layout.pack(*values) == bytes(cls(*values))
