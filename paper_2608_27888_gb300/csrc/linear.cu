@@ -7,13 +7,15 @@
 // One persistent CTA per SM.  A tile is 128 rows of one expert times BN columns;
 // its operands come in chunks of 64 of the contraction (128 bytes, the swizzle's
 // width) through a ring of shared-memory stages:
-//   warp 0       issues the TMA copies.  Gathered rows (x through rows[]) come by
-//                tile::gather4, four rows an instruction, all lanes issuing; rows
-//                past an expert's end get an index outside the matrix, which TMA
-//                fills with zeros -- so an expert may end anywhere in a tile, and
-//                anywhere in a chunk of kDw's contraction.
+//   warp 0       issues the TMA copies.
 //   warp 1       issues the MMAs (M = 128, N = BN) into one of two TMEM
 //                accumulators.
+//   warps 2, 3   copy what TMA boxes cannot: gathered rows (x through rows[]), and
+//                the chunk of kDw's contraction in which an expert ends, whose
+//                rest has to be zeros.  16-byte cp.async, 4 rows of 128 bytes an
+//                instruction, that arrive at the stage's barrier by themselves; the
+//                proxy fence is the MMA warp's.  (A fence by the copying threads
+//                waits for all of their copies in flight, 2,000 cycles a chunk.)
 //   warps 4..11  the epilogue of one accumulator while the other is filled: 16
 //                columns at a time through a warp's own shared memory, so that
 //                global memory sees 32-byte runs of a row, not one row a lane.
@@ -59,6 +61,8 @@ struct Args {
   const int32_t *rows, *offsets;
   const float *bias;
   const void *residual;
+  const uint8_t *x, *dz;  // the gathered operand, and kDw's other one
+  uint64_t ld_x, ld_dz;
   void *out, *z;
   uint64_t ld_out, ld_z, ld_residual;
   uint32_t num_experts, num_rows, x_rows;
@@ -91,14 +95,23 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, uin
       "l"(map), "r"(bar), "r"(x), "r"(y), "r"(e)
       : "memory");
 }
-// Four rows of 64 columns from column x on; the map's box is one row high.
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, const int32_t (&r)[4]) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], "
-      "[%2];\n" ::"r"(dst),
-      "l"(map), "r"(bar), "r"(x), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
-      : "memory");
+// 16 bytes from src, or 16 zeros.  The copies have no "memory" clobber: it would
+// have every one of them read the kernel's parameters again.
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src, bool zeros) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %2, 0;\ncp.async.cg.shared.global [%0], [%1], 16, p;\n}\n" ::"r"(dst),
+               "l"(src), "r"((uint32_t)zeros));
 }
+// 16 bytes, of which the first n come from src and the others are 0.
+__device__ __forceinline__ void copy16_part(uint32_t dst, const uint8_t *src, uint32_t n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(n));
+}
+// An arrival at bar once all of this thread's copies so far have landed.
+__device__ __forceinline__ void copy_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];\n" ::"r"(bar) : "memory");
+}
+// Between other threads' copies, whose arrival this thread has waited for, and the
+// tensor core's reads.
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
 // D[tmem] (+)= A[smem] x B[smem]
 __device__ __forceinline__ void umma_ss(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
                                         uint32_t accum) {
@@ -120,22 +133,26 @@ constexpr uint32_t kSw128Hi = (1024u >> 4) | (1u << 14) | (2u << 29);
 // ------------------------------------------------------------ waits
 
 // A bounded wait.  The first one that gives up sets the status word and the
-// CTA's quit flag, which ends the others'.
+// CTA's quit flag, which ends the others'.  The clock is looked at every 64 tries:
+// reading %globaltimer takes about as long as a chunk's MMAs.
 struct Waiter {
   volatile uint32_t *quit;
   unsigned int *status;
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
     if (mbar_try_wait(bar, parity)) return true;
-    const uint64_t t0 = global_ns();
-    while (!mbar_try_wait(bar, parity)) {
+    uint64_t t0 = 0;
+    for (uint32_t tries = 1;; ++tries) {
+      if (mbar_try_wait(bar, parity)) return true;
+      if (tries % 64) continue;
       if (*quit) return false;
-      if (global_ns() - t0 > kWaitLimitNs) {
+      const uint64_t now = global_ns();
+      if (t0 == 0) t0 = now;
+      if (now - t0 > kWaitLimitNs) {
         *quit = 1;
         atomicOr(status, 1u);
         return false;
       }
     }
-    return true;
   }
 };
 
@@ -191,11 +208,11 @@ __device__ __forceinline__ uint32_t bucket_of_tile(const uint32_t *tile, uint32_
 
 template <int MODE, int BN>
 struct Tiles {
-  const Args &a;
   const Shared &s;
-  uint32_t cols, row_tiles;
+  uint32_t num_experts, height, depth, cols, row_tiles;
   uint64_t total;
-  __device__ __forceinline__ Tiles(const Args &args, const Shared &sh) : a(args), s(sh) {
+  __device__ __forceinline__ Tiles(const Args &a, const Shared &sh)
+      : s(sh), num_experts(a.num_experts), height(a.height), depth(a.depth) {
     cols = (a.width + BN - 1) / BN;
     row_tiles = (a.height + kRows - 1) / kRows;
     total = MODE == kDw ? (uint64_t)a.num_experts * row_tiles * cols : (uint64_t)s.tile[a.num_experts + 1] * cols;
@@ -211,7 +228,7 @@ struct Tiles {
       r = (uint32_t)(t - o.e * per);
       many = row_tiles;
     } else {
-      o.e = bucket_of_tile(s.tile, a.num_experts, (uint32_t)(t / cols));
+      o.e = bucket_of_tile(s.tile, num_experts, (uint32_t)(t / cols));
       r = (uint32_t)(t - (uint64_t)s.tile[o.e] * cols);
       many = s.tile[o.e + 1] - s.tile[o.e];
     }
@@ -222,14 +239,14 @@ struct Tiles {
     const uint32_t begin = (uint32_t)s.off[o.e], count = (uint32_t)max(s.off[o.e + 1] - s.off[o.e], 0);
     if constexpr (MODE == kDw) {
       o.row = row;
-      o.rows = min(kRows, a.height - row);
+      o.rows = min(kRows, height - row);
       o.begin = begin;
       o.depth = count;
     } else {
       o.row = begin + row;
       o.rows = min(kRows, count - row);
       o.begin = 0;
-      o.depth = o.e < a.num_experts ? a.depth : 0u;
+      o.depth = o.e < num_experts ? depth : 0u;
     }
     return o;
   }
@@ -273,18 +290,18 @@ __device__ __forceinline__ uint32_t staged(uint32_t r, uint32_t c) {
 
 template <int MODE, int BN>
 __global__ void __launch_bounds__(kThreads, 1)
-    k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_ag,
-             const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_bg, const Args a) {
+    k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Args a) {
   constexpr uint32_t kStages = stages(BN), kStage = stage_bytes(BN);
   extern __shared__ uint8_t raw[];
   uint8_t *ring = raw + (1024 - (saddr(raw) & 1023)) % 1024;
   uint8_t *staging = ring + kRing;
   Shared &s = *reinterpret_cast<Shared *>(staging + kEpilogueWarps * 32 * kStageCols * 4);
   const uint32_t warp = uniform(threadIdx.x / 32), lane = threadIdx.x & 31;
+  const bool copies = MODE == kDw || (MODE == kForward && a.rows);  // warps 2 and 3 fill the stages, too
 
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < kStages; ++i) {
-      mbar_init(saddr(&s.full[i]), 1);
+      mbar_init(saddr(&s.full[i]), copies ? 65 : 1);  // TMA's, and every copying lane's
       mbar_init(saddr(&s.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -309,42 +326,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
       const Tile o = tiles.at(t);
       const uint32_t chunks = (o.depth + kChunk - 1) / kChunk;
-      int32_t idx[4];
-      if (MODE == kForward && a.rows) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t r = lane * 4 + i;
-          const int32_t at = r < o.rows ? (int32_t)ld_word((const uint32_t *)a.rows + o.row + r) : -1;
-          idx[i] = (uint32_t)at < a.x_rows ? at : (int32_t)a.x_rows;
-        }
-      }
       for (uint32_t c = 0; c < chunks; ++c, ++issued) {
         const uint32_t st = issued % kStages;
-        if (MODE == kDw) {  // the rows of this chunk; past the expert's end: none
-          const uint32_t r0 = c * kChunk + (lane & 15) * 4;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool in = r0 + i < o.depth;
-            const int32_t at = !in ? -1 : a.rows ? (int32_t)ld_word((const uint32_t *)a.rows + o.begin + r0 + i)
-                                                 : (int32_t)(o.begin + r0 + i);
-            idx[i] = (uint32_t)at < a.x_rows ? at : (int32_t)a.x_rows;
-          }
-        }
-        ok = wait(saddr(&s.empty[st]), ((issued / kStages) & 1) ^ 1);
-        ok = __all_sync(0xFFFFFFFFu, ok);
+        ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.empty[st]), ((issued / kStages) & 1) ^ 1));
         if (!ok) break;
         const uint32_t bar = saddr(&s.full[st]);
         const uint32_t sa = saddr(ring) + st * kStage, sb = sa + kABytes;
         if constexpr (MODE != kDw) {
-          const uint32_t pieces = MODE == kForward && a.rows ? (o.rows + 3) / 4 : (o.rows + 31) / 32;
-          const uint32_t bytes = pieces * (MODE == kForward && a.rows ? 512u : 4096u);
-          if (lane == 0) expect_tx(bar, bytes + BN * 128);
+          const uint32_t boxes = copies ? 0 : (o.rows + 31) / 32;
+          if (lane == 0) expect_tx(bar, boxes * 4096 + BN * 128);
           __syncwarp();
-          if (MODE == kForward && a.rows) {
-            if (lane < pieces) tma_gather4(sa + lane * 512, &map_ag, bar, (int32_t)(c * kChunk), idx);
-          } else if (lane < pieces) {
-            tma_2d(sa + lane * 4096, &map_a, bar, (int32_t)(c * kChunk), (int32_t)(o.row + lane * 32));
-          }
+          if (lane < boxes) tma_2d(sa + lane * 4096, &map_a, bar, (int32_t)(c * kChunk), (int32_t)(o.row + lane * 32));
           if constexpr (MODE == kForward) {
             if (lane == 0) tma_3d(sb, &map_b, bar, (int32_t)(c * kChunk), (int32_t)o.col, (int32_t)o.e);
           } else {
@@ -353,29 +345,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         } else {
           const bool whole = (c + 1) * kChunk <= o.depth;
-          if (lane == 0) expect_tx(bar, kABytes + BN * 128);
+          if (lane == 0) expect_tx(bar, whole ? kABytes + (a.rows ? 0 : BN * 128) : 0);
           __syncwarp();
-          const uint32_t g = lane & 15, half = lane >> 4;
-          if (whole) {
-            if (lane < 2)
-              tma_2d(sa + lane * 8192, &map_a, bar, (int32_t)(o.row + lane * 64), (int32_t)(o.begin + c * kChunk));
-          } else {
-            int32_t own[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const uint32_t r = c * kChunk + g * 4 + i;
-              own[i] = (int32_t)(r < o.depth ? o.begin + r : a.num_rows);
-            }
-            tma_gather4(sa + half * 8192 + g * 512, &map_ag, bar, (int32_t)(o.row + half * 64), own);
-          }
-          if (whole && !a.rows) {
-            if (lane < BN / 64)
-              tma_2d(sb + lane * 8192, &map_b, bar, (int32_t)(o.col + lane * 64), (int32_t)(o.begin + c * kChunk));
-          } else {
-#pragma unroll
-            for (uint32_t j = half; j < BN / 64; j += 2)
-              tma_gather4(sb + j * 8192 + g * 512, &map_bg, bar, (int32_t)(o.col + j * 64), idx);
-          }
+          if (whole && lane < 2)
+            tma_2d(sa + lane * 8192, &map_a, bar, (int32_t)(o.row + lane * 64), (int32_t)(o.begin + c * kChunk));
+          if (whole && !a.rows && lane < BN / 64)
+            tma_2d(sb + lane * 8192, &map_b, bar, (int32_t)(o.col + lane * 64), (int32_t)(o.begin + c * kChunk));
         }
       }
     }
@@ -402,6 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t st = used % kStages;
         ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.full[st]), (used / kStages) & 1));
         if (!ok) break;
+        if (copies) fence_async();
         fence_after();
         any = true;
         const uint32_t sa = saddr(ring) + st * kStage;
@@ -422,6 +398,106 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       mbar_wait(saddr(&s.drain), 0);
     }
+  } else if (warp < 4 && copies) {
+    // A copy is 4 rows of 128 bytes; this lane has row lane / 8 of it, piece lane % 8,
+    // which the swizzle moves by the row's place in its group of eight.  A warp's
+    // instructions wait for one another's results, so a chunk's copies are straight
+    // code: what depends on the row (its address, whether it is zeros) is worked
+    // out before, and only a matrix's last columns take the form with a count.
+    // (Per-copy tests and addresses: 100 cycles a copy, 1,067 us instead of 380 for
+    // 32,768 gathered rows, 2,048 -> 4,096 wide.)
+    constexpr int kMany = MODE == kDw ? 8 : 16;  // copies of a chunk (kDw: per 64 columns) by this warp
+    const uint32_t half = warp - 2, sub = lane >> 3, piece = lane & 7;
+    const uint32_t first = half * kMany * 4;  // first row of this warp
+    const uint32_t to0 = (first + sub) * 128 + ((piece ^ sub) << 4), to1 = to0 ^ 64;  // even and odd copies
+    const uint8_t *x = a.x, *dz = a.dz;
+    const uint64_t pitch = a.ld_x * 2, pitch_dz = a.ld_dz * 2;
+    const uint32_t *rows = (const uint32_t *)a.rows;
+    const uint32_t x_rows = a.x_rows, depth = a.depth, width = a.width, height = a.height;
+    uint32_t issued = 0;
+    bool ok = true;
+    for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
+      const Tile o = tiles.at(t);
+      const uint32_t chunks = (o.depth + kChunk - 1) / kChunk;
+      const uint8_t *src[kMany];
+      uint32_t zeros = 0;  // bit i: copy i's row is none of x's
+      // the rows of copies from `from` on; those at `last` and beyond are zeros
+      const auto look = [&](uint32_t from, uint32_t last) {
+        int32_t at[kMany];
+#pragma unroll
+        for (int i = 0; i < kMany; ++i) {
+          const uint32_t r = from + i * 4 + sub;
+          at[i] = r >= last ? -1 : rows ? (int32_t)ld_word(rows + r) : (int32_t)r;
+        }
+        zeros = 0;
+#pragma unroll
+        for (int i = 0; i < kMany; ++i) {
+          const bool none = (uint32_t)at[i] >= x_rows;
+          zeros |= (uint32_t)none << i;
+          src[i] = x + (none ? 0 : (uint64_t)(uint32_t)at[i] * pitch) + piece * 16;
+        }
+      };
+      if (MODE == kForward) look(o.row + first, o.row + o.rows);
+      else if (chunks && (rows || o.depth < kChunk)) look(o.begin + first, o.begin + o.depth);
+      for (uint32_t c = 0; c < chunks; ++c, ++issued) {
+        const uint32_t st = issued % kStages;
+        ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.empty[st]), ((issued / kStages) & 1) ^ 1));
+        if (!ok) break;
+        const uint32_t sa = saddr(ring) + st * kStage, sb = sa + kABytes;
+        if constexpr (MODE == kForward) {
+          const uint32_t col = c * kChunk;
+          if (col + kChunk <= depth) {
+#pragma unroll
+            for (int i0 = 0; i0 < kMany; i0 += 4)
+              if (first + i0 * 4 < o.rows) {  // four copies, 16 rows; rows past the tile's end are of no use
+#pragma unroll
+                for (int i = i0; i < i0 + 4; ++i)
+                  copy16(sa + (i & 1 ? to1 : to0) + i * 512, src[i] + (uint64_t)col * 2, (zeros >> i) & 1);
+              }
+          } else {
+            const uint32_t n = col + piece * 8 < depth ? min(16u, (depth - col - piece * 8) * 2) : 0u;
+#pragma unroll
+            for (int i = 0; i < kMany; ++i)
+              copy16_part(sa + (i & 1 ? to1 : to0) + i * 512, n ? src[i] + (uint64_t)col * 2 : x, (zeros >> i) & 1 ? 0u : n);
+          }
+        } else {
+          const bool whole = (c + 1) * kChunk <= o.depth;
+          if (rows || !whole) {
+#pragma unroll
+            for (uint32_t j = 0; j < BN / 64; ++j) {
+              const uint32_t col = o.col + j * 64;
+              if (col + 64 <= width) {
+#pragma unroll
+                for (int i = 0; i < kMany; ++i)
+                  copy16(sb + j * 8192 + (i & 1 ? to1 : to0) + i * 512, src[i] + (uint64_t)col * 2, (zeros >> i) & 1);
+              } else {
+                const uint32_t n = col + piece * 8 < width ? min(16u, (width - col - piece * 8) * 2) : 0u;
+#pragma unroll
+                for (int i = 0; i < kMany; ++i)
+                  copy16_part(sb + j * 8192 + (i & 1 ? to1 : to0) + i * 512, n ? src[i] + (uint64_t)col * 2 : x,
+                              (zeros >> i) & 1 ? 0u : n);
+              }
+            }
+          }
+          if (!whole) {
+            for (int i = 0; i < kMany; ++i) {
+              const uint32_t at = c * kChunk + first + i * 4 + sub;
+#pragma unroll
+              for (uint32_t j = 0; j < 2; ++j) {
+                const uint32_t col = o.row + j * 64 + piece * 8;
+                const uint32_t n = at < o.depth && col < height ? min(16u, (height - col) * 2) : 0u;
+                copy16_part(sa + j * 8192 + (i & 1 ? to1 : to0) + i * 512,
+                            n ? dz + (uint64_t)(o.begin + at) * pitch_dz + col * 2 : dz, n);
+              }
+            }
+          } else if (c + 1 < chunks && (rows || (c + 2) * kChunk > o.depth)) {
+            look(o.begin + (c + 1) * kChunk + first, o.begin + o.depth);
+          }
+        }
+        copy_arrive(saddr(&s.full[st]));
+      }
+    }
+    if (!ok) asm volatile("cp.async.wait_all;\n" ::: "memory");  // none lands after the CTA's end
   } else if (warp >= 4) {
     const uint32_t w = warp - 4, quarter = warp & 3;
     const uint32_t part = (w >> 2) * (BN / 2);  // each set of four warps takes half of the columns
@@ -703,12 +779,15 @@ unsigned int *status_word() {
 
 template <int MODE, int BN>
 cudaError_t launch_tile(const Operand &A, const Operand &B, Args a, uint64_t tiles_bound, int sms, cudaStream_t st) {
-  CUtensorMap ma, mag, mb, mbg;
-  bool ok = make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 32) && make_map(&mag, A, 2, 64, 1);
-  if (MODE == kDw) ok = ok && make_map(&mb, B, 2, 64, 64) && make_map(&mbg, B, 2, 64, 1);
-  else ok = ok && make_map(&mb, B, 3, 64, MODE == kForward ? BN : 64);
-  if (!ok) return cudaErrorInvalidValue;
-  if (MODE != kDw) mbg = mb;
+  CUtensorMap ma, mb;
+  if (!make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 32) ||
+      !make_map(&mb, B, MODE == kDw ? 2 : 3, 64, MODE == kForward ? BN : 64))
+    return cudaErrorInvalidValue;
+  const Operand &x = MODE == kDw ? B : A;
+  a.x = (const uint8_t *)x.p;
+  a.ld_x = x.ld;
+  a.dz = (const uint8_t *)A.p;
+  a.ld_dz = A.ld;
   static std::atomic<uint64_t> allowed{0};  // devices that know of the kernel's shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -719,7 +798,7 @@ cudaError_t launch_tile(const Operand &A, const Operand &B, Args a, uint64_t til
     if (dev < 64) allowed.fetch_or(1ull << dev);
   }
   const unsigned grid = (unsigned)std::min<uint64_t>(tiles_bound, (uint64_t)sms);
-  return launch_pdl(k_linear<MODE, BN>, grid, kThreads, kSharedBytes, st, ma, mag, mb, mbg, a);
+  return launch_pdl(k_linear<MODE, BN>, grid, kThreads, kSharedBytes, st, ma, mb, a);
 }
 
 // Row tiles of num_rows rows in num_experts segments (and those of no expert), at most.
