@@ -2,7 +2,8 @@
 //
 //   forward   y_i  = act(W_e x_{r(i)} + b_e) + residual_i    contraction over K
 //   kDx       dx_i = W_e^T dz_i                               contraction over N
-//   kDw       dw_e = sum_i dz_i x_{r(i)}^T                    contraction over e's rows
+//   kDw       dw_e = sum_i dz_i x_{r(i)}^T                    contraction over e's rows; computed
+//             transposed, so that the operand that may be gathered is the narrower one
 //
 // One persistent CTA per SM.  A tile is 128 rows of one expert times BN columns;
 // its operands come in chunks of 64 of the contraction (128 bytes, the swizzle's
@@ -10,7 +11,7 @@
 //   warp 0       issues the TMA copies.
 //   warp 1       issues the MMAs (M = 128, N = BN) into one of two TMEM
 //                accumulators.
-//   warps 2, 3   copy what TMA boxes cannot: gathered rows (x through rows[]), and
+//   warps 2, 3 (kDw: 12, 13 as well)  copy what TMA boxes cannot: gathered rows (x through rows[]), and
 //                the chunk of kDw's contraction in which an expert ends, whose
 //                rest has to be zeros.  16-byte cp.async, 4 rows of 128 bytes an
 //                instruction, that arrive at the stage's barrier by themselves; the
@@ -33,7 +34,10 @@ namespace {
 
 enum Mode { kForward = 0, kDx = 1, kDw = 2 };
 
-constexpr int kThreads = 384;
+// Warps that copy rows: a chunk's copies take a warp 300 cycles, and in kDw, whose rows
+// change from chunk to chunk, as long again for their addresses.
+constexpr int copy_warps(int mode) { return mode == kDw ? 4 : 2; }
+constexpr int threads(int mode) { return 320 + 32 * copy_warps(mode); }
 constexpr int kEpilogueWarps = 8;
 constexpr uint32_t kRows = 128;   // rows of a tile
 constexpr uint32_t kChunk = 64;   // contraction elements of a stage
@@ -49,7 +53,7 @@ constexpr uint32_t stages(int BN) {
 }
 
 struct Shared {
-  uint64_t full[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+  uint64_t full[kMaxStages], copied[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
   uint32_t tmem, quit;
   int32_t off[NTC_MAX_EXPERTS + 2];       // first row of each expert; [E]: of no expert; [E + 1]: the end
   uint32_t tile[NTC_MAX_EXPERTS + 2];     // first row tile of each expert (and of no expert); the total
@@ -61,13 +65,13 @@ struct Args {
   const int32_t *rows, *offsets;
   const float *bias;
   const void *residual;
-  const uint8_t *x, *dz;  // the gathered operand, and kDw's other one
+  const uint8_t *x, *dz;  // the operand that may be gathered, and kDw's other one
   uint64_t ld_x, ld_dz;
   void *out, *z;
   uint64_t ld_out, ld_z, ld_residual;
   uint32_t num_experts, num_rows, x_rows;
   uint32_t width;      // columns of the output
-  uint32_t height;     // kDw: rows of one expert's output
+  uint32_t height;     // kDw: rows of one expert's (transposed) output
   uint32_t depth;      // contraction length (not kDw: there it is the expert's rows)
   uint32_t activation;
   float slope;
@@ -160,7 +164,7 @@ struct Waiter {
 
 struct Tile {
   uint32_t e;         // expert; num_experts: rows of no expert
-  uint32_t row;       // first row: of the matrix (kDw: of the expert's output)
+  uint32_t row;       // first row: of the matrix (kDw: of the expert's transposed output)
   uint32_t rows;      // rows inside, at most 128
   uint32_t col;       // first column
   uint32_t depth;     // contraction length; 0: the tile is zeros
@@ -289,7 +293,7 @@ __device__ __forceinline__ uint32_t staged(uint32_t r, uint32_t c) {
 // ------------------------------------------------------------ the kernel
 
 template <int MODE, int BN>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(threads(MODE), 1)
     k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Args a) {
   constexpr uint32_t kStages = stages(BN), kStage = stage_bytes(BN);
   extern __shared__ uint8_t raw[];
@@ -297,11 +301,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t *staging = ring + kRing;
   Shared &s = *reinterpret_cast<Shared *>(staging + kEpilogueWarps * 32 * kStageCols * 4);
   const uint32_t warp = uniform(threadIdx.x / 32), lane = threadIdx.x & 31;
-  const bool copies = MODE == kDw || (MODE == kForward && a.rows);  // warps 2 and 3 fill the stages, too
 
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < kStages; ++i) {
-      mbar_init(saddr(&s.full[i]), copies ? 65 : 1);  // TMA's, and every copying lane's
+      mbar_init(saddr(&s.full[i]), 1);
+      mbar_init(saddr(&s.copied[i]), 32 * copy_warps(MODE));
       mbar_init(saddr(&s.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -333,7 +337,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const uint32_t bar = saddr(&s.full[st]);
         const uint32_t sa = saddr(ring) + st * kStage, sb = sa + kABytes;
         if constexpr (MODE != kDw) {
-          const uint32_t boxes = copies ? 0 : (o.rows + 31) / 32;
+          const uint32_t boxes = MODE == kForward && a.rows ? 0 : (o.rows + 31) / 32;
           if (lane == 0) expect_tx(bar, boxes * 4096 + BN * 128);
           __syncwarp();
           if (lane < boxes) tma_2d(sa + lane * 4096, &map_a, bar, (int32_t)(c * kChunk), (int32_t)(o.row + lane * 32));
@@ -345,11 +349,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         } else {
           const bool whole = (c + 1) * kChunk <= o.depth;
-          if (lane == 0) expect_tx(bar, whole ? kABytes + (a.rows ? 0 : BN * 128) : 0);
+          if (lane == 0) expect_tx(bar, whole ? (a.rows ? 0 : kABytes) + BN * 128 : 0);
           __syncwarp();
-          if (whole && lane < 2)
+          if (whole && !a.rows && lane < 2)
             tma_2d(sa + lane * 8192, &map_a, bar, (int32_t)(o.row + lane * 64), (int32_t)(o.begin + c * kChunk));
-          if (whole && !a.rows && lane < BN / 64)
+          if (whole && lane < BN / 64)
             tma_2d(sb + lane * 8192, &map_b, bar, (int32_t)(o.col + lane * 64), (int32_t)(o.begin + c * kChunk));
         }
       }
@@ -363,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                            ((MODE != kForward ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((kRows >> 4) << 24);
     // 16 of the contraction: 32 bytes along a K-major row, 16 rows of an MN-major block
     constexpr uint32_t kStepA = MODE == kDw ? 2048 >> 4 : 32 >> 4, kStepB = MODE != kForward ? 2048 >> 4 : 32 >> 4;
-    uint32_t used = 0, acc = 0;
+    uint32_t used = 0, acc = 0, phases = 0;  // phases: bit of each stage's copied barrier
     bool ok = true, any = false;
     for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
       const Tile o = tiles.at(t);
@@ -376,8 +380,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (uint32_t c = 0; c < chunks; ++c, ++used) {
         const uint32_t st = used % kStages;
         ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.full[st]), (used / kStages) & 1));
+        if (ok && (a.rows || (MODE == kDw && (c + 1) * kChunk > o.depth))) {
+          ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.copied[st]), (phases >> st) & 1));
+          phases ^= 1u << st;
+          fence_async();
+        }
         if (!ok) break;
-        if (copies) fence_async();
         fence_after();
         any = true;
         const uint32_t sa = saddr(ring) + st * kStage;
@@ -398,51 +406,62 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       mbar_wait(saddr(&s.drain), 0);
     }
-  } else if (warp < 4 && copies) {
+  } else if (warp < 4 || warp >= 12) {
     // A copy is 4 rows of 128 bytes; this lane has row lane / 8 of it, piece lane % 8,
     // which the swizzle moves by the row's place in its group of eight.  A warp's
     // instructions wait for one another's results, so a chunk's copies are straight
     // code: what depends on the row (its address, whether it is zeros) is worked
     // out before, and only a matrix's last columns take the form with a count.
-    // (Per-copy tests and addresses: 100 cycles a copy, 1,067 us instead of 380 for
+    // (Per-copy tests and addresses: 100 cycles a copy, 1,067 us instead of 364 for
     // 32,768 gathered rows, 2,048 -> 4,096 wide.)
-    constexpr int kMany = MODE == kDw ? 8 : 16;  // copies of a chunk (kDw: per 64 columns) by this warp
-    const uint32_t half = warp - 2, sub = lane >> 3, piece = lane & 7;
-    const uint32_t first = half * kMany * 4;  // first row of this warp
+    constexpr int kMany = (MODE == kDw ? 16 : 32) / copy_warps(MODE);  // copies of a chunk (kDw: per 64 columns) by this warp
+    const uint32_t sub = lane >> 3, piece = lane & 7;
+    const uint32_t first = (warp < 4 ? warp - 2 : warp - 10) * kMany * 4;  // first row of this warp
     const uint32_t to0 = (first + sub) * 128 + ((piece ^ sub) << 4), to1 = to0 ^ 64;  // even and odd copies
     const uint8_t *x = a.x, *dz = a.dz;
     const uint64_t pitch = a.ld_x * 2, pitch_dz = a.ld_dz * 2;
     const uint32_t *rows = (const uint32_t *)a.rows;
     const uint32_t x_rows = a.x_rows, depth = a.depth, width = a.width, height = a.height;
     uint32_t issued = 0;
-    bool ok = true;
+    bool ok = MODE == kDw || (MODE == kForward && rows);  // else there is nothing to copy
     for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
       const Tile o = tiles.at(t);
       const uint32_t chunks = (o.depth + kChunk - 1) / kChunk;
       const uint8_t *src[kMany];
       uint32_t zeros = 0;  // bit i: copy i's row is none of x's
-      // the rows of copies from `from` on; those at `last` and beyond are zeros
-      const auto look = [&](uint32_t from, uint32_t last) {
-        int32_t at[kMany];
+      const uint32_t last = MODE == kDw ? o.begin + o.depth : o.row + o.rows;  // rows from here on are zeros
+      // fetch: the rows of x of the positions from `from` on, whatever `last` says
+      // (the loads are not conditional); look: their addresses
+      const auto fetch = [&](uint32_t from, int32_t (&at)[kMany]) {
 #pragma unroll
         for (int i = 0; i < kMany; ++i) {
-          const uint32_t r = from + i * 4 + sub;
-          at[i] = r >= last ? -1 : rows ? (int32_t)ld_word(rows + r) : (int32_t)r;
+          const uint32_t r = min(from + i * 4 + sub, last - 1);
+          at[i] = rows ? (int32_t)ld_word(rows + r) : (int32_t)r;
         }
+      };
+      const auto look = [&](uint32_t from, const int32_t (&at)[kMany]) {
         zeros = 0;
 #pragma unroll
         for (int i = 0; i < kMany; ++i) {
-          const bool none = (uint32_t)at[i] >= x_rows;
+          const bool none = (uint32_t)at[i] >= x_rows || from + i * 4 + sub >= last;
           zeros |= (uint32_t)none << i;
           src[i] = x + (none ? 0 : (uint64_t)(uint32_t)at[i] * pitch) + piece * 16;
         }
       };
-      if (MODE == kForward) look(o.row + first, o.row + o.rows);
-      else if (chunks && (rows || o.depth < kChunk)) look(o.begin + first, o.begin + o.depth);
-      for (uint32_t c = 0; c < chunks; ++c, ++issued) {
+      int32_t one[kMany], two[kMany];  // kDw: the rows of the next chunk, and of the one after it
+      if (chunks) {
+        const uint32_t from = (MODE == kDw ? o.begin : o.row) + first;
+        fetch(from, one);
+        look(from, one);
+        if (MODE == kDw) fetch(from + kChunk, one);
+      }
+      // `next` has been asked for one chunk ago, `later` is asked for now: they change
+      // places from chunk to chunk, for a register copy would wait for the loads
+      const auto step = [&](uint32_t c, int32_t (&next)[kMany], int32_t (&later)[kMany]) {
         const uint32_t st = issued % kStages;
         ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.empty[st]), ((issued / kStages) & 1) ^ 1));
-        if (!ok) break;
+        if (!ok) return;
+        ++issued;
         const uint32_t sa = saddr(ring) + st * kStage, sb = sa + kABytes;
         if constexpr (MODE == kForward) {
           const uint32_t col = c * kChunk;
@@ -460,45 +479,52 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int i = 0; i < kMany; ++i)
               copy16_part(sa + (i & 1 ? to1 : to0) + i * 512, n ? src[i] + (uint64_t)col * 2 : x, (zeros >> i) & 1 ? 0u : n);
           }
+          copy_arrive(saddr(&s.copied[st]));
         } else {
           const bool whole = (c + 1) * kChunk <= o.depth;
+          if (!rows && whole && (c + 2) * kChunk <= o.depth) return;
+          fetch(o.begin + (c + 2) * kChunk + first, later);
           if (rows || !whole) {
 #pragma unroll
-            for (uint32_t j = 0; j < BN / 64; ++j) {
-              const uint32_t col = o.col + j * 64;
-              if (col + 64 <= width) {
+            for (uint32_t j = 0; j < 2; ++j) {
+              const uint32_t col = o.row + j * 64;
+              if (col + 64 <= height) {
 #pragma unroll
                 for (int i = 0; i < kMany; ++i)
-                  copy16(sb + j * 8192 + (i & 1 ? to1 : to0) + i * 512, src[i] + (uint64_t)col * 2, (zeros >> i) & 1);
+                  copy16(sa + j * 8192 + (i & 1 ? to1 : to0) + i * 512, src[i] + (uint64_t)col * 2, (zeros >> i) & 1);
               } else {
-                const uint32_t n = col + piece * 8 < width ? min(16u, (width - col - piece * 8) * 2) : 0u;
+                const uint32_t n = col + piece * 8 < height ? min(16u, (height - col - piece * 8) * 2) : 0u;
 #pragma unroll
                 for (int i = 0; i < kMany; ++i)
-                  copy16_part(sb + j * 8192 + (i & 1 ? to1 : to0) + i * 512, n ? src[i] + (uint64_t)col * 2 : x,
+                  copy16_part(sa + j * 8192 + (i & 1 ? to1 : to0) + i * 512, n ? src[i] + (uint64_t)col * 2 : x,
                               (zeros >> i) & 1 ? 0u : n);
               }
             }
-          }
-          if (!whole) {
-            for (int i = 0; i < kMany; ++i) {
-              const uint32_t at = c * kChunk + first + i * 4 + sub;
+            if (!whole) {
+              for (int i = 0; i < kMany; ++i) {
+                const uint32_t at = c * kChunk + first + i * 4 + sub;
 #pragma unroll
-              for (uint32_t j = 0; j < 2; ++j) {
-                const uint32_t col = o.row + j * 64 + piece * 8;
-                const uint32_t n = at < o.depth && col < height ? min(16u, (height - col) * 2) : 0u;
-                copy16_part(sa + j * 8192 + (i & 1 ? to1 : to0) + i * 512,
-                            n ? dz + (uint64_t)(o.begin + at) * pitch_dz + col * 2 : dz, n);
+                for (uint32_t j = 0; j < BN / 64; ++j) {
+                  const uint32_t col = o.col + j * 64 + piece * 8;
+                  const uint32_t n = at < o.depth && col < width ? min(16u, (width - col) * 2) : 0u;
+                  copy16_part(sb + j * 8192 + (i & 1 ? to1 : to0) + i * 512,
+                              n ? dz + (uint64_t)(o.begin + at) * pitch_dz + col * 2 : dz, n);
+                }
               }
             }
-          } else if (c + 1 < chunks && (rows || (c + 2) * kChunk > o.depth)) {
-            look(o.begin + (c + 1) * kChunk + first, o.begin + o.depth);
+            copy_arrive(saddr(&s.copied[st]));
           }
+          if (!rows) fetch(o.begin + (c + 1) * kChunk + first, next);  // chunks may have been passed over
+          look(o.begin + (c + 1) * kChunk + first, next);
         }
-        copy_arrive(saddr(&s.full[st]));
+      };
+      for (uint32_t c = 0; ok && c < chunks; c += 2) {
+        step(c, one, two);
+        if (ok && c + 1 < chunks) step(c + 1, two, one);
       }
     }
     if (!ok) asm volatile("cp.async.wait_all;\n" ::: "memory");  // none lands after the CTA's end
-  } else if (warp >= 4) {
+  } else {
     const uint32_t w = warp - 4, quarter = warp & 3;
     const uint32_t part = (w >> 2) * (BN / 2);  // each set of four warps takes half of the columns
     uint8_t *mine = staging + w * 32 * kStageCols * 4;
@@ -513,13 +539,44 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_after();
       }
       const int32_t high = (int32_t)o.rows - (int32_t)(quarter * 32);  // rows of this warp inside
-      const uint64_t row0 = (MODE == kDw ? (uint64_t)o.e * a.height : 0) + o.row + quarter * 32;
+      const uint64_t row0 = o.row + quarter * 32;
       if (high > 0) {
         for (uint32_t c0 = part; c0 < part + BN / 2 && o.col + c0 < a.width; c0 += kStageCols) {
+          uint32_t r[16];
           if (!zero) {
-            uint32_t r[16];
             tmem_ld16(tmem + ((quarter * 32) << 16) + (acc & 1) * BN + c0, r);
             tmem_wait_ld();
+          }
+          if constexpr (MODE == kDw) {
+            // dw is [out_dim][in_dim]: a column of the tile is a run of its row
+            float v[16] = {};
+            const uint32_t j = lane >> 1, k0 = (lane & 1) * 16;
+            if (!zero) {
+#pragma unroll
+              for (uint32_t q = 0; q < 16; ++q)
+                *reinterpret_cast<uint32_t *>(mine + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4) = r[q];
+              __syncwarp();
+#pragma unroll
+              for (uint32_t q = 0; q < 4; ++q) {
+                const float4 f = *reinterpret_cast<const float4 *>(mine + j * 128 + (((k0 / 4 + q) ^ (j & 7)) << 4));
+                v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
+              }
+            }
+            if (o.col + c0 + j < a.width) {
+              const uint64_t at = ((uint64_t)o.e * a.width + o.col + c0 + j) * a.ld_out + o.row + quarter * 32 + k0;
+#pragma unroll
+              for (uint32_t q = 0; q < 2; ++q) {
+                const int n = min(8, high - (int32_t)(k0 + 8 * q));
+                float u[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
+                if (n > 0) store8(a.out, at + 8 * q, n, a.vec_out, bf16, u);
+              }
+            }
+            __syncwarp();
+            continue;
+          }
+          if (!zero) {
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q)
               asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(base + staged(lane, q)), "r"(r[4 * q]),
@@ -783,11 +840,10 @@ cudaError_t launch_tile(const Operand &A, const Operand &B, Args a, uint64_t til
   if (!make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 32) ||
       !make_map(&mb, B, MODE == kDw ? 2 : 3, 64, MODE == kForward ? BN : 64))
     return cudaErrorInvalidValue;
-  const Operand &x = MODE == kDw ? B : A;
-  a.x = (const uint8_t *)x.p;
-  a.ld_x = x.ld;
-  a.dz = (const uint8_t *)A.p;
-  a.ld_dz = A.ld;
+  a.x = (const uint8_t *)A.p;
+  a.ld_x = A.ld;
+  a.dz = (const uint8_t *)B.p;
+  a.ld_dz = B.ld;
   static std::atomic<uint64_t> allowed{0};  // devices that know of the kernel's shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -798,7 +854,7 @@ cudaError_t launch_tile(const Operand &A, const Operand &B, Args a, uint64_t til
     if (dev < 64) allowed.fetch_or(1ull << dev);
   }
   const unsigned grid = (unsigned)std::min<uint64_t>(tiles_bound, (uint64_t)sms);
-  return launch_pdl(k_linear<MODE, BN>, grid, kThreads, kSharedBytes, st, ma, mb, a);
+  return launch_pdl(k_linear<MODE, BN>, grid, threads(MODE), kSharedBytes, st, ma, mb, a);
 }
 
 // Row tiles of num_rows rows in num_experts segments (and those of no expert), at most.
@@ -1049,9 +1105,10 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
     a.out = dw;
     a.rows = rows;
     a.x_rows = (uint32_t)d.num_x_rows;
-    a.height = d.out_dim;
+    a.width = d.out_dim;
+    a.height = d.in_dim;
     a.vec_out = rows_are_vec(dw, d.in_dim, 2);
-    if (e == cudaSuccess) e = launch_product<kDw>(Z, X, a, st);
+    if (e == cudaSuccess) e = launch_product<kDw>(X, Z, a, st);
   }
   return op_cuda(e, what);
 }
