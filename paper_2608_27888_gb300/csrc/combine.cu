@@ -13,100 +13,130 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// One thread per (token, 16 bytes of columns); the token's rows are read four at
-// a time so that their latencies overlap.
-template <typename T>
+// Pieces of a row of `dim` elements that start at column c: whole 16-byte ones when
+// VEC (all rows start on 16 bytes and dim is a multiple of Vec<T>::N).
+template <typename T, bool VEC>
+__device__ __forceinline__ uint4 load_piece(const T *p, int n) {
+  if constexpr (VEC) return *reinterpret_cast<const uint4 *>(p);
+  float v[Vec<T>::N];
+  load_vec<T>(p, n, false, v);
+  return Vec<T>::pack(v);  // exact: the values are T's
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_piece(T *p, int n, const float (&v)[Vec<T>::N]) {
+  if constexpr (VEC) *reinterpret_cast<uint4 *>(p) = Vec<T>::pack(v);
+  else store_vec<T>(p, n, false, v);
+}
+
+// One thread per (token, 16 bytes of columns).  The places and weights of eight
+// entries are read first, then their pieces, all eight in flight.
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads)
-    k_combine(ntc_combine_desc d, const T *y, const int32_t *place, const float *weights, const int32_t *offsets,
-              const T *residual, T *out, bool vec_y, bool vec_out, bool vec_res) {
-  constexpr int N = Vec<T>::N;
+    k_combine(const ntc_combine_desc d, const T *y, const int32_t *place, const float *weights, const int32_t *offsets,
+              const T *residual, T *out) {
+  constexpr int N = Vec<T>::N, kBatch = 8;
   pdl_wait();
   pdl_trigger();
   const int32_t live = offsets ? offset_at(offsets, d.num_experts, (int32_t)d.num_rows) : (int32_t)d.num_rows;
-  const uint32_t pieces = (d.dim + N - 1) / N;
+  const uint32_t pieces = (d.dim + N - 1) / N, k = d.top_k;
   const uint64_t total = d.num_tokens * pieces;
   for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += (uint64_t)gridDim.x * kThreads) {
     const uint64_t t = i / pieces;
     const uint32_t c = (uint32_t)(i - t * pieces) * N;
     const int n = min((int)(d.dim - c), N);
-    float acc[N];
-    if (residual) {
-      load_vec<T>(residual + t * d.ld_residual + c, n, vec_res, acc);
-    } else {
-#pragma unroll
-      for (int q = 0; q < N; ++q) acc[q] = 0.0f;
-    }
     float sum[N];
 #pragma unroll
     for (int q = 0; q < N; ++q) sum[q] = 0.0f;
-    for (uint32_t j0 = 0; j0 < d.top_k; j0 += 4) {
-      float v[4][N], w[4];
+    uint4 r = make_uint4(0, 0, 0, 0);
+    if (residual) r = load_piece<T, VEC>(residual + t * d.ld_residual + c, n);
+    for (uint32_t j0 = 0; j0 < k; j0 += kBatch) {
+      int32_t p[kBatch];
+      float w[kBatch];
+      uint4 v[kBatch];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint32_t j = j0 + u;
-        const int32_t p = j < d.top_k ? place[t * d.top_k + j] : -1;
-        const bool in = p >= 0 && p < live;
-        w[u] = in ? (weights ? weights[t * d.top_k + j] : 1.0f) : 0.0f;
-        if (in) {
-          load_vec<T>(y + (uint64_t)p * d.ld_y + c, n, vec_y, v[u]);
-        } else {
-#pragma unroll
-          for (int q = 0; q < N; ++q) v[u][q] = 0.0f;
+      for (int u = 0; u < kBatch; ++u) {
+        p[u] = -1;
+        w[u] = 1.0f;
+        if (j0 + u < k) {
+          p[u] = place[t * k + j0 + u];
+          if (weights) w[u] = weights[t * k + j0 + u];
         }
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < kBatch; ++u)
+        if ((uint32_t)p[u] < (uint32_t)live) v[u] = load_piece<T, VEC>(y + (uint64_t)(uint32_t)p[u] * d.ld_y + c, n);
 #pragma unroll
-        for (int q = 0; q < N; ++q) sum[q] = fmaf(w[u], v[u][q], sum[q]);
+      for (int u = 0; u < kBatch; ++u)
+        if ((uint32_t)p[u] < (uint32_t)live) {
+          float f[N];
+          Vec<T>::unpack(v[u], f);
+#pragma unroll
+          for (int q = 0; q < N; ++q) sum[q] = fmaf(w[u], f[q], sum[q]);
+        }
     }
+    if (residual) {
+      float f[N];
+      Vec<T>::unpack(r, f);
 #pragma unroll
-    for (int q = 0; q < N; ++q) acc[q] += sum[q];
-    store_vec<T>(out + t * d.ld_out + c, n, vec_out, acc);
+      for (int q = 0; q < N; ++q) sum[q] += f[q];
+    }
+    store_piece<T, VEC>(out + t * d.ld_out + c, n, sum);
   }
 }
 
 // One warp per entry (token, slot): its row of dy is written and its dot product
-// summed in the same pass.  dout's row is read once per slot, after the first time
-// from L1 or L2.
-template <typename T>
+// summed in the same pass, four pieces of each row in flight.  dout's row is read
+// once per slot, after the first time from L1 or L2.
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads)
-    k_combine_back(ntc_combine_desc d, const T *dout, const T *y, const int32_t *place, const float *weights,
-                   const int32_t *offsets, T *dy, float *dweights, bool vec_y, bool vec_out, bool vec_dy) {
-  constexpr int N = Vec<T>::N;
+    k_combine_back(const ntc_combine_desc d, const T *dout, const T *y, const int32_t *place, const float *weights,
+                   const int32_t *offsets, T *dy, float *dweights) {
+  constexpr int N = Vec<T>::N, kBatch = 4;
   pdl_wait();
   pdl_trigger();
   const int32_t live = offsets ? offset_at(offsets, d.num_experts, (int32_t)d.num_rows) : (int32_t)d.num_rows;
   const uint64_t entries = d.num_tokens * d.top_k;
-  const uint32_t lane = threadIdx.x & 31;
+  const uint32_t lane = threadIdx.x & 31, dim = d.dim;
   for (uint64_t i = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32; i < entries;
        i += (uint64_t)gridDim.x * (kThreads / 32)) {
     const uint64_t t = i / d.top_k;
     const int32_t p = place[i];
-    const bool in = p >= 0 && p < live;
+    const bool in = (uint32_t)p < (uint32_t)live;
     const float w = in ? (weights ? weights[i] : 1.0f) : 0.0f;
-    const bool writes = dy && p >= 0 && (uint64_t)p < d.num_rows;
+    const bool reads = dweights && in, writes = dy && (uint32_t)p < (uint64_t)d.num_rows;
+    const T *g0 = dout + t * d.ld_out, *y0 = y + (reads ? (uint64_t)(uint32_t)p * d.ld_y : 0);
+    T *dy0 = dy + (writes ? (uint64_t)(uint32_t)p * dim : 0);
     float dot = 0.0f;
-#pragma unroll 2
-    for (uint32_t c = lane * N; c < d.dim; c += 32 * N) {
-      const int n = min((int)(d.dim - c), N);
-      float g[N];
-      if (in) load_vec<T>(dout + t * d.ld_out + c, n, vec_out, g);
-      if (dweights && in) {
-        float v[N];
-        load_vec<T>(y + (uint64_t)p * d.ld_y + c, n, vec_y, v);
+    for (uint32_t c0 = lane * N; c0 < dim; c0 += 32 * N * kBatch) {
+      uint4 g[kBatch], v[kBatch];
 #pragma unroll
-        for (int q = 0; q < N; ++q) dot = fmaf(g[q], v[q], dot);
+      for (int u = 0; u < kBatch; ++u) {
+        const uint32_t c = c0 + u * 32 * N;
+        g[u] = v[u] = make_uint4(0, 0, 0, 0);
+        if (c < dim) {
+          const int n = min((int)(dim - c), N);
+          if (in) g[u] = load_piece<T, VEC>(g0 + c, n);
+          if (reads) v[u] = load_piece<T, VEC>(y0 + c, n);
+        }
       }
-      if (writes) {
 #pragma unroll
-        for (int q = 0; q < N; ++q) g[q] = in ? g[q] * w : 0.0f;
-        store_vec<T>(dy + (uint64_t)p * d.dim + c, n, vec_dy, g);
+      for (int u = 0; u < kBatch; ++u) {
+        const uint32_t c = c0 + u * 32 * N;
+        float a[N], b[N];
+        Vec<T>::unpack(g[u], a);
+        Vec<T>::unpack(v[u], b);
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+          dot = fmaf(a[q], b[q], dot);
+          a[q] = in ? a[q] * w : 0.0f;
+        }
+        if (writes && c < dim) store_piece<T, VEC>(dy0 + c, min((int)(dim - c), N), a);
       }
     }
     if (dweights) {
 #pragma unroll
       for (int s = 16; s; s >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, s);
-      if (lane == 0) dweights[i] = dot;
+      if (lane == 0) dweights[i] = reads ? dot : 0.0f;
     }
   }
 }
@@ -131,10 +161,10 @@ ntc_status forward(const ntc_combine_desc &d, const void *y, const int32_t *plac
   constexpr uint32_t N = Vec<T>::N;
   const uint64_t total = d.num_tokens * ((d.dim + N - 1) / N);
   const unsigned grid = (unsigned)std::min<uint64_t>((total + kThreads - 1) / kThreads, (uint64_t)sm_count() * 64);
-  return op_cuda(launch_pdl(k_combine<T>, grid, kThreads, 0, st, d, (const T *)y, place, weights, offsets,
-                            (const T *)residual, (T *)out, rows_are_vec(y, d.ld_y, sizeof(T)),
-                            rows_are_vec(out, d.ld_out, sizeof(T)),
-                            residual && rows_are_vec(residual, d.ld_residual, sizeof(T))),
+  const bool vec = d.dim % N == 0 && rows_are_vec(y, d.ld_y, sizeof(T)) && rows_are_vec(out, d.ld_out, sizeof(T)) &&
+                   (!residual || rows_are_vec(residual, d.ld_residual, sizeof(T)));
+  return op_cuda(launch_pdl(vec ? k_combine<T, true> : k_combine<T, false>, grid, kThreads, 0, st, d, (const T *)y, place,
+                            weights, offsets, (const T *)residual, (T *)out),
                  "ntc_combine");
 }
 
@@ -144,9 +174,10 @@ ntc_status backward(const ntc_combine_desc &d, const void *dout, const void *y, 
   const uint64_t entries = d.num_tokens * d.top_k;
   const unsigned grid =
       (unsigned)std::min<uint64_t>((entries + kThreads / 32 - 1) / (kThreads / 32), (uint64_t)sm_count() * 64);
-  return op_cuda(launch_pdl(k_combine_back<T>, grid, kThreads, 0, st, d, (const T *)dout, (const T *)y, place, weights,
-                            offsets, (T *)dy, dweights, y && rows_are_vec(y, d.ld_y, sizeof(T)),
-                            rows_are_vec(dout, d.ld_out, sizeof(T)), dy && rows_are_vec(dy, d.dim, sizeof(T))),
+  const bool vec = d.dim % Vec<T>::N == 0 && rows_are_vec(dout, d.ld_out, sizeof(T)) &&
+                   (!dweights || rows_are_vec(y, d.ld_y, sizeof(T))) && (!dy || rows_are_vec(dy, d.dim, sizeof(T)));
+  return op_cuda(launch_pdl(vec ? k_combine_back<T, true> : k_combine_back<T, false>, grid, kThreads, 0, st, d,
+                            (const T *)dout, (const T *)y, place, weights, offsets, (T *)dy, dweights),
                  "ntc_combine_backward");
 }
 

@@ -258,6 +258,21 @@ struct Tiles {
 
 // ------------------------------------------------------------ epilogue
 
+// The normal distribution function Phi(z), and e = exp(-z^2 / 2), which its density
+// shares: erf by Abramowitz and Stegun, formula 7.1.26 (absolute error 1.5e-7, so
+// Phi's is below 1e-7, less than one rounding to bf16 or fp16 of anything above 2^-13).
+// Fewer instructions than erff and expf, which bound k_dz.
+__device__ __forceinline__ float normal_cdf(float z, float &e) {
+  e = __expf(-0.5f * z * z);
+  const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
+  float q = fmaf(1.061405429f, t, -1.453152027f);
+  q = fmaf(q, t, 1.421413741f);
+  q = fmaf(q, t, -0.284496736f);
+  q = fmaf(q, t, 0.254829592f);
+  q *= 0.5f * t * e;  // the upper tail of |z|
+  return z < 0.0f ? q : 1.0f - q;
+}
+
 __device__ __forceinline__ void activate(uint32_t act, float slope, float (&v)[8]) {
   if (act == NTC_ACT_RELU) {
 #pragma unroll
@@ -267,7 +282,10 @@ __device__ __forceinline__ void activate(uint32_t act, float slope, float (&v)[8
     for (int i = 0; i < 8; ++i) v[i] = v[i] > 0.0f ? v[i] : slope * v[i];
   } else if (act == NTC_ACT_GELU) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = 0.5f * v[i] * (1.0f + erff(v[i] * 0.70710678f));
+    for (int i = 0; i < 8; ++i) {
+      float e;
+      v[i] *= normal_cdf(v[i], e);
+    }
   } else if (act == NTC_ACT_SILU) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __fdividef(v[i], 1.0f + __expf(-v[i]));
@@ -650,11 +668,14 @@ __device__ __forceinline__ float act_slope(uint32_t act, float slope, float z) {
   switch (act) {
     case NTC_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
     case NTC_ACT_LEAKY: return z > 0.0f ? 1.0f : slope;
-    case NTC_ACT_GELU:
-      return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * expf(-0.5f * z * z);
+    case NTC_ACT_GELU: {
+      float e;
+      const float p = normal_cdf(z, e);
+      return fmaf(z * 0.39894228f, e, p);
+    }
     case NTC_ACT_SILU: {
-      const float s = 1.0f / (1.0f + expf(-z));
-      return s * (1.0f + z * (1.0f - s));
+      const float s = __fdividef(1.0f, 1.0f + __expf(-z));
+      return s * fmaf(z, 1.0f - s, 1.0f);
     }
     default: return 1.0f;
   }
@@ -668,7 +689,6 @@ struct DzArgs {
   uint64_t ld_dy, ld_z;
   uint32_t num_experts, num_rows, width, pitch, activation;
   float slope;
-  uint32_t bf16, vec_dy, vec_z;
 };
 
 constexpr int kDzThreads = 256;
@@ -680,7 +700,10 @@ struct TableShared {
 };
 
 // dz = dy act'(z), rounded for the two products, and its column sums per row
-// tile before that rounding.  One pass over dy and z, HBM-bound.
+// tile before that rounding.  One pass over dy and z, HBM-bound: a warp has four
+// rows' loads in flight.  VEC: every row of dy and z starts on 16 bytes and ends on
+// a whole piece of 8.
+template <typename T, bool VEC>
 __global__ void __launch_bounds__(kDzThreads) k_dz(const DzArgs a) {
   extern __shared__ uint8_t raw[];
   TableShared &s = *reinterpret_cast<TableShared *>(raw);
@@ -692,24 +715,47 @@ __global__ void __launch_bounds__(kDzThreads) k_dz(const DzArgs a) {
   const uint32_t col = blockIdx.x * kDzCols + lane * 8;
   const int n = min(8, (int)a.width - (int)col);
   const uint32_t total = s.tile[a.num_experts];
+  const bool acts = a.activation != NTC_ACT_NONE;
+  const T *dy = (const T *)a.dy + col, *z = (const T *)a.z + col;
+  T *dz = a.dz ? (T *)a.dz + col : nullptr;
   for (uint32_t q = blockIdx.y; q < total; q += gridDim.y) {
     const uint32_t e = bucket_of_tile(s.tile, a.num_experts, q);
     const uint32_t row = (uint32_t)s.off[e] + (q - s.tile[e]) * kRows;
     const uint32_t rows = min(kRows, (uint32_t)s.off[e + 1] - row);
     float sum[8] = {};
     if (n > 0) {
-#pragma unroll 4
-      for (uint32_t r = warp; r < rows; r += 8) {
-        float g[8], z[8];
-        load8(a.dy, (uint64_t)(row + r) * a.ld_dy + col, n, a.vec_dy, a.bf16, g);
-        if (a.activation != NTC_ACT_NONE) {
-          load8(a.z, (uint64_t)(row + r) * a.ld_z + col, n, a.vec_z, a.bf16, z);
+      for (uint32_t r0 = warp; r0 < rows; r0 += 32) {
+        uint4 qg[4], qz[4];
+        if constexpr (VEC) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) g[i] *= act_slope(a.activation, a.slope, z[i]);
+          for (uint32_t u = 0; u < 4; ++u) {
+            qg[u] = qz[u] = make_uint4(0, 0, 0, 0);
+            if (r0 + 8 * u < rows) {
+              qg[u] = *reinterpret_cast<const uint4 *>(dy + (uint64_t)(row + r0 + 8 * u) * a.ld_dy);
+              if (acts) qz[u] = *reinterpret_cast<const uint4 *>(z + (uint64_t)(row + r0 + 8 * u) * a.ld_z);
+            }
+          }
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += g[i];
-        if (a.dz) store8(a.dz, (uint64_t)(row + r) * a.pitch + col, 8, true, a.bf16, g);  // pads: 0
+        for (uint32_t u = 0; u < 4; ++u) {
+          const uint32_t r = r0 + 8 * u;
+          if (r >= rows) break;
+          float g[8], v[8];
+          if constexpr (VEC) {
+            Vec<T>::unpack(qg[u], g);
+            Vec<T>::unpack(qz[u], v);
+          } else {
+            load_vec<T>(dy + (uint64_t)(row + r) * a.ld_dy, n, false, g);
+            if (acts) load_vec<T>(z + (uint64_t)(row + r) * a.ld_z, n, false, v);
+          }
+          if (acts) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) g[i] *= act_slope(a.activation, a.slope, v[i]);
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sum[i] += i < n ? g[i] : 0.0f;
+          if (dz) store_vec<T>(dz + (uint64_t)(row + r) * a.pitch, 8, true, g);  // the pads' values are never read
+        }
       }
     }
     if (a.part) {
@@ -1072,13 +1118,13 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
     k.pitch = (uint32_t)round8(d.out_dim);
     k.activation = d.activation;
     k.slope = d.leaky_slope;
-    k.bf16 = d.type == NTC_TYPE_BF16;
-    k.vec_dy = rows_are_vec(dy, d.ld_y, 2);
-    k.vec_z = z && rows_are_vec(z, d.ld_z, 2);
+    const bool vec = d.out_dim % 8 == 0 && rows_are_vec(dy, d.ld_y, 2) && (!z || rows_are_vec(z, d.ld_z, 2));
     const unsigned cols = (d.out_dim + kDzCols - 1) / kDzCols;
     const unsigned high = (unsigned)std::min<uint64_t>(row_tiles_bound(d.num_rows, d.num_experts),
                                                        std::max(1u, (unsigned)sm_count() * 8 / cols));
-    e = launch_pdl(k_dz, dim3(cols, high), kDzThreads, sizeof(TableShared), st, k);
+    const auto kernel = d.type == NTC_TYPE_BF16 ? (vec ? k_dz<__nv_bfloat16, true> : k_dz<__nv_bfloat16, false>)
+                                                : (vec ? k_dz<__half, true> : k_dz<__half, false>);
+    e = launch_pdl(kernel, dim3(cols, high), kDzThreads, sizeof(TableShared), st, k);
     if (e == cudaSuccess && db)
       e = launch_pdl(k_db, dim3((d.out_dim + 31) / 32, std::min(d.num_experts, 1024u)), kDzThreads, sizeof(TableShared), st,
                      (const float *)part, offsets, d.num_experts, (uint32_t)d.num_rows, d.out_dim, k.pitch, db);
