@@ -5,7 +5,10 @@
 //                  from them every chunk's first position of every expert
 //   k_order_place  each entry's position: its chunk's first plus its rank, which a
 //                  warp finds with __match_any_sync and the warps' counts before it
-// Nothing waits on another CTA.  Up to kOneCta entries one CTA does all of it.
+// Nothing waits on another CTA.  Up to kOneCta entries one CTA does all of it; up to
+// kFewChunks chunks every CTA of k_order_place sums the counts itself, in the time
+// of one pass over them, and k_order_scan (8 to 11 us at 64 chunks of 257 counts) is
+// not launched.
 // Reads 4 bytes and writes 8 an entry; at the sizes in use launches are the cost.
 #include "experts.cuh"
 
@@ -13,10 +16,11 @@ using namespace ntc;
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 1024;
 constexpr int kOrderWarps = kThreads / 32;
 constexpr uint32_t kChunk = 4096;   // entries of one CTA
 constexpr uint32_t kOneCta = 4096;  // up to here one launch does it all
+constexpr uint32_t kFewChunks = 128;
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
 __device__ __forceinline__ uint32_t bucket_of(int32_t id, uint32_t E) { return (uint32_t)id < E ? (uint32_t)id : E; }
@@ -155,15 +159,41 @@ __global__ void __launch_bounds__(kThreads)
   }
 }
 
+// firsts: every chunk's first position of each bucket or, when `offsets` is given,
+// every chunk's counts: then this CTA sums them, and the first CTA writes offsets.
 __global__ void __launch_bounds__(kThreads)
-    k_order_place(const int32_t *ids, uint32_t n, uint32_t top_k, uint32_t E, const uint32_t *firsts, int32_t *rows,
-                  int32_t *place) {
+    k_order_place(const int32_t *ids, uint32_t n, uint32_t top_k, uint32_t E, const uint32_t *firsts, uint32_t chunks,
+                  int32_t *rows, int32_t *place, int32_t *offsets) {
   extern __shared__ uint32_t sh[];
-  const uint32_t begin = blockIdx.x * kChunk, end = min(begin + kChunk, n);
-  const uint32_t *first = firsts + (size_t)blockIdx.x * (E + 1);
+  __shared__ uint32_t sums[kOrderWarps];
+  const uint32_t B = E + 1, begin = blockIdx.x * kChunk, end = min(begin + kChunk, n);
+  uint32_t *first = sh + kOrderWarps * B;
   pdl_wait();
   pdl_trigger();
-  place_chunk(ids, begin, end, top_k, E, sh, rows, place, [&](uint32_t b) { return ld_word(first + b); });
+  uint32_t base = 0;
+  for (uint32_t b0 = 0; b0 < B; b0 += kThreads) {
+    const uint32_t b = b0 + threadIdx.x;
+    if (!offsets) {
+      if (b < B) first[b] = ld_word(firsts + (size_t)blockIdx.x * B + b);
+      continue;
+    }
+    uint32_t all = 0, before = 0, total;
+    if (b < B) {
+#pragma unroll 16
+      for (uint32_t c = 0; c < chunks; ++c) {
+        const uint32_t v = firsts[(size_t)c * B + b];
+        all += v;
+        before += c < blockIdx.x ? v : 0u;
+      }
+    }
+    const uint32_t at = base + cta_scan(all, sums, total);
+    if (b < B) {
+      first[b] = at + before;
+      if (blockIdx.x == 0) offsets[b] = (int32_t)at;
+    }
+    base += total;
+  }
+  place_chunk(ids, begin, end, top_k, E, sh, rows, place, [&](uint32_t b) { return first[b]; });
 }
 
 // More than 48 KB of shared memory has to be asked for, once per device and kernel.
@@ -206,11 +236,13 @@ extern "C" NTC_API ntc_status ntc_expert_order(const int32_t *ids, size_t n, uin
   }
   uint32_t *counts = (uint32_t *)workspace;
   const uint32_t chunks = (N + kChunk - 1) / kChunk;
-  const size_t smem = (size_t)kOrderWarps * B * 4;
+  const size_t smem = (size_t)(kOrderWarps + 1) * B * 4;
+  const bool few = chunks <= kFewChunks;
   e = allow(k_order_place, smem);
   if (e == cudaSuccess) e = launch_pdl(k_order_count, chunks, kThreads, (size_t)B * 4, st, ids, N, E, counts);
-  if (e == cudaSuccess) e = launch_pdl(k_order_scan, 1, kThreads, 0, st, counts, chunks, E, offsets);
+  if (e == cudaSuccess && !few) e = launch_pdl(k_order_scan, 1, kThreads, 0, st, counts, chunks, E, offsets);
   if (e == cudaSuccess)
-    e = launch_pdl(k_order_place, chunks, kThreads, smem, st, ids, N, top_k, E, (const uint32_t *)counts, rows, place);
+    e = launch_pdl(k_order_place, chunks, kThreads, smem, st, ids, N, top_k, E, (const uint32_t *)counts, chunks, rows,
+                   place, few ? offsets : (int32_t *)nullptr);
   return op_cuda(e, "ntc_expert_order");
 }

@@ -4,11 +4,18 @@
 //   best top_groups groups (a group's value: the sum of its two largest c);
 //   w_j = scale * s_j / (renormalize ? sum_i s_i : 1)
 //
-// One warp per token; lane i holds the V consecutive experts from i * V on in
-// registers, so the row is read once, with vector loads, and a lower lane always
-// has the lower indices: ties need no index comparison.  The choice goes by
-// order-preserving integer keys of c (0 = masked out): redux.sync finds the
-// warp's maximum in one instruction where floats would need five shuffles.
+// G lanes (8, 16 or a whole warp) have a token; lane i of them holds the V
+// consecutive experts from i * V on in registers, so the row is read once, with
+// vector loads, and a lower lane always has the lower indices: ties need no index
+// comparison between lanes.  The choice goes by order-preserving integer keys of c
+// (0 = masked out).  Reading the row is cheap; instructions are the bound:
+//   - up to V = 8 each lane ranks its own keys (28 comparisons), puts them in shared
+//     memory in descending order and keeps the order's indices in one register;
+//     every choice then compares heads only: one reduction, one ballot;
+//   - a token of few experts has 8 or 16 lanes, so that a warp's instructions serve
+//     two or four tokens.
+// 32,768 tokens, 256 experts, top 8 of 4 of 8 groups, sigmoid and bias, bf16: 50.6 us
+// with a search of all registers per choice.
 #include "experts.cuh"
 
 using namespace ntc;
@@ -34,13 +41,7 @@ __device__ __forceinline__ bool live_logit(float &l) {
   return live;
 }
 
-__device__ __forceinline__ float sigmoid(float l) { return 1.0f / (1.0f + expf(-l)); }
-
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int s = 16; s; s >>= 1) v += __shfl_xor_sync(kAll, v, s);
-  return v;
-}
+__device__ __forceinline__ float sigmoid(float l) { return __fdividef(1.0f, 1.0f + expf(-l)); }
 
 // V consecutive elements from p on, n of them inside the row.
 template <typename T, int V>
@@ -75,11 +76,41 @@ __device__ __forceinline__ void load_run(const T *p, int n, bool vec, float (&l)
   }
 }
 
-// Clears the keys of the experts outside the kept groups.
-template <int V>
-__device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const ntc_route_desc &d, uint32_t lane) {
+// Reductions over the G lanes of a token (whole groups of a converged warp).
+template <int G>
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  if constexpr (G == 32) return __reduce_max_sync(kAll, v);
+#pragma unroll
+  for (int s = G / 2; s; s >>= 1) v = max(v, __shfl_xor_sync(kAll, v, s));
+  return v;
+}
+template <int G>
+__device__ __forceinline__ uint32_t group_add(uint32_t v) {
+  if constexpr (G == 32) return __reduce_add_sync(kAll, v);
+#pragma unroll
+  for (int s = G / 2; s; s >>= 1) v += __shfl_xor_sync(kAll, v, s);
+  return v;
+}
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int s = G / 2; s; s >>= 1) v += __shfl_xor_sync(kAll, v, s);
+  return v;
+}
+// The lowest lane of the token's G for which `is` holds (G where none).
+template <int G>
+__device__ __forceinline__ uint32_t group_first(bool is, uint32_t lane) {
+  uint32_t b = __ballot_sync(kAll, is);
+  if constexpr (G < 32) b = (b >> (lane & ~(uint32_t)(G - 1))) & ((1u << G) - 1);
+  return b ? __ffs(b) - 1 : G;
+}
+
+// Clears the keys of the experts outside the kept groups.  sub: the lane's place
+// among the token's G.
+template <int V, int G>
+__device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const ntc_route_desc &d, uint32_t lane, uint32_t sub) {
   const uint32_t per = d.num_experts / d.num_groups;
-  const uint32_t e0 = lane * V;
+  const uint32_t e0 = sub * V;
   uint32_t mine = 0;  // lane g: the key of group g's value
   if (per % V == 0 && ((per / V) & (per / V - 1)) == 0) {
     // a group is the registers of per / V neighbouring lanes
@@ -95,55 +126,70 @@ __device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const ntc_route_
       a = max(a, oa);
     }
     const uint32_t v = a ? key_of(value_of(a) + (b ? value_of(b) : 0.0f)) : 0u;
-    mine = __shfl_sync(kAll, v, min(lane * (per / V), 31u));
-    if (lane >= d.num_groups) mine = 0;
+    mine = __shfl_sync(kAll, v, min(sub * (per / V), (uint32_t)G - 1), G);
+    if (sub >= d.num_groups) mine = 0;
   } else {
     for (uint32_t g = 0; g < d.num_groups; ++g) {
       uint32_t a = 0, b = 0, many = 0;
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (e0 + i >= g * per && e0 + i < (g + 1) * per) a = max(a, key[i]);
-      a = __reduce_max_sync(kAll, a);
+      a = group_max<G>(a);
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (e0 + i >= g * per && e0 + i < (g + 1) * per) {
           many += key[i] == a;
           if (key[i] < a) b = max(b, key[i]);
         }
-      many = __reduce_add_sync(kAll, many);
-      b = __reduce_max_sync(kAll, b);
+      many = group_add<G>(many);
+      b = group_max<G>(b);
       if (many > 1) b = a;
-      if (lane == g && a) mine = key_of(value_of(a) + (b ? value_of(b) : 0.0f));
+      if (sub == g && a) mine = key_of(value_of(a) + (b ? value_of(b) : 0.0f));
     }
   }
   uint32_t kept = 0;  // bit g: group g stays
   for (uint32_t r = 0; r < d.top_groups; ++r) {
-    const uint32_t m = __reduce_max_sync(kAll, mine);
-    if (m == 0) break;
-    const uint32_t g = __ffs(__ballot_sync(kAll, mine == m)) - 1;
-    kept |= 1u << g;
-    if (lane == g) mine = 0;
+    const uint32_t m = group_max<G>(mine);
+    const uint32_t g = group_first<G>(mine == m && m, lane);
+    if (g < G) kept |= 1u << g;
+    if (sub == g) mine = 0;
   }
+  if (per % V == 0) {
+    const bool keep = (kept >> min(e0 / per, 31u)) & 1;
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
-    const uint32_t g = min((e0 + i) / per, 31u);
-    if (!((kept >> g) & 1)) key[i] = 0;
+    for (int i = 0; i < V; ++i) key[i] = keep ? key[i] : 0u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (!((kept >> min((e0 + i) / per, 31u)) & 1)) key[i] = 0;
   }
 }
 
-template <typename T, int V>
+template <typename T, int V, int G>
 __global__ void __launch_bounds__(kWarps * 32)
-    k_route(ntc_route_desc d, uint64_t n, const T *logits, uint64_t ld, const float *bias, int32_t *ids, float *weights,
-            bool vec) {
-  const uint32_t lane = threadIdx.x & 31;
-  const uint32_t e0 = lane * V;
+    k_route(const ntc_route_desc d, uint64_t n, const T *logits, uint64_t ld, const float *bias, int32_t *ids,
+            float *weights, bool vec) {
+  constexpr bool kSorted = V <= 8;
+  __shared__ uint32_t sorted[kSorted ? kWarps * 32 * V : 1];  // [warp][rank][lane]
+  __shared__ __align__(16) float score[kWarps * 32 * V];      // [warp][lane][V]
+  const uint32_t lane = threadIdx.x & 31, sub = lane & (G - 1), warp = threadIdx.x / 32;
+  const uint32_t e0 = sub * V;
   const int have = max(0, min(V, (int)d.num_experts - (int)e0));
+  const uint32_t k = d.top_k;
+  uint32_t *heads = sorted + (kSorted ? warp * 32 * V + lane : 0);
+  float *scores = score + warp * 32 * V;
   pdl_wait();
   pdl_trigger();
-  for (uint64_t t = (uint64_t)blockIdx.x * kWarps + threadIdx.x / 32; t < n; t += (uint64_t)gridDim.x * kWarps) {
+  float b[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) b[i] = bias && i < have ? bias[e0 + i] : 0.0f;
+  constexpr uint32_t kTokens = kWarps * 32 / G;  // of a CTA at a time
+  for (uint64_t t0 = (uint64_t)blockIdx.x * kTokens; t0 < n; t0 += (uint64_t)gridDim.x * kTokens) {
+    const uint64_t t = t0 + threadIdx.x / G;
+    const bool real = t < n;  // the lanes of no token go along with the others
     float s[V];
     uint32_t key[V];
-    load_run<T, V>(logits + t * ld + e0, have, vec, s);
+    load_run<T, V>(logits + (real ? t : t0) * ld + e0, have, vec, s);
     uint32_t live = 0;  // bit i: expert e0 + i is not masked
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -153,62 +199,84 @@ __global__ void __launch_bounds__(kWarps * 32)
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if ((live >> i) & 1) top = max(top, key_of(s[i]));
-      top = __reduce_max_sync(kAll, top);
-      const float m = value_of(top);  // unused when nothing is live
+      const float m = value_of(group_max<G>(top));  // unused when nothing is live
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         s[i] = (live >> i) & 1 ? expf(s[i] - m) : 0.0f;
         sum += s[i];
       }
-      sum = warp_sum(sum);
+      const float inverse = 1.0f / group_sum<G>(sum);
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[i] = (live >> i) & 1 ? s[i] / sum : 0.0f;
+      for (int i = 0; i < V; ++i) s[i] = (live >> i) & 1 ? s[i] * inverse : 0.0f;
     } else {
 #pragma unroll
       for (int i = 0; i < V; ++i) s[i] = (live >> i) & 1 ? sigmoid(s[i]) : 0.0f;
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float c = bias && i < have ? s[i] + bias[e0 + i] : s[i];
+      const float c = s[i] + b[i];
       key[i] = ((live >> i) & 1) && c == c ? key_of(c) : 0u;
     }
-    if (d.num_groups > 1) keep_groups<V>(key, d, lane);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < V; ++i) scores[lane * V + i] = s[i];
+    if (d.num_groups > 1) keep_groups<V, G>(key, d, lane, sub);
 
-    int32_t id = -1;   // lane j: the j-th choice
-    float sj = 0.0f;
-    for (uint32_t j = 0; j < d.top_k; ++j) {
-      uint32_t a = 0;
+    int32_t id = -1;  // lane j of the token: the j-th choice
+    if constexpr (kSorted) {
+      // this lane's keys in descending order, ties by index
+      uint32_t order = 0;  // 4 bits each: the indices in that order
 #pragma unroll
-      for (int i = 0; i < V; ++i) a = max(a, key[i]);
-      const uint32_t m = __reduce_max_sync(kAll, a);
-      if (m == 0) break;
-      const uint32_t src = __ffs(__ballot_sync(kAll, a == m)) - 1;
-      int32_t e = 0;
-      float v = 0.0f;
-      if (lane == src) {
-        bool found = false;
+      for (int i = 0; i < V; ++i) {
+        uint32_t rank = 0;
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (key[i] == m && !found) {
-            found = true;
-            key[i] = 0;
-            e = (int32_t)e0 + i;
-            v = s[i];
-          }
+        for (int j = 0; j < V; ++j)
+          if (j != i) rank += j < i ? key[j] >= key[i] : key[j] > key[i];
+        order |= (uint32_t)i << (4 * rank);
+        heads[rank * 32] = key[i];
       }
-      e = __shfl_sync(kAll, e, src);
-      v = __shfl_sync(kAll, v, src);
-      if (lane == j) id = e, sj = v;
+      uint32_t at = 0, head = heads[0];
+      for (uint32_t j = 0; j < k; ++j) {
+        const uint32_t m = group_max<G>(head);
+        const uint32_t src = group_first<G>(head == m && m, lane);
+        const int32_t e = __shfl_sync(kAll, (int32_t)(e0 + (order & 15)), src & (G - 1), G);
+        if (sub == j && src < G) id = e;
+        if (sub == src) {
+          order >>= 4;
+          head = ++at < V ? heads[at * 32] : 0u;
+        }
+      }
+    } else {
+      for (uint32_t j = 0; j < k; ++j) {
+        uint32_t a = 0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) a = max(a, key[i]);
+        const uint32_t m = group_max<G>(a);
+        if (m == 0) break;
+        const uint32_t src = group_first<G>(a == m, lane);
+        int32_t e = 0;
+        if (sub == src) {
+#pragma unroll
+          for (int i = V - 1; i >= 0; --i)
+            if (key[i] == m) e = i;
+#pragma unroll
+          for (int i = 0; i < V; ++i) key[i] = i == e ? 0u : key[i];
+        }
+        e = __shfl_sync(kAll, (int32_t)e0 + e, src);
+        if (sub == j) id = e;
+      }
     }
+    __syncwarp();
+    const float sj = id >= 0 ? scores[(lane - sub) * V + id] : 0.0f;
     float w = sj;
     if (d.renormalize) {
-      const float sum = warp_sum(sj);
+      const float sum = group_sum<G>(sj);
       w = sum > 0.0f ? sj / sum : 0.0f;
     }
-    if (lane < d.top_k) {
-      ids[t * d.top_k + lane] = id;
-      weights[t * d.top_k + lane] = w * d.scale;
+    if (real && sub < k) {
+      ids[t * k + sub] = id;
+      weights[t * k + sub] = w * d.scale;
     }
   }
 }
@@ -218,58 +286,64 @@ __global__ void __launch_bounds__(kWarps * 32)
 // elsewhere: the row's other logits cancel out and are not read.  A sigmoid's is
 // at the chosen ones only, too.  Without renormalization every logit of a softmax
 // has one: dl_e = sum over j with id_j = e of s_j dw_j, less s_e sum_j s_j dw_j.
-// One warp per token, lane j has choice j; a row of fp32 in shared memory takes
-// the chosen experts' values and leaves in 16-byte stores.
-template <typename T>
+// G lanes per token (8, or a warp where top_k or the experts are more), lane j has
+// choice j; a row of fp32 in shared memory takes the chosen experts' values and
+// leaves in 16-byte stores by all of the warp's lanes.
+template <typename T, int G>
 __global__ void __launch_bounds__(kWarps * 32)
-    k_route_back(ntc_route_desc d, uint64_t n, const T *logits, uint64_t ld, const int32_t *ids, const float *dweights,
-                 T *dlogits, bool vec) {
-  extern __shared__ float rows[];
+    k_route_back(const ntc_route_desc d, uint64_t n, const T *logits, uint64_t ld, const int32_t *ids,
+                 const float *dweights, T *dlogits, bool vec) {
+  extern __shared__ __align__(16) float rows[];
   constexpr int N = Vec<T>::N;
-  const uint32_t lane = threadIdx.x & 31, E = d.num_experts, pitch = (E + 3) / 4 * 4;
-  float *row = rows + (threadIdx.x / 32) * pitch;
+  constexpr uint32_t kTokens = 32 / G;  // of a warp at a time
+  const uint32_t lane = threadIdx.x & 31, sub = lane & (G - 1), E = d.num_experts, pitch = (E + 7) / 8 * 8, k = d.top_k;
+  float *all = rows + threadIdx.x / 32 * kTokens * pitch, *row = all + lane / G * pitch;
   const bool softmax = d.score == NTC_SCORE_SOFTMAX, dense = softmax && !d.renormalize;
   pdl_wait();
   pdl_trigger();
-  for (uint64_t t = (uint64_t)blockIdx.x * kWarps + threadIdx.x / 32; t < n; t += (uint64_t)gridDim.x * kWarps) {
-    const T *l = logits + t * ld;
-    for (uint32_t e = lane * 4; e < pitch; e += 128)
-      *reinterpret_cast<float4 *>(row + e) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    int32_t id = lane < d.top_k ? ids[t * d.top_k + lane] : -1;
+  for (uint64_t t0 = ((uint64_t)blockIdx.x * kWarps + threadIdx.x / 32) * kTokens; t0 < n;
+       t0 += (uint64_t)gridDim.x * kWarps * kTokens) {
+    const uint64_t t = t0 + lane / G;
+    const bool real = t < n;
+    const T *l = logits + (real ? t : t0) * ld;
+    int32_t id = real && sub < k ? ids[t * k + sub] : -1;
     if (id >= (int32_t)E) id = -1;
-    const float dw = id >= 0 ? dweights[t * d.top_k + lane] * d.scale : 0.0f;
+    for (uint32_t e = lane * 4; e < kTokens * pitch; e += 128)
+      *reinterpret_cast<float4 *>(all + e) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const float dw = id >= 0 ? dweights[t * k + sub] * d.scale : 0.0f;
     float lj = id >= 0 ? to_f<T>(l[id]) : -INFINITY;
     const bool live = live_logit(lj);
     float m = 0.0f, z = 1.0f;  // softmax: its maximum and sum, over the row or the chosen
     if (dense) {
       uint32_t top = 0;
-      for (uint32_t e = lane; e < E; e += 32) {
+      for (uint32_t e = sub; e < E; e += G) {
         float v = to_f<T>(l[e]);
         if (live_logit(v)) top = max(top, key_of(v));
       }
-      m = value_of(__reduce_max_sync(kAll, top));
+      m = value_of(group_max<G>(top));
       float sum = 0.0f;
-      for (uint32_t e = lane; e < E; e += 32) {
+      for (uint32_t e = sub; e < E; e += G) {
         float v = to_f<T>(l[e]);
         if (live_logit(v)) sum += expf(v - m);
       }
-      z = warp_sum(sum);
+      z = group_sum<G>(sum);
     } else if (softmax) {
-      m = value_of(__reduce_max_sync(kAll, live ? key_of(lj) : 0u));
+      m = value_of(group_max<G>(live ? key_of(lj) : 0u));
     }
     const float s = !live ? 0.0f : softmax ? expf(lj - m) / z : sigmoid(lj);
     float ds = dw;
     if (d.renormalize) {
-      const float sum = warp_sum(s), dot = warp_sum(dw * s);
+      const float sum = group_sum<G>(s), dot = group_sum<G>(dw * s);
       // softmax: s / sum is p, so s ds = p (dw - sum dw p); sigmoid: ds as it is
       ds = sum > 0.0f ? (dw - dot / sum) / sum : 0.0f;
     }
     float v = softmax ? s * ds : s * (1.0f - s) * ds;
-    const float dot = dense ? warp_sum(v) : 0.0f;
+    const float dot = dense ? group_sum<G>(v) : 0.0f;
     // a repeated id: its first lane has the sum, in the order of the lanes
-    const uint32_t same = __match_any_sync(kAll, id);
+    const uint32_t tag = id >= 0 ? (lane / G << 16) | (uint32_t)id : 0xFFFF0000u | lane;
+    const uint32_t same = __match_any_sync(kAll, tag);
     const bool first = (uint32_t)__ffs(same) - 1 == lane;
-    if (__any_sync(kAll, id >= 0 && !first)) {
+    if (__any_sync(kAll, !first)) {
       float sum = 0.0f;
       for (uint32_t j = 0; j < 32; ++j) {
         const float o = __shfl_sync(kAll, v, j);
@@ -280,20 +354,29 @@ __global__ void __launch_bounds__(kWarps * 32)
     __syncwarp();
     if (id >= 0 && first && live) row[id] = v;
     __syncwarp();
-    T *out = dlogits + t * E;
-    for (uint32_t e = lane * N; e < E; e += 32 * N) {
-      float f[N];
-      const int have = min((int)(E - e), N);
 #pragma unroll
-      for (int i = 0; i < N; ++i) f[i] = i < have ? row[e + i] : 0.0f;
-      if (dense) {
+    for (uint32_t j = 0; j < kTokens; ++j) {
+      if (t0 + j >= n) break;
+      const float mj = __shfl_sync(kAll, m, j * G), zj = __shfl_sync(kAll, z, j * G), dj = __shfl_sync(kAll, dot, j * G);
+      const T *lj = logits + (t0 + j) * ld;
+      T *out = dlogits + (t0 + j) * E;
+      for (uint32_t e = lane * N; e < E; e += 32 * N) {
+        float f[N];
+        const int have = min((int)(E - e), N);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-          float x = i < have ? to_f<T>(l[e + i]) : -INFINITY;
-          f[i] = live_logit(x) ? f[i] - expf(x - m) / z * dot : 0.0f;
+        for (int i = 0; i < N; i += 4) {
+          const float4 q = *reinterpret_cast<const float4 *>(all + j * pitch + e + i);  // pitch: a multiple of 8
+          f[i] = q.x, f[i + 1] = q.y, f[i + 2] = q.z, f[i + 3] = q.w;
         }
+        if (dense) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            float x = i < have ? to_f<T>(lj[e + i]) : -INFINITY;
+            f[i] = live_logit(x) ? f[i] - expf(x - mj) / zj * dj : 0.0f;
+          }
+        }
+        store_vec<T>(out + e, have, vec, f);
       }
-      store_vec<T>(out + e, have, vec, f);
     }
     __syncwarp();
   }
@@ -324,33 +407,53 @@ ntc_status check_groups(const ntc_route_desc *d) {
   return NTC_OK;
 }
 
-template <typename T, int V>
+template <typename T, int V, int G>
 cudaError_t launch(const ntc_route_desc &d, uint64_t n, const void *logits, uint64_t ld, const float *bias,
                    int32_t *ids, float *weights, cudaStream_t st) {
-  const unsigned grid = (unsigned)std::min<uint64_t>((n + kWarps - 1) / kWarps, (uint64_t)sm_count() * 64);
+  constexpr uint64_t kTokens = kWarps * 32 / G;
+  const unsigned grid = (unsigned)std::min<uint64_t>((n + kTokens - 1) / kTokens, (uint64_t)sm_count() * 16);
   constexpr size_t kRun = V * sizeof(T) < 16 ? V * sizeof(T) : 16;  // bytes of one load
   const bool vec = ((uintptr_t)logits % kRun) == 0 && (ld * sizeof(T)) % kRun == 0;
-  return launch_pdl(k_route<T, V>, grid, kWarps * 32, 0, st, d, n, (const T *)logits, ld, bias, ids, weights, vec);
+  return launch_pdl(k_route<T, V, G>, grid, kWarps * 32, 0, st, d, n, (const T *)logits, ld, bias, ids, weights, vec);
 }
 
+// Lanes per token: 8 up to 64 experts and 16 up to 128 where the choices and the
+// groups fit in as many lanes, else a warp.
 template <typename T>
 cudaError_t forward(const ntc_route_desc &d, uint64_t n, const void *logits, uint64_t ld, const float *bias,
                     int32_t *ids, float *weights, cudaStream_t st) {
-  if (d.num_experts <= 32) return launch<T, 1>(d, n, logits, ld, bias, ids, weights, st);
-  if (d.num_experts <= 64) return launch<T, 2>(d, n, logits, ld, bias, ids, weights, st);
-  if (d.num_experts <= 128) return launch<T, 4>(d, n, logits, ld, bias, ids, weights, st);
-  if (d.num_experts <= 256) return launch<T, 8>(d, n, logits, ld, bias, ids, weights, st);
-  if (d.num_experts <= 512) return launch<T, 16>(d, n, logits, ld, bias, ids, weights, st);
-  return launch<T, 32>(d, n, logits, ld, bias, ids, weights, st);
+  const uint32_t E = d.num_experts, lanes = std::max(d.top_k, d.num_groups);
+  if (lanes <= 8) {
+    if (E <= 8) return launch<T, 1, 8>(d, n, logits, ld, bias, ids, weights, st);
+    if (E <= 16) return launch<T, 2, 8>(d, n, logits, ld, bias, ids, weights, st);
+    if (E <= 32) return launch<T, 4, 8>(d, n, logits, ld, bias, ids, weights, st);
+    if (E <= 64) return launch<T, 8, 8>(d, n, logits, ld, bias, ids, weights, st);
+  }
+  if (lanes <= 16 && E > 32 && E <= 128) return launch<T, 8, 16>(d, n, logits, ld, bias, ids, weights, st);
+  if (E <= 32) return launch<T, 1, 32>(d, n, logits, ld, bias, ids, weights, st);
+  if (E <= 64) return launch<T, 2, 32>(d, n, logits, ld, bias, ids, weights, st);
+  if (E <= 128) return launch<T, 4, 32>(d, n, logits, ld, bias, ids, weights, st);
+  if (E <= 256) return launch<T, 8, 32>(d, n, logits, ld, bias, ids, weights, st);
+  if (E <= 512) return launch<T, 16, 32>(d, n, logits, ld, bias, ids, weights, st);
+  return launch<T, 32, 32>(d, n, logits, ld, bias, ids, weights, st);
 }
 
+template <typename T, int G>
+cudaError_t launch_back(const ntc_route_desc &d, uint64_t n, const void *logits, uint64_t ld, const int32_t *ids,
+                        const float *dweights, void *dlogits, cudaStream_t st) {
+  constexpr uint64_t kTokens = kWarps * 32 / G;
+  const unsigned grid = (unsigned)std::min<uint64_t>((n + kTokens - 1) / kTokens, (uint64_t)sm_count() * 16);
+  return launch_pdl(k_route_back<T, G>, grid, kWarps * 32, kTokens * ((d.num_experts + 7) / 8 * 8) * 4, st, d, n,
+                    (const T *)logits, ld, ids, dweights, (T *)dlogits, rows_are_vec(dlogits, d.num_experts, sizeof(T)));
+}
+
+// Eight lanes per token while its choices fit in them and four tokens' rows a warp
+// leave room for four CTAs on an SM.
 template <typename T>
 cudaError_t backward(const ntc_route_desc &d, uint64_t n, const void *logits, uint64_t ld, const int32_t *ids,
                      const float *dweights, void *dlogits, cudaStream_t st) {
-  const unsigned grid = (unsigned)std::min<uint64_t>((n + kWarps - 1) / kWarps, (uint64_t)sm_count() * 64);
-  return launch_pdl(k_route_back<T>, grid, kWarps * 32, (size_t)kWarps * ((d.num_experts + 3) / 4 * 4) * 4, st, d, n,
-                    (const T *)logits, ld, ids, dweights, (T *)dlogits,
-                    rows_are_vec(dlogits, d.num_experts, sizeof(T)));
+  if (d.top_k <= 8 && d.num_experts <= 512) return launch_back<T, 8>(d, n, logits, ld, ids, dweights, dlogits, st);
+  return launch_back<T, 32>(d, n, logits, ld, ids, dweights, dlogits, st);
 }
 
 }  // namespace
