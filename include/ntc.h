@@ -413,8 +413,9 @@ typedef enum { NTC_TYPE_FP32 = 0, NTC_TYPE_FP16 = 1, NTC_TYPE_BF16 = 2 } ntc_typ
  * value stay, ties to the lower group.  ids are the top_k experts of the largest
  * c, in descending order, ties to the lower index; weights are
  * scale * s_j / (renormalize ? sum of the chosen s : 1), without the bias.
- * A logit of -inf or NaN masks its expert out (s = 0, never chosen); +inf counts
- * as the largest finite value.  Where fewer than top_k experts are left, the
+ * A logit of -inf or NaN masks its expert out (s = 0, never chosen), a bias of
+ * -inf or NaN keeps it from being chosen; a logit of +inf counts as the largest
+ * finite value.  Where fewer than top_k experts are left, the
  * remaining ids are -1 and their weights 0; where the chosen s sum to 0 the
  * renormalized weights are 0.  Scores and sums are fp32. */
 typedef struct {

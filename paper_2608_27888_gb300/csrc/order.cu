@@ -1,14 +1,13 @@
 // The stable order of (token, slot) entries by expert: a counting sort.
 //
 //   k_order_count  the experts' counts of every chunk of kChunk entries
-//   k_order_scan   one CTA: each expert's total, the experts' first positions, and
-//                  from them every chunk's first position of every expert
-//   k_order_place  each entry's position: its chunk's first plus its rank, which a
-//                  warp finds with __match_any_sync and the warps' counts before it
-// Nothing waits on another CTA.  Up to kOneCta entries one CTA does all of it; up to
-// kFewChunks chunks every CTA of k_order_place sums the counts itself, in the time
-// of one pass over them, and k_order_scan (8 to 11 us at 64 chunks of 257 counts) is
-// not launched.
+//   k_order_scan   a warp per expert: its counts become the entries of it in the
+//                  chunks before each chunk, and its total
+//   k_order_place  the experts' first positions from the totals (every CTA for
+//                  itself), and each entry's position: its expert's first, the chunks'
+//                  before, and its rank in the chunk, which a warp finds by ballots
+//                  and the warps' counts before it
+// Nothing waits on another CTA.  Up to kOneCta entries one CTA does all of it.
 // Reads 4 bytes and writes 8 an entry; at the sizes in use launches are the cost.
 #include "experts.cuh"
 
@@ -16,11 +15,10 @@ using namespace ntc;
 
 namespace {
 
-constexpr int kThreads = 1024;
+constexpr int kThreads = 512;
 constexpr int kOrderWarps = kThreads / 32;
-constexpr uint32_t kChunk = 4096;   // entries of one CTA
+constexpr uint32_t kChunk = 2048;   // entries of one CTA
 constexpr uint32_t kOneCta = 4096;  // up to here one launch does it all
-constexpr uint32_t kFewChunks = 128;
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
 __device__ __forceinline__ uint32_t bucket_of(int32_t id, uint32_t E) { return (uint32_t)id < E ? (uint32_t)id : E; }
@@ -73,8 +71,15 @@ __device__ __forceinline__ void place_chunk(const int32_t *ids, uint32_t begin, 
   for (uint32_t i0 = a; i0 < z; i0 += 32) {
     const uint32_t i = i0 + lane;
     const bool in = i < z;
-    const uint32_t b = in ? bucket_of(ids[i], E) : 0xFFFFFFFFu;
-    const uint32_t same = __match_any_sync(kAll, b);
+    const uint32_t b = in ? bucket_of(ids[i], E) : B;
+    // the lanes of the same bucket, a ballot per bit of its number (__match_any_sync
+    // goes through the warp's distinct values one by one: 16.5 us instead of 9 at 256
+    // experts and 262,144 entries)
+    uint32_t same = kAll;
+    for (uint32_t bit = 1; bit <= B; bit <<= 1) {
+      const uint32_t with = __ballot_sync(kAll, b & bit);
+      same &= b & bit ? with : ~with;
+    }
     const uint32_t before = __popc(same & ((1u << lane) - 1));
     uint32_t at = 0;
     if (in) at = mine[b] + before;
@@ -117,9 +122,9 @@ __global__ void __launch_bounds__(kThreads)
   place_chunk(ids, 0, n, top_k, E, sh, rows, place, [&](uint32_t b) { return first[b]; });
 }
 
-// counts[chunk][bucket]
+// counts[bucket][pitch]: of every chunk
 __global__ void __launch_bounds__(kThreads)
-    k_order_count(const int32_t *ids, uint32_t n, uint32_t E, uint32_t *counts) {
+    k_order_count(const int32_t *ids, uint32_t n, uint32_t E, uint32_t *counts, uint32_t pitch) {
   extern __shared__ uint32_t sh[];
   const uint32_t B = E + 1, begin = blockIdx.x * kChunk, end = min(begin + kChunk, n);
   for (uint32_t b = threadIdx.x; b < B; b += kThreads) sh[b] = 0;
@@ -128,42 +133,43 @@ __global__ void __launch_bounds__(kThreads)
   pdl_trigger();
   for (uint32_t i = begin + threadIdx.x; i < end; i += kThreads) atomicAdd(&sh[bucket_of(ids[i], E)], 1u);
   __syncthreads();
-  for (uint32_t b = threadIdx.x; b < B; b += kThreads) counts[(size_t)blockIdx.x * B + b] = sh[b];
+  for (uint32_t b = threadIdx.x; b < B; b += kThreads) counts[(size_t)b * pitch + blockIdx.x] = sh[b];
 }
 
-// One CTA: counts[chunk][bucket] become each chunk's first position of each bucket.
-__global__ void __launch_bounds__(kThreads)
-    k_order_scan(uint32_t *counts, uint32_t chunks, uint32_t E, int32_t *offsets) {
-  __shared__ uint32_t sums[kOrderWarps];
-  const uint32_t B = E + 1;
+// One warp per bucket: exclusive sums along the chunks, four a lane, and the total.
+__global__ void __launch_bounds__(256)
+    k_order_scan(uint32_t *counts, uint32_t chunks, uint32_t pitch, uint32_t B, uint32_t *totals) {
+  const uint32_t b = blockIdx.x * 8 + threadIdx.x / 32, lane = threadIdx.x & 31;
   pdl_wait();
   pdl_trigger();
+  if (b >= B) return;
+  uint32_t *row = counts + (size_t)b * pitch;
   uint32_t base = 0;
-  for (uint32_t b0 = 0; b0 < B; b0 += kThreads) {
-    const uint32_t b = b0 + threadIdx.x;
-    uint32_t mine = 0, total;
-    if (b < B)
-#pragma unroll 8
-      for (uint32_t c = 0; c < chunks; ++c) mine += counts[(size_t)c * B + b];
-    uint32_t at = base + cta_scan(mine, sums, total);
-    if (b < B) {
-      offsets[b] = (int32_t)at;
-#pragma unroll 8
-      for (uint32_t c = 0; c < chunks; ++c) {
-        const uint32_t v = counts[(size_t)c * B + b];
-        counts[(size_t)c * B + b] = at;
-        at += v;
-      }
+  for (uint32_t c0 = 0; c0 < chunks; c0 += 128) {
+    const uint32_t c = c0 + lane * 4;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (c < pitch) v = *reinterpret_cast<const uint4 *>(row + c);
+    if (c + 0 >= chunks) v.x = 0;  // the pads hold anything
+    if (c + 1 >= chunks) v.y = 0;
+    if (c + 2 >= chunks) v.z = 0;
+    if (c + 3 >= chunks) v.w = 0;
+    const uint32_t mine = v.x + v.y + v.z + v.w;
+    uint32_t in = mine;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const uint32_t o = __shfl_up_sync(kAll, in, s);
+      if (lane >= (uint32_t)s) in += o;
     }
-    base += total;
+    const uint32_t at = base + in - mine;
+    if (c < pitch) *reinterpret_cast<uint4 *>(row + c) = make_uint4(at, at + v.x, at + v.x + v.y, at + v.x + v.y + v.z);
+    base += __shfl_sync(kAll, in, 31);
   }
+  if (lane == 0) totals[b] = base;
 }
 
-// firsts: every chunk's first position of each bucket or, when `offsets` is given,
-// every chunk's counts: then this CTA sums them, and the first CTA writes offsets.
 __global__ void __launch_bounds__(kThreads)
-    k_order_place(const int32_t *ids, uint32_t n, uint32_t top_k, uint32_t E, const uint32_t *firsts, uint32_t chunks,
-                  int32_t *rows, int32_t *place, int32_t *offsets) {
+    k_order_place(const int32_t *ids, uint32_t n, uint32_t top_k, uint32_t E, const uint32_t *before, uint32_t pitch,
+                  const uint32_t *totals, int32_t *rows, int32_t *place, int32_t *offsets) {
   extern __shared__ uint32_t sh[];
   __shared__ uint32_t sums[kOrderWarps];
   const uint32_t B = E + 1, begin = blockIdx.x * kChunk, end = min(begin + kChunk, n);
@@ -173,28 +179,20 @@ __global__ void __launch_bounds__(kThreads)
   uint32_t base = 0;
   for (uint32_t b0 = 0; b0 < B; b0 += kThreads) {
     const uint32_t b = b0 + threadIdx.x;
-    if (!offsets) {
-      if (b < B) first[b] = ld_word(firsts + (size_t)blockIdx.x * B + b);
-      continue;
-    }
-    uint32_t all = 0, before = 0, total;
+    const uint32_t chunks_before = b < B ? before[(size_t)b * pitch + blockIdx.x] : 0u;
+    uint32_t total;
+    const uint32_t at = base + cta_scan(b < B ? totals[b] : 0u, sums, total);
     if (b < B) {
-#pragma unroll 16
-      for (uint32_t c = 0; c < chunks; ++c) {
-        const uint32_t v = firsts[(size_t)c * B + b];
-        all += v;
-        before += c < blockIdx.x ? v : 0u;
-      }
-    }
-    const uint32_t at = base + cta_scan(all, sums, total);
-    if (b < B) {
-      first[b] = at + before;
+      first[b] = at + chunks_before;
       if (blockIdx.x == 0) offsets[b] = (int32_t)at;
     }
     base += total;
   }
   place_chunk(ids, begin, end, top_k, E, sh, rows, place, [&](uint32_t b) { return first[b]; });
 }
+
+// A row of counts: the chunks, a multiple of four.
+uint32_t count_pitch(size_t n) { return (uint32_t)(((n + kChunk - 1) / kChunk + 3) / 4 * 4); }
 
 // More than 48 KB of shared memory has to be asked for, once per device and kernel.
 template <typename K>
@@ -207,7 +205,7 @@ cudaError_t allow(K kernel, size_t bytes) {
 
 extern "C" NTC_API size_t ntc_expert_order_workspace(size_t n, uint32_t num_experts) {
   if (n > INT_MAX || num_experts < 1 || num_experts > NTC_MAX_EXPERTS || n <= kOneCta) return 0;
-  return (n + kChunk - 1) / kChunk * (num_experts + 1) * 4;
+  return ((size_t)count_pitch(n) + 1) * (num_experts + 1) * 4;
 }
 
 extern "C" NTC_API ntc_status ntc_expert_order(const int32_t *ids, size_t n, uint32_t top_k, uint32_t num_experts,
@@ -235,14 +233,14 @@ extern "C" NTC_API ntc_status ntc_expert_order(const int32_t *ids, size_t n, uin
     return op_cuda(e, "ntc_expert_order");
   }
   uint32_t *counts = (uint32_t *)workspace;
-  const uint32_t chunks = (N + kChunk - 1) / kChunk;
+  const uint32_t chunks = (N + kChunk - 1) / kChunk, pitch = count_pitch(n);
+  uint32_t *totals = counts + (size_t)pitch * B;
   const size_t smem = (size_t)(kOrderWarps + 1) * B * 4;
-  const bool few = chunks <= kFewChunks;
   e = allow(k_order_place, smem);
-  if (e == cudaSuccess) e = launch_pdl(k_order_count, chunks, kThreads, (size_t)B * 4, st, ids, N, E, counts);
-  if (e == cudaSuccess && !few) e = launch_pdl(k_order_scan, 1, kThreads, 0, st, counts, chunks, E, offsets);
+  if (e == cudaSuccess) e = launch_pdl(k_order_count, chunks, kThreads, (size_t)B * 4, st, ids, N, E, counts, pitch);
+  if (e == cudaSuccess) e = launch_pdl(k_order_scan, (B + 7) / 8, 256, 0, st, counts, chunks, pitch, B, totals);
   if (e == cudaSuccess)
-    e = launch_pdl(k_order_place, chunks, kThreads, smem, st, ids, N, top_k, E, (const uint32_t *)counts, chunks, rows,
-                   place, few ? offsets : (int32_t *)nullptr);
+    e = launch_pdl(k_order_place, chunks, kThreads, smem, st, ids, N, top_k, E, (const uint32_t *)counts, pitch,
+                   (const uint32_t *)totals, rows, place, offsets);
   return op_cuda(e, "ntc_expert_order");
 }

@@ -7,11 +7,12 @@
 // G lanes (8, 16 or a whole warp) have a token; lane i of them holds the V
 // consecutive experts from i * V on in registers, so the row is read once, with
 // vector loads, and a lower lane always has the lower indices: ties need no index
-// comparison between lanes.  The choice goes by order-preserving integer keys of c
-// (0 = masked out).  Reading the row is cheap; instructions are the bound:
-//   - up to V = 8 each lane ranks its own keys (28 comparisons), puts them in shared
-//     memory in descending order and keeps the order's indices in one register;
-//     every choice then compares heads only: one reduction, one ballot;
+// comparison between lanes.  A masked expert's choice value is -inf.  Reading the
+// row is cheap; instructions are the bound:
+//   - up to V = 8 each lane sorts its own values (minima and maxima, without indices)
+//     into shared memory; a choice then compares heads only: one reduction and one
+//     ballot.  Which of the lane's experts it was is found at the end, for all
+//     choices at once: lane j searches choice j's value;
 //   - a token of few experts has 8 or 16 lanes, so that a warp's instructions serve
 //     two or four tokens.
 // 32,768 tokens, 256 experts, top 8 of 4 of 8 groups, sigmoid and bias, bf16: 50.6 us
@@ -41,7 +42,7 @@ __device__ __forceinline__ bool live_logit(float &l) {
   return live;
 }
 
-__device__ __forceinline__ float sigmoid(float l) { return __fdividef(1.0f, 1.0f + expf(-l)); }
+__device__ __forceinline__ float sigmoid(float l) { return __fdividef(1.0f, 1.0f + __expf(-l)); }
 
 // V consecutive elements from p on, n of them inside the row.
 template <typename T, int V>
@@ -78,6 +79,17 @@ __device__ __forceinline__ void load_run(const T *p, int n, bool vec, float (&l)
 
 // Reductions over the G lanes of a token (whole groups of a converged warp).
 template <int G>
+__device__ __forceinline__ float group_max(float v) {
+  if constexpr (G == 32) {
+    float m;
+    asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;\n" : "=f"(m) : "f"(v));
+    return m;
+  }
+#pragma unroll
+  for (int s = G / 2; s; s >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, s));
+  return v;
+}
+template <int G>
 __device__ __forceinline__ uint32_t group_max(uint32_t v) {
   if constexpr (G == 32) return __reduce_max_sync(kAll, v);
 #pragma unroll
@@ -105,63 +117,108 @@ __device__ __forceinline__ uint32_t group_first(bool is, uint32_t lane) {
   return b ? __ffs(b) - 1 : G;
 }
 
-// Clears the keys of the experts outside the kept groups.  sub: the lane's place
-// among the token's G.
+// How the experts lie in groups, the same for every token.
+struct Grouping {
+  uint32_t groups, top, per, mine;  // experts per group; the group of this lane's experts
+  bool lanes;   // every lane's experts are of one group
+  bool blocks;  // and a group's lanes are a power of two
+};
+template <int V>
+__device__ __forceinline__ Grouping grouping(const ntc_route_desc &d, uint32_t sub) {
+  Grouping g;
+  g.groups = d.num_groups;
+  g.top = d.top_groups;
+  g.per = d.num_experts / d.num_groups;
+  g.mine = min(sub * V / g.per, 31u);
+  g.lanes = g.per % V == 0;
+  g.blocks = g.lanes && ((g.per / V) & (g.per / V - 1)) == 0;
+  return g;
+}
+
+// Masks the experts outside the kept groups.  sub: the lane's place among the
+// token's G.
 template <int V, int G>
-__device__ __forceinline__ void keep_groups(uint32_t (&key)[V], const ntc_route_desc &d, uint32_t lane, uint32_t sub) {
-  const uint32_t per = d.num_experts / d.num_groups;
-  const uint32_t e0 = sub * V;
-  uint32_t mine = 0;  // lane g: the key of group g's value
-  if (per % V == 0 && ((per / V) & (per / V - 1)) == 0) {
+__device__ __forceinline__ void keep_groups(float (&c)[V], const Grouping &gr, uint32_t lane, uint32_t sub) {
+  const uint32_t per = gr.per, e0 = sub * V;
+  float mine = -INFINITY;  // lane g: group g's value; a group of one live expert has that one's
+  const auto value = [](float a, float b) { return b > -INFINITY ? a + b : a; };
+  if (gr.blocks) {
     // a group is the registers of per / V neighbouring lanes
-    uint32_t a = 0, b = 0;  // the two largest keys
+    float a = c[0], b = -INFINITY;  // the two largest
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      b = max(b, min(a, key[i]));
-      a = max(a, key[i]);
+    for (int i = 1; i < V; ++i) {
+      b = fmaxf(b, fminf(a, c[i]));
+      a = fmaxf(a, c[i]);
     }
     for (uint32_t s = 1; s < per / V; s <<= 1) {
-      const uint32_t oa = __shfl_xor_sync(kAll, a, s), ob = __shfl_xor_sync(kAll, b, s);
-      b = max(min(a, oa), max(b, ob));
-      a = max(a, oa);
+      const float oa = __shfl_xor_sync(kAll, a, s), ob = __shfl_xor_sync(kAll, b, s);
+      b = fmaxf(fminf(a, oa), fmaxf(b, ob));
+      a = fmaxf(a, oa);
     }
-    const uint32_t v = a ? key_of(value_of(a) + (b ? value_of(b) : 0.0f)) : 0u;
-    mine = __shfl_sync(kAll, v, min(sub * (per / V), (uint32_t)G - 1), G);
-    if (sub >= d.num_groups) mine = 0;
+    mine = __shfl_sync(kAll, value(a, b), min(sub * (per / V), (uint32_t)G - 1), G);
+    if (sub >= gr.groups) mine = -INFINITY;
   } else {
-    for (uint32_t g = 0; g < d.num_groups; ++g) {
-      uint32_t a = 0, b = 0, many = 0;
+    for (uint32_t g = 0; g < gr.groups; ++g) {
+      float a = -INFINITY, b = -INFINITY;
+      uint32_t many = 0;
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        if (e0 + i >= g * per && e0 + i < (g + 1) * per) a = max(a, key[i]);
+        if (e0 + i >= g * per && e0 + i < (g + 1) * per) a = fmaxf(a, c[i]);
       a = group_max<G>(a);
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (e0 + i >= g * per && e0 + i < (g + 1) * per) {
-          many += key[i] == a;
-          if (key[i] < a) b = max(b, key[i]);
+          many += c[i] == a;
+          if (c[i] < a) b = fmaxf(b, c[i]);
         }
       many = group_add<G>(many);
       b = group_max<G>(b);
       if (many > 1) b = a;
-      if (sub == g && a) mine = key_of(value_of(a) + (b ? value_of(b) : 0.0f));
+      if (sub == g) mine = value(a, b);
     }
   }
   uint32_t kept = 0;  // bit g: group g stays
-  for (uint32_t r = 0; r < d.top_groups; ++r) {
-    const uint32_t m = group_max<G>(mine);
-    const uint32_t g = group_first<G>(mine == m && m, lane);
-    if (g < G) kept |= 1u << g;
-    if (sub == g) mine = 0;
+  for (uint32_t r = 0; r < gr.top; ++r) {
+    const float m = group_max<G>(mine);
+    const uint32_t g = group_first<G>(mine == m, lane);  // of the masked ones, too: that changes nothing
+    kept |= 1u << (g & 31);
+    if (sub == g) mine = -INFINITY;
   }
-  if (per % V == 0) {
-    const bool keep = (kept >> min(e0 / per, 31u)) & 1;
+  if (gr.lanes) {
+    const bool keep = (kept >> gr.mine) & 1;
 #pragma unroll
-    for (int i = 0; i < V; ++i) key[i] = keep ? key[i] : 0u;
+    for (int i = 0; i < V; ++i) c[i] = keep ? c[i] : -INFINITY;
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (!((kept >> min((e0 + i) / per, 31u)) & 1)) key[i] = 0;
+      if (!((kept >> min((e0 + i) / per, 31u)) & 1)) c[i] = -INFINITY;
+  }
+}
+
+// Descending order by minima and maxima (odd-even merges; V a power of two up to 8).
+template <int V>
+__device__ __forceinline__ void sort_down(float (&k)[V]) {
+  const auto order = [&](int i, int j) {
+    const float a = fmaxf(k[i], k[j]);
+    k[j] = fminf(k[i], k[j]);
+    k[i] = a;
+  };
+  if constexpr (V >= 2) {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) order(i, i + 1);
+  }
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      order(i, i + 2);
+      order(i + 1, i + 3);
+      order(i + 1, i + 2);
+    }
+  }
+  if constexpr (V >= 8) {
+    order(0, 4), order(1, 5), order(2, 6), order(3, 7);
+    order(2, 4), order(3, 5);
+    order(1, 2), order(3, 4), order(5, 6);
   }
 }
 
@@ -170,104 +227,122 @@ __global__ void __launch_bounds__(kWarps * 32)
     k_route(const ntc_route_desc d, uint64_t n, const T *logits, uint64_t ld, const float *bias, int32_t *ids,
             float *weights, bool vec) {
   constexpr bool kSorted = V <= 8;
-  __shared__ uint32_t sorted[kSorted ? kWarps * 32 * V : 1];  // [warp][rank][lane]
-  __shared__ __align__(16) float score[kWarps * 32 * V];      // [warp][lane][V]
+  constexpr int kHeads = V + 1;  // the last one: -inf
+  __shared__ float sorted[kSorted ? kWarps * 32 * kHeads : 1];        // [warp][rank][lane]
+  __shared__ __align__(16) float values[kSorted ? kWarps * 32 * V : 4];  // [warp][lane][V]
+  __shared__ __align__(16) float score[kWarps * 32 * V];              // [warp][lane][V]
   const uint32_t lane = threadIdx.x & 31, sub = lane & (G - 1), warp = threadIdx.x / 32;
   const uint32_t e0 = sub * V;
   const int have = max(0, min(V, (int)d.num_experts - (int)e0));
   const uint32_t k = d.top_k;
-  uint32_t *heads = sorted + (kSorted ? warp * 32 * V + lane : 0);
+  const bool softmax = d.score == NTC_SCORE_SOFTMAX;
+  const Grouping gr = grouping<V>(d, sub);
+  float *heads = sorted + (kSorted ? warp * 32 * kHeads + lane : 0);
+  float *all = values + (kSorted ? warp * 32 * V : 0);
   float *scores = score + warp * 32 * V;
+  if (kSorted) heads[V * 32] = -INFINITY;
   pdl_wait();
   pdl_trigger();
-  float b[V];
+  // the bias, and the logit that an expert has to exceed: -inf; +inf where the bias masks it
+  float b[V], least[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) b[i] = bias && i < have ? bias[e0 + i] : 0.0f;
+  for (int i = 0; i < V; ++i) {
+    b[i] = bias && i < have ? bias[e0 + i] : 0.0f;
+    least[i] = b[i] > -INFINITY ? -INFINITY : INFINITY;
+  }
   constexpr uint32_t kTokens = kWarps * 32 / G;  // of a CTA at a time
   for (uint64_t t0 = (uint64_t)blockIdx.x * kTokens; t0 < n; t0 += (uint64_t)gridDim.x * kTokens) {
     const uint64_t t = t0 + threadIdx.x / G;
     const bool real = t < n;  // the lanes of no token go along with the others
-    float s[V];
-    uint32_t key[V];
-    load_run<T, V>(logits + (real ? t : t0) * ld + e0, have, vec, s);
-    uint32_t live = 0;  // bit i: expert e0 + i is not masked
+    float l[V], s[V], c[V];
+    load_run<T, V>(logits + (real ? t : t0) * ld + e0, have, vec, l);
+    if (softmax) {
+      // a masked logit becomes -inf, whose score is 0 (fmaxf: NaN -> -inf)
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < have && live_logit(s[i])) live |= 1u << i;
-    if (d.score == NTC_SCORE_SOFTMAX) {
-      uint32_t top = 0;
+      for (int i = 0; i < V; ++i) l[i] = fminf(fmaxf(l[i], -INFINITY), 3.402823466e38f);
+      float top = l[0];
 #pragma unroll
-      for (int i = 0; i < V; ++i)
-        if ((live >> i) & 1) top = max(top, key_of(s[i]));
-      const float m = value_of(group_max<G>(top));  // unused when nothing is live
+      for (int i = 1; i < V; ++i) top = fmaxf(top, l[i]);
+      const float m = fmaxf(group_max<G>(top), -3.402823466e38f);
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        s[i] = (live >> i) & 1 ? expf(s[i] - m) : 0.0f;
+        s[i] = __expf(l[i] - m);
         sum += s[i];
       }
-      const float inverse = 1.0f / group_sum<G>(sum);
+      sum = group_sum<G>(sum);
+      const float inverse = sum > 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[i] = (live >> i) & 1 ? s[i] * inverse : 0.0f;
+      for (int i = 0; i < V; ++i) s[i] *= inverse;
     } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[i] = (live >> i) & 1 ? sigmoid(s[i]) : 0.0f;
+      for (int i = 0; i < V; ++i) s[i] = sigmoid(l[i]);
     }
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float c = s[i] + b[i];
-      key[i] = ((live >> i) & 1) && c == c ? key_of(c) : 0u;
-    }
-    __syncwarp();
+    for (int i = 0; i < V; ++i) c[i] = l[i] > least[i] ? s[i] + b[i] : -INFINITY;
+    if (gr.groups > 1) keep_groups<V, G>(c, gr, lane, sub);
+    __syncwarp();  // the last token's reads of shared memory
 #pragma unroll
     for (int i = 0; i < V; ++i) scores[lane * V + i] = s[i];
-    if (d.num_groups > 1) keep_groups<V, G>(key, d, lane, sub);
 
     int32_t id = -1;  // lane j of the token: the j-th choice
     if constexpr (kSorted) {
-      // this lane's keys in descending order, ties by index
-      uint32_t order = 0;  // 4 bits each: the indices in that order
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        uint32_t rank = 0;
+      for (int i = 0; i < V; ++i) all[lane * V + i] = c[i];
+      sort_down<V>(c);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-          if (j != i) rank += j < i ? key[j] >= key[i] : key[j] > key[i];
-        order |= (uint32_t)i << (4 * rank);
-        heads[rank * 32] = key[i];
-      }
-      uint32_t at = 0, head = heads[0];
+      for (int i = 1; i < V; ++i) heads[i * 32] = c[i];
+      int at = 0;
+      float head = c[0];
+      uint32_t from = 0;  // lane j: the lane that had choice j, and its value
+      float what = -INFINITY;
       for (uint32_t j = 0; j < k; ++j) {
-        const uint32_t m = group_max<G>(head);
-        const uint32_t src = group_first<G>(head == m && m, lane);
-        const int32_t e = __shfl_sync(kAll, (int32_t)(e0 + (order & 15)), src & (G - 1), G);
-        if (sub == j && src < G) id = e;
+        const float m = group_max<G>(head);
+        const uint32_t src = group_first<G>(head == m, lane);
+        if (sub == j) from = src, what = m;
         if (sub == src) {
-          order >>= 4;
-          head = ++at < V ? heads[at * 32] : 0u;
+          at = min(at + 1, V);
+          head = heads[at * 32];
         }
+      }
+      __syncwarp();
+      // equal values of one lane follow one another: how many choices before this one
+      // were such, by the last choice that was not
+      const uint32_t from_before = __shfl_up_sync(kAll, from, 1);
+      const float what_before = __shfl_up_sync(kAll, what, 1);
+      const bool same = sub > 0 && from_before == from && what_before == what;
+      uint32_t left = 0;
+      if (__any_sync(kAll, same)) {
+        const uint32_t starts = __ballot_sync(kAll, !same) & (kAll >> (31 - lane));
+        left = lane - (31 - __clz(starts));
+      }
+      if (what > -INFINITY) {
+        const float *theirs = all + (lane - sub + from) * V;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (theirs[i] == what && left-- == 0) id = (int32_t)(from * V) + i;
       }
     } else {
       for (uint32_t j = 0; j < k; ++j) {
-        uint32_t a = 0;
+        float a = c[0];
 #pragma unroll
-        for (int i = 0; i < V; ++i) a = max(a, key[i]);
-        const uint32_t m = group_max<G>(a);
-        if (m == 0) break;
+        for (int i = 1; i < V; ++i) a = fmaxf(a, c[i]);
+        const float m = group_max<G>(a);
+        if (!(m > -INFINITY)) break;
         const uint32_t src = group_first<G>(a == m, lane);
         int32_t e = 0;
         if (sub == src) {
 #pragma unroll
           for (int i = V - 1; i >= 0; --i)
-            if (key[i] == m) e = i;
+            if (c[i] == m) e = i;
 #pragma unroll
-          for (int i = 0; i < V; ++i) key[i] = i == e ? 0u : key[i];
+          for (int i = 0; i < V; ++i) c[i] = i == e ? -INFINITY : c[i];
         }
         e = __shfl_sync(kAll, (int32_t)e0 + e, src);
         if (sub == j) id = e;
       }
+      __syncwarp();
     }
-    __syncwarp();
     const float sj = id >= 0 ? scores[(lane - sub) * V + id] : 0.0f;
     float w = sj;
     if (d.renormalize) {

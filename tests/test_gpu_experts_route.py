@@ -190,3 +190,31 @@ def test_empty_route(ntc):
     ids, w = ntc.route(l, 2)
     assert ids.shape == (0, 2) and w.shape == (0, 2)
     assert ntc.route_backward(l, ids, w).shape == (0, 16)
+
+
+@pytest.mark.parametrize("E", [16, 100, 300])
+def test_a_bias_of_minus_infinity_or_nan_masks_an_expert(ntc, E):
+    l = apart(5, E, seed=3)
+    bias = torch.zeros(E)
+    bias[::3] = -math.inf
+    bias[1::3] = math.nan
+    ids, w = ntc.route(l.cuda(), 5, bias=bias.cuda(), score="sigmoid")
+    masked = l.clone()
+    masked[:, ::3] = -math.inf
+    masked[:, 1::3] = -math.inf
+    want_ids, want = R.route(masked, 5, None, "sigmoid")
+    assert torch.equal(ids.cpu(), want_ids)
+    check_weights(w, want, l)
+
+
+def test_equal_values_of_one_lane_in_any_number(ntc):
+    """Runs of equal values inside and across the lanes' shares of a row, with more choices than a share holds."""
+    g = torch.Generator().manual_seed(5)
+    for E in (8, 24, 64, 128, 200, 256):
+        for k in (4, 8, 9, 20):
+            if k > E:
+                continue
+            l = torch.randint(0, 3, (50, E), generator=g).float()
+            want, _ = R.route(l, k, None, "sigmoid")
+            ids, _ = ntc.route(l.cuda(), k, score="sigmoid")
+            assert torch.equal(ids.cpu(), want), (E, k)
