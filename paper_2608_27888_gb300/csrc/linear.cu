@@ -75,7 +75,8 @@ struct Args {
   uint32_t depth;      // contraction length (not kDw: there it is the expert's rows)
   uint32_t activation;
   float slope;
-  uint32_t bf16, vec_out, vec_z, vec_residual;
+  uint32_t bf16;
+  uint32_t vec_out;    // every row of out, z and residual is whole 16-byte pieces
   unsigned int *status;
 };
 
@@ -292,13 +293,21 @@ __device__ __forceinline__ void activate(uint32_t act, float slope, float (&v)[8
   }
 }
 
-__device__ __forceinline__ void load8(const void *p, uint64_t at, int n, bool vec, bool bf16, float (&v)[8]) {
-  if (bf16) load_vec<__nv_bfloat16>((const __nv_bfloat16 *)p + at, n, vec, v);
-  else load_vec<__half>((const __half *)p + at, n, vec, v);
+// Eight elements at a 16-byte boundary, and one anywhere.
+__device__ __forceinline__ void load8(const void *p, uint64_t at, bool bf16, float (&v)[8]) {
+  const uint4 q = *reinterpret_cast<const uint4 *>((const uint16_t *)p + at);
+  if (bf16) Vec<__nv_bfloat16>::unpack(q, v);
+  else Vec<__half>::unpack(q, v);
 }
-__device__ __forceinline__ void store8(void *p, uint64_t at, int n, bool vec, bool bf16, const float (&v)[8]) {
-  if (bf16) store_vec<__nv_bfloat16>((__nv_bfloat16 *)p + at, n, vec, v);
-  else store_vec<__half>((__half *)p + at, n, vec, v);
+__device__ __forceinline__ void store8(void *p, uint64_t at, bool bf16, const float (&v)[8]) {
+  *reinterpret_cast<uint4 *>((uint16_t *)p + at) = bf16 ? Vec<__nv_bfloat16>::pack(v) : Vec<__half>::pack(v);
+}
+__device__ __forceinline__ float load1(const void *p, uint64_t at, bool bf16) {
+  return bf16 ? to_f<__nv_bfloat16>(((const __nv_bfloat16 *)p)[at]) : to_f<__half>(((const __half *)p)[at]);
+}
+__device__ __forceinline__ void store1(void *p, uint64_t at, bool bf16, float v) {
+  if (bf16) ((__nv_bfloat16 *)p)[at] = from_f<__nv_bfloat16>(v);
+  else ((__half *)p)[at] = from_f<__half>(v);
 }
 
 // Offset of 16-byte piece c (0..3) of row r in a warp's staging, 64 bytes a row:
@@ -580,15 +589,24 @@ __global__ void __launch_bounds__(threads(MODE), 1)
                 v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
               }
             }
-            if (o.col + c0 + j < a.width) {
-              const uint64_t at = ((uint64_t)o.e * a.width + o.col + c0 + j) * a.ld_out + o.row + quarter * 32 + k0;
+            if (a.vec_out) {
+              if (o.col + c0 + j < a.width) {
+                const uint64_t at = ((uint64_t)o.e * a.width + o.col + c0 + j) * a.ld_out + o.row + quarter * 32 + k0;
 #pragma unroll
-              for (uint32_t q = 0; q < 2; ++q) {
-                const int n = min(8, high - (int32_t)(k0 + 8 * q));
-                float u[8];
+                for (uint32_t q = 0; q < 2; ++q) {
+                  float u[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
-                if (n > 0) store8(a.out, at + 8 * q, n, a.vec_out, bf16, u);
+                  for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
+                  if ((int32_t)(k0 + 8 * q) < high) store8(a.out, at + 8 * q, bf16, u);
+                }
+              }
+            } else {  // rows at odd addresses: a row's 32 values by 32 lanes
+#pragma unroll
+              for (uint32_t q = 0; q < 16; ++q) {
+                float x = 0.0f;
+                if (!zero) x = *reinterpret_cast<const float *>(mine + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4);
+                if (o.col + c0 + q < a.width && (int32_t)lane < high)
+                  store1(a.out, ((uint64_t)o.e * a.width + o.col + c0 + q) * a.ld_out + o.row + quarter * 32 + lane, bf16, x);
               }
             }
             __syncwarp();
@@ -602,13 +620,47 @@ __global__ void __launch_bounds__(threads(MODE), 1)
                            : "memory");
             __syncwarp();
           }
+          if (!a.vec_out) {
+            // rows at odd addresses: lanes on consecutive columns, two rows at a time
+            const uint32_t col = o.col + c0 + (lane & 15);
+            if (col < a.width) {
+              const float b = MODE == kForward && a.bias && !zero ? a.bias[(uint64_t)o.e * a.width + col] : 0.0f;
+              const int32_t r0 = lane >> 4;
+#pragma unroll
+              for (int32_t it = 0; it < 16; it += 8) {  // eight rows' loads, then eight rows' values
+                float v[8], x[8];
+#pragma unroll
+                for (int32_t i = 0; i < 8; ++i) {
+                  const int32_t rl = r0 + 2 * (it + i);
+                  x[i] = 0.0f;
+                  if (MODE == kForward && a.residual && !zero && rl < high)
+                    x[i] = load1(a.residual, (row0 + rl) * a.ld_residual + col, bf16);
+                  v[i] = zero ? 0.0f
+                              : *reinterpret_cast<const float *>(mine + staged(rl, (lane & 15) >> 2) + (lane & 3) * 4) + b;
+                }
+                if constexpr (MODE == kForward) {
+                  if (a.z) {
+#pragma unroll
+                    for (int32_t i = 0; i < 8; ++i)
+                      if (r0 + 2 * (it + i) < high) store1(a.z, (row0 + r0 + 2 * (it + i)) * a.ld_z + col, bf16, v[i]);
+                  }
+                  if (!zero) activate(a.activation, a.slope, v);
+                }
+#pragma unroll
+                for (int32_t i = 0; i < 8; ++i)
+                  if (r0 + 2 * (it + i) < high)
+                    store1(a.out, (row0 + r0 + 2 * (it + i)) * a.ld_out + col, bf16, v[i] + x[i]);
+              }
+            }
+            __syncwarp();
+            continue;
+          }
           const uint32_t col = o.col + c0 + (lane & 1) * 8;
-          const int n = min(8, (int)a.width - (int)col);
-          if (n > 0) {
+          if (col < a.width) {  // vec_out: whole pieces of 8 columns
             float b[8];
             if (MODE == kForward && a.bias && !zero) {
 #pragma unroll
-              for (int i = 0; i < 8; ++i) b[i] = i < n ? a.bias[(uint64_t)o.e * a.width + col + i] : 0.0f;
+              for (int i = 0; i < 8; ++i) b[i] = a.bias[(uint64_t)o.e * a.width + col + i];
             } else {
 #pragma unroll
               for (int i = 0; i < 8; ++i) b[i] = 0.0f;
@@ -628,18 +680,18 @@ __global__ void __launch_bounds__(threads(MODE), 1)
                   v[4] = g.x + b[4], v[5] = g.y + b[5], v[6] = g.z + b[6], v[7] = g.w + b[7];
                 }
                 if constexpr (MODE == kForward) {
-                  if (a.z) store8(a.z, (row0 + rl) * a.ld_z + col, n, a.vec_z, bf16, v);
+                  if (a.z) store8(a.z, (row0 + rl) * a.ld_z + col, bf16, v);
                   if (!zero) {
                     activate(a.activation, a.slope, v);
                     if (a.residual) {
                       float x[8];
-                      load8(a.residual, (row0 + rl) * a.ld_residual + col, n, a.vec_residual, bf16, x);
+                      load8(a.residual, (row0 + rl) * a.ld_residual + col, bf16, x);
 #pragma unroll
                       for (int i = 0; i < 8; ++i) v[i] += x[i];
                     }
                   }
                 }
-                store8(a.out, (row0 + rl) * a.ld_out + col, n, a.vec_out, bf16, v);
+                store8(a.out, (row0 + rl) * a.ld_out + col, bf16, v);
               }
             }
           }
@@ -701,8 +753,8 @@ struct TableShared {
 
 // dz = dy act'(z), rounded for the two products, and its column sums per row
 // tile before that rounding.  One pass over dy and z, HBM-bound: a warp has four
-// rows' loads in flight.  VEC: every row of dy and z starts on 16 bytes and ends on
-// a whole piece of 8.
+// rows' loads in flight.  VEC: every row of dy and z is whole 16-byte pieces.  dz's
+// pads are never read: TMA's matrix ends at the width.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kDzThreads) k_dz(const DzArgs a) {
   extern __shared__ uint8_t raw[];
@@ -712,56 +764,69 @@ __global__ void __launch_bounds__(kDzThreads) k_dz(const DzArgs a) {
   pdl_trigger();
   make_table(s.off, s.tile, a.offsets, a.num_experts, a.num_rows);
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
-  const uint32_t col = blockIdx.x * kDzCols + lane * 8;
-  const int n = min(8, (int)a.width - (int)col);
+  // this lane's columns: a piece of eight, or eight 32 apart
+  const auto col = [&](uint32_t i) { return blockIdx.x * kDzCols + (VEC ? lane * 8 + i : lane + 32 * i); };
   const uint32_t total = s.tile[a.num_experts];
   const bool acts = a.activation != NTC_ACT_NONE;
-  const T *dy = (const T *)a.dy + col, *z = (const T *)a.z + col;
-  T *dz = a.dz ? (T *)a.dz + col : nullptr;
+  const T *dy = (const T *)a.dy, *z = (const T *)a.z;
+  T *dz = (T *)a.dz;
   for (uint32_t q = blockIdx.y; q < total; q += gridDim.y) {
     const uint32_t e = bucket_of_tile(s.tile, a.num_experts, q);
     const uint32_t row = (uint32_t)s.off[e] + (q - s.tile[e]) * kRows;
     const uint32_t rows = min(kRows, (uint32_t)s.off[e + 1] - row);
     float sum[8] = {};
-    if (n > 0) {
-      for (uint32_t r0 = warp; r0 < rows; r0 += 32) {
-        uint4 qg[4], qz[4];
-        if constexpr (VEC) {
+    if constexpr (VEC) {
+      if (col(0) < a.width)
+        for (uint32_t r0 = warp; r0 < rows; r0 += 32) {
+          uint4 qg[4], qz[4];
 #pragma unroll
           for (uint32_t u = 0; u < 4; ++u) {
             qg[u] = qz[u] = make_uint4(0, 0, 0, 0);
             if (r0 + 8 * u < rows) {
-              qg[u] = *reinterpret_cast<const uint4 *>(dy + (uint64_t)(row + r0 + 8 * u) * a.ld_dy);
-              if (acts) qz[u] = *reinterpret_cast<const uint4 *>(z + (uint64_t)(row + r0 + 8 * u) * a.ld_z);
+              qg[u] = *reinterpret_cast<const uint4 *>(dy + (uint64_t)(row + r0 + 8 * u) * a.ld_dy + col(0));
+              if (acts) qz[u] = *reinterpret_cast<const uint4 *>(z + (uint64_t)(row + r0 + 8 * u) * a.ld_z + col(0));
             }
           }
-        }
 #pragma unroll
-        for (uint32_t u = 0; u < 4; ++u) {
-          const uint32_t r = r0 + 8 * u;
-          if (r >= rows) break;
-          float g[8], v[8];
-          if constexpr (VEC) {
+          for (uint32_t u = 0; u < 4; ++u) {
+            const uint32_t r = r0 + 8 * u;
+            if (r >= rows) break;
+            float g[8], v[8];
             Vec<T>::unpack(qg[u], g);
             Vec<T>::unpack(qz[u], v);
-          } else {
-            load_vec<T>(dy + (uint64_t)(row + r) * a.ld_dy, n, false, g);
-            if (acts) load_vec<T>(z + (uint64_t)(row + r) * a.ld_z, n, false, v);
-          }
-          if (acts) {
+            if (acts) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[i] *= act_slope(a.activation, a.slope, v[i]);
-          }
+              for (int i = 0; i < 8; ++i) g[i] *= act_slope(a.activation, a.slope, v[i]);
+            }
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sum[i] += i < n ? g[i] : 0.0f;
-          if (dz) store_vec<T>(dz + (uint64_t)(row + r) * a.pitch, 8, true, g);  // the pads' values are never read
+            for (int i = 0; i < 8; ++i) sum[i] += g[i];
+            if (dz) *reinterpret_cast<uint4 *>(dz + (uint64_t)(row + r) * a.pitch + col(0)) = Vec<T>::pack(g);
+          }
         }
+    } else {
+      for (uint32_t r = warp; r < rows; r += 8) {
+        float g[8], v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          g[i] = v[i] = 0.0f;
+          if (col(i) < a.width) {
+            g[i] = to_f<T>(dy[(uint64_t)(row + r) * a.ld_dy + col(i)]);
+            if (acts) v[i] = to_f<T>(z[(uint64_t)(row + r) * a.ld_z + col(i)]);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (col(i) < a.width) {
+            if (acts) g[i] *= act_slope(a.activation, a.slope, v[i]);
+            sum[i] += g[i];
+            if (dz) dz[(uint64_t)(row + r) * a.pitch + col(i)] = from_f<T>(g[i]);
+          }
       }
     }
     if (a.part) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sums[warp][lane * 8 + i] = sum[i];
+      for (int i = 0; i < 8; ++i) sums[warp][col(i) - blockIdx.x * kDzCols] = sum[i];
       __syncthreads();
       const uint32_t c = blockIdx.x * kDzCols + threadIdx.x;
       if (c < a.width) {
@@ -1054,9 +1119,8 @@ extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void
   a.activation = d.activation;
   a.slope = d.leaky_slope;
   a.bf16 = d.type == NTC_TYPE_BF16;
-  a.vec_out = rows_are_vec(y, d.ld_y, 2);
-  a.vec_z = z && rows_are_vec(z, d.ld_z, 2);
-  a.vec_residual = residual && rows_are_vec(residual, d.ld_residual, 2);
+  a.vec_out = d.out_dim % 8 == 0 && rows_are_vec(y, d.ld_y, 2) && (!z || rows_are_vec(z, d.ld_z, 2)) &&
+              (!residual || rows_are_vec(residual, d.ld_residual, 2));
   a.status = status;
   return op_cuda(launch_product<kForward>(X, W, a, st), "ntc_linear");
 }
