@@ -100,6 +100,9 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, uin
       "l"(map), "r"(bar), "r"(x), "r"(y), "r"(e)
       : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
+  asm volatile("prefetch.tensormap [%0];\n" ::"l"(map) : "memory");
+}
 // 16 bytes from src, or 16 zeros.  The copies have no "memory" clobber: it would
 // have every one of them read the kernel's parameters again.
 __device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src, bool zeros) {
@@ -321,7 +324,8 @@ __device__ __forceinline__ uint32_t staged(uint32_t r, uint32_t c) {
 
 template <int MODE, int BN>
 __global__ void __launch_bounds__(threads(MODE), 1)
-    k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Args a) {
+    k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32,
+             const __grid_constant__ CUtensorMap map_b, const Args a) {
   constexpr uint32_t kStages = stages(BN), kStage = stage_bytes(BN);
   extern __shared__ uint8_t raw[];
   uint8_t *ring = raw + (1024 - (saddr(raw) & 1023)) % 1024;
@@ -344,6 +348,11 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     mbar_init_fence();
   }
   if (warp == 2) tmem_alloc(saddr(&s.tmem));
+  if (warp == 0 && elect_one()) {
+    prefetch_map(&map_a);
+    if (MODE != kDw) prefetch_map(&map_a32);
+    prefetch_map(&map_b);
+  }
   pdl_wait();
   make_table(s.off, s.tile, a.offsets, a.num_experts, a.num_rows);
   fence_after();
@@ -356,33 +365,46 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     bool ok = true;
     for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
       const Tile o = tiles.at(t);
-      const uint32_t chunks = (o.depth + kChunk - 1) / kChunk;
+      const uint32_t depth = uniform(o.depth), chunks = (depth + kChunk - 1) / kChunk, e = uniform(o.e);
+      const int32_t row = (int32_t)uniform(o.row), col = (int32_t)uniform(o.col), begin = (int32_t)uniform(o.begin);
+      const uint32_t boxes = uniform(MODE == kForward && a.rows ? 0 : (o.rows + 31) / 32);  // of 32 rows; 4: one of 128
       for (uint32_t c = 0; c < chunks; ++c, ++issued) {
         const uint32_t st = issued % kStages;
         ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.empty[st]), ((issued / kStages) & 1) ^ 1));
         if (!ok) break;
-        const uint32_t bar = saddr(&s.full[st]);
-        const uint32_t sa = saddr(ring) + st * kStage, sb = sa + kABytes;
-        if constexpr (MODE != kDw) {
-          const uint32_t boxes = MODE == kForward && a.rows ? 0 : (o.rows + 31) / 32;
-          if (lane == 0) expect_tx(bar, boxes * 4096 + BN * 128);
-          __syncwarp();
-          if (lane < boxes) tma_2d(sa + lane * 4096, &map_a, bar, (int32_t)(c * kChunk), (int32_t)(o.row + lane * 32));
-          if constexpr (MODE == kForward) {
-            if (lane == 0) tma_3d(sb, &map_b, bar, (int32_t)(c * kChunk), (int32_t)o.col, (int32_t)o.e);
+        // One elected lane issues a chunk's copies, with operands the compiler knows to
+        // be uniform: from several lanes they go out one by one, 75 cycles each.
+        const uint32_t bar = uniform(saddr(&s.full[st]));
+        const uint32_t sa = uniform(saddr(ring) + st * kStage), sb = sa + kABytes;
+        const int32_t k = (int32_t)(c * kChunk);
+        if (elect_one()) {
+          if constexpr (MODE != kDw) {
+            if (boxes == 4) {
+              expect_tx(bar, kABytes + BN * 128);
+              tma_2d(sa, &map_a, bar, k, row);
+            } else {
+              expect_tx(bar, boxes * 4096 + BN * 128);
+              for (uint32_t j = 0; j < boxes; ++j) tma_2d(sa + j * 4096, &map_a32, bar, k, row + (int32_t)j * 32);
+            }
+            if constexpr (MODE == kForward) {
+              tma_3d(sb, &map_b, bar, k, col, (int32_t)e);
+            } else {
+#pragma unroll
+              for (uint32_t j = 0; j < BN / 64; ++j) tma_3d(sb + j * 8192, &map_b, bar, col + (int32_t)j * 64, k, (int32_t)e);
+            }
+          } else if ((c + 1) * kChunk <= depth) {
+            expect_tx(bar, (a.rows ? 0 : kABytes) + BN * 128);
+            if (!a.rows) {
+#pragma unroll
+              for (uint32_t j = 0; j < 2; ++j) tma_2d(sa + j * 8192, &map_a, bar, row + (int32_t)j * 64, begin + k);
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < BN / 64; ++j) tma_2d(sb + j * 8192, &map_b, bar, col + (int32_t)j * 64, begin + k);
           } else {
-            if (lane < BN / 64)
-              tma_3d(sb + lane * 8192, &map_b, bar, (int32_t)(o.col + lane * 64), (int32_t)(c * kChunk), (int32_t)o.e);
+            mbar_arrive(bar);  // the copying warps bring all of it
           }
-        } else {
-          const bool whole = (c + 1) * kChunk <= o.depth;
-          if (lane == 0) expect_tx(bar, whole ? (a.rows ? 0 : kABytes) + BN * 128 : 0);
-          __syncwarp();
-          if (whole && !a.rows && lane < 2)
-            tma_2d(sa + lane * 8192, &map_a, bar, (int32_t)(o.row + lane * 64), (int32_t)(o.begin + c * kChunk));
-          if (whole && lane < BN / 64)
-            tma_2d(sb + lane * 8192, &map_b, bar, (int32_t)(o.col + lane * 64), (int32_t)(o.begin + c * kChunk));
         }
+        __syncwarp();
       }
     }
     pdl_trigger();
@@ -947,8 +969,8 @@ unsigned int *status_word() {
 
 template <int MODE, int BN>
 cudaError_t launch_tile(const Operand &A, const Operand &B, Args a, uint64_t tiles_bound, int sms, cudaStream_t st) {
-  CUtensorMap ma, mb;
-  if (!make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 32) ||
+  CUtensorMap ma, ma32, mb;
+  if (!make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 128) || !make_map(&ma32, A, 2, 64, 32) ||
       !make_map(&mb, B, MODE == kDw ? 2 : 3, 64, MODE == kForward ? BN : 64))
     return cudaErrorInvalidValue;
   a.x = (const uint8_t *)A.p;
@@ -965,7 +987,7 @@ cudaError_t launch_tile(const Operand &A, const Operand &B, Args a, uint64_t til
     if (dev < 64) allowed.fetch_or(1ull << dev);
   }
   const unsigned grid = (unsigned)std::min<uint64_t>(tiles_bound, (uint64_t)sms);
-  return launch_pdl(k_linear<MODE, BN>, grid, threads(MODE), kSharedBytes, st, ma, mb, a);
+  return launch_pdl(k_linear<MODE, BN>, grid, threads(MODE), kSharedBytes, st, ma, ma32, mb, a);
 }
 
 // Row tiles of num_rows rows in num_experts segments (and those of no expert), at most.
