@@ -416,29 +416,30 @@ __global__ void __launch_bounds__(threads(MODE), 1)
                            ((MODE != kForward ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((kRows >> 4) << 24);
     // 16 of the contraction: 32 bytes along a K-major row, 16 rows of an MN-major block
     constexpr uint32_t kStepA = MODE == kDw ? 2048 >> 4 : 32 >> 4, kStepB = MODE != kForward ? 2048 >> 4 : 32 >> 4;
+    // Everything the issuing lane needs derives from values known to be uniform: the
+    // MMAs of a chunk of a narrow tile take less time than moving operands would.
+    const uint32_t ring_lo = uniform(sw128_lo(saddr(ring), 8192)), columns = uniform(tmem);
     uint32_t used = 0, acc = 0, phases = 0;  // phases: bit of each stage's copied barrier
     bool ok = true, any = false;
     for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
       const Tile o = tiles.at(t);
-      if (o.depth == 0) continue;
-      const uint32_t chunks = (o.depth + kChunk - 1) / kChunk;
+      const uint32_t depth = uniform(o.depth), chunks = (depth + kChunk - 1) / kChunk;
+      if (chunks == 0) continue;
       ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.acc_empty[acc & 1]), ((acc >> 1) & 1) ^ 1));
       if (!ok) break;
       fence_after();
-      const uint32_t d = uniform(tmem + (acc & 1) * BN);
+      const uint32_t d = columns + (acc & 1) * BN;
       for (uint32_t c = 0; c < chunks; ++c, ++used) {
         const uint32_t st = used % kStages;
         ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.full[st]), (used / kStages) & 1));
-        if (ok && (a.rows || (MODE == kDw && (c + 1) * kChunk > o.depth))) {
+        if (ok && (a.rows || (MODE == kDw && (c + 1) * kChunk > depth))) {
           ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.copied[st]), (phases >> st) & 1));
           phases ^= 1u << st;
           fence_async();
         }
         if (!ok) break;
-        fence_after();
         any = true;
-        const uint32_t sa = saddr(ring) + st * kStage;
-        const uint32_t alo = uniform(sw128_lo(sa, 8192)), blo = uniform(sw128_lo(sa + kABytes, 8192));
+        const uint32_t alo = ring_lo + st * (kStage >> 4), blo = alo + (kABytes >> 4);
         if (elect_one()) {
 #pragma unroll
           for (uint32_t k = 0; k < kChunk / 16; ++k)
