@@ -305,8 +305,8 @@ __device__ __forceinline__ void load8(const void *p, uint64_t at, bool bf16, flo
 __device__ __forceinline__ void store8(void *p, uint64_t at, bool bf16, const float (&v)[8]) {
   *reinterpret_cast<uint4 *>((uint16_t *)p + at) = bf16 ? Vec<__nv_bfloat16>::pack(v) : Vec<__half>::pack(v);
 }
-__device__ __forceinline__ float load1(const void *p, uint64_t at, bool bf16) {
-  return bf16 ? to_f<__nv_bfloat16>(((const __nv_bfloat16 *)p)[at]) : to_f<__half>(((const __half *)p)[at]);
+__device__ __forceinline__ float from_bits(uint16_t b, bool bf16) {
+  return bf16 ? __uint_as_float((uint32_t)b << 16) : __half2float(__ushort_as_half(b));
 }
 __device__ __forceinline__ void store1(void *p, uint64_t at, bool bf16, float v) {
   if (bf16) ((__nv_bfloat16 *)p)[at] = from_f<__nv_bfloat16>(v);
@@ -649,18 +649,22 @@ __global__ void __launch_bounds__(threads(MODE), 1)
             if (col < a.width) {
               const float b = MODE == kForward && a.bias && !zero ? a.bias[(uint64_t)o.e * a.width + col] : 0.0f;
               const int32_t r0 = lane >> 4;
+              // the residual's 16 rows are asked for first, as bits: a conversion would wait
+              uint16_t x[16];
 #pragma unroll
-              for (int32_t it = 0; it < 16; it += 8) {  // eight rows' loads, then eight rows' values
-                float v[8], x[8];
+              for (int32_t i = 0; i < 16; ++i) {
+                x[i] = 0;
+                if (MODE == kForward && a.residual && !zero && r0 + 2 * i < high)
+                  x[i] = ((const uint16_t *)a.residual)[(row0 + r0 + 2 * i) * a.ld_residual + col];
+              }
 #pragma unroll
-                for (int32_t i = 0; i < 8; ++i) {
-                  const int32_t rl = r0 + 2 * (it + i);
-                  x[i] = 0.0f;
-                  if (MODE == kForward && a.residual && !zero && rl < high)
-                    x[i] = load1(a.residual, (row0 + rl) * a.ld_residual + col, bf16);
+              for (int32_t it = 0; it < 16; it += 8) {
+                float v[8];
+#pragma unroll
+                for (int32_t i = 0; i < 8; ++i)
                   v[i] = zero ? 0.0f
-                              : *reinterpret_cast<const float *>(mine + staged(rl, (lane & 15) >> 2) + (lane & 3) * 4) + b;
-                }
+                              : *reinterpret_cast<const float *>(mine + staged(r0 + 2 * (it + i), (lane & 15) >> 2) +
+                                                                 (lane & 3) * 4) + b;
                 if constexpr (MODE == kForward) {
                   if (a.z) {
 #pragma unroll
@@ -672,7 +676,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
 #pragma unroll
                 for (int32_t i = 0; i < 8; ++i)
                   if (r0 + 2 * (it + i) < high)
-                    store1(a.out, (row0 + r0 + 2 * (it + i)) * a.ld_out + col, bf16, v[i] + x[i]);
+                    store1(a.out, (row0 + r0 + 2 * (it + i)) * a.ld_out + col, bf16, v[i] + from_bits(x[it + i], bf16));
               }
             }
             __syncwarp();
@@ -827,23 +831,26 @@ __global__ void __launch_bounds__(kDzThreads) k_dz(const DzArgs a) {
           }
         }
     } else {
-      for (uint32_t r = warp; r < rows; r += 8) {
-        float g[8], v[8];
+      for (uint32_t r0 = warp; r0 < rows; r0 += 16) {
+        T g[2][8], v[2][8];  // two rows' loads in flight
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          g[i] = v[i] = 0.0f;
-          if (col(i) < a.width) {
-            g[i] = to_f<T>(dy[(uint64_t)(row + r) * a.ld_dy + col(i)]);
-            if (acts) v[i] = to_f<T>(z[(uint64_t)(row + r) * a.ld_z + col(i)]);
-          }
-        }
+        for (uint32_t u = 0; u < 2; ++u)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (col(i) < a.width) {
-            if (acts) g[i] *= act_slope(a.activation, a.slope, v[i]);
-            sum[i] += g[i];
-            if (dz) dz[(uint64_t)(row + r) * a.pitch + col(i)] = from_f<T>(g[i]);
-          }
+          for (int i = 0; i < 8; ++i)
+            if (col(i) < a.width && r0 + 8 * u < rows) {
+              g[u][i] = dy[(uint64_t)(row + r0 + 8 * u) * a.ld_dy + col(i)];
+              if (acts) v[u][i] = z[(uint64_t)(row + r0 + 8 * u) * a.ld_z + col(i)];
+            }
+#pragma unroll
+        for (uint32_t u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (col(i) < a.width && r0 + 8 * u < rows) {
+              float x = to_f<T>(g[u][i]);
+              if (acts) x *= act_slope(a.activation, a.slope, to_f<T>(v[u][i]));
+              sum[i] += x;
+              if (dz) dz[(uint64_t)(row + r0 + 8 * u) * a.pitch + col(i)] = from_f<T>(x);
+            }
       }
     }
     if (a.part) {
