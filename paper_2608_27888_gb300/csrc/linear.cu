@@ -23,7 +23,7 @@
 // A weight matrix [N][K] is read as it lies: K-major in the forward product,
 // MN-major (the descriptors' transpose bits) in kDx; kDw takes both operands
 // MN-major.  Nothing is transposed in memory.
-#include "experts.cuh"
+#include "linear.cuh"
 #include "tcgen05.cuh"
 
 #include <cuda.h>
@@ -60,25 +60,6 @@ struct Shared {
 };
 constexpr size_t kSharedBytes = 1024 + kRing + kEpilogueWarps * 32 * kStageCols * 4 + sizeof(Shared);
 static_assert(kSharedBytes <= 232448, "shared memory of one CTA");
-
-struct Args {
-  const int32_t *rows, *offsets;
-  const float *bias;
-  const void *residual;
-  const uint8_t *x, *dz;  // the operand that may be gathered, and kDw's other one
-  uint64_t ld_x, ld_dz;
-  void *out, *z;
-  uint64_t ld_out, ld_z, ld_residual;
-  uint32_t num_experts, num_rows, x_rows;
-  uint32_t width;      // columns of the output
-  uint32_t height;     // kDw: rows of one expert's (transposed) output
-  uint32_t depth;      // contraction length (not kDw: there it is the expert's rows)
-  uint32_t activation;
-  float slope;
-  uint32_t bf16;
-  uint32_t vec_out;    // every row of out, z and residual is whole 16-byte pieces
-  unsigned int *status;
-};
 
 __device__ unsigned int g_linear_status;
 
@@ -219,7 +200,7 @@ struct Tiles {
   const Shared &s;
   uint32_t num_experts, height, depth, cols, row_tiles;
   uint64_t total;
-  __device__ __forceinline__ Tiles(const Args &a, const Shared &sh)
+  __device__ __forceinline__ Tiles(const LinearArgs &a, const Shared &sh)
       : s(sh), num_experts(a.num_experts), height(a.height), depth(a.depth) {
     cols = (a.width + BN - 1) / BN;
     row_tiles = (a.height + kRows - 1) / kRows;
@@ -262,43 +243,8 @@ struct Tiles {
 
 // ------------------------------------------------------------ epilogue
 
-// The normal distribution function Phi(z), and e = exp(-z^2 / 2), which its density
-// shares: erf by Abramowitz and Stegun, formula 7.1.26 (absolute error 1.5e-7, so
-// Phi's is below 1e-7, less than one rounding to bf16 or fp16 of anything above 2^-13).
-// Fewer instructions than erff and expf, which bound k_dz.
-__device__ __forceinline__ float normal_cdf(float z, float &e) {
-  e = __expf(-0.5f * z * z);
-  const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
-  float q = fmaf(1.061405429f, t, -1.453152027f);
-  q = fmaf(q, t, 1.421413741f);
-  q = fmaf(q, t, -0.284496736f);
-  q = fmaf(q, t, 0.254829592f);
-  q *= 0.5f * t * e;  // the upper tail of |z|
-  return z < 0.0f ? q : 1.0f - q;
-}
-
-__device__ __forceinline__ void activate(uint32_t act, float slope, float (&v)[8]) {
-  if (act == NTC_ACT_RELU) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = v[i] < 0.0f ? 0.0f : v[i];  // NaN stays
-  } else if (act == NTC_ACT_LEAKY) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = v[i] > 0.0f ? v[i] : slope * v[i];
-  } else if (act == NTC_ACT_GELU) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float e;
-      v[i] *= normal_cdf(v[i], e);
-    }
-  } else if (act == NTC_ACT_SILU) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __fdividef(v[i], 1.0f + __expf(-v[i]));
-  }
-}
-
-// Eight elements at a 16-byte boundary, and one anywhere.
-__device__ __forceinline__ void load8(const void *p, uint64_t at, bool bf16, float (&v)[8]) {
-  const uint4 q = *reinterpret_cast<const uint4 *>((const uint16_t *)p + at);
+// Eight elements, and one.
+__device__ __forceinline__ void unpack8(const uint4 &q, bool bf16, float (&v)[8]) {
   if (bf16) Vec<__nv_bfloat16>::unpack(q, v);
   else Vec<__half>::unpack(q, v);
 }
@@ -325,7 +271,7 @@ __device__ __forceinline__ uint32_t staged(uint32_t r, uint32_t c) {
 template <int MODE, int BN>
 __global__ void __launch_bounds__(threads(MODE), 1)
     k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32,
-             const __grid_constant__ CUtensorMap map_b, const Args a) {
+             const __grid_constant__ CUtensorMap map_b, const LinearArgs a) {
   constexpr uint32_t kStages = stages(BN), kStage = stage_bytes(BN);
   extern __shared__ uint8_t raw[];
   uint8_t *ring = raw + (1024 - (saddr(raw) & 1023)) % 1024;
@@ -576,6 +522,15 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     if (!ok) asm volatile("cp.async.wait_all;\n" ::: "memory");  // none lands after the CTA's end
   } else {
     const uint32_t w = warp - 4, quarter = warp & 3;
+    // copies of the arguments: with asm in the loop the compiler would read them from
+    // the parameters at every use
+    const float *const bias = a.bias;
+    const uint16_t *const residual = (const uint16_t *)a.residual;
+    uint16_t *const out = (uint16_t *)a.out, *const z = (uint16_t *)a.z;
+    const uint64_t ld_out = a.ld_out, ld_z = a.ld_z, ld_residual = a.ld_residual;
+    const uint32_t width = a.width, act = a.activation;
+    const float slope = a.slope;
+    const bool vec = a.vec_out;
     const uint32_t part = (w >> 2) * (BN / 2);  // each set of four warps takes half of the columns
     uint8_t *mine = staging + w * 32 * kStageCols * 4;
     const uint32_t base = saddr(mine);
@@ -584,14 +539,35 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     for (uint64_t t = blockIdx.x; t < tiles.total; t += gridDim.x) {
       const Tile o = tiles.at(t);
       const bool zero = o.depth == 0;
+      const int32_t high = (int32_t)o.rows - (int32_t)(quarter * 32);  // rows of this warp inside
+      const uint64_t row0 = o.row + quarter * 32;
+      // The bias and the residual of 16 columns, asked for 16 columns ahead: the first
+      // ones while the tile is still being multiplied.
+      float4 bias0, bias1;
+      uint4 res0, res1;
+      const auto ask = [&](uint32_t c0) {
+        const uint32_t col = o.col + c0 + (lane & 1) * 8;
+        bias0 = bias1 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (col >= width) return;
+        if (bias) {
+          const float4 *b = reinterpret_cast<const float4 *>(bias + (uint64_t)o.e * width + col);
+          bias0 = b[0];
+          bias1 = b[1];
+        }
+        if (residual) {
+          const uint16_t *r = residual + (row0 + (lane >> 1)) * ld_residual + col;
+          if ((int32_t)(lane >> 1) < high) res0 = *reinterpret_cast<const uint4 *>(r);
+          if ((int32_t)(lane >> 1) + 16 < high) res1 = *reinterpret_cast<const uint4 *>(r + 16 * ld_residual);
+        }
+      };
+      const bool asks = MODE == kForward && !zero && high > 0 && vec;
+      if (asks) ask(part);
       if (!zero) {
         if (!__all_sync(0xFFFFFFFFu, wait(saddr(&s.acc_full[acc & 1]), (acc >> 1) & 1))) break;
         fence_after();
       }
-      const int32_t high = (int32_t)o.rows - (int32_t)(quarter * 32);  // rows of this warp inside
-      const uint64_t row0 = o.row + quarter * 32;
       if (high > 0) {
-        for (uint32_t c0 = part; c0 < part + BN / 2 && o.col + c0 < a.width; c0 += kStageCols) {
+        for (uint32_t c0 = part; c0 < part + BN / 2 && o.col + c0 < width; c0 += kStageCols) {
           uint32_t r[16];
           if (!zero) {
             tmem_ld16(tmem + ((quarter * 32) << 16) + (acc & 1) * BN + c0, r);
@@ -612,15 +588,15 @@ __global__ void __launch_bounds__(threads(MODE), 1)
                 v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
               }
             }
-            if (a.vec_out) {
-              if (o.col + c0 + j < a.width) {
-                const uint64_t at = ((uint64_t)o.e * a.width + o.col + c0 + j) * a.ld_out + o.row + quarter * 32 + k0;
+            if (vec) {
+              if (o.col + c0 + j < width) {
+                const uint64_t at = ((uint64_t)o.e * width + o.col + c0 + j) * ld_out + o.row + quarter * 32 + k0;
 #pragma unroll
                 for (uint32_t q = 0; q < 2; ++q) {
                   float u[8];
 #pragma unroll
                   for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
-                  if ((int32_t)(k0 + 8 * q) < high) store8(a.out, at + 8 * q, bf16, u);
+                  if ((int32_t)(k0 + 8 * q) < high) store8(out, at + 8 * q, bf16, u);
                 }
               }
             } else {  // rows at odd addresses: a row's 32 values by 32 lanes
@@ -628,8 +604,8 @@ __global__ void __launch_bounds__(threads(MODE), 1)
               for (uint32_t q = 0; q < 16; ++q) {
                 float x = 0.0f;
                 if (!zero) x = *reinterpret_cast<const float *>(mine + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4);
-                if (o.col + c0 + q < a.width && (int32_t)lane < high)
-                  store1(a.out, ((uint64_t)o.e * a.width + o.col + c0 + q) * a.ld_out + o.row + quarter * 32 + lane, bf16, x);
+                if (o.col + c0 + q < width && (int32_t)lane < high)
+                  store1(out, ((uint64_t)o.e * width + o.col + c0 + q) * ld_out + o.row + quarter * 32 + lane, bf16, x);
               }
             }
             __syncwarp();
@@ -643,19 +619,19 @@ __global__ void __launch_bounds__(threads(MODE), 1)
                            : "memory");
             __syncwarp();
           }
-          if (!a.vec_out) {
+          if (!vec) {
             // rows at odd addresses: lanes on consecutive columns, two rows at a time
             const uint32_t col = o.col + c0 + (lane & 15);
-            if (col < a.width) {
-              const float b = MODE == kForward && a.bias && !zero ? a.bias[(uint64_t)o.e * a.width + col] : 0.0f;
+            if (col < width) {
+              const float b = MODE == kForward && bias && !zero ? bias[(uint64_t)o.e * width + col] : 0.0f;
               const int32_t r0 = lane >> 4;
               // the residual's 16 rows are asked for first, as bits: a conversion would wait
               uint16_t x[16];
 #pragma unroll
               for (int32_t i = 0; i < 16; ++i) {
                 x[i] = 0;
-                if (MODE == kForward && a.residual && !zero && r0 + 2 * i < high)
-                  x[i] = ((const uint16_t *)a.residual)[(row0 + r0 + 2 * i) * a.ld_residual + col];
+                if (MODE == kForward && residual && !zero && r0 + 2 * i < high)
+                  x[i] = (residual)[(row0 + r0 + 2 * i) * ld_residual + col];
               }
 #pragma unroll
               for (int32_t it = 0; it < 16; it += 8) {
@@ -666,59 +642,56 @@ __global__ void __launch_bounds__(threads(MODE), 1)
                               : *reinterpret_cast<const float *>(mine + staged(r0 + 2 * (it + i), (lane & 15) >> 2) +
                                                                  (lane & 3) * 4) + b;
                 if constexpr (MODE == kForward) {
-                  if (a.z) {
+                  if (z) {
 #pragma unroll
                     for (int32_t i = 0; i < 8; ++i)
-                      if (r0 + 2 * (it + i) < high) store1(a.z, (row0 + r0 + 2 * (it + i)) * a.ld_z + col, bf16, v[i]);
+                      if (r0 + 2 * (it + i) < high) store1(z, (row0 + r0 + 2 * (it + i)) * ld_z + col, bf16, v[i]);
                   }
-                  if (!zero) activate(a.activation, a.slope, v);
+                  if (!zero) activate(act, slope, v);
                 }
 #pragma unroll
                 for (int32_t i = 0; i < 8; ++i)
                   if (r0 + 2 * (it + i) < high)
-                    store1(a.out, (row0 + r0 + 2 * (it + i)) * a.ld_out + col, bf16, v[i] + from_bits(x[it + i], bf16));
+                    store1(out, (row0 + r0 + 2 * (it + i)) * ld_out + col, bf16, v[i] + from_bits(x[it + i], bf16));
               }
             }
             __syncwarp();
             continue;
           }
           const uint32_t col = o.col + c0 + (lane & 1) * 8;
-          if (col < a.width) {  // vec_out: whole pieces of 8 columns
-            float b[8];
-            if (MODE == kForward && a.bias && !zero) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) b[i] = a.bias[(uint64_t)o.e * a.width + col + i];
-            } else {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) b[i] = 0.0f;
+          if (col < width) {  // vec_out: whole pieces of 8 columns
+            float b[8] = {};
+            uint4 x[2];
+            if (asks) {
+              b[0] = bias0.x, b[1] = bias0.y, b[2] = bias0.z, b[3] = bias0.w;
+              b[4] = bias1.x, b[5] = bias1.y, b[6] = bias1.z, b[7] = bias1.w;
+              x[0] = res0, x[1] = res1;
+              if (c0 + kStageCols < part + BN / 2) ask(c0 + kStageCols);
             }
 #pragma unroll
             for (uint32_t it = 0; it < 2; ++it) {
               const uint32_t rl = (lane >> 1) + 16 * it;
               if ((int32_t)rl < high) {
-                float v[8];
-                if (zero) {
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) v[i] = 0.0f;
-                } else {
+                float v[8] = {};
+                if (!zero) {
                   const float4 f = *reinterpret_cast<const float4 *>(mine + staged(rl, (lane & 1) * 2));
                   const float4 g = *reinterpret_cast<const float4 *>(mine + staged(rl, (lane & 1) * 2 + 1));
                   v[0] = f.x + b[0], v[1] = f.y + b[1], v[2] = f.z + b[2], v[3] = f.w + b[3];
                   v[4] = g.x + b[4], v[5] = g.y + b[5], v[6] = g.z + b[6], v[7] = g.w + b[7];
                 }
                 if constexpr (MODE == kForward) {
-                  if (a.z) store8(a.z, (row0 + rl) * a.ld_z + col, bf16, v);
+                  if (z) store8(z, (row0 + rl) * ld_z + col, bf16, v);
                   if (!zero) {
-                    activate(a.activation, a.slope, v);
-                    if (a.residual) {
-                      float x[8];
-                      load8(a.residual, (row0 + rl) * a.ld_residual + col, bf16, x);
+                    activate(act, slope, v);
+                    if (residual) {
+                      float u[8];
+                      unpack8(x[it], bf16, u);
 #pragma unroll
-                      for (int i = 0; i < 8; ++i) v[i] += x[i];
+                      for (int i = 0; i < 8; ++i) v[i] += u[i];
                     }
                   }
                 }
-                store8(a.out, (row0 + rl) * a.ld_out + col, bf16, v);
+                store8(out, (row0 + rl) * ld_out + col, bf16, v);
               }
             }
           }
@@ -976,7 +949,7 @@ unsigned int *status_word() {
 }
 
 template <int MODE, int BN>
-cudaError_t launch_tile(const Operand &A, const Operand &B, Args a, uint64_t tiles_bound, int sms, cudaStream_t st) {
+cudaError_t launch_tile(const Operand &A, const Operand &B, LinearArgs a, uint64_t tiles_bound, int sms, cudaStream_t st) {
   CUtensorMap ma, ma32, mb;
   if (!make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 128) || !make_map(&ma32, A, 2, 64, 32) ||
       !make_map(&mb, B, MODE == kDw ? 2 : 3, 64, MODE == kForward ? BN : 64))
@@ -1003,15 +976,19 @@ uint64_t row_tiles_bound(uint64_t num_rows, uint64_t num_experts) {
   return std::min<uint64_t>(num_rows, (num_rows + kRows - 1) / kRows + num_experts);
 }
 
-// The width of a tile: the widest whose tiles still fill the SMs.
+// The width of a tile: the widest whose tiles still fill the SMs, 128 at most where
+// an expert has few rows on average.  Such tiles stream weights, and only the two
+// warps that hold the rows work on their columns (256 rows of 32 experts, 1,024 ->
+// 2,048, gelu, bias and residual: 39.7 us at 256 columns, 36.6 at 128, 40.0 at 64).
 template <int MODE>
-cudaError_t launch_product(const Operand &A, const Operand &B, const Args &a, cudaStream_t st) {
+cudaError_t launch_product(const Operand &A, const Operand &B, const LinearArgs &a, cudaStream_t st) {
   const int sms = sm_count();
   const uint64_t high = MODE == kDw ? (uint64_t)a.num_experts * ((a.height + kRows - 1) / kRows)
                                     : row_tiles_bound(a.num_rows, a.num_experts);
   if (high == 0) return cudaSuccess;
   const auto tiles = [&](uint32_t bn) { return high * ((a.width + bn - 1) / bn); };
-  if (tiles(256) >= (uint64_t)sms) return launch_tile<MODE, 256>(A, B, a, tiles(256), sms, st);
+  const bool thin = MODE != kDw && a.num_rows <= 32ull * a.num_experts;
+  if (!thin && tiles(256) >= (uint64_t)sms) return launch_tile<MODE, 256>(A, B, a, tiles(256), sms, st);
   if (tiles(128) >= (uint64_t)sms) return launch_tile<MODE, 128>(A, B, a, tiles(128), sms, st);
   return launch_tile<MODE, 64>(A, B, a, tiles(64), sms, st);
 }
@@ -1107,7 +1084,7 @@ cudaError_t operand_w(const ntc_linear_desc &d, const void *w, uint8_t *&ws, Ope
 }  // namespace
 
 extern "C" NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, const void *w) {
-  if (check(desc)) return 0;
+  if (check(desc) || few_rows(desc->num_rows)) return 0;
   return (x_packs(*desc, x) ? x_bytes(*desc) : 0) + (w_packs(*desc, w) ? w_bytes(*desc) : 0);
 }
 
@@ -1123,15 +1100,7 @@ extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void
     return op_fail(NTC_ERR_INVALID_ARG, "a buffer is not aligned to its element (2 bytes)");
   if ((uintptr_t)bias & 3) return op_fail(NTC_ERR_INVALID_ARG, "bias is not aligned to 4 bytes");
   if (ntc_status s = check_workspace(workspace, workspace_bytes, ntc_linear_workspace(desc, x, w))) return s;
-  unsigned int *status = status_word();
-  if (!status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
-  cudaStream_t st = (cudaStream_t)cuda_stream;
-  uint8_t *ws = (uint8_t *)workspace;
-  Operand X, W;
-  cudaError_t e = operand_x(d, x, ws, &X, st);
-  if (e == cudaSuccess) e = operand_w(d, w, ws, &W, st);
-  if (e != cudaSuccess) return op_cuda(e, "ntc_linear");
-  Args a{};
+  LinearArgs a{};
   a.rows = rows;
   a.offsets = offsets;
   a.bias = bias;
@@ -1149,10 +1118,22 @@ extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void
   a.activation = d.activation;
   a.slope = d.leaky_slope;
   a.bf16 = d.type == NTC_TYPE_BF16;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (few_rows(d.num_rows)) {
+    a.x = (const uint8_t *)x;
+    a.ld_x = d.ld_x;
+    return op_cuda(launch_few(a, w, d.ld_w, d.stride_w, st), "ntc_linear");
+  }
   a.vec_out = d.out_dim % 8 == 0 && rows_are_vec(y, d.ld_y, 2) && (!z || rows_are_vec(z, d.ld_z, 2)) &&
-              (!residual || rows_are_vec(residual, d.ld_residual, 2));
-  a.status = status;
-  return op_cuda(launch_product<kForward>(X, W, a, st), "ntc_linear");
+              (!residual || rows_are_vec(residual, d.ld_residual, 2)) && ((uintptr_t)bias & 15) == 0;
+  a.status = status_word();
+  if (!a.status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
+  uint8_t *ws = (uint8_t *)workspace;
+  Operand X, W;
+  cudaError_t e = operand_x(d, x, ws, &X, st);
+  if (e == cudaSuccess) e = operand_w(d, w, ws, &W, st);
+  if (e == cudaSuccess) e = launch_product<kForward>(X, W, a, st);
+  return op_cuda(e, "ntc_linear");
 }
 
 extern "C" NTC_API size_t ntc_linear_backward_workspace(const ntc_linear_desc *desc, const void *dy, const void *x,
@@ -1223,7 +1204,7 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
       e = launch_pdl(k_db, dim3((d.out_dim + 31) / 32, std::min(d.num_experts, 1024u)), kDzThreads, sizeof(TableShared), st,
                      (const float *)part, offsets, d.num_experts, (uint32_t)d.num_rows, d.out_dim, k.pitch, db);
   }
-  Args a{};
+  LinearArgs a{};
   a.offsets = offsets;
   a.num_experts = d.num_experts;
   a.num_rows = (uint32_t)d.num_rows;

@@ -84,24 +84,31 @@ __device__ __forceinline__ float group_max(float v) {
     float m;
     asm("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;\n" : "=f"(m) : "f"(v));
     return m;
-  }
+  } else {
 #pragma unroll
-  for (int s = G / 2; s; s >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, s));
-  return v;
+    for (int s = G / 2; s; s >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, s));
+    return v;
+  }
 }
 template <int G>
 __device__ __forceinline__ uint32_t group_max(uint32_t v) {
-  if constexpr (G == 32) return __reduce_max_sync(kAll, v);
+  if constexpr (G == 32) {
+    return __reduce_max_sync(kAll, v);
+  } else {
 #pragma unroll
-  for (int s = G / 2; s; s >>= 1) v = max(v, __shfl_xor_sync(kAll, v, s));
-  return v;
+    for (int s = G / 2; s; s >>= 1) v = max(v, __shfl_xor_sync(kAll, v, s));
+    return v;
+  }
 }
 template <int G>
 __device__ __forceinline__ uint32_t group_add(uint32_t v) {
-  if constexpr (G == 32) return __reduce_add_sync(kAll, v);
+  if constexpr (G == 32) {
+    return __reduce_add_sync(kAll, v);
+  } else {
 #pragma unroll
-  for (int s = G / 2; s; s >>= 1) v += __shfl_xor_sync(kAll, v, s);
-  return v;
+    for (int s = G / 2; s; s >>= 1) v += __shfl_xor_sync(kAll, v, s);
+    return v;
+  }
 }
 template <int G>
 __device__ __forceinline__ float group_sum(float v) {

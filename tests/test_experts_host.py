@@ -121,10 +121,12 @@ def test_linear_pointer_refusals():
     assert call(f, good, 1, None) == BAD  # no rows, and num_x_rows differs
     assert call(f, good, 2, None) == BAD  # several experts without offsets
     assert call(f, good, 1, P + 2) == BAD
-    odd = made(ntc.ntc_linear_desc, LINEAR, dict(ld_x=65))
+    odd = made(ntc.ntc_linear_desc, LINEAR, dict(ld_x=65, num_rows=1000))
+    even = made(ntc.ntc_linear_desc, LINEAR, dict(num_rows=1000))
     need = ntc._lib.ntc_linear_workspace(odd, P, P)
-    assert need > 0 and ntc._lib.ntc_linear_workspace(d, P, P) == 0
-    assert ntc._lib.ntc_linear_workspace(d, P + 8, P) > 0 and ntc._lib.ntc_linear_workspace(d, P, P + 2) > 0
+    assert need > 0 and ntc._lib.ntc_linear_workspace(even, P, P) == 0
+    assert ntc._lib.ntc_linear_workspace(even, P + 8, P) > 0 and ntc._lib.ntc_linear_workspace(even, P, P + 2) > 0
+    assert ntc._lib.ntc_linear_workspace(d, P + 8, P + 2) == 0  # few rows are read where they lie
     assert f(odd, *good[:8], P, need - 1, None) == BAD
     assert f(odd, *good[:8], None, need, None) == BAD
     assert f(odd, *good[:8], P + 8, need, None) == BAD
