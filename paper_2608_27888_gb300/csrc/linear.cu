@@ -53,7 +53,7 @@ constexpr uint32_t stages(int BN) {
 }
 
 struct Shared {
-  uint64_t full[kMaxStages], copied[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+  uint64_t full[kMaxStages], copied[kMaxStages], go[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
   uint32_t tmem, quit;
   int32_t off[NTC_MAX_EXPERTS + 2];       // first row of each expert; [E]: of no expert; [E + 1]: the end
   uint32_t tile[NTC_MAX_EXPERTS + 2];     // first row tile of each expert (and of no expert); the total
@@ -243,22 +243,6 @@ struct Tiles {
 
 // ------------------------------------------------------------ epilogue
 
-// Eight elements, and one.
-__device__ __forceinline__ void unpack8(const uint4 &q, bool bf16, float (&v)[8]) {
-  if (bf16) Vec<__nv_bfloat16>::unpack(q, v);
-  else Vec<__half>::unpack(q, v);
-}
-__device__ __forceinline__ void store8(void *p, uint64_t at, bool bf16, const float (&v)[8]) {
-  *reinterpret_cast<uint4 *>((uint16_t *)p + at) = bf16 ? Vec<__nv_bfloat16>::pack(v) : Vec<__half>::pack(v);
-}
-__device__ __forceinline__ float from_bits(uint16_t b, bool bf16) {
-  return bf16 ? __uint_as_float((uint32_t)b << 16) : __half2float(__ushort_as_half(b));
-}
-__device__ __forceinline__ void store1(void *p, uint64_t at, bool bf16, float v) {
-  if (bf16) ((__nv_bfloat16 *)p)[at] = from_f<__nv_bfloat16>(v);
-  else ((__half *)p)[at] = from_f<__half>(v);
-}
-
 // Offset of 16-byte piece c (0..3) of row r in a warp's staging, 64 bytes a row:
 // the pieces of two rows are mixed so that eight lanes meet eight banks' groups
 // both when lanes hold rows and when they hold pieces.
@@ -266,9 +250,222 @@ __device__ __forceinline__ uint32_t staged(uint32_t r, uint32_t c) {
   return (r >> 1) * 128 + (((((r & 1) << 2) | c) ^ ((r >> 1) & 3)) << 4);
 }
 
+// A warp's part of a tile: 32 rows (of which `high` are inside) times `cols` columns.
+struct Strip {
+  uint32_t e;
+  int32_t high;
+  uint64_t row;  // first row
+  uint32_t col;  // first column
+  int32_t cols;  // at most 0: none
+  uint32_t lane;
+};
+
+// What happens to 32 rows x 32 columns of an accumulator, a lane having a row: they
+// go through the warp's staging, 16 columns at a time, and leave in 32-byte runs.
+// The work of 16 values a lane is laid out side by side: a warp's epilogue is bound by
+// the latency of its own instructions, and has to end within the next tile's MMAs
+// (32 x 512 cycles at K = 2,048; the arguments are copies for the same reason).
+template <typename T>
+struct Epilogue {
+  const float *bias;
+  const T *residual;
+  T *out, *z;
+  uint64_t ld_out, ld_z, ld_residual;
+  uint32_t width, height, act;
+  float slope;
+  bool vec;
+  __device__ __forceinline__ explicit Epilogue(const LinearArgs &a)
+      : bias(a.bias), residual((const T *)a.residual), out((T *)a.out), z((T *)a.z), ld_out(a.ld_out), ld_z(a.ld_z),
+        ld_residual(a.ld_residual), width(a.width), height(a.height), act(a.activation), slope(a.slope),
+        vec(a.vec_out != 0) {}
+
+  // The bias and the residual of the next 32 columns.
+  struct Ahead {
+    float4 b[2][2];
+    uint4 r[2][2];
+  };
+  __device__ __forceinline__ void ask(Ahead &x, uint32_t e, const Strip &g, int32_t c) const {
+    if (!vec) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t at = c + 16 * h + (int32_t)(g.lane & 1) * 8;
+      x.b[h][0] = x.b[h][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      x.r[h][0] = x.r[h][1] = make_uint4(0, 0, 0, 0);
+      if (at < g.cols) {
+        if (bias) {
+          const float4 *b = reinterpret_cast<const float4 *>(bias + (uint64_t)e * width + g.col + at);
+          x.b[h][0] = b[0];
+          x.b[h][1] = b[1];
+        }
+        if (residual) {
+          const T *r = residual + (g.row + (g.lane >> 1)) * ld_residual + g.col + at;
+          if ((int32_t)(g.lane >> 1) < g.high) x.r[h][0] = *reinterpret_cast<const uint4 *>(r);
+          if ((int32_t)(g.lane >> 1) + 16 < g.high) x.r[h][1] = *reinterpret_cast<const uint4 *>(r + 16 * ld_residual);
+        }
+      }
+    }
+  }
+
+  // Rows of whole 16-byte pieces: lane i has a piece of rows i / 2 and i / 2 + 16.
+  template <bool FORWARD>
+  __device__ __forceinline__ void store_rows(const Strip &g, uint32_t e, int32_t c, const uint32_t (&r)[32], Ahead &ahead,
+                                             uint8_t *mine) const {
+    const uint32_t rl = g.lane >> 1;
+    const bool in0 = (int32_t)rl < g.high, in1 = (int32_t)rl + 16 < g.high;
+    Ahead x;
+    if (FORWARD) {
+      x = ahead;
+      if (c + 32 < g.cols) ask(ahead, e, g, c + 32);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q)
+        *reinterpret_cast<uint4 *>(mine + staged(g.lane, q)) =
+            make_uint4(r[16 * h + 4 * q], r[16 * h + 4 * q + 1], r[16 * h + 4 * q + 2], r[16 * h + 4 * q + 3]);
+      __syncwarp();
+      float v[16];
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q) {
+        const float4 f = *reinterpret_cast<const float4 *>(mine + staged(rl + 16 * (q >> 1), (g.lane & 1) * 2 + (q & 1)));
+        v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
+      }
+      __syncwarp();
+      const int32_t at = c + 16 * h + (int32_t)(g.lane & 1) * 8;
+      const bool put0 = in0 && at < g.cols, put1 = in1 && at < g.cols;
+      if constexpr (FORWARD) {
+        const float b[8] = {x.b[h][0].x, x.b[h][0].y, x.b[h][0].z, x.b[h][0].w,
+                            x.b[h][1].x, x.b[h][1].y, x.b[h][1].z, x.b[h][1].w};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += b[i & 7];
+        if (z) put(z + (g.row + rl) * ld_z + g.col + at, ld_z, v, put0, put1);
+        activate(act, slope, v);
+        if (residual) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            float u[8];
+            Vec<T>::unpack(x.r[h][q], u);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[8 * q + i] += u[i];
+          }
+        }
+      }
+      put(out + (g.row + rl) * ld_out + g.col + at, ld_out, v, put0, put1);
+    }
+  }
+  static __device__ __forceinline__ void put(T *p, uint64_t ld, const float (&v)[16], bool put0, bool put1) {
+    float a[8], b[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a[i] = v[i], b[i] = v[8 + i];
+    if (put0) *reinterpret_cast<uint4 *>(p) = Vec<T>::pack(a);
+    if (put1) *reinterpret_cast<uint4 *>(p + 16 * ld) = Vec<T>::pack(b);
+  }
+
+  // Rows at odd addresses: lanes on consecutive columns, two rows at a time.
+  template <bool FORWARD>
+  __device__ __forceinline__ void store_odd_rows(const Strip &g, uint32_t e, int32_t c, const uint32_t (&r)[32],
+                                                 uint8_t *mine) const {
+    const int32_t r0 = g.lane >> 4;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t at = c + 16 * h + (int32_t)(g.lane & 15);
+      const bool in = at < g.cols;
+      const uint64_t col = g.col + at;
+      // the residual's 16 rows are asked for first, as bits: a conversion would wait
+      T x[16];
+      float b = 0.0f;
+      if (FORWARD && in) {
+        if (bias) b = bias[(uint64_t)e * width + col];
+        if (residual) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (r0 + 2 * i < g.high) x[i] = residual[(g.row + r0 + 2 * i) * ld_residual + col];
+        }
+      }
+#pragma unroll
+      for (uint32_t q = 0; q < 4; ++q)
+        *reinterpret_cast<uint4 *>(mine + staged(g.lane, q)) =
+            make_uint4(r[16 * h + 4 * q], r[16 * h + 4 * q + 1], r[16 * h + 4 * q + 2], r[16 * h + 4 * q + 3]);
+      __syncwarp();
+      float v[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        v[i] = *reinterpret_cast<const float *>(mine + staged(r0 + 2 * i, (g.lane & 15) >> 2) + (g.lane & 3) * 4) + b;
+      __syncwarp();
+      if constexpr (FORWARD) {
+        if (z && in) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (r0 + 2 * i < g.high) z[(g.row + r0 + 2 * i) * ld_z + col] = from_f<T>(v[i]);
+        }
+        activate(act, slope, v);
+        if (residual) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (in && r0 + 2 * i < g.high) v[i] += to_f<T>(x[i]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (in && r0 + 2 * i < g.high) out[(g.row + r0 + 2 * i) * ld_out + col] = from_f<T>(v[i]);
+    }
+  }
+
+  // dw is [out_dim][in_dim]: a column of the tile is a run of its row.
+  __device__ __forceinline__ void store_dw(const Strip &g, int32_t c, const uint32_t (&r)[32], uint8_t *mine) const {
+    const uint32_t lane = g.lane;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (uint32_t q = 0; q < 16; ++q)
+        *reinterpret_cast<uint32_t *>(mine + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4) = r[16 * h + q];
+      __syncwarp();
+      T *to = out + ((uint64_t)g.e * width + g.col + c + 16 * h) * ld_out + g.row;
+      if (vec) {  // a lane has half of a row's 32 values
+        const uint32_t j = lane >> 1, k0 = (lane & 1) * 16;
+        float v[16];
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
+          const float4 f = *reinterpret_cast<const float4 *>(mine + j * 128 + (((k0 / 4 + q) ^ (j & 7)) << 4));
+          v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
+        }
+        if (c + 16 * h + (int32_t)j < g.cols) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            float u[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
+            if ((int32_t)(k0 + 8 * q) < g.high) *reinterpret_cast<uint4 *>(to + j * ld_out + k0 + 8 * q) = Vec<T>::pack(u);
+          }
+        }
+      } else {  // rows at odd addresses: a row's 32 values by 32 lanes
+#pragma unroll
+        for (uint32_t q = 0; q < 16; ++q) {
+          const float x = *reinterpret_cast<const float *>(mine + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4);
+          if (c + 16 * h + (int32_t)q < g.cols && (int32_t)lane < g.high) to[q * ld_out + lane] = from_f<T>(x);
+        }
+      }
+      __syncwarp();
+    }
+  }
+
+  // Rows of no expert, and the gradient of an expert without rows.
+  __device__ __forceinline__ void zero_rows(const Strip &g) const {
+    for (int32_t r = 0; r < min(g.high, 32); ++r)
+      for (int32_t c = (int32_t)g.lane; c < g.cols; c += 32) {
+        out[(g.row + r) * ld_out + g.col + c] = from_f<T>(0.0f);
+        if (z) z[(g.row + r) * ld_z + g.col + c] = from_f<T>(0.0f);
+      }
+  }
+  __device__ __forceinline__ void zero_dw(const Strip &g) const {
+    for (int32_t c = 0; c < g.cols; ++c)
+      if ((int32_t)g.lane < g.high) out[((uint64_t)g.e * width + g.col + c) * ld_out + g.row + g.lane] = from_f<T>(0.0f);
+  }
+};
+
 // ------------------------------------------------------------ the kernel
 
-template <int MODE, int BN>
+template <int MODE, int BN, typename T>
 __global__ void __launch_bounds__(threads(MODE), 1)
     k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32,
              const __grid_constant__ CUtensorMap map_b, const LinearArgs a) {
@@ -283,6 +480,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     for (uint32_t i = 0; i < kStages; ++i) {
       mbar_init(saddr(&s.full[i]), 1);
       mbar_init(saddr(&s.copied[i]), 32 * copy_warps(MODE));
+      mbar_init(saddr(&s.go[i]), 1);
       mbar_init(saddr(&s.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -348,6 +546,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
             for (uint32_t j = 0; j < BN / 64; ++j) tma_2d(sb + j * 8192, &map_b, bar, col + (int32_t)j * 64, begin + k);
           } else {
             mbar_arrive(bar);  // the copying warps bring all of it
+            if (!a.rows) mbar_arrive(saddr(&s.go[st]));
           }
         }
         __syncwarp();
@@ -358,7 +557,8 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
         mbar_wait(saddr(&s.full[j % kStages]), (j / kStages) & 1);
   } else if (warp == 1) {
-    const uint32_t idesc = (1u << 4) | (a.bf16 << 7) | (a.bf16 << 10) | ((MODE == kDw ? 1u : 0u) << 15) |
+    constexpr uint32_t kBf16 = std::is_same<T, __half>::value ? 0 : 1;
+    constexpr uint32_t idesc = (1u << 4) | (kBf16 << 7) | (kBf16 << 10) | ((MODE == kDw ? 1u : 0u) << 15) |
                            ((MODE != kForward ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((kRows >> 4) << 24);
     // 16 of the contraction: 32 bytes along a K-major row, 16 rows of an MN-major block
     constexpr uint32_t kStepA = MODE == kDw ? 2048 >> 4 : 32 >> 4, kStepB = MODE != kForward ? 2048 >> 4 : 32 >> 4;
@@ -418,7 +618,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     const uint64_t pitch = a.ld_x * 2, pitch_dz = a.ld_dz * 2;
     const uint32_t *rows = (const uint32_t *)a.rows;
     const uint32_t x_rows = a.x_rows, depth = a.depth, width = a.width, height = a.height;
-    uint32_t issued = 0;
+    uint32_t issued = 0, went = 0;  // went: phase of each stage's go barrier
     bool ok = MODE == kDw || (MODE == kForward && rows);  // else there is nothing to copy
     for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
       const Tile o = tiles.at(t);
@@ -455,7 +655,21 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       // places from chunk to chunk, for a register copy would wait for the loads
       const auto step = [&](uint32_t c, int32_t (&next)[kMany], int32_t (&later)[kMany]) {
         const uint32_t st = issued % kStages;
-        ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.empty[st]), ((issued / kStages) & 1) ^ 1));
+        if (MODE == kDw && !rows) {
+          // Only the chunk in which the expert ends is copied.  Its stage is handed over
+          // by the TMA warp: nothing would hold these warps to the pace of the empty
+          // barriers, and two phases later a barrier looks like before.
+          if ((c + 1) * kChunk <= o.depth) {
+            ++issued;
+            return;
+          }
+          ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.go[st]), (went >> st) & 1));
+          went ^= 1u << st;
+          fetch(o.begin + c * kChunk + first, next);
+          look(o.begin + c * kChunk + first, next);
+        } else {
+          ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.empty[st]), ((issued / kStages) & 1) ^ 1));
+        }
         if (!ok) return;
         ++issued;
         const uint32_t sa = saddr(ring) + st * kStage, sb = sa + kABytes;
@@ -478,40 +692,36 @@ __global__ void __launch_bounds__(threads(MODE), 1)
           copy_arrive(saddr(&s.copied[st]));
         } else {
           const bool whole = (c + 1) * kChunk <= o.depth;
-          if (!rows && whole && (c + 2) * kChunk <= o.depth) return;
-          fetch(o.begin + (c + 2) * kChunk + first, later);
-          if (rows || !whole) {
+          if (rows) fetch(o.begin + (c + 2) * kChunk + first, later);
 #pragma unroll
-            for (uint32_t j = 0; j < 2; ++j) {
-              const uint32_t col = o.row + j * 64;
-              if (col + 64 <= height) {
+          for (uint32_t j = 0; j < 2; ++j) {
+            const uint32_t col = o.row + j * 64;
+            if (col + 64 <= height) {
 #pragma unroll
-                for (int i = 0; i < kMany; ++i)
-                  copy16(sa + j * 8192 + (i & 1 ? to1 : to0) + i * 512, src[i] + (uint64_t)col * 2, (zeros >> i) & 1);
-              } else {
-                const uint32_t n = col + piece * 8 < height ? min(16u, (height - col - piece * 8) * 2) : 0u;
+              for (int i = 0; i < kMany; ++i)
+                copy16(sa + j * 8192 + (i & 1 ? to1 : to0) + i * 512, src[i] + (uint64_t)col * 2, (zeros >> i) & 1);
+            } else {
+              const uint32_t n = col + piece * 8 < height ? min(16u, (height - col - piece * 8) * 2) : 0u;
 #pragma unroll
-                for (int i = 0; i < kMany; ++i)
-                  copy16_part(sa + j * 8192 + (i & 1 ? to1 : to0) + i * 512, n ? src[i] + (uint64_t)col * 2 : x,
-                              (zeros >> i) & 1 ? 0u : n);
-              }
+              for (int i = 0; i < kMany; ++i)
+                copy16_part(sa + j * 8192 + (i & 1 ? to1 : to0) + i * 512, n ? src[i] + (uint64_t)col * 2 : x,
+                            (zeros >> i) & 1 ? 0u : n);
             }
-            if (!whole) {
-              for (int i = 0; i < kMany; ++i) {
-                const uint32_t at = c * kChunk + first + i * 4 + sub;
-#pragma unroll
-                for (uint32_t j = 0; j < BN / 64; ++j) {
-                  const uint32_t col = o.col + j * 64 + piece * 8;
-                  const uint32_t n = at < o.depth && col < width ? min(16u, (width - col) * 2) : 0u;
-                  copy16_part(sb + j * 8192 + (i & 1 ? to1 : to0) + i * 512,
-                              n ? dz + (uint64_t)(o.begin + at) * pitch_dz + col * 2 : dz, n);
-                }
-              }
-            }
-            copy_arrive(saddr(&s.copied[st]));
           }
-          if (!rows) fetch(o.begin + (c + 1) * kChunk + first, next);  // chunks may have been passed over
-          look(o.begin + (c + 1) * kChunk + first, next);
+          if (!whole) {
+            for (int i = 0; i < kMany; ++i) {
+              const uint32_t at = c * kChunk + first + i * 4 + sub;
+#pragma unroll
+              for (uint32_t j = 0; j < BN / 64; ++j) {
+                const uint32_t col = o.col + j * 64 + piece * 8;
+                const uint32_t n = at < o.depth && col < width ? min(16u, (width - col) * 2) : 0u;
+                copy16_part(sb + j * 8192 + (i & 1 ? to1 : to0) + i * 512,
+                            n ? dz + (uint64_t)(o.begin + at) * pitch_dz + col * 2 : dz, n);
+              }
+            }
+          }
+          copy_arrive(saddr(&s.copied[st]));
+          if (rows) look(o.begin + (c + 1) * kChunk + first, next);
         }
       };
       for (uint32_t c = 0; ok && c < chunks; c += 2) {
@@ -522,188 +732,38 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     if (!ok) asm volatile("cp.async.wait_all;\n" ::: "memory");  // none lands after the CTA's end
   } else {
     const uint32_t w = warp - 4, quarter = warp & 3;
-    // copies of the arguments: with asm in the loop the compiler would read them from
-    // the parameters at every use
-    const float *const bias = a.bias;
-    const uint16_t *const residual = (const uint16_t *)a.residual;
-    uint16_t *const out = (uint16_t *)a.out, *const z = (uint16_t *)a.z;
-    const uint64_t ld_out = a.ld_out, ld_z = a.ld_z, ld_residual = a.ld_residual;
-    const uint32_t width = a.width, act = a.activation;
-    const float slope = a.slope;
-    const bool vec = a.vec_out;
+    const Epilogue<T> ep(a);
     const uint32_t part = (w >> 2) * (BN / 2);  // each set of four warps takes half of the columns
     uint8_t *mine = staging + w * 32 * kStageCols * 4;
-    const uint32_t base = saddr(mine);
-    const bool bf16 = a.bf16;
     uint32_t acc = 0;
     for (uint64_t t = blockIdx.x; t < tiles.total; t += gridDim.x) {
       const Tile o = tiles.at(t);
-      const bool zero = o.depth == 0;
-      const int32_t high = (int32_t)o.rows - (int32_t)(quarter * 32);  // rows of this warp inside
-      const uint64_t row0 = o.row + quarter * 32;
-      // The bias and the residual of 16 columns, asked for 16 columns ahead: the first
-      // ones while the tile is still being multiplied.
-      float4 bias0, bias1;
-      uint4 res0, res1;
-      const auto ask = [&](uint32_t c0) {
-        const uint32_t col = o.col + c0 + (lane & 1) * 8;
-        bias0 = bias1 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (col >= width) return;
-        if (bias) {
-          const float4 *b = reinterpret_cast<const float4 *>(bias + (uint64_t)o.e * width + col);
-          bias0 = b[0];
-          bias1 = b[1];
-        }
-        if (residual) {
-          const uint16_t *r = residual + (row0 + (lane >> 1)) * ld_residual + col;
-          if ((int32_t)(lane >> 1) < high) res0 = *reinterpret_cast<const uint4 *>(r);
-          if ((int32_t)(lane >> 1) + 16 < high) res1 = *reinterpret_cast<const uint4 *>(r + 16 * ld_residual);
-        }
-      };
-      const bool asks = MODE == kForward && !zero && high > 0 && vec;
-      if (asks) ask(part);
-      if (!zero) {
-        if (!__all_sync(0xFFFFFFFFu, wait(saddr(&s.acc_full[acc & 1]), (acc >> 1) & 1))) break;
-        fence_after();
+      const Strip g{MODE == kDw ? o.e : 0u, (int32_t)o.rows - (int32_t)(quarter * 32), (uint64_t)o.row + quarter * 32,
+                    o.col + part, (int32_t)min((uint32_t)BN / 2, ep.width - min(ep.width, o.col + part)), lane};
+      if (o.depth == 0) {
+        if (MODE == kDw) ep.zero_dw(g);
+        else ep.zero_rows(g);
+        continue;
       }
-      if (high > 0) {
-        for (uint32_t c0 = part; c0 < part + BN / 2 && o.col + c0 < width; c0 += kStageCols) {
-          uint32_t r[16];
-          if (!zero) {
-            tmem_ld16(tmem + ((quarter * 32) << 16) + (acc & 1) * BN + c0, r);
-            tmem_wait_ld();
-          }
-          if constexpr (MODE == kDw) {
-            // dw is [out_dim][in_dim]: a column of the tile is a run of its row
-            float v[16] = {};
-            const uint32_t j = lane >> 1, k0 = (lane & 1) * 16;
-            if (!zero) {
-#pragma unroll
-              for (uint32_t q = 0; q < 16; ++q)
-                *reinterpret_cast<uint32_t *>(mine + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4) = r[q];
-              __syncwarp();
-#pragma unroll
-              for (uint32_t q = 0; q < 4; ++q) {
-                const float4 f = *reinterpret_cast<const float4 *>(mine + j * 128 + (((k0 / 4 + q) ^ (j & 7)) << 4));
-                v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
-              }
-            }
-            if (vec) {
-              if (o.col + c0 + j < width) {
-                const uint64_t at = ((uint64_t)o.e * width + o.col + c0 + j) * ld_out + o.row + quarter * 32 + k0;
-#pragma unroll
-                for (uint32_t q = 0; q < 2; ++q) {
-                  float u[8];
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
-                  if ((int32_t)(k0 + 8 * q) < high) store8(out, at + 8 * q, bf16, u);
-                }
-              }
-            } else {  // rows at odd addresses: a row's 32 values by 32 lanes
-#pragma unroll
-              for (uint32_t q = 0; q < 16; ++q) {
-                float x = 0.0f;
-                if (!zero) x = *reinterpret_cast<const float *>(mine + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4);
-                if (o.col + c0 + q < width && (int32_t)lane < high)
-                  store1(out, ((uint64_t)o.e * width + o.col + c0 + q) * ld_out + o.row + quarter * 32 + lane, bf16, x);
-              }
-            }
-            __syncwarp();
-            continue;
-          }
-          if (!zero) {
-#pragma unroll
-            for (uint32_t q = 0; q < 4; ++q)
-              asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(base + staged(lane, q)), "r"(r[4 * q]),
-                           "r"(r[4 * q + 1]), "r"(r[4 * q + 2]), "r"(r[4 * q + 3])
-                           : "memory");
-            __syncwarp();
-          }
-          if (!vec) {
-            // rows at odd addresses: lanes on consecutive columns, two rows at a time
-            const uint32_t col = o.col + c0 + (lane & 15);
-            if (col < width) {
-              const float b = MODE == kForward && bias && !zero ? bias[(uint64_t)o.e * width + col] : 0.0f;
-              const int32_t r0 = lane >> 4;
-              // the residual's 16 rows are asked for first, as bits: a conversion would wait
-              uint16_t x[16];
-#pragma unroll
-              for (int32_t i = 0; i < 16; ++i) {
-                x[i] = 0;
-                if (MODE == kForward && residual && !zero && r0 + 2 * i < high)
-                  x[i] = (residual)[(row0 + r0 + 2 * i) * ld_residual + col];
-              }
-#pragma unroll
-              for (int32_t it = 0; it < 16; it += 8) {
-                float v[8];
-#pragma unroll
-                for (int32_t i = 0; i < 8; ++i)
-                  v[i] = zero ? 0.0f
-                              : *reinterpret_cast<const float *>(mine + staged(r0 + 2 * (it + i), (lane & 15) >> 2) +
-                                                                 (lane & 3) * 4) + b;
-                if constexpr (MODE == kForward) {
-                  if (z) {
-#pragma unroll
-                    for (int32_t i = 0; i < 8; ++i)
-                      if (r0 + 2 * (it + i) < high) store1(z, (row0 + r0 + 2 * (it + i)) * ld_z + col, bf16, v[i]);
-                  }
-                  if (!zero) activate(act, slope, v);
-                }
-#pragma unroll
-                for (int32_t i = 0; i < 8; ++i)
-                  if (r0 + 2 * (it + i) < high)
-                    store1(out, (row0 + r0 + 2 * (it + i)) * ld_out + col, bf16, v[i] + from_bits(x[it + i], bf16));
-              }
-            }
-            __syncwarp();
-            continue;
-          }
-          const uint32_t col = o.col + c0 + (lane & 1) * 8;
-          if (col < width) {  // vec_out: whole pieces of 8 columns
-            float b[8] = {};
-            uint4 x[2];
-            if (asks) {
-              b[0] = bias0.x, b[1] = bias0.y, b[2] = bias0.z, b[3] = bias0.w;
-              b[4] = bias1.x, b[5] = bias1.y, b[6] = bias1.z, b[7] = bias1.w;
-              x[0] = res0, x[1] = res1;
-              if (c0 + kStageCols < part + BN / 2) ask(c0 + kStageCols);
-            }
-#pragma unroll
-            for (uint32_t it = 0; it < 2; ++it) {
-              const uint32_t rl = (lane >> 1) + 16 * it;
-              if ((int32_t)rl < high) {
-                float v[8] = {};
-                if (!zero) {
-                  const float4 f = *reinterpret_cast<const float4 *>(mine + staged(rl, (lane & 1) * 2));
-                  const float4 g = *reinterpret_cast<const float4 *>(mine + staged(rl, (lane & 1) * 2 + 1));
-                  v[0] = f.x + b[0], v[1] = f.y + b[1], v[2] = f.z + b[2], v[3] = f.w + b[3];
-                  v[4] = g.x + b[4], v[5] = g.y + b[5], v[6] = g.z + b[6], v[7] = g.w + b[7];
-                }
-                if constexpr (MODE == kForward) {
-                  if (z) store8(z, (row0 + rl) * ld_z + col, bf16, v);
-                  if (!zero) {
-                    activate(act, slope, v);
-                    if (residual) {
-                      float u[8];
-                      unpack8(x[it], bf16, u);
-#pragma unroll
-                      for (int i = 0; i < 8; ++i) v[i] += u[i];
-                    }
-                  }
-                }
-                store8(out, (row0 + rl) * ld_out + col, bf16, v);
-              }
-            }
-          }
-          __syncwarp();
+      typename Epilogue<T>::Ahead ahead;
+      if (MODE == kForward) ep.ask(ahead, o.e, g, 0);
+      if (!__all_sync(0xFFFFFFFFu, wait(saddr(&s.acc_full[acc & 1]), (acc >> 1) & 1))) break;
+      fence_after();
+      const uint32_t from = tmem + ((quarter * 32) << 16) + (acc & 1) * BN + part;
+      if (g.high > 0) {
+        for (int32_t c = 0; c < g.cols; c += 32) {
+          uint32_t r[32];
+          tmem_ld32(from + c, r);
+          tmem_wait_ld();
+          if constexpr (MODE == kDw) ep.store_dw(g, c, r, mine);
+          else if (ep.vec) ep.template store_rows<MODE == kForward>(g, o.e, c, r, ahead, mine);
+          else ep.template store_odd_rows<MODE == kForward>(g, o.e, c, r, mine);
         }
       }
-      if (!zero) {
-        fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(saddr(&s.acc_empty[acc & 1]));
-        ++acc;
-      }
+      fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(saddr(&s.acc_empty[acc & 1]));
+      ++acc;
     }
   }
   fence_before();
@@ -948,7 +1008,7 @@ unsigned int *status_word() {
   return p;
 }
 
-template <int MODE, int BN>
+template <int MODE, int BN, typename T>
 cudaError_t launch_tile(const Operand &A, const Operand &B, LinearArgs a, uint64_t tiles_bound, int sms, cudaStream_t st) {
   CUtensorMap ma, ma32, mb;
   if (!make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 128) || !make_map(&ma32, A, 2, 64, 32) ||
@@ -963,12 +1023,12 @@ cudaError_t launch_tile(const Operand &A, const Operand &B, LinearArgs a, uint64
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !((allowed.load() >> dev) & 1)) {
-    e = cudaFuncSetAttribute(k_linear<MODE, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes);
+    e = cudaFuncSetAttribute(k_linear<MODE, BN, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes);
     if (e != cudaSuccess) return e;
     if (dev < 64) allowed.fetch_or(1ull << dev);
   }
   const unsigned grid = (unsigned)std::min<uint64_t>(tiles_bound, (uint64_t)sms);
-  return launch_pdl(k_linear<MODE, BN>, grid, threads(MODE), kSharedBytes, st, ma, ma32, mb, a);
+  return launch_pdl(k_linear<MODE, BN, T>, grid, threads(MODE), kSharedBytes, st, ma, ma32, mb, a);
 }
 
 // Row tiles of num_rows rows in num_experts segments (and those of no expert), at most.
@@ -980,17 +1040,22 @@ uint64_t row_tiles_bound(uint64_t num_rows, uint64_t num_experts) {
 // an expert has few rows on average.  Such tiles stream weights, and only the two
 // warps that hold the rows work on their columns (256 rows of 32 experts, 1,024 ->
 // 2,048, gelu, bias and residual: 39.7 us at 256 columns, 36.6 at 128, 40.0 at 64).
-template <int MODE>
-cudaError_t launch_product(const Operand &A, const Operand &B, const LinearArgs &a, cudaStream_t st) {
+template <int MODE, typename T>
+cudaError_t launch_product_of(const Operand &A, const Operand &B, const LinearArgs &a, cudaStream_t st) {
   const int sms = sm_count();
   const uint64_t high = MODE == kDw ? (uint64_t)a.num_experts * ((a.height + kRows - 1) / kRows)
                                     : row_tiles_bound(a.num_rows, a.num_experts);
   if (high == 0) return cudaSuccess;
   const auto tiles = [&](uint32_t bn) { return high * ((a.width + bn - 1) / bn); };
   const bool thin = MODE != kDw && a.num_rows <= 32ull * a.num_experts;
-  if (!thin && tiles(256) >= (uint64_t)sms) return launch_tile<MODE, 256>(A, B, a, tiles(256), sms, st);
-  if (tiles(128) >= (uint64_t)sms) return launch_tile<MODE, 128>(A, B, a, tiles(128), sms, st);
-  return launch_tile<MODE, 64>(A, B, a, tiles(64), sms, st);
+  if (!thin && tiles(256) >= (uint64_t)sms) return launch_tile<MODE, 256, T>(A, B, a, tiles(256), sms, st);
+  if (tiles(128) >= (uint64_t)sms) return launch_tile<MODE, 128, T>(A, B, a, tiles(128), sms, st);
+  return launch_tile<MODE, 64, T>(A, B, a, tiles(64), sms, st);
+}
+
+template <int MODE>
+cudaError_t launch_product(const Operand &A, const Operand &B, const LinearArgs &a, cudaStream_t st) {
+  return a.bf16 ? launch_product_of<MODE, __nv_bfloat16>(A, B, a, st) : launch_product_of<MODE, __half>(A, B, a, st);
 }
 
 // ------------------------------------------------------------ workspaces

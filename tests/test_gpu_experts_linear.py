@@ -361,3 +361,30 @@ def test_a_layer_on_its_own_stream_and_in_a_graph(ntc):
     y = ntc.linear(args[1], args[2][0], stream=s)
     s.synchronize()
     assert torch.equal(y, ntc.linear(args[1], args[2][0]))
+
+
+@pytest.mark.parametrize("rows_of", ["whole chunks", "any", "one long and many short"])
+def test_dw_of_long_contractions(ntc, rows_of):
+    """Many chunks per tile and many tiles per CTA: no wait of any warp runs out, whatever its pace."""
+    g = gen(21)
+    E, K, N = 16, 512, 1024
+    counts = {"whole chunks": [2048] * E, "any": [2048 - 37 * e for e in range(E)],
+              "one long and many short": [20000] + [e for e in range(1, E)]}[rows_of]
+    offsets = torch.tensor([0] + counts, device="cuda").cumsum(0).int()
+    M = sum(counts)
+    x, dy = normal(g, M, K, dtype=torch.bfloat16), normal(g, M, N, dtype=torch.bfloat16)
+    w = normal(g, E, N, K, std=0.05, dtype=torch.bfloat16)
+    want = R.linear_backward(dy, x, w, None, None, offsets, "none")
+    rows = torch.arange(M, dtype=torch.int32, device="cuda")
+    for r in (None, rows):
+        for _ in range(10):
+            _, dw, _ = ntc.linear_backward(dy, x, w, rows=r, offsets=offsets, need=("dw",))
+        ntc.ntc_linear_status(torch.cuda.current_stream().cuda_stream)
+        R.assert_within(dw, *want[1])
+    for _ in range(10):
+        dx, _, _ = ntc.linear_backward(dy, x, w, offsets=offsets, need=("dx",))
+        y = ntc.linear(x, w, rows=rows, offsets=offsets)
+    ntc.ntc_linear_status(torch.cuda.current_stream().cuda_stream)
+    R.assert_within(dx, *want[0])
+    ref, _, bound, _ = R.linear(x, w, None, None, offsets)
+    R.assert_within(y, ref, bound)
