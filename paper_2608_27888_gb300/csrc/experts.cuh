@@ -38,6 +38,25 @@ inline int sm_count() {
   return sms;
 }
 
+// -------------------------------------------------------- special functions
+
+// exp(x) and 1 / x by the hardware's approximations (2 ulp and 1 ulp, and exp the
+// rounding of x log2(e)); results below 2^-126 are 0.  One instruction each: the
+// forms that keep subnormals take several, and the kernels here that use them are
+// bound by instructions.
+__device__ __forceinline__ float quick_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float quick_exp(float x) { return quick_exp2(x * 1.44269504f); }
+__device__ __forceinline__ float quick_inverse(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float quick_sigmoid(float x) { return quick_inverse(1.0f + quick_exp(-x)); }
+
 // ------------------------------------------------------------- element types
 
 template <typename T>

@@ -776,20 +776,28 @@ __global__ void __launch_bounds__(threads(MODE), 1)
 
 // ------------------------------------------------------------ dz, db, copies
 
-__device__ __forceinline__ float act_slope(uint32_t act, float slope, float z) {
-  switch (act) {
-    case NTC_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
-    case NTC_ACT_LEAKY: return z > 0.0f ? 1.0f : slope;
-    case NTC_ACT_GELU: {
+// g *= act'(z), one test of the kind for all values.
+template <int N>
+__device__ __forceinline__ void times_slope(uint32_t act, float slope, const float (&z)[N], float (&g)[N]) {
+  if (act == NTC_ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) g[i] *= z[i] > 0.0f ? 1.0f : 0.0f;
+  } else if (act == NTC_ACT_LEAKY) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) g[i] *= z[i] > 0.0f ? 1.0f : slope;
+  } else if (act == NTC_ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
       float e;
-      const float p = normal_cdf(z, e);
-      return fmaf(z * 0.39894228f, e, p);
+      const float p = normal_cdf(z[i], e);
+      g[i] *= fmaf(z[i] * 0.39894228f, e, p);
     }
-    case NTC_ACT_SILU: {
-      const float s = __fdividef(1.0f, 1.0f + __expf(-z));
-      return s * fmaf(z, 1.0f - s, 1.0f);
+  } else if (act == NTC_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float s = quick_sigmoid(z[i]);
+      g[i] *= s * fmaf(z[i], 1.0f - s, 1.0f);
     }
-    default: return 1.0f;
   }
 }
 
@@ -816,7 +824,7 @@ struct TableShared {
 // rows' loads in flight.  VEC: every row of dy and z is whole 16-byte pieces.  dz's
 // pads are never read: TMA's matrix ends at the width.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(kDzThreads) k_dz(const DzArgs a) {
+__global__ void __launch_bounds__(kDzThreads, VEC ? 4 : 2) k_dz(const DzArgs a) {
   extern __shared__ uint8_t raw[];
   TableShared &s = *reinterpret_cast<TableShared *>(raw);
   __shared__ float sums[8][kDzCols];
@@ -827,7 +835,9 @@ __global__ void __launch_bounds__(kDzThreads) k_dz(const DzArgs a) {
   // this lane's columns: a piece of eight, or eight 32 apart
   const auto col = [&](uint32_t i) { return blockIdx.x * kDzCols + (VEC ? lane * 8 + i : lane + 32 * i); };
   const uint32_t total = s.tile[a.num_experts];
-  const bool acts = a.activation != NTC_ACT_NONE;
+  const uint32_t act = a.activation;
+  const float slope = a.slope;
+  const bool acts = act != NTC_ACT_NONE;
   const T *dy = (const T *)a.dy, *z = (const T *)a.z;
   T *dz = (T *)a.dz;
   for (uint32_t q = blockIdx.y; q < total; q += gridDim.y) {
@@ -854,36 +864,38 @@ __global__ void __launch_bounds__(kDzThreads) k_dz(const DzArgs a) {
             float g[8], v[8];
             Vec<T>::unpack(qg[u], g);
             Vec<T>::unpack(qz[u], v);
-            if (acts) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) g[i] *= act_slope(a.activation, a.slope, v[i]);
-            }
+            if (acts) times_slope(act, slope, v, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += g[i];
             if (dz) *reinterpret_cast<uint4 *>(dz + (uint64_t)(row + r) * a.pitch + col(0)) = Vec<T>::pack(g);
           }
         }
     } else {
-      for (uint32_t r0 = warp; r0 < rows; r0 += 16) {
-        T g[2][8], v[2][8];  // two rows' loads in flight
+      for (uint32_t r0 = warp; r0 < rows; r0 += 32) {
+        T qg[4][8], qz[4][8];
 #pragma unroll
-        for (uint32_t u = 0; u < 2; ++u)
+        for (uint32_t u = 0; u < 4; ++u)
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < 8; ++i) {
+            qg[u][i] = qz[u][i] = from_f<T>(0.0f);
             if (col(i) < a.width && r0 + 8 * u < rows) {
-              g[u][i] = dy[(uint64_t)(row + r0 + 8 * u) * a.ld_dy + col(i)];
-              if (acts) v[u][i] = z[(uint64_t)(row + r0 + 8 * u) * a.ld_z + col(i)];
+              qg[u][i] = dy[(uint64_t)(row + r0 + 8 * u) * a.ld_dy + col(i)];
+              if (acts) qz[u][i] = z[(uint64_t)(row + r0 + 8 * u) * a.ld_z + col(i)];
             }
+          }
 #pragma unroll
-        for (uint32_t u = 0; u < 2; ++u)
+        for (uint32_t u = 0; u < 4; ++u) {
+          float g[8], v[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (col(i) < a.width && r0 + 8 * u < rows) {
-              float x = to_f<T>(g[u][i]);
-              if (acts) x *= act_slope(a.activation, a.slope, to_f<T>(v[u][i]));
-              sum[i] += x;
-              if (dz) dz[(uint64_t)(row + r0 + 8 * u) * a.pitch + col(i)] = from_f<T>(x);
-            }
+          for (int i = 0; i < 8; ++i) g[i] = to_f<T>(qg[u][i]), v[i] = to_f<T>(qz[u][i]);
+          times_slope(act, slope, v, g);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            sum[i] += g[i];  // 0 outside
+            if (dz && col(i) < a.width && r0 + 8 * u < rows)
+              dz[(uint64_t)(row + r0 + 8 * u) * a.pitch + col(i)] = from_f<T>(g[i]);
+          }
+        }
       }
     }
     if (a.part) {
@@ -934,25 +946,33 @@ __global__ void __launch_bounds__(kDzThreads)
   }
 }
 
-// A matrix TMA cannot read, copied to rows of `pitch` elements (the pads hold 0).
-__global__ void __launch_bounds__(256)
-    k_pack(const uint16_t *src, uint64_t ld, uint64_t stride, uint32_t cols, uint32_t rows, uint64_t total, uint16_t *dst,
-           uint32_t pitch) {
+// Matrices TMA cannot read, copied to rows of `pitch` elements (the pads hold 0): the
+// operand x, the operand w, or both, in one launch.
+struct Pack {
+  const uint16_t *src;
+  uint16_t *dst;
+  uint64_t ld, stride, pieces;  // pieces of eight elements, of all matrices
+  uint32_t cols, rows, pitch;
+};
+__global__ void __launch_bounds__(256) k_pack(const Pack first, const Pack second) {
   pdl_wait();
   pdl_trigger();
-  const uint32_t pieces = pitch / 8;
+  const uint64_t total = first.pieces + second.pieces;
   for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (uint64_t)gridDim.x * 256) {
-    const uint64_t row = i / pieces;  // of all matrices
-    const uint32_t c = (uint32_t)(i - row * pieces) * 8;
-    const uint64_t m = row / rows;
-    const uint16_t *p = src + m * stride + (row - m * rows) * ld + c;
+    const bool one = i < first.pieces;
+    const Pack &k = one ? first : second;
+    const uint64_t j = one ? i : i - first.pieces;
+    const uint32_t wide = k.pitch / 8;
+    const uint64_t row = j / wide, m = row / k.rows;  // row: of all matrices
+    const uint32_t c = (uint32_t)(j - row * wide) * 8;
+    const uint16_t *p = k.src + m * k.stride + (row - m * k.rows) * k.ld + c;
     uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t lo = c + 2 * j < cols ? p[2 * j] : 0u, hi = c + 2 * j + 1 < cols ? p[2 * j + 1] : 0u;
-      w[j] = lo | (hi << 16);
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t lo = c + 2 * q < k.cols ? p[2 * q] : 0u, hi = c + 2 * q + 1 < k.cols ? p[2 * q + 1] : 0u;
+      w[q] = lo | (hi << 16);
     }
-    *reinterpret_cast<uint4 *>(dst + row * pitch + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4 *>(k.dst + row * k.pitch + c) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -1118,32 +1138,34 @@ ntc_status check_workspace(const void *p, size_t have, size_t need) {
   return NTC_OK;
 }
 
-cudaError_t pack(const void *src, uint64_t ld, uint64_t stride, uint32_t cols, uint64_t rows, uint64_t many, void *dst,
-                 cudaStream_t st) {
-  const uint32_t pitch = (uint32_t)round8(cols);
-  const uint64_t total = rows * many * (pitch / 8);
-  const unsigned grid = (unsigned)std::min<uint64_t>((total + 255) / 256, (uint64_t)sm_count() * 32);
-  return launch_pdl(k_pack, grid, 256, 0, st, (const uint16_t *)src, ld, stride, cols, (uint32_t)rows, total,
-                    (uint16_t *)dst, pitch);
-}
-
-// The operands x and w, through the workspace where TMA cannot read them.
-cudaError_t operand_x(const ntc_linear_desc &d, const void *x, uint8_t *&ws, Operand *o, cudaStream_t st) {
-  *o = Operand{x, d.in_dim, d.num_x_rows, d.ld_x};
-  if (!x_packs(d, x)) return cudaSuccess;
-  const cudaError_t e = pack(x, d.ld_x, 0, d.in_dim, d.num_x_rows, 1, ws, st);
-  *o = Operand{ws, d.in_dim, d.num_x_rows, round8(d.in_dim)};
-  ws += x_bytes(d);
-  return e;
-}
-cudaError_t operand_w(const ntc_linear_desc &d, const void *w, uint8_t *&ws, Operand *o, cudaStream_t st) {
-  *o = Operand{w, d.in_dim, d.out_dim, d.ld_w, d.num_experts, d.stride_w};
-  if (!w_packs(d, w)) return cudaSuccess;
-  const cudaError_t e = pack(w, d.ld_w, d.stride_w, d.in_dim, d.out_dim, d.num_experts, ws, st);
-  const uint64_t p = round8(d.in_dim);
-  *o = Operand{ws, d.in_dim, d.out_dim, p, d.num_experts, p * d.out_dim};
-  ws += w_bytes(d);
-  return e;
+// The operands x and w, through the workspace where TMA cannot read them (a null one
+// is not wanted).
+cudaError_t operands(const ntc_linear_desc &d, const void *x, const void *w, uint8_t *ws, Operand *X, Operand *W,
+                     cudaStream_t st) {
+  const uint32_t pitch = (uint32_t)round8(d.in_dim);
+  Pack job[2] = {};
+  int jobs = 0;
+  if (x) {
+    *X = Operand{x, d.in_dim, d.num_x_rows, d.ld_x};
+    if (x_packs(d, x)) {
+      job[jobs++] = Pack{(const uint16_t *)x, (uint16_t *)ws, d.ld_x, 0, d.num_x_rows * (pitch / 8), d.in_dim,
+                         (uint32_t)d.num_x_rows, pitch};
+      *X = Operand{ws, d.in_dim, d.num_x_rows, pitch};
+      ws += x_bytes(d);
+    }
+  }
+  if (w) {
+    *W = Operand{w, d.in_dim, d.out_dim, d.ld_w, d.num_experts, d.stride_w};
+    if (w_packs(d, w)) {
+      job[jobs++] = Pack{(const uint16_t *)w, (uint16_t *)ws, d.ld_w, d.stride_w,
+                         (uint64_t)d.num_experts * d.out_dim * (pitch / 8), d.in_dim, d.out_dim, pitch};
+      *W = Operand{ws, d.in_dim, d.out_dim, pitch, d.num_experts, (uint64_t)pitch * d.out_dim};
+    }
+  }
+  if (jobs == 0) return cudaSuccess;
+  const uint64_t pieces = job[0].pieces + job[1].pieces;
+  const unsigned grid = (unsigned)std::min<uint64_t>((pieces + 255) / 256, (uint64_t)sm_count() * 32);
+  return launch_pdl(k_pack, grid, 256, 0, st, job[0], job[1]);
 }
 
 }  // namespace
@@ -1193,10 +1215,8 @@ extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void
               (!residual || rows_are_vec(residual, d.ld_residual, 2)) && ((uintptr_t)bias & 15) == 0;
   a.status = status_word();
   if (!a.status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
-  uint8_t *ws = (uint8_t *)workspace;
   Operand X, W;
-  cudaError_t e = operand_x(d, x, ws, &X, st);
-  if (e == cudaSuccess) e = operand_w(d, w, ws, &W, st);
+  cudaError_t e = operands(d, x, w, (uint8_t *)workspace, &X, &W, st);
   if (e == cudaSuccess) e = launch_product<kForward>(X, W, a, st);
   return op_cuda(e, "ntc_linear");
 }
@@ -1277,24 +1297,22 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
   a.bf16 = d.type == NTC_TYPE_BF16;
   a.ld_out = d.in_dim;
   a.status = status;
+  Operand X, W;
+  if (e == cudaSuccess) e = operands(d, dw ? x : nullptr, dx ? w : nullptr, ws, &X, &W, st);
   if (e == cudaSuccess && dx) {
-    Operand W;
-    e = operand_w(d, w, ws, &W, st);
     a.out = dx;
     a.depth = d.out_dim;
     a.vec_out = rows_are_vec(dx, d.in_dim, 2);
-    if (e == cudaSuccess) e = launch_product<kDx>(Z, W, a, st);
+    e = launch_product<kDx>(Z, W, a, st);
   }
   if (e == cudaSuccess && dw) {
-    Operand X;
-    e = operand_x(d, x, ws, &X, st);
     a.out = dw;
     a.rows = rows;
     a.x_rows = (uint32_t)d.num_x_rows;
     a.width = d.out_dim;
     a.height = d.in_dim;
     a.vec_out = rows_are_vec(dw, d.in_dim, 2);
-    if (e == cudaSuccess) e = launch_product<kDw>(X, Z, a, st);
+    e = launch_product<kDw>(X, Z, a, st);
   }
   return op_cuda(e, what);
 }

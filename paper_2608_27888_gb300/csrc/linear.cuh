@@ -29,13 +29,14 @@ struct LinearArgs {
 // Phi's is below 1e-7, less than one rounding to bf16 or fp16 of anything above 2^-13).
 // Fewer instructions than erff and expf, which bound k_dz.
 __device__ __forceinline__ float normal_cdf(float z, float &e) {
-  e = __expf(-0.5f * z * z);
-  const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
-  float q = fmaf(1.061405429f, t, -1.453152027f);
-  q = fmaf(q, t, 1.421413741f);
-  q = fmaf(q, t, -0.284496736f);
-  q = fmaf(q, t, 0.254829592f);
-  q *= 0.5f * t * e;  // the upper tail of |z|
+  e = quick_exp2(-0.72134752f * z * z);  // log2(e) / 2
+  const float t = quick_inverse(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
+  // the upper tail of |z|: half of the formula's polynomial, times t e
+  float q = fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+  q = fmaf(q, t, 0.5f * 1.421413741f);
+  q = fmaf(q, t, 0.5f * -0.284496736f);
+  q = fmaf(q, t, 0.5f * 0.254829592f);
+  q *= t * e;
   return z < 0.0f ? q : 1.0f - q;
 }
 
@@ -55,7 +56,7 @@ __device__ __forceinline__ void activate(uint32_t act, float slope, float (&v)[N
     }
   } else if (act == NTC_ACT_SILU) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = __fdividef(v[i], 1.0f + __expf(-v[i]));
+    for (int i = 0; i < N; ++i) v[i] *= quick_sigmoid(v[i]);
   }
 }
 

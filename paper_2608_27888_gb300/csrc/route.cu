@@ -42,8 +42,6 @@ __device__ __forceinline__ bool live_logit(float &l) {
   return live;
 }
 
-__device__ __forceinline__ float sigmoid(float l) { return __fdividef(1.0f, 1.0f + __expf(-l)); }
-
 // V consecutive elements from p on, n of them inside the row.
 template <typename T, int V>
 __device__ __forceinline__ void load_run(const T *p, int n, bool vec, float (&l)[V]) {
@@ -274,7 +272,7 @@ __global__ void __launch_bounds__(kWarps * 32)
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        s[i] = __expf(l[i] - m);
+        s[i] = quick_exp(l[i] - m);
         sum += s[i];
       }
       sum = group_sum<G>(sum);
@@ -283,7 +281,7 @@ __global__ void __launch_bounds__(kWarps * 32)
       for (int i = 0; i < V; ++i) s[i] *= inverse;
     } else {
 #pragma unroll
-      for (int i = 0; i < V; ++i) s[i] = sigmoid(l[i]);
+      for (int i = 0; i < V; ++i) s[i] = quick_sigmoid(l[i]);
     }
 #pragma unroll
     for (int i = 0; i < V; ++i) c[i] = l[i] > least[i] ? s[i] + b[i] : -INFINITY;
@@ -406,13 +404,13 @@ __global__ void __launch_bounds__(kWarps * 32)
       float sum = 0.0f;
       for (uint32_t e = sub; e < E; e += G) {
         float v = to_f<T>(l[e]);
-        if (live_logit(v)) sum += expf(v - m);
+        if (live_logit(v)) sum += quick_exp(v - m);
       }
       z = group_sum<G>(sum);
     } else if (softmax) {
       m = value_of(group_max<G>(live ? key_of(lj) : 0u));
     }
-    const float s = !live ? 0.0f : softmax ? expf(lj - m) / z : sigmoid(lj);
+    const float s = !live ? 0.0f : softmax ? quick_exp(lj - m) / z : quick_sigmoid(lj);
     float ds = dw;
     if (d.renormalize) {
       const float sum = group_sum<G>(s), dot = group_sum<G>(dw * s);
@@ -454,7 +452,7 @@ __global__ void __launch_bounds__(kWarps * 32)
 #pragma unroll
           for (int i = 0; i < N; ++i) {
             float x = i < have ? to_f<T>(lj[e + i]) : -INFINITY;
-            f[i] = live_logit(x) ? f[i] - expf(x - mj) / zj * dj : 0.0f;
+            f[i] = live_logit(x) ? f[i] - quick_exp(x - mj) / zj * dj : 0.0f;
           }
         }
         store_vec<T>(out + e, have, vec, f);
