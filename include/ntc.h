@@ -470,7 +470,8 @@ NTC_API ntc_status ntc_expert_order(const int32_t *ids, size_t n, uint32_t top_k
  * reads a row of zeros.
  * Any width, stride and alignment is taken; where TMA cannot read an operand
  * (address not a multiple of 16 bytes, or leading dimension not of 8 elements)
- * the call copies it into the workspace first. */
+ * the call copies it into the workspace first, and gathered rows of large products,
+ * too. */
 typedef struct {
   ntc_type type;        /* NTC_TYPE_FP16 or NTC_TYPE_BF16: x, w, y, z, residual */
   uint32_t in_dim;      /* K, 1 .. 2^20                                        */
@@ -490,7 +491,8 @@ typedef struct {
 
 /* Bytes of workspace for a call with this descriptor and these operands (16-byte
  * aligned when not 0); 0 for a descriptor the call would refuse. */
-NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, const void *w);
+NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, const int32_t *rows,
+                                    const void *w);
 
 /* x[num_x_rows][ld_x], w[E][N][ld_w], bias[E][N] fp32 (contiguous) or NULL,
  * residual[num_rows][ld_residual] or NULL, rows[num_rows] int32 or NULL,
@@ -510,7 +512,7 @@ NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void *x, const 
  * summed for db before that rounding.  dx, dw in the operands' type.  act'(0) is
  * 0 (ReLU) or leaky_slope.  The sums' order is fixed: equal calls give equal bits. */
 NTC_API size_t ntc_linear_backward_workspace(const ntc_linear_desc *desc, const void *dy, const void *x,
-                                             const void *w);
+                                             const int32_t *rows, const void *w);
 NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, const void *dy, const void *z, const void *x,
                                        const int32_t *rows, const int32_t *offsets, const void *w, void *dx,
                                        void *dw, float *db, void *workspace, size_t workspace_bytes,

@@ -17,6 +17,11 @@
 //                instruction, that arrive at the stage's barrier by themselves; the
 //                proxy fence is the MMA warp's.  (A fence by the copying threads
 //                waits for all of their copies in flight, 2,000 cycles a chunk.)
+// Where experts have many rows, two CTAs on neighbouring SMs have a tile of 256 x 256
+// (cta_group::2): each holds its 128 rows of A, half of B and its rows of the
+// accumulator, one issues the MMAs of both.  That is a third less to copy and to
+// read from shared memory per product, which is what bounds the large products, by
+// bandwidth and by power.
 //   warps 4..11  the epilogue of one accumulator while the other is filled: 16
 //                columns at a time through a warp's own shared memory, so that
 //                global memory sees 32-byte runs of a row, not one row a lane.
@@ -47,13 +52,16 @@ constexpr uint32_t kRing = 196608;  // bytes of all stages
 constexpr uint32_t kStageCols = 16;  // columns of the epilogue's staging
 constexpr uint32_t kMaxStages = 8;
 
-constexpr uint32_t stage_bytes(int BN) { return kABytes + (uint32_t)BN * 128; }
-constexpr uint32_t stages(int BN) {
-  return kRing / stage_bytes(BN) < kMaxStages ? kRing / stage_bytes(BN) : kMaxStages;
+// Columns of a tile whose operand lies in one CTA's shared memory.
+constexpr int own_cols(int BN, bool pair) { return pair ? BN / 2 : BN; }
+constexpr uint32_t stage_bytes(int cols) { return kABytes + (uint32_t)cols * 128; }
+constexpr uint32_t stages(int cols) {
+  return kRing / stage_bytes(cols) < kMaxStages ? kRing / stage_bytes(cols) : kMaxStages;
 }
 
 struct Shared {
-  uint64_t full[kMaxStages], copied[kMaxStages], go[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], drain;
+  uint64_t full[kMaxStages], copied[kMaxStages], peer_copied[kMaxStages], go[kMaxStages], empty[kMaxStages];
+  uint64_t acc_full[2], acc_empty[2], drain;
   uint32_t tmem, quit;
   int32_t off[NTC_MAX_EXPERTS + 2];       // first row of each expert; [E]: of no expert; [E + 1]: the end
   uint32_t tile[NTC_MAX_EXPERTS + 2];     // first row tile of each expert (and of no expert); the total
@@ -68,18 +76,88 @@ __device__ unsigned int g_linear_status;
 __device__ __forceinline__ void expect_tx(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(bar), "r"(bytes) : "memory");
 }
+// PAIR: the copy completes on a barrier that may be the other CTA's.
+template <bool PAIR>
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, int32_t y) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n" ::"r"(dst),
-      "l"(map), "r"(bar), "r"(x), "r"(y)
-      : "memory");
+  if constexpr (PAIR)
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], "
+        "[%2];\n" ::"r"(dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n" ::"r"(dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y)
+        : "memory");
 }
+template <bool PAIR>
 __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap *map, uint32_t bar, int32_t x, int32_t y, int32_t e) {
+  if constexpr (PAIR)
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, "
+        "%5}], [%2];\n" ::"r"(dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(e)
+        : "memory");
+  else
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n" ::"r"(
+            dst),
+        "l"(map), "r"(bar), "r"(x), "r"(y), "r"(e)
+        : "memory");
+}
+// The pair of CTAs: an address in CTA `rank`'s shared memory, an arrival there, a
+// barrier of both CTAs' threads, a wait that sees what the other CTA did before.
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void arrive_there(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
+}
+template <bool PAIR>
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
+  if constexpr (!PAIR) return mbar_try_wait(bar, parity);
+  uint32_t ok;
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];\n" ::"r"(
-          dst),
-      "l"(map), "r"(bar), "r"(x), "r"(y), "r"(e)
+      "{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+      "selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
       : "memory");
+  return ok != 0;
+}
+// All 512 columns of tensor memory, of both CTAs where there are two.
+template <bool PAIR>
+__device__ __forceinline__ void tmem_take(uint32_t to) {
+  if constexpr (PAIR) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(to), "r"(512u) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n" ::: "memory");
+  } else {
+    tmem_alloc(to);
+  }
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_give(uint32_t tmem) {
+  if constexpr (PAIR)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(512u) : "memory");
+  else
+    tmem_dealloc(tmem);
+}
+// Arrival at bar (PAIR: of both CTAs) once the MMAs so far are done.
+template <bool PAIR>
+__device__ __forceinline__ void commit(uint32_t bar) {
+  if constexpr (PAIR)
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n" ::"r"(bar),
+        "h"((uint16_t)3)
+        : "memory");
+  else
+    umma_commit(bar);
 }
 __device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
   asm volatile("prefetch.tensormap [%0];\n" ::"l"(map) : "memory");
@@ -101,14 +179,22 @@ __device__ __forceinline__ void copy_arrive(uint32_t bar) {
 // Between other threads' copies, whose arrival this thread has waited for, and the
 // tensor core's reads.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory"); }
-// D[tmem] (+)= A[smem] x B[smem]
+// D[tmem] (+)= A[smem] x B[smem].  PAIR: 256 rows, half of A, B and D in each CTA.
+template <bool PAIR>
 __device__ __forceinline__ void umma_ss(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
                                         uint32_t accum) {
-  asm volatile(
-      "{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %6, 0;\nmov.b64 a, {%1, %2};\nmov.b64 b, {%3, %4};\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}\n" ::"r"(d),
-      "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accum)
-      : "memory");
+  if constexpr (PAIR)
+    asm volatile(
+        "{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %6, 0;\nmov.b64 a, {%1, %2};\nmov.b64 b, {%3, %4};\n"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, p;\n}\n" ::"r"(d),
+        "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accum)
+        : "memory");
+  else
+    asm volatile(
+        "{\n.reg .pred p;\n.reg .b64 a, b;\nsetp.ne.b32 p, %6, 0;\nmov.b64 a, {%1, %2};\nmov.b64 b, {%3, %4};\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}\n" ::"r"(d),
+        "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accum)
+        : "memory");
 }
 
 // Descriptor words of a 128-byte-swizzled operand: 8-row groups 1,024 bytes apart
@@ -124,14 +210,15 @@ constexpr uint32_t kSw128Hi = (1024u >> 4) | (1u << 14) | (2u << 29);
 // A bounded wait.  The first one that gives up sets the status word and the
 // CTA's quit flag, which ends the others'.  The clock is looked at every 64 tries:
 // reading %globaltimer takes about as long as a chunk's MMAs.
+template <bool PAIR>
 struct Waiter {
   volatile uint32_t *quit;
   unsigned int *status;
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
-    if (mbar_try_wait(bar, parity)) return true;
+    if (try_wait<PAIR>(bar, parity)) return true;
     uint64_t t0 = 0;
     for (uint32_t tries = 1;; ++tries) {
-      if (mbar_try_wait(bar, parity)) return true;
+      if (try_wait<PAIR>(bar, parity)) return true;
       if (tries % 64) continue;
       if (*quit) return false;
       const uint64_t now = global_ns();
@@ -149,8 +236,9 @@ struct Waiter {
 
 struct Tile {
   uint32_t e;         // expert; num_experts: rows of no expert
-  uint32_t row;       // first row: of the matrix (kDw: of the expert's transposed output)
+  uint32_t row;       // first row (of this CTA): of the matrix (kDw: of the expert's transposed output)
   uint32_t rows;      // rows inside, at most 128
+  uint32_t all_rows;  // of both CTAs of a pair
   uint32_t col;       // first column
   uint32_t depth;     // contraction length; 0: the tile is zeros
   uint32_t begin;     // kDw: first row of the contraction
@@ -158,8 +246,9 @@ struct Tile {
 
 // Experts' rows and row tiles, from offsets that are only trusted to lie
 // anywhere: they are held inside 0..num_rows, an expert that ends before it begins
-// has no rows.  Called by the whole CTA; ends with a barrier.
-__device__ __forceinline__ void make_table(int32_t *off, uint32_t *tile, const int32_t *offsets, uint32_t E, uint32_t num_rows) {
+// has no rows.  `high`: rows of a tile.  Called by the whole CTA; ends with a barrier.
+__device__ __forceinline__ void make_table(int32_t *off, uint32_t *tile, const int32_t *offsets, uint32_t E, uint32_t num_rows,
+                                           uint32_t high = kRows) {
   for (uint32_t e = threadIdx.x; e <= E; e += blockDim.x)
     off[e] = offsets ? offset_at(offsets, e, (int32_t)num_rows) : e ? (int32_t)num_rows : 0;
   if (threadIdx.x == 0) off[E + 1] = (int32_t)num_rows;
@@ -169,7 +258,7 @@ __device__ __forceinline__ void make_table(int32_t *off, uint32_t *tile, const i
     uint32_t base = 0;
     for (uint32_t e0 = 0; e0 <= E; e0 += 32) {
       const uint32_t e = e0 + lane;
-      const uint32_t mine = e <= E ? ((uint32_t)max(off[e + 1] - off[e], 0) + kRows - 1) / kRows : 0u;
+      const uint32_t mine = e <= E ? ((uint32_t)max(off[e + 1] - off[e], 0) + high - 1) / high : 0u;
       uint32_t in = mine;
 #pragma unroll
       for (int s = 1; s < 32; s <<= 1) {
@@ -195,18 +284,19 @@ __device__ __forceinline__ uint32_t bucket_of_tile(const uint32_t *tile, uint32_
   return lo;
 }
 
-template <int MODE, int BN>
+template <int MODE, int BN, bool PAIR>
 struct Tiles {
+  static constexpr uint32_t kHigh = PAIR ? 2 * kRows : kRows, kBandTiles = kBand * kRows / kHigh;
   const Shared &s;
-  uint32_t num_experts, height, depth, cols, row_tiles;
+  uint32_t num_experts, height, depth, cols, row_tiles, shift;  // shift: this CTA's rows in the pair's
   uint64_t total;
-  __device__ __forceinline__ Tiles(const LinearArgs &a, const Shared &sh)
-      : s(sh), num_experts(a.num_experts), height(a.height), depth(a.depth) {
+  __device__ __forceinline__ Tiles(const LinearArgs &a, const Shared &sh, uint32_t rank)
+      : s(sh), num_experts(a.num_experts), height(a.height), depth(a.depth), shift(rank * kRows) {
     cols = (a.width + BN - 1) / BN;
-    row_tiles = (a.height + kRows - 1) / kRows;
+    row_tiles = (a.height + kHigh - 1) / kHigh;
     total = MODE == kDw ? (uint64_t)a.num_experts * row_tiles * cols : (uint64_t)s.tile[a.num_experts + 1] * cols;
   }
-  // Within an expert: bands of kBand row tiles, columns inside a band, rows inside
+  // Within an expert: bands of row tiles, columns inside a band, rows inside
   // a column, so that the CTAs at work at one time share operands.
   __device__ __forceinline__ Tile at(uint64_t t) const {
     Tile o;
@@ -221,19 +311,19 @@ struct Tiles {
       r = (uint32_t)(t - (uint64_t)s.tile[o.e] * cols);
       many = s.tile[o.e + 1] - s.tile[o.e];
     }
-    const uint32_t band = r / (kBand * cols), in = r - band * kBand * cols;
-    const uint32_t high = min(kBand, many - band * kBand);
-    const uint32_t row = (band * kBand + in % high) * kRows;
+    const uint32_t band = r / (kBandTiles * cols), in = r - band * kBandTiles * cols;
+    const uint32_t high = min(kBandTiles, many - band * kBandTiles);
+    const uint32_t row = (band * kBandTiles + in % high) * kHigh;
     o.col = in / high * BN;
     const uint32_t begin = (uint32_t)s.off[o.e], count = (uint32_t)max(s.off[o.e + 1] - s.off[o.e], 0);
+    o.all_rows = min(kHigh, (MODE == kDw ? height : count) - row);
+    o.rows = PAIR ? min(kRows, o.all_rows - min(o.all_rows, shift)) : o.all_rows;
     if constexpr (MODE == kDw) {
-      o.row = row;
-      o.rows = min(kRows, height - row);
+      o.row = row + shift;
       o.begin = begin;
       o.depth = count;
     } else {
-      o.row = begin + row;
-      o.rows = min(kRows, count - row);
+      o.row = begin + row + shift;
       o.begin = 0;
       o.depth = o.e < num_experts ? depth : 0u;
     }
@@ -465,87 +555,103 @@ struct Epilogue {
 
 // ------------------------------------------------------------ the kernel
 
-template <int MODE, int BN, typename T>
+template <int MODE, int BN, typename T, bool PAIR>
 __global__ void __launch_bounds__(threads(MODE), 1)
     k_linear(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32,
              const __grid_constant__ CUtensorMap map_b, const LinearArgs a) {
-  constexpr uint32_t kStages = stages(BN), kStage = stage_bytes(BN);
+  constexpr int kOwn = own_cols(BN, PAIR);
+  constexpr uint32_t kStages = stages(kOwn), kStage = stage_bytes(kOwn);
   extern __shared__ uint8_t raw[];
   uint8_t *ring = raw + (1024 - (saddr(raw) & 1023)) % 1024;
   uint8_t *staging = ring + kRing;
   Shared &s = *reinterpret_cast<Shared *>(staging + kEpilogueWarps * 32 * kStageCols * 4);
   const uint32_t warp = uniform(threadIdx.x / 32), lane = threadIdx.x & 31;
+  // PAIR: CTAs 2i and 2i + 1 have one tile; the even one issues the MMAs
+  const uint32_t rank = PAIR ? blockIdx.x & 1 : 0, first_tile = PAIR ? blockIdx.x / 2 : blockIdx.x;
+  const uint32_t tile_step = PAIR ? gridDim.x / 2 : gridDim.x;
 
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < kStages; ++i) {
       mbar_init(saddr(&s.full[i]), 1);
+      mbar_init(saddr(&s.peer_copied[i]), 1);
       mbar_init(saddr(&s.copied[i]), 32 * copy_warps(MODE));
       mbar_init(saddr(&s.go[i]), 1);
       mbar_init(saddr(&s.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(saddr(&s.acc_full[i]), 1);
-      mbar_init(saddr(&s.acc_empty[i]), kEpilogueWarps);
+      mbar_init(saddr(&s.acc_empty[i]), PAIR ? 2 * kEpilogueWarps : kEpilogueWarps);
     }
     mbar_init(saddr(&s.drain), 1);
     s.quit = 0;
     mbar_init_fence();
   }
-  if (warp == 2) tmem_alloc(saddr(&s.tmem));
+  if (warp == 2) tmem_take<PAIR>(saddr(&s.tmem));
   if (warp == 0 && elect_one()) {
     prefetch_map(&map_a);
     if (MODE != kDw) prefetch_map(&map_a32);
     prefetch_map(&map_b);
   }
   pdl_wait();
-  make_table(s.off, s.tile, a.offsets, a.num_experts, a.num_rows);
+  make_table(s.off, s.tile, a.offsets, a.num_experts, a.num_rows, PAIR ? 2 * kRows : kRows);
   fence_after();
+  if (PAIR) pair_sync();  // both CTAs' barriers are there
   const uint32_t tmem = s.tmem;
-  const Waiter wait{&s.quit, a.status};
-  const Tiles<MODE, BN> tiles(a, s);
+  // what the other CTA's threads signal is waited for across the pair; that costs
+  // the copying warps all of their copies in flight, so nothing else is
+  const Waiter<false> wait{&s.quit, a.status};
+  const Waiter<PAIR> wait_pair{&s.quit, a.status};
+  const Tiles<MODE, BN, PAIR> tiles(a, s, rank);
 
   if (warp == 0) {
     uint32_t issued = 0;
     bool ok = true;
-    for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
+    for (uint64_t t = first_tile; ok && t < tiles.total; t += tile_step) {
       const Tile o = tiles.at(t);
       const uint32_t depth = uniform(o.depth), chunks = (depth + kChunk - 1) / kChunk, e = uniform(o.e);
-      const int32_t row = (int32_t)uniform(o.row), col = (int32_t)uniform(o.col), begin = (int32_t)uniform(o.begin);
-      const uint32_t boxes = uniform(MODE == kForward && a.rows ? 0 : (o.rows + 31) / 32);  // of 32 rows; 4: one of 128
+      const int32_t row = (int32_t)uniform(o.row), begin = (int32_t)uniform(o.begin);
+      const int32_t col = (int32_t)uniform(o.col + rank * kOwn);  // of this CTA's half of the other operand
+      // boxes of 32 rows (4: one of 128), of this CTA and of the pair
+      const bool gathers = MODE == kForward && a.rows;
+      const uint32_t boxes = uniform(gathers ? 0 : (o.rows + 31) / 32);
+      const uint32_t all_boxes =
+          uniform(gathers ? 0 : (min(o.all_rows, kRows) + 31) / 32 + (o.all_rows - min(o.all_rows, kRows) + 31) / 32);
       for (uint32_t c = 0; c < chunks; ++c, ++issued) {
         const uint32_t st = issued % kStages;
         ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.empty[st]), ((issued / kStages) & 1) ^ 1));
         if (!ok) break;
         // One elected lane issues a chunk's copies, with operands the compiler knows to
         // be uniform: from several lanes they go out one by one, 75 cycles each.
-        const uint32_t bar = uniform(saddr(&s.full[st]));
+        const uint32_t bar = uniform(PAIR ? in_cta(saddr(&s.full[st]), 0) : saddr(&s.full[st]));
         const uint32_t sa = uniform(saddr(ring) + st * kStage), sb = sa + kABytes;
         const int32_t k = (int32_t)(c * kChunk);
         if (elect_one()) {
+          constexpr uint32_t kBoth = PAIR ? 2 : 1;
           if constexpr (MODE != kDw) {
+            if (rank == 0) expect_tx(saddr(&s.full[st]), all_boxes * 4096 + kBoth * kOwn * 128);
             if (boxes == 4) {
-              expect_tx(bar, kABytes + BN * 128);
-              tma_2d(sa, &map_a, bar, k, row);
+              tma_2d<PAIR>(sa, &map_a, bar, k, row);
             } else {
-              expect_tx(bar, boxes * 4096 + BN * 128);
-              for (uint32_t j = 0; j < boxes; ++j) tma_2d(sa + j * 4096, &map_a32, bar, k, row + (int32_t)j * 32);
+              for (uint32_t j = 0; j < boxes; ++j) tma_2d<PAIR>(sa + j * 4096, &map_a32, bar, k, row + (int32_t)j * 32);
             }
             if constexpr (MODE == kForward) {
-              tma_3d(sb, &map_b, bar, k, col, (int32_t)e);
+              tma_3d<PAIR>(sb, &map_b, bar, k, col, (int32_t)e);
             } else {
 #pragma unroll
-              for (uint32_t j = 0; j < BN / 64; ++j) tma_3d(sb + j * 8192, &map_b, bar, col + (int32_t)j * 64, k, (int32_t)e);
+              for (uint32_t j = 0; j < kOwn / 64; ++j)
+                tma_3d<PAIR>(sb + j * 8192, &map_b, bar, col + (int32_t)j * 64, k, (int32_t)e);
             }
           } else if ((c + 1) * kChunk <= depth) {
-            expect_tx(bar, (a.rows ? 0 : kABytes) + BN * 128);
+            if (rank == 0) expect_tx(saddr(&s.full[st]), kBoth * ((a.rows ? 0 : kABytes) + kOwn * 128));
             if (!a.rows) {
 #pragma unroll
-              for (uint32_t j = 0; j < 2; ++j) tma_2d(sa + j * 8192, &map_a, bar, row + (int32_t)j * 64, begin + k);
+              for (uint32_t j = 0; j < 2; ++j) tma_2d<PAIR>(sa + j * 8192, &map_a, bar, row + (int32_t)j * 64, begin + k);
             }
 #pragma unroll
-            for (uint32_t j = 0; j < BN / 64; ++j) tma_2d(sb + j * 8192, &map_b, bar, col + (int32_t)j * 64, begin + k);
+            for (uint32_t j = 0; j < kOwn / 64; ++j)
+              tma_2d<PAIR>(sb + j * 8192, &map_b, bar, col + (int32_t)j * 64, begin + k);
           } else {
-            mbar_arrive(bar);  // the copying warps bring all of it
+            if (rank == 0) mbar_arrive(saddr(&s.full[st]));  // the copying warps bring all of it
             if (!a.rows) mbar_arrive(saddr(&s.go[st]));
           }
         }
@@ -553,13 +659,31 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       }
     }
     pdl_trigger();
-    if (!ok)  // the copies in flight land before the CTA ends
+    if (!ok && rank == 0)  // the copies in flight land before the CTA (and its pair) ends
       for (uint32_t j = issued > kStages ? issued - kStages : 0; j < issued; ++j)
         mbar_wait(saddr(&s.full[j % kStages]), (j / kStages) & 1);
+  } else if (warp == 1 && rank != 0) {
+    // What this CTA's warps have copied is passed on to the CTA that issues the MMAs.
+    uint32_t used = 0, phases = 0;
+    bool ok = MODE == kDw;
+    for (uint64_t t = first_tile; ok && t < tiles.total; t += tile_step) {
+      const Tile o = tiles.at(t);
+      const uint32_t chunks = (o.depth + kChunk - 1) / kChunk;
+      for (uint32_t c = 0; c < chunks; ++c, ++used) {
+        if ((c + 1) * kChunk <= o.depth) continue;
+        const uint32_t st = used % kStages;
+        ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.copied[st]), (phases >> st) & 1));
+        if (!ok) break;
+        phases ^= 1u << st;
+        fence_async();
+        if (lane == 0) arrive_there(in_cta(saddr(&s.peer_copied[st]), 0));
+        __syncwarp();
+      }
+    }
   } else if (warp == 1) {
     constexpr uint32_t kBf16 = std::is_same<T, __half>::value ? 0 : 1;
     constexpr uint32_t idesc = (1u << 4) | (kBf16 << 7) | (kBf16 << 10) | ((MODE == kDw ? 1u : 0u) << 15) |
-                           ((MODE != kForward ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | ((kRows >> 4) << 24);
+                           ((MODE != kForward ? 1u : 0u) << 16) | ((uint32_t)(BN >> 3) << 17) | (((PAIR ? 2 * kRows : kRows) >> 4) << 24);
     // 16 of the contraction: 32 bytes along a K-major row, 16 rows of an MN-major block
     constexpr uint32_t kStepA = MODE == kDw ? 2048 >> 4 : 32 >> 4, kStepB = MODE != kForward ? 2048 >> 4 : 32 >> 4;
     // Everything the issuing lane needs derives from values known to be uniform: the
@@ -567,11 +691,11 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     const uint32_t ring_lo = uniform(sw128_lo(saddr(ring), 8192)), columns = uniform(tmem);
     uint32_t used = 0, acc = 0, phases = 0;  // phases: bit of each stage's copied barrier
     bool ok = true, any = false;
-    for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
+    for (uint64_t t = first_tile; ok && t < tiles.total; t += tile_step) {
       const Tile o = tiles.at(t);
       const uint32_t depth = uniform(o.depth), chunks = (depth + kChunk - 1) / kChunk;
       if (chunks == 0) continue;
-      ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.acc_empty[acc & 1]), ((acc >> 1) & 1) ^ 1));
+      ok = __all_sync(0xFFFFFFFFu, wait_pair(saddr(&s.acc_empty[acc & 1]), ((acc >> 1) & 1) ^ 1));
       if (!ok) break;
       fence_after();
       const uint32_t d = columns + (acc & 1) * BN;
@@ -580,6 +704,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
         ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.full[st]), (used / kStages) & 1));
         if (ok && (a.rows || (MODE == kDw && (c + 1) * kChunk > depth))) {
           ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.copied[st]), (phases >> st) & 1));
+          if (PAIR && ok) ok = __all_sync(0xFFFFFFFFu, wait_pair(saddr(&s.peer_copied[st]), (phases >> st) & 1));
           phases ^= 1u << st;
           fence_async();
         }
@@ -589,16 +714,16 @@ __global__ void __launch_bounds__(threads(MODE), 1)
         if (elect_one()) {
 #pragma unroll
           for (uint32_t k = 0; k < kChunk / 16; ++k)
-            umma_ss(d, alo + k * kStepA, kSw128Hi, blo + k * kStepB, kSw128Hi, idesc, (c | k) != 0);
-          umma_commit(saddr(&s.empty[st]));
-          if (c + 1 == chunks) umma_commit(saddr(&s.acc_full[acc & 1]));
+            umma_ss<PAIR>(d, alo + k * kStepA, kSw128Hi, blo + k * kStepB, kSw128Hi, idesc, (c | k) != 0);
+          commit<PAIR>(saddr(&s.empty[st]));
+          if (c + 1 == chunks) commit<PAIR>(saddr(&s.acc_full[acc & 1]));
         }
         __syncwarp();
       }
       ++acc;
     }
     if (!ok && any) {
-      if (elect_one()) umma_commit(saddr(&s.drain));
+      if (elect_one()) commit<PAIR>(saddr(&s.drain));
       __syncwarp();
       mbar_wait(saddr(&s.drain), 0);
     }
@@ -620,7 +745,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     const uint32_t x_rows = a.x_rows, depth = a.depth, width = a.width, height = a.height;
     uint32_t issued = 0, went = 0;  // went: phase of each stage's go barrier
     bool ok = MODE == kDw || (MODE == kForward && rows);  // else there is nothing to copy
-    for (uint64_t t = blockIdx.x; ok && t < tiles.total; t += gridDim.x) {
+    for (uint64_t t = first_tile; ok && t < tiles.total; t += tile_step) {
       const Tile o = tiles.at(t);
       const uint32_t chunks = (o.depth + kChunk - 1) / kChunk;
       const uint8_t *src[kMany];
@@ -645,11 +770,15 @@ __global__ void __launch_bounds__(threads(MODE), 1)
         }
       };
       int32_t one[kMany], two[kMany];  // kDw: the rows of the next chunk, and of the one after it
-      if (chunks) {
+      if (chunks && (MODE == kDw || o.rows)) {
         const uint32_t from = (MODE == kDw ? o.begin : o.row) + first;
         fetch(from, one);
         look(from, one);
         if (MODE == kDw) fetch(from + kChunk, one);
+      } else {  // the second CTA of a pair may have no rows
+        zeros = 0xFFFFFFFFu;
+#pragma unroll
+        for (int i = 0; i < kMany; ++i) src[i] = x;
       }
       // `next` has been asked for one chunk ago, `later` is asked for now: they change
       // places from chunk to chunk, for a register copy would wait for the loads
@@ -712,8 +841,8 @@ __global__ void __launch_bounds__(threads(MODE), 1)
             for (int i = 0; i < kMany; ++i) {
               const uint32_t at = c * kChunk + first + i * 4 + sub;
 #pragma unroll
-              for (uint32_t j = 0; j < BN / 64; ++j) {
-                const uint32_t col = o.col + j * 64 + piece * 8;
+              for (uint32_t j = 0; j < kOwn / 64; ++j) {
+                const uint32_t col = o.col + rank * kOwn + j * 64 + piece * 8;
                 const uint32_t n = at < o.depth && col < width ? min(16u, (width - col) * 2) : 0u;
                 copy16_part(sb + j * 8192 + (i & 1 ? to1 : to0) + i * 512,
                             n ? dz + (uint64_t)(o.begin + at) * pitch_dz + col * 2 : dz, n);
@@ -736,7 +865,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     const uint32_t part = (w >> 2) * (BN / 2);  // each set of four warps takes half of the columns
     uint8_t *mine = staging + w * 32 * kStageCols * 4;
     uint32_t acc = 0;
-    for (uint64_t t = blockIdx.x; t < tiles.total; t += gridDim.x) {
+    for (uint64_t t = first_tile; t < tiles.total; t += tile_step) {
       const Tile o = tiles.at(t);
       const Strip g{MODE == kDw ? o.e : 0u, (int32_t)o.rows - (int32_t)(quarter * 32), (uint64_t)o.row + quarter * 32,
                     o.col + part, (int32_t)min((uint32_t)BN / 2, ep.width - min(ep.width, o.col + part)), lane};
@@ -762,15 +891,20 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       }
       fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(saddr(&s.acc_empty[acc & 1]));
+      if (lane == 0) {
+        if (PAIR) arrive_there(in_cta(saddr(&s.acc_empty[acc & 1]), 0));
+        else mbar_arrive(saddr(&s.acc_empty[acc & 1]));
+      }
       ++acc;
     }
   }
   fence_before();
-  __syncthreads();
+  __syncwarp();
+  if (PAIR) pair_sync();  // neither CTA is gone while the other may signal it
+  else __syncthreads();
   if (warp == 2) {
     fence_after();
-    tmem_dealloc(tmem);
+    tmem_give<PAIR>(tmem);
   }
 }
 
@@ -946,33 +1080,59 @@ __global__ void __launch_bounds__(kDzThreads)
   }
 }
 
-// Matrices TMA cannot read, copied to rows of `pitch` elements (the pads hold 0): the
-// operand x, the operand w, or both, in one launch.
+// Matrices that the product does not read where they lie, copied to rows of `pitch`
+// elements (the pads hold 0): x or w, or both, in one launch.  With an index, row i
+// is row index[i] of the source, zeros where there is none.
 struct Pack {
   const uint16_t *src;
+  const int32_t *index;
   uint16_t *dst;
-  uint64_t ld, stride, pieces;  // pieces of eight elements, of all matrices
-  uint32_t cols, rows, pitch;
+  uint64_t ld, stride, all_rows;  // all_rows: of all matrices
+  uint32_t cols, rows, pitch, src_rows;
+  uint32_t vec;                   // the source's rows are whole 16-byte pieces
 };
+// A warp per row, four pieces of a lane in flight.
 __global__ void __launch_bounds__(256) k_pack(const Pack first, const Pack second) {
+  const uint32_t lane = threadIdx.x & 31;
   pdl_wait();
   pdl_trigger();
-  const uint64_t total = first.pieces + second.pieces;
-  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (uint64_t)gridDim.x * 256) {
-    const bool one = i < first.pieces;
+  const uint64_t total = first.all_rows + second.all_rows;
+  for (uint64_t i = (uint64_t)blockIdx.x * 8 + threadIdx.x / 32; i < total; i += (uint64_t)gridDim.x * 8) {
+    const bool one = i < first.all_rows;
     const Pack &k = one ? first : second;
-    const uint64_t j = one ? i : i - first.pieces;
-    const uint32_t wide = k.pitch / 8;
-    const uint64_t row = j / wide, m = row / k.rows;  // row: of all matrices
-    const uint32_t c = (uint32_t)(j - row * wide) * 8;
-    const uint16_t *p = k.src + m * k.stride + (row - m * k.rows) * k.ld + c;
-    uint32_t w[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint32_t lo = c + 2 * q < k.cols ? p[2 * q] : 0u, hi = c + 2 * q + 1 < k.cols ? p[2 * q + 1] : 0u;
-      w[q] = lo | (hi << 16);
+    const uint64_t row = one ? i : i - first.all_rows, m = row / k.rows;
+    uint64_t from = row - m * k.rows;
+    uint32_t cols = k.cols;
+    if (k.index) {
+      const int32_t at = (int32_t)ld_word((const uint32_t *)k.index + row);
+      if ((uint32_t)at >= k.src_rows) cols = 0;
+      from = cols ? (uint32_t)at : 0;
     }
-    *reinterpret_cast<uint4 *>(k.dst + row * k.pitch + c) = make_uint4(w[0], w[1], w[2], w[3]);
+    const uint16_t *p = k.src + m * k.stride + from * k.ld;
+    uint16_t *to = k.dst + row * k.pitch;
+    if (k.vec) {
+      for (uint32_t c0 = lane * 8; c0 < k.pitch; c0 += 1024) {
+        uint4 q[4];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+          q[u] = make_uint4(0, 0, 0, 0);
+          if (c0 + 256 * u < cols) q[u] = *reinterpret_cast<const uint4 *>(p + c0 + 256 * u);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+          if (c0 + 256 * u < k.pitch) *reinterpret_cast<uint4 *>(to + c0 + 256 * u) = q[u];
+      }
+    } else {
+      for (uint32_t c = lane * 8; c < k.pitch; c += 256) {
+        uint32_t w[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const uint32_t lo = c + 2 * q < cols ? p[c + 2 * q] : 0u, hi = c + 2 * q + 1 < cols ? p[c + 2 * q + 1] : 0u;
+          w[q] = lo | (hi << 16);
+        }
+        *reinterpret_cast<uint4 *>(to + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
   }
 }
 
@@ -1028,11 +1188,11 @@ unsigned int *status_word() {
   return p;
 }
 
-template <int MODE, int BN, typename T>
+template <int MODE, int BN, typename T, bool PAIR = false>
 cudaError_t launch_tile(const Operand &A, const Operand &B, LinearArgs a, uint64_t tiles_bound, int sms, cudaStream_t st) {
   CUtensorMap ma, ma32, mb;
   if (!make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 128) || !make_map(&ma32, A, 2, 64, 32) ||
-      !make_map(&mb, B, MODE == kDw ? 2 : 3, 64, MODE == kForward ? BN : 64))
+      !make_map(&mb, B, MODE == kDw ? 2 : 3, 64, MODE == kForward ? own_cols(BN, PAIR) : 64))
     return cudaErrorInvalidValue;
   a.x = (const uint8_t *)A.p;
   a.ld_x = A.ld;
@@ -1043,17 +1203,45 @@ cudaError_t launch_tile(const Operand &A, const Operand &B, LinearArgs a, uint64
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !((allowed.load() >> dev) & 1)) {
-    e = cudaFuncSetAttribute(k_linear<MODE, BN, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes);
+    e = cudaFuncSetAttribute(k_linear<MODE, BN, T, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSharedBytes);
     if (e != cudaSuccess) return e;
     if (dev < 64) allowed.fetch_or(1ull << dev);
   }
-  const unsigned grid = (unsigned)std::min<uint64_t>(tiles_bound, (uint64_t)sms);
-  return launch_pdl(k_linear<MODE, BN, T>, grid, threads(MODE), kSharedBytes, st, ma, ma32, mb, a);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(PAIR ? 2 * (unsigned)std::min<uint64_t>(tiles_bound, (uint64_t)sms / 2)
+                          : (unsigned)std::min<uint64_t>(tiles_bound, (uint64_t)sms));
+  cfg.blockDim = dim3(threads(MODE));
+  cfg.dynamicSmemBytes = kSharedBytes;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  if (pdl_enabled()) {
+    at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (PAIR) {
+    at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    at[cfg.numAttrs].val.clusterDim.x = 2;
+    at[cfg.numAttrs].val.clusterDim.y = at[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  cfg.attrs = at;
+  return cudaLaunchKernelEx(&cfg, k_linear<MODE, BN, T, PAIR>, ma, ma32, mb, a);
 }
 
 // Row tiles of num_rows rows in num_experts segments (and those of no expert), at most.
 uint64_t row_tiles_bound(uint64_t num_rows, uint64_t num_experts) {
   return std::min<uint64_t>(num_rows, (num_rows + kRows - 1) / kRows + num_experts);
+}
+
+// Whether pairs of CTAs take a product: experts with 1,024 rows or more on average (a
+// tile of theirs has 256), and a tile for every SM.  Without an index: the copies of
+// gathered rows would have to be passed on from one CTA to the other, chunk by chunk
+// (944 us instead of 363 by single CTAs, 32,768 rows, 2,048 -> 4,096).  Without one,
+// 352 us by single CTAs and 292 by pairs.
+bool pairs_take(int mode, uint64_t num_rows, uint64_t num_experts, uint64_t width, uint64_t height) {
+  const uint64_t high = mode == kDw ? num_experts * ((height + 255) / 256) : (num_rows + 255) / 256 + num_experts;
+  return (mode == kDw ? height >= 256 : num_rows >= 1024 * num_experts) &&
+         high * ((width + 255) / 256) >= (uint64_t)sm_count();
 }
 
 // The width of a tile: the widest whose tiles still fill the SMs, 128 at most where
@@ -1067,6 +1255,8 @@ cudaError_t launch_product_of(const Operand &A, const Operand &B, const LinearAr
                                     : row_tiles_bound(a.num_rows, a.num_experts);
   if (high == 0) return cudaSuccess;
   const auto tiles = [&](uint32_t bn) { return high * ((a.width + bn - 1) / bn); };
+  if (!a.rows && pairs_take(MODE, a.num_rows, a.num_experts, a.width, a.height))
+    return launch_tile<MODE, 256, T, true>(A, B, a, tiles(256), sms, st);
   const bool thin = MODE != kDw && a.num_rows <= 32ull * a.num_experts;
   if (!thin && tiles(256) >= (uint64_t)sms) return launch_tile<MODE, 256, T>(A, B, a, tiles(256), sms, st);
   if (tiles(128) >= (uint64_t)sms) return launch_tile<MODE, 128, T>(A, B, a, tiles(128), sms, st);
@@ -1084,12 +1274,24 @@ uint64_t round8(uint64_t x) { return (x + 7) / 8 * 8; }
 uint64_t round256(uint64_t x) { return (x + 255) / 256 * 256; }
 
 bool tma_reads(const void *p, uint64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+// Gathered rows are copied in order where pairs of CTAs then take the product and its
+// other width pays for the copy: 40 us of 32,768 rows of 2,048, against 363 - 295 (out
+// 4,096 wide) in the forward product, 481 - 323 in dw.
+bool x_gathers(const ntc_linear_desc &d, const int32_t *rows, bool dw) {
+  return rows && d.out_dim >= (dw ? 1024u : 2048u) &&
+         (dw ? pairs_take(kDw, d.num_rows, d.num_experts, d.out_dim, d.in_dim)
+             : pairs_take(kForward, d.num_rows, d.num_experts, d.out_dim, 0));
+}
 bool x_packs(const ntc_linear_desc &d, const void *x) { return !tma_reads(x, d.ld_x); }
 bool w_packs(const ntc_linear_desc &d, const void *w) {
   return !tma_reads(w, d.ld_w) || (d.num_experts > 1 && d.stride_w % 8);
 }
 bool dz_writes(const ntc_linear_desc &d, const void *dy) { return d.activation != NTC_ACT_NONE || !tma_reads(dy, d.ld_y); }
-uint64_t x_bytes(const ntc_linear_desc &d) { return round256(d.num_x_rows * round8(d.in_dim) * 2); }
+// of the copy of x, if there is one
+uint64_t x_bytes(const ntc_linear_desc &d, const void *x, const int32_t *rows, bool dw) {
+  if (x_gathers(d, rows, dw)) return round256(d.num_rows * round8(d.in_dim) * 2);
+  return x_packs(d, x) ? round256(d.num_x_rows * round8(d.in_dim) * 2) : 0;
+}
 uint64_t w_bytes(const ntc_linear_desc &d) { return round256((uint64_t)d.num_experts * d.out_dim * round8(d.in_dim) * 2); }
 uint64_t dz_bytes(const ntc_linear_desc &d) { return round256(d.num_rows * round8(d.out_dim) * 2); }
 uint64_t part_bytes(const ntc_linear_desc &d) {
@@ -1138,41 +1340,62 @@ ntc_status check_workspace(const void *p, size_t have, size_t need) {
   return NTC_OK;
 }
 
-// The operands x and w, through the workspace where TMA cannot read them (a null one
-// is not wanted).
-cudaError_t operands(const ntc_linear_desc &d, const void *x, const void *w, uint8_t *ws, Operand *X, Operand *W,
-                     cudaStream_t st) {
+// The operands x and w, through the workspace where they are copied (a null one is
+// not wanted); *rows is null afterwards where the copy has x in order.
+cudaError_t operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, bool dw, const void *w, uint8_t *ws,
+                     Operand *X, Operand *W, cudaStream_t st) {
   const uint32_t pitch = (uint32_t)round8(d.in_dim);
   Pack job[2] = {};
   int jobs = 0;
   if (x) {
+    const bool gathers = x_gathers(d, *rows, dw);
     *X = Operand{x, d.in_dim, d.num_x_rows, d.ld_x};
-    if (x_packs(d, x)) {
-      job[jobs++] = Pack{(const uint16_t *)x, (uint16_t *)ws, d.ld_x, 0, d.num_x_rows * (pitch / 8), d.in_dim,
-                         (uint32_t)d.num_x_rows, pitch};
-      *X = Operand{ws, d.in_dim, d.num_x_rows, pitch};
-      ws += x_bytes(d);
+    if (gathers || x_packs(d, x)) {
+      const uint64_t n = gathers ? d.num_rows : d.num_x_rows;
+      Pack &k = job[jobs++];
+      k.src = (const uint16_t *)x;
+      k.index = gathers ? *rows : nullptr;
+      k.dst = (uint16_t *)ws;
+      k.ld = d.ld_x;
+      k.all_rows = n;
+      k.cols = d.in_dim;
+      k.rows = (uint32_t)n;
+      k.pitch = pitch;
+      k.src_rows = (uint32_t)d.num_x_rows;
+      k.vec = d.in_dim % 8 == 0 && tma_reads(x, d.ld_x);
+      *X = Operand{ws, d.in_dim, n, pitch};
+      ws += x_bytes(d, x, *rows, dw);
+      if (gathers) *rows = nullptr;
     }
   }
   if (w) {
     *W = Operand{w, d.in_dim, d.out_dim, d.ld_w, d.num_experts, d.stride_w};
     if (w_packs(d, w)) {
-      job[jobs++] = Pack{(const uint16_t *)w, (uint16_t *)ws, d.ld_w, d.stride_w,
-                         (uint64_t)d.num_experts * d.out_dim * (pitch / 8), d.in_dim, d.out_dim, pitch};
+      Pack &k = job[jobs++];
+      k.src = (const uint16_t *)w;
+      k.dst = (uint16_t *)ws;
+      k.ld = d.ld_w;
+      k.stride = d.stride_w;
+      k.all_rows = (uint64_t)d.num_experts * d.out_dim;
+      k.cols = d.in_dim;
+      k.rows = d.out_dim;
+      k.pitch = pitch;
       *W = Operand{ws, d.in_dim, d.out_dim, pitch, d.num_experts, (uint64_t)pitch * d.out_dim};
     }
   }
   if (jobs == 0) return cudaSuccess;
-  const uint64_t pieces = job[0].pieces + job[1].pieces;
-  const unsigned grid = (unsigned)std::min<uint64_t>((pieces + 255) / 256, (uint64_t)sm_count() * 32);
+  if (jobs == 1) job[1].rows = 1;  // no rows, but a divisor
+  const uint64_t total = job[0].all_rows + job[1].all_rows;  // warps' worth
+  const unsigned grid = (unsigned)std::min<uint64_t>((total + 7) / 8, (uint64_t)sm_count() * 32);
   return launch_pdl(k_pack, grid, 256, 0, st, job[0], job[1]);
 }
 
 }  // namespace
 
-extern "C" NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, const void *w) {
+extern "C" NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, const int32_t *rows,
+                                               const void *w) {
   if (check(desc) || few_rows(desc->num_rows)) return 0;
-  return (x_packs(*desc, x) ? x_bytes(*desc) : 0) + (w_packs(*desc, w) ? w_bytes(*desc) : 0);
+  return x_bytes(*desc, x, rows, false) + (w_packs(*desc, w) ? w_bytes(*desc) : 0);
 }
 
 extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void *x, const int32_t *rows,
@@ -1186,7 +1409,7 @@ extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void
   if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)y | (uintptr_t)z | (uintptr_t)residual) & 1)
     return op_fail(NTC_ERR_INVALID_ARG, "a buffer is not aligned to its element (2 bytes)");
   if ((uintptr_t)bias & 3) return op_fail(NTC_ERR_INVALID_ARG, "bias is not aligned to 4 bytes");
-  if (ntc_status s = check_workspace(workspace, workspace_bytes, ntc_linear_workspace(desc, x, w))) return s;
+  if (ntc_status s = check_workspace(workspace, workspace_bytes, ntc_linear_workspace(desc, x, rows, w))) return s;
   LinearArgs a{};
   a.rows = rows;
   a.offsets = offsets;
@@ -1216,15 +1439,17 @@ extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void
   a.status = status_word();
   if (!a.status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
   Operand X, W;
-  cudaError_t e = operands(d, x, w, (uint8_t *)workspace, &X, &W, st);
+  cudaError_t e = operands(d, x, &rows, false, w, (uint8_t *)workspace, &X, &W, st);
+  a.rows = rows;
+  a.x_rows = (uint32_t)X.rows;
   if (e == cudaSuccess) e = launch_product<kForward>(X, W, a, st);
   return op_cuda(e, "ntc_linear");
 }
 
 extern "C" NTC_API size_t ntc_linear_backward_workspace(const ntc_linear_desc *desc, const void *dy, const void *x,
-                                                        const void *w) {
+                                                        const int32_t *rows, const void *w) {
   if (check(desc)) return 0;
-  return (dz_writes(*desc, dy) ? dz_bytes(*desc) : 0) + (x_packs(*desc, x) ? x_bytes(*desc) : 0) +
+  return (dz_writes(*desc, dy) ? dz_bytes(*desc) : 0) + x_bytes(*desc, x, rows, true) +
          (w_packs(*desc, w) ? w_bytes(*desc) : 0) + part_bytes(*desc);
 }
 
@@ -1241,7 +1466,8 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
   if (((uintptr_t)dy | (uintptr_t)z | (uintptr_t)x | (uintptr_t)w | (uintptr_t)dx | (uintptr_t)dw) & 1)
     return op_fail(NTC_ERR_INVALID_ARG, "a buffer is not aligned to its element (2 bytes)");
   if ((uintptr_t)db & 3) return op_fail(NTC_ERR_INVALID_ARG, "db is not aligned to 4 bytes");
-  if (ntc_status s = check_workspace(workspace, workspace_bytes, ntc_linear_backward_workspace(desc, dy, x, w))) return s;
+  if (ntc_status s = check_workspace(workspace, workspace_bytes, ntc_linear_backward_workspace(desc, dy, x, rows, w)))
+    return s;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const char *what = "ntc_linear_backward";
   cudaError_t e = cudaSuccess;
@@ -1298,7 +1524,7 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
   a.ld_out = d.in_dim;
   a.status = status;
   Operand X, W;
-  if (e == cudaSuccess) e = operands(d, dw ? x : nullptr, dx ? w : nullptr, ws, &X, &W, st);
+  if (e == cudaSuccess) e = operands(d, dw ? x : nullptr, &rows, true, dx ? w : nullptr, ws, &X, &W, st);
   if (e == cudaSuccess && dx) {
     a.out = dx;
     a.depth = d.out_dim;
@@ -1308,7 +1534,7 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
   if (e == cudaSuccess && dw) {
     a.out = dw;
     a.rows = rows;
-    a.x_rows = (uint32_t)d.num_x_rows;
+    a.x_rows = (uint32_t)X.rows;
     a.width = d.out_dim;
     a.height = d.in_dim;
     a.vec_out = rows_are_vec(dw, d.in_dim, 2);

@@ -223,7 +223,7 @@ def linear(x, w, bias=None, *, rows=None, offsets=None, activation: str = "none"
     px, pw = x.data_ptr(), w.data_ptr()
     y = torch.empty((m, N), dtype=dt, device=dev)
     z = torch.empty((m, N), dtype=dt, device=dev) if save else None
-    size = _lib.ntc_linear_workspace(d, px, pw)
+    size = _lib.ntc_linear_workspace(d, px, r, pw)
     ws = torch.empty((size,), dtype=torch.uint8, device=dev) if size else None
     _check(_lib.ntc_linear(d, px, r, o, pw, b, res, y.data_ptr(), z.data_ptr() if save else None,
                            ws.data_ptr() if size else None, size, _raw_stream(dev.index)))
@@ -260,7 +260,7 @@ def linear_backward(dy, x, w, *, z=None, rows=None, offsets=None, activation: st
     dx = torch.empty((m, K), dtype=dt, device=dev) if "dx" in need else None
     dw = torch.empty(w.shape, dtype=dt, device=dev) if "dw" in need else None
     db = torch.empty(w.shape[:-1], dtype=_F32, device=dev) if "db" in need else None
-    size = _lib.ntc_linear_backward_workspace(d, py, px, pw)
+    size = _lib.ntc_linear_backward_workspace(d, py, px, r, pw)
     ws = torch.empty((size,), dtype=torch.uint8, device=dev) if size else None
     _check(_lib.ntc_linear_backward(d, py, pz, px, r, o, pw, None if dx is None else dx.data_ptr(),
                                     None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(),

@@ -124,9 +124,9 @@ def _load():
         "ntc_route_backward": ([P, S, P, S, P, P, P, P], I),
         "ntc_expert_order_workspace": ([S, ctypes.c_uint32], S),
         "ntc_expert_order": ([P, S, ctypes.c_uint32, ctypes.c_uint32, P, P, P, P, S, P], I),
-        "ntc_linear_workspace": ([P, P, P], S),
+        "ntc_linear_workspace": ([P, P, P, P], S),
         "ntc_linear": ([P, P, P, P, P, P, P, P, P, P, S, P], I),
-        "ntc_linear_backward_workspace": ([P, P, P, P], S),
+        "ntc_linear_backward_workspace": ([P, P, P, P, P], S),
         "ntc_linear_backward": ([P, P, P, P, P, P, P, P, P, P, P, S, P], I),
         "ntc_linear_status": ([P], I),
         "ntc_combine": ([P, P, P, P, P, P, P, P], I),
@@ -244,8 +244,8 @@ def ntc_expert_order(ids, n, top_k, num_experts, rows, place, offsets, workspace
     _check(_lib.ntc_expert_order(ids, n, top_k, num_experts, rows, place, offsets, workspace, workspace_bytes, stream))
 
 
-def ntc_linear_workspace(desc, x, w) -> int:
-    return _lib.ntc_linear_workspace(ctypes.byref(desc), x, w)
+def ntc_linear_workspace(desc, x, rows, w) -> int:
+    return _lib.ntc_linear_workspace(ctypes.byref(desc), x, rows, w)
 
 
 def ntc_linear(desc, x, rows, offsets, w, bias, residual, y, z, workspace, workspace_bytes, stream):
@@ -253,8 +253,8 @@ def ntc_linear(desc, x, rows, offsets, w, bias, residual, y, z, workspace, works
                            stream))
 
 
-def ntc_linear_backward_workspace(desc, dy, x, w) -> int:
-    return _lib.ntc_linear_backward_workspace(ctypes.byref(desc), dy, x, w)
+def ntc_linear_backward_workspace(desc, dy, x, rows, w) -> int:
+    return _lib.ntc_linear_backward_workspace(ctypes.byref(desc), dy, x, rows, w)
 
 
 def ntc_linear_backward(desc, dy, z, x, rows, offsets, w, dx, dw, db, workspace, workspace_bytes, stream):

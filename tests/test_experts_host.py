@@ -123,15 +123,19 @@ def test_linear_pointer_refusals():
     assert call(f, good, 1, P + 2) == BAD
     odd = made(ntc.ntc_linear_desc, LINEAR, dict(ld_x=65, num_rows=1000))
     even = made(ntc.ntc_linear_desc, LINEAR, dict(num_rows=1000))
-    need = ntc._lib.ntc_linear_workspace(odd, P, P)
-    assert need > 0 and ntc._lib.ntc_linear_workspace(even, P, P) == 0
-    assert ntc._lib.ntc_linear_workspace(even, P + 8, P) > 0 and ntc._lib.ntc_linear_workspace(even, P, P + 2) > 0
-    assert ntc._lib.ntc_linear_workspace(d, P + 8, P + 2) == 0  # few rows are read where they lie
+    need = ntc._lib.ntc_linear_workspace(odd, P, P, P)
+    assert need > 0 and ntc._lib.ntc_linear_workspace(even, P, P, P) == 0
+    assert ntc._lib.ntc_linear_workspace(even, P + 8, P, P) > 0 and ntc._lib.ntc_linear_workspace(even, P, P, P + 2) > 0
+    assert ntc._lib.ntc_linear_workspace(d, P + 8, P, P + 2) == 0  # few rows are read where they lie
+    big = made(ntc.ntc_linear_desc, LINEAR, dict(num_rows=65536, out_dim=4096, ld_y=4096, ld_z=4096, ld_residual=4096,
+                                                 stride_w=64 * 4096))
+    assert ntc._lib.ntc_linear_workspace(big, P, P, P) >= 65536 * 64 * 2  # gathered rows in order
+    assert ntc._lib.ntc_linear_workspace(big, P, None, P) == 0
     assert f(odd, *good[:8], P, need - 1, None) == BAD
     assert f(odd, *good[:8], None, need, None) == BAD
     assert f(odd, *good[:8], P + 8, need, None) == BAD
     assert f(None, *good, None) == BAD
-    need = ntc._lib.ntc_linear_backward_workspace(d, P, P, P)
+    need = ntc._lib.ntc_linear_backward_workspace(d, P, P, P, P)
     back = [P, P, P, P, P, P, P, P, P, P, need]
     for i in (0, 1, 2, 5):  # dy, z, x, w
         assert call(b, back, i, None) == BAD
@@ -140,8 +144,8 @@ def test_linear_pointer_refusals():
     assert call(b, back, 10, need - 1) == BAD
     assert b(d, P, P, P, P, P, P, None, None, None, P, need, None) == ntc.NTC_OK  # nothing asked for
     refused = made(ntc.ntc_linear_desc, LINEAR, dict(in_dim=0))
-    assert ntc._lib.ntc_linear_workspace(refused, P, P) == 0
-    assert ntc._lib.ntc_linear_backward_workspace(refused, P, P, P) == 0
+    assert ntc._lib.ntc_linear_workspace(refused, P, P, P) == 0
+    assert ntc._lib.ntc_linear_backward_workspace(refused, P, P, P, P) == 0
 
 
 @pytest.mark.parametrize("over", [dict(type=4), dict(dim=0), dict(dim=(1 << 20) + 1), dict(top_k=0), dict(top_k=33),

@@ -388,3 +388,27 @@ def test_dw_of_long_contractions(ntc, rows_of):
     R.assert_within(dx, *want[0])
     ref, _, bound, _ = R.linear(x, w, None, None, offsets)
     R.assert_within(y, ref, bound)
+
+
+# rows of each expert, in, out: many rows per expert and enough tiles of 256 x 256 for pairs of CTAs, with rows, columns
+# and contractions that end anywhere in them (in the second CTA's half, at its first row, before it)
+@pytest.mark.parametrize("counts,K,N", [((2048, 2048), 64, 4096), ((1300, 1537, 1025, 3000), 200, 2600),
+                                        ((0, 4097, 128, 300), 1000, 2568), ((5000,), 333, 2049)])
+@pytest.mark.parametrize("gather", [False, True])
+def test_large_products(ntc, counts, K, N, gather):
+    g = gen(sum(counts) + K)
+    E, M = len(counts), sum(counts) + 5
+    offsets = torch.tensor([0] + list(counts), device="cuda").cumsum(0).int()
+    T = M // 2 + 7
+    rows = torch.randint(-1, T, (M,), generator=g, device="cuda").int() if gather else None
+    x = normal(g, T if gather else M, K, dtype=torch.bfloat16)
+    w, b = normal(g, E, N, K, std=K ** -0.5, dtype=torch.bfloat16), normal(g, E, N)
+    r, z, dy = (normal(g, M, N, dtype=torch.bfloat16) for _ in range(3))
+    y, wz, yb, zb = R.linear(x, w, b, rows, offsets, "gelu", residual=r)
+    got, gz = ntc.linear(x, w, b, rows=rows, offsets=offsets, activation="gelu", residual=r, save=True)
+    R.assert_within(got, y, yb, "y")
+    R.assert_within(gz, wz, zb, "z")
+    got = ntc.linear_backward(dy, x, w, z=z, rows=rows, offsets=offsets, activation="silu")
+    for name, a, (ref, bound) in zip(("dx", "dw", "db"), got, R.linear_backward(dy, x, w, z, rows, offsets, "silu")):
+        R.assert_within(a, ref, bound, name)
+    ntc.ntc_linear_status(torch.cuda.current_stream().cuda_stream)
