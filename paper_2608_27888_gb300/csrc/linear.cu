@@ -727,6 +727,30 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       __syncwarp();
       mbar_wait(saddr(&s.drain), 0);
     }
+  } else if (MODE == kDx && warp < 4) {
+    // Nothing is copied here: these two warps add up the bias' gradient, 32 columns of an
+    // expert at a time, from the sums that k_dz has left for every 128 rows.
+    if (a.db) {
+      const float *part = a.part;
+      const uint32_t width = a.depth, pitch = a.part_pitch, strips = (width + 31) / 32, E = a.num_experts;
+      for (uint64_t u = (uint64_t)blockIdx.x * 2 + warp - 2; u < (uint64_t)E * strips; u += (uint64_t)gridDim.x * 2) {
+        const uint32_t e = (uint32_t)(u / strips), col = (uint32_t)(u - (uint64_t)e * strips) * 32 + lane;
+        uint32_t from = PAIR ? 0 : s.tile[e];
+        if (PAIR) {  // the table counts tiles of 256 rows
+          for (uint32_t i = lane; i < e; i += 32) from += ((uint32_t)max(s.off[i + 1] - s.off[i], 0) + kRows - 1) / kRows;
+          from = __reduce_add_sync(0xFFFFFFFFu, from);
+        }
+        const uint32_t to = from + ((uint32_t)max(s.off[e + 1] - s.off[e], 0) + kRows - 1) / kRows;
+        if (col < width) {
+          float v[4] = {};  // every fourth tile: shorter sums, and loads side by side
+          for (uint32_t q = from; q < to; q += 4)
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i)
+              if (q + i < to) v[i] += part[(uint64_t)(q + i) * pitch + col];
+          a.db[(uint64_t)e * width + col] = (v[0] + v[1]) + (v[2] + v[3]);
+        }
+      }
+    }
   } else if (warp < 4 || warp >= 12) {
     // A copy is 4 rows of 128 bytes; this lane has row lane / 8 of it, piece lane % 8,
     // which the swizzle moves by the row's place in its group of eight.  A warp's
@@ -935,6 +959,76 @@ __device__ __forceinline__ void times_slope(uint32_t act, float slope, const flo
   }
 }
 
+// Matrices that the product does not read where they lie, copied to rows of `pitch`
+// elements (the pads hold 0): x or w, or both, in one launch.  With an index, row i
+// is row index[i] of the source, zeros where there is none.
+struct Pack {
+  const uint16_t *src;
+  const int32_t *index;
+  uint16_t *dst;
+  uint64_t ld, stride, all_rows;  // all_rows: of all matrices
+  uint32_t cols, rows, pitch, src_rows;
+  uint32_t vec;                   // the source's rows are whole 16-byte pieces
+};
+struct Packs {
+  Pack job[2];
+  uint64_t total;  // rows of both
+};
+// CTA `cta` of `ctas` of 256 threads: a warp per row, four pieces of a lane in flight.
+__device__ __forceinline__ void pack_rows(const Packs &p, uint32_t cta, uint32_t ctas) {
+  const uint32_t lane = threadIdx.x & 31;
+  for (uint64_t i = (uint64_t)cta * 8 + threadIdx.x / 32; i < p.total; i += (uint64_t)ctas * 8) {
+    const bool one = i < p.job[0].all_rows;
+    const Pack &k = one ? p.job[0] : p.job[1];
+    const uint64_t row = one ? i : i - p.job[0].all_rows, m = row / k.rows;
+    uint64_t from = row - m * k.rows;
+    uint32_t cols = k.cols;
+    if (k.index) {
+      const int32_t at = (int32_t)ld_word((const uint32_t *)k.index + row);
+      if ((uint32_t)at >= k.src_rows) cols = 0;
+      from = cols ? (uint32_t)at : 0;
+    }
+    const uint16_t *src = k.src + m * k.stride + from * k.ld;
+    uint16_t *to = k.dst + row * k.pitch;
+    if (k.vec) {
+      for (uint32_t c0 = lane * 8; c0 < k.pitch; c0 += 1024) {
+        uint4 q[4];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u) {
+          q[u] = make_uint4(0, 0, 0, 0);
+          if (c0 + 256 * u < cols) q[u] = *reinterpret_cast<const uint4 *>(src + c0 + 256 * u);
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+          if (c0 + 256 * u < k.pitch) *reinterpret_cast<uint4 *>(to + c0 + 256 * u) = q[u];
+      }
+    } else {
+      for (uint32_t c0 = lane * 8; c0 < k.pitch; c0 += 1024) {
+        uint16_t v[4][8];
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+#pragma unroll
+          for (uint32_t q = 0; q < 8; ++q) {
+            v[u][q] = 0;
+            if (c0 + 256 * u + q < cols) v[u][q] = src[c0 + 256 * u + q];
+          }
+#pragma unroll
+        for (uint32_t u = 0; u < 4; ++u)
+          if (c0 + 256 * u < k.pitch)
+            *reinterpret_cast<uint4 *>(to + c0 + 256 * u) =
+                make_uint4(v[u][0] | (uint32_t)v[u][1] << 16, v[u][2] | (uint32_t)v[u][3] << 16,
+                           v[u][4] | (uint32_t)v[u][5] << 16, v[u][6] | (uint32_t)v[u][7] << 16);
+      }
+    }
+  }
+}
+
+__global__ void __launch_bounds__(256) k_pack(const Packs p) {
+  pdl_wait();
+  pdl_trigger();
+  pack_rows(p, blockIdx.x, gridDim.x);
+}
+
 struct DzArgs {
   const void *dy, *z;
   const int32_t *offsets;
@@ -943,6 +1037,8 @@ struct DzArgs {
   uint64_t ld_dy, ld_z;
   uint32_t num_experts, num_rows, width, pitch, activation;
   float slope;
+  uint32_t high;  // rows of CTAs for dz; those after them copy operands
+  Packs packs;
 };
 
 constexpr int kDzThreads = 256;
@@ -964,6 +1060,10 @@ __global__ void __launch_bounds__(kDzThreads, VEC ? 4 : 2) k_dz(const DzArgs a) 
   __shared__ float sums[8][kDzCols];
   pdl_wait();
   pdl_trigger();
+  if (blockIdx.y >= a.high) {
+    pack_rows(a.packs, (blockIdx.y - a.high) * gridDim.x + blockIdx.x, (gridDim.y - a.high) * gridDim.x);
+    return;
+  }
   make_table(s.off, s.tile, a.offsets, a.num_experts, a.num_rows);
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32;
   // this lane's columns: a piece of eight, or eight 32 apart
@@ -974,7 +1074,7 @@ __global__ void __launch_bounds__(kDzThreads, VEC ? 4 : 2) k_dz(const DzArgs a) 
   const bool acts = act != NTC_ACT_NONE;
   const T *dy = (const T *)a.dy, *z = (const T *)a.z;
   T *dz = (T *)a.dz;
-  for (uint32_t q = blockIdx.y; q < total; q += gridDim.y) {
+  for (uint32_t q = blockIdx.y; q < total; q += a.high) {
     const uint32_t e = bucket_of_tile(s.tile, a.num_experts, q);
     const uint32_t row = (uint32_t)s.off[e] + (q - s.tile[e]) * kRows;
     const uint32_t rows = min(kRows, (uint32_t)s.off[e + 1] - row);
@@ -1049,7 +1149,7 @@ __global__ void __launch_bounds__(kDzThreads, VEC ? 4 : 2) k_dz(const DzArgs a) 
 }
 
 // db_e = the sums of e's row tiles, in a fixed order: eight slices of the tiles,
-// then the slices.
+// then the slices.  For calls without dx, whose product does it on the side.
 __global__ void __launch_bounds__(kDzThreads)
     k_db(const float *part, const int32_t *offsets, uint32_t E, uint32_t num_rows, uint32_t width, uint32_t pitch, float *db) {
   extern __shared__ uint8_t raw[];
@@ -1076,62 +1176,6 @@ __global__ void __launch_bounds__(kDzThreads)
 #pragma unroll
       for (int w = 0; w < 8; ++w) t += sums[w][lane];
       db[(uint64_t)e * width + c] = t;
-    }
-  }
-}
-
-// Matrices that the product does not read where they lie, copied to rows of `pitch`
-// elements (the pads hold 0): x or w, or both, in one launch.  With an index, row i
-// is row index[i] of the source, zeros where there is none.
-struct Pack {
-  const uint16_t *src;
-  const int32_t *index;
-  uint16_t *dst;
-  uint64_t ld, stride, all_rows;  // all_rows: of all matrices
-  uint32_t cols, rows, pitch, src_rows;
-  uint32_t vec;                   // the source's rows are whole 16-byte pieces
-};
-// A warp per row, four pieces of a lane in flight.
-__global__ void __launch_bounds__(256) k_pack(const Pack first, const Pack second) {
-  const uint32_t lane = threadIdx.x & 31;
-  pdl_wait();
-  pdl_trigger();
-  const uint64_t total = first.all_rows + second.all_rows;
-  for (uint64_t i = (uint64_t)blockIdx.x * 8 + threadIdx.x / 32; i < total; i += (uint64_t)gridDim.x * 8) {
-    const bool one = i < first.all_rows;
-    const Pack &k = one ? first : second;
-    const uint64_t row = one ? i : i - first.all_rows, m = row / k.rows;
-    uint64_t from = row - m * k.rows;
-    uint32_t cols = k.cols;
-    if (k.index) {
-      const int32_t at = (int32_t)ld_word((const uint32_t *)k.index + row);
-      if ((uint32_t)at >= k.src_rows) cols = 0;
-      from = cols ? (uint32_t)at : 0;
-    }
-    const uint16_t *p = k.src + m * k.stride + from * k.ld;
-    uint16_t *to = k.dst + row * k.pitch;
-    if (k.vec) {
-      for (uint32_t c0 = lane * 8; c0 < k.pitch; c0 += 1024) {
-        uint4 q[4];
-#pragma unroll
-        for (uint32_t u = 0; u < 4; ++u) {
-          q[u] = make_uint4(0, 0, 0, 0);
-          if (c0 + 256 * u < cols) q[u] = *reinterpret_cast<const uint4 *>(p + c0 + 256 * u);
-        }
-#pragma unroll
-        for (uint32_t u = 0; u < 4; ++u)
-          if (c0 + 256 * u < k.pitch) *reinterpret_cast<uint4 *>(to + c0 + 256 * u) = q[u];
-      }
-    } else {
-      for (uint32_t c = lane * 8; c < k.pitch; c += 256) {
-        uint32_t w[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const uint32_t lo = c + 2 * q < cols ? p[c + 2 * q] : 0u, hi = c + 2 * q + 1 < cols ? p[c + 2 * q + 1] : 0u;
-          w[q] = lo | (hi << 16);
-        }
-        *reinterpret_cast<uint4 *>(to + c) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
     }
   }
 }
@@ -1191,9 +1235,10 @@ unsigned int *status_word() {
 template <int MODE, int BN, typename T, bool PAIR = false>
 cudaError_t launch_tile(const Operand &A, const Operand &B, LinearArgs a, uint64_t tiles_bound, int sms, cudaStream_t st) {
   CUtensorMap ma, ma32, mb;
-  if (!make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 128) || !make_map(&ma32, A, 2, 64, 32) ||
+  if (!make_map(&ma, A, 2, 64, MODE == kDw ? 64 : 128) || (MODE != kDw && !make_map(&ma32, A, 2, 64, 32)) ||
       !make_map(&mb, B, MODE == kDw ? 2 : 3, 64, MODE == kForward ? own_cols(BN, PAIR) : 64))
     return cudaErrorInvalidValue;
+  if (MODE == kDw) ma32 = ma;
   a.x = (const uint8_t *)A.p;
   a.ld_x = A.ld;
   a.dz = (const uint8_t *)B.p;
@@ -1341,18 +1386,19 @@ ntc_status check_workspace(const void *p, size_t have, size_t need) {
 }
 
 // The operands x and w, through the workspace where they are copied (a null one is
-// not wanted); *rows is null afterwards where the copy has x in order.
-cudaError_t operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, bool dw, const void *w, uint8_t *ws,
-                     Operand *X, Operand *W, cudaStream_t st) {
+// not wanted), and the copies to make; *rows is null afterwards where the copy has x
+// in order.
+Packs operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, bool dw, const void *w, uint8_t *ws, Operand *X,
+               Operand *W) {
   const uint32_t pitch = (uint32_t)round8(d.in_dim);
-  Pack job[2] = {};
+  Packs p{};
   int jobs = 0;
   if (x) {
     const bool gathers = x_gathers(d, *rows, dw);
     *X = Operand{x, d.in_dim, d.num_x_rows, d.ld_x};
     if (gathers || x_packs(d, x)) {
       const uint64_t n = gathers ? d.num_rows : d.num_x_rows;
-      Pack &k = job[jobs++];
+      Pack &k = p.job[jobs++];
       k.src = (const uint16_t *)x;
       k.index = gathers ? *rows : nullptr;
       k.dst = (uint16_t *)ws;
@@ -1371,7 +1417,7 @@ cudaError_t operands(const ntc_linear_desc &d, const void *x, const int32_t **ro
   if (w) {
     *W = Operand{w, d.in_dim, d.out_dim, d.ld_w, d.num_experts, d.stride_w};
     if (w_packs(d, w)) {
-      Pack &k = job[jobs++];
+      Pack &k = p.job[jobs++];
       k.src = (const uint16_t *)w;
       k.dst = (uint16_t *)ws;
       k.ld = d.ld_w;
@@ -1383,11 +1429,13 @@ cudaError_t operands(const ntc_linear_desc &d, const void *x, const int32_t **ro
       *W = Operand{ws, d.in_dim, d.out_dim, pitch, d.num_experts, (uint64_t)pitch * d.out_dim};
     }
   }
-  if (jobs == 0) return cudaSuccess;
-  if (jobs == 1) job[1].rows = 1;  // no rows, but a divisor
-  const uint64_t total = job[0].all_rows + job[1].all_rows;  // warps' worth
-  const unsigned grid = (unsigned)std::min<uint64_t>((total + 7) / 8, (uint64_t)sm_count() * 32);
-  return launch_pdl(k_pack, grid, 256, 0, st, job[0], job[1]);
+  for (; jobs < 2; ++jobs) p.job[jobs].rows = 1;  // no rows, but a divisor
+  p.total = p.job[0].all_rows + p.job[1].all_rows;
+  return p;
+}
+unsigned pack_ctas(const Packs &p) { return (unsigned)std::min<uint64_t>((p.total + 7) / 8, (uint64_t)sm_count() * 32); }
+cudaError_t launch_packs(const Packs &p, cudaStream_t st) {
+  return p.total ? launch_pdl(k_pack, pack_ctas(p), 256, 0, st, p) : cudaSuccess;
 }
 
 }  // namespace
@@ -1439,7 +1487,7 @@ extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void
   a.status = status_word();
   if (!a.status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
   Operand X, W;
-  cudaError_t e = operands(d, x, &rows, false, w, (uint8_t *)workspace, &X, &W, st);
+  cudaError_t e = launch_packs(operands(d, x, &rows, false, w, (uint8_t *)workspace, &X, &W), st);
   a.rows = rows;
   a.x_rows = (uint32_t)X.rows;
   if (e == cudaSuccess) e = launch_product<kForward>(X, W, a, st);
@@ -1489,8 +1537,11 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
     Z = Operand{dz, d.out_dim, d.num_rows, round8(d.out_dim)};
     ws += dz_bytes(d);
   }
+  Operand X, W;
+  const Packs packs = operands(d, dw ? x : nullptr, &rows, true, dx ? w : nullptr, ws, &X, &W);
   if ((writes && (dx || dw)) || db) {
     DzArgs k{};
+    k.packs = packs;
     k.dy = dy;
     k.z = z;
     k.offsets = offsets;
@@ -1506,14 +1557,17 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
     k.slope = d.leaky_slope;
     const bool vec = d.out_dim % 8 == 0 && rows_are_vec(dy, d.ld_y, 2) && (!z || rows_are_vec(z, d.ld_z, 2));
     const unsigned cols = (d.out_dim + kDzCols - 1) / kDzCols;
-    const unsigned high = (unsigned)std::min<uint64_t>(row_tiles_bound(d.num_rows, d.num_experts),
-                                                       std::max(1u, (unsigned)sm_count() * 8 / cols));
+    k.high = (uint32_t)std::min<uint64_t>(row_tiles_bound(d.num_rows, d.num_experts),
+                                          std::max(1u, (unsigned)sm_count() * 8 / cols));
+    const unsigned more = packs.total ? (pack_ctas(packs) + cols - 1) / cols : 0;
     const auto kernel = d.type == NTC_TYPE_BF16 ? (vec ? k_dz<__nv_bfloat16, true> : k_dz<__nv_bfloat16, false>)
                                                 : (vec ? k_dz<__half, true> : k_dz<__half, false>);
-    e = launch_pdl(kernel, dim3(cols, high), kDzThreads, sizeof(TableShared), st, k);
-    if (e == cudaSuccess && db)
+    e = launch_pdl(kernel, dim3(cols, k.high + more), kDzThreads, sizeof(TableShared), st, k);
+    if (e == cudaSuccess && db && !dx)  // else idle warps of dx's product sum it
       e = launch_pdl(k_db, dim3((d.out_dim + 31) / 32, std::min(d.num_experts, 1024u)), kDzThreads, sizeof(TableShared), st,
                      (const float *)part, offsets, d.num_experts, (uint32_t)d.num_rows, d.out_dim, k.pitch, db);
+  } else {
+    e = launch_packs(packs, st);
   }
   LinearArgs a{};
   a.offsets = offsets;
@@ -1523,9 +1577,10 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
   a.bf16 = d.type == NTC_TYPE_BF16;
   a.ld_out = d.in_dim;
   a.status = status;
-  Operand X, W;
-  if (e == cudaSuccess) e = operands(d, dw ? x : nullptr, &rows, true, dx ? w : nullptr, ws, &X, &W, st);
   if (e == cudaSuccess && dx) {
+    a.part = db ? part : nullptr;
+    a.db = db;
+    a.part_pitch = (uint32_t)round8(d.out_dim);
     a.out = dx;
     a.depth = d.out_dim;
     a.vec_out = rows_are_vec(dx, d.in_dim, 2);

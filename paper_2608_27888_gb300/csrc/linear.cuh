@@ -22,6 +22,10 @@ struct LinearArgs {
   uint32_t bf16;
   uint32_t vec_out;    // every row of out, z and residual is whole 16-byte pieces, and bias starts on one
   unsigned int *status;
+  // dx: sums of dz over every 128 rows of an expert, and the bias' gradient to make of them
+  const float *part;
+  float *db;
+  uint32_t part_pitch;
 };
 
 // The normal distribution function Phi(z), and e = exp(-z^2 / 2), which its density
