@@ -394,8 +394,9 @@ NTC_API ntc_status ntc_kmeans_map(const float *h_features, uint32_t n, uint32_t 
  *
  * The calls keep no state and need no context.  Every pointer is a device
  * pointer unless named h_*; matrices are row-major with a leading dimension in
- * elements; calls are asynchronous on cuda_stream (a cudaStream_t) and may be
- * captured in a graph.  Outputs must not overlap inputs.  Indices that come
+ * elements; calls are asynchronous on cuda_stream (a cudaStream_t) and, after a
+ * first one of their kind on the device, may be captured in a graph.  Outputs must
+ * not overlap inputs.  Indices that come
  * from device memory (ids, rows, place, offsets) are checked by the kernels: no
  * value of theirs leads outside the buffers. */
 
@@ -496,7 +497,7 @@ NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, 
 
 /* x[num_x_rows][ld_x], w[E][N][ld_w], bias[E][N] fp32 (contiguous) or NULL,
  * residual[num_rows][ld_residual] or NULL, rows[num_rows] int32 or NULL,
- * offsets[E + 1] int32 (non-decreasing) or NULL; out: y[num_rows][ld_y] and,
+ * offsets[E + 1] int32 (from 0 on, non-decreasing) or NULL; out: y[num_rows][ld_y] and,
  * unless NULL, z[num_rows][ld_z]. */
 NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void *x, const int32_t *rows,
                               const int32_t *offsets, const void *w, const float *bias, const void *residual,

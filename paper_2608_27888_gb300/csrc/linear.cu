@@ -1210,7 +1210,7 @@ bool make_map(CUtensorMap *m, const Operand &o, int dims, uint32_t box_cols, uin
   const EncodeTiled fn = encode_tiled();
   if (!fn) return false;
   const cuuint64_t size[3] = {o.cols, o.rows, o.many};
-  const cuuint64_t step[2] = {o.ld * 2, o.many > 1 ? o.stride * 2 : o.ld * o.rows * 2};
+  const cuuint64_t step[2] = {o.ld * 2, (o.many > 1 ? o.stride : o.ld) * 2};
   const cuuint32_t box[3] = {box_cols, box_rows, 1}, ones[3] = {1, 1, 1};
   return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT16, (cuuint32_t)dims, const_cast<void *>(o.p), size, step, box, ones,
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,

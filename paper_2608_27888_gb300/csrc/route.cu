@@ -75,6 +75,31 @@ __device__ __forceinline__ void load_run(const T *p, int n, bool vec, float (&l)
   }
 }
 
+// V values to and from shared memory (at a multiple of V values), four at a time.
+template <int V>
+__device__ __forceinline__ void put_run(float *p, const float (&v)[V]) {
+  if constexpr (V % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) p[i] = v[i];
+  }
+}
+template <int V>
+__device__ __forceinline__ void get_run(const float *p, float (&v)[V]) {
+  if constexpr (V % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      const float4 q = *reinterpret_cast<const float4 *>(p + i);
+      v[i] = q.x, v[i + 1] = q.y, v[i + 2] = q.z, v[i + 3] = q.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = p[i];
+  }
+}
+
 // Reductions over the G lanes of a token (whole groups of a converged warp).
 template <int G>
 __device__ __forceinline__ float group_max(float v) {
@@ -287,13 +312,11 @@ __global__ void __launch_bounds__(kWarps * 32)
     for (int i = 0; i < V; ++i) c[i] = l[i] > least[i] ? s[i] + b[i] : -INFINITY;
     if (gr.groups > 1) keep_groups<V, G>(c, gr, lane, sub);
     __syncwarp();  // the last token's reads of shared memory
-#pragma unroll
-    for (int i = 0; i < V; ++i) scores[lane * V + i] = s[i];
+    put_run<V>(scores + lane * V, s);
 
     int32_t id = -1;  // lane j of the token: the j-th choice
     if constexpr (kSorted) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) all[lane * V + i] = c[i];
+      put_run<V>(all + lane * V, c);
       sort_down<V>(c);
 #pragma unroll
       for (int i = 1; i < V; ++i) heads[i * 32] = c[i];
@@ -322,7 +345,8 @@ __global__ void __launch_bounds__(kWarps * 32)
         left = lane - (31 - __clz(starts));
       }
       if (what > -INFINITY) {
-        const float *theirs = all + (lane - sub + from) * V;
+        float theirs[V];
+        get_run<V>(all + (lane - sub + from) * V, theirs);
 #pragma unroll
         for (int i = 0; i < V; ++i)
           if (theirs[i] == what && left-- == 0) id = (int32_t)(from * V) + i;
@@ -491,7 +515,8 @@ template <typename T, int V, int G>
 cudaError_t launch(const ntc_route_desc &d, uint64_t n, const void *logits, uint64_t ld, const float *bias,
                    int32_t *ids, float *weights, cudaStream_t st) {
   constexpr uint64_t kTokens = kWarps * 32 / G;
-  const unsigned grid = (unsigned)std::min<uint64_t>((n + kTokens - 1) / kTokens, (uint64_t)sm_count() * 16);
+  // eight CTAs an SM, as many as fit: tokens come in turns, the last turn is short
+  const unsigned grid = (unsigned)std::min<uint64_t>((n + kTokens - 1) / kTokens, (uint64_t)sm_count() * 8);
   constexpr size_t kRun = V * sizeof(T) < 16 ? V * sizeof(T) : 16;  // bytes of one load
   const bool vec = ((uintptr_t)logits % kRun) == 0 && (ld * sizeof(T)) % kRun == 0;
   return launch_pdl(k_route<T, V, G>, grid, kWarps * 32, 0, st, d, n, (const T *)logits, ld, bias, ids, weights, vec);
@@ -522,7 +547,7 @@ template <typename T, int G>
 cudaError_t launch_back(const ntc_route_desc &d, uint64_t n, const void *logits, uint64_t ld, const int32_t *ids,
                         const float *dweights, void *dlogits, cudaStream_t st) {
   constexpr uint64_t kTokens = kWarps * 32 / G;
-  const unsigned grid = (unsigned)std::min<uint64_t>((n + kTokens - 1) / kTokens, (uint64_t)sm_count() * 16);
+  const unsigned grid = (unsigned)std::min<uint64_t>((n + kTokens - 1) / kTokens, (uint64_t)sm_count() * 64);
   return launch_pdl(k_route_back<T, G>, grid, kWarps * 32, kTokens * ((d.num_experts + 7) / 8 * 8) * 4, st, d, n,
                     (const T *)logits, ld, ids, dweights, (T *)dlogits, rows_are_vec(dlogits, d.num_experts, sizeof(T)));
 }
