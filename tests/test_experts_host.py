@@ -171,39 +171,24 @@ def test_combine_pointer_refusals():
     assert f(none, None, None, None, None, None, None, None) == ntc.NTC_OK
 
 
-def test_the_python_functions_check_their_tensors():
+def test_the_python_functions_check_their_arguments():
     import torch
-    from paper_2608_27888_gb300 import experts
-    for call in (lambda: ntc.route(torch.zeros(2, 8), 2), lambda: ntc.linear(torch.zeros(2, 8), torch.zeros(4, 8)),
-                 lambda: ntc.combine(torch.zeros(2, 8), torch.zeros(2, 1, dtype=torch.int32)),
-                 lambda: ntc.expert_order(torch.zeros(2, 1, dtype=torch.int32), 2)):
+    cpu = torch.zeros(2, 8)
+    ids = torch.zeros(2, 1, dtype=torch.int32)
+    for call in (lambda: ntc.route(cpu, 2), lambda: ntc.route_backward(cpu, ids, cpu[:, :1]), lambda: ntc.linear(cpu, cpu),
+                 lambda: ntc.linear_backward(cpu, cpu, cpu), lambda: ntc.combine(cpu, ids),
+                 lambda: ntc.combine_backward(cpu, cpu, ids), lambda: ntc.expert_order(ids, 2)):
         with pytest.raises(ValueError, match="CUDA tensor"):
             call()
-    cpu = torch.device("cpu")
-    with pytest.raises(ValueError, match="shape"):
-        experts._array(torch.zeros(3), "bias", (4,), torch.float32, cpu)
-    with pytest.raises(ValueError, match="float32"):
-        experts._array(torch.zeros(4).half(), "bias", (4,), torch.float32, cpu)
-    with pytest.raises(ValueError, match="contiguous"):
-        experts._array(torch.zeros(8)[::2], "bias", (4,), torch.float32, cpu)
-    with pytest.raises(ValueError, match="last dimension"):
-        experts._matrix(torch.zeros(4, 3).t(), "x", 3, 4, torch.float32, cpu)
-    with pytest.raises(ValueError, match="overlapping"):
-        experts._matrix(torch.zeros(1, 4).expand(3, 4), "x", 3, 4, torch.float32, cpu)
-    with pytest.raises(ValueError, match="must be one of"):
-        experts._choice(ntc.ACTIVATIONS, "tanh", "activation")
-    with pytest.raises(ValueError, match="out of range"):
-        experts._pack(experts._ROUTE, -1, 1, 1, 1, 0, True, 1.0, 0)
-    with pytest.raises(ValueError, match="two or three"):
-        experts._operands(torch.zeros(2, 3), torch.zeros(3), cpu)
+    with pytest.raises(TypeError, match="w must be a tensor"):
+        ntc.linear(cpu, [1.0])
+    with pytest.raises(ValueError, match="activation must be one of"):
+        ntc.linear(cpu, cpu, activation="tanh")
+    with pytest.raises(ValueError, match="score must be one of"):
+        ntc.route(cpu, 2, score="max")
+    with pytest.raises(ValueError, match="need must name"):
+        ntc.linear_backward(cpu, cpu, cpu, need=("dz",))
+    with pytest.raises(ValueError, match="need must name"):
+        ntc.combine_backward(cpu, cpu, ids, need=("y",))
     with pytest.raises(AttributeError):
         ntc.no_such_name
-
-
-def test_packed_descriptors_are_the_structures():
-    """experts.py packs the descriptors with struct: the same bytes as the ctypes structures."""
-    from paper_2608_27888_gb300 import experts
-    for layout, cls in ((experts._ROUTE, ntc.ntc_route_desc), (experts._LINEAR, ntc.ntc_linear_desc),
-                        (experts._COMBINE, ntc.ntc_combine_desc)):
-        values = [1.5 if t is ctypes.c_float else i + 3 for i, (_, t) in enumerate(cls._fields_)]
-        assert layout.pack(*values) == bytes(cls(*values))
