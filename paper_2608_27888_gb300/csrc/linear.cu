@@ -17,14 +17,14 @@
 //                instruction, that arrive at the stage's barrier by themselves; the
 //                proxy fence is the MMA warp's.  (A fence by the copying threads
 //                waits for all of their copies in flight, 2,000 cycles a chunk.)
+//   warps 4..11  the epilogue of one accumulator while the other is filled: 16
+//                columns at a time through a warp's own shared memory, so that
+//                global memory sees 32-byte runs of a row, not one row a lane.
 // Where experts have many rows, two CTAs on neighbouring SMs have a tile of 256 x 256
 // (cta_group::2): each holds its 128 rows of A, half of B and its rows of the
 // accumulator, one issues the MMAs of both.  That is a third less to copy and to
 // read from shared memory per product, which is what bounds the large products, by
 // bandwidth and by power.
-//   warps 4..11  the epilogue of one accumulator while the other is filled: 16
-//                columns at a time through a warp's own shared memory, so that
-//                global memory sees 32-byte runs of a row, not one row a lane.
 // A weight matrix [N][K] is read as it lies: K-major in the forward product,
 // MN-major (the descriptors' transpose bits) in kDx; kDw takes both operands
 // MN-major.  Nothing is transposed in memory.
