@@ -17,9 +17,9 @@
 //                instruction, that arrive at the stage's barrier by themselves; the
 //                proxy fence is the MMA warp's.  (A fence by the copying threads
 //                waits for all of their copies in flight, 2,000 cycles a chunk.)
-//   warps 4..11  the epilogue of one accumulator while the other is filled: 16
-//                columns at a time through a warp's own shared memory, so that
-//                global memory sees 32-byte runs of a row, not one row a lane.
+//   warps 4..11  the epilogue of one accumulator while the other is filled: a lane
+//                has a row and 32 columns, which are rounded and leave through the
+//                warp's own shared memory in 64-byte runs.
 // Where experts have many rows, two CTAs on neighbouring SMs have a tile of 256 x 256
 // (cta_group::2): each holds its 128 rows of A, half of B and its rows of the
 // accumulator, one issues the MMAs of both.  That is a third less to copy and to
@@ -350,11 +350,13 @@ struct Strip {
   uint32_t lane;
 };
 
-// What happens to 32 rows x 32 columns of an accumulator, a lane having a row: they
-// go through the warp's staging, 16 columns at a time, and leave in 32-byte runs.
-// The work of 16 values a lane is laid out side by side: a warp's epilogue is bound by
-// the latency of its own instructions, and has to end within the next tile's MMAs
-// (32 x 512 cycles at K = 2,048; the arguments are copies for the same reason).
+// What happens to 32 rows x 32 columns of an accumulator, a lane having a row: rounded,
+// they go through the warp's staging.  The work of 32 values is laid out side by
+// side: a warp's epilogue is bound by the latency of its own instructions, and has to
+// end within the next tile's MMAs (32 x 512 cycles at K = 2,048; the arguments are
+// copies for the same reason).  At short contractions it does not: 16,384 rows, 128 ->
+// 2,048, one expert take 32.8 us, 38.3 with fp32 values staged and 32-byte runs (K =
+// 1,024: 45.9 and 51.8), about 15 without an epilogue.
 template <typename T>
 struct Epilogue {
   const float *bias;
@@ -369,86 +371,78 @@ struct Epilogue {
         ld_residual(a.ld_residual), width(a.width), height(a.height), act(a.activation), slope(a.slope),
         vec(a.vec_out != 0) {}
 
-  // The bias and the residual of the next 32 columns.
+  // The bias and the residual of this lane's row in the next 32 columns.
   struct Ahead {
-    float4 b[2][2];
-    uint4 r[2][2];
+    float4 b[8];
+    uint4 r[4];
   };
   __device__ __forceinline__ void ask(Ahead &x, uint32_t e, const Strip &g, int32_t c) const {
     if (!vec) return;
+    if (bias) {
+      const float4 *b = reinterpret_cast<const float4 *>(bias + (uint64_t)e * width + g.col + c);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int32_t at = c + 16 * h + (int32_t)(g.lane & 1) * 8;
-      x.b[h][0] = x.b[h][1] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      x.r[h][0] = x.r[h][1] = make_uint4(0, 0, 0, 0);
-      if (at < g.cols) {
-        if (bias) {
-          const float4 *b = reinterpret_cast<const float4 *>(bias + (uint64_t)e * width + g.col + at);
-          x.b[h][0] = b[0];
-          x.b[h][1] = b[1];
-        }
-        if (residual) {
-          const T *r = residual + (g.row + (g.lane >> 1)) * ld_residual + g.col + at;
-          if ((int32_t)(g.lane >> 1) < g.high) x.r[h][0] = *reinterpret_cast<const uint4 *>(r);
-          if ((int32_t)(g.lane >> 1) + 16 < g.high) x.r[h][1] = *reinterpret_cast<const uint4 *>(r + 16 * ld_residual);
-        }
-      }
+      for (int q = 0; q < 8; ++q) x.b[q] = c + 4 * q < g.cols ? b[q] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    }
+    if (residual) {
+      const uint4 *r = reinterpret_cast<const uint4 *>(residual + (g.row + g.lane) * ld_residual + g.col + c);
+      const bool in = (int32_t)g.lane < g.high;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x.r[q] = in && c + 8 * q < g.cols ? r[q] : make_uint4(0, 0, 0, 0);
     }
   }
 
-  // Rows of whole 16-byte pieces: lane i has a piece of rows i / 2 and i / 2 + 16.
+  // Rows of whole 16-byte pieces, this lane's row and 32 columns of it.
   template <bool FORWARD>
   __device__ __forceinline__ void store_rows(const Strip &g, uint32_t e, int32_t c, const uint32_t (&r)[32], Ahead &ahead,
                                              uint8_t *mine) const {
-    const uint32_t rl = g.lane >> 1;
-    const bool in0 = (int32_t)rl < g.high, in1 = (int32_t)rl + 16 < g.high;
-    Ahead x;
-    if (FORWARD) {
-      x = ahead;
-      if (c + 32 < g.cols) ask(ahead, e, g, c + 32);
-    }
+    float v[32];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+    if constexpr (FORWARD) {
+      if (bias) {
 #pragma unroll
-      for (uint32_t q = 0; q < 4; ++q)
-        *reinterpret_cast<uint4 *>(mine + staged(g.lane, q)) =
-            make_uint4(r[16 * h + 4 * q], r[16 * h + 4 * q + 1], r[16 * h + 4 * q + 2], r[16 * h + 4 * q + 3]);
-      __syncwarp();
-      float v[16];
-#pragma unroll
-      for (uint32_t q = 0; q < 4; ++q) {
-        const float4 f = *reinterpret_cast<const float4 *>(mine + staged(rl + 16 * (q >> 1), (g.lane & 1) * 2 + (q & 1)));
-        v[4 * q] = f.x, v[4 * q + 1] = f.y, v[4 * q + 2] = f.z, v[4 * q + 3] = f.w;
+        for (int q = 0; q < 8; ++q)
+          v[4 * q] += ahead.b[q].x, v[4 * q + 1] += ahead.b[q].y, v[4 * q + 2] += ahead.b[q].z, v[4 * q + 3] += ahead.b[q].w;
       }
-      __syncwarp();
-      const int32_t at = c + 16 * h + (int32_t)(g.lane & 1) * 8;
-      const bool put0 = in0 && at < g.cols, put1 = in1 && at < g.cols;
-      if constexpr (FORWARD) {
-        const float b[8] = {x.b[h][0].x, x.b[h][0].y, x.b[h][0].z, x.b[h][0].w,
-                            x.b[h][1].x, x.b[h][1].y, x.b[h][1].z, x.b[h][1].w};
+      uint4 x[4];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += b[i & 7];
-        if (z) put(z + (g.row + rl) * ld_z + g.col + at, ld_z, v, put0, put1);
-        activate(act, slope, v);
-        if (residual) {
+      for (int q = 0; q < 4; ++q) x[q] = ahead.r[q];
+      if (c + 32 < g.cols) ask(ahead, e, g, c + 32);
+      if (z) put(z, ld_z, g, c, v, mine);
+      activate(act, slope, v);
+      if (residual) {
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            float u[8];
-            Vec<T>::unpack(x.r[h][q], u);
+        for (int q = 0; q < 4; ++q) {
+          float u[8];
+          Vec<T>::unpack(x[q], u);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[8 * q + i] += u[i];
-          }
+          for (int i = 0; i < 8; ++i) v[8 * q + i] += u[i];
         }
       }
-      put(out + (g.row + rl) * ld_out + g.col + at, ld_out, v, put0, put1);
     }
+    put(out, ld_out, g, c, v, mine);
   }
-  static __device__ __forceinline__ void put(T *p, uint64_t ld, const float (&v)[16], bool put0, bool put1) {
-    float a[8], b[8];
+  // Rounded, through the warp's staging, and out in 64-byte runs of eight rows at a time.
+  static __device__ __forceinline__ void put(T *to, uint64_t ld, const Strip &g, int32_t c, const float (&v)[32],
+                                             uint8_t *mine) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a[i] = v[i], b[i] = v[8 + i];
-    if (put0) *reinterpret_cast<uint4 *>(p) = Vec<T>::pack(a);
-    if (put1) *reinterpret_cast<uint4 *>(p + 16 * ld) = Vec<T>::pack(b);
+    for (uint32_t q = 0; q < 4; ++q) {
+      float a[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = v[8 * q + i];
+      *reinterpret_cast<uint4 *>(mine + staged(g.lane, q)) = Vec<T>::pack(a);
+    }
+    __syncwarp();
+    const uint32_t row = g.lane >> 2;
+    const int32_t at = c + (int32_t)(g.lane & 3) * 8;
+    uint4 p[4];
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) p[j] = *reinterpret_cast<const uint4 *>(mine + staged(row + 8 * j, g.lane & 3));
+    __syncwarp();
+    T *from = to + (g.row + row) * ld + g.col + at;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j)
+      if ((int32_t)(row + 8 * j) < g.high && at < g.cols) *reinterpret_cast<uint4 *>(from + 8 * j * ld) = p[j];
   }
 
   // Rows at odd addresses: lanes on consecutive columns, two rows at a time.
