@@ -116,6 +116,11 @@ __device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ void arrive_there(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
 }
+// The same where only tensor memory is handed over, whose loads have ended: the release
+// above would first wait for all of the warp's stores to be visible.
+__device__ __forceinline__ void signal_there(uint32_t bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(bar) : "memory");
+}
 __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
 }
@@ -689,7 +694,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       const Tile o = tiles.at(t);
       const uint32_t depth = uniform(o.depth), chunks = (depth + kChunk - 1) / kChunk;
       if (chunks == 0) continue;
-      ok = __all_sync(0xFFFFFFFFu, wait_pair(saddr(&s.acc_empty[acc & 1]), ((acc >> 1) & 1) ^ 1));
+      ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.acc_empty[acc & 1]), ((acc >> 1) & 1) ^ 1));
       if (!ok) break;
       fence_after();
       const uint32_t d = columns + (acc & 1) * BN;
@@ -910,7 +915,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       fence_before();
       __syncwarp();
       if (lane == 0) {
-        if (PAIR) arrive_there(in_cta(saddr(&s.acc_empty[acc & 1]), 0));
+        if (PAIR) signal_there(in_cta(saddr(&s.acc_empty[acc & 1]), 0));
         else mbar_arrive(saddr(&s.acc_empty[acc & 1]));
       }
       ++acc;
