@@ -1277,14 +1277,20 @@ uint64_t row_tiles_bound(uint64_t num_rows, uint64_t num_experts) {
   return std::min<uint64_t>(num_rows, (num_rows + kRows - 1) / kRows + num_experts);
 }
 
-// Whether pairs of CTAs take a product: experts with 1,024 rows or more on average (a
-// tile of theirs has 256), and a tile for every SM.  Without an index: the copies of
-// gathered rows would have to be passed on from one CTA to the other, chunk by chunk
-// (944 us instead of 363 by single CTAs, 32,768 rows, 2,048 -> 4,096).  Without one,
-// 352 us by single CTAs and 292 by pairs.
-bool pairs_take(int mode, uint64_t num_rows, uint64_t num_experts, uint64_t width, uint64_t height) {
+// Whether pairs of CTAs take a product: a tile for every SM, and
+//   forward and dx: 1,024 of the contraction or more (at 512 a tile's MMAs end before the
+//     epilogue, and single CTAs wait for less: 16 experts of 768 rows, 512 -> 2,048: 45.3
+//     us single, 45.7 pairs; 1,024 -> 2,048: 54.3, 50.3; 2,048 -> 4,096: 147, 136) and 128
+//     rows an expert (2,048 -> 1,024, 32 experts: 40.6 and 35.4 us; with fewer the half of
+//     a tile of 256 rows is empty and weights' bytes count: 32 rows, dx, 27.8 and 29.8);
+//   dw: 256 rows an expert, its contraction (2,048 -> 4,096, 32 experts: 199 and 203 us at
+//     32 rows, 226 and 221 at 256, 284 and 265 at 512).
+// Never with an index: the copies of gathered rows would have to be passed on from one
+// CTA to the other, chunk by chunk (944 us instead of 363 by single CTAs, 32,768 rows,
+// 2,048 -> 4,096).
+bool pairs_take(int mode, uint64_t num_rows, uint64_t num_experts, uint64_t width, uint64_t height, uint64_t depth) {
   const uint64_t high = mode == kDw ? num_experts * ((height + 255) / 256) : (num_rows + 255) / 256 + num_experts;
-  return (mode == kDw ? height >= 256 : num_rows >= 1024 * num_experts) &&
+  return (mode == kDw ? height >= 256 && num_rows >= 256 * num_experts : depth >= 1024 && num_rows >= 128 * num_experts) &&
          high * ((width + 255) / 256) >= (uint64_t)sm_count();
 }
 
@@ -1299,7 +1305,7 @@ cudaError_t launch_product_of(const Operand &A, const Operand &B, const LinearAr
                                     : row_tiles_bound(a.num_rows, a.num_experts);
   if (high == 0) return cudaSuccess;
   const auto tiles = [&](uint32_t bn) { return high * ((a.width + bn - 1) / bn); };
-  if (!a.rows && pairs_take(MODE, a.num_rows, a.num_experts, a.width, a.height))
+  if (!a.rows && pairs_take(MODE, a.num_rows, a.num_experts, a.width, a.height, a.depth))
     return launch_tile<MODE, 256, T, true>(A, B, a, tiles(256), sms, st);
   const bool thin = MODE != kDw && a.num_rows <= 32ull * a.num_experts;
   if (!thin && tiles(256) >= (uint64_t)sms) return launch_tile<MODE, 256, T>(A, B, a, tiles(256), sms, st);
@@ -1319,12 +1325,15 @@ uint64_t round256(uint64_t x) { return (x + 255) / 256 * 256; }
 
 bool tma_reads(const void *p, uint64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 // Gathered rows are copied in order where pairs of CTAs then take the product and its
-// other width pays for the copy: 40 us of 32,768 rows of 2,048, against 363 - 295 (out
-// 4,096 wide) in the forward product, 481 - 323 in dw.
+// other width pays for the copy.  Forward, from 768 rows an expert (16 experts, 2,048 ->
+// 4,096: 154 us with the gather in the product, 147 with the copy; 1,024 -> 2,048: 59.3,
+// 58.3; 32 experts of 512 rows: 72.0, 74.7; 2,048 -> 1,024: 47.2, 53.7).  dw, whose gather
+// costs more (32 experts of 256 rows, 2,048 -> 1,024: 76 and 74 us; 4,096: 261 and 231).
 bool x_gathers(const ntc_linear_desc &d, const int32_t *rows, bool dw) {
-  return rows && d.out_dim >= (dw ? 1024u : 2048u) &&
-         (dw ? pairs_take(kDw, d.num_rows, d.num_experts, d.out_dim, d.in_dim)
-             : pairs_take(kForward, d.num_rows, d.num_experts, d.out_dim, 0));
+  if (!rows) return false;
+  if (dw) return d.out_dim >= 1024 && pairs_take(kDw, d.num_rows, d.num_experts, d.out_dim, d.in_dim, 0);
+  return d.out_dim >= 2048 && d.num_rows >= 768ull * d.num_experts &&
+         pairs_take(kForward, d.num_rows, d.num_experts, d.out_dim, 0, d.in_dim);
 }
 bool x_packs(const ntc_linear_desc &d, const void *x) { return !tma_reads(x, d.ld_x); }
 bool w_packs(const ntc_linear_desc &d, const void *w) {
