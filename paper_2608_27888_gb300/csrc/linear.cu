@@ -1277,40 +1277,67 @@ uint64_t row_tiles_bound(uint64_t num_rows, uint64_t num_experts) {
   return std::min<uint64_t>(num_rows, (num_rows + kRows - 1) / kRows + num_experts);
 }
 
-// Whether pairs of CTAs take a product: a tile for every SM, and
-//   forward and dx: 1,024 of the contraction or more (at 512 a tile's MMAs end before the
+// Row tiles of `high` rows that the experts are likely to have: the last one of each is
+// half empty, where they have so many rows.
+uint64_t likely_tiles(uint64_t num_rows, uint64_t num_experts, uint64_t high) {
+  if (num_experts == 1) return (num_rows + high - 1) / high;
+  if (num_rows * 8 <= num_experts * high * 7) return std::min(num_rows, num_experts);
+  return num_rows / high + num_experts / 2;
+}
+
+// The tile of a product: the one whose rounds of a tile per SM (or pair of SMs) take least
+// time.  Where a tile of 64 columns takes 100, one of 128 takes 135, of 256 columns 190,
+// and a pair's of 256 x 256 175 (one round of 300 rows, 2,048 -> 1,024: 11.5, 13.8, 17.6
+// us with the launch; two rounds of 64 columns for 2,000 rows 19.8, one of 128 14.7; two
+// rounds of 4,000 rows, 2,048 -> 4,096: 45.9 us single, 43.5 pairs).
+// Pairs take
+//   forward and dx: from 1,024 of the contraction (at 512 a tile's MMAs end before the
 //     epilogue, and single CTAs wait for less: 16 experts of 768 rows, 512 -> 2,048: 45.3
 //     us single, 45.7 pairs; 1,024 -> 2,048: 54.3, 50.3; 2,048 -> 4,096: 147, 136) and 128
 //     rows an expert (2,048 -> 1,024, 32 experts: 40.6 and 35.4 us; with fewer the half of
 //     a tile of 256 rows is empty and weights' bytes count: 32 rows, dx, 27.8 and 29.8);
-//   dw: 256 rows an expert, its contraction (2,048 -> 4,096, 32 experts: 199 and 203 us at
-//     32 rows, 226 and 221 at 256, 284 and 265 at 512).
-// Never with an index: the copies of gathered rows would have to be passed on from one
-// CTA to the other, chunk by chunk (944 us instead of 363 by single CTAs, 32,768 rows,
-// 2,048 -> 4,096).
-bool pairs_take(int mode, uint64_t num_rows, uint64_t num_experts, uint64_t width, uint64_t height, uint64_t depth) {
-  const uint64_t high = mode == kDw ? num_experts * ((height + 255) / 256) : (num_rows + 255) / 256 + num_experts;
-  return (mode == kDw ? height >= 256 && num_rows >= 256 * num_experts : depth >= 1024 && num_rows >= 128 * num_experts) &&
-         high * ((width + 255) / 256) >= (uint64_t)sm_count();
+//   dw: from 256 rows an expert, its contraction (2,048 -> 4,096, 32 experts: 199 and 203
+//     us at 32 rows, 226 and 221 at 256, 284 and 265 at 512);
+//   more tiles than pairs of SMs (64 tiles: 11.2 us single, 12.5 pairs);
+//   no index: the copies of gathered rows would have to be passed on from one CTA to the
+//     other, chunk by chunk (944 us instead of 363 by single CTAs, 32,768 rows, 2,048 ->
+//     4,096).
+// Experts of few rows and a long contraction stream their weights, best in 128 columns (8
+// rows of 32 experts, 2,048 -> 1,024, in 64, 128 and 256 columns: 42.2, 29.9, 31.4 us;
+// 2,048 -> 4,096: 134, 90.6, 93.3; but 1,024 -> 2,048: 40.2, 30.7, 30.2).
+struct Shape {
+  uint32_t cols;
+  bool pair;
+};
+Shape best_shape(int mode, uint64_t num_rows, uint64_t num_experts, uint64_t width, uint64_t height, uint64_t depth,
+                 bool gathers) {
+  const uint64_t sms = (uint64_t)sm_count(), pairs = std::max<uint64_t>(sms / 2, 1);
+  const auto tiles = [&](uint64_t high, uint64_t cols) {
+    const uint64_t down = mode == kDw ? num_experts * ((height + high - 1) / high) : likely_tiles(num_rows, num_experts, high);
+    return down * ((width + cols - 1) / cols);
+  };
+  const auto rounds = [](uint64_t n, uint64_t of) { return (n + of - 1) / of; };
+  const uint64_t t64 = rounds(tiles(kRows, 64), sms) * 100, t128 = rounds(tiles(kRows, 128), sms) * 135,
+                 t256 = rounds(tiles(kRows, 256), sms) * 190, two = tiles(2 * kRows, 256);
+  if (!gathers && two > pairs && rounds(two, pairs) * 175 <= std::min(std::min(t64, t128), t256) &&
+      (mode == kDw ? height >= 256 && num_rows >= 256 * num_experts : depth >= 1024 && num_rows >= 128 * num_experts))
+    return {256, true};
+  if (mode != kDw && depth >= 2048 && num_rows <= kRows * num_experts && tiles(kRows, 128) > sms) return {128, false};
+  return {t256 <= t128 && t256 <= t64 ? 256u : t128 <= t64 ? 128u : 64u, false};
 }
 
-// The width of a tile: the widest whose tiles still fill the SMs, 128 at most where
-// an expert has few rows on average.  Such tiles stream weights, and only the two
-// warps that hold the rows work on their columns (256 rows of 32 experts, 1,024 ->
-// 2,048, gelu, bias and residual: 39.7 us at 256 columns, 36.6 at 128, 40.0 at 64).
 template <int MODE, typename T>
 cudaError_t launch_product_of(const Operand &A, const Operand &B, const LinearArgs &a, cudaStream_t st) {
-  const int sms = sm_count();
   const uint64_t high = MODE == kDw ? (uint64_t)a.num_experts * ((a.height + kRows - 1) / kRows)
                                     : row_tiles_bound(a.num_rows, a.num_experts);
   if (high == 0) return cudaSuccess;
-  const auto tiles = [&](uint32_t bn) { return high * ((a.width + bn - 1) / bn); };
-  if (!a.rows && pairs_take(MODE, a.num_rows, a.num_experts, a.width, a.height, a.depth))
-    return launch_tile<MODE, 256, T, true>(A, B, a, tiles(256), sms, st);
-  const bool thin = MODE != kDw && a.num_rows <= 32ull * a.num_experts;
-  if (!thin && tiles(256) >= (uint64_t)sms) return launch_tile<MODE, 256, T>(A, B, a, tiles(256), sms, st);
-  if (tiles(128) >= (uint64_t)sms) return launch_tile<MODE, 128, T>(A, B, a, tiles(128), sms, st);
-  return launch_tile<MODE, 64, T>(A, B, a, tiles(64), sms, st);
+  const Shape s = best_shape(MODE, a.num_rows, a.num_experts, a.width, a.height, a.depth, a.rows != nullptr);
+  const uint64_t bound = high * ((a.width + s.cols - 1) / s.cols);
+  const int sms = sm_count();
+  if (s.pair) return launch_tile<MODE, 256, T, true>(A, B, a, bound, sms, st);
+  if (s.cols == 256) return launch_tile<MODE, 256, T>(A, B, a, bound, sms, st);
+  if (s.cols == 128) return launch_tile<MODE, 128, T>(A, B, a, bound, sms, st);
+  return launch_tile<MODE, 64, T>(A, B, a, bound, sms, st);
 }
 
 template <int MODE>
@@ -1331,9 +1358,9 @@ bool tma_reads(const void *p, uint64_t ld) { return ((uintptr_t)p & 15) == 0 && 
 // costs more (32 experts of 256 rows, 2,048 -> 1,024: 76 and 74 us; 4,096: 261 and 231).
 bool x_gathers(const ntc_linear_desc &d, const int32_t *rows, bool dw) {
   if (!rows) return false;
-  if (dw) return d.out_dim >= 1024 && pairs_take(kDw, d.num_rows, d.num_experts, d.out_dim, d.in_dim, 0);
+  if (dw) return d.out_dim >= 1024 && best_shape(kDw, d.num_rows, d.num_experts, d.out_dim, d.in_dim, 0, false).pair;
   return d.out_dim >= 2048 && d.num_rows >= 768ull * d.num_experts &&
-         pairs_take(kForward, d.num_rows, d.num_experts, d.out_dim, 0, d.in_dim);
+         best_shape(kForward, d.num_rows, d.num_experts, d.out_dim, 0, d.in_dim, false).pair;
 }
 bool x_packs(const ntc_linear_desc &d, const void *x) { return !tma_reads(x, d.ld_x); }
 bool w_packs(const ntc_linear_desc &d, const void *w) {

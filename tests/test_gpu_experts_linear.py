@@ -412,3 +412,11 @@ def test_large_products(ntc, counts, K, N, gather):
     for name, a, (ref, bound) in zip(("dx", "dw", "db"), got, R.linear_backward(dy, x, w, z, rows, offsets, "silu")):
         R.assert_within(a, ref, bound, name)
     ntc.ntc_linear_status(torch.cuda.current_stream().cuda_stream)
+
+
+# the same where the contraction is long: what pairs of CTAs take, with pairs whose second CTA has all, some or no rows
+@pytest.mark.parametrize("counts,K,N", [((1000, 1100, 900, 1000), 4104, 4104), ((0, 2300, 128, 1300, 129), 1100, 4100),
+                                        ((4000,), 1096, 4098)])
+@pytest.mark.parametrize("gather", [False, True])
+def test_large_products_of_long_contractions(ntc, counts, K, N, gather):
+    test_large_products(ntc, counts, K, N, gather)
