@@ -247,6 +247,8 @@ struct Tile {
   uint32_t col;       // first column
   uint32_t depth;     // contraction length; 0: the tile is zeros
   uint32_t begin;     // kDw: first row of the contraction
+  uint32_t part;      // kDw: which part of the expert's rows
+  uint32_t index;     // kDw: of the tiles of this expert and part
 };
 
 // Experts' rows and row tiles, from offsets that are only trusted to lie
@@ -293,13 +295,13 @@ template <int MODE, int BN, bool PAIR>
 struct Tiles {
   static constexpr uint32_t kHigh = PAIR ? 2 * kRows : kRows, kBandTiles = kBand * kRows / kHigh;
   const Shared &s;
-  uint32_t num_experts, height, depth, cols, row_tiles, shift;  // shift: this CTA's rows in the pair's
+  uint32_t num_experts, height, depth, cols, row_tiles, split, shift;  // shift: this CTA's rows in the pair's
   uint64_t total;
   __device__ __forceinline__ Tiles(const LinearArgs &a, const Shared &sh, uint32_t rank)
-      : s(sh), num_experts(a.num_experts), height(a.height), depth(a.depth), shift(rank * kRows) {
+      : s(sh), num_experts(a.num_experts), height(a.height), depth(a.depth), split(a.split), shift(rank * kRows) {
     cols = (a.width + BN - 1) / BN;
     row_tiles = (a.height + kHigh - 1) / kHigh;
-    total = MODE == kDw ? (uint64_t)a.num_experts * row_tiles * cols : (uint64_t)s.tile[a.num_experts + 1] * cols;
+    total = MODE == kDw ? (uint64_t)a.num_experts * row_tiles * cols * split : (uint64_t)s.tile[a.num_experts + 1] * cols;
   }
   // Within an expert: bands of row tiles, columns inside a band, rows inside
   // a column, so that the CTAs at work at one time share operands.
@@ -308,8 +310,10 @@ struct Tiles {
     uint32_t many, r;
     if constexpr (MODE == kDw) {
       const uint64_t per = (uint64_t)row_tiles * cols;
-      o.e = (uint32_t)(t / per);
-      r = (uint32_t)(t - o.e * per);
+      const uint32_t q = (uint32_t)(t / per);
+      o.part = q / num_experts;
+      o.e = q - o.part * num_experts;
+      o.index = r = (uint32_t)(t - q * per);
       many = row_tiles;
     } else {
       o.e = bucket_of_tile(s.tile, num_experts, (uint32_t)(t / cols));
@@ -325,8 +329,10 @@ struct Tiles {
     o.rows = PAIR ? min(kRows, o.all_rows - min(o.all_rows, shift)) : o.all_rows;
     if constexpr (MODE == kDw) {
       o.row = row + shift;
-      o.begin = begin;
-      o.depth = count;
+      const uint64_t chunks = (count + kChunk - 1) / kChunk;
+      const uint32_t from = (uint32_t)(chunks * o.part / split) * kChunk;
+      o.begin = begin + from;
+      o.depth = min(count, (uint32_t)(chunks * (o.part + 1) / split) * kChunk) - min(count, from);
     } else {
       o.row = begin + row + shift;
       o.begin = 0;
@@ -367,16 +373,17 @@ struct Epilogue {
   const float *bias;
   const T *residual;
   T *out, *z;
+  float *sums;
   uint64_t ld_out, ld_z, ld_residual;
-  uint32_t width, height, act;
+  uint32_t width, height, experts, act;
   float slope;
   bool vec;
   __device__ __forceinline__ explicit Epilogue(const LinearArgs &a)
-      : bias(a.bias), residual((const T *)a.residual), out((T *)a.out), z((T *)a.z), ld_out(a.ld_out), ld_z(a.ld_z),
-        ld_residual(a.ld_residual), width(a.width), height(a.height), act(a.activation), slope(a.slope),
+      : bias(a.bias), residual((const T *)a.residual), out((T *)a.out), z((T *)a.z), sums(a.sums), ld_out(a.ld_out), ld_z(a.ld_z),
+        ld_residual(a.ld_residual), width(a.width), height(a.height), experts(a.num_experts), act(a.activation), slope(a.slope),
         vec(a.vec_out != 0) {}
 
-  // The bias and the residual of this lane's row in the next 32 columns.
+  // The bias of the next 32 columns, and the residual's pieces as put() stores them.
   struct Ahead {
     float4 b[8];
     uint4 r[4];
@@ -389,10 +396,12 @@ struct Epilogue {
       for (int q = 0; q < 8; ++q) x.b[q] = c + 4 * q < g.cols ? b[q] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     }
     if (residual) {
-      const uint4 *r = reinterpret_cast<const uint4 *>(residual + (g.row + g.lane) * ld_residual + g.col + c);
-      const bool in = (int32_t)g.lane < g.high;
+      const int32_t row = (int32_t)(g.lane >> 2), at = c + (int32_t)(g.lane & 3) * 8;
+      const T *r = residual + (g.row + row) * ld_residual + g.col + at;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) x.r[q] = in && c + 8 * q < g.cols ? r[q] : make_uint4(0, 0, 0, 0);
+      for (int q = 0; q < 4; ++q)
+        x.r[q] = row + 8 * q < g.high && at < g.cols ? *reinterpret_cast<const uint4 *>(r + 8 * q * ld_residual)
+                                                     : make_uint4(0, 0, 0, 0);
     }
   }
 
@@ -417,12 +426,17 @@ struct Epilogue {
       activate(act, slope, v);
       if (residual) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+        for (uint32_t q = 0; q < 4; ++q)
+          *reinterpret_cast<uint4 *>(mine + staged((g.lane >> 2) + 8 * q, g.lane & 3)) = x[q];
+        __syncwarp();
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {
           float u[8];
-          Vec<T>::unpack(x[q], u);
+          Vec<T>::unpack(*reinterpret_cast<const uint4 *>(mine + staged(g.lane, q)), u);
 #pragma unroll
           for (int i = 0; i < 8; ++i) v[8 * q + i] += u[i];
         }
+        __syncwarp();
       }
     }
     put(out, ld_out, g, c, v, mine);
@@ -501,16 +515,18 @@ struct Epilogue {
   }
 
   // dw is [out_dim][in_dim]: a column of the tile is a run of its row.
-  __device__ __forceinline__ void store_dw(const Strip &g, int32_t c, const uint32_t (&r)[32], uint8_t *mine) const {
+  __device__ __forceinline__ void store_dw(const Strip &g, uint32_t part, int32_t c, const uint32_t (&r)[32],
+                                           uint8_t *mine) const {
     const uint32_t lane = g.lane;
+    const uint64_t at = (uint64_t)g.e * width + g.col + c;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
       for (uint32_t q = 0; q < 16; ++q)
         *reinterpret_cast<uint32_t *>(mine + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4) = r[16 * h + q];
       __syncwarp();
-      T *to = out + ((uint64_t)g.e * width + g.col + c + 16 * h) * ld_out + g.row;
-      if (vec) {  // a lane has half of a row's 32 values
+      T *to = out + (at + 16 * h) * ld_out + g.row;
+      if (vec && !sums) {  // a lane has half of a row's 32 values
         const uint32_t j = lane >> 1, k0 = (lane & 1) * 16;
         float v[16];
 #pragma unroll
@@ -526,6 +542,13 @@ struct Epilogue {
             for (int i = 0; i < 8; ++i) u[i] = v[8 * q + i];
             if ((int32_t)(k0 + 8 * q) < g.high) *reinterpret_cast<uint4 *>(to + j * ld_out + k0 + 8 * q) = Vec<T>::pack(u);
           }
+        }
+      } else if (sums) {
+        float *sum = sums + ((uint64_t)part * experts * width + at + 16 * h) * height + g.row + lane;
+#pragma unroll
+        for (uint32_t q = 0; q < 16; ++q) {
+          const float x = *reinterpret_cast<const float *>(mine + q * 128 + (((lane >> 2) ^ (q & 7)) << 4) + (lane & 3) * 4);
+          if (c + 16 * h + (int32_t)q < g.cols && (int32_t)lane < g.high) sum[(uint64_t)q * height] = x;
         }
       } else {  // rows at odd addresses: a row's 32 values by 32 lanes
 #pragma unroll
@@ -546,9 +569,25 @@ struct Epilogue {
         if (z) z[(g.row + r) * ld_z + g.col + c] = from_f<T>(0.0f);
       }
   }
-  __device__ __forceinline__ void zero_dw(const Strip &g) const {
-    for (int32_t c = 0; c < g.cols; ++c)
-      if ((int32_t)g.lane < g.high) out[((uint64_t)g.e * width + g.col + c) * ld_out + g.row + g.lane] = from_f<T>(0.0f);
+  // Share i of n of an expert's whole (part of the) gradient, thread k of the epilogue's.
+  __device__ __forceinline__ void zero_dw(uint32_t e, uint32_t part, uint32_t i, uint32_t n, uint32_t k) const {
+    if (sums) zero_share(sums + ((uint64_t)part * experts + e) * width * height, i, n, k);
+    else zero_share(out + (uint64_t)e * width * height, i, n, k);
+  }
+  template <typename U>
+  __device__ __forceinline__ void zero_share(U *p, uint32_t i, uint32_t n, uint32_t k) const {
+    constexpr uint32_t kPiece = 16 / sizeof(U);
+    const uint64_t all = (uint64_t)width * height, share = (all + n - 1) / n, from = min(all, share * i),
+                   to = min(all, share * (i + 1));
+    U *const first = p + from, *const last = p + to;
+    // up to the first whole 16 bytes, those, and the rest
+    U *const up = reinterpret_cast<U *>(((uintptr_t)first + 15) & ~(uintptr_t)15), *const whole = up < last ? up : last;
+    const uint64_t pieces = (uint64_t)(last - whole) / kPiece;
+    if (k < (uint32_t)(whole - first)) first[k] = from_f<U>(0.0f);
+    for (uint64_t q = k; q < pieces; q += kEpilogueWarps * 32)
+      reinterpret_cast<uint4 *>(whole)[q] = make_uint4(0, 0, 0, 0);
+    U *const rest = whole + pieces * kPiece;
+    if (k < (uint32_t)(last - rest)) rest[k] = from_f<U>(0.0f);
   }
 };
 
@@ -765,7 +804,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     const uint8_t *x = a.x, *dz = a.dz;
     const uint64_t pitch = a.ld_x * 2, pitch_dz = a.ld_dz * 2;
     const uint32_t *rows = (const uint32_t *)a.rows;
-    const uint32_t x_rows = a.x_rows, depth = a.depth, width = a.width, height = a.height;
+    const uint32_t x_rows = a.x_rows, depth = a.depth, has = a.x_cols, width = a.width, height = a.height;
     uint32_t issued = 0, went = 0;  // went: phase of each stage's go barrier
     bool ok = MODE == kDw || (MODE == kForward && rows);  // else there is nothing to copy
     for (uint64_t t = first_tile; ok && t < tiles.total; t += tile_step) {
@@ -836,7 +875,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
                   copy16(sa + (i & 1 ? to1 : to0) + i * 512, src[i] + (uint64_t)col * 2, (zeros >> i) & 1);
               }
           } else {
-            const uint32_t n = col + piece * 8 < depth ? min(16u, (depth - col - piece * 8) * 2) : 0u;
+            const uint32_t n = col + piece * 8 < has ? min(16u, (has - col - piece * 8) * 2) : 0u;
 #pragma unroll
             for (int i = 0; i < kMany; ++i)
               copy16_part(sa + (i & 1 ? to1 : to0) + i * 512, n ? src[i] + (uint64_t)col * 2 : x, (zeros >> i) & 1 ? 0u : n);
@@ -893,7 +932,8 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       const Strip g{MODE == kDw ? o.e : 0u, (int32_t)o.rows - (int32_t)(quarter * 32), (uint64_t)o.row + quarter * 32,
                     o.col + part, (int32_t)min((uint32_t)BN / 2, ep.width - min(ep.width, o.col + part)), lane};
       if (o.depth == 0) {
-        if (MODE == kDw) ep.zero_dw(g);
+        if (MODE == kDw) ep.zero_dw(o.e, o.part, PAIR ? 2 * o.index + rank : o.index,
+                                    (PAIR ? 2 : 1) * tiles.row_tiles * tiles.cols, w * 32 + lane);
         else ep.zero_rows(g);
         continue;
       }
@@ -907,7 +947,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
           uint32_t r[32];
           tmem_ld32(from + c, r);
           tmem_wait_ld();
-          if constexpr (MODE == kDw) ep.store_dw(g, c, r, mine);
+          if constexpr (MODE == kDw) ep.store_dw(g, o.part, c, r, mine);
           else if (ep.vec) ep.template store_rows<MODE == kForward>(g, o.e, c, r, ahead, mine);
           else ep.template store_odd_rows<MODE == kForward>(g, o.e, c, r, mine);
         }
@@ -965,23 +1005,68 @@ struct Pack {
   const uint16_t *src;
   const int32_t *index;
   uint16_t *dst;
-  uint64_t ld, stride, all_rows;  // all_rows: of all matrices
+  const int32_t *offsets;  // weights: the experts' rows
+  uint64_t ld, stride;
+  uint32_t all_rows;       // of all matrices
   uint32_t cols, rows, pitch, src_rows;
-  uint32_t vec;                   // the source's rows are whole 16-byte pieces
+  uint32_t num_experts, num_rows;
+  uint32_t lanes, turns;   // of a warp that have a row: one for 16 bytes, or all; turns of a warp for all rows
+  uint32_t vec;            // the source's rows are whole 16-byte pieces
 };
 struct Packs {
   Pack job[2];
-  uint64_t total;  // rows of both
+  uint64_t total;  // turns of a warp for both
 };
-// CTA `cta` of `ctas` of 256 threads: a warp per row, four pieces of a lane in flight.
+// The 16 bytes at element `from` of a row of n elements (an aligned address); zeros where
+// the row is not.
+__device__ __forceinline__ uint4 row_piece(const uint16_t *row, int32_t from, int32_t n) {
+  if (from >= 0 && from + 8 <= n) return *reinterpret_cast<const uint4 *>(row + from);
+  uint32_t w[4] = {0, 0, 0, 0};
+  if (from < n && from + 8 > 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (from + i >= 0 && from + i < n) w[i / 2] |= (uint32_t)row[from + i] << (16 * (i & 1));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Eight 16-bit elements from the `by`-th (0..7) of sixteen on, zeros from the n-th of them.
+__device__ __forceinline__ uint4 shifted(const uint4 &a, const uint4 &b, uint32_t by, int32_t n) {
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = by & 4 ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = by & 2 ? w[i + 1] : w[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = by & 1 ? __funnelshift_r(w[i], w[i + 1], 16) : w[i];
+    w[i] = 2 * i + 1 < n ? w[i] : 2 * i < n ? w[i] & 0xFFFFu : 0u;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// CTA `cta` of `ctas` of 256 threads: a warp per row, four pieces of a lane in flight,
+// or for several short rows.  Weights of experts without rows are left out.
 __device__ __forceinline__ void pack_rows(const Packs &p, uint32_t cta, uint32_t ctas) {
-  const uint32_t lane = threadIdx.x & 31;
+  __shared__ uint32_t live[NTC_MAX_EXPERTS / 32];  // bit e: expert e has rows
+  const Pack &w = p.job[0].offsets ? p.job[0] : p.job[1];
+  if (w.offsets) {
+    for (uint32_t e0 = threadIdx.x & ~31u; e0 < w.num_experts; e0 += 256) {
+      const uint32_t e = min(e0 + (threadIdx.x & 31), w.num_experts - 1);
+      const uint32_t bits = __ballot_sync(0xFFFFFFFFu, offset_at(w.offsets, e + 1, (int32_t)w.num_rows) >
+                                                           offset_at(w.offsets, e, (int32_t)w.num_rows));
+      if ((threadIdx.x & 31) == 0) live[e0 / 32] = bits;
+    }
+    __syncthreads();
+  }
   for (uint64_t i = (uint64_t)cta * 8 + threadIdx.x / 32; i < p.total; i += (uint64_t)ctas * 8) {
-    const bool one = i < p.job[0].all_rows;
+    const bool one = i < p.job[0].turns;
     const Pack &k = one ? p.job[0] : p.job[1];
-    const uint64_t row = one ? i : i - p.job[0].all_rows, m = row / k.rows;
-    uint64_t from = row - m * k.rows;
+    const uint32_t lanes = k.lanes, lane = threadIdx.x & (lanes - 1);
+    const uint64_t row = (one ? i : i - p.job[0].turns) * (32 / lanes) + (threadIdx.x & 31) / lanes;
+    if (row >= k.all_rows) continue;
+    const uint32_t m = (uint32_t)row / k.rows;
+    uint64_t from = row - (uint64_t)m * k.rows;
     uint32_t cols = k.cols;
+    if (k.offsets && !((live[m / 32] >> (m % 32)) & 1)) continue;
     if (k.index) {
       const int32_t at = (int32_t)ld_word((const uint32_t *)k.index + row);
       if ((uint32_t)at >= k.src_rows) cols = 0;
@@ -1002,21 +1087,28 @@ __device__ __forceinline__ void pack_rows(const Packs &p, uint32_t cta, uint32_t
           if (c0 + 256 * u < k.pitch) *reinterpret_cast<uint4 *>(to + c0 + 256 * u) = q[u];
       }
     } else {
+      // aligned 16-byte pieces, two for each of the copy's; those at the row's ends have
+      // parts of its neighbours, where it has any
+      const bool edge = row == 0 || row + 1 == k.all_rows || (k.index && (from == 0 || from + 1 == k.src_rows));
+      const uint32_t shift = (uint32_t)((uintptr_t)src & 15) / 2;
       for (uint32_t c0 = lane * 8; c0 < k.pitch; c0 += 1024) {
-        uint16_t v[4][8];
+        uint4 q[4][2];
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u)
 #pragma unroll
-          for (uint32_t q = 0; q < 8; ++q) {
-            v[u][q] = 0;
-            if (c0 + 256 * u + q < cols) v[u][q] = src[c0 + 256 * u + q];
+          for (uint32_t h = 0; h < 2; ++h) {
+            const int32_t from = (int32_t)(c0 + 256 * u + 8 * h) - (int32_t)shift;
+            q[u][h] = make_uint4(0, 0, 0, 0);
+            if (from < (int32_t)cols) {
+              if (!edge) q[u][h] = *reinterpret_cast<const uint4 *>(src + from);
+              else q[u][h] = row_piece(src, from, (int32_t)cols);
+            }
           }
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u)
           if (c0 + 256 * u < k.pitch)
             *reinterpret_cast<uint4 *>(to + c0 + 256 * u) =
-                make_uint4(v[u][0] | (uint32_t)v[u][1] << 16, v[u][2] | (uint32_t)v[u][3] << 16,
-                           v[u][4] | (uint32_t)v[u][5] << 16, v[u][6] | (uint32_t)v[u][7] << 16);
+                shifted(q[u][0], q[u][1], shift, (int32_t)cols - (int32_t)(c0 + 256 * u));
       }
     }
   }
@@ -1026,6 +1118,26 @@ __global__ void __launch_bounds__(256) k_pack(const Packs p) {
   pdl_wait();
   pdl_trigger();
   pack_rows(p, blockIdx.x, gridDim.x);
+}
+
+// dw from the sums of its contraction's parts, in order.
+template <typename T>
+__global__ void __launch_bounds__(256) k_sum(const float *sums, uint32_t parts, uint64_t n, T *dw) {
+  pdl_wait();
+  pdl_trigger();
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) {
+    float v = 0.0f;
+    uint32_t s = 0;
+    for (; s + 8 <= parts; s += 8) {
+      float u[8];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) u[j] = sums[(s + j) * n + i];
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) v += u[j];
+    }
+    for (; s < parts; ++s) v += sums[s * n + i];
+    dw[i] = from_f<T>(v);
+  }
 }
 
 struct DzArgs {
@@ -1332,7 +1444,7 @@ cudaError_t launch_product_of(const Operand &A, const Operand &B, const LinearAr
                                     : row_tiles_bound(a.num_rows, a.num_experts);
   if (high == 0) return cudaSuccess;
   const Shape s = best_shape(MODE, a.num_rows, a.num_experts, a.width, a.height, a.depth, a.rows != nullptr);
-  const uint64_t bound = high * ((a.width + s.cols - 1) / s.cols);
+  const uint64_t bound = high * ((a.width + s.cols - 1) / s.cols) * (MODE == kDw ? a.split : 1);
   const int sms = sm_count();
   if (s.pair) return launch_tile<MODE, 256, T, true>(A, B, a, bound, sms, st);
   if (s.cols == 256) return launch_tile<MODE, 256, T>(A, B, a, bound, sms, st);
@@ -1362,6 +1474,14 @@ bool x_gathers(const ntc_linear_desc &d, const int32_t *rows, bool dw) {
   return d.out_dim >= 2048 && d.num_rows >= 768ull * d.num_experts &&
          best_shape(kForward, d.num_rows, d.num_experts, d.out_dim, 0, d.in_dim, false).pair;
 }
+// Parts of dw's contraction: where its tiles leave SMs idle, each SM gets one, of eight
+// chunks of 64 rows or more; their sums in fp32 are added in order by a second kernel.
+uint32_t dw_split(const ntc_linear_desc &d) {
+  const Shape s = best_shape(kDw, d.num_rows, d.num_experts, d.out_dim, d.in_dim, 0, true);
+  const uint64_t tiles = (uint64_t)d.num_experts * ((d.in_dim + kRows - 1) / kRows) * ((d.out_dim + s.cols - 1) / s.cols);
+  const uint64_t parts = std::min(sm_count() / tiles, d.num_rows / d.num_experts / (8 * kChunk));
+  return parts < 2 || best_shape(kDw, d.num_rows, d.num_experts, d.out_dim, d.in_dim, 0, false).pair ? 1 : (uint32_t)parts;
+}
 bool x_packs(const ntc_linear_desc &d, const void *x) { return !tma_reads(x, d.ld_x); }
 bool w_packs(const ntc_linear_desc &d, const void *w) {
   return !tma_reads(w, d.ld_w) || (d.num_experts > 1 && d.stride_w % 8);
@@ -1376,6 +1496,11 @@ uint64_t w_bytes(const ntc_linear_desc &d) { return round256((uint64_t)d.num_exp
 uint64_t dz_bytes(const ntc_linear_desc &d) { return round256(d.num_rows * round8(d.out_dim) * 2); }
 uint64_t part_bytes(const ntc_linear_desc &d) {
   return round256(row_tiles_bound(d.num_rows, d.num_experts) * round8(d.out_dim) * 4);
+}
+
+uint64_t sum_bytes(const ntc_linear_desc &d) {
+  const uint64_t parts = dw_split(d);
+  return parts > 1 ? round256(parts * d.num_experts * d.out_dim * d.in_dim * 4) : 0;
 }
 
 ntc_status check(const ntc_linear_desc *d) {
@@ -1423,8 +1548,8 @@ ntc_status check_workspace(const void *p, size_t have, size_t need) {
 // The operands x and w, through the workspace where they are copied (a null one is
 // not wanted), and the copies to make; *rows is null afterwards where the copy has x
 // in order.
-Packs operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, bool dw, const void *w, uint8_t *ws, Operand *X,
-               Operand *W) {
+Packs operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, const int32_t *offsets, bool dw, const void *w,
+               uint8_t *ws, Operand *X, Operand *W) {
   const uint32_t pitch = (uint32_t)round8(d.in_dim);
   Packs p{};
   int jobs = 0;
@@ -1438,7 +1563,7 @@ Packs operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, bo
       k.index = gathers ? *rows : nullptr;
       k.dst = (uint16_t *)ws;
       k.ld = d.ld_x;
-      k.all_rows = n;
+      k.all_rows = (uint32_t)n;
       k.cols = d.in_dim;
       k.rows = (uint32_t)n;
       k.pitch = pitch;
@@ -1457,7 +1582,10 @@ Packs operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, bo
       k.dst = (uint16_t *)ws;
       k.ld = d.ld_w;
       k.stride = d.stride_w;
-      k.all_rows = (uint64_t)d.num_experts * d.out_dim;
+      k.all_rows = d.num_experts * d.out_dim;  // at most 2^30
+      k.offsets = offsets;
+      k.num_experts = d.num_experts;
+      k.num_rows = (uint32_t)d.num_rows;
       k.cols = d.in_dim;
       k.rows = d.out_dim;
       k.pitch = pitch;
@@ -1465,7 +1593,11 @@ Packs operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, bo
     }
   }
   for (; jobs < 2; ++jobs) p.job[jobs].rows = 1;  // no rows, but a divisor
-  p.total = p.job[0].all_rows + p.job[1].all_rows;
+  for (Pack &k : p.job) {
+    for (k.lanes = 1; k.lanes < 32 && k.lanes * 8 < k.pitch;) k.lanes *= 2;
+    k.turns = (uint32_t)(((uint64_t)k.all_rows * k.lanes + 31) / 32);
+  }
+  p.total = (uint64_t)p.job[0].turns + p.job[1].turns;
   return p;
 }
 unsigned pack_ctas(const Packs &p) { return (unsigned)std::min<uint64_t>((p.total + 7) / 8, (uint64_t)sm_count() * 32); }
@@ -1522,9 +1654,10 @@ extern "C" NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void
   a.status = status_word();
   if (!a.status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
   Operand X, W;
-  cudaError_t e = launch_packs(operands(d, x, &rows, false, w, (uint8_t *)workspace, &X, &W), st);
+  cudaError_t e = launch_packs(operands(d, x, &rows, offsets, false, w, (uint8_t *)workspace, &X, &W), st);
   a.rows = rows;
   a.x_rows = (uint32_t)X.rows;
+  a.x_cols = X.p == x ? d.in_dim : (uint32_t)round8(d.in_dim);
   if (e == cudaSuccess) e = launch_product<kForward>(X, W, a, st);
   return op_cuda(e, "ntc_linear");
 }
@@ -1533,7 +1666,7 @@ extern "C" NTC_API size_t ntc_linear_backward_workspace(const ntc_linear_desc *d
                                                         const int32_t *rows, const void *w) {
   if (check(desc)) return 0;
   return (dz_writes(*desc, dy) ? dz_bytes(*desc) : 0) + x_bytes(*desc, x, rows, true) +
-         (w_packs(*desc, w) ? w_bytes(*desc) : 0) + part_bytes(*desc);
+         (w_packs(*desc, w) ? w_bytes(*desc) : 0) + part_bytes(*desc) + sum_bytes(*desc);
 }
 
 extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, const void *dy, const void *z,
@@ -1564,6 +1697,8 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
   uint8_t *ws = (uint8_t *)workspace;
   float *part = (float *)ws;
   ws += part_bytes(d);
+  float *sums = (float *)ws;
+  ws += sum_bytes(d);
   const bool writes = dz_writes(d, dy);
   void *dz = nullptr;
   Operand Z{dy, d.out_dim, d.num_rows, d.ld_y};
@@ -1573,7 +1708,13 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
     ws += dz_bytes(d);
   }
   Operand X, W;
-  const Packs packs = operands(d, dw ? x : nullptr, &rows, true, dx ? w : nullptr, ws, &X, &W);
+  const Packs packs = operands(d, dw ? x : nullptr, &rows, offsets, true, dx ? w : nullptr, ws, &X, &W);
+  // Idle warps of dx's product add up db, two of each CTA, unless that is more than
+  // eight strips of 32 columns for each (2 tokens, 101 experts, 3,008 wide, dx and db: 84
+  // us by the 24 warps of its twelve tiles).
+  const uint64_t strips = (uint64_t)d.num_experts * ((d.out_dim + 31) / 32);
+  const bool db_with_dx =
+      db && dx && strips <= 16 * std::min<uint64_t>(row_tiles_bound(d.num_rows, d.num_experts), (uint64_t)sm_count());
   if ((writes && (dx || dw)) || db) {
     DzArgs k{};
     k.packs = packs;
@@ -1598,7 +1739,7 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
     const auto kernel = d.type == NTC_TYPE_BF16 ? (vec ? k_dz<__nv_bfloat16, true> : k_dz<__nv_bfloat16, false>)
                                                 : (vec ? k_dz<__half, true> : k_dz<__half, false>);
     e = launch_pdl(kernel, dim3(cols, k.high + more), kDzThreads, sizeof(TableShared), st, k);
-    if (e == cudaSuccess && db && !dx)  // else idle warps of dx's product sum it
+    if (e == cudaSuccess && db && !db_with_dx)
       e = launch_pdl(k_db, dim3((d.out_dim + 31) / 32, std::min(d.num_experts, 1024u)), kDzThreads, sizeof(TableShared), st,
                      (const float *)part, offsets, d.num_experts, (uint32_t)d.num_rows, d.out_dim, k.pitch, db);
   } else {
@@ -1613,8 +1754,8 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
   a.ld_out = d.in_dim;
   a.status = status;
   if (e == cudaSuccess && dx) {
-    a.part = db ? part : nullptr;
-    a.db = db;
+    a.part = db_with_dx ? part : nullptr;
+    a.db = db_with_dx ? db : nullptr;
     a.part_pitch = (uint32_t)round8(d.out_dim);
     a.out = dx;
     a.depth = d.out_dim;
@@ -1628,7 +1769,15 @@ extern "C" NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, c
     a.width = d.out_dim;
     a.height = d.in_dim;
     a.vec_out = rows_are_vec(dw, d.in_dim, 2);
+    a.split = dw_split(d);
+    a.sums = a.split > 1 ? sums : nullptr;
     e = launch_product<kDw>(X, Z, a, st);
+    if (e == cudaSuccess && a.sums) {
+      const uint64_t n = (uint64_t)d.num_experts * d.out_dim * d.in_dim;
+      const unsigned grid = (unsigned)std::min<uint64_t>((n + 255) / 256, (uint64_t)sm_count() * 8);
+      e = a.bf16 ? launch_pdl(k_sum<__nv_bfloat16>, grid, 256, 0, st, (const float *)sums, a.split, n, (__nv_bfloat16 *)dw)
+                 : launch_pdl(k_sum<__half>, grid, 256, 0, st, (const float *)sums, a.split, n, (__half *)dw);
+    }
   }
   return op_cuda(e, what);
 }

@@ -14,6 +14,7 @@ struct LinearArgs {
   void *out, *z;
   uint64_t ld_out, ld_z, ld_residual;
   uint32_t num_experts, num_rows, x_rows;
+  uint32_t x_cols;     // elements of a row of x that gathers read: those past depth are zeros
   uint32_t width;      // columns of the output
   uint32_t height;     // dw: rows of one expert's (transposed) output
   uint32_t depth;      // contraction length (not dw: there it is the expert's rows)
@@ -26,6 +27,9 @@ struct LinearArgs {
   const float *part;
   float *db;
   uint32_t part_pitch;
+  // dw in `split` parts of the contraction: the parts' sums [split][E][width][height], or NULL for one part
+  float *sums;
+  uint32_t split;
 };
 
 // The normal distribution function Phi(z), and e = exp(-z^2 / 2), which its density

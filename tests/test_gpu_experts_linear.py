@@ -420,3 +420,33 @@ def test_large_products(ntc, counts, K, N, gather):
 @pytest.mark.parametrize("gather", [False, True])
 def test_large_products_of_long_contractions(ntc, counts, K, N, gather):
     test_large_products(ntc, counts, K, N, gather)
+
+
+# rows of each expert, in, out: few tiles of dw and many rows, whose contraction is split; experts with fewer chunks of
+# rows than parts, with one row, with none; and experts without rows at any size of their gradient
+@pytest.mark.parametrize("counts,K,N", [((5000,), 17, 47), ((7446,), 133, 278), ((3000, 1, 0, 65, 4000), 40, 72),
+                                        ((0, 0, 9000), 129, 130), ((12000, 12000), 64, 64)])
+@pytest.mark.parametrize("gather", [False, True])
+def test_dw_of_few_tiles(ntc, counts, K, N, gather):
+    test_large_products(ntc, counts, K, N, gather)
+
+
+@pytest.mark.parametrize("K,N", [(1, 1), (3, 5), (28, 3462), (16, 300), (333, 77), (200, 640)])
+def test_experts_without_rows(ntc, K, N):
+    g = gen(K + N)
+    E, M = 90, 41
+    offsets = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    offsets[8:] = 17
+    offsets[70:] = M
+    x, dy = normal(g, M, K, dtype=torch.float16), normal(g, M, N, dtype=torch.float16)
+    w = normal(g, E, N, K, std=K ** -0.5, dtype=torch.float16)
+    empty = offsets[1:] == offsets[:-1]
+    w[empty] = float("nan")  # not read
+    y = ntc.linear(x, w, offsets=offsets)
+    got = ntc.linear_backward(dy, x, w, offsets=offsets)
+    w[empty] = 0
+    ref, _, bound, _ = R.linear(x, w, None, None, offsets)
+    R.assert_within(y, ref, bound)
+    for name, a, (ref, bound) in zip(("dx", "dw", "db"), got, R.linear_backward(dy, x, w, None, None, offsets, "none")):
+        R.assert_within(a, ref, bound, name)
+    assert not got[1][empty].any() and not got[2][empty].any()
