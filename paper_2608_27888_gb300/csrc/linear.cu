@@ -25,6 +25,12 @@
 // accumulator, one issues the MMAs of both.  That is a third less to copy and to
 // read from shared memory per product, which is what bounds the large products, by
 // bandwidth and by power.
+// Where dw has few tiles, parts of its contraction have a CTA each; the parts' sums are
+// added in order (k_sum; 7,446 rows, 133 -> 278, all gradients: 57 us in one part, 30).
+// What bounds it: 32,768 rows, 2,048 -> 4,096, 16 experts take 283 to 294 us, 1.87 to 1.94
+// PFLOP/s, the board's power; K of 1,024 and less the epilogue (16,384 rows, 1,024 ->
+// 2,048: 42 us, 1.64 PFLOP/s); few rows the weights' bytes (256 rows of 32 experts, 1,024
+// -> 2,048: 30 us, 4.4 TB/s).
 // A weight matrix [N][K] is read as it lies: K-major in the forward product,
 // MN-major (the descriptors' transpose bits) in kDx; kDw takes both operands
 // MN-major.  Nothing is transposed in memory.
@@ -366,8 +372,8 @@ struct Strip {
 // side: a warp's epilogue is bound by the latency of its own instructions, and has to
 // end within the next tile's MMAs (32 x 512 cycles at K = 2,048; the arguments are
 // copies for the same reason).  At short contractions it does not: 16,384 rows, 128 ->
-// 2,048, one expert take 32.8 us, 38.3 with fp32 values staged and 32-byte runs (K =
-// 1,024: 45.9 and 51.8), about 15 without an epilogue.
+// 2,048, one expert take 26 us, about 11 without an epilogue (33 with fp32 values staged
+// and 32-byte runs).
 template <typename T>
 struct Epilogue {
   const float *bias;
