@@ -127,9 +127,9 @@ def test_linear_pointer_refusals():
     assert need > 0 and ntc._lib.ntc_linear_workspace(even, P, P, P) == 0
     assert ntc._lib.ntc_linear_workspace(even, P + 8, P, P) > 0 and ntc._lib.ntc_linear_workspace(even, P, P, P + 2) > 0
     assert ntc._lib.ntc_linear_workspace(d, P + 8, P, P + 2) == 0  # few rows are read where they lie
-    big = made(ntc.ntc_linear_desc, LINEAR, dict(num_rows=65536, out_dim=4096, ld_y=4096, ld_z=4096, ld_residual=4096,
-                                                 stride_w=64 * 4096))
-    assert ntc._lib.ntc_linear_workspace(big, P, P, P) >= 65536 * 64 * 2  # gathered rows in order
+    big = made(ntc.ntc_linear_desc, LINEAR, dict(num_rows=65536, in_dim=2048, ld_x=2048, ld_w=2048, out_dim=4096, ld_y=4096,
+                                                 ld_z=4096, ld_residual=4096, stride_w=2048 * 4096))
+    assert ntc._lib.ntc_linear_workspace(big, P, P, P) >= 65536 * 2048 * 2  # gathered rows in order
     assert ntc._lib.ntc_linear_workspace(big, P, None, P) == 0
     assert f(odd, *good[:8], P, need - 1, None) == BAD
     assert f(odd, *good[:8], None, need, None) == BAD
