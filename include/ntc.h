@@ -498,7 +498,8 @@ NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, 
 /* x[num_x_rows][ld_x], w[E][N][ld_w], bias[E][N] fp32 (contiguous) or NULL,
  * residual[num_rows][ld_residual] or NULL, rows[num_rows] int32 or NULL,
  * offsets[E + 1] int32 (from 0 on, non-decreasing) or NULL; out: y[num_rows][ld_y] and,
- * unless NULL, z[num_rows][ld_z]. */
+ * unless NULL, z[num_rows][ld_z].  An offset outside 0..num_rows counts as the nearer end
+ * and one above a later offset as that one; rows before the first have no result. */
 NTC_API ntc_status ntc_linear(const ntc_linear_desc *desc, const void *x, const int32_t *rows,
                               const int32_t *offsets, const void *w, const float *bias, const void *residual,
                               void *y, void *z, void *workspace, size_t workspace_bytes, void *cuda_stream);

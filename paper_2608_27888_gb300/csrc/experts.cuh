@@ -150,7 +150,10 @@ inline bool rows_are_vec(const void *p, uint64_t ld, size_t elem) {
   return ((uintptr_t)p & 15) == 0 && (ld * elem) % 16 == 0;
 }
 
-// Offset e of the experts' rows, held inside 0..n whatever the memory says.
+// Offset e of the experts' rows, held inside 0..n whatever the memory says.  The linear
+// layers also take an offset that is above a later one as that one: then no two experts
+// share a row, and there are no more row tiles than n rows of E experts can have, which is
+// what workspaces are sized by.
 __device__ __forceinline__ int32_t offset_at(const int32_t *offsets, uint32_t e, int32_t n) {
   return min(max((int32_t)ld_word(reinterpret_cast<const uint32_t *>(offsets) + e), 0), n);
 }

@@ -257,21 +257,28 @@ struct Tile {
   uint32_t index;     // kDw: of the tiles of this expert and part
 };
 
-// Experts' rows and row tiles, from offsets that are only trusted to lie
-// anywhere: they are held inside 0..num_rows, an expert that ends before it begins
-// has no rows.  `high`: rows of a tile.  Called by the whole CTA; ends with a barrier.
+// Experts' rows and row tiles, from offsets that may be anything: off[] lies inside
+// 0..num_rows and does not decrease.  `high`: rows of a tile.  Called by the whole CTA; ends
+// with a barrier.
 __device__ __forceinline__ void make_table(int32_t *off, uint32_t *tile, const int32_t *offsets, uint32_t E, uint32_t num_rows,
                                            uint32_t high = kRows) {
   for (uint32_t e = threadIdx.x; e <= E; e += blockDim.x)
     off[e] = offsets ? offset_at(offsets, e, (int32_t)num_rows) : e ? (int32_t)num_rows : 0;
   if (threadIdx.x == 0) off[E + 1] = (int32_t)num_rows;
   __syncthreads();
+  bool falls = false;
+  for (uint32_t e = threadIdx.x; e <= E; e += blockDim.x) falls |= off[e] > off[e + 1];
+  if (__syncthreads_or(falls)) {
+    if (threadIdx.x == 0)
+      for (uint32_t e = E; e-- > 0;) off[e] = min(off[e], off[e + 1]);
+    __syncthreads();
+  }
   if (threadIdx.x < 32) {
     const uint32_t lane = threadIdx.x;
     uint32_t base = 0;
     for (uint32_t e0 = 0; e0 <= E; e0 += 32) {
       const uint32_t e = e0 + lane;
-      const uint32_t mine = e <= E ? ((uint32_t)max(off[e + 1] - off[e], 0) + high - 1) / high : 0u;
+      const uint32_t mine = e <= E ? ((uint32_t)(off[e + 1] - off[e]) + high - 1) / high : 0u;
       uint32_t in = mine;
 #pragma unroll
       for (int s = 1; s < 32; s <<= 1) {
@@ -330,7 +337,7 @@ struct Tiles {
     const uint32_t high = min(kBandTiles, many - band * kBandTiles);
     const uint32_t row = (band * kBandTiles + in % high) * kHigh;
     o.col = in / high * BN;
-    const uint32_t begin = (uint32_t)s.off[o.e], count = (uint32_t)max(s.off[o.e + 1] - s.off[o.e], 0);
+    const uint32_t begin = (uint32_t)s.off[o.e], count = (uint32_t)(s.off[o.e + 1] - s.off[o.e]);
     o.all_rows = min(kHigh, (MODE == kDw ? height : count) - row);
     o.rows = PAIR ? min(kRows, o.all_rows - min(o.all_rows, shift)) : o.all_rows;
     if constexpr (MODE == kDw) {
@@ -786,10 +793,10 @@ __global__ void __launch_bounds__(threads(MODE), 1)
         const uint32_t e = (uint32_t)(u / strips), col = (uint32_t)(u - (uint64_t)e * strips) * 32 + lane;
         uint32_t from = PAIR ? 0 : s.tile[e];
         if (PAIR) {  // the table counts tiles of 256 rows
-          for (uint32_t i = lane; i < e; i += 32) from += ((uint32_t)max(s.off[i + 1] - s.off[i], 0) + kRows - 1) / kRows;
+          for (uint32_t i = lane; i < e; i += 32) from += ((uint32_t)(s.off[i + 1] - s.off[i]) + kRows - 1) / kRows;
           from = __reduce_add_sync(0xFFFFFFFFu, from);
         }
-        const uint32_t to = from + ((uint32_t)max(s.off[e + 1] - s.off[e], 0) + kRows - 1) / kRows;
+        const uint32_t to = from + ((uint32_t)(s.off[e + 1] - s.off[e]) + kRows - 1) / kRows;
         if (col < width) {
           float v[4] = {};  // every fourth tile: shorter sums, and loads side by side
           for (uint32_t q = from; q < to; q += 4)

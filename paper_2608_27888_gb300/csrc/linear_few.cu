@@ -58,6 +58,13 @@ __device__ __forceinline__ uint4 load_piece(const uint16_t *p, int n) {
   return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
+// The smallest of the offsets from e on: offset e where none is above a later one.
+__device__ __forceinline__ int32_t offset_before(const int32_t *offsets, uint32_t e, uint32_t E, int32_t n) {
+  int32_t least = n;
+  for (; e <= E; ++e) least = min(least, offset_at(offsets, e, n));
+  return least;
+}
+
 // Lane i of a warp: row i / 4 (and 8 more) of W and of x, elements i % 4 * 8 on of
 // every 32.
 // TWO: more than 8 rows in the call, a second MMA for each.
@@ -76,18 +83,26 @@ __global__ void __launch_bounds__(kThreads, 2) k_linear_few(const FewArgs f) {
   if (warp == 0) {
     uint32_t many = 0;
     int32_t end = 0;
-    for (uint32_t e0 = 0; e0 < E; e0 += 32) {
-      const uint32_t e = e0 + lane;
-      int32_t b = 0, n = 0;
-      if (e < E) {
-        b = a.offsets ? offset_at(a.offsets, e, (int32_t)a.num_rows) : 0;
-        end = a.offsets ? offset_at(a.offsets, e + 1, (int32_t)a.num_rows) : (int32_t)a.num_rows;
-        n = max(end - b, 0);
+    bool falls = false;  // an offset is above the next: once more, with offset_before
+    for (bool again = false;; again = true) {
+      for (uint32_t e0 = 0; e0 < E; e0 += 32) {
+        const uint32_t e = e0 + lane;
+        const int32_t rows = (int32_t)a.num_rows;
+        int32_t b = 0, n = 0;
+        if (e < E) {
+          b = !a.offsets ? 0 : again ? offset_before(a.offsets, e, E, rows) : offset_at(a.offsets, e, rows);
+          end = !a.offsets ? rows : again ? offset_before(a.offsets, e + 1, E, rows) : offset_at(a.offsets, e + 1, rows);
+          n = end - b;
+        }
+        falls |= n < 0;
+        const uint32_t has = __ballot_sync(0xFFFFFFFFu, n > 0);
+        const uint32_t at = many + __popc(has & ((1u << lane) - 1));
+        if (n > 0) begin[at] = b, count[at] = n, which[at] = (uint16_t)e;
+        many += __popc(has);
       }
-      const uint32_t has = __ballot_sync(0xFFFFFFFFu, n > 0);
-      const uint32_t at = many + __popc(has & ((1u << lane) - 1));
-      if (n > 0) begin[at] = b, count[at] = n, which[at] = (uint16_t)e;
-      many += __popc(has);
+      if (again || !__any_sync(0xFFFFFFFFu, falls)) break;
+      many = 0;
+      __syncwarp();
     }
     const int32_t last = __shfl_sync(0xFFFFFFFFu, end, (E - 1) & 31);
     if (lane == 0) active = many, live = (uint32_t)last;
