@@ -257,6 +257,36 @@ struct Tile {
   uint32_t index;     // kDw: of the tiles of this expert and part
 };
 
+// The row tiles before each expert, by one warp; whether an offset is above the next.
+__device__ __forceinline__ bool scan_tiles(const int32_t *off, uint32_t *tile, uint32_t E, uint32_t high) {
+  const uint32_t lane = threadIdx.x;
+  uint32_t base = 0;
+  bool falls = false;
+  for (uint32_t e0 = 0; e0 <= E; e0 += 32) {
+    const uint32_t e = e0 + lane;
+    const int32_t rows = e <= E ? off[e + 1] - off[e] : 0;
+    falls |= rows < 0;
+    const uint32_t mine = ((uint32_t)rows + high - 1) / high;
+    uint32_t in = mine;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, in, s);
+      if (lane >= (uint32_t)s) in += o;
+    }
+    if (e <= E) tile[e] = base + in - mine;
+    base += __shfl_sync(0xFFFFFFFFu, in, 31);
+  }
+  if (lane == 0) tile[E + 1] = base;
+  return __any_sync(0xFFFFFFFFu, falls);
+}
+// Holds each offset below those after it.  A call, so that the rest of the kernels does not
+// lie around code that valid offsets never need (64 rows of 32 experts: 31.0 us inlined, 30.5).
+__device__ __noinline__ void hold_offsets(int32_t *off, uint32_t *tile, uint32_t E, uint32_t high) {
+  if (threadIdx.x == 0)
+    for (uint32_t e = E; e-- > 0;) off[e] = min(off[e], off[e + 1]);
+  __syncwarp();
+  scan_tiles(off, tile, E, high);
+}
 // Experts' rows and row tiles, from offsets that may be anything: off[] lies inside
 // 0..num_rows and does not decrease.  `high`: rows of a tile.  Called by the whole CTA; ends
 // with a barrier.
@@ -266,30 +296,7 @@ __device__ __forceinline__ void make_table(int32_t *off, uint32_t *tile, const i
     off[e] = offsets ? offset_at(offsets, e, (int32_t)num_rows) : e ? (int32_t)num_rows : 0;
   if (threadIdx.x == 0) off[E + 1] = (int32_t)num_rows;
   __syncthreads();
-  bool falls = false;
-  for (uint32_t e = threadIdx.x; e <= E; e += blockDim.x) falls |= off[e] > off[e + 1];
-  if (__syncthreads_or(falls)) {
-    if (threadIdx.x == 0)
-      for (uint32_t e = E; e-- > 0;) off[e] = min(off[e], off[e + 1]);
-    __syncthreads();
-  }
-  if (threadIdx.x < 32) {
-    const uint32_t lane = threadIdx.x;
-    uint32_t base = 0;
-    for (uint32_t e0 = 0; e0 <= E; e0 += 32) {
-      const uint32_t e = e0 + lane;
-      const uint32_t mine = e <= E ? ((uint32_t)(off[e + 1] - off[e]) + high - 1) / high : 0u;
-      uint32_t in = mine;
-#pragma unroll
-      for (int s = 1; s < 32; s <<= 1) {
-        const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, in, s);
-        if (lane >= (uint32_t)s) in += o;
-      }
-      if (e <= E) tile[e] = base + in - mine;
-      base += __shfl_sync(0xFFFFFFFFu, in, 31);
-    }
-    if (lane == 0) tile[E + 1] = base;
-  }
+  if (threadIdx.x < 32 && scan_tiles(off, tile, E, high)) hold_offsets(off, tile, E, high);
   __syncthreads();
 }
 

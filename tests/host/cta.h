@@ -17,10 +17,12 @@
 #undef __device__
 #undef __host__
 #undef __forceinline__
+#undef __noinline__
 #undef __shared__
 #define __device__
 #define __host__
 #define __forceinline__ inline
+#define __noinline__
 #define __shared__ static
 
 struct Dim {
@@ -36,7 +38,6 @@ struct Warp {
 };
 static std::unique_ptr<std::barrier<>> whole;
 static std::vector<std::unique_ptr<Warp>> warps;
-static std::vector<uint32_t> votes;
 static Warp &mine() { return *warps[threadIdx.x / 32]; }
 static uint32_t lane() { return threadIdx.x & 31; }
 // Every lane's v, seen by all of the warp's lanes.
@@ -55,7 +56,6 @@ static void run_cta(uint32_t threads, F f) {
   whole = std::make_unique<std::barrier<>>(threads);
   warps.clear();
   for (uint32_t i = 0; i < threads / 32; ++i) warps.push_back(std::make_unique<Warp>());
-  votes.assign(threads, 0);
   std::vector<std::thread> all;
   for (uint32_t t = 0; t < threads; ++t)
     all.emplace_back([=] {
@@ -67,14 +67,7 @@ static void run_cta(uint32_t threads, F f) {
 }  // namespace host
 
 static inline void __syncthreads() { host::whole->arrive_and_wait(); }
-static inline int __syncthreads_or(int v) {
-  host::votes[threadIdx.x] = v != 0;
-  __syncthreads();
-  int any = 0;
-  for (uint32_t x : host::votes) any |= (int)x;
-  __syncthreads();
-  return any;
-}
+static inline void __syncwarp() { host::mine().sync.arrive_and_wait(); }
 static inline uint32_t __shfl_sync(unsigned, uint32_t v, int from) {
   return host::exchange(v, [=](const uint32_t *s) { return s[from & 31]; });
 }
@@ -88,6 +81,7 @@ static inline uint32_t __ballot_sync(unsigned, bool is) {
     return b;
   });
 }
+static inline bool __any_sync(unsigned m, bool is) { return __ballot_sync(m, is) != 0; }
 static inline uint32_t __funnelshift_r(uint32_t lo, uint32_t hi, uint32_t by) {
   return by & 31 ? lo >> (by & 31) | hi << (32 - (by & 31)) : lo;
 }

@@ -13,7 +13,7 @@ CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
 
 
 def function(src, name):
-    return re.search(rf"^(?:__device__ |inline |static )*(?:__forceinline__ )?[\w: ]+\b{name}\([^;]*?\) {{\n.*?^}}", src, re.M | re.S).group(0)
+    return re.search(rf"^(?:__device__ |inline |static )*(?:__forceinline__ |__noinline__ )?[\w: ]+\b{name}\([^;]*?\) {{\n.*?^}}", src, re.M | re.S).group(0)
 
 
 @pytest.fixture(scope="module")
@@ -24,8 +24,8 @@ def experts(tmp_path_factory):
     for f in ("experts.cpp", "cta.h"):
         (d / f).symlink_to(os.path.join(ROOT, "tests", "host", f))
     shared, linear = (open(os.path.join(CSRC, f)).read() for f in ("experts.cuh", "linear.cu"))
-    parts = [function(shared, "offset_at"), "constexpr uint32_t kRows = 128;", function(linear, "make_table"),
-             function(linear, "row_tiles_bound")]
+    parts = [function(shared, "offset_at"), "constexpr uint32_t kRows = 128;", function(linear, "scan_tiles"),
+             function(linear, "hold_offsets"), function(linear, "make_table"), function(linear, "row_tiles_bound")]
     (d / "parts.cuh").write_text("\n".join(parts) + "\n")
     exe = str(d / "experts")
     subprocess.run(["g++", "-O1", "-std=c++20", "-pthread", "-I", os.path.join(CUDA, "include"), "-I", str(d),
