@@ -521,9 +521,9 @@ NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, const void *
                                        void *cuda_stream);
 
 /* Whether a kernel of ntc_linear or ntc_linear_backward gave up one of its
- * bounded waits (200 ms each) on the current device since the last call of
- * this: NTC_ERR_CUDA then (results since are invalid), and the record is
- * cleared.  Synchronises the stream. */
+ * bounded waits (200 ms in which its CTA issued no work) on the current device
+ * since the last call of this: NTC_ERR_CUDA then (results since are invalid), and
+ * the record is cleared.  Synchronises the stream. */
 NTC_API ntc_status ntc_linear_status(void *cuda_stream);
 
 /* The blend: out_t = residual_t + sum_j weights[t][j] * y[place[t][j]] over j <

@@ -68,7 +68,7 @@ constexpr uint32_t stages(int cols) {
 struct Shared {
   uint64_t full[kMaxStages], copied[kMaxStages], peer_copied[kMaxStages], go[kMaxStages], empty[kMaxStages];
   uint64_t acc_full[2], acc_empty[2], drain;
-  uint32_t tmem, quit;
+  uint32_t tmem, quit, chunks;  // chunks: that the TMA warp has gone through
   int32_t off[NTC_MAX_EXPERTS + 2];       // first row of each expert; [E]: of no expert; [E + 1]: the end
   uint32_t tile[NTC_MAX_EXPERTS + 2];     // first row tile of each expert (and of no expert); the total
 };
@@ -218,22 +218,27 @@ constexpr uint32_t kSw128Hi = (1024u >> 4) | (1u << 14) | (2u << 29);
 
 // ------------------------------------------------------------ waits
 
-// A bounded wait.  The first one that gives up sets the status word and the
-// CTA's quit flag, which ends the others'.  The clock is looked at every 64 tries:
-// reading %globaltimer takes about as long as a chunk's MMAs.
+// A bounded wait: it gives up when the CTA has issued no chunk for that long.  (A limit for
+// the wait as a whole would end valid ones: the epilogue and the copies of dw's last chunk
+// wait for a tile's whole contraction, which may be every row of the call.)  The first one
+// that gives up sets the status word and the CTA's quit flag, which ends the others'.  The
+// clock is looked at every 64 tries: reading %globaltimer takes about as long as a chunk's
+// MMAs.
 template <bool PAIR>
 struct Waiter {
-  volatile uint32_t *quit;
+  volatile uint32_t *quit, *chunks;
   unsigned int *status;
   __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const {
     if (try_wait<PAIR>(bar, parity)) return true;
     uint64_t t0 = 0;
+    uint32_t seen = 0;
     for (uint32_t tries = 1;; ++tries) {
       if (try_wait<PAIR>(bar, parity)) return true;
       if (tries % 64) continue;
       if (*quit) return false;
       const uint64_t now = global_ns();
-      if (t0 == 0) t0 = now;
+      const uint32_t many = *chunks;
+      if (t0 == 0 || many != seen) t0 = now, seen = many;
       if (now - t0 > kWaitLimitNs) {
         *quit = 1;
         atomicOr(status, 1u);
@@ -646,7 +651,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       mbar_init(saddr(&s.acc_empty[i]), PAIR ? 2 * kEpilogueWarps : kEpilogueWarps);
     }
     mbar_init(saddr(&s.drain), 1);
-    s.quit = 0;
+    s.quit = s.chunks = 0;
     mbar_init_fence();
   }
   if (warp == 2) tmem_take<PAIR>(saddr(&s.tmem));
@@ -662,8 +667,8 @@ __global__ void __launch_bounds__(threads(MODE), 1)
   const uint32_t tmem = s.tmem;
   // what the other CTA's threads signal is waited for across the pair; that costs
   // the copying warps all of their copies in flight, so nothing else is
-  const Waiter<false> wait{&s.quit, a.status};
-  const Waiter<PAIR> wait_pair{&s.quit, a.status};
+  const Waiter<false> wait{&s.quit, &s.chunks, a.status};
+  const Waiter<PAIR> wait_pair{&s.quit, &s.chunks, a.status};
   const Tiles<MODE, BN, PAIR> tiles(a, s, rank);
 
   if (warp == 0) {
@@ -689,6 +694,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
         const uint32_t sa = uniform(saddr(ring) + st * kStage), sb = sa + kABytes;
         const int32_t k = (int32_t)(c * kChunk);
         if (elect_one()) {
+          *(volatile uint32_t *)&s.chunks = issued + 1;
           constexpr uint32_t kBoth = PAIR ? 2 : 1;
           if constexpr (MODE != kDw) {
             if (rank == 0) expect_tx(saddr(&s.full[st]), all_boxes * 4096 + kBoth * kOwn * 128);

@@ -12,6 +12,10 @@ CSRC = os.path.join(ROOT, "paper_2608_27888_gb300", "csrc")
 CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
 
 
+def template_struct(src, name):
+    return re.search(rf"^template <[^\n]*>\nstruct {name} {{\n.*?^}};", src, re.M | re.S).group(0)
+
+
 def function(src, name):
     return re.search(rf"^(?:__device__ |inline |static )*(?:__forceinline__ |__noinline__ )?[\w: ]+\b{name}\([^;]*?\) {{\n.*?^}}", src, re.M | re.S).group(0)
 
@@ -25,7 +29,8 @@ def experts(tmp_path_factory):
         (d / f).symlink_to(os.path.join(ROOT, "tests", "host", f))
     shared, linear = (open(os.path.join(CSRC, f)).read() for f in ("experts.cuh", "linear.cu"))
     parts = [function(shared, "offset_at"), "constexpr uint32_t kRows = 128;", function(linear, "scan_tiles"),
-             function(linear, "hold_offsets"), function(linear, "make_table"), function(linear, "row_tiles_bound")]
+             function(linear, "hold_offsets"), function(linear, "make_table"), function(linear, "row_tiles_bound"),
+             template_struct(linear, "Waiter")]
     (d / "parts.cuh").write_text("\n".join(parts) + "\n")
     exe = str(d / "experts")
     subprocess.run(["g++", "-O1", "-std=c++20", "-pthread", "-I", os.path.join(CUDA, "include"), "-I", str(d),
@@ -73,3 +78,17 @@ def test_offsets_as_asked_for_are_taken_as_they_are(experts):
         offsets = [0] + sorted(rng.randint(0, n) for _ in range(E))
         off = experts("table", 128, n, *offsets).splitlines()[0]
         assert [int(x) for x in off.split()] == offsets + [n]
+
+
+def test_a_wait_goes_on_while_its_cta_gets_on(experts):
+    """A tile's contraction may take any time; only a CTA that stands still gives up."""
+    opened, status, ms = map(int, experts("wait", 5000, 1).split())
+    assert opened and status == 0 and ms == 5000
+    opened, status, ms = map(int, experts("wait", 5000, 150).split())
+    assert opened and status == 0
+    opened, status, ms = map(int, experts("wait", 150, 0).split())
+    assert opened and status == 0
+    opened, status, ms = map(int, experts("wait", 5000, 0).split())
+    assert not opened and status == 1 and 200 <= ms <= 210
+    opened, status, ms = map(int, experts("wait", 5000, 300).split())
+    assert not opened and status == 1 and 200 <= ms <= 310
