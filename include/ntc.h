@@ -472,7 +472,8 @@ NTC_API ntc_status ntc_expert_order(const int32_t *ids, size_t n, uint32_t top_k
  * Any width, stride and alignment is taken; where TMA cannot read an operand
  * (address not a multiple of 16 bytes, or leading dimension not of 8 elements)
  * the call copies it into the workspace first, and gathered rows of large products,
- * too. */
+ * too.  Nothing outside an operand is read; what lies between its rows may be, and has
+ * no effect. */
 typedef struct {
   ntc_type type;        /* NTC_TYPE_FP16 or NTC_TYPE_BF16: x, w, y, z, residual */
   uint32_t in_dim;      /* K, 1 .. 2^20                                        */

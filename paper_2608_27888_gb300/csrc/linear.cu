@@ -1039,6 +1039,7 @@ struct Pack {
   uint16_t *dst;
   const int32_t *offsets;  // weights: the experts' rows
   uint64_t ld, stride;
+  uint64_t span;           // elements from the first matrix's first to the last one's last
   uint32_t all_rows;       // of all matrices
   uint32_t cols, rows, pitch, src_rows;
   uint32_t num_experts, num_rows;
@@ -1049,10 +1050,11 @@ struct Packs {
   Pack job[2];
   uint64_t total;  // turns of a warp for both
 };
+__device__ __forceinline__ uint4 load16(const uint16_t *p) { return *reinterpret_cast<const uint4 *>(p); }
 // The 16 bytes at element `from` of a row of n elements (an aligned address); zeros where
 // the row is not.
 __device__ __forceinline__ uint4 row_piece(const uint16_t *row, int32_t from, int32_t n) {
-  if (from >= 0 && from + 8 <= n) return *reinterpret_cast<const uint4 *>(row + from);
+  if (from >= 0 && from + 8 <= n) return load16(row + from);
   uint32_t w[4] = {0, 0, 0, 0};
   if (from < n && from + 8 > 0) {
 #pragma unroll
@@ -1112,7 +1114,7 @@ __device__ __forceinline__ void pack_rows(const Packs &p, uint32_t cta, uint32_t
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u) {
           q[u] = make_uint4(0, 0, 0, 0);
-          if (c0 + 256 * u < cols) q[u] = *reinterpret_cast<const uint4 *>(src + c0 + 256 * u);
+          if (c0 + 256 * u < cols) q[u] = load16(src + c0 + 256 * u);
         }
 #pragma unroll
         for (uint32_t u = 0; u < 4; ++u)
@@ -1120,9 +1122,10 @@ __device__ __forceinline__ void pack_rows(const Packs &p, uint32_t cta, uint32_t
       }
     } else {
       // aligned 16-byte pieces, two for each of the copy's; those at the row's ends have
-      // parts of its neighbours, where it has any
-      const bool edge = row == 0 || row + 1 == k.all_rows || (k.index && (from == 0 || from + 1 == k.src_rows));
+      // parts of what lies beside it, unless that is outside the operand
       const uint32_t shift = (uint32_t)((uintptr_t)src & 15) / 2;
+      const uint64_t at = (uint64_t)(src - k.src);
+      const bool edge = at < shift || at - shift + (shift + cols + 7) / 8 * 8 > k.span;
       for (uint32_t c0 = lane * 8; c0 < k.pitch; c0 += 1024) {
         uint4 q[4][2];
 #pragma unroll
@@ -1132,8 +1135,7 @@ __device__ __forceinline__ void pack_rows(const Packs &p, uint32_t cta, uint32_t
             const int32_t from = (int32_t)(c0 + 256 * u + 8 * h) - (int32_t)shift;
             q[u][h] = make_uint4(0, 0, 0, 0);
             if (from < (int32_t)cols) {
-              if (!edge) q[u][h] = *reinterpret_cast<const uint4 *>(src + from);
-              else q[u][h] = row_piece(src, from, (int32_t)cols);
+              q[u][h] = edge ? row_piece(src, from, (int32_t)cols) : load16(src + from);
             }
           }
 #pragma unroll
@@ -1602,6 +1604,7 @@ Packs operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, co
       k.index = gathers ? *rows : nullptr;
       k.dst = (uint16_t *)ws;
       k.ld = d.ld_x;
+      k.span = (d.num_x_rows - 1) * d.ld_x + d.in_dim;
       k.all_rows = (uint32_t)n;
       k.cols = d.in_dim;
       k.rows = (uint32_t)n;
@@ -1621,6 +1624,7 @@ Packs operands(const ntc_linear_desc &d, const void *x, const int32_t **rows, co
       k.dst = (uint16_t *)ws;
       k.ld = d.ld_w;
       k.stride = d.stride_w;
+      k.span = (d.num_experts > 1 ? (d.num_experts - 1) * d.stride_w : 0) + (d.out_dim - 1) * d.ld_w + d.in_dim;
       k.all_rows = d.num_experts * d.out_dim;  // at most 2^30
       k.offsets = offsets;
       k.num_experts = d.num_experts;

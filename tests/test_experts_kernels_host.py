@@ -12,12 +12,12 @@ CSRC = os.path.join(ROOT, "paper_2608_27888_gb300", "csrc")
 CUDA = os.environ.get("CUDA_HOME", "/usr/local/cuda")
 
 
-def template_struct(src, name):
-    return re.search(rf"^template <[^\n]*>\nstruct {name} {{\n.*?^}};", src, re.M | re.S).group(0)
+def struct(src, name):
+    return re.search(rf"^(?:template <[^\n]*>\n)?struct {name} {{\n.*?^}};", src, re.M | re.S).group(0)
 
 
 def function(src, name):
-    return re.search(rf"^(?:__device__ |inline |static )*(?:__forceinline__ |__noinline__ )?[\w: ]+\b{name}\([^;]*?\) {{\n.*?^}}", src, re.M | re.S).group(0)
+    return re.search(rf"^[^\n/#]*\b{name}\([^;{{]*\) {{(?:[^\n]*}}$|\n.*?^}})", src, re.M | re.S).group(0)
 
 
 @pytest.fixture(scope="module")
@@ -28,9 +28,12 @@ def experts(tmp_path_factory):
     for f in ("experts.cpp", "cta.h"):
         (d / f).symlink_to(os.path.join(ROOT, "tests", "host", f))
     shared, linear = (open(os.path.join(CSRC, f)).read() for f in ("experts.cuh", "linear.cu"))
-    parts = [function(shared, "offset_at"), "constexpr uint32_t kRows = 128;", function(linear, "scan_tiles"),
-             function(linear, "hold_offsets"), function(linear, "make_table"), function(linear, "row_tiles_bound"),
-             template_struct(linear, "Waiter")]
+    parts = ["enum Mode { kForward = 0, kDx = 1, kDw = 2 };", "constexpr uint32_t kRows = 128;", function(shared, "offset_at")]
+    parts += [function(linear, f) for f in ("scan_tiles", "hold_offsets", "make_table", "row_tiles_bound")]
+    parts += [struct(linear, s) for s in ("Waiter", "Pack", "Packs", "Shape")]
+    parts += [function(linear, f) for f in ("row_piece", "shifted", "pack_rows", "likely_tiles", "best_shape", "pitch_of",
+                                            "round256", "tma_reads", "x_gathers", "x_packs", "w_packs", "x_bytes", "w_bytes",
+                                            "operands")]
     (d / "parts.cuh").write_text("\n".join(parts) + "\n")
     exe = str(d / "experts")
     subprocess.run(["g++", "-O1", "-std=c++20", "-pthread", "-I", os.path.join(CUDA, "include"), "-I", str(d),
@@ -92,3 +95,17 @@ def test_a_wait_goes_on_while_its_cta_gets_on(experts):
     assert not opened and status == 1 and 200 <= ms <= 210
     opened, status, ms = map(int, experts("wait", 5000, 300).split())
     assert not opened and status == 1 and 200 <= ms <= 310
+
+
+# in_dim, out_dim, experts, rows, rows of x, then leading dimensions, offsets from 16 bytes, strides; with and without an
+# index.  in_dim below 8: more rows than the first and the last reach past the matrix's ends in pieces of 16 bytes.
+@pytest.mark.parametrize("K", [1, 2, 3, 5, 6, 7, 8, 9, 17, 100, 333, 1031])
+@pytest.mark.parametrize("gap,off", [(0, 0), (0, 1), (0, 4), (1, 0), (1, 3), (3, 7), (8, 2)])
+def test_copies_read_nothing_outside_their_operands(experts, K, gap, off):
+    E, N, ld = 3, 5, K + gap
+    for x_rows in (1, 40):
+        out = experts("pack", K, N, E, x_rows, x_rows, ld, off, ld, N * ld + gap, off, 0)
+        assert out.endswith("done\n") and len(out.splitlines()) == 2, out
+    if K == 333:  # copied by an index: rows in any order, some of them none of x's (sizes from which dw's product asks for it)
+        out = experts("pack", K, 1024, 16, 4500, 300, ld, off, ld, 1024 * ld, off, 1)
+        assert out.endswith("copied 1 1\ndone\n") and len(out.splitlines()) == 2, out
