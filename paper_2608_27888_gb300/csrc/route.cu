@@ -441,7 +441,8 @@ __global__ void __launch_bounds__(kWarps * 32)
       // softmax: s / sum is p, so s ds = p (dw - sum dw p); sigmoid: ds as it is
       ds = sum > 0.0f ? (dw - dot / sum) / sum : 0.0f;
     }
-    float v = softmax ? s * ds : s * (1.0f - s) * ds;
+    // 1 - s as the sigmoid of -l: the difference loses its digits where s is near 1
+    float v = softmax ? s * ds : s * quick_sigmoid(-lj) * ds;
     const float dot = dense ? group_sum<G>(v) : 0.0f;
     // a repeated id: its first lane has the sum, in the order of the lanes
     const uint32_t tag = id >= 0 ? (lane / G << 16) | (uint32_t)id : 0xFFFF0000u | lane;

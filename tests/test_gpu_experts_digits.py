@@ -1,0 +1,27 @@
+"""The router's fp32 results to a relative bound, where a formula's plain evaluation loses its digits."""
+import pytest
+import torch
+
+import tests.experts_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ntc():
+    from paper_2608_27888_gb300 import ntc
+    return ntc
+
+
+@pytest.mark.parametrize("k", [2, 9])
+def test_sigmoid_gradient_of_large_logits(ntc, k):
+    """s (1 - s) dw to a relative bound where s is near 1: exp's argument is off by 2^-24 |l|, each of its few
+    operations by 2^-22 at most."""
+    l = torch.linspace(-40, 40, 161)[:, None].repeat(1, 12)
+    ids = torch.arange(k, dtype=torch.int32).repeat(161, 1)
+    dw = torch.randn(161, k, generator=torch.Generator().manual_seed(3))
+    got = ntc.route_backward(l.cuda(), ids.cuda(), dw.cuda(), score="sigmoid", renormalize=False).cpu()
+    d = l.double()[:, :k]
+    want = 1 / (1 + torch.exp(-d)) / (1 + torch.exp(d)) * dw.double()
+    R.assert_within(got[:, :k], want, want.abs() * (2.0 ** -23 * d.abs() * 2 + 2.0 ** -19))
+    assert (got[:, k:] == 0).all()
