@@ -139,6 +139,13 @@ __device__ __forceinline__ float group_sum(float v) {
   for (int s = G / 2; s; s >>= 1) v += __shfl_xor_sync(kAll, v, s);
   return v;
 }
+// In how many of the token's G lanes `is` holds.
+template <int G>
+__device__ __forceinline__ uint32_t group_count(bool is, uint32_t lane) {
+  uint32_t b = __ballot_sync(kAll, is);
+  if constexpr (G < 32) b &= ((1u << G) - 1) << (lane & ~(uint32_t)(G - 1));
+  return __popc(b);
+}
 // The lowest lane of the token's G for which `is` holds (G where none).
 template <int G>
 __device__ __forceinline__ uint32_t group_first(bool is, uint32_t lane) {
@@ -438,8 +445,9 @@ __global__ void __launch_bounds__(kWarps * 32)
     float ds = dw;
     if (d.renormalize) {
       const float sum = group_sum<G>(s), dot = group_sum<G>(dw * s);
-      // softmax: s / sum is p, so s ds = p (dw - sum dw p); sigmoid: ds as it is
-      ds = sum > 0.0f ? (dw - dot / sum) / sum : 0.0f;
+      // softmax: s / sum is p, so s ds = p (dw - sum dw p); sigmoid: ds as it is.  The weight of
+      // a choice that has the sum to itself is constant: 0, not the rounding of dw s / s
+      ds = group_count<G>(s > 0.0f, lane) > 1 ? (dw - dot / sum) / sum : 0.0f;
     }
     // 1 - s as the sigmoid of -l: the difference loses its digits where s is near 1
     float v = softmax ? s * ds : s * quick_sigmoid(-lj) * ds;

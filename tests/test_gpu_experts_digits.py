@@ -25,3 +25,18 @@ def test_sigmoid_gradient_of_large_logits(ntc, k):
     want = 1 / (1 + torch.exp(-d)) / (1 + torch.exp(d)) * dw.double()
     R.assert_within(got[:, :k], want, want.abs() * (2.0 ** -23 * d.abs() * 2 + 2.0 ** -19))
     assert (got[:, k:] == 0).all()
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_one_choice_alone_has_no_gradient(ntc, score):
+    """Renormalized over one chosen expert a weight is the scale whatever the logits are: exact zeros."""
+    g = torch.Generator(device="cuda").manual_seed(4)
+    l = torch.randn(4096, 16, generator=g, device="cuda") * 3
+    ids, _ = ntc.route(l, 1, score=score)
+    dw = torch.randn(4096, 1, generator=g, device="cuda")
+    assert not ntc.route_backward(l, ids, dw, score=score).any()
+    # the only one left of several: the others masked, or none
+    for k in (2, 9):
+        some = torch.cat([torch.full((4096, k - 1), -1, dtype=torch.int32, device="cuda"), ids], 1)
+        dw = torch.randn(4096, k, generator=g, device="cuda")
+        assert not ntc.route_backward(l, some, dw, score=score).any()
