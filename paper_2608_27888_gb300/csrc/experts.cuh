@@ -56,6 +56,15 @@ __device__ __forceinline__ float quick_inverse(float x) {
   return y;
 }
 __device__ __forceinline__ float quick_sigmoid(float x) { return quick_inverse(1.0f + quick_exp(-x)); }
+// The same without the rounding of x log2(e), which costs a result 2^-24 |x|: t ln 2 is
+// subtracted from x again, and exp(x) = 2^t exp(x - t ln 2).  For fp32 results; x is held
+// where neither 2^t nor the difference overflows and 1 / (1 + exp(x)) is 0 at the end.
+__device__ __forceinline__ float fine_exp(float x) {
+  x = fminf(fmaxf(x, -128.0f), 88.7f);
+  const float t = x * 1.44269504f, e = quick_exp2(t);
+  return fmaf(e, fmaf(t, -0.693147182f, x), e);
+}
+__device__ __forceinline__ float fine_sigmoid(float x) { return quick_inverse(1.0f + fine_exp(-x)); }
 
 // ------------------------------------------------------------- element types
 

@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kWarps * 32)
   constexpr int kHeads = V + 1;  // the last one: -inf
   __shared__ float sorted[kSorted ? kWarps * 32 * kHeads : 1];        // [warp][rank][lane]
   __shared__ __align__(16) float values[kSorted ? kWarps * 32 * V : 4];  // [warp][lane][V]
-  __shared__ __align__(16) float score[kWarps * 32 * V];              // [warp][lane][V]
+  __shared__ __align__(16) float kept[kWarps * 32 * V];               // [warp][lane][V], the logits
   const uint32_t lane = threadIdx.x & 31, sub = lane & (G - 1), warp = threadIdx.x / 32;
   const uint32_t e0 = sub * V;
   const int have = max(0, min(V, (int)d.num_experts - (int)e0));
@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kWarps * 32)
   const Grouping gr = grouping<V>(d, sub);
   float *heads = sorted + (kSorted ? warp * 32 * kHeads + lane : 0);
   float *all = values + (kSorted ? warp * 32 * V : 0);
-  float *scores = score + warp * 32 * V;
+  float *logit = kept + warp * 32 * V;
   if (kSorted) heads[V * 32] = -INFINITY;
   pdl_wait();
   pdl_trigger();
@@ -291,7 +291,7 @@ __global__ void __launch_bounds__(kWarps * 32)
   for (uint64_t t0 = (uint64_t)blockIdx.x * kTokens; t0 < n; t0 += (uint64_t)gridDim.x * kTokens) {
     const uint64_t t = t0 + threadIdx.x / G;
     const bool real = t < n;  // the lanes of no token go along with the others
-    float l[V], s[V], c[V];
+    float l[V], s[V], c[V], m = 0.0f, inverse = 1.0f;
     load_run<T, V>(logits + (real ? t : t0) * ld + e0, have, vec, l);
     if (softmax) {
       // a masked logit becomes -inf, whose score is 0 (fmaxf: NaN -> -inf)
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kWarps * 32)
       float top = l[0];
 #pragma unroll
       for (int i = 1; i < V; ++i) top = fmaxf(top, l[i]);
-      const float m = fmaxf(group_max<G>(top), -3.402823466e38f);
+      m = fmaxf(group_max<G>(top), -3.402823466e38f);
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -308,7 +308,7 @@ __global__ void __launch_bounds__(kWarps * 32)
         sum += s[i];
       }
       sum = group_sum<G>(sum);
-      const float inverse = sum > 0.0f ? 1.0f / sum : 0.0f;
+      inverse = sum > 0.0f ? 1.0f / sum : 0.0f;
 #pragma unroll
       for (int i = 0; i < V; ++i) s[i] *= inverse;
     } else {
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(kWarps * 32)
     for (int i = 0; i < V; ++i) c[i] = l[i] > least[i] ? s[i] + b[i] : -INFINITY;
     if (gr.groups > 1) keep_groups<V, G>(c, gr, lane, sub);
     __syncwarp();  // the last token's reads of shared memory
-    put_run<V>(scores + lane * V, s);
+    put_run<V>(logit + lane * V, l);
 
     int32_t id = -1;  // lane j of the token: the j-th choice
     if constexpr (kSorted) {
@@ -379,7 +379,12 @@ __global__ void __launch_bounds__(kWarps * 32)
       }
       __syncwarp();
     }
-    const float sj = id >= 0 ? scores[(lane - sub) * V + id] : 0.0f;
+    // the weights are results in fp32: the chosen ones' scores once more, finely
+    float sj = 0.0f;
+    if (id >= 0) {
+      const float lj = logit[(lane - sub) * V + id];
+      sj = softmax ? fine_exp(lj - m) * inverse : fine_sigmoid(lj);
+    }
     float w = sj;
     if (d.renormalize) {
       const float sum = group_sum<G>(sj);
@@ -435,13 +440,13 @@ __global__ void __launch_bounds__(kWarps * 32)
       float sum = 0.0f;
       for (uint32_t e = sub; e < E; e += G) {
         float v = to_f<T>(l[e]);
-        if (live_logit(v)) sum += quick_exp(v - m);
+        if (live_logit(v)) sum += quick_exp(v - m);  // its large terms are near 0 and need no more
       }
       z = group_sum<G>(sum);
     } else if (softmax) {
       m = value_of(group_max<G>(live ? key_of(lj) : 0u));
     }
-    const float s = !live ? 0.0f : softmax ? quick_exp(lj - m) / z : quick_sigmoid(lj);
+    const float s = !live ? 0.0f : softmax ? fine_exp(lj - m) / z : fine_sigmoid(lj);
     float ds = dw;
     if (d.renormalize) {
       const float sum = group_sum<G>(s), dot = group_sum<G>(dw * s);
@@ -450,7 +455,7 @@ __global__ void __launch_bounds__(kWarps * 32)
       ds = group_count<G>(s > 0.0f, lane) > 1 ? (dw - dot / sum) / sum : 0.0f;
     }
     // 1 - s as the sigmoid of -l: the difference loses its digits where s is near 1
-    float v = softmax ? s * ds : s * quick_sigmoid(-lj) * ds;
+    float v = softmax ? s * ds : s * fine_sigmoid(-lj) * ds;
     const float dot = dense ? group_sum<G>(v) : 0.0f;
     // a repeated id: its first lane has the sum, in the order of the lanes
     const uint32_t tag = id >= 0 ? (lane / G << 16) | (uint32_t)id : 0xFFFF0000u | lane;
@@ -485,7 +490,7 @@ __global__ void __launch_bounds__(kWarps * 32)
 #pragma unroll
           for (int i = 0; i < N; ++i) {
             float x = i < have ? to_f<T>(lj[e + i]) : -INFINITY;
-            f[i] = live_logit(x) ? f[i] - quick_exp(x - mj) / zj * dj : 0.0f;
+            f[i] = live_logit(x) ? f[i] - fine_exp(x - mj) / zj * dj : 0.0f;
           }
         }
         store_vec<T>(out + e, have, vec, f);
