@@ -8,6 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/Exceptions.h>
 
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -21,6 +22,16 @@ using at::Tensor;
 const Tensor &tensor(PyObject *o, const char *name) {
   TORCH_CHECK_TYPE(THPVariable_Check(o), name, " must be a tensor, not ", Py_TYPE(o)->tp_name);
   return THPVariable_Unpack(o);
+}
+
+// A result has no gradient, whatever its inputs ask for: said once, for a model would train on
+// without it.
+void not_recorded(std::initializer_list<PyObject *> inputs) {
+  if (!at::GradMode::is_enabled()) return;
+  for (PyObject *o : inputs)
+    if (THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad())
+      TORCH_WARN_ONCE("autograd does not record route, linear and combine: their results have no gradient. route_backward, "
+                      "linear_backward and combine_backward compute it.");
 }
 
 int64_t integer(PyObject *o, const char *name) {
@@ -130,6 +141,7 @@ bool takes(Py_ssize_t have, Py_ssize_t want) {
 PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   if (!takes(n_args, 8)) return nullptr;
+  not_recorded({a[0]});
   const Tensor &logits = tensor(a[0], "logits");
   on_device(logits, "logits");
   two_dims(logits, "logits");
@@ -231,6 +243,7 @@ ntc_linear_desc linear_desc(const Tensor &x, const Tensor &w, uint32_t activatio
 PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   if (!takes(n_args, 9)) return nullptr;
+  not_recorded({a[0], a[1], a[2], a[7]});
   const Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "w");
   on_device(x, "x");
   int64_t m = x.dim() ? x.size(0) : 0;
@@ -326,6 +339,7 @@ ntc_combine_desc combine_desc(const Tensor &y, const Tensor &place, PyObject *of
 PyObject *combine(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   if (!takes(n_args, 5)) return nullptr;
+  not_recorded({a[0], a[2], a[4]});
   const Tensor &y = tensor(a[0], "y"), &place = tensor(a[1], "place");
   ntc_combine_desc d = combine_desc(y, place, a[3]);
   const int64_t T = place.size(0), k = place.size(1), D = y.size(1);

@@ -8,6 +8,12 @@ call is queued and where those allocations live; tensors of another stream are t
 caller's to order, as for any torch call.  Matrices may have any row stride; their
 last dimension is contiguous.  Wrong tensors and values raise ValueError, what the
 library refuses NtcError.
+
+Autograd does not record these calls: a result has no gradient, and an input that requires
+one draws a warning.  The ``*_backward`` functions compute the gradients.  A call returns
+before its kernels have run; ``ntc.ntc_linear_status`` tells whether one of ``linear`` or
+``linear_backward`` gave up a wait since it was last asked, which makes results invalid
+(a fault of the machine, for valid calls get on).
 """
 from __future__ import annotations
 
