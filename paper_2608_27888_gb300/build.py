@@ -4,7 +4,8 @@ Each .cu file under csrc/ compiles to an object in parallel; the objects link
 into ``_build/libntc.so`` with the CUDA runtime linked statically, so the
 library needs nothing but the driver at run time.  Beside it g++ compiles
 ``_build/_experts.so``, the torch binding of the routed-expert calls
-(csrc/torch/), against the installed torch's headers.
+(csrc/torch/), against the installed torch's headers; without torch it is left out,
+for the library does not need it.
 """
 from __future__ import annotations
 
@@ -47,10 +48,13 @@ def _run(cmd, what):
     return r.stdout + r.stderr
 
 
-def _binding_object() -> str:
+def _binding_object() -> str | None:
     import sysconfig
 
-    import torch
+    try:
+        import torch
+    except ImportError:
+        return None
     t = os.path.join(os.path.dirname(torch.__file__), "include")
     obj = os.path.join(BUILD, f"experts_binding.{torch.__version__}.o")
     if _stale(obj, [BINDING_SOURCE, os.path.join(INCLUDE, "ntc.h")]):
@@ -99,7 +103,8 @@ def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False) 
         tmp = LIB + f".tmp{os.getpid()}"
         _run([nvcc, *ARCH, "-shared", "-cudart", "static", "-Xlinker", "-soname=libntc.so", "-o", tmp, *objs], "link")
         os.replace(tmp, LIB)
-    _link_binding(binding)
+    if binding:
+        _link_binding(binding)
     return LIB
 
 
