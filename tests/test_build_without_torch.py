@@ -10,7 +10,7 @@ sys.modules["torch"] = None
 from paper_2608_27888_gb300 import build
 assert build.build().endswith("libntc.so")
 from paper_2608_27888_gb300 import ntc
-assert ntc.ntc_status_string(0)
+assert ntc._lib.ntc_status_string(0)
 assert ntc.ntc_expert_order_workspace(1 << 20, 64) > 0
 try:
     ntc.route
