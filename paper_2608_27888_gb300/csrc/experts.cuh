@@ -133,17 +133,8 @@ struct Vec {
   }
 };
 
-// n <= N elements at p: one load when `vec` (p on a 16-byte boundary and n = N),
-// else one by one; absent ones are 0.
-template <typename T>
-__device__ __forceinline__ void load_vec(const T *p, int n, bool vec, float (&v)[Vec<T>::N]) {
-  if (vec && n >= Vec<T>::N) {
-    Vec<T>::unpack(*reinterpret_cast<const uint4 *>(p), v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < Vec<T>::N; ++i) v[i] = i < n ? to_f<T>(p[i]) : 0.0f;
-  }
-}
+// n <= N elements to p: one store when `vec` (p on a 16-byte boundary) and n = N, else one
+// by one.
 template <typename T>
 __device__ __forceinline__ void store_vec(T *p, int n, bool vec, const float (&v)[Vec<T>::N]) {
   if (vec && n >= Vec<T>::N) {

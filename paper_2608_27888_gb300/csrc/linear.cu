@@ -670,6 +670,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
   const Waiter<false> wait{&s.quit, &s.chunks, a.status};
   const Waiter<PAIR> wait_pair{&s.quit, &s.chunks, a.status};
   const Tiles<MODE, BN, PAIR> tiles(a, s, rank);
+  const int32_t *const index = PAIR ? nullptr : a.rows;  // best_shape: pairs take no gather
 
   if (warp == 0) {
     uint32_t issued = 0;
@@ -680,7 +681,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       const int32_t row = (int32_t)uniform(o.row), begin = (int32_t)uniform(o.begin);
       const int32_t col = (int32_t)uniform(o.col + rank * kOwn);  // of this CTA's half of the other operand
       // boxes of 32 rows (4: one of 128), of this CTA and of the pair
-      const bool gathers = MODE == kForward && a.rows;
+      const bool gathers = MODE == kForward && index;
       const uint32_t boxes = uniform(gathers ? 0 : (o.rows + 31) / 32);
       const uint32_t all_boxes =
           uniform(gathers ? 0 : (min(o.all_rows, kRows) + 31) / 32 + (o.all_rows - min(o.all_rows, kRows) + 31) / 32);
@@ -711,8 +712,8 @@ __global__ void __launch_bounds__(threads(MODE), 1)
                 tma_3d<PAIR>(sb + j * 8192, &map_b, bar, col + (int32_t)j * 64, k, (int32_t)e);
             }
           } else if ((c + 1) * kChunk <= depth) {
-            if (rank == 0) expect_tx(saddr(&s.full[st]), kBoth * ((a.rows ? 0 : kABytes) + kOwn * 128));
-            if (!a.rows) {
+            if (rank == 0) expect_tx(saddr(&s.full[st]), kBoth * ((index ? 0 : kABytes) + kOwn * 128));
+            if (!index) {
 #pragma unroll
               for (uint32_t j = 0; j < 2; ++j) tma_2d<PAIR>(sa + j * 8192, &map_a, bar, row + (int32_t)j * 64, begin + k);
             }
@@ -721,7 +722,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
               tma_2d<PAIR>(sb + j * 8192, &map_b, bar, col + (int32_t)j * 64, begin + k);
           } else {
             if (rank == 0) mbar_arrive(saddr(&s.full[st]));  // the copying warps bring all of it
-            if (!a.rows) mbar_arrive(saddr(&s.go[st]));
+            if (!index) mbar_arrive(saddr(&s.go[st]));
           }
         }
         __syncwarp();
@@ -771,7 +772,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
       for (uint32_t c = 0; c < chunks; ++c, ++used) {
         const uint32_t st = used % kStages;
         ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.full[st]), (used / kStages) & 1));
-        if (ok && (a.rows || (MODE == kDw && (c + 1) * kChunk > depth))) {
+        if (ok && (index || (MODE == kDw && (c + 1) * kChunk > depth))) {
           ok = __all_sync(0xFFFFFFFFu, wait(saddr(&s.copied[st]), (phases >> st) & 1));
           if (PAIR && ok) ok = __all_sync(0xFFFFFFFFu, wait_pair(saddr(&s.peer_copied[st]), (phases >> st) & 1));
           phases ^= 1u << st;
@@ -834,7 +835,7 @@ __global__ void __launch_bounds__(threads(MODE), 1)
     const uint32_t to0 = (first + sub) * 128 + ((piece ^ sub) << 4), to1 = to0 ^ 64;  // even and odd copies
     const uint8_t *x = a.x, *dz = a.dz;
     const uint64_t pitch = a.ld_x * 2, pitch_dz = a.ld_dz * 2;
-    const uint32_t *rows = (const uint32_t *)a.rows;
+    const uint32_t *rows = (const uint32_t *)index;
     const uint32_t x_rows = a.x_rows, depth = a.depth, has = a.x_cols, width = a.width, height = a.height;
     uint32_t issued = 0, went = 0;  // went: phase of each stage's go barrier
     bool ok = MODE == kDw || (MODE == kForward && rows);  // else there is nothing to copy
