@@ -412,6 +412,9 @@ __global__ void __launch_bounds__(kWarps * 32)
   extern __shared__ __align__(16) float rows[];
   constexpr int N = Vec<T>::N;
   constexpr uint32_t kTokens = 32 / G;  // of a warp at a time
+  // rows' pieces in flight: more of them cost registers, and so CTAs (32,768 tokens of 256 experts, fp32: 11.0 us
+  // by two, 8.8 by four; 65,536 of 64, bf16: 9.1 and 9.9)
+  constexpr int kTurns = sizeof(T) == 4 ? 4 : 2;
   const uint32_t lane = threadIdx.x & 31, sub = lane & (G - 1), E = d.num_experts, pitch = (E + 7) / 8 * 8, k = d.top_k;
   float *all = rows + threadIdx.x / 32 * kTokens * pitch, *row = all + lane / G * pitch;
   const bool softmax = d.score == NTC_SCORE_SOFTMAX, dense = softmax && !d.renormalize;
@@ -472,30 +475,38 @@ __global__ void __launch_bounds__(kWarps * 32)
     __syncwarp();
     if (id >= 0 && first && live) row[id] = v;
     __syncwarp();
+    // the rows leave; with_rest: all live logits have a gradient, in 16 bits without fine_exp's digits
+    const auto leave = [&](auto with_rest) {
 #pragma unroll
-    for (uint32_t j = 0; j < kTokens; ++j) {
-      if (t0 + j >= n) break;
-      const float mj = __shfl_sync(kAll, m, j * G), zj = __shfl_sync(kAll, z, j * G), dj = __shfl_sync(kAll, dot, j * G);
-      const T *lj = logits + (t0 + j) * ld;
-      T *out = dlogits + (t0 + j) * E;
-      for (uint32_t e = lane * N; e < E; e += 32 * N) {
-        float f[N];
-        const int have = min((int)(E - e), N);
+      for (uint32_t j = 0; j < kTokens; ++j) {
+        if (t0 + j >= n) break;
+        const float mj = __shfl_sync(kAll, m, j * G), dj = with_rest.value ? __shfl_sync(kAll, dot / z, j * G) : 0.0f;
+        const T *lj = logits + (t0 + j) * ld;
+        T *out = dlogits + (t0 + j) * E;
+#pragma unroll kTurns
+        for (uint32_t e = lane * N; e < E; e += 32 * N) {
+          float f[N];
+          const int have = min((int)(E - e), N);
 #pragma unroll
-        for (int i = 0; i < N; i += 4) {
-          const float4 q = *reinterpret_cast<const float4 *>(all + j * pitch + e + i);  // pitch: a multiple of 8
-          f[i] = q.x, f[i + 1] = q.y, f[i + 2] = q.z, f[i + 3] = q.w;
-        }
-        if (dense) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            float x = i < have ? to_f<T>(lj[e + i]) : -INFINITY;
-            f[i] = live_logit(x) ? f[i] - fine_exp(x - mj) / zj * dj : 0.0f;
+          for (int i = 0; i < N; i += 4) {
+            const float4 q = *reinterpret_cast<const float4 *>(all + j * pitch + e + i);  // pitch: a multiple of 8
+            f[i] = q.x, f[i + 1] = q.y, f[i + 2] = q.z, f[i + 3] = q.w;
           }
+          if constexpr (with_rest.value) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+              float x = i < have ? to_f<T>(lj[e + i]) : -INFINITY;
+              const bool is = live_logit(x);
+              const float s = sizeof(T) == 4 ? fine_exp(x - mj) : quick_exp(x - mj);
+              f[i] = is ? f[i] - s * dj : 0.0f;
+            }
+          }
+          store_vec<T>(out + e, have, vec, f);
         }
-        store_vec<T>(out + e, have, vec, f);
       }
-    }
+    };
+    if (dense) leave(std::true_type{});
+    else leave(std::false_type{});
     __syncwarp();
   }
 }
