@@ -5,6 +5,9 @@
 with the experts and their weights from a linear router.  ``forward`` keeps what
 ``backward`` needs when asked to; ``backward`` returns every gradient.  Every product,
 routing, ordering and blending step is one library call; torch holds the tensors.
+Every result between the calls is rounded to the layer's type, the router's logits among
+them; gradients are computed by ``backward``, not by autograd.  After a step
+``ntc.ntc_linear_status`` says whether a kernel gave up a wait, which makes results invalid.
 """
 from __future__ import annotations
 
