@@ -15,8 +15,8 @@
 //     choices at once: lane j searches choice j's value;
 //   - a token of few experts has 8 or 16 lanes, so that a warp's instructions serve
 //     two or four tokens.
-// 32,768 tokens, 256 experts, top 8 of 4 of 8 groups, sigmoid and bias, bf16: 26 us
-// (issue slots 68 % busy), 50.6 with a search of all registers per choice.
+// 32,768 tokens, 256 experts, top 8 of 4 of 8 groups, sigmoid and bias, bf16: 25 us
+// (issue slots 67 % busy), 50.6 with a search of all registers per choice.
 #include "experts.cuh"
 
 using namespace ntc;
