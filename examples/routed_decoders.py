@@ -3,7 +3,8 @@
 The teacher is the framework's own decode: a G-buffer's queries, each through the
 decoder of its texture set.  The student sees the same latent features and no set id:
 a layer of routed experts learns which expert decodes what.  After the training steps
-the student decodes a batch through a CUDA graph, as a renderer would replay it.
+the student decodes a batch through a CUDA graph, as a renderer would replay it, with its
+weights in 16 bits and in 4.
 
     python examples/routed_decoders.py [--steps 200] [--experts 8] [--top-k 2]
 """
@@ -16,6 +17,7 @@ import torch
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 from paper_2608_27888_gb300 import ntc, workloads as W  # noqa: E402
+from paper_2608_27888_gb300.optim import AdamW  # noqa: E402
 from paper_2608_27888_gb300.routed import RoutedExperts  # noqa: E402
 
 
@@ -29,26 +31,19 @@ def teacher(name="gbuffer-1080p"):
     return x.to(torch.bfloat16), y
 
 
-def train(steps=200, experts=8, top_k=2, hidden=128, batch=8192, rate=0.02, seed=0, log=print):
+def train(steps=200, experts=8, top_k=2, hidden=128, batch=8192, rate=0.02, seed=0, log=print, bits=32, balance=1e-4):
     """The trained layer and the mean squared error before and after."""
     g = torch.Generator(device="cuda").manual_seed(seed)
     x, target = teacher()
     layer = RoutedExperts(x.shape[1], hidden, target.shape[1], experts, top_k, generator=g)
-    master = {n: getattr(layer, n).float() for n in layer.NAMES}  # fp32 copies that the steps add up in
-    moment = {n: (torch.zeros_like(p), torch.zeros_like(p)) for n, p in master.items()}
+    adam = AdamW(layer.parameters(), lr=rate, beta2=0.99, weight_decay=0.0, bits=bits)
     errors = []
     for step in range(1, steps + 1):
         at = torch.randint(0, x.shape[0], (batch,), generator=g, device="cuda")
         out, kept = layer.forward(x[at], keep=True)
         diff = out.float() - target[at]
-        grads, _ = layer.backward((diff * (2.0 / diff.numel())).to(out.dtype), kept)
-        for n, p in master.items():  # Adam
-            m, v = moment[n]
-            d = grads[n].float()
-            m.mul_(0.9).add_(d, alpha=0.1)
-            v.mul_(0.99).addcmul_(d, d, value=0.01)
-            p.sub_(rate * (m / (1 - 0.9 ** step)) / ((v / (1 - 0.99 ** step)).sqrt() + 1e-8))
-            getattr(layer, n).copy_(p)
+        grads, _ = layer.backward((diff * (2.0 / diff.numel())).to(out.dtype), kept, balance)
+        adam.step(grads)
         layer.balance(kept[6])
         errors.append(diff.square().mean())
         if log and step % 50 == 1:
@@ -62,23 +57,25 @@ def main():
     ap.add_argument("--steps", type=int, default=200)
     ap.add_argument("--experts", type=int, default=8)
     ap.add_argument("--top-k", type=int, default=2)
+    ap.add_argument("--bits", type=int, default=32, choices=(8, 32), help="of the optimizer's moments")
     a = ap.parse_args()
-    layer, first, last, x, target = train(a.steps, a.experts, a.top_k)
+    layer, first, last, x, target = train(a.steps, a.experts, a.top_k, bits=a.bits)
     print(f"mean squared error {first:.5f} -> {last:.5f} after {a.steps} steps")
 
     batch = x[:4096].clone()
-    layer.forward(batch)  # first use of every kernel, outside the capture
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
-        out = layer.forward(batch)
-    start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
-    start.record()
-    for _ in range(100):
-        graph.replay()
-    end.record()
-    torch.cuda.synchronize()
-    print(f"{batch.shape[0]} texels decoded in {start.elapsed_time(end) * 10:.1f} us a pass, "
-          f"error {float((out.float() - target[:4096]).square().mean()):.5f}")
+    for name, served in (("16", layer), ("4", layer.pack4(group=32))):
+        served.forward(batch)  # first use of every kernel, outside the capture
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = served.forward(batch)
+        start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        start.record()
+        for _ in range(100):
+            graph.replay()
+        end.record()
+        torch.cuda.synchronize()
+        print(f"weights in {name} bits: {batch.shape[0]} texels decoded in {start.elapsed_time(end) * 10:.1f} us a pass, "
+              f"error {float((out.float() - target[:4096]).square().mean()):.5f}")
 
 
 if __name__ == "__main__":

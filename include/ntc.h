@@ -560,6 +560,126 @@ NTC_API ntc_status ntc_combine_backward(const ntc_combine_desc *desc, const void
                                         const int32_t *place, const float *weights, const int32_t *offsets,
                                         void *dy, float *dweights, void *cuda_stream);
 
+/* The loss that spreads tokens over the experts.  With p_t = softmax(l_t), or
+ * sigmoid(l_t) divided by its sum, over the live logits (as ntc_route's: -inf and
+ * NaN are masked and have p = 0), c_e = how many entries of ids are expert e, C =
+ * the sum of the c_e, and n' = how many tokens have an id in 0..num_experts-1 (the
+ * others are padding and count nowhere):
+ *   mean_e = (1 / n') sum over those tokens of p_te
+ *   loss   = scale * num_experts * sum_e (c_e / C) mean_e
+ * which is scale where the load is even.  With n' = 0 all of it is 0.  Sums are
+ * fp32 in a fixed order: equal calls give equal bits. */
+typedef struct {
+  uint32_t num_experts; /* 1 .. NTC_MAX_EXPERTS                    */
+  uint32_t top_k;       /* ids of a token, 1 .. NTC_MAX_TOP_K      */
+  uint32_t score;       /* NTC_SCORE_SOFTMAX or NTC_SCORE_SIGMOID  */
+  float scale;          /* finite                                  */
+  ntc_type type;        /* of the logits and of their gradient     */
+} ntc_balance_desc;
+
+/* logits[n][ld_logits >= num_experts], ids[n][top_k] int32; n * top_k < 2^31.
+ * out: loss[1] fp32, counts[num_experts + 1] int32 (the c_e, and after them n'),
+ * mean[num_experts] fp32.  workspace: ntc_balance_loss_workspace bytes (16-byte
+ * aligned; may be NULL when that is 0). */
+NTC_API size_t ntc_balance_loss_workspace(const ntc_balance_desc *desc, size_t n);
+NTC_API ntc_status ntc_balance_loss(const ntc_balance_desc *desc, size_t n, const void *logits, size_t ld_logits,
+                                    const int32_t *ids, float *loss, int32_t *counts, float *mean,
+                                    void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* The gradient of the logits, dlogits[n][num_experts] (contiguous, desc->type),
+ * with counts as ntc_balance_loss wrote them (the counts themselves have no
+ * gradient): with a = dloss * scale * num_experts / (n' C), a counted token has
+ *   softmax: dl_te = a p_te (c_e - sum_i c_i p_ti)
+ *   sigmoid: the same times sigmoid(-l_te)
+ * and masked logits, and all of a token that does not count, have 0.  dloss[1]
+ * fp32 or NULL (1); residual[n][ld_residual] of desc->type or NULL: added before
+ * the one rounding, as the router's own gradient. */
+NTC_API ntc_status ntc_balance_loss_backward(const ntc_balance_desc *desc, size_t n, const void *logits,
+                                             size_t ld_logits, const int32_t *ids, const int32_t *counts,
+                                             const float *dloss, const void *residual, size_t ld_residual,
+                                             void *dlogits, void *cuda_stream);
+
+/* One AdamW step of many tensors in one call.  With g' = grad_scale * g and t = step:
+ *   m <- beta1 m + (1 - beta1) g'         v <- beta2 v + (1 - beta2) g'^2
+ *   p <- (1 - lr weight_decay) p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, p rounded once to its type; copy, where there is one, receives the new
+ * p rounded to its own type (the 16-bit weights of fp32 masters).
+ * moment_bits 32: m and v are fp32.  moment_bits 8: m and v hold e4m3 codes of m
+ * and of sqrt(v), in blocks of NTC_ADAMW_BLOCK consecutive elements with an fp32
+ * scale each, scale_m[i / NTC_ADAMW_BLOCK] and scale_v[...]: value = code * scale,
+ * scale = (largest magnitude of the block) / 448, rounded to nearest; a root that is
+ * not 0 keeps a code that is not 0, so that no division loses its denominator.  The
+ * step itself uses the moments before they are rounded.  A moment that changes by
+ * less than half of a code's distance (up to 1/16 of its value) keeps its code; what
+ * the block's largest does is exact, and the others move with it.  A block whose
+ * largest is below 2^-100 is 0; one with an infinity or a NaN reads back as NaN. */
+#define NTC_ADAMW_BLOCK 256u
+typedef struct {
+  void *param;             /* count elements of param_type                        */
+  const void *grad;        /* of grad_type                                        */
+  void *m, *v;             /* fp32, or e4m3 codes                                 */
+  float *scale_m, *scale_v; /* ceil(count / NTC_ADAMW_BLOCK) each; 8 bits only    */
+  void *copy;              /* of copy_type, or NULL                               */
+  uint64_t count;          /* below 2^40                                          */
+  ntc_type param_type, grad_type, copy_type;
+} ntc_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay, grad_scale; /* finite; 0 <= beta < 1; eps, weight_decay >= 0 */
+  uint64_t step;        /* t: 1 at the first step                                  */
+  uint32_t moment_bits; /* 32 or 8                                                 */
+} ntc_adamw_desc;
+
+/* h_tensors: HOST array of num_tensors (at most 2^20) entries, copied by the
+ * call.  No buffer that is written may overlap another buffer of the call.  d_lr,
+ * d_grad_scale (fp32[1]) and d_step (int32[1]; below 1 counts as 1) replace desc's
+ * values unless NULL and are read on the device, so that a captured call can be
+ * replayed with new ones; workspace: NTC_ADAMW_WORKSPACE bytes (16-byte aligned)
+ * where one of them is given, else it may be NULL.  Kernels per call: one for every
+ * 400 tensors, and one more with a workspace. */
+#define NTC_ADAMW_WORKSPACE 16u
+NTC_API ntc_status ntc_adamw(const ntc_adamw_desc *desc, const ntc_adamw_tensor *h_tensors, size_t num_tensors,
+                             const float *d_lr, const int32_t *d_step, const float *d_grad_scale,
+                             void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* Weights in 4 bits: w[e][n][k] ~ scale[e][n][k / group] * q[e][n][k], q = -8..7.
+ * packed[e][n] has ceil(in_dim / 2) bytes, q + 8 of an even k in the low half of byte
+ * k / 2 and of an odd k in the high half; scales[e][n] has ceil(in_dim / group)
+ * values of `type`.  Any strides and alignment are taken; rows of packed that start
+ * on 16 bytes are read fastest. */
+typedef struct {
+  ntc_type type;          /* NTC_TYPE_FP16 or NTC_TYPE_BF16: the scales            */
+  uint32_t in_dim;        /* K, 1 .. 2^20                                          */
+  uint32_t out_dim;       /* N, 1 .. 2^20                                          */
+  uint32_t num_experts;   /* 1 .. NTC_MAX_EXPERTS                                  */
+  uint32_t group;         /* 32, 64 or 128                                         */
+  uint64_t ld_packed;     /* bytes from row to row, >= ceil(in_dim / 2)            */
+  uint64_t stride_packed; /* bytes from expert to expert                           */
+  uint64_t ld_scales;     /* elements, >= ceil(in_dim / group)                     */
+  uint64_t stride_scales;
+} ntc_pack4_desc;
+
+/* scale = max |w| of the group / 7, rounded to `type`; q = w / scale rounded to
+ * nearest even and held in -8..7 (0 where the scale is 0).  A group with an infinity
+ * or a NaN has the scale NaN.  Where in_dim is odd the last half byte is q = 0.
+ * w[E][N][ld_w] of w_type, stride_w elements from expert to expert. */
+NTC_API ntc_status ntc_pack4(const ntc_pack4_desc *desc, const void *w, ntc_type w_type, uint64_t ld_w,
+                             uint64_t stride_w, uint8_t *packed, void *scales, void *cuda_stream);
+/* The reverse: w[E][N][ld_w] of desc->type, scale * q rounded once. */
+NTC_API ntc_status ntc_unpack4(const ntc_pack4_desc *desc, const uint8_t *packed, const void *scales, void *w,
+                               uint64_t ld_w, uint64_t stride_w, void *cuda_stream);
+
+/* ntc_linear (without z) with weights in 4 bits.  desc's ld_w, stride_w and ld_z are
+ * not read; its type, in_dim, out_dim and num_experts are those of `weights`.  Calls
+ * of few rows per expert (up to 32 on average) multiply the numbers q themselves, exact in 16 bits, and
+ * the groups' fp32 sums by their scales; larger ones unpack the weights of experts
+ * that have rows into the workspace, rounded to 16 bits, and take ntc_linear's product. */
+NTC_API size_t ntc_linear4_workspace(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, const void *x,
+                                     const int32_t *rows);
+NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, const void *x,
+                               const int32_t *rows, const int32_t *offsets, const uint8_t *packed,
+                               const void *scales, const float *bias, const void *residual, void *y,
+                               void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 /* Human-readable message of the last failed call on this host thread (no
  * paper counterpart). */
 NTC_API const char *ntc_last_error(void);

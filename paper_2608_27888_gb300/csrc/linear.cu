@@ -1580,13 +1580,6 @@ ntc_status check_rows(const ntc_linear_desc &d, const int32_t *rows, const int32
   return NTC_OK;
 }
 
-ntc_status check_workspace(const void *p, size_t have, size_t need) {
-  if (have < need || (need && !p))
-    return op_fail(NTC_ERR_INVALID_ARG, "the workspace has %zu bytes, %zu are needed", have, need);
-  if (need && ((uintptr_t)p & 15)) return op_fail(NTC_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
-  return NTC_OK;
-}
-
 // The operands x and w, through the workspace where they are copied (a null one is
 // not wanted), and the copies to make; *rows is null afterwards where the copy has x
 // in order.
@@ -1650,6 +1643,21 @@ cudaError_t launch_packs(const Packs &p, cudaStream_t st) {
 }
 
 }  // namespace
+
+namespace ntc {
+
+ntc_status check_linear(const ntc_linear_desc *d) { return check(d); }
+ntc_status check_linear_rows(const ntc_linear_desc &d, const int32_t *rows, const int32_t *offsets) {
+  return check_rows(d, rows, offsets);
+}
+ntc_status check_workspace(const void *p, size_t have, size_t need) {
+  if (have < need || (need && !p))
+    return op_fail(NTC_ERR_INVALID_ARG, "the workspace has %zu bytes, %zu are needed", have, need);
+  if (need && ((uintptr_t)p & 15)) return op_fail(NTC_ERR_INVALID_ARG, "workspace is not 16-byte aligned");
+  return NTC_OK;
+}
+
+}  // namespace ntc
 
 extern "C" NTC_API size_t ntc_linear_workspace(const ntc_linear_desc *desc, const void *x, const int32_t *rows,
                                                const void *w) {

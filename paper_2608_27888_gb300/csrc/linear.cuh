@@ -70,6 +70,63 @@ __device__ __forceinline__ void activate(uint32_t act, float slope, float (&v)[N
   }
 }
 
+// c += a b: 16 x 16 rows of A times 16 x 8 columns of B, fp16 or bf16.
+template <typename T>
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (std::is_same<T, __half>::value)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The smallest of the offsets from e on: offset e where none is above a later one.
+__device__ __forceinline__ int32_t offset_before(const int32_t *offsets, uint32_t e, uint32_t E, int32_t n) {
+  int32_t least = n;
+  for (; e <= E; ++e) least = min(least, offset_at(offsets, e, n));
+  return least;
+}
+
+// A warp lists the experts that have rows (first row, rows, number) in shared memory:
+// *active of them, and *live rows of any.
+__device__ __forceinline__ void list_experts(const LinearArgs &a, uint32_t lane, int32_t *begin, int32_t *count, uint16_t *which,
+                                             uint32_t *active, uint32_t *live) {
+  const uint32_t E = a.num_experts;
+  uint32_t many = 0;
+  int32_t end = 0;
+  bool falls = false;  // an offset is above the next: once more, with offset_before
+  for (bool again = false;; again = true) {
+    for (uint32_t e0 = 0; e0 < E; e0 += 32) {
+      const uint32_t e = e0 + lane;
+      const int32_t rows = (int32_t)a.num_rows;
+      int32_t b = 0, n = 0;
+      if (e < E) {
+        b = !a.offsets ? 0 : again ? offset_before(a.offsets, e, E, rows) : offset_at(a.offsets, e, rows);
+        end = !a.offsets ? rows : again ? offset_before(a.offsets, e + 1, E, rows) : offset_at(a.offsets, e + 1, rows);
+        n = end - b;
+      }
+      falls |= n < 0;
+      const uint32_t has = __ballot_sync(0xFFFFFFFFu, n > 0);
+      const uint32_t at = many + __popc(has & ((1u << lane) - 1));
+      if (n > 0) begin[at] = b, count[at] = n, which[at] = (uint16_t)e;
+      many += __popc(has);
+    }
+    if (again || !__any_sync(0xFFFFFFFFu, falls)) break;
+    many = 0;
+    __syncwarp();
+  }
+  const int32_t last = __shfl_sync(0xFFFFFFFFu, end, (E - 1) & 31);
+  if (lane == 0) *active = many, *live = (uint32_t)last;
+}
+
+// What the linear layers' calls refuse: the descriptor, its rows and offsets, a workspace.
+ntc_status check_linear(const ntc_linear_desc *d);
+ntc_status check_linear_rows(const ntc_linear_desc &d, const int32_t *rows, const int32_t *offsets);
+ntc_status check_workspace(const void *p, size_t have, size_t need);
+
 // y = act(x w^T + b) + residual for few rows per expert (linear_few.cu), and when it
 // takes the call.
 bool few_rows(uint64_t num_rows);

@@ -34,18 +34,6 @@ struct FewArgs {
   uint32_t split;  // warps along K: 1, 2, 4 or 8
 };
 
-template <typename T>
-__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  if constexpr (std::is_same<T, __half>::value)
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  else
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
 // Eight elements from p on, n of them inside (the others 0): 16 bytes at once when
 // VEC (then n is 0 or 8, unless K ends inside: n = 8 at most).
 template <bool VEC>
@@ -56,13 +44,6 @@ __device__ __forceinline__ uint4 load_piece(const uint16_t *p, int n) {
   for (int i = 0; i < 4; ++i)
     v[i] = (2 * i < n ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
   return make_uint4(v[0], v[1], v[2], v[3]);
-}
-
-// The smallest of the offsets from e on: offset e where none is above a later one.
-__device__ __forceinline__ int32_t offset_before(const int32_t *offsets, uint32_t e, uint32_t E, int32_t n) {
-  int32_t least = n;
-  for (; e <= E; ++e) least = min(least, offset_at(offsets, e, n));
-  return least;
 }
 
 // Lane i of a warp: row i / 4 (and 8 more) of W and of x, elements i % 4 * 8 on of
@@ -80,33 +61,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_linear_few(const FewArgs f) {
   const uint32_t E = a.num_experts, K = a.depth, N = a.width, split = f.split;
   pdl_wait();
   pdl_trigger();
-  if (warp == 0) {
-    uint32_t many = 0;
-    int32_t end = 0;
-    bool falls = false;  // an offset is above the next: once more, with offset_before
-    for (bool again = false;; again = true) {
-      for (uint32_t e0 = 0; e0 < E; e0 += 32) {
-        const uint32_t e = e0 + lane;
-        const int32_t rows = (int32_t)a.num_rows;
-        int32_t b = 0, n = 0;
-        if (e < E) {
-          b = !a.offsets ? 0 : again ? offset_before(a.offsets, e, E, rows) : offset_at(a.offsets, e, rows);
-          end = !a.offsets ? rows : again ? offset_before(a.offsets, e + 1, E, rows) : offset_at(a.offsets, e + 1, rows);
-          n = end - b;
-        }
-        falls |= n < 0;
-        const uint32_t has = __ballot_sync(0xFFFFFFFFu, n > 0);
-        const uint32_t at = many + __popc(has & ((1u << lane) - 1));
-        if (n > 0) begin[at] = b, count[at] = n, which[at] = (uint16_t)e;
-        many += __popc(has);
-      }
-      if (again || !__any_sync(0xFFFFFFFFu, falls)) break;
-      many = 0;
-      __syncwarp();
-    }
-    const int32_t last = __shfl_sync(0xFFFFFFFFu, end, (E - 1) & 31);
-    if (lane == 0) active = many, live = (uint32_t)last;
-  }
+  if (warp == 0) list_experts(a, lane, begin, count, which, &active, &live);
   __syncthreads();
 
   const uint32_t blocks = kWarps / split;  // of 16 rows of W in a CTA

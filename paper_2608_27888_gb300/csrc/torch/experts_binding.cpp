@@ -6,12 +6,17 @@
 // defaults), checks its tensors, allocates its outputs and workspace with torch on
 // the current stream and makes the one library call of its name.
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_strided.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+
+#include <memory>
+#include <vector>
 
 #include "ntc.h"
 
@@ -31,7 +36,7 @@ void not_recorded(std::initializer_list<PyObject *> inputs) {
   for (PyObject *o : inputs)
     if (THPVariable_Check(o) && THPVariable_Unpack(o).requires_grad())
       TORCH_WARN_ONCE("autograd does not record route, linear and combine: their results have no gradient. route_backward, "
-                      "linear_backward and combine_backward compute it.");
+                      "linear_backward and combine_backward compute it. Nor does it record balance_loss, linear4, pack4 and unpack4.");
 }
 
 int64_t integer(PyObject *o, const char *name) {
@@ -379,9 +384,346 @@ PyObject *combine_backward(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+ntc_balance_desc balance_desc(const Tensor &logits, const Tensor &ids, PyObject *score, PyObject *scale) {
+  on_device(logits, "logits");
+  two_dims(logits, "logits");
+  two_dims(ids, "ids");
+  ntc_balance_desc d;
+  d.num_experts = (uint32_t)std::min<int64_t>(logits.size(1), 0xFFFFFFFFll);
+  d.top_k = (uint32_t)std::min<int64_t>(ids.size(1), 0xFFFFFFFFll);
+  d.score = small(score, "score");
+  d.scale = real(scale, "scale");
+  d.type = type_of(logits, "logits");
+  return d;
+}
+
+// logits, ids, score, scale -> loss, counts, mean
+PyObject *balance_loss(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!takes(n_args, 4)) return nullptr;
+  not_recorded({a[0]});
+  const Tensor &logits = tensor(a[0], "logits"), &ids = tensor(a[1], "ids");
+  const ntc_balance_desc d = balance_desc(logits, ids, a[2], a[3]);
+  const int64_t n = logits.size(0), E = logits.size(1);
+  const uint64_t ld = matrix(logits, "logits", n, E, logits.scalar_type(), logits);
+  const int32_t *i = array<int32_t>(a[1], "ids", {n, ids.size(1)}, at::kInt, logits);
+  Tensor loss = fresh({}, at::kFloat, logits), counts = fresh({E + 1}, at::kInt, logits), mean = fresh({E}, at::kFloat, logits);
+  const size_t size = ntc_balance_loss_workspace(&d, (size_t)n);
+  Tensor ws = size ? fresh({(int64_t)size}, at::kByte, logits) : Tensor();
+  if (!done(ntc_balance_loss(&d, (size_t)n, logits.data_ptr(), ld, i, (float *)loss.data_ptr(), (int32_t *)counts.data_ptr(),
+                             (float *)mean.data_ptr(), size ? ws.data_ptr() : nullptr, size, stream_of(logits))))
+    return nullptr;
+  return tuple({wrap(loss), wrap(counts), wrap(mean)});
+  END_HANDLE_TH_ERRORS
+}
+
+// The address of a tensor of one element; None is null.
+template <typename T>
+const T *scalar(PyObject *o, const char *name, at::ScalarType dtype, const Tensor &on) {
+  if (o == Py_None) return nullptr;
+  const Tensor &t = tensor(o, name);
+  like(t, name, dtype, on);
+  TORCH_CHECK_VALUE(t.numel() == 1, name, " must have one element, not ", t.numel());
+  return (const T *)t.data_ptr();
+}
+
+// logits, ids, counts, dloss, residual, score, scale -> dlogits
+PyObject *balance_loss_backward(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!takes(n_args, 7)) return nullptr;
+  const Tensor &logits = tensor(a[0], "logits"), &ids = tensor(a[1], "ids");
+  const ntc_balance_desc d = balance_desc(logits, ids, a[5], a[6]);
+  const int64_t n = logits.size(0), E = logits.size(1);
+  const uint64_t ld = matrix(logits, "logits", n, E, logits.scalar_type(), logits);
+  const int32_t *i = array<int32_t>(a[1], "ids", {n, ids.size(1)}, at::kInt, logits);
+  TORCH_CHECK_TYPE(a[2] != Py_None, "counts must be a tensor, not None");
+  const int32_t *c = array<int32_t>(a[2], "counts", {E + 1}, at::kInt, logits);
+  const float *g = scalar<float>(a[3], "dloss", at::kFloat, logits);
+  const void *residual = nullptr;
+  uint64_t ld_residual = (uint64_t)E;
+  if (a[4] != Py_None) {
+    const Tensor &r = tensor(a[4], "residual");
+    ld_residual = matrix(r, "residual", n, E, logits.scalar_type(), logits);
+    residual = r.data_ptr();
+  }
+  Tensor out = fresh({n, E}, logits.scalar_type(), logits);
+  if (!done(ntc_balance_loss_backward(&d, (size_t)n, logits.data_ptr(), ld, i, c, g, residual, ld_residual, out.data_ptr(),
+                                      stream_of(logits))))
+    return nullptr;
+  return wrap(out);
+  END_HANDLE_TH_ERRORS
+}
+
+// The tensors of a sequence; an entry may be None where `optional`.
+struct Tensors {
+  PyObject *fast;
+  const char *name;
+  Tensors(PyObject *o, const char *n) : fast(PySequence_Fast(o, "")), name(n) {
+    if (!fast) {
+      PyErr_Clear();
+      TORCH_CHECK_TYPE(false, name, " must be a sequence of tensors");
+    }
+  }
+  Tensors(const Tensors &) = delete;
+  ~Tensors() { Py_DECREF(fast); }
+  Py_ssize_t size() const { return PySequence_Fast_GET_SIZE(fast); }
+  bool none(Py_ssize_t i) const { return PySequence_Fast_GET_ITEM(fast, i) == Py_None; }
+  const Tensor &at(Py_ssize_t i) const { return tensor(PySequence_Fast_GET_ITEM(fast, i), name); }
+  void as_many(Py_ssize_t n) const {
+    TORCH_CHECK_VALUE(size() == n, name, " must have an entry for each parameter: ", n, ", not ", size());
+  }
+};
+void same(const Tensor &t, const char *name, Py_ssize_t i, const Tensor &p) {
+  TORCH_CHECK_VALUE(t.device() == p.device(), name, "[", i, "] is on ", t.device(), ", its parameter on ", p.device());
+  TORCH_CHECK_VALUE(t.sizes() == p.sizes(), name, "[", i, "] must have shape ", p.sizes(), ", not ", t.sizes());
+  TORCH_CHECK_VALUE(t.is_contiguous(), name, "[", i, "] must be contiguous");
+}
+void changed(const Tensor &t) {  // as an operation in place
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
+// params, grads, m, v, scales, copies, step, lr, beta1, beta2, eps, weight_decay, grad_scale -> None
+PyObject *adamw(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!takes(n_args, 13)) return nullptr;
+  const Tensors params(a[0], "params"), grads(a[1], "grads"), m(a[2], "m"), v(a[3], "v");
+  const Py_ssize_t n = params.size();
+  grads.as_many(n);
+  m.as_many(n);
+  v.as_many(n);
+  std::unique_ptr<Tensors> scales, copies;
+  if (a[4] != Py_None) scales.reset(new Tensors(a[4], "scales")), scales->as_many(n);
+  if (a[5] != Py_None) copies.reset(new Tensors(a[5], "copies")), copies->as_many(n);
+  ntc_adamw_desc d;
+  const auto number = [](PyObject *o, const char *name) {
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) {
+      PyErr_Clear();
+      TORCH_CHECK_TYPE(false, name, " must be a number");
+    }
+    return x;
+  };
+  const bool t_step = THPVariable_Check(a[6]), t_lr = THPVariable_Check(a[7]), t_scale = THPVariable_Check(a[12]);
+  int64_t step = 1;
+  if (!t_step) step = integer(a[6], "step");
+  TORCH_CHECK_VALUE(step >= 1, "step must be at least 1, not ", step);
+  d.step = (uint64_t)step;
+  d.lr = t_lr ? 0.0 : number(a[7], "lr");
+  d.beta1 = number(a[8], "beta1");
+  d.beta2 = number(a[9], "beta2");
+  d.eps = number(a[10], "eps");
+  d.weight_decay = number(a[11], "weight_decay");
+  d.grad_scale = t_scale ? 1.0 : number(a[12], "grad_scale");
+  if (n == 0) Py_RETURN_NONE;
+  const bool eight = m.at(0).scalar_type() == at::kFloat8_e4m3fn;
+  TORCH_CHECK_VALUE(eight == (bool)scales, eight ? "moments in float8_e4m3fn need scales" : "scales are for moments in float8_e4m3fn");
+  d.moment_bits = eight ? 8 : 32;
+  const at::ScalarType moments = eight ? at::kFloat8_e4m3fn : at::kFloat;
+  const Tensor &first = params.at(0);
+  on_device(first, "params[0]");
+  std::vector<ntc_adamw_tensor> t((size_t)n);
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    const Tensor &p = params.at(i), &g = grads.at(i), &mi = m.at(i), &vi = v.at(i);
+    same(p, "params", i, p);
+    TORCH_CHECK_VALUE(p.device() == first.device(), "params[", i, "] is on ", p.device(), ", params[0] on ", first.device());
+    same(g, "grads", i, p);
+    same(mi, "m", i, p);
+    same(vi, "v", i, p);
+    TORCH_CHECK_VALUE(mi.scalar_type() == moments && vi.scalar_type() == moments, "m[", i, "] and v[", i, "] must be ", moments,
+                      " like m[0], not ", mi.scalar_type(), " and ", vi.scalar_type());
+    ntc_adamw_tensor &x = t[(size_t)i];
+    x.param = p.data_ptr();
+    x.grad = g.data_ptr();
+    x.m = mi.data_ptr();
+    x.v = vi.data_ptr();
+    x.scale_m = x.scale_v = nullptr;
+    x.copy = nullptr;
+    x.count = (uint64_t)p.numel();
+    x.param_type = type_of(p, "a parameter");
+    x.grad_type = type_of(g, "a gradient");
+    x.copy_type = NTC_TYPE_FP32;
+    if (eight) {
+      const Tensor &s = scales->at(i);
+      const int64_t blocks = (p.numel() + NTC_ADAMW_BLOCK - 1) / NTC_ADAMW_BLOCK;
+      TORCH_CHECK_VALUE(s.scalar_type() == at::kFloat && s.device() == p.device() && s.dim() == 2 && s.size(0) == 2 && s.size(1) == blocks &&
+                            (blocks <= 1 || s.stride(1) == 1),
+                        "scales[", i, "] must be Float of shape [2, ", blocks, "] on ", p.device(), ", contiguous along the last dimension");
+      x.scale_m = (float *)s.data_ptr();
+      x.scale_v = x.scale_m + s.stride(0);
+    }
+    if (copies && !copies->none(i)) {
+      const Tensor &c = copies->at(i);
+      same(c, "copies", i, p);
+      x.copy = c.data_ptr();
+      x.copy_type = type_of(c, "a copy");
+    }
+  }
+  const float *lr = t_lr ? scalar<float>(a[7], "lr", at::kFloat, first) : nullptr;
+  const int32_t *count = t_step ? scalar<int32_t>(a[6], "step", at::kInt, first) : nullptr;
+  const float *scale = t_scale ? scalar<float>(a[12], "grad_scale", at::kFloat, first) : nullptr;
+  const bool device = lr || count || scale;
+  Tensor ws = device ? fresh({(int64_t)NTC_ADAMW_WORKSPACE}, at::kByte, first) : Tensor();
+  if (!done(ntc_adamw(&d, t.data(), (size_t)n, lr, count, scale, device ? ws.data_ptr() : nullptr, device ? NTC_ADAMW_WORKSPACE : 0,
+                      stream_of(first))))
+    return nullptr;
+  for (Py_ssize_t i = 0; i < n; ++i) {
+    changed(params.at(i));
+    changed(m.at(i));
+    changed(v.at(i));
+    if (eight) changed(scales->at(i));
+    if (t[(size_t)i].copy) changed(copies->at(i));
+  }
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// The strides of an array [E, N, cols] or [N, cols], in elements.
+void rows_of(const Tensor &t, const char *name, int64_t E, int64_t N, int64_t cols, at::ScalarType dtype, const Tensor &on, uint64_t &ld,
+             uint64_t &stride) {
+  like(t, name, dtype, on);
+  const int64_t dims = t.dim();
+  TORCH_CHECK_VALUE((dims == 3 || (dims == 2 && E == 1)) && (dims == 2 || t.size(0) == E) && t.size(dims - 2) == N && t.size(dims - 1) == cols,
+                    name, " must have shape [", E, ", ", N, ", ", cols, "], not ", t.sizes());
+  TORCH_CHECK_VALUE(cols <= 1 || t.stride(dims - 1) == 1, name, " must be contiguous along its last dimension");
+  ld = (uint64_t)(N > 1 ? t.stride(dims - 2) : cols);
+  stride = E > 1 ? (uint64_t)t.stride(0) : ld * (uint64_t)N;
+}
+int64_t groups_of(int64_t K, uint32_t group) {
+  TORCH_CHECK_VALUE(group == 32 || group == 64 || group == 128, "group must be 32, 64 or 128, not ", group);
+  return (K + group - 1) / group;
+}
+// The descriptor of packed weights and their scales.
+ntc_pack4_desc pack4_desc(const Tensor &packed, const Tensor &scales, int64_t K, uint32_t group) {
+  const int64_t dims = packed.dim();
+  TORCH_CHECK_VALUE(dims == 2 || dims == 3, "packed must have two or three dimensions, not ", dims);
+  TORCH_CHECK_VALUE(K >= 1 && K <= 0xFFFFFFFFll, "d_in is out of range: ", K);
+  const int64_t E = dims == 3 ? packed.size(0) : 1, N = packed.size(dims - 2);
+  TORCH_CHECK_VALUE(E <= 0xFFFFFFFFll && N <= 0xFFFFFFFFll, "packed is too large");
+  ntc_pack4_desc d;
+  d.type = type_of(scales, "scales");
+  d.in_dim = (uint32_t)K;
+  d.out_dim = (uint32_t)N;
+  d.num_experts = (uint32_t)E;
+  d.group = group;
+  rows_of(packed, "packed", E, N, (K + 1) / 2, at::kByte, packed, d.ld_packed, d.stride_packed);
+  rows_of(scales, "scales", E, N, groups_of(K, group), scales.scalar_type(), packed, d.ld_scales, d.stride_scales);
+  return d;
+}
+
+// w, group, dtype -> packed, scales
+PyObject *pack4(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!takes(n_args, 3)) return nullptr;
+  not_recorded({a[0]});
+  const Tensor &w = tensor(a[0], "w");
+  on_device(w, "w");
+  const int64_t dims = w.dim();
+  TORCH_CHECK_VALUE(dims == 2 || dims == 3, "w must have two or three dimensions, not ", dims);
+  const int64_t E = dims == 3 ? w.size(0) : 1, N = w.size(dims - 2), K = w.size(dims - 1);
+  const uint32_t group = small(a[1], "group");
+  const ntc_type w_type = type_of(w, "w");
+  at::ScalarType dtype = w_type == NTC_TYPE_FP32 ? at::kBFloat16 : w.scalar_type();
+  if (a[2] != Py_None) {
+    TORCH_CHECK_TYPE(THPDtype_Check(a[2]), "dtype must be a torch.dtype");
+    dtype = ((THPDtype *)a[2])->scalar_type;
+  }
+  TORCH_CHECK_VALUE(dtype == at::kHalf || dtype == at::kBFloat16, "dtype must be float16 or bfloat16, not ", dtype);
+  TORCH_CHECK_VALUE(E >= 1 && N >= 1 && K >= 1 && E <= 0xFFFFFFFFll && N <= 0xFFFFFFFFll && K <= 0xFFFFFFFFll, "w has shape ", w.sizes());
+  uint64_t ld, stride;
+  rows_of(w, "w", E, N, K, w.scalar_type(), w, ld, stride);
+  const int64_t G = groups_of(K, group), bytes = (K + 1) / 2, pitch = (bytes + 15) / 16 * 16;
+  std::vector<int64_t> shape = {N, bytes}, strides = {pitch, 1}, s_shape = {N, G};
+  if (dims == 3) {
+    shape.insert(shape.begin(), E);
+    strides.insert(strides.begin(), N * pitch);
+    s_shape.insert(s_shape.begin(), E);
+  }
+  Tensor packed = at::empty_strided(shape, strides, at::TensorOptions().dtype(at::kByte).device(w.device()));
+  Tensor scales = fresh(s_shape, dtype, w);
+  const ntc_pack4_desc d = pack4_desc(packed, scales, K, group);
+  if (!done(ntc_pack4(&d, w.data_ptr(), w_type, ld, stride, (uint8_t *)packed.data_ptr(), scales.data_ptr(), stream_of(w)))) return nullptr;
+  return tuple({wrap(packed), wrap(scales)});
+  END_HANDLE_TH_ERRORS
+}
+
+// packed, scales, d_in, group -> w
+PyObject *unpack4(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!takes(n_args, 4)) return nullptr;
+  not_recorded({a[1]});
+  const Tensor &packed = tensor(a[0], "packed"), &scales = tensor(a[1], "scales");
+  on_device(packed, "packed");
+  const int64_t K = integer(a[2], "d_in");
+  const ntc_pack4_desc d = pack4_desc(packed, scales, K, small(a[3], "group"));
+  std::vector<int64_t> shape = packed.sizes().vec();
+  shape.back() = K;
+  Tensor w = fresh(shape, scales.scalar_type(), packed);
+  if (!done(ntc_unpack4(&d, (const uint8_t *)packed.data_ptr(), scales.data_ptr(), w.data_ptr(), (uint64_t)K,
+                        (uint64_t)K * d.out_dim, stream_of(packed))))
+    return nullptr;
+  return wrap(w);
+  END_HANDLE_TH_ERRORS
+}
+
+// x, packed, scales, bias, group, rows, offsets, activation, leaky_slope, residual -> y
+PyObject *linear4(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (!takes(n_args, 10)) return nullptr;
+  not_recorded({a[0], a[2], a[3], a[9]});
+  const Tensor &x = tensor(a[0], "x"), &packed = tensor(a[1], "packed"), &scales = tensor(a[2], "scales");
+  on_device(x, "x");
+  two_dims(x, "x");
+  const int64_t K = x.size(1);
+  like(packed, "packed", at::kByte, x);
+  like(scales, "scales", x.scalar_type(), x);
+  const ntc_pack4_desc p = pack4_desc(packed, scales, K, small(a[4], "group"));
+  const int64_t E = p.num_experts, N = p.out_dim;
+  int64_t m = x.size(0);
+  if (a[5] != Py_None) {
+    const Tensor &r = tensor(a[5], "rows");
+    TORCH_CHECK_VALUE(r.dim() == 1, "rows must have one dimension, not ", r.dim());
+    m = r.size(0);
+  }
+  ntc_linear_desc d;
+  d.type = type_of(x, "x");
+  d.in_dim = p.in_dim;
+  d.out_dim = p.out_dim;
+  d.num_experts = p.num_experts;
+  d.activation = small(a[7], "activation");
+  d.leaky_slope = real(a[8], "leaky_slope");
+  d.num_rows = (uint64_t)m;
+  d.num_x_rows = (uint64_t)x.size(0);
+  d.ld_x = matrix(x, "x", x.size(0), K, x.scalar_type(), x);
+  d.ld_w = d.stride_w = 0;
+  d.ld_y = d.ld_z = d.ld_residual = (uint64_t)N;
+  const int32_t *rows = array<int32_t>(a[5], "rows", {m}, at::kInt, x);
+  const int32_t *offsets = array<int32_t>(a[6], "offsets", {E + 1}, at::kInt, x);
+  const float *bias = nullptr;
+  if (a[3] != Py_None) {
+    if (E == 1 && tensor(a[3], "bias").dim() == 1) bias = array<float>(a[3], "bias", {N}, at::kFloat, x);
+    else bias = array<float>(a[3], "bias", {E, N}, at::kFloat, x);
+  }
+  const void *residual = nullptr;
+  if (a[9] != Py_None) {
+    const Tensor &r = tensor(a[9], "residual");
+    d.ld_residual = matrix(r, "residual", m, N, x.scalar_type(), x);
+    residual = r.data_ptr();
+  }
+  Tensor y = fresh({m, N}, x.scalar_type(), x);
+  const size_t size = ntc_linear4_workspace(&d, &p, x.data_ptr(), rows);
+  Tensor ws = size ? fresh({(int64_t)size}, at::kByte, x) : Tensor();
+  if (!done(ntc_linear4(&d, &p, x.data_ptr(), rows, offsets, (const uint8_t *)packed.data_ptr(), scales.data_ptr(), bias, residual,
+                        y.data_ptr(), size ? ws.data_ptr() : nullptr, size, stream_of(x))))
+    return nullptr;
+  return wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
 #define ENTRY(f) {#f, (PyCFunction)(void (*)(void))f, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(route),           ENTRY(route_backward), ENTRY(expert_order),     ENTRY(linear),
-                         ENTRY(linear_backward), ENTRY(combine),        ENTRY(combine_backward), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(linear_backward), ENTRY(combine),        ENTRY(combine_backward), ENTRY(balance_loss),
+                         ENTRY(balance_loss_backward), ENTRY(adamw),    ENTRY(pack4),            ENTRY(unpack4),
+                         ENTRY(linear4),         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_experts", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

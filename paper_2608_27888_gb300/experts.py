@@ -113,3 +113,74 @@ def combine_backward(dout, y, place, weights=None, offsets=None, *, need=("dy", 
             return combine_backward(dout, y, place, weights, offsets, need=need)
     _needs(need, ("dy", "dweights"))
     return _c.combine_backward(dout, y, place, weights, offsets, "dy" in need, "dweights" in need)
+
+
+def balance_loss(logits, ids, *, score: str = "softmax", scale: float = 1.0, stream=None):
+    """(loss, counts, mean) of a batch's logits [n, experts] and choices ids [n, top_k]: see ntc_balance_loss.
+
+    loss is scale * experts * sum(counts / sum(counts) * mean) over the experts, with mean [experts] the mean
+    probabilities of the tokens that have an expert; counts int32 [experts + 1] has the experts' entries and, last, the
+    number of those tokens.  balance_loss_backward takes counts."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return balance_loss(logits, ids, score=score, scale=scale)
+    return _c.balance_loss(logits, ids, _choice(_SCORES, score, "score"), scale)
+
+
+def balance_loss_backward(logits, ids, counts, *, dloss=None, residual=None, score: str = "softmax", scale: float = 1.0,
+                          stream=None):
+    """The gradient of balance_loss's logits, plus residual (such as route_backward's): see ntc_balance_loss_backward.
+
+    dloss: the loss' own gradient, an fp32 tensor of one element (default: 1)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return balance_loss_backward(logits, ids, counts, dloss=dloss, residual=residual, score=score, scale=scale)
+    return _c.balance_loss_backward(logits, ids, counts, dloss, residual, _choice(_SCORES, score, "score"), scale)
+
+
+def adamw(params, grads, m, v, *, step, lr, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+          weight_decay: float = 0.01, grad_scale=1.0, scales=None, copies=None, stream=None):
+    """One AdamW step of a list of tensors, in place: see ntc_adamw.
+
+    params and grads in fp32, fp16 or bf16, each tensor in its own; m and v fp32, or float8_e4m3fn with scales: fp32
+    [2, ceil(numel / 256)] for each tensor.  All start at zero.  copies: None, or a list with None or a tensor for each
+    parameter, which receives the parameter in its own type.  step counts from 1.  step (int32), lr and grad_scale
+    (fp32) may be CUDA tensors of one element: a call captured in a graph reads them at every replay.  optim.AdamW keeps
+    the moments and counts the steps."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return adamw(params, grads, m, v, step=step, lr=lr, beta1=beta1, beta2=beta2, eps=eps,
+                         weight_decay=weight_decay, grad_scale=grad_scale, scales=scales, copies=copies)
+    return _c.adamw(params, grads, m, v, scales, copies, step, lr, beta1, beta2, eps, weight_decay, grad_scale)
+
+
+def pack4(w, *, group: int = 128, dtype=None, stream=None):
+    """(packed, scales) of weights [E, N, K] (or [N, K]) in 4 bits with a scale for every `group` along K: see ntc_pack4.
+
+    packed uint8 [E, N, ceil(K / 2)], its rows starting on 16 bytes; scales [E, N, ceil(K / group)] of `dtype` (float16
+    or bfloat16; default: w's, bfloat16 for float32)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return pack4(w, group=group, dtype=dtype)
+    return _c.pack4(w, group, dtype)
+
+
+def unpack4(packed, scales, d_in: int, *, group: int = 128, stream=None):
+    """The weights [E, N, d_in] (or [N, d_in]) of packed and scales, in the scales' type: see ntc_unpack4."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return unpack4(packed, scales, d_in, group=group)
+    return _c.unpack4(packed, scales, d_in, group)
+
+
+def linear4(x, packed, scales, bias=None, *, group: int = 128, rows=None, offsets=None, activation: str = "none",
+            leaky_slope: float = 0.01, residual=None, stream=None):
+    """linear with weights in 4 bits, as pack4 makes them: see ntc_linear4.
+
+    scales have x's type; the other arguments are linear's."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return linear4(x, packed, scales, bias, group=group, rows=rows, offsets=offsets, activation=activation,
+                           leaky_slope=leaky_slope, residual=residual)
+    return _c.linear4(x, packed, scales, bias, group, rows, offsets, _choice(_ACTIVATIONS, activation, "activation"),
+                      leaky_slope, residual)

@@ -38,11 +38,14 @@ EXPORTS = ("ntc_create", "ntc_decode", "ntc_decode_host", "ntc_destroy", "ntc_de
            "ntc_bucket_static", "ntc_kmeans_map", "ntc_debug_wait_timeout", "ntc_last_error",
            "ntc_status_string", "ntc_route", "ntc_route_backward", "ntc_expert_order",
            "ntc_expert_order_workspace", "ntc_linear", "ntc_linear_workspace", "ntc_linear_backward",
-           "ntc_linear_backward_workspace", "ntc_linear_status", "ntc_combine", "ntc_combine_backward")
+           "ntc_linear_backward_workspace", "ntc_linear_status", "ntc_combine", "ntc_combine_backward",
+           "ntc_balance_loss_workspace", "ntc_balance_loss", "ntc_balance_loss_backward", "ntc_adamw", "ntc_pack4",
+           "ntc_unpack4", "ntc_linear4_workspace", "ntc_linear4")
 
 # routed experts
 NTC_MAX_EXPERTS, NTC_MAX_TOP_K = 1024, 32
 NTC_TYPE_FP32, NTC_TYPE_FP16, NTC_TYPE_BF16 = range(3)
+NTC_ADAMW_BLOCK, NTC_ADAMW_WORKSPACE = 256, 16
 SCORES = {"softmax": 0, "sigmoid": 1}
 ACTIVATIONS = {"none": 0, "relu": 1, "leaky": 2, "gelu": 3, "silu": 4}
 
@@ -91,6 +94,26 @@ class ntc_combine_desc(ctypes.Structure):
                     (f, ctypes.c_uint64) for f in ("num_tokens", "num_rows", "ld_y", "ld_out", "ld_residual")]
 
 
+class ntc_balance_desc(ctypes.Structure):
+    _fields_ = [("num_experts", ctypes.c_uint32), ("top_k", ctypes.c_uint32), ("score", ctypes.c_uint32),
+                ("scale", ctypes.c_float), ("type", ctypes.c_int)]
+
+
+class ntc_adamw_tensor(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in ("param", "grad", "m", "v", "scale_m", "scale_v", "copy")] + [
+        ("count", ctypes.c_uint64)] + [(f, ctypes.c_int) for f in ("param_type", "grad_type", "copy_type")]
+
+
+class ntc_adamw_desc(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_double) for f in ("lr", "beta1", "beta2", "eps", "weight_decay", "grad_scale")] + [
+        ("step", ctypes.c_uint64), ("moment_bits", ctypes.c_uint32)]
+
+
+class ntc_pack4_desc(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int)] + [(f, ctypes.c_uint32) for f in ("in_dim", "out_dim", "num_experts", "group")] + [
+        (f, ctypes.c_uint64) for f in ("ld_packed", "stride_packed", "ld_scales", "stride_scales")]
+
+
 class NtcError(RuntimeError):
     def __init__(self, status, msg):
         super().__init__(f"{msg} (status {status})")
@@ -131,6 +154,14 @@ def _load():
         "ntc_linear_status": ([P], I),
         "ntc_combine": ([P, P, P, P, P, P, P, P], I),
         "ntc_combine_backward": ([P, P, P, P, P, P, P, P, P], I),
+        "ntc_balance_loss_workspace": ([P, S], S),
+        "ntc_balance_loss": ([P, S, P, S, P, P, P, P, P, S, P], I),
+        "ntc_balance_loss_backward": ([P, S, P, S, P, P, P, P, S, P, P], I),
+        "ntc_adamw": ([P, P, S, P, P, P, P, S, P], I),
+        "ntc_pack4": ([P, P, I, ctypes.c_uint64, ctypes.c_uint64, P, P, P], I),
+        "ntc_unpack4": ([P, P, P, P, ctypes.c_uint64, ctypes.c_uint64, P], I),
+        "ntc_linear4_workspace": ([P, P, P, P], S),
+        "ntc_linear4": ([P, P, P, P, P, P, P, P, P, P, P, S, P], I),
         "ntc_last_error": ([], ctypes.c_char_p),
         "ntc_status_string": ([I], ctypes.c_char_p),
     }
@@ -272,6 +303,44 @@ def ntc_combine(desc, y, place, weights, offsets, residual, out, stream):
 
 def ntc_combine_backward(desc, dout, y, place, weights, offsets, dy, dweights, stream):
     _check(_lib.ntc_combine_backward(ctypes.byref(desc), dout, y, place, weights, offsets, dy, dweights, stream))
+
+
+def ntc_balance_loss_workspace(desc, n) -> int:
+    return _lib.ntc_balance_loss_workspace(ctypes.byref(desc), n)
+
+
+def ntc_balance_loss(desc, n, logits, ld_logits, ids, loss, counts, mean, workspace, workspace_bytes, stream):
+    _check(_lib.ntc_balance_loss(ctypes.byref(desc), n, logits, ld_logits, ids, loss, counts, mean, workspace,
+                                 workspace_bytes, stream))
+
+
+def ntc_balance_loss_backward(desc, n, logits, ld_logits, ids, counts, dloss, residual, ld_residual, dlogits, stream):
+    _check(_lib.ntc_balance_loss_backward(ctypes.byref(desc), n, logits, ld_logits, ids, counts, dloss, residual,
+                                          ld_residual, dlogits, stream))
+
+
+def ntc_adamw(desc, tensors, d_lr, d_step, d_grad_scale, workspace, workspace_bytes, stream):
+    """`tensors`: a sequence of ntc_adamw_tensor."""
+    t = (ntc_adamw_tensor * len(tensors))(*tensors)
+    _check(_lib.ntc_adamw(ctypes.byref(desc), t, len(tensors), d_lr, d_step, d_grad_scale, workspace, workspace_bytes,
+                          stream))
+
+
+def ntc_pack4(desc, w, w_type, ld_w, stride_w, packed, scales, stream):
+    _check(_lib.ntc_pack4(ctypes.byref(desc), w, w_type, ld_w, stride_w, packed, scales, stream))
+
+
+def ntc_unpack4(desc, packed, scales, w, ld_w, stride_w, stream):
+    _check(_lib.ntc_unpack4(ctypes.byref(desc), packed, scales, w, ld_w, stride_w, stream))
+
+
+def ntc_linear4_workspace(desc, weights, x, rows) -> int:
+    return _lib.ntc_linear4_workspace(ctypes.byref(desc), ctypes.byref(weights), x, rows)
+
+
+def ntc_linear4(desc, weights, x, rows, offsets, packed, scales, bias, residual, y, workspace, workspace_bytes, stream):
+    _check(_lib.ntc_linear4(ctypes.byref(desc), ctypes.byref(weights), x, rows, offsets, packed, scales, bias, residual,
+                            y, workspace, workspace_bytes, stream))
 
 
 def kmeans_map(features, m, init, max_iters=100):
@@ -456,7 +525,8 @@ class Decoder:
 
 # The routed-expert calls on torch tensors live in experts.py, which imports torch;
 # they are names of this module that are looked up when first used.
-_EXPERTS = ("route", "route_backward", "expert_order", "linear", "linear_backward", "combine", "combine_backward")
+_EXPERTS = ("route", "route_backward", "expert_order", "linear", "linear_backward", "combine", "combine_backward",
+            "balance_loss", "balance_loss_backward", "adamw", "pack4", "unpack4", "linear4")
 
 
 def __getattr__(name):
