@@ -660,7 +660,8 @@ typedef struct {
 
 /* scale = max |w| of the group / 7, rounded to `type`; q = w / scale rounded to
  * nearest even and held in -8..7 (0 where the scale is 0).  A group with an infinity
- * or a NaN has the scale NaN.  Where in_dim is odd the last half byte is q = 0.
+ * or a NaN has the scale NaN; one whose scale is above the type's largest number has an
+ * infinite scale and reads back as NaN.  Where in_dim is odd the last half byte is q = 0.
  * w[E][N][ld_w] of w_type, stride_w elements from expert to expert. */
 NTC_API ntc_status ntc_pack4(const ntc_pack4_desc *desc, const void *w, ntc_type w_type, uint64_t ld_w,
                              uint64_t stride_w, uint8_t *packed, void *scales, void *cuda_stream);

@@ -17,65 +17,133 @@ using namespace ntc;
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
-constexpr int kEndCtas = 8, kEndThreads = 512;  // the second kernel: a cluster
+constexpr int kEndCtas = 8, kEndThreads = 1024;  // the second kernel: a cluster
+
+// Threads of a CTA of the forward call by the experts of a lane: one CTA an SM where 64 registers do, so that
+// few sums are left to add.
+constexpr int threads(int V) { return V <= 8 ? 1024 : 256; }
 
 // A token's logits in G lanes.  ROWS: lane `sub` has the V consecutive experts from
 // sub * V on (vector loads); else every G-th, so that the lanes' loads are runs.
 template <typename T, int V, int G, bool ROWS>
 struct Row {
-  float l[V];
-  uint32_t live = 0;  // bit i: l[i] is inside the row and not masked
+  // as they are in memory, -inf outside the row: what is loaded ahead is not waited for
+  static constexpr int kWords = ROWS ? V * (int)sizeof(T) / 4 : V;
+  static constexpr uint32_t kNone = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00u : 0xFF80u;
+  uint32_t w[kWords];
 
   static __device__ __forceinline__ uint32_t expert(uint32_t sub, int i) { return ROWS ? sub * V + i : i * G + sub; }
+  static __device__ __forceinline__ uint32_t bits(const T *p) {
+    if constexpr (sizeof(T) == 4) return *reinterpret_cast<const uint32_t *>(p);
+    else return *reinterpret_cast<const uint16_t *>(p);
+  }
   __device__ __forceinline__ void load(const T *row, uint32_t E, uint32_t sub) {
-    if constexpr (ROWS) {
-      load_run<T, V>(row + sub * V, (int)E - (int)(sub * V), true, l);
-    } else {
+    if constexpr (!ROWS) {
 #pragma unroll
-      for (int i = 0; i < V; ++i) l[i] = expert(sub, i) < E ? to_f<T>(row[expert(sub, i)]) : -INFINITY;
+      for (int i = 0; i < V; ++i) w[i] = expert(sub, i) < E ? bits(row + expert(sub, i)) : kNone;
+    } else {
+      const int n = (int)E - (int)(sub * V);
+      row += sub * V;
+      if (n >= V) {
+        if constexpr (kWords % 4 == 0) {
+#pragma unroll
+          for (int i = 0; i < kWords; i += 4) {
+            const uint4 q = *reinterpret_cast<const uint4 *>(row + i * 4 / (int)sizeof(T));
+            w[i] = q.x, w[i + 1] = q.y, w[i + 2] = q.z, w[i + 3] = q.w;
+          }
+        } else if constexpr (kWords == 2) {
+          const uint2 q = *reinterpret_cast<const uint2 *>(row);
+          w[0] = q.x, w[1] = q.y;
+        } else {
+          w[0] = *reinterpret_cast<const uint32_t *>(row);
+        }
+      } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) w[i] = i < n ? bits(row + i) : kNone;
+      } else {
+#pragma unroll
+        for (int i = 0; i < V; i += 2)
+          w[i / 2] = (i < n ? bits(row + i) : kNone) | (i + 1 < n ? bits(row + i + 1) : kNone) << 16;
+      }
     }
   }
-  // The probabilities but for their sum, which is returned; `slope`: a sigmoid's slope over its value.
-  // Both scores are taken relative to the largest logit m (a sigmoid where m < 0): the sum is
-  // not 0, and keeps its digits, wherever the row lies.
-  __device__ __forceinline__ float scores(bool softmax, float (&p)[V], float (&slope)[V], float &top, uint32_t &at) {
-    live = 0;
-    float mine = -INFINITY;
-    at = 0;
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else if constexpr (!ROWS) return unpack2<T>(w[i]).x;
+    else return i & 1 ? unpack2<T>(w[i / 2]).y : unpack2<T>(w[i / 2]).x;
+  }
+  __device__ __forceinline__ void values(float (&l)[V]) const {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      if (live_logit(l[i])) live |= 1u << i;
-      else l[i] = -INFINITY;
-      if (l[i] > mine) mine = l[i], at = i;
-    }
-    top = mine;
-    const float m = value_of(group_max<G>(live ? key_of(mine) : 0u));
+    for (int i = 0; i < V; ++i) l[i] = at(i);
+  }
+};
+
+// What a token's scores are made of, G lanes with V values each.
+template <int V, int G>
+struct Scores {
+  float l[V];
+  __device__ __forceinline__ float largest() const {  // of the lane; NaN has no part in it
+    float m = l[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) m = fmaxf(m, l[i]);
+    return fmaxf(m, -INFINITY);
+  }
+  // The probabilities but for their sum, which is returned; `slope`: a sigmoid's slope over
+  // its value.  m: the largest logit of the token.  0 where the logit is masked.
+  //
+  // exp(x) is fine_exp's formula without its bounds: a masked or NaN logit is first held where
+  // exp is 0 and nothing overflows.  A token far outside of what that allows, or whose
+  // sigmoids are all small, makes its warp take the careful form.
+  __device__ __forceinline__ float scores(bool softmax, float m, float (&p)[V], float (&slope)[V]) const {
     float sum = 0.0f;
+    if (__any_sync(kAll, softmax ? !(fabsf(m) < 8e37f) : !(m >= 0.0f && m < 8e37f))) return careful(softmax, m, p, slope);
     if (softmax) {
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        p[i] = live >> i & 1 ? fine_exp(l[i] - m) : 0.0f;
+        const float x = fmaxf(l[i], -8.5e37f) - m, t = x * 1.44269504f, e = quick_exp2(t);
+        p[i] = fmaf(e, fmaf(t, -0.693147182f, x), e);
         sum += p[i];
       }
     } else {
-      // sigmoid(l) exp(-c) with c = min(m, 0): for x = l - c, e = exp(-|x|) it is e / (1 + e exp(c)) at
-      // x <= 0 and 1 / (1 + e) above, where c = 0
-      const float c = fminf(m, 0.0f), scale = fine_exp(c);
+      // at -88 and below 1 / (1 + exp(-l)) is below the smallest normal number, and 0
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float x = l[i] - c, e = fine_exp(-fabsf(x));
-        const bool low = x <= 0.0f;
-        const float d = quick_inverse(low ? fmaf(e, scale, 1.0f) : 1.0f + e);
-        p[i] = live >> i & 1 ? (low ? e * d : d) : 0.0f;
-        slope[i] = low ? d : e * d;  // sigmoid(-l)
+        const float x = fmaxf(l[i], -88.0f), t = x * -1.44269504f, q = quick_exp2(t), e = fmaf(q, fmaf(t, -0.693147182f, -x), q);
+        p[i] = quick_inverse(1.0f + e);
+        slope[i] = e * p[i];
         sum += p[i];
       }
     }
     return group_sum<G>(sum);
   }
+  // Any logits.  A sigmoid is taken times exp(-c), c = min(m, 0): the sum is not 0, and keeps its digits,
+  // wherever the row lies.  For x = l - c and e = exp(-|x|) it is e / (1 + e exp(c)) at x <= 0 and
+  // 1 / (1 + e) above, where c = 0.
+  __device__ __forceinline__ float careful(bool softmax, float m, float (&p)[V], float (&slope)[V]) const {
+    float sum = 0.0f;
+    m = fminf(m, 3.402823466e38f);
+    const float c = softmax ? m : fminf(m, 0.0f), scale = softmax ? 0.0f : fine_exp(c);
+#pragma unroll 1
+    for (int i = 0; i < V; ++i) {
+      float v = 0.0f;
+#pragma unroll
+      for (int j = 0; j < V; ++j)  // registers have no index
+        if (j == i) v = l[j];
+      const bool live = live_logit(v);
+      const float x = v - c, e = fine_exp(-fabsf(x));
+      const bool low = x <= 0.0f;
+      const float d = quick_inverse(low ? fmaf(e, scale, 1.0f) : 1.0f + e);
+      const float q = !live ? 0.0f : low ? e * d : d, s = low ? d : e * d;  // s: sigmoid(-l)
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (j == i) p[j] = q, slope[j] = s;
+      sum += q;
+    }
+    return group_sum<G>(sum);
+  }
 };
+
+constexpr int kBackThreads = 256;
 
 struct Sums {  // of the CTAs, in the workspace
   float *p;        // [ctas][pitch]
@@ -92,9 +160,10 @@ struct Balance {  // what the forward call writes
 
 // Tokens of the call, E experts: counts in shared memory, p in registers and then there.
 template <typename T, int V, int G, bool ROWS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(threads(V))
     k_balance(const uint32_t E, const uint32_t k, const bool softmax, uint64_t n, const T *logits, uint64_t ld,
               const int32_t *ids, const Sums out, const Balance end) {
+  constexpr int kThreads = threads(V), kWarps = kThreads / 32;
   __shared__ float part[kWarps][V * G];
   __shared__ int32_t count[V * G + 1];
   constexpr uint32_t kTokens = 32 / G;  // of a warp at a time
@@ -107,24 +176,38 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
   for (int i = 0; i < V; ++i) acc[i] = 0.0f;
   uint32_t tokens = 0;
-  for (uint64_t t0 = ((uint64_t)blockIdx.x * kWarps + warp) * kTokens; t0 < n; t0 += (uint64_t)gridDim.x * kWarps * kTokens) {
-    const uint64_t t = t0 + lane / G;
-    const bool real = t < n;
-    Row<T, V, G, ROWS> row;
-    row.load(logits + (real ? t : t0) * ld, E, sub);
-    bool some = false;
-    for (uint32_t j = sub; j < k; j += G) {
-      const uint32_t id = real ? (uint32_t)ids[t * k + j] : E;
-      if (id < E) {
-        atomicAdd(count + id, 1);
-        some = true;
+  // 32-bit counts: n * top_k is below 2^31
+  const uint32_t by_tokens = gridDim.x * kWarps * kTokens, total = (uint32_t)n;
+  uint32_t t0 = (blockIdx.x * kWarps + warp) * kTokens;
+  Row<T, V, G, ROWS> row, next;
+  uint32_t id = E, next_id = E;  // the lane's first choice
+  const auto fetch = [&](uint32_t first, Row<T, V, G, ROWS> &r, uint32_t &choice) {
+    const uint32_t t = min(first + lane / G, total - 1);
+    r.load(logits + t * ld, E, sub);
+    choice = sub < k && first + lane / G < total ? (uint32_t)ids[t * k + sub] : E;
+  };
+  if (t0 < total) fetch(t0, next, next_id);
+  for (; t0 < total; t0 += by_tokens) {
+    row = next, id = next_id;
+    if (t0 + by_tokens < total) fetch(t0 + by_tokens, next, next_id);
+    bool some = id < E;
+    if (some) atomicAdd(count + id, 1);
+    if (k > G) {  // the others
+      const uint32_t t = t0 + lane / G;
+      for (uint32_t j = sub + G; j < k; j += G) {
+        const uint32_t other = t < total ? (uint32_t)ids[t * k + j] : E;
+        if (other < E) {
+          atomicAdd(count + other, 1);
+          some = true;
+        }
       }
     }
     const bool counts = group_count<G>(some, lane) > 0;
-    float p[V], slope[V], top;
-    uint32_t at;
-    const float sum = row.scores(softmax, p, slope, top, at);
-    const float by = counts && sum > 0.0f ? 1.0f / sum : 0.0f;
+    Scores<V, G> s;
+    row.values(s.l);
+    float p[V], slope[V];
+    const float sum = s.scores(softmax, group_max<G>(s.largest()), p, slope);
+    const float by = counts && sum > 0.0f ? quick_inverse(sum) : 0.0f;
 #pragma unroll
     for (int i = 0; i < V; ++i) acc[i] = fmaf(p[i], by, acc[i]);
     tokens += counts && sub == 0;
@@ -200,7 +283,7 @@ __global__ void __cluster_dims__(kEndCtas, 1, 1) __launch_bounds__(kEndThreads)
   uint32_t c = 0;
   if (e < E && slice < slices) {
     const uint32_t rows = (ctas + slices - 1) / slices, to = min(ctas, (slice + 1) * rows);
-#pragma unroll 4
+#pragma unroll 8
     for (uint32_t r = slice * rows; r < to; ++r) {
       s += in.p[(uint64_t)r * in.pitch + e];
       c += (uint32_t)in.count[(uint64_t)r * (in.pitch + 1) + e];
@@ -247,11 +330,11 @@ __global__ void __cluster_dims__(kEndCtas, 1, 1) __launch_bounds__(kEndThreads)
 // counts' place: the sum of p times them keeps its digits where one p is near 1, and is
 // exactly 0 where the counts are equal.
 template <typename T, int V, int G, bool ROWS>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kBackThreads)
     k_balance_back(const uint32_t E, const uint32_t k, const bool softmax, uint64_t n, const T *logits, uint64_t ld,
                    const int32_t *ids, const int32_t *counts, const float *dloss, float scale, const T *residual,
                    uint64_t ld_residual, T *dlogits) {
-  constexpr uint32_t kTokens = 32 / G;
+  constexpr uint32_t kTokens = 32 / G, kWarps = kBackThreads / 32;
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32, sub = lane & (G - 1);
   using R = Row<T, V, G, ROWS>;
   pdl_wait();
@@ -267,26 +350,30 @@ __global__ void __launch_bounds__(kThreads)
   all = group_add<G>(all);
   const int32_t live = counts[E];
   const float a = live > 0 && all ? (dloss ? *dloss : 1.0f) * scale * (float)E / (float)live / (float)all : 0.0f;
-  for (uint64_t t0 = ((uint64_t)blockIdx.x * kWarps + warp) * kTokens; t0 < n; t0 += (uint64_t)gridDim.x * kWarps * kTokens) {
-    const uint64_t t = t0 + lane / G;
-    const bool real = t < n;
-    R row;
-    row.load(logits + (real ? t : t0) * ld, E, sub);
+  const uint32_t by_tokens = gridDim.x * kWarps * kTokens, tokens = (uint32_t)n;
+  for (uint32_t t0 = (blockIdx.x * kWarps + warp) * kTokens; t0 < tokens; t0 += by_tokens) {
+    const uint32_t t = min(t0 + lane / G, tokens - 1);
+    const bool real = t0 + lane / G < tokens;
+    R row, add;
+    row.load(logits + t * ld, E, sub);
+    if (residual) add.load(residual + t * ld_residual, E, sub);
     bool some = false;
-    for (uint32_t j = sub; j < k; j += G) some |= real && (uint32_t)ids[t * k + j] < E;
-    float p[V], slope[V], top;
-    uint32_t at;
-    const float sum = row.scores(softmax, p, slope, top, at);
-    const bool has = group_count<G>(some, lane) > 0 && sum > 0.0f;
-    const float by = has ? 1.0f / sum : 0.0f;
+    for (uint32_t j = sub; j < k; j += G) some |= (uint32_t)ids[t * k + j] < E;
+    Scores<V, G> s;
+    row.values(s.l);
     // the likeliest expert's count
+    float top = -INFINITY;
     int32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-      if (at == i) mine = c[i];
-    const uint32_t key = row.live ? key_of(top) : 0u;
-    const uint32_t first = group_first<G>(key == group_max<G>(key), lane);
+      if (s.l[i] > top) top = s.l[i], mine = c[i];
+    const float m = group_max<G>(top);
+    const uint32_t first = group_first<G>(top == m, lane);
     const int32_t ref = __shfl_sync(kAll, mine, first, G);
+    float p[V], slope[V];
+    const float sum = s.scores(softmax, m, p, slope);
+    const bool has = group_count<G>(some, lane) > 0 && sum > 0.0f;
+    const float by = has ? 1.0f / sum : 0.0f;
     float dot = 0.0f, d[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -297,18 +384,15 @@ __global__ void __launch_bounds__(kThreads)
     dot = group_sum<G>(dot);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      d[i] = a * p[i] * (d[i] - dot);
+      d[i] = a * p[i] * (d[i] - dot);  // p is 0 where the logit is masked or the token does not count
       if (!softmax) d[i] *= slope[i];
-      if (!(row.live >> i & 1) || !has) d[i] = 0.0f;
     }
     if (!real) continue;  // no lane of the token takes part in what follows
     if (residual) {
-      R add;
-      add.load(residual + t * ld_residual, E, sub);
 #pragma unroll
-      for (int i = 0; i < V; ++i) d[i] += add.l[i];
+      for (int i = 0; i < V; ++i) d[i] += add.at(i);
     }
-    T *out = dlogits + t * E;
+    T *out = dlogits + (uint64_t)t * E;
     if constexpr (ROWS) {
       store_run<T, V>(out + sub * V, (int)E - (int)(sub * V), true, d);
     } else {
@@ -342,13 +426,14 @@ cudaError_t by_experts(uint32_t E, F &&f) {
   if (E <= 512) return f(integral_constant<int, 16>{}, integral_constant<int, 32>{});
   return f(integral_constant<int, 32>{}, integral_constant<int, 32>{});
 }
-uint32_t tokens_of_cta(uint32_t E) { return kWarps * (E <= 64 ? 4 : E <= 128 ? 2 : 1); }
+uint32_t tokens_of_warp(uint32_t E) { return E <= 64 ? 4 : E <= 128 ? 2 : 1; }
 
-// CTAs of the forward call: one while its warps have few turns, else two an SM at most, for every CTA's
-// sums are read again.
+// CTAs of the forward call: one while its warps have few turns, else as many as run at
+// once, for every CTA's sums are read again.
 uint32_t forward_ctas(uint64_t n, uint32_t E) {
-  const uint64_t turns = (n + tokens_of_cta(E) - 1) / tokens_of_cta(E);
-  return turns <= 4 ? 1 : (uint32_t)std::min<uint64_t>(turns, (uint64_t)sm_count() * 2);
+  const uint32_t warps = threads(E <= 256 ? 8 : 16) / 32, resident = E <= 256 ? 1 : 2;
+  const uint64_t turns = (n + warps * tokens_of_warp(E) - 1) / (warps * tokens_of_warp(E));
+  return turns <= 4 ? 1 : (uint32_t)std::min<uint64_t>(turns, (uint64_t)sm_count() * resident);
 }
 uint32_t pitch_of(uint32_t E) { return (E + 7) / 8 * 8; }
 
@@ -365,7 +450,7 @@ cudaError_t forward(const ntc_balance_desc &d, uint64_t n, const void *logits, u
   const uint32_t E = d.num_experts, ctas = forward_ctas(n, E);
   cudaError_t e = by_experts(E, [&](auto v, auto g) {
     constexpr int V = decltype(v)::value, G = decltype(g)::value;
-    return launch_pdl(runs<T, V>(logits, ld) ? k_balance<T, V, G, true> : k_balance<T, V, G, false>, ctas, kThreads, 0, st, E,
+    return launch_pdl(runs<T, V>(logits, ld) ? k_balance<T, V, G, true> : k_balance<T, V, G, false>, ctas, threads(V), 0, st, E,
                       d.top_k, d.score == NTC_SCORE_SOFTMAX, n, (const T *)logits, ld, ids, sums, end);
   });
   if (e != cudaSuccess || ctas == 1) return e;
@@ -377,12 +462,12 @@ template <typename T>
 cudaError_t backward(const ntc_balance_desc &d, uint64_t n, const void *logits, uint64_t ld, const int32_t *ids,
                      const int32_t *counts, const float *dloss, const void *residual, uint64_t ld_residual, void *dlogits,
                      cudaStream_t st) {
-  const uint32_t E = d.num_experts, per = tokens_of_cta(E);
+  const uint32_t E = d.num_experts, per = tokens_of_warp(E) * kBackThreads / 32;
   const unsigned grid = (unsigned)std::min<uint64_t>((n + per - 1) / per, (uint64_t)sm_count() * 8);
   return by_experts(E, [&](auto v, auto g) {
     constexpr int V = decltype(v)::value, G = decltype(g)::value;
     const bool rows = runs<T, V>(logits, ld) && runs<T, V>(dlogits, E) && (!residual || runs<T, V>(residual, ld_residual));
-    return launch_pdl(rows ? k_balance_back<T, V, G, true> : k_balance_back<T, V, G, false>, grid, kThreads, 0, st, E,
+    return launch_pdl(rows ? k_balance_back<T, V, G, true> : k_balance_back<T, V, G, false>, grid, kBackThreads, 0, st, E,
                       d.top_k, d.score == NTC_SCORE_SOFTMAX, n, (const T *)logits, ld, ids, counts, dloss, d.scale,
                       (const T *)residual, ld_residual, (T *)dlogits);
   });

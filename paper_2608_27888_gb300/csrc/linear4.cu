@@ -5,9 +5,8 @@
 // Few rows per expert: the weights' bytes are read once and are the bound, half a byte a
 // weight.  A warp takes 16 rows of the weights.  Chunks of 128 along K (64 bytes a row)
 // come through a ring of its own in shared memory by cp.async, so that their latency costs
-// no registers, and leave it word by word: eight weights of one row, whose halves of
-// q + 8 in the mantissa of a 16-bit number become q by one subtraction, exactly.  They are
-// the A operand of mma.sync.m16n8k16; eight rows of x are the B operand.  A word gives the
+// no registers, and leave it word by word: eight weights of one row, whose numbers q
+// become 16-bit ones exactly.  They are the A operand of mma.sync.m16n8k16; eight rows of x are the B operand.  A word gives the
 // pairs (0, 4), (1, 5), (2, 6), (3, 7) of its weights without a shuffle; x's pairs are made
 // to match, for an MMA's k order is free as long as both operands agree.  A group's sum is
 // scaled in fp32, so that no product of a scale and a weight is rounded.
@@ -37,8 +36,8 @@ struct FewArgs {
   const uint16_t *scales;
   uint64_t ld_packed, stride_packed, ld_scales, stride_scales;
   uint32_t group, groups;
-  uint32_t split;        // warps along K: 1, 2, 4 or 8
-  uint32_t vec_w, vec_x; // rows start on 16 bytes
+  uint32_t split;  // warps along K: 1, 2, 4 or 8
+  uint32_t vec_w;  // rows of packed start on 16 bytes
 };
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {  // the rest of the 16 are zeros
@@ -55,45 +54,41 @@ __device__ __forceinline__ uint32_t lds(uint32_t at) {
   return v;
 }
 
-// A row of x: eight elements from p on, n of them inside (the others 0).
-__device__ __forceinline__ uint4 load_x(const uint16_t *p, int n, bool vec) {
-  if (vec && n >= 8) return *reinterpret_cast<const uint4 *>(p);
-  uint32_t v[4];
+// `bytes` bytes from src on, and zeros: 16 bytes to shared memory, from any address.
+__device__ __noinline__ void copy_bytes(uint32_t dst, const uint8_t *src, uint32_t bytes) {
+  uint32_t v[4] = {};
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    v[i] = (2 * i < n ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)p[2 * i + 1] << 16 : 0u);
-  return make_uint4(v[0], v[1], v[2], v[3]);
+  for (uint32_t i = 0; i < 16; ++i)
+    if (i < bytes) v[i / 4] |= (uint32_t)src[i] << (8 * (i & 3));
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
 }
 
-// Eight weights of a word as pairs (0, 4), (1, 5), (2, 6), (3, 7): the halves of q + 8 in
-// the low mantissa bits of 1024 (fp16) or 128 (bf16), less 1032 or 136.
-template <typename T>
-__device__ __forceinline__ void weights(uint32_t w, uint32_t (&v)[4]) {
-  constexpr bool kHalf = std::is_same<T, __half>::value;
+// A row of x: eight elements from k on (zeros past K).  VEC: K and the rows' starts are whole pieces.
+template <bool VEC>
+__device__ __forceinline__ uint4 load_x(const uint16_t *row, uint32_t k, uint32_t K) {
+  if constexpr (VEC) {
+    return k < K ? *reinterpret_cast<const uint4 *>(row + k) : make_uint4(0, 0, 0, 0);
+  } else {
+    uint32_t v[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t m = (w >> (4 * i) & 0x000F000Fu) | (kHalf ? 0x64006400u : 0x43004300u);
-    if constexpr (kHalf) {
-      const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&m), __half2half2(__ushort_as_half(0x6408)));
-      v[i] = *reinterpret_cast<const uint32_t *>(&r);
-    } else {
-      const __nv_bfloat162 r =
-          __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&m), __bfloat162bfloat162(__ushort_as_bfloat16(0x4308)));
-      v[i] = *reinterpret_cast<const uint32_t *>(&r);
-    }
+    for (int i = 0; i < 4; ++i)
+      v[i] = (k + 2 * i < K ? (uint32_t)row[k + 2 * i] : 0u) | (k + 2 * i + 1 < K ? (uint32_t)row[k + 2 * i + 1] << 16 : 0u);
+    return make_uint4(v[0], v[1], v[2], v[3]);
   }
 }
 
-// NT: blocks of eight rows of x that a warp takes at a time.
-template <typename T, int NT>
-__global__ void __launch_bounds__(kThreads, 2) k_linear4_few(const FewArgs f) {
+// NT: blocks of eight rows of x that a warp takes at a time.  `split` warps are a team,
+// which takes its units by itself.
+template <typename T, int NT, bool VEC, int GROUP>
+__global__ void __launch_bounds__(kThreads, NT == 4 ? 2 : 3) k_linear4_few(const FewArgs f) {
   extern __shared__ __align__(16) uint8_t ring[];
+  constexpr int kScales = kChunk / GROUP;  // of a row in a chunk
   const LinearArgs &a = f.a;
   __shared__ int32_t begin[NTC_MAX_EXPERTS];   // of the experts with rows: first row,
   __shared__ int32_t count[NTC_MAX_EXPERTS];   // rows,
   __shared__ uint16_t which[NTC_MAX_EXPERTS];  // and number
   __shared__ uint32_t active, live;
-  __shared__ float part[kWarps][16][8 * NT + 1];  // sums of 16 rows of weights times x's
+  __shared__ float part[kWarps][8 * NT][17];  // sums of x's rows times 16 rows of weights
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, t = lane & 3;
   const uint32_t K = a.depth, N = a.width, split = f.split;
   pdl_wait();
@@ -101,137 +96,140 @@ __global__ void __launch_bounds__(kThreads, 2) k_linear4_few(const FewArgs f) {
   if (warp == 0) list_experts(a, lane, begin, count, which, &active, &live);
   __syncthreads();
 
-  const uint32_t blocks = kWarps / split;  // of 16 rows of weights in a CTA
-  const uint32_t per = (N + 16 * blocks - 1) / (16 * blocks);
-  const uint32_t slice = warp % split, block = warp / split;
+  const uint32_t teams = kWarps / split, team = warp / split, slice = warp % split;
+  const auto team_sync = [&] {
+    if (split == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(split * 32) : "memory");
+  };
+  const uint32_t per = (N + 15) / 16;
   const uint32_t chunks = (K + kChunk - 1) / kChunk, run = (chunks + split - 1) / split;
   const uint32_t c_from = min(slice * run, chunks), c_to = min(c_from + run, chunks);
-  const uint32_t row_bytes = (K + 1) / 2, steps_of_group = f.group / 32;
-  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + warp * kStages * kStageBytes;
-  for (uint32_t u = blockIdx.x; u < active * per; u += gridDim.x) {
-    const uint32_t i = u / per, col0 = (u - i * per) * 16 * blocks, n0 = col0 + block * 16;
+  const int32_t row_bytes = (int32_t)(K + 1) / 2;
+  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + warp * kStages * kStageBytes, last = mine + kStages * kStageBytes;
+  const uint32_t to_stage = g * kPitch + t * 16, from_stage = g * kPitch + t * 4;
+  for (uint32_t u = blockIdx.x * teams + team; u < active * per; u += gridDim.x * teams) {
+    const uint32_t i = u / per, n0 = (u - i * per) * 16;
     const uint32_t e = which[i];
-    const uint8_t *w = f.packed + e * f.stride_packed;
-    const uint16_t *s = f.scales + e * f.stride_scales;
     const bool in0 = n0 + g < N, in1 = n0 + g + 8 < N;
-    const uint16_t *s0 = s + (in0 ? n0 + g : 0) * f.ld_scales, *s1 = s + (in1 ? n0 + g + 8 : 0) * f.ld_scales;
-    // The chunk's 16 rows of 64 bytes: two pieces of 16 bytes a lane.
-    const auto fetch = [&](uint32_t c) {
-      if (c < c_to && n0 < N) {
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const uint32_t r = (lane + 32 * q) >> 2, off = c * 64 + (lane & 3) * 16;
-          const uint32_t have = n0 + r < N && off < row_bytes ? min(row_bytes - off, 16u) : 0;
-          const uint8_t *src = w + (have ? (n0 + r) * f.ld_packed + off : 0);
-          const uint32_t dst = mine + (c - c_from) % kStages * kStageBytes + r * kPitch + (lane & 3) * 16;
-          if (f.vec_w) {
-            copy16(dst, src, have);
-          } else {
-            uint32_t v[4] = {};
-            for (uint32_t b = 0; b < have; ++b) {
-              const uint32_t x = (uint32_t)src[b] << (8 * (b & 3));
-#pragma unroll
-              for (int j = 0; j < 4; ++j) v[j] |= b >> 2 == j ? x : 0u;
-            }
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-          }
-        }
-      }
-      copies_commit();
-    };
-    // The scales of a chunk's steps; of a step that does not end a group, nothing.
-    const auto scale_of = [&](uint32_t c, float (&v)[2][4]) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[0][j] = v[1][j] = 0.0f;
-        const uint32_t at = (c * kChunk + j * 32) / f.group;
-        if (((j + 1) & (steps_of_group - 1)) == 0 && c < c_to && at < f.groups) {
-          if (in0) v[0][j] = to_f<T>(reinterpret_cast<const T *>(s0)[at]);
-          if (in1) v[1][j] = to_f<T>(reinterpret_cast<const T *>(s1)[at]);
-        }
-      }
-    };
+    // The lane's two pieces of 16 bytes of a chunk: rows g and g + 8, bytes t * 16 on
+    const uint8_t *w0 = f.packed + e * f.stride_packed + (uint64_t)(in0 ? n0 + g : 0) * f.ld_packed + c_from * 64 + t * 16;
+    const uint8_t *w1 = in1 ? w0 + 8 * f.ld_packed : w0;
+    const int32_t left = row_bytes - (int32_t)(c_from * 64 + t * 16);
+    const T *s0 = (const T *)f.scales + e * f.stride_scales + (uint64_t)(in0 ? n0 + g : 0) * f.ld_scales + c_from * kScales;
+    const T *s1 = in1 ? s0 + 8 * f.ld_scales : s0;
     for (int32_t m0 = 0; m0 < count[i]; m0 += 8 * NT) {
       const int32_t rows = min(count[i] - m0, 8 * NT);
+      team_sync();  // nobody reads the ring's last chunks or the sums any more
+      uint32_t fetched = c_from, to = mine + to_stage;
+      const uint8_t *p0 = w0, *p1 = w1;
+      int32_t have = left;
+      const auto fetch = [&] {
+        if (fetched < c_to) {
+          const uint32_t n = (uint32_t)min(max(have, 0), 16), n0_ = in0 ? n : 0, n1_ = in1 ? n : 0;
+          if (f.vec_w) {
+            copy16(to, n ? p0 : w0, n0_);
+            copy16(to + 8 * kPitch, n ? p1 : w1, n1_);
+          } else {
+            copy_bytes(to, p0, n0_);
+            copy_bytes(to + 8 * kPitch, p1, n1_);
+          }
+          p0 += 64, p1 += 64, have -= 64, ++fetched;
+          to = to + kStageBytes >= last ? to + kStageBytes - kStages * kStageBytes : to + kStageBytes;
+        }
+        copies_commit();
+      };
+#pragma unroll 1
+      for (int c = 0; c < kStages - 1; ++c) fetch();
       const uint16_t *x[NT];
-      bool real[NT];
+      uint32_t end[NT];  // K, or 0 where there is no row
 #pragma unroll
       for (int h = 0; h < NT; ++h) {
         const int32_t r = (int32_t)g + 8 * h;
         int32_t at = -1;
         if (r < rows) at = a.rows ? (int32_t)ld_word((const uint32_t *)a.rows + begin[i] + m0 + r) : begin[i] + m0 + r;
-        real[h] = (uint32_t)at < a.x_rows;
-        x[h] = (const uint16_t *)a.x + (real[h] ? (uint64_t)(uint32_t)at * a.ld_x : 0);
+        end[h] = (uint32_t)at < a.x_rows ? K : 0;
+        x[h] = (const uint16_t *)a.x + (end[h] ? (uint64_t)(uint32_t)at * a.ld_x : 0);
       }
       float sum[NT][4] = {}, of_group[NT][4] = {};
-      __syncwarp();  // nobody reads the ring's last chunks any more
-      for (int c = 0; c < kStages - 1; ++c) fetch(c_from + c);
-      float scale[2][4], next[2][4];
-      scale_of(c_from, next);
-      for (uint32_t c = c_from; c < c_to; ++c) {
-        uint4 q[4][NT];
+      T next[2][kScales];
+      uint32_t at_scale = 0;
+      const auto scale_of = [&](uint32_t c) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t k = c * kChunk + j * 32 + t * 8;
-          const int have = (int)min(K - min(k, K), 8u);
-#pragma unroll
-          for (int h = 0; h < NT; ++h)
-            q[j][h] = have && real[h] ? load_x(x[h] + k, have, f.vec_x) : make_uint4(0, 0, 0, 0);
+        for (int j = 0; j < kScales; ++j) {
+          const bool is = c < c_to && (kScales == 1 || c * kScales + j < f.groups);
+          next[0][j] = is ? s0[at_scale + j] : from_f<T>(0.0f);
+          next[1][j] = is ? s1[at_scale + j] : from_f<T>(0.0f);
         }
+        at_scale += kScales;
+      };
+      scale_of(c_from);
+      uint4 q[NT], ahead[NT];
+      uint32_t k = c_from * kChunk + t * 8, stage = mine + from_stage;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) scale[0][j] = next[0][j], scale[1][j] = next[1][j];
-        scale_of(c + 1, next);
+      for (int h = 0; h < NT; ++h) ahead[h] = load_x<VEC>(x[h], k, end[h]);
+#pragma unroll 1
+      for (uint32_t c = c_from; c < c_to; ++c) {
+        float scale[2][kScales];
+#pragma unroll
+        for (int j = 0; j < kScales; ++j) scale[0][j] = to_f<T>(next[0][j]), scale[1][j] = to_f<T>(next[1][j]);
+        scale_of(c + 1);
         copies_wait<kStages - 2>();
         __syncwarp();
-        fetch(c + kStages - 1);
-        const uint32_t at = mine + (c - c_from) % kStages * kStageBytes + g * kPitch + t * 4;
+        fetch();
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          uint32_t lo[4], hi[4];
-          weights<T>(lds(at + j * 16), lo);
-          weights<T>(lds(at + 8 * kPitch + j * 16), hi);
+          k += 32;
 #pragma unroll
           for (int h = 0; h < NT; ++h) {
-            const uint4 &v = q[j][h];
+            q[h] = ahead[h];
+            ahead[h] = load_x<VEC>(x[h], k, end[h]);
+          }
+          uint32_t lo[4], hi[4];
+          numbers4<T>(lds(stage + j * 16), lo);
+          numbers4<T>(lds(stage + 8 * kPitch + j * 16), hi);
+#pragma unroll
+          for (int h = 0; h < NT; ++h) {
+            const uint4 &v = q[h];
             mma<T>(of_group[h], lo[0], hi[0], lo[1], hi[1], __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632));
             mma<T>(of_group[h], lo[2], hi[2], lo[3], hi[3], __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
           }
-          if (((j + 1) & (steps_of_group - 1)) == 0) {
+          if ((j + 1) % (GROUP / 32) == 0) {
 #pragma unroll
             for (int h = 0; h < NT; ++h) {
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
-                sum[h][r] = fmaf(scale[r >> 1][j], of_group[h][r], sum[h][r]);
+                sum[h][r] = fmaf(scale[r >> 1][j / (GROUP / 32)], of_group[h][r], sum[h][r]);
                 of_group[h][r] = 0.0f;
               }
             }
           }
         }
+        stage = stage + kStageBytes >= last ? stage + kStageBytes - kStages * kStageBytes : stage + kStageBytes;
       }
       copies_wait<0>();
 #pragma unroll
       for (int h = 0; h < NT; ++h) {
-        part[warp][g][8 * h + 2 * t] = sum[h][0];
-        part[warp][g][8 * h + 2 * t + 1] = sum[h][1];
-        part[warp][g + 8][8 * h + 2 * t] = sum[h][2];
-        part[warp][g + 8][8 * h + 2 * t + 1] = sum[h][3];
+        part[warp][8 * h + 2 * t][g] = sum[h][0];
+        part[warp][8 * h + 2 * t + 1][g] = sum[h][1];
+        part[warp][8 * h + 2 * t][g + 8] = sum[h][2];
+        part[warp][8 * h + 2 * t + 1][g + 8] = sum[h][3];
       }
-      __syncthreads();
+      team_sync();
       // 16 threads write a row's 16 columns
-      for (uint32_t b = 0; b < blocks; ++b) {
-        const uint32_t n = threadIdx.x & 15, col = col0 + b * 16 + n;
-        for (int32_t r = threadIdx.x >> 4; r < rows; r += kThreads / 16) {
-          if (col >= N) break;
+      const uint32_t n = lane & 15, col = n0 + n;
+      if (col < N) {
+        const float bias = a.bias ? a.bias[(uint64_t)e * N + col] : 0.0f;
+#pragma unroll 1
+        for (int32_t r = slice * 2 + (lane >> 4); r < rows; r += 2 * split) {
           float v[1] = {0.0f};
-          for (uint32_t p = 0; p < split; ++p) v[0] += part[b * split + p][n][r];
-          if (a.bias) v[0] += a.bias[(uint64_t)e * N + col];
+          for (uint32_t p = 0; p < split; ++p) v[0] += part[team * split + p][r][n];
+          v[0] += bias;
           activate(a.activation, a.slope, v);
           const uint64_t row = (uint64_t)(begin[i] + m0) + r;
           if (a.residual) v[0] += to_f<T>(((const T *)a.residual)[row * a.ld_residual + col]);
           ((T *)a.out)[row * a.ld_out + col] = from_f<T>(v[0]);
         }
       }
-      __syncthreads();
     }
   }
   // rows of no expert
@@ -242,18 +240,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_linear4_few(const FewArgs f) {
   }
 }
 
-template <typename T, int NT>
-cudaError_t launch(const FewArgs &f, unsigned grid, cudaStream_t st) {
+template <typename T, int NT, bool VEC, int GROUP>
+cudaError_t launch(const FewArgs &f, uint64_t units, cudaStream_t st) {
   static std::atomic<uint64_t> allowed{0};  // devices that know of the kernel's shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !((allowed.load() >> dev) & 1)) {
-    e = cudaFuncSetAttribute(k_linear4_few<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+    e = cudaFuncSetAttribute(k_linear4_few<T, NT, VEC, GROUP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
     if (e != cudaSuccess) return e;
     if (dev < 64) allowed.fetch_or(1ull << dev);
   }
-  return launch_pdl(k_linear4_few<T, NT>, grid, kThreads, kRingBytes, st, f);
+  const uint64_t ctas = (units * f.split + kWarps - 1) / kWarps;
+  const unsigned grid = (unsigned)std::min<uint64_t>(ctas, (uint64_t)sm_count() * (NT == 4 ? 2 : 3));
+  return launch_pdl(k_linear4_few<T, NT, VEC, GROUP>, grid, kThreads, kRingBytes, st, f);
 }
 
 // Rows of an expert that has any, on average, where the choices are spread evenly.
@@ -343,20 +343,25 @@ extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc
   f.group = p.group;
   f.groups = (d.in_dim + p.group - 1) / p.group;
   f.vec_w = ((uintptr_t)packed & 15) == 0 && p.ld_packed % 16 == 0 && (d.num_experts == 1 || p.stride_packed % 16 == 0);
-  f.vec_x = rows_are_vec(x, d.ld_x, 2);
-  // Warps along K until the warps that the SMs hold are at work, none with less than two chunks.
-  const int sms = sm_count();
+  const bool vec_x = d.in_dim % 8 == 0 && rows_are_vec(x, d.ld_x, 2);
+  // Warps along K until the warps that the SMs hold are at work.
   const uint64_t experts = std::min<uint64_t>(d.num_experts, d.num_rows), units = experts * ((d.out_dim + 15) / 16);
   f.split = 1;
-  while (f.split < 8 && units * f.split < 16ull * sms && d.in_dim >= 4 * f.split * kChunk) f.split *= 2;
-  const uint32_t columns = 16 * (kWarps / f.split);
-  const uint64_t ctas = experts * ((d.out_dim + columns - 1) / columns);
-  const unsigned grid = (unsigned)std::min<uint64_t>(ctas, (uint64_t)sms * 2);
+  while (f.split < 8 && units * f.split < 16ull * sm_count() && d.in_dim > f.split * kChunk) f.split *= 2;
   const uint64_t mean = mean_rows(d);
   const int nt = d.num_rows <= 8 || mean <= 4 ? 1 : d.num_rows <= 16 || mean <= 10 ? 2 : 4;
-  const auto go = [&](auto type) {
+  using std::integral_constant;
+  const auto by_rows = [&](auto type, auto vec, auto group) {
     using T = decltype(type);
-    return nt == 1 ? launch<T, 1>(f, grid, st) : nt == 2 ? launch<T, 2>(f, grid, st) : launch<T, 4>(f, grid, st);
+    constexpr bool V = decltype(vec)::value;
+    constexpr int G = decltype(group)::value;
+    return nt == 1 ? launch<T, 1, V, G>(f, units, st) : nt == 2 ? launch<T, 2, V, G>(f, units, st) : launch<T, 4, V, G>(f, units, st);
   };
+  const auto by_group = [&](auto type, auto vec) {
+    return p.group == 32   ? by_rows(type, vec, integral_constant<int, 32>{})
+           : p.group == 64 ? by_rows(type, vec, integral_constant<int, 64>{})
+                           : by_rows(type, vec, integral_constant<int, 128>{});
+  };
+  const auto go = [&](auto type) { return vec_x ? by_group(type, std::true_type{}) : by_group(type, std::false_type{}); };
   return op_cuda(bf16 ? go(__nv_bfloat16()) : go(__half()), "ntc_linear4");
 }

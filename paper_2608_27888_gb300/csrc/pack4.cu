@@ -46,15 +46,32 @@ struct Pack4 {
   uint32_t in_dim, out_dim, num_experts, group;
 };
 
-// w / s rounded to nearest even, held in -8..7: the product with 1 / s, put right by the
-// remainder w - q s, which one fused operation gives without rounding (q has four bits,
-// the remainder no more digits than w or s).
-__device__ __forceinline__ float quotient(float w, float s, float inv) {
-  float q = rintf(w * inv);
-  const float r = fmaf(-q, s, w), half = 0.5f * s;
-  if (r > half || r < -half) q += r > 0.0f ? 1.0f : -1.0f;
-  else if ((r == half || r == -half) && ((int)q & 1)) q += r > 0.0f ? 1.0f : -1.0f;
-  return fminf(fmaxf(q, -8.0f), 7.0f);
+// Two quotients w / s, correctly rounded to fp32: the product with an approximate 1 / s,
+// put right by its remainder, which one fused operation gives exactly.
+__device__ __forceinline__ float2 quotients(float2 w, float s, float inv) {
+  uint64_t x, i, m, q, r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(w.x), "f"(w.y));
+  asm("mov.b64 %0, {%1, %1};" : "=l"(i) : "f"(inv));
+  asm("mov.b64 %0, {%1, %1};" : "=l"(m) : "f"(-s));
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(q) : "l"(x), "l"(i));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(q), "l"(m), "l"(x));
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(q) : "l"(r), "l"(i), "l"(q));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(w.x), "=f"(w.y) : "l"(q));
+  return w;
+}
+// q + 8 of a quotient in the low four bits: rounded to nearest even by 1.5 * 2^23.  Quotients
+// of 16-bit numbers are no nearer to a half than fp32 tells, so the rounding is that of
+// w / s itself.  fp32 weights may be: `nearest` looks at the remainder.
+template <typename W>
+__device__ __forceinline__ uint32_t number(float quotient, float w, float s) {
+  float q = fminf(fmaxf(quotient, -8.0f), 7.0f);
+  if constexpr (sizeof(W) == 4) {
+    const float n = rintf(q), r = fmaf(-n, s, w), half = 0.5f * s;
+    const bool odd = (int)n & 1;
+    if (fabsf(r) > half || (fabsf(r) == half && odd)) q = n + (r > 0.0f ? 1.0f : -1.0f);
+    q = fminf(fmaxf(q, -8.0f), 7.0f);
+  }
+  return __float_as_uint(q + 12582920.0f);
 }
 
 template <typename W, typename T, bool VEC>
@@ -70,21 +87,36 @@ __global__ void __launch_bounds__(kThreads) k_pack4(const Pack4 a, const Turns t
     const uint32_t have = n < a.out_dim && k < a.in_dim ? min(a.in_dim - k, 8u) : 0;
     const W *w = (const W *)a.w + (have ? e * a.stride_w + n * a.ld_w + k : 0);
     float v[8];
+    uint32_t top = 0;  // the bits of the largest magnitude: NaN is above infinity, and infinity above numbers
     if (VEC && have == 8) {
+      if constexpr (sizeof(W) == 2) {  // two at a time, as whole numbers of 16 bits
+        const uint4 raw = __ldcs((const uint4 *)w);
+        const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+        uint32_t two = 0;
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        float f[Vec<W>::N];
-        Vec<W>::unpack(__ldcs((const uint4 *)w + i), f);
+        for (int i = 0; i < 4; ++i) {
+          two = __vmaxu2(two, words[i] & 0x7FFF7FFFu);
+          const float2 f = unpack2<W>(words[i]);
+          v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        }
+        top = __float_as_uint(unpack2<W>(max(two >> 16, two & 0xFFFFu)).x);
+      } else {
 #pragma unroll
-        for (int j = 0; j < Vec<W>::N; ++j) v[i * Vec<W>::N + j] = f[j];
+        for (int i = 0; i < kLoads; ++i) {
+          float f[Vec<W>::N];
+          Vec<W>::unpack(__ldcs((const uint4 *)w + i), f);
+#pragma unroll
+          for (int j = 0; j < Vec<W>::N; ++j) v[i * Vec<W>::N + j] = f[j];
+        }
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = i < (int)have ? to_f<W>(w[i]) : 0.0f;
     }
-    uint32_t top = 0;
+    if (sizeof(W) == 4 || !VEC || have != 8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+    }
     for (uint32_t s = 1; s < members; s <<= 1) top = max(top, __shfl_xor_sync(kAll, top, s));
     const float largest = __uint_as_float(top);
     const bool finite = largest < INFINITY;
@@ -96,10 +128,16 @@ __global__ void __launch_bounds__(kThreads) k_pack4(const Pack4 a, const Turns t
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= 18446744073709551616.0f;
     }
-    const float inv = some ? 1.0f / s : 0.0f;
-    uint32_t q = 0;
+    uint32_t q = 0x88888888u;
+    if (some) {
+      const float inv = quick_inverse(s);
+      q = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q |= (uint32_t)(some ? (int)quotient(v[i], s, inv) + 8 : 8) << (4 * i);
+      for (int i = 0; i < 8; i += 2) {
+        const float2 r = quotients(make_float2(v[i], v[i + 1]), s, inv);
+        q |= (number<W>(r.x, v[i], s) & 15u) << (4 * i) | (number<W>(r.y, v[i + 1], s) & 15u) << (4 * i + 4);
+      }
+    }
     if (have) {
       uint8_t *out = a.packed + e * a.stride_packed + n * a.ld_packed + k / 2;
       if (have == 8 && ((uintptr_t)out & 3) == 0) {
@@ -109,6 +147,17 @@ __global__ void __launch_bounds__(kThreads) k_pack4(const Pack4 a, const Turns t
       }
       if ((lane & (members - 1)) == 0) ((T *)a.scales)[e * a.stride_scales + n * a.ld_scales + k / a.group] = scale;
     }
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
+  if constexpr (std::is_same<T, __half>::value) {
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+  } else {
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
   }
 }
 
@@ -133,11 +182,23 @@ __global__ void __launch_bounds__(kThreads) k_unpack4(const Unpack a, const Turn
     } else {
       for (uint32_t i = 0; i < (have + 1) / 2; ++i) q |= (uint32_t)in[i] << (8 * i);
     }
-    const float s = to_f<T>(((const T *)a.scales)[e * a.stride_scales + n * a.ld_scales + k / a.group]);
-    float v[8];
+    // a number times the scale in 16 bits: one rounding, of the exact product
+    const uint32_t s = *(const uint16_t *)((const T *)a.scales + e * a.stride_scales + n * a.ld_scales + k / a.group) * 0x10001u;
+    uint32_t v[4];
+    numbers4<T>(q, v);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = s * (float)((int)(q >> (4 * i) & 15) - 8);
-    store_vec<T>((T *)a.w + e * a.stride_w + n * a.ld_w + k, (int)have, VEC, v);
+    for (int i = 0; i < 4; ++i) v[i] = times<T>(v[i], s);
+    const uint4 out = make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410),
+                                 __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
+    T *to = (T *)a.w + e * a.stride_w + n * a.ld_w + k;
+    if (VEC && have == 8) {
+      *(uint4 *)to = out;
+    } else {
+      const uint32_t word[4] = {out.x, out.y, out.z, out.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < (int)have) ((uint16_t *)to)[i] = (uint16_t)(word[i / 2] >> (16 * (i & 1)));
+    }
   }
 }
 

@@ -68,7 +68,7 @@ def test_groups_that_are_zero_tiny_huge_or_not_numbers(ntc, dtype):
     good = ~torch.isnan(s).repeat_interleave(32, -1)
     assert torch.equal(S.nibbles(packed, 64)[good], q[good])
     back = ntc.unpack4(packed, scales, 64, group=32)
-    assert bool(torch.isnan(back[~good]).all()) and bool(torch.isfinite(back[good]).all())
+    assert bool(torch.isnan(back[~good]).all()) and torch.equal(back[good], S.values(packed, scales, 64, 32).to(dtype)[good])
 
 
 def test_strided_weights(ntc):
