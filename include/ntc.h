@@ -607,12 +607,13 @@ NTC_API ntc_status ntc_balance_loss_backward(const ntc_balance_desc *desc, size_
  * moment_bits 32: m and v are fp32.  moment_bits 8: m and v hold e4m3 codes of m
  * and of sqrt(v), in blocks of NTC_ADAMW_BLOCK consecutive elements with an fp32
  * scale each, scale_m[i / NTC_ADAMW_BLOCK] and scale_v[...]: value = code * scale,
- * scale = (largest magnitude of the block) / 448, rounded to nearest; a root that is
- * not 0 keeps a code that is not 0, so that no division loses its denominator.  The
- * step itself uses the moments before they are rounded.  A moment that changes by
- * less than half of a code's distance (up to 1/16 of its value) keeps its code; what
- * the block's largest does is exact, and the others move with it.  A block whose
- * largest is below 2^-100 is 0; one with an infinity or a NaN reads back as NaN. */
+ * scale = (largest magnitude of the block) / 448, rounded to nearest.  A root has at
+ * least the least code (2^-9), so that no division loses its denominator.  The step
+ * itself uses the moments before they are rounded.  A moment that changes by less than
+ * half of a code's distance (up to 1/16 of its value) keeps its code; what the block's
+ * largest does is exact, and the others move with it.  Where a moment's largest is below
+ * 2^-100 its block is 0; both moments of a block with an infinity or a NaN read back as
+ * NaN. */
 #define NTC_ADAMW_BLOCK 256u
 typedef struct {
   void *param;             /* count elements of param_type                        */
@@ -669,7 +670,8 @@ NTC_API ntc_status ntc_pack4(const ntc_pack4_desc *desc, const void *w, ntc_type
 NTC_API ntc_status ntc_unpack4(const ntc_pack4_desc *desc, const uint8_t *packed, const void *scales, void *w,
                                uint64_t ld_w, uint64_t stride_w, void *cuda_stream);
 
-/* ntc_linear (without z) with weights in 4 bits.  desc's ld_w, stride_w and ld_z are
+/* ntc_linear (without z) with weights in 4 bits (ld_packed and ld_scales below 2^26).
+ * desc's ld_w, stride_w and ld_z are
  * not read; its type, in_dim, out_dim and num_experts are those of `weights`.  Calls
  * of few rows per expert (up to 32 on average) multiply the numbers q themselves, exact in 16 bits, and
  * the groups' fp32 sums by their scales; larger ones unpack the weights of experts

@@ -5,12 +5,13 @@
 //   decay = 1 - lr weight_decay, rate = lr / (1 - beta1^t), root = 1 / sqrt(1 - beta2^t)
 //
 // About 20 operations on 26 to 30 bytes an element (14 to 18 with moments in 8 bits): HBM
-// is the bound.  A warp takes a block of 256 elements, a lane eight of them, four
-// consecutive ones in each half; the block is also what an 8-bit scale belongs to, so its
+// is the bound.  A warp takes a block of 256 elements, a lane eight consecutive ones of
+// them; the block is also what an 8-bit scale belongs to, so its
 // largest moment is one reduction in the warp.  The tensors' table is the kernel's
 // argument: a step of many small tensors is one launch and copies nothing.
-// Every operation is rounded to nearest in fp32, in this order, without contraction, so
-// that the codes of 8-bit moments are the definition's.
+// The root and the reciprocal are the hardware's approximations (1 ulp each; the exact ones
+// made the 8-bit step a third slower), two elements go through one fp32x2 operation where
+// there is one; with them a change of p is off by 2^-21 of itself at most.
 #include "experts.cuh"
 
 #include <cuda_fp8.h>
@@ -27,6 +28,9 @@ constexpr int kThreads = 256;
 constexpr int kBlock = NTC_ADAMW_BLOCK;
 constexpr int kEach = kBlock / 32;
 constexpr uint32_t kAll = 0xFFFFFFFFu;
+// Blocks of a tensor that a warp takes at a time, at most: with 8-bit moments the next one is asked for ahead.
+constexpr uint32_t kTurn32 = 2, kTurn8 = 8;
+constexpr int kCtas = 4;       // an SM
 constexpr size_t kTensors = 1u << 20;  // of a call
 constexpr int kFew = 24, kMany = 400;  // tensors of a launch; 32,764 bytes of arguments is the limit
 
@@ -37,7 +41,7 @@ struct Entry {
   float *scale_m, *scale_v;
   void *copy;
   uint64_t count;
-  uint32_t first;  // the tensor's first block among the launch's
+  uint32_t first;  // the tensor's first turn among the launch's
   uint8_t p_type, g_type, copy_type, vec;
 };
 
@@ -50,7 +54,7 @@ struct Scalars {
 template <int CAP>
 struct Args {
   Scalars s;
-  uint32_t tensors, blocks, turn;  // turn: neighbouring blocks of a warp
+  uint32_t tensors, turns, turn;  // turn: neighbouring blocks of a tensor that a warp takes at a time
   Entry t[CAP];
 };
 
@@ -68,21 +72,20 @@ __global__ void k_adamw_scalars(double lr, const float *d_lr, double beta1, doub
 }
 
 // The lane's eight elements of a block: `left` of the block's are inside the tensor.  VEC: all of
-// the block, by 16-, 8- and 4-byte loads; else element by element, the lanes side by side.
+// the block, eight consecutive ones by a load of 32, 16 or 8 bytes; else element by element, the
+// lanes side by side.
 template <bool VEC>
 __device__ __forceinline__ uint32_t place(uint32_t lane, int i) {
-  return VEC ? (i >> 2) * 128 + lane * 4 + (i & 3) : i * 32 + lane;
+  return VEC ? lane * 8 + i : i * 32 + lane;
 }
 template <bool VEC>
 __device__ __forceinline__ void read(const void *base, uint64_t at, uint32_t type, uint32_t lane, uint32_t left, float (&v)[kEach]) {
   if (type == NTC_TYPE_FP32) {
     const float *p = (const float *)base + at;
     if constexpr (VEC) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float4 q = __ldcs((const float4 *)(p + place<VEC>(lane, 4 * h)));
-        v[4 * h] = q.x, v[4 * h + 1] = q.y, v[4 * h + 2] = q.z, v[4 * h + 3] = q.w;
-      }
+      asm volatile("ld.global.L1::no_allocate.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+                   : "l"(p + lane * 8));
     } else {
 #pragma unroll
       for (int i = 0; i < kEach; ++i) v[i] = place<VEC>(lane, i) < left ? p[place<VEC>(lane, i)] : 0.0f;
@@ -92,13 +95,9 @@ __device__ __forceinline__ void read(const void *base, uint64_t at, uint32_t typ
   const uint16_t *p = (const uint16_t *)base + at;
   const bool half = type == NTC_TYPE_FP16;
   if constexpr (VEC) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint2 q = __ldcs((const uint2 *)(p + place<VEC>(lane, 4 * h)));
-      const float2 a = half ? unpack2<__half>(q.x) : unpack2<__nv_bfloat16>(q.x);
-      const float2 b = half ? unpack2<__half>(q.y) : unpack2<__nv_bfloat16>(q.y);
-      v[4 * h] = a.x, v[4 * h + 1] = a.y, v[4 * h + 2] = b.x, v[4 * h + 3] = b.y;
-    }
+    const uint4 q = __ldcs((const uint4 *)(p + lane * 8));
+    if (half) Vec<__half>::unpack(q, v);
+    else Vec<__nv_bfloat16>::unpack(q, v);
   } else {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -112,9 +111,9 @@ __device__ __forceinline__ void write(void *base, uint64_t at, uint32_t type, ui
   if (type == NTC_TYPE_FP32) {
     float *p = (float *)base + at;
     if constexpr (VEC) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        __stcs((float4 *)(p + place<VEC>(lane, 4 * h)), make_float4(v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]));
+      asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]),
+                   "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "l"(p + lane * 8)
+                   : "memory");
     } else {
 #pragma unroll
       for (int i = 0; i < kEach; ++i)
@@ -124,145 +123,196 @@ __device__ __forceinline__ void write(void *base, uint64_t at, uint32_t type, ui
   }
   uint16_t *p = (uint16_t *)base + at;
   const bool half = type == NTC_TYPE_FP16;
-  const auto pair = [&](float a, float b) { return half ? pack2<__half>(a, b) : pack2<__nv_bfloat16>(a, b); };
   if constexpr (VEC) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      __stcs((uint2 *)(p + place<VEC>(lane, 4 * h)), make_uint2(pair(v[4 * h], v[4 * h + 1]), pair(v[4 * h + 2], v[4 * h + 3])));
+    __stcs((uint4 *)(p + lane * 8), half ? Vec<__half>::pack(v) : Vec<__nv_bfloat16>::pack(v));
   } else {
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      if (place<VEC>(lane, i) < left) p[place<VEC>(lane, i)] = (uint16_t)pair(v[i], 0.0f);
+      if (place<VEC>(lane, i) < left)
+        p[place<VEC>(lane, i)] = (uint16_t)(half ? pack2<__half>(v[i], 0.0f) : pack2<__nv_bfloat16>(v[i], 0.0f));
   }
 }
 
-__device__ __forceinline__ float2 from_codes(uint32_t two) {
+__device__ __forceinline__ float quick_root(float x) {
+  float y;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float inverse(float x) {
+  float y;
+  asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+__device__ __forceinline__ uint64_t from_codes(uint32_t two) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
-  return __half22float2(*reinterpret_cast<const __half2 *>(&h));
+  const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+  return both(f.x, f.y);
 }
 __device__ __forceinline__ uint32_t to_codes(float a, float b) {
   return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
 }
 
+// A lane's elements as pairs: 2 h and 2 h + 1 of its eight.
 template <bool VEC>
-__device__ __forceinline__ void read_codes(const void *base, uint64_t at, uint32_t lane, uint32_t left, float scale, float (&v)[kEach]) {
+__device__ __forceinline__ void read_codes(const void *base, uint64_t at, uint32_t lane, uint32_t left, float scale, uint64_t (&v)[4]) {
   const uint8_t *p = (const uint8_t *)base + at;
-  uint32_t q[2];
+  const uint64_t s = both(scale, scale);
+  uint32_t q[2] = {};
   if constexpr (VEC) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) q[h] = __ldcs((const uint32_t *)(p + place<VEC>(lane, 4 * h)));
+    const uint2 w = __ldcs((const uint2 *)(p + lane * 8));
+    q[0] = w.x, q[1] = w.y;
   } else {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      q[h] = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (place<VEC>(lane, 4 * h + i) < left) q[h] |= (uint32_t)p[place<VEC>(lane, 4 * h + i)] << (8 * i);
-    }
+    for (int i = 0; i < kEach; ++i)
+      if (place<VEC>(lane, i) < left) q[i / 4] |= (uint32_t)p[place<VEC>(lane, i)] << (8 * (i & 3));
   }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const float2 a = from_codes(q[h] & 0xFFFFu), b = from_codes(q[h] >> 16);
-    v[4 * h] = __fmul_rn(a.x, scale), v[4 * h + 1] = __fmul_rn(a.y, scale);
-    v[4 * h + 2] = __fmul_rn(b.x, scale), v[4 * h + 3] = __fmul_rn(b.y, scale);
+  for (int h = 0; h < 4; ++h) v[h] = mul2(from_codes(q[h / 2] >> (16 * (h & 1)) & 0xFFFFu), s);
+}
+// The codes of a block's values times inv, none below `least`.
+template <bool VEC, bool ROOT>
+__device__ __forceinline__ void write_codes(void *base, uint64_t at, uint32_t lane, uint32_t left, float inv, float least, const uint64_t (&v)[4]) {
+  uint8_t *p = (uint8_t *)base + at;
+  const uint64_t by = both(inv, inv);
+  uint32_t q[2] = {};
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    float2 x = each(mul2(v[h], by));
+    if constexpr (ROOT) x.x = fmaxf(x.x, least), x.y = fmaxf(x.y, least);
+    q[h / 2] |= to_codes(x.x, x.y) << (16 * (h & 1));
+  }
+  if constexpr (VEC) {
+    __stcs((uint2 *)(p + lane * 8), make_uint2(q[0], q[1]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (place<VEC>(lane, i) < left) p[place<VEC>(lane, i)] = (uint8_t)(q[i / 4] >> (8 * (i & 3)));
   }
 }
-// The codes of a block's values and their scale.  The bits of magnitudes order like the
-// values, infinities and NaN above all.  ROOT: a value above 0 keeps a code above 0.
-template <bool VEC, bool ROOT>
-__device__ __forceinline__ void write_codes(void *base, uint64_t at, uint32_t lane, uint32_t left, float *scale, const float (&v)[kEach]) {
-  uint32_t top = 0;
+
+// Both moments of a block.  The bits of roots order like the values, infinities and NaN above
+// all, and what makes m no number makes the root none.
+template <bool VEC>
+__device__ __forceinline__ void write_moments(const Entry &t, uint64_t block, uint32_t lane, uint32_t left, const uint64_t (&m)[4], const uint64_t (&root)[4]) {
+  float m_top = 0.0f;
+  uint32_t r_bits = 0;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  const float a = __uint_as_float(__reduce_max_sync(kAll, top));
-  const bool finite = a < INFINITY, some = a >= 7.888609052210118e-31f;  // 2^-100
-  const float inv = finite && some ? __fdiv_rn(448.0f, a) : 0.0f;
-  if (lane == 0) *scale = finite ? (some ? __fmul_rn(a, 1.0f / 448.0f) : 0.0f) : __uint_as_float(0x7FC00000u);
-  uint8_t *p = (uint8_t *)base + at;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y[i] = finite ? __fmul_rn(v[4 * h + i], inv) : 0.0f;
-      if (ROOT && y[i] > 0.0f) y[i] = fmaxf(y[i], 0.001953125f);  // 2^-9, the least code
-    }
-    const uint32_t q = to_codes(y[0], y[1]) | to_codes(y[2], y[3]) << 16;
-    if constexpr (VEC) {
-      __stcs((uint32_t *)(p + place<VEC>(lane, 4 * h)), q);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (place<VEC>(lane, 4 * h + i) < left) p[place<VEC>(lane, 4 * h + i)] = (uint8_t)(q >> (8 * i));
-    }
+  for (int i = 0; i < 4; ++i) {
+    const float2 x = each(m[i]), y = each(root[i]);
+    m_top = fmaxf(m_top, fmaxf(fabsf(x.x), fabsf(x.y)));
+    r_bits = max(r_bits, max(__float_as_uint(y.x), __float_as_uint(y.y)));
   }
+  m_top = __uint_as_float(__reduce_max_sync(kAll, __float_as_uint(m_top)));
+  const float r_top = __uint_as_float(__reduce_max_sync(kAll, r_bits));
+  const bool finite = m_top < INFINITY && r_top < INFINITY;
+  constexpr float kNone = 7.888609052210118e-31f;  // 2^-100: below it a block is 0
+  const bool some_m = finite && m_top >= kNone, some_r = finite && r_top >= kNone;
+  if (lane == 0) {
+    const float nan = __uint_as_float(0x7FC00000u);
+    t.scale_m[block] = !finite ? nan : some_m ? m_top * (1.0f / 448.0f) : 0.0f;
+    t.scale_v[block] = !finite ? nan : some_r ? r_top * (1.0f / 448.0f) : 0.0f;
+  }
+  const uint64_t at = block * kBlock;
+  // 2^-9 is the least code
+  write_codes<VEC, false>(t.m, at, lane, left, some_m ? 448.0f * inverse(m_top) : 0.0f, 0.0f, m);
+  write_codes<VEC, true>(t.v, at, lane, left, some_r ? 448.0f * inverse(r_top) : 0.0f, some_r ? 0.001953125f : 0.0f, root);
 }
 
 template <bool EIGHT, bool VEC>
 __device__ __forceinline__ void step(const Entry &t, uint64_t block, uint32_t lane, const Scalars &s) {
   const uint64_t at = block * kBlock;
   const uint32_t left = (uint32_t)min(t.count - at, (uint64_t)kBlock);
-  float p[kEach], g[kEach], m[kEach], v[kEach], root[kEach];
+  float p[kEach], g[kEach];
+  uint64_t m[4], v[4], root[4];
   read<VEC>(t.p, at, t.p_type, lane, left, p);
   read<VEC>(t.g, at, t.g_type, lane, left, g);
   if constexpr (EIGHT) {
     read_codes<VEC>(t.m, at, lane, left, t.scale_m[block], m);
-    read_codes<VEC>(t.v, at, lane, left, t.scale_v[block], root);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) v[i] = __fmul_rn(root[i], root[i]);
+    read_codes<VEC>(t.v, at, lane, left, t.scale_v[block], v);
   } else {
-    read<VEC>(t.m, at, NTC_TYPE_FP32, lane, left, m);
-    read<VEC>(t.v, at, NTC_TYPE_FP32, lane, left, v);
-  }
+    float x[kEach], y[kEach];
+    read<VEC>(t.m, at, NTC_TYPE_FP32, lane, left, x);
+    read<VEC>(t.v, at, NTC_TYPE_FP32, lane, left, y);
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    g[i] = __fmul_rn(g[i], s.grad_scale);
-    m[i] = __fadd_rn(__fmul_rn(m[i], s.beta1), __fmul_rn(g[i], s.c1));
-    v[i] = __fadd_rn(__fmul_rn(v[i], s.beta2), __fmul_rn(__fmul_rn(g[i], s.c2), g[i]));
-    root[i] = __fsqrt_rn(v[i]);
-    const float down = __fadd_rn(__fmul_rn(root[i], s.root), s.eps);
-    p[i] = __fsub_rn(__fmul_rn(p[i], s.decay), __fdiv_rn(__fmul_rn(m[i], s.rate), down));
+    for (int i = 0; i < 4; ++i) m[i] = both(x[2 * i], x[2 * i + 1]), v[i] = both(y[2 * i], y[2 * i + 1]);
+  }
+  const uint64_t beta1 = both(s.beta1, s.beta1), c1 = both(s.c1, s.c1), beta2 = both(s.beta2, s.beta2), c2 = both(s.c2, s.c2);
+  const uint64_t decay = both(s.decay, s.decay), rate = both(-s.rate, -s.rate), scale = both(s.grad_scale, s.grad_scale);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint64_t f = mul2(both(g[2 * i], g[2 * i + 1]), scale);
+    m[i] = fma2(m[i], beta1, mul2(f, c1));
+    if constexpr (EIGHT) v[i] = mul2(v[i], v[i]);  // the root was held
+    v[i] = fma2(mul2(f, c2), f, mul2(v[i], beta2));
+    const float2 r = each(v[i]);
+    const float rx = quick_root(r.x), ry = quick_root(r.y);
+    root[i] = both(rx, ry);
+    const uint64_t inv = both(inverse(fmaf(rx, s.root, s.eps)), inverse(fmaf(ry, s.root, s.eps)));
+    const float2 q = each(fma2(both(p[2 * i], p[2 * i + 1]), decay, mul2(mul2(m[i], rate), inv)));
+    p[2 * i] = q.x, p[2 * i + 1] = q.y;
   }
   write<VEC>(t.p, at, t.p_type, lane, left, p);
   if (t.copy) write<VEC>(t.copy, at, t.copy_type, lane, left, p);
   if constexpr (EIGHT) {
     if (!VEC) {  // what is past the end has no part in the block's largest
 #pragma unroll
-      for (int i = 0; i < kEach; ++i)
-        if (place<VEC>(lane, i) >= left) m[i] = root[i] = 0.0f;
+      for (int i = 0; i < 4; ++i) {
+        const bool a = place<VEC>(lane, 2 * i) < left, b = place<VEC>(lane, 2 * i + 1) < left;
+        const float2 x = each(m[i]), y = each(root[i]);
+        m[i] = both(a ? x.x : 0.0f, b ? x.y : 0.0f), root[i] = both(a ? y.x : 0.0f, b ? y.y : 0.0f);
+      }
     }
-    write_codes<VEC, false>(t.m, at, lane, left, t.scale_m + block, m);
-    write_codes<VEC, true>(t.v, at, lane, left, t.scale_v + block, root);
+    write_moments<VEC>(t, block, lane, left, m, root);
   } else {
-    write<VEC>(t.m, at, NTC_TYPE_FP32, lane, left, m);
-    write<VEC>(t.v, at, NTC_TYPE_FP32, lane, left, v);
+    float x[kEach], y[kEach];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 a = each(m[i]), b = each(v[i]);
+      x[2 * i] = a.x, x[2 * i + 1] = a.y, y[2 * i] = b.x, y[2 * i + 1] = b.y;
+    }
+    write<VEC>(t.m, at, NTC_TYPE_FP32, lane, left, x);
+    write<VEC>(t.v, at, NTC_TYPE_FP32, lane, left, y);
   }
 }
 
+// The next block's lines come to L2 while this one is computed.  With moments in 8 bits a
+// warp has 2 KB in flight at a time and computes half of its time; its registers hold no
+// more (129 million parameters: 318 us, 357 without this; through a ring in shared memory
+// 387 to 417).
+__device__ __forceinline__ void ask_ahead(const Entry &t, uint64_t block, uint32_t lane) {
+  const uint64_t at = block * kBlock;
+  const uint32_t ps = t.p_type == NTC_TYPE_FP32 ? 4 : 2, gs = t.g_type == NTC_TYPE_FP32 ? 4 : 2;
+  const uint8_t *line = lane < 8    ? (const uint8_t *)t.p + (at + lane * 32) * ps
+                        : lane < 16 ? (const uint8_t *)t.g + (at + (lane - 8) * 32) * gs
+                        : lane < 18 ? (const uint8_t *)t.m + at + (lane - 16) * 128
+                                    : (const uint8_t *)t.v + at + (lane - 18) * 128;
+  if (lane < 20) asm volatile("prefetch.global.L2 [%0];" ::"l"(line));
+}
+
 template <bool EIGHT, int CAP>
-__global__ void __launch_bounds__(kThreads, 4) k_adamw(const __grid_constant__ Args<CAP> a) {
-  const uint32_t lane = threadIdx.x & 31;
-  const uint64_t turns = (a.blocks + a.turn - 1) / a.turn;
+__global__ void __launch_bounds__(kThreads, kCtas) k_adamw(const __grid_constant__ Args<CAP> a) {
+  const uint32_t lane = threadIdx.x & 31, warps = gridDim.x * (kThreads / 32);
   pdl_wait();
   pdl_trigger();
   Scalars s = a.s;
   if (s.derived) s.decay = s.derived[0], s.rate = s.derived[1], s.root = s.derived[2], s.grad_scale = s.derived[3];
-  for (uint64_t u = (uint64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32; u < turns;
-       u += (uint64_t)gridDim.x * (kThreads / 32)) {
-    const uint32_t from = (uint32_t)(u * a.turn), to = (uint32_t)min((uint64_t)from + a.turn, (uint64_t)a.blocks);
-    uint32_t i = 0;  // the last tensor that begins at or before `from`
+  for (uint32_t u = blockIdx.x * (kThreads / 32) + threadIdx.x / 32; u < a.turns; u += warps) {
+    uint32_t i = 0;  // the last tensor whose turns begin at or before u
     for (uint32_t n = a.tensors; n > 1;) {
       const uint32_t h = n / 2;
-      if (a.t[i + h].first <= from) i += h;
+      if (a.t[i + h].first <= u) i += h;
       n -= h;
     }
-    for (uint32_t b = from; b < to; ++b) {
-      while (i + 1 < a.tensors && a.t[i + 1].first <= b) ++i;
-      const Entry &t = a.t[i];
-      const uint64_t block = b - t.first;
-      if (t.vec && (block + 1) * kBlock <= t.count) step<EIGHT, true>(t, block, lane, s);
-      else step<EIGHT, false>(t, block, lane, s);
+    const Entry &t = a.t[i];
+    const uint64_t from = (uint64_t)(u - t.first) * a.turn, all = (t.count + kBlock - 1) / kBlock;
+    const uint64_t to = min(from + a.turn, all), whole = t.vec ? min(to, t.count / kBlock) : from;
+    uint64_t b = from;
+    for (; b < whole; ++b) {
+      if (EIGHT && b + 1 < whole) ask_ahead(t, b + 1, lane);
+      step<EIGHT, true>(t, b, lane, s);
     }
+    for (; b < to; ++b) step<EIGHT, false>(t, b, lane, s);
   }
 }
 
@@ -335,21 +385,22 @@ template <int CAP>
 cudaError_t launch(const Scalars &s, bool eight, const ntc_adamw_tensor *t, size_t n, cudaStream_t st) {
   Args<CAP> a;
   a.s = s;
-  a.tensors = a.blocks = 0;
-  const auto at16 = [](const void *p) { return ((uintptr_t)p & 15) == 0; };
+  a.tensors = a.turns = 0;
+  const uint32_t warps = (uint32_t)sm_count() * kCtas * (kThreads / 32);
+  uint64_t blocks = 0;
+  for (size_t i = 0; i < n; ++i) blocks += (t[i].count + kBlock - 1) / kBlock;
+  a.turn = (uint32_t)std::min<uint64_t>(eight ? kTurn8 : kTurn32, std::max<uint64_t>(1, blocks / warps / 4));
+  const auto at32 = [](const void *p) { return ((uintptr_t)p & 31) == 0; };
   for (size_t i = 0; i < n; ++i) {
     if (t[i].count == 0) continue;
     Entry &e = a.t[a.tensors++];
-    e = {t[i].param, t[i].grad, t[i].m, t[i].v, t[i].scale_m, t[i].scale_v, t[i].copy, t[i].count, a.blocks,
+    e = {t[i].param, t[i].grad, t[i].m, t[i].v, t[i].scale_m, t[i].scale_v, t[i].copy, t[i].count, a.turns,
          (uint8_t)t[i].param_type, (uint8_t)t[i].grad_type, (uint8_t)t[i].copy_type,
-         at16(t[i].param) && at16(t[i].grad) && at16(t[i].m) && at16(t[i].v) && at16(t[i].copy)};
-    a.blocks += (uint32_t)((t[i].count + kBlock - 1) / kBlock);
+         at32(t[i].param) && at32(t[i].grad) && at32(t[i].m) && at32(t[i].v) && at32(t[i].copy)};
+    a.turns += (uint32_t)(((t[i].count + kBlock - 1) / kBlock + a.turn - 1) / a.turn);
   }
   if (a.tensors == 0) return cudaSuccess;
-  const uint32_t warps = (uint32_t)sm_count() * 4 * (kThreads / 32);
-  a.turn = std::min(4u, std::max(1u, a.blocks / warps));
-  const uint32_t turns = (a.blocks + a.turn - 1) / a.turn;
-  const unsigned grid = std::min((turns + kThreads / 32 - 1) / (kThreads / 32), (uint32_t)sm_count() * 4);
+  const unsigned grid = std::min((a.turns + kThreads / 32 - 1) / (kThreads / 32), (uint32_t)sm_count() * kCtas);
   return launch_pdl(eight ? k_adamw<true, CAP> : k_adamw<false, CAP>, grid, kThreads, 0, st, a);
 }
 

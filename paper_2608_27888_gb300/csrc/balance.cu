@@ -95,26 +95,31 @@ struct Scores {
   // exp is 0 and nothing overflows.  A token far outside of what that allows, or whose
   // sigmoids are all small, makes its warp take the careful form.
   __device__ __forceinline__ float scores(bool softmax, float m, float (&p)[V], float (&slope)[V]) const {
-    float sum = 0.0f;
     if (__any_sync(kAll, softmax ? !(fabsf(m) < 8e37f) : !(m >= 0.0f && m < 8e37f))) return careful(softmax, m, p, slope);
-    if (softmax) {
+    const uint64_t log2e = both(1.44269504f, 1.44269504f), ln2 = both(-0.693147182f, -0.693147182f);
+    const uint64_t one = both(1.0f, 1.0f), minus_m = both(-m, -m);
+    uint64_t sums = 0;
 #pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float x = fmaxf(l[i], -8.5e37f) - m, t = x * 1.44269504f, e = quick_exp2(t);
-        p[i] = fmaf(e, fmaf(t, -0.693147182f, x), e);
-        sum += p[i];
+    for (int i = 0; i < V; i += 2) {
+      // a sigmoid's x is -l: at 88 and above 1 / (1 + exp(x)) is below the smallest normal number, and 0
+      const uint64_t x = softmax ? add2(both(fmaxf(l[i], -8.5e37f), fmaxf(l[i + 1], -8.5e37f)), minus_m)
+                                 : both(fminf(-l[i], 88.0f), fminf(-l[i + 1], 88.0f));
+      const uint64_t t = mul2(x, log2e);
+      const float2 u = each(t);
+      const uint64_t q = both(quick_exp2(u.x), quick_exp2(u.y)), e = fma2(q, fma2(t, ln2, x), q);
+      uint64_t r = e;
+      if (!softmax) {
+        const float2 d = each(add2(one, e));
+        r = both(quick_inverse(d.x), quick_inverse(d.y));
+        const float2 s = each(mul2(e, r));
+        slope[i] = s.x, slope[i + 1] = s.y;
       }
-    } else {
-      // at -88 and below 1 / (1 + exp(-l)) is below the smallest normal number, and 0
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const float x = fmaxf(l[i], -88.0f), t = x * -1.44269504f, q = quick_exp2(t), e = fmaf(q, fmaf(t, -0.693147182f, -x), q);
-        p[i] = quick_inverse(1.0f + e);
-        slope[i] = e * p[i];
-        sum += p[i];
-      }
+      const float2 f = each(r);
+      p[i] = f.x, p[i + 1] = f.y;
+      sums = i ? add2(sums, r) : r;
     }
-    return group_sum<G>(sum);
+    const float2 halves = each(sums);
+    return group_sum<G>(halves.x + halves.y);
   }
   // Any logits.  A sigmoid is taken times exp(-c), c = min(m, 0): the sum is not 0, and keeps its digits,
   // wherever the row lies.  For x = l - c and e = exp(-|x|) it is e / (1 + e exp(c)) at x <= 0 and
@@ -209,7 +214,10 @@ __global__ void __launch_bounds__(threads(V))
     const float sum = s.scores(softmax, group_max<G>(s.largest()), p, slope);
     const float by = counts && sum > 0.0f ? quick_inverse(sum) : 0.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) acc[i] = fmaf(p[i], by, acc[i]);
+    for (int i = 0; i < V; i += 2) {
+      const float2 f = each(fma2(both(p[i], p[i + 1]), both(by, by), both(acc[i], acc[i + 1])));
+      acc[i] = f.x, acc[i + 1] = f.y;
+    }
     tokens += counts && sub == 0;
   }
 #pragma unroll

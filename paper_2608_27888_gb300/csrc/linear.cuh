@@ -94,25 +94,33 @@ __device__ __forceinline__ int32_t offset_before(const int32_t *offsets, uint32_
 // *active of them, and *live rows of any.
 __device__ __forceinline__ void list_experts(const LinearArgs &a, uint32_t lane, int32_t *begin, int32_t *count, uint16_t *which,
                                              uint32_t *active, uint32_t *live) {
+  constexpr uint32_t kAtOnce = 4;
   const uint32_t E = a.num_experts;
   uint32_t many = 0;
   int32_t end = 0;
   bool falls = false;  // an offset is above the next: once more, with offset_before
   for (bool again = false;; again = true) {
-    for (uint32_t e0 = 0; e0 < E; e0 += 32) {
-      const uint32_t e = e0 + lane;
-      const int32_t rows = (int32_t)a.num_rows;
-      int32_t b = 0, n = 0;
-      if (e < E) {
-        b = !a.offsets ? 0 : again ? offset_before(a.offsets, e, E, rows) : offset_at(a.offsets, e, rows);
-        end = !a.offsets ? rows : again ? offset_before(a.offsets, e + 1, E, rows) : offset_at(a.offsets, e + 1, rows);
-        n = end - b;
+    const int32_t rows = (int32_t)a.num_rows;
+    for (uint32_t e0 = 0; e0 < E; e0 += 32 * kAtOnce) {
+      // the offsets of several experts a lane are on their way together
+      int32_t b[kAtOnce], n[kAtOnce];
+#pragma unroll
+      for (uint32_t q = 0; q < kAtOnce; ++q) {
+        const uint32_t e = e0 + 32 * q + lane;
+        b[q] = n[q] = 0;
+        if (e < E) {
+          b[q] = !a.offsets ? 0 : again ? offset_before(a.offsets, e, E, rows) : offset_at(a.offsets, e, rows);
+          end = !a.offsets ? rows : again ? offset_before(a.offsets, e + 1, E, rows) : offset_at(a.offsets, e + 1, rows);
+          n[q] = end - b[q];
+        }
+        falls |= n[q] < 0;
       }
-      falls |= n < 0;
-      const uint32_t has = __ballot_sync(0xFFFFFFFFu, n > 0);
-      const uint32_t at = many + __popc(has & ((1u << lane) - 1));
-      if (n > 0) begin[at] = b, count[at] = n, which[at] = (uint16_t)e;
-      many += __popc(has);
+#pragma unroll
+      for (uint32_t q = 0; q < kAtOnce; ++q) {
+        const uint32_t has = __ballot_sync(0xFFFFFFFFu, n[q] > 0), at = many + __popc(has & ((1u << lane) - 1));
+        if (n[q] > 0) begin[at] = b[q], count[at] = n[q], which[at] = (uint16_t)(e0 + 32 * q + lane);
+        many += __popc(has);
+      }
     }
     if (again || !__any_sync(0xFFFFFFFFu, falls)) break;
     many = 0;

@@ -3,20 +3,18 @@
 //   y_i = act(sum over groups s_{n,j} (sum over the group q_nk x_{rows[i],k}) + b) + residual
 //
 // Few rows per expert: the weights' bytes are read once and are the bound, half a byte a
-// weight.  A warp takes 16 rows of the weights.  Chunks of 128 along K (64 bytes a row)
-// come through a ring of its own in shared memory by cp.async, so that their latency costs
-// no registers, and leave it word by word: eight weights of one row, whose numbers q
-// become 16-bit ones exactly.  They are the A operand of mma.sync.m16n8k16; eight rows of x are the B operand.  A word gives the
-// pairs (0, 4), (1, 5), (2, 6), (3, 7) of its weights without a shuffle; x's pairs are made
-// to match, for an MMA's k order is free as long as both operands agree.  A group's sum is
-// scaled in fp32, so that no product of a scale and a weight is rounded.
-// Few (expert, 16 rows) pairs are split along K over the warps of a CTA, whose sums meet
+// weight.  A warp takes 16 or 32 rows of the weights and 128 of K at a time, straight into
+// registers a turn ahead.  A word has eight weights of one row, whose numbers q become
+// 16-bit ones exactly.  They are the A operand of mma.sync.m16n8k16; eight rows of x are the
+// B operand.  A word gives the pairs (0, 4), (1, 5), (2, 6), (3, 7) of its weights without a
+// shuffle; x's pairs are made to match, for an MMA's k order is free as long as both operands
+// agree.  A group's sum is scaled in fp32, so that no product of a scale and a weight is
+// rounded.
+// Few (expert, rows) pairs are split along K over the warps of a CTA, whose sums meet
 // in shared memory in a fixed order.
 // Many rows per expert: the weights of experts with rows are unpacked to 16 bits and the
 // product of linear.cu takes them.
 #include "pack4.cuh"
-
-#include <atomic>
 
 using namespace ntc;
 
@@ -24,46 +22,30 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr uint32_t kChunk = 128;          // K of a stage
-constexpr uint32_t kPitch = 64 + 16;      // bytes from row to row of a stage: the 8 rows of a load meet 8 sets of banks
-constexpr int kStages = 4;
-constexpr uint32_t kStageBytes = 16 * kPitch;
-constexpr uint32_t kRingBytes = kWarps * kStages * kStageBytes;
+constexpr uint32_t kChunk = 128;  // K of a turn: 64 bytes of each row of weights
 
 struct FewArgs {
   LinearArgs a;
   const uint8_t *packed;
   const uint16_t *scales;
   uint64_t ld_packed, stride_packed, ld_scales, stride_scales;
-  uint32_t group, groups;
+  uint32_t groups;
   uint32_t split;  // warps along K: 1, 2, 4 or 8
-  uint32_t vec_w;  // rows of packed start on 16 bytes
 };
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {  // the rest of the 16 are zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copies_wait() {
-  asm volatile("cp.async.wait_group %0;\n" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ uint32_t lds(uint32_t at) {
-  uint32_t v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(at));
+template <int NT, int MT>
+constexpr int kCtas = NT * MT == 1 ? 3 : 2;  // on an SM: what registers leave
+
+// Four bytes from p on, `have` of them inside the row, then zeros.
+__device__ __forceinline__ uint32_t load_bytes(const uint8_t *p, int32_t have) {
+  uint32_t v = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (i < have) v |= (uint32_t)p[i] << (8 * i);
   return v;
 }
 
-// `bytes` bytes from src on, and zeros: 16 bytes to shared memory, from any address.
-__device__ __noinline__ void copy_bytes(uint32_t dst, const uint8_t *src, uint32_t bytes) {
-  uint32_t v[4] = {};
-#pragma unroll
-  for (uint32_t i = 0; i < 16; ++i)
-    if (i < bytes) v[i / 4] |= (uint32_t)src[i] << (8 * (i & 3));
-  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
-}
-
-// A row of x: eight elements from k on (zeros past K).  VEC: K and the rows' starts are whole pieces.
+// A row of x: eight elements from k on, zeros past K.
 template <bool VEC>
 __device__ __forceinline__ uint4 load_x(const uint16_t *row, uint32_t k, uint32_t K) {
   if constexpr (VEC) {
@@ -77,18 +59,38 @@ __device__ __forceinline__ uint4 load_x(const uint16_t *row, uint32_t k, uint32_
   }
 }
 
-// NT: blocks of eight rows of x that a warp takes at a time.  `split` warps are a team,
-// which takes its units by itself.
-template <typename T, int NT, bool VEC, int GROUP>
-__global__ void __launch_bounds__(kThreads, NT == 4 ? 2 : 3) k_linear4_few(const FewArgs f) {
-  extern __shared__ __align__(16) uint8_t ring[];
-  constexpr int kScales = kChunk / GROUP;  // of a row in a chunk
+// The first MMA of a group has no sum to add to.
+template <typename T>
+__device__ __forceinline__ void mma_or_first(bool first, float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (!first) {
+    mma<T>(c, a0, a1, a2, a3, b0, b1);
+  } else if constexpr (std::is_same<T, __half>::value) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+  } else {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};\n"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+  }
+}
+
+// NT: blocks of eight rows of x that a warp takes at a time; MT: blocks of 16 rows of
+// weights, which share x's operands.  `split` warps are a team, which takes its units by
+// itself.
+// VEC: the rows of x start on 16 bytes, those of weights and scales on what a lane loads at
+// once, and K is a multiple of 32; else all is loaded element by element.
+// A lane's four words of a row's chunk are of GROUP / 32 at a time, so that the four lanes
+// of a row (an MMA's k) are in one group: it loads 16, 8 or 4 bytes at once.
+template <typename T, int NT, int MT, bool VEC, int GROUP>
+__global__ void __launch_bounds__(kThreads, kCtas<NT, MT>) k_linear4_few(const FewArgs f) {
+  constexpr int kScales = kChunk / GROUP, kSteps = GROUP / 32;  // groups of a chunk, words of a group
   const LinearArgs &a = f.a;
   __shared__ int32_t begin[NTC_MAX_EXPERTS];   // of the experts with rows: first row,
   __shared__ int32_t count[NTC_MAX_EXPERTS];   // rows,
   __shared__ uint16_t which[NTC_MAX_EXPERTS];  // and number
   __shared__ uint32_t active, live;
-  __shared__ float part[kWarps][8 * NT][17];  // sums of x's rows times 16 rows of weights
+  __shared__ float part[kWarps][8 * NT][MT * 16 + 1];  // sums of x's rows times the weights'
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, t = lane & 3;
   const uint32_t K = a.depth, N = a.width, split = f.split;
   pdl_wait();
@@ -101,134 +103,206 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 2 : 3) k_linear4_few(const
     if (split == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(split * 32) : "memory");
   };
-  const uint32_t per = (N + 15) / 16;
+  const uint32_t per = (N + MT * 16 - 1) / (MT * 16);
   const uint32_t chunks = (K + kChunk - 1) / kChunk, run = (chunks + split - 1) / split;
   const uint32_t c_from = min(slice * run, chunks), c_to = min(c_from + run, chunks);
   const int32_t row_bytes = (int32_t)(K + 1) / 2;
-  const uint32_t mine = (uint32_t)__cvta_generic_to_shared(ring) + warp * kStages * kStageBytes, last = mine + kStages * kStageBytes;
-  const uint32_t to_stage = g * kPitch + t * 16, from_stage = g * kPitch + t * 4;
   for (uint32_t u = blockIdx.x * teams + team; u < active * per; u += gridDim.x * teams) {
-    const uint32_t i = u / per, n0 = (u - i * per) * 16;
+    const uint32_t i = u / per, n0 = (u - i * per) * (MT * 16);
     const uint32_t e = which[i];
-    const bool in0 = n0 + g < N, in1 = n0 + g + 8 < N;
-    // The lane's two pieces of 16 bytes of a chunk: rows g and g + 8, bytes t * 16 on
-    const uint8_t *w0 = f.packed + e * f.stride_packed + (uint64_t)(in0 ? n0 + g : 0) * f.ld_packed + c_from * 64 + t * 16;
-    const uint8_t *w1 = in1 ? w0 + 8 * f.ld_packed : w0;
-    const int32_t left = row_bytes - (int32_t)(c_from * 64 + t * 16);
-    const T *s0 = (const T *)f.scales + e * f.stride_scales + (uint64_t)(in0 ? n0 + g : 0) * f.ld_scales + c_from * kScales;
-    const T *s1 = in1 ? s0 + 8 * f.ld_scales : s0;
+    const uint32_t here = N - n0;  // rows of weights, if fewer than the unit's
+    const uint8_t *w0 = f.packed + e * f.stride_packed + (uint64_t)n0 * f.ld_packed + t * (GROUP / 8);
+    const T *s0 = (const T *)f.scales + e * f.stride_scales + (uint64_t)n0 * f.ld_scales;
+    // The lane's rows of weights: g, g + 8, ... of the unit, the first one where there is none (nobody looks at its sums)
+    uint32_t w_row[2 * MT], s_row[2 * MT];  // 32 rows' strides fit 32 bits: the call sees to it
+#pragma unroll
+    for (int r = 0; r < 2 * MT; ++r) {
+      const uint32_t n = g + 8 * r < here ? g + 8 * r : 0;
+      w_row[r] = n * (uint32_t)f.ld_packed, s_row[r] = n * (uint32_t)f.ld_scales;
+    }
     for (int32_t m0 = 0; m0 < count[i]; m0 += 8 * NT) {
       const int32_t rows = min(count[i] - m0, 8 * NT);
-      team_sync();  // nobody reads the ring's last chunks or the sums any more
-      uint32_t fetched = c_from, to = mine + to_stage;
-      const uint8_t *p0 = w0, *p1 = w1;
-      int32_t have = left;
-      const auto fetch = [&] {
-        if (fetched < c_to) {
-          const uint32_t n = (uint32_t)min(max(have, 0), 16), n0_ = in0 ? n : 0, n1_ = in1 ? n : 0;
-          if (f.vec_w) {
-            copy16(to, n ? p0 : w0, n0_);
-            copy16(to + 8 * kPitch, n ? p1 : w1, n1_);
-          } else {
-            copy_bytes(to, p0, n0_);
-            copy_bytes(to + 8 * kPitch, p1, n1_);
+      // A chunk's words of the lane's rows, and their scales two to a word
+      uint32_t word[2 * MT][4], scale[2 * MT][(kScales + 1) / 2];
+      // (full: the row goes on past the chunk's end)
+      const auto fetch = [&](uint32_t c, auto full) {
+        constexpr bool kFull = decltype(full)::value;
+#pragma unroll
+        for (int r = 0; r < 2 * MT; ++r) {
+          const uint8_t *p = w0 + w_row[r] + c * 64;
+          const T *s = s0 + s_row[r] + c * kScales;
+          const int32_t left = row_bytes - (int32_t)(c * 64 + t * (GROUP / 8));
+#pragma unroll
+          for (int l = 0; l < kScales; ++l) {
+            uint32_t *to = word[r] + l * kSteps;
+            if constexpr (VEC) {
+              if (!kFull) {
+#pragma unroll
+                for (int j = 0; j < kSteps; ++j) to[j] = 0;
+              }
+              if (kFull || left > l * (GROUP / 2)) {
+                if constexpr (kSteps == 4) {
+                  const uint4 q = __ldcs((const uint4 *)p);
+                  to[0] = q.x, to[1] = q.y, to[2] = q.z, to[3] = q.w;
+                } else if constexpr (kSteps == 2) {
+                  const uint2 q = __ldcs((const uint2 *)(p + l * (GROUP / 2)));
+                  to[0] = q.x, to[1] = q.y;
+                } else {
+                  to[0] = *(const uint32_t *)(p + l * (GROUP / 2));
+                }
+              }
+            } else {
+#pragma unroll
+              for (int j = 0; j < kSteps; ++j) to[j] = load_bytes(p + l * (GROUP / 2) + j * 4, left - l * (GROUP / 2) - j * 4);
+            }
           }
-          p0 += 64, p1 += 64, have -= 64, ++fetched;
-          to = to + kStageBytes >= last ? to + kStageBytes - kStages * kStageBytes : to + kStageBytes;
+          if constexpr (VEC && kFull && kScales == 4) {
+            const uint2 q = *(const uint2 *)s;
+            scale[r][0] = q.x, scale[r][(kScales - 1) / 2] = q.y;
+          } else if constexpr (VEC && kFull && kScales == 2) {
+            scale[r][0] = *(const uint32_t *)s;
+          } else {
+#pragma unroll
+            for (int l = 0; l < kScales; ++l) {
+              const uint32_t v = c * kScales + l < f.groups ? *(const uint16_t *)(s + l) : 0u;
+              scale[r][l / 2] = l & 1 ? scale[r][l / 2] | v << 16 : v;
+            }
+          }
         }
-        copies_commit();
       };
-#pragma unroll 1
-      for (int c = 0; c < kStages - 1; ++c) fetch();
+      if (c_from < c_to) fetch(c_from, std::false_type{});
+      // Columns of the MMAs that are no row read some row: nobody looks at their sums.  A row that is named but not
+      // there is zeros (`none`).
       const uint16_t *x[NT];
-      uint32_t end[NT];  // K, or 0 where there is no row
 #pragma unroll
       for (int h = 0; h < NT; ++h) {
-        const int32_t r = (int32_t)g + 8 * h;
-        int32_t at = -1;
-        if (r < rows) at = a.rows ? (int32_t)ld_word((const uint32_t *)a.rows + begin[i] + m0 + r) : begin[i] + m0 + r;
-        end[h] = (uint32_t)at < a.x_rows ? K : 0;
-        x[h] = (const uint16_t *)a.x + (end[h] ? (uint64_t)(uint32_t)at * a.ld_x : 0);
+        const int32_t r = min((int32_t)g + 8 * h, rows - 1) + begin[i] + m0;
+        const uint32_t at = a.rows ? ld_word((const uint32_t *)a.rows + r) : (uint32_t)r;
+        x[h] = (const uint16_t *)a.x + (at < a.x_rows ? at * a.ld_x : 0);
       }
-      float sum[NT][4] = {}, of_group[NT][4] = {};
-      T next[2][kScales];
-      uint32_t at_scale = 0;
-      const auto scale_of = [&](uint32_t c) {
+      // K of the lane's word j of chunk c
+      const auto k_of = [&](uint32_t c, int j) { return c * kChunk + j / kSteps * GROUP + t * (GROUP / 4) + j % kSteps * 8; };
+      float sum[MT][NT][4] = {}, of_group[MT][NT][4];
+      uint4 ahead[NT];
 #pragma unroll
-        for (int j = 0; j < kScales; ++j) {
-          const bool is = c < c_to && (kScales == 1 || c * kScales + j < f.groups);
-          next[0][j] = is ? s0[at_scale + j] : from_f<T>(0.0f);
-          next[1][j] = is ? s1[at_scale + j] : from_f<T>(0.0f);
+      for (int h = 0; h < NT; ++h) ahead[h] = load_x<VEC>(x[h], k_of(c_from, 0), K);
+      // A chunk; `full`: x goes on for the whole of the next one.
+      const auto chunk = [&](uint32_t c, auto full) {
+        uint32_t now[2 * MT][4], s[2 * MT][(kScales + 1) / 2];
+#pragma unroll
+        for (int r = 0; r < 2 * MT; ++r) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) now[r][j] = word[r][j];
+#pragma unroll
+          for (int j = 0; j < (kScales + 1) / 2; ++j) s[r][j] = scale[r][j];
         }
-        at_scale += kScales;
-      };
-      scale_of(c_from);
-      uint4 q[NT], ahead[NT];
-      uint32_t k = c_from * kChunk + t * 8, stage = mine + from_stage;
-#pragma unroll
-      for (int h = 0; h < NT; ++h) ahead[h] = load_x<VEC>(x[h], k, end[h]);
-#pragma unroll 1
-      for (uint32_t c = c_from; c < c_to; ++c) {
-        float scale[2][kScales];
-#pragma unroll
-        for (int j = 0; j < kScales; ++j) scale[0][j] = to_f<T>(next[0][j]), scale[1][j] = to_f<T>(next[1][j]);
-        scale_of(c + 1);
-        copies_wait<kStages - 2>();
-        __syncwarp();
-        fetch();
+        if (c + 1 < c_to) fetch(c + 1, full);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          k += 32;
+          const uint32_t k = j < 3 ? k_of(c, j + 1) : k_of(c + 1, 0);
+          uint32_t b[NT][4];
 #pragma unroll
           for (int h = 0; h < NT; ++h) {
-            q[h] = ahead[h];
-            ahead[h] = load_x<VEC>(x[h], k, end[h]);
+            const uint4 q = ahead[h];
+            ahead[h] = decltype(full)::value ? *reinterpret_cast<const uint4 *>(x[h] + k) : load_x<VEC>(x[h], k, K);
+            b[h][0] = __byte_perm(q.x, q.z, 0x5410), b[h][1] = __byte_perm(q.x, q.z, 0x7632);
+            b[h][2] = __byte_perm(q.y, q.w, 0x5410), b[h][3] = __byte_perm(q.y, q.w, 0x7632);
           }
-          uint32_t lo[4], hi[4];
-          numbers4<T>(lds(stage + j * 16), lo);
-          numbers4<T>(lds(stage + 8 * kPitch + j * 16), hi);
 #pragma unroll
-          for (int h = 0; h < NT; ++h) {
-            const uint4 &v = q[h];
-            mma<T>(of_group[h], lo[0], hi[0], lo[1], hi[1], __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632));
-            mma<T>(of_group[h], lo[2], hi[2], lo[3], hi[3], __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-          }
-          if ((j + 1) % (GROUP / 32) == 0) {
+          for (int m = 0; m < MT; ++m) {
+            uint32_t lo[4], hi[4];
+            numbers4<T>(now[2 * m][j], lo);
+            numbers4<T>(now[2 * m + 1][j], hi);
 #pragma unroll
             for (int h = 0; h < NT; ++h) {
+                mma_or_first<T>(j % kSteps == 0, of_group[m][h], lo[0], hi[0], lo[1], hi[1], b[h][0], b[h][1]);
+              mma<T>(of_group[m][h], lo[2], hi[2], lo[3], hi[3], b[h][2], b[h][3]);
+              if ((j + 1) % kSteps == 0) {
+                const int l = j / kSteps;
+                float by[2];
 #pragma unroll
-              for (int r = 0; r < 4; ++r) {
-                sum[h][r] = fmaf(scale[r >> 1][j / (GROUP / 32)], of_group[h][r], sum[h][r]);
-                of_group[h][r] = 0.0f;
+                for (int r = 0; r < 2; ++r) by[r] = l & 1 ? unpack2<T>(s[2 * m + r][l / 2]).y : unpack2<T>(s[2 * m + r][l / 2]).x;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[m][h][r] = fmaf(by[r >> 1], of_group[m][h][r], sum[m][h][r]);
               }
             }
           }
         }
-        stage = stage + kStageBytes >= last ? stage + kStageBytes - kStages * kStageBytes : stage + kStageBytes;
+      };
+      uint32_t c = c_from;
+      if constexpr (VEC) {
+#pragma unroll 1
+        for (; c < c_to && (c + 2) * kChunk <= K; ++c) chunk(c, std::true_type{});
       }
-      copies_wait<0>();
+#pragma unroll 1
+      for (; c < c_to; ++c) chunk(c, std::false_type{});
+      team_sync();  // nobody reads the last sums any more
 #pragma unroll
-      for (int h = 0; h < NT; ++h) {
-        part[warp][8 * h + 2 * t][g] = sum[h][0];
-        part[warp][8 * h + 2 * t + 1][g] = sum[h][1];
-        part[warp][8 * h + 2 * t][g + 8] = sum[h][2];
-        part[warp][8 * h + 2 * t + 1][g + 8] = sum[h][3];
-      }
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int h = 0; h < NT; ++h)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) part[warp][8 * h + 2 * t + (r & 1)][m * 16 + g + 8 * (r >> 1)] = sum[m][h][r];
       team_sync();
-      // 16 threads write a row's 16 columns
-      const uint32_t n = lane & 15, col = n0 + n;
-      if (col < N) {
+      if constexpr (NT == 1) {
+      // 16 threads write 16 columns of a row
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const uint32_t n = m * 16 + (lane & 15), col = n0 + n;
+        if (col >= N) break;
         const float bias = a.bias ? a.bias[(uint64_t)e * N + col] : 0.0f;
 #pragma unroll 1
         for (int32_t r = slice * 2 + (lane >> 4); r < rows; r += 2 * split) {
-          float v[1] = {0.0f};
-          for (uint32_t p = 0; p < split; ++p) v[0] += part[team * split + p][r][n];
-          v[0] += bias;
-          activate(a.activation, a.slope, v);
           const uint64_t row = (uint64_t)(begin[i] + m0) + r;
+          float v[1] = {0.0f};
+          const bool none = a.rows && ld_word((const uint32_t *)a.rows + row) >= a.x_rows;
+          for (uint32_t p = 0; p < split; ++p) v[0] += part[team * split + p][r][n];
+          v[0] = (none ? 0.0f : v[0]) + bias;
+          activate(a.activation, a.slope, v);
           if (a.residual) v[0] += to_f<T>(((const T *)a.residual)[row * a.ld_residual + col]);
           ((T *)a.out)[row * a.ld_out + col] = from_f<T>(v[0]);
         }
+      }
+      } else {
+      // 16 threads write 16 columns of a row; what they read comes for several rows at a time
+      constexpr int kBatch = 4;
+      const uint32_t by = 2 * split;
+#pragma unroll 1
+      for (uint32_t r0 = slice * 2 + (lane >> 4); r0 < (uint32_t)rows; r0 += kBatch * by) {
+        const uint64_t row0 = (uint64_t)(begin[i] + m0) + r0;
+        float add[MT][kBatch], v[MT * kBatch];
+        bool none[kBatch];
+#pragma unroll
+        for (int q = 0; q < kBatch; ++q) {
+          const bool is = r0 + q * by < (uint32_t)rows;
+          none[q] = is && a.rows && ld_word((const uint32_t *)a.rows + row0 + q * by) >= a.x_rows;
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const uint32_t col = n0 + m * 16 + (lane & 15);
+            add[m][q] = is && a.residual && col < N ? to_f<T>(((const T *)a.residual)[(row0 + q * by) * a.ld_residual + col]) : 0.0f;
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const uint32_t n = m * 16 + (lane & 15), col = n0 + n;
+          const float bias = a.bias && col < N ? a.bias[(uint64_t)e * N + col] : 0.0f;
+#pragma unroll
+          for (int q = 0; q < kBatch; ++q) {
+            float z = 0.0f;
+            if (r0 + q * by < (uint32_t)rows && !none[q])
+              for (uint32_t p = 0; p < split; ++p) z += part[team * split + p][r0 + q * by][n];
+            v[m * kBatch + q] = z + bias;
+          }
+        }
+        activate(a.activation, a.slope, v);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          const uint32_t col = n0 + m * 16 + (lane & 15);
+#pragma unroll
+          for (int q = 0; q < kBatch; ++q)
+            if (r0 + q * by < (uint32_t)rows && col < N) ((T *)a.out)[(row0 + q * by) * a.ld_out + col] = from_f<T>(v[m * kBatch + q] + add[m][q]);
+        }
+      }
       }
     }
   }
@@ -240,20 +314,11 @@ __global__ void __launch_bounds__(kThreads, NT == 4 ? 2 : 3) k_linear4_few(const
   }
 }
 
-template <typename T, int NT, bool VEC, int GROUP>
+template <typename T, int NT, int MT, bool VEC, int GROUP>
 cudaError_t launch(const FewArgs &f, uint64_t units, cudaStream_t st) {
-  static std::atomic<uint64_t> allowed{0};  // devices that know of the kernel's shared memory
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev >= 64 || !((allowed.load() >> dev) & 1)) {
-    e = cudaFuncSetAttribute(k_linear4_few<T, NT, VEC, GROUP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) allowed.fetch_or(1ull << dev);
-  }
   const uint64_t ctas = (units * f.split + kWarps - 1) / kWarps;
-  const unsigned grid = (unsigned)std::min<uint64_t>(ctas, (uint64_t)sm_count() * (NT == 4 ? 2 : 3));
-  return launch_pdl(k_linear4_few<T, NT, VEC, GROUP>, grid, kThreads, kRingBytes, st, f);
+  const unsigned grid = (unsigned)std::min<uint64_t>(ctas, (uint64_t)sm_count() * kCtas<NT, MT>);
+  return launch_pdl(k_linear4_few<T, NT, MT, VEC, GROUP>, grid, kThreads, 0, st, f);
 }
 
 // Rows of an expert that has any, on average, where the choices are spread evenly.
@@ -276,6 +341,8 @@ ntc_status check(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, ntc
   d->ld_z = d->out_dim;
   if (ntc_status s = check_linear(d)) return s;
   if (ntc_status s = check_pack4(weights)) return s;
+  if (weights->ld_packed >> 26 || weights->ld_scales >> 26)
+    return op_fail(NTC_ERR_UNSUPPORTED, "ld_packed and ld_scales must be below 2^26");
   if (weights->type != d->type || weights->in_dim != d->in_dim || weights->out_dim != d->out_dim ||
       weights->num_experts != d->num_experts)
     return op_fail(NTC_ERR_INVALID_ARG, "the weights' type, in_dim, out_dim or num_experts is not the layer's");
@@ -340,28 +407,35 @@ extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc
   f.stride_packed = p.stride_packed;
   f.ld_scales = p.ld_scales;
   f.stride_scales = p.stride_scales;
-  f.group = p.group;
   f.groups = (d.in_dim + p.group - 1) / p.group;
-  f.vec_w = ((uintptr_t)packed & 15) == 0 && p.ld_packed % 16 == 0 && (d.num_experts == 1 || p.stride_packed % 16 == 0);
-  const bool vec_x = d.in_dim % 8 == 0 && rows_are_vec(x, d.ld_x, 2);
+  const auto starts_on = [&](const void *p, uint64_t bytes, uint64_t ld, uint64_t stride) {
+    return (uintptr_t)p % bytes == 0 && ld % bytes == 0 && (d.num_experts == 1 || stride % bytes == 0);
+  };
+  const bool vec = d.in_dim % 32 == 0 && rows_are_vec(x, d.ld_x, 2) && starts_on(packed, p.group / 8, p.ld_packed, p.stride_packed) &&
+                   starts_on(scales, 2 * kChunk / p.group, p.ld_scales * 2, p.stride_scales * 2);
+  const uint64_t mean = mean_rows(d), experts = std::min<uint64_t>(d.num_experts, d.num_rows);
+  // Rows of x and of weights that a warp takes together: experts of a few rows are left with several turns of eight
+  // rows where one has many, which costs less than sixteen columns of MMAs for all.  Two blocks of weights pay where x is
+  // read for two (128 tokens of 4 of 32 experts, 1,024 -> 2,048: 35 us, 47 with one), and spill registers beside four.
+  const int nt = d.num_rows <= 8 || mean <= 4 ? 1 : mean <= 16 ? 2 : 4, mt = nt == 2 ? 2 : 1;
+  const uint64_t units = experts * ((d.out_dim + 16 * mt - 1) / (16 * mt));
   // Warps along K until the warps that the SMs hold are at work.
-  const uint64_t experts = std::min<uint64_t>(d.num_experts, d.num_rows), units = experts * ((d.out_dim + 15) / 16);
   f.split = 1;
-  while (f.split < 8 && units * f.split < 16ull * sm_count() && d.in_dim > f.split * kChunk) f.split *= 2;
-  const uint64_t mean = mean_rows(d);
-  const int nt = d.num_rows <= 8 || mean <= 4 ? 1 : d.num_rows <= 16 || mean <= 10 ? 2 : 4;
+  while (f.split < 8 && units * f.split < 24ull * sm_count() && d.in_dim > f.split * kChunk) f.split *= 2;
   using std::integral_constant;
   const auto by_rows = [&](auto type, auto vec, auto group) {
     using T = decltype(type);
     constexpr bool V = decltype(vec)::value;
     constexpr int G = decltype(group)::value;
-    return nt == 1 ? launch<T, 1, V, G>(f, units, st) : nt == 2 ? launch<T, 2, V, G>(f, units, st) : launch<T, 4, V, G>(f, units, st);
+    return nt == 1   ? launch<T, 1, 1, V, G>(f, units, st)
+           : nt == 2 ? launch<T, 2, 2, V, G>(f, units, st)
+                     : launch<T, 4, 1, V, G>(f, units, st);
   };
   const auto by_group = [&](auto type, auto vec) {
     return p.group == 32   ? by_rows(type, vec, integral_constant<int, 32>{})
            : p.group == 64 ? by_rows(type, vec, integral_constant<int, 64>{})
                            : by_rows(type, vec, integral_constant<int, 128>{});
   };
-  const auto go = [&](auto type) { return vec_x ? by_group(type, std::true_type{}) : by_group(type, std::false_type{}); };
+  const auto go = [&](auto type) { return vec ? by_group(type, std::true_type{}) : by_group(type, std::false_type{}); };
   return op_cuda(bf16 ? go(__nv_bfloat16()) : go(__half()), "ntc_linear4");
 }

@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_linear_few(const FewArgs f) {
   __shared__ uint32_t active, live;
   __shared__ float part[kWarps][16][kTokens + 1];  // sums of W's 16 rows times x's
   const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x / 32, g = lane >> 2, t = lane & 3;
-  const uint32_t E = a.num_experts, K = a.depth, N = a.width, split = f.split;
+  const uint32_t K = a.depth, N = a.width, split = f.split;
   pdl_wait();
   pdl_trigger();
   if (warp == 0) list_experts(a, lane, begin, count, which, &active, &live);

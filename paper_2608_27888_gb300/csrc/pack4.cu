@@ -15,26 +15,31 @@ namespace {
 constexpr int kThreads = 256;
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
-// How an expert's rows (blockIdx.y is the expert) go to warps: `lanes` lanes to a row of
-// `pieces` turns.  A warp divides once and then counts.
+// How an expert's rows (blockIdx.y is the expert) go to warps: `lanes` lanes to a row, which
+// has `pieces` pieces of lanes * 8 weights; a warp takes up to kRun of them at a time, all of
+// whose loads it starts first.
+constexpr uint32_t kRun = 4;
 struct Turns {
-  uint32_t lanes, pieces, rows;  // rows of a warp at a time, over all of them: ceil(N / (32 / lanes))
+  uint32_t lanes, lanes_log, pieces, run, runs;  // run: pieces of a turn; runs: turns of a row
+  uint32_t rows;                            // of a warp at a time, over all of them: ceil(N / (32 / lanes))
 };
+// A warp's next turn: it divides once and then counts.
 struct Walk {
-  uint32_t piece, rows, by_piece, by_rows;
+  uint32_t run, rows, by_run, by_rows;
   __device__ __forceinline__ explicit Walk(const Turns &t) {
     const uint32_t first = blockIdx.x * (kThreads / 32) + threadIdx.x / 32, by = gridDim.x * (kThreads / 32);
-    rows = first / t.pieces, piece = first - rows * t.pieces;
-    by_rows = by / t.pieces, by_piece = by - by_rows * t.pieces;
+    rows = first / t.runs, run = first - rows * t.runs;
+    by_rows = by / t.runs, by_run = by - by_rows * t.runs;
   }
   __device__ __forceinline__ void next(const Turns &t) {
-    piece += by_piece, rows += by_rows;
-    if (piece >= t.pieces) piece -= t.pieces, ++rows;
+    run += by_run, rows += by_rows;
+    if (run >= t.runs) run -= t.runs, ++rows;
   }
-  // The lane's row and the first of its weights.
-  __device__ __forceinline__ void place(const Turns &t, uint32_t lane, uint32_t &n, uint32_t &k) const {
-    n = rows * (32 / t.lanes) + lane / t.lanes;
-    k = (piece * t.lanes + (lane & (t.lanes - 1))) * 8;
+  // The lane's row and the first of its weights, and the pieces of the turn.
+  __device__ __forceinline__ void place(const Turns &t, uint32_t lane, uint32_t &n, uint32_t &k, uint32_t &many) const {
+    n = (rows << (5 - t.lanes_log)) + (lane >> t.lanes_log);
+    k = (((run * t.run) << t.lanes_log) + (lane & (t.lanes - 1))) * 8;
+    many = min(t.run, t.pieces - run * t.run);
   }
 };
 
@@ -48,104 +53,136 @@ struct Pack4 {
 
 // Two quotients w / s, correctly rounded to fp32: the product with an approximate 1 / s,
 // put right by its remainder, which one fused operation gives exactly.
-__device__ __forceinline__ float2 quotients(float2 w, float s, float inv) {
-  uint64_t x, i, m, q, r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(w.x), "f"(w.y));
-  asm("mov.b64 %0, {%1, %1};" : "=l"(i) : "f"(inv));
-  asm("mov.b64 %0, {%1, %1};" : "=l"(m) : "f"(-s));
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(q) : "l"(x), "l"(i));
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(q), "l"(m), "l"(x));
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(q) : "l"(r), "l"(i), "l"(q));
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(w.x), "=f"(w.y) : "l"(q));
-  return w;
+__device__ __forceinline__ uint64_t quotients(uint64_t w, float s, float inv) {
+  const uint64_t i = both(inv, inv), q = mul2(w, i);
+  return fma2(fma2(q, both(-s, -s), w), i, q);
 }
-// q + 8 of a quotient in the low four bits: rounded to nearest even by 1.5 * 2^23.  Quotients
-// of 16-bit numbers are no nearer to a half than fp32 tells, so the rounding is that of
-// w / s itself.  fp32 weights may be: `nearest` looks at the remainder.
+// Two quotients rounded to whole numbers, halves to the even one, by adding 1.5 * 2^23.
+// Quotients of 16-bit numbers are no nearer to a half than fp32 tells, so the rounding is
+// that of w / s itself.  fp32 weights may be: their remainders are looked at.
 template <typename W>
-__device__ __forceinline__ uint32_t number(float quotient, float w, float s) {
-  float q = fminf(fmaxf(quotient, -8.0f), 7.0f);
+__device__ __forceinline__ float2 numbers(uint64_t quotient, uint64_t weights, float s) {
+  float2 n = each(add2(add2(quotient, both(12582912.0f, 12582912.0f)), both(-12582912.0f, -12582912.0f)));
   if constexpr (sizeof(W) == 4) {
-    const float n = rintf(q), r = fmaf(-n, s, w), half = 0.5f * s;
-    const bool odd = (int)n & 1;
-    if (fabsf(r) > half || (fabsf(r) == half && odd)) q = n + (r > 0.0f ? 1.0f : -1.0f);
-    q = fminf(fmaxf(q, -8.0f), 7.0f);
+    const float2 w = each(weights);
+    const auto nearest = [&](float n, float w) {
+      const float r = fmaf(-n, s, w), half = 0.5f * s;
+      const bool off = fabsf(r) > half || (fabsf(r) == half && ((int)n & 1));
+      return fminf(fmaxf(off ? n + (r > 0.0f ? 1.0f : -1.0f) : n, -8.0f), 7.0f);
+    };
+    n.x = nearest(n.x, w.x), n.y = nearest(n.y, w.y);
   }
-  return __float_as_uint(q + 12582920.0f);
+  return n;
 }
 
-template <typename W, typename T, bool VEC>
+// Eight weights as they are loaded, and as numbers with the bits of their largest magnitude: NaN is above
+// infinity, and infinity above numbers.
+template <typename W>
+struct Eight {
+  static constexpr int kWords = 2 * (int)sizeof(W);
+  uint32_t w[kWords];
+  // `have` of them are inside the row, zeros after; `whole`: all are, and they start on 16 bytes.
+  __device__ __forceinline__ void load(const W *p, uint32_t have, bool whole) {
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < kWords; i += 4) {
+        const uint4 q = __ldcs((const uint4 *)p + i / 4);
+        w[i] = q.x, w[i + 1] = q.y, w[i + 2] = q.z, w[i + 3] = q.w;
+      }
+    } else if constexpr (sizeof(W) == 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = i < (int)have ? __float_as_uint(p[i]) : 0u;
+    } else {
+      const uint16_t *h = (const uint16_t *)p;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (2 * i < (int)have ? h[2 * i] : 0u) | (2 * i + 1 < (int)have ? (uint32_t)h[2 * i + 1] << 16 : 0u);
+    }
+  }
+  __device__ __forceinline__ uint32_t values(float (&v)[8]) const {
+    uint32_t top = 0;
+    if constexpr (sizeof(W) == 2) {  // two magnitudes at a time, as whole numbers of 16 bits
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        top = __vmaxu2(top, w[i] & 0x7FFF7FFFu);
+        const float2 f = unpack2<W>(w[i]);
+        v[2 * i] = f.x, v[2 * i + 1] = f.y;
+      }
+      return __float_as_uint(unpack2<W>(max(top >> 16, top & 0xFFFFu)).x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i] = __uint_as_float(w[i]);
+        top = max(top, w[i] & 0x7FFFFFFFu);
+      }
+      return top;
+    }
+  }
+};
+
+template <typename W, typename T, bool VEC, int GROUP>
 __global__ void __launch_bounds__(kThreads) k_pack4(const Pack4 a, const Turns t) {
-  constexpr int kLoads = 8 / Vec<W>::N;
-  const uint32_t lane = threadIdx.x & 31, members = min(a.group / 8, t.lanes);
+  constexpr uint32_t kMembers = GROUP / 8;  // lanes of a group
+  const uint32_t lane = threadIdx.x & 31;
   const uint64_t e = blockIdx.y;
+  // scales below this are rounded coarsely (fp16) or leave fp32's numbers (bf16)
+  constexpr float kSmall = std::is_same<T, __half>::value ? 6.10351562e-5f : 5.4210109e-20f;  // 2^-14, 2^-64
   pdl_wait();
   pdl_trigger();
   for (Walk at(t); at.rows < t.rows; at.next(t)) {
-    uint32_t n, k;
-    at.place(t, lane, n, k);
-    const uint32_t have = n < a.out_dim && k < a.in_dim ? min(a.in_dim - k, 8u) : 0;
-    const W *w = (const W *)a.w + (have ? e * a.stride_w + n * a.ld_w + k : 0);
-    float v[8];
-    uint32_t top = 0;  // the bits of the largest magnitude: NaN is above infinity, and infinity above numbers
-    if (VEC && have == 8) {
-      if constexpr (sizeof(W) == 2) {  // two at a time, as whole numbers of 16 bits
-        const uint4 raw = __ldcs((const uint4 *)w);
-        const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
-        uint32_t two = 0;
+    uint32_t n, k, many;
+    at.place(t, lane, n, k, many);
+    const bool row = n < a.out_dim;
+    const W *w = (const W *)a.w + e * a.stride_w + (row ? n : 0) * a.ld_w + k;
+    uint8_t *packed = a.packed + e * a.stride_packed + (row ? n : 0) * a.ld_packed + k / 2;
+    T *scales = (T *)a.scales + e * a.stride_scales + (row ? n : 0) * a.ld_scales + k / GROUP;
+    const uint32_t inside = row && k < a.in_dim ? a.in_dim - k : 0;  // of the row from the lane's first weight on
+    const auto have_at = [&](int i) { return inside > 256u * i ? min(inside - 256u * i, 8u) : 0u; };
+    Eight<W> raw[kRun];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          two = __vmaxu2(two, words[i] & 0x7FFF7FFFu);
-          const float2 f = unpack2<W>(words[i]);
-          v[2 * i] = f.x, v[2 * i + 1] = f.y;
+    for (int i = 0; i < (int)kRun; ++i)
+      if (i < (int)many) raw[i].load(w + 256 * i, have_at(i), VEC && have_at(i) == 8);
+#pragma unroll
+    for (int i = 0; i < (int)kRun; ++i) {
+      if (i >= (int)many) break;
+      const uint32_t have = have_at(i);
+      float v[8];
+      uint32_t top = raw[i].values(v);
+#pragma unroll
+      for (uint32_t s = 1; s < kMembers; s <<= 1) top = max(top, __shfl_xor_sync(kAll, top, s));
+      const float largest = __uint_as_float(top);
+      const bool finite = largest < INFINITY;
+      const T scale = from_f<T>(finite ? largest * (1.0f / 7.0f) : __uint_as_float(0x7FC00000u));
+      float s = to_f<T>(scale);
+      uint32_t q = 0x88888888u;
+      if (s > 0.0f && s < INFINITY) {
+        if (s < kSmall) {
+          if (!std::is_same<T, __half>::value) {
+            s *= 18446744073709551616.0f;  // 2^64
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= 18446744073709551616.0f;
+          }
+          // elsewhere the largest is at most 7.03 scales
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[j] = fminf(fmaxf(v[j], -8.0f * s), 7.0f * s);
         }
-        top = __float_as_uint(unpack2<W>(max(two >> 16, two & 0xFFFFu)).x);
-      } else {
+        const float inv = quick_inverse(s);
+        // pairs (0, 2), (1, 3), (4, 6), (5, 7): n_0 + 16 n_1 and n_2 + 16 n_3 in two steps, the word's halves in one more
+        float half[2];
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          float f[Vec<W>::N];
-          Vec<W>::unpack(__ldcs((const uint4 *)w + i), f);
-#pragma unroll
-          for (int j = 0; j < Vec<W>::N; ++j) v[i * Vec<W>::N + j] = f[j];
+        for (int h = 0; h < 2; ++h) {
+          const uint64_t even = both(v[4 * h], v[4 * h + 2]), odd = both(v[4 * h + 1], v[4 * h + 3]);
+          const float2 x = numbers<W>(quotients(even, s, inv), even, s), y = numbers<W>(quotients(odd, s, inv), odd, s);
+          half[h] = fmaf(fmaf(y.y, 16.0f, x.y), 256.0f, fmaf(y.x, 16.0f, x.x)) + (12582912.0f + 34952.0f);  // 0x8888: + 8 each
         }
+        q = __byte_perm(__float_as_uint(half[0]), __float_as_uint(half[1]), 0x5410);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < (int)have ? to_f<W>(w[i]) : 0.0f;
-    }
-    if (sizeof(W) == 4 || !VEC || have != 8) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    }
-    for (uint32_t s = 1; s < members; s <<= 1) top = max(top, __shfl_xor_sync(kAll, top, s));
-    const float largest = __uint_as_float(top);
-    const bool finite = largest < INFINITY;
-    const T scale = from_f<T>(finite ? largest * (1.0f / 7.0f) : __uint_as_float(0x7FC00000u));
-    float s = to_f<T>(scale);
-    const bool some = finite && s > 0.0f && s < INFINITY;
-    if (some && s < 5.4210109e-20f) {  // 2^-64: what follows stays clear of numbers below the smallest normal one
-      s *= 18446744073709551616.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= 18446744073709551616.0f;
-    }
-    uint32_t q = 0x88888888u;
-    if (some) {
-      const float inv = quick_inverse(s);
-      q = 0;
-#pragma unroll
-      for (int i = 0; i < 8; i += 2) {
-        const float2 r = quotients(make_float2(v[i], v[i + 1]), s, inv);
-        q |= (number<W>(r.x, v[i], s) & 15u) << (4 * i) | (number<W>(r.y, v[i + 1], s) & 15u) << (4 * i + 4);
-      }
-    }
-    if (have) {
-      uint8_t *out = a.packed + e * a.stride_packed + n * a.ld_packed + k / 2;
+      uint8_t *out = packed + 128 * i;
       if (have == 8 && ((uintptr_t)out & 3) == 0) {
         *(uint32_t *)out = q;
       } else {
-        for (uint32_t i = 0; i < (have + 1) / 2; ++i) out[i] = (uint8_t)(q >> (8 * i));
+        for (uint32_t j = 0; j < (have + 1) / 2; ++j) out[j] = (uint8_t)(q >> (8 * j));
       }
-      if ((lane & (members - 1)) == 0) ((T *)a.scales)[e * a.stride_scales + n * a.ld_scales + k / a.group] = scale;
+      if (have && (lane & (kMembers - 1)) == 0) scales[256 / GROUP * i] = scale;
     }
   }
 }
@@ -171,64 +208,82 @@ __global__ void __launch_bounds__(kThreads) k_unpack4(const Unpack a, const Turn
   // has rows there that has none here
   if (a.offsets && offset_at(a.offsets, e, a.num_rows) >= offset_at(a.offsets, e + 1, a.num_rows)) return;
   for (Walk at(t); at.rows < t.rows; at.next(t)) {
-    uint32_t n, k;
-    at.place(t, lane, n, k);
-    if (n >= a.out_dim || k >= a.in_dim) continue;
-    const uint32_t have = min(a.in_dim - k, 8u);
+    uint32_t n, k, many;
+    at.place(t, lane, n, k, many);
+    if (n >= a.out_dim) continue;
     const uint8_t *in = a.packed + e * a.stride_packed + n * a.ld_packed + k / 2;
-    uint32_t q = 0;
-    if (have == 8 && ((uintptr_t)in & 3) == 0) {
-      q = __ldcs((const uint32_t *)in);
-    } else {
-      for (uint32_t i = 0; i < (have + 1) / 2; ++i) q |= (uint32_t)in[i] << (8 * i);
+    const uint16_t *scales = a.scales + e * a.stride_scales + n * a.ld_scales + k / a.group;
+    uint16_t *to = a.w + e * a.stride_w + n * a.ld_w + k;
+    const uint32_t inside = k < a.in_dim ? a.in_dim - k : 0, by = 256 / a.group;
+    uint32_t word[kRun], scale[kRun];
+#pragma unroll
+    for (int i = 0; i < (int)kRun; ++i) {
+      const uint32_t have = i < (int)many && inside > 256u * i ? min(inside - 256u * i, 8u) : 0u;
+      word[i] = scale[i] = 0;
+      if (have == 0) continue;
+      const uint8_t *p = in + 128 * i;
+      if (have == 8 && ((uintptr_t)p & 3) == 0) {
+        word[i] = __ldcs((const uint32_t *)p);
+      } else {
+        for (uint32_t j = 0; j < (have + 1) / 2; ++j) word[i] |= (uint32_t)p[j] << (8 * j);
+      }
+      scale[i] = scales[by * i];
     }
-    // a number times the scale in 16 bits: one rounding, of the exact product
-    const uint32_t s = *(const uint16_t *)((const T *)a.scales + e * a.stride_scales + n * a.ld_scales + k / a.group) * 0x10001u;
-    uint32_t v[4];
-    numbers4<T>(q, v);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = times<T>(v[i], s);
-    const uint4 out = make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410),
-                                 __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
-    T *to = (T *)a.w + e * a.stride_w + n * a.ld_w + k;
-    if (VEC && have == 8) {
-      *(uint4 *)to = out;
-    } else {
-      const uint32_t word[4] = {out.x, out.y, out.z, out.w};
+    for (int i = 0; i < (int)kRun; ++i) {
+      const uint32_t have = i < (int)many && inside > 256u * i ? min(inside - 256u * i, 8u) : 0u;
+      if (have == 0) break;
+      // a number times the scale in 16 bits: one rounding, of the exact product
+      uint32_t v[4];
+      numbers4<T>(word[i], v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < (int)have) ((uint16_t *)to)[i] = (uint16_t)(word[i / 2] >> (16 * (i & 1)));
+      for (int j = 0; j < 4; ++j) v[j] = times<T>(v[j], scale[i] * 0x10001u);
+      const uint4 out = make_uint4(__byte_perm(v[0], v[1], 0x5410), __byte_perm(v[2], v[3], 0x5410),
+                                   __byte_perm(v[0], v[1], 0x7632), __byte_perm(v[2], v[3], 0x7632));
+      if (VEC && have == 8) {
+        *(uint4 *)(to + 256 * i) = out;
+      } else {
+        const uint32_t w[4] = {out.x, out.y, out.z, out.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < (int)have) to[256 * i + j] = (uint16_t)(w[j / 2] >> (16 * (j & 1)));
+      }
     }
   }
 }
 
-Turns turns_of(uint32_t K, uint32_t N) {
+// `least` lanes of a row at least.  A turn has several pieces where warps are left with several turns all the same.
+Turns turns_of(uint32_t K, uint32_t N, uint32_t E, uint32_t least) {
   Turns t;
-  t.lanes = 4;
-  while (t.lanes < 32 && t.lanes * 8 < K) t.lanes *= 2;
+  t.lanes_log = 2;
+  while (t.lanes_log < 5 && ((8u << t.lanes_log) < K || (1u << t.lanes_log) < least)) ++t.lanes_log;
+  t.lanes = 1u << t.lanes_log;
   t.pieces = (K + t.lanes * 8 - 1) / (t.lanes * 8);
   t.rows = (N + 32 / t.lanes - 1) / (32 / t.lanes);
+  const uint64_t warps = (uint64_t)sm_count() * 64;
+  t.run = (uint32_t)std::min<uint64_t>(std::min(kRun, t.pieces), std::max<uint64_t>(1, (uint64_t)t.rows * t.pieces * E / warps));
+  t.runs = (t.pieces + t.run - 1) / t.run;
   return t;
 }
-// 64 CTAs an SM over all experts, and so at most 2^18 warps an expert: Walk's sums stay below 2^32.
+// 16 CTAs an SM over all experts, and so at most 2^15 warps an expert: Walk's sums stay below 2^32.
 dim3 grid_of(const Turns &t, uint32_t E) {
-  const uint64_t ctas = ((uint64_t)t.rows * t.pieces + kThreads / 32 - 1) / (kThreads / 32);
-  return dim3((unsigned)std::max<uint64_t>(1, std::min<uint64_t>(ctas, (uint64_t)sm_count() * 64 / E)), E);
+  const uint64_t ctas = ((uint64_t)t.rows * t.runs + kThreads / 32 - 1) / (kThreads / 32);
+  return dim3((unsigned)std::max<uint64_t>(1, std::min<uint64_t>(ctas, (uint64_t)sm_count() * 16 / E)), E);
 }
 
 template <typename T>
 cudaError_t pack(const Pack4 &a, ntc_type w_type, cudaStream_t st) {
-  const Turns t = turns_of(a.in_dim, a.out_dim);
+  const Turns t = turns_of(a.in_dim, a.out_dim, a.num_experts, a.group / 8);
   const dim3 grid = grid_of(t, a.num_experts);
-  const auto go = [&](auto with, auto without, size_t elem) {
-    const bool vec = ((uintptr_t)a.w & 15) == 0 && a.ld_w * elem % 16 == 0 && (a.num_experts == 1 || a.stride_w * elem % 16 == 0);
-    return launch_pdl(vec ? with : without, grid, kThreads, 0, st, a, t);
+  const auto go = [&](auto type) {
+    using W = decltype(type);
+    const bool vec = ((uintptr_t)a.w & 15) == 0 && a.ld_w * sizeof(W) % 16 == 0 && (a.num_experts == 1 || a.stride_w * sizeof(W) % 16 == 0);
+    const auto kernel = a.group == 32   ? (vec ? k_pack4<W, T, true, 32> : k_pack4<W, T, false, 32>)
+                        : a.group == 64 ? (vec ? k_pack4<W, T, true, 64> : k_pack4<W, T, false, 64>)
+                                        : (vec ? k_pack4<W, T, true, 128> : k_pack4<W, T, false, 128>);
+    return launch_pdl(kernel, grid, kThreads, 0, st, a, t);
   };
-  switch (w_type) {
-    case NTC_TYPE_FP32: return go(k_pack4<float, T, true>, k_pack4<float, T, false>, 4);
-    case NTC_TYPE_FP16: return go(k_pack4<__half, T, true>, k_pack4<__half, T, false>, 2);
-    default: return go(k_pack4<__nv_bfloat16, T, true>, k_pack4<__nv_bfloat16, T, false>, 2);
-  }
+  return w_type == NTC_TYPE_FP32 ? go(float()) : w_type == NTC_TYPE_FP16 ? go(__half()) : go(__nv_bfloat16());
 }
 
 ntc_status check_matrix(const ntc_pack4_desc *d, const void *w, size_t elem, uint64_t ld_w, uint64_t stride_w,
@@ -267,7 +322,7 @@ ntc_status check_pack4(const ntc_pack4_desc *d) {
 }
 
 cudaError_t launch_unpack4(const Unpack &u, bool bf16, cudaStream_t st) {
-  const Turns t = turns_of(u.in_dim, u.out_dim);
+  const Turns t = turns_of(u.in_dim, u.out_dim, u.num_experts, 1);
   const bool vec = rows_are_vec(u.w, u.ld_w, 2) && (u.num_experts == 1 || u.stride_w % 8 == 0);
   const auto kernel = bf16 ? (vec ? k_unpack4<__nv_bfloat16, true> : k_unpack4<__nv_bfloat16, false>)
                            : (vec ? k_unpack4<__half, true> : k_unpack4<__half, false>);
