@@ -607,9 +607,9 @@ NTC_API ntc_status ntc_balance_loss_backward(const ntc_balance_desc *desc, size_
  * moment_bits 32: m and v are fp32.  moment_bits 8: m and v hold e4m3 codes of m
  * and of sqrt(v), in blocks of NTC_ADAMW_BLOCK consecutive elements with an fp32
  * scale each, scale_m[i / NTC_ADAMW_BLOCK] and scale_v[...]: value = code * scale,
- * scale = (largest magnitude of the block) / 448, rounded to nearest.  A root has at
- * least the least code (2^-9), so that no division loses its denominator.  The step
- * itself uses the moments before they are rounded.  A moment that changes by less than
+ * scale = (largest magnitude of the block) / 448, rounded to nearest.  A root that is
+ * not 0 has at least the least code (2^-9), so that no division loses its denominator.
+ * The step itself uses the moments before they are rounded.  A moment that changes by less than
  * half of a code's distance (up to 1/16 of its value) keeps its code; what the block's
  * largest does is exact, and the others move with it.  Where a moment's largest is below
  * 2^-100 its block is 0; both moments of a block with an infinity or a NaN read back as

@@ -9,9 +9,11 @@
 // them; the block is also what an 8-bit scale belongs to, so its
 // largest moment is one reduction in the warp.  The tensors' table is the kernel's
 // argument: a step of many small tensors is one launch and copies nothing.
-// The root and the reciprocal are the hardware's approximations (1 ulp each; the exact ones
-// made the 8-bit step a third slower), two elements go through one fp32x2 operation where
-// there is one; with them a change of p is off by 2^-21 of itself at most.
+// The moments, their roots, codes and scales are rounded to nearest in fp32, operation by
+// operation in the order above and without contraction: a last digit that is off makes
+// another code of about one moment in a million, and codes near the least one are far apart.
+// The change of p is not: its reciprocal is the hardware's, 2^-21 of the change at most.  Two
+// elements go through one fp32x2 operation where there is one.
 #include "experts.cuh"
 
 #include <cuda_fp8.h>
@@ -47,6 +49,7 @@ struct Entry {
 
 struct Scalars {
   float beta1, c1, beta2, c2, eps;
+  float one;  // 1, which the compiler does not know: it makes one operation of an fp32x2 product and sum, rounded once
   float decay, rate, root, grad_scale;  // unless `derived` has them
   const float *derived;
 };
@@ -133,10 +136,16 @@ __device__ __forceinline__ void write(void *base, uint64_t at, uint32_t type, ui
   }
 }
 
-__device__ __forceinline__ float quick_root(float x) {
-  float y;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
+// Square roots of two numbers, rounded to nearest: the product with an approximate reciprocal
+// root, corrected by its remainder, which a fused operation gives exactly (Markstein's
+// correction).  Numbers from 2^-100 to 2^100: there no remainder leaves fp32.
+__device__ __forceinline__ uint64_t roots(uint64_t v) {
+  const float2 x = each(v);
+  float a, b;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(x.x));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(x.y));
+  const uint64_t y = both(a, b), r = mul2(v, y), minus_r = mul2(r, both(-1.0f, -1.0f));
+  return fma2(fma2(minus_r, r, v), mul2(y, both(0.5f, 0.5f)), r);
 }
 __device__ __forceinline__ float inverse(float x) {
   float y;
@@ -170,16 +179,19 @@ __device__ __forceinline__ void read_codes(const void *base, uint64_t at, uint32
 #pragma unroll
   for (int h = 0; h < 4; ++h) v[h] = mul2(from_codes(q[h / 2] >> (16 * (h & 1)) & 0xFFFFu), s);
 }
-// The codes of a block's values times inv, none below `least`.
+// The codes of a block's values times inv.  ROOT: what is not 0 gets at least the least code, 2^-9.
 template <bool VEC, bool ROOT>
-__device__ __forceinline__ void write_codes(void *base, uint64_t at, uint32_t lane, uint32_t left, float inv, float least, const uint64_t (&v)[4]) {
+__device__ __forceinline__ void write_codes(void *base, uint64_t at, uint32_t lane, uint32_t left, float inv, const uint64_t (&v)[4]) {
   uint8_t *p = (uint8_t *)base + at;
   const uint64_t by = both(inv, inv);
   uint32_t q[2] = {};
 #pragma unroll
   for (int h = 0; h < 4; ++h) {
     float2 x = each(mul2(v[h], by));
-    if constexpr (ROOT) x.x = fmaxf(x.x, least), x.y = fmaxf(x.y, least);
+    if constexpr (ROOT) {
+      if (x.x > 0.0f) x.x = fmaxf(x.x, 0.001953125f);
+      if (x.y > 0.0f) x.y = fmaxf(x.y, 0.001953125f);
+    }
     q[h / 2] |= to_codes(x.x, x.y) << (16 * (h & 1));
   }
   if constexpr (VEC) {
@@ -214,9 +226,8 @@ __device__ __forceinline__ void write_moments(const Entry &t, uint64_t block, ui
     t.scale_v[block] = !finite ? nan : some_r ? r_top * (1.0f / 448.0f) : 0.0f;
   }
   const uint64_t at = block * kBlock;
-  // 2^-9 is the least code
-  write_codes<VEC, false>(t.m, at, lane, left, some_m ? 448.0f * inverse(m_top) : 0.0f, 0.0f, m);
-  write_codes<VEC, true>(t.v, at, lane, left, some_r ? 448.0f * inverse(r_top) : 0.0f, some_r ? 0.001953125f : 0.0f, root);
+  write_codes<VEC, false>(t.m, at, lane, left, some_m ? __fdiv_rn(448.0f, m_top) : 0.0f, m);
+  write_codes<VEC, true>(t.v, at, lane, left, some_r ? __fdiv_rn(448.0f, r_top) : 0.0f, root);
 }
 
 template <bool EIGHT, bool VEC>
@@ -239,16 +250,29 @@ __device__ __forceinline__ void step(const Entry &t, uint64_t block, uint32_t la
   }
   const uint64_t beta1 = both(s.beta1, s.beta1), c1 = both(s.c1, s.c1), beta2 = both(s.beta2, s.beta2), c2 = both(s.c2, s.c2);
   const uint64_t decay = both(s.decay, s.decay), rate = both(-s.rate, -s.rate), scale = both(s.grad_scale, s.grad_scale);
+  const uint64_t one = both(s.one, s.one);
+  float least = INFINITY, most = 0.0f;  // of v
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const uint64_t f = mul2(both(g[2 * i], g[2 * i + 1]), scale);
-    m[i] = fma2(m[i], beta1, mul2(f, c1));
+    m[i] = fma2(mul2(m[i], beta1), one, mul2(f, c1));
     if constexpr (EIGHT) v[i] = mul2(v[i], v[i]);  // the root was held
-    v[i] = fma2(mul2(f, c2), f, mul2(v[i], beta2));
+    v[i] = fma2(mul2(v[i], beta2), one, mul2(mul2(f, c2), f));
     const float2 r = each(v[i]);
-    const float rx = quick_root(r.x), ry = quick_root(r.y);
-    root[i] = both(rx, ry);
-    const uint64_t inv = both(inverse(fmaf(rx, s.root, s.eps)), inverse(fmaf(ry, s.root, s.eps)));
+    least = fminf(least, fminf(r.x, r.y)), most = fmaxf(most, fmaxf(r.x, r.y));
+    root[i] = roots(v[i]);
+  }
+  if (!(least >= 7.89e-31f && most <= 1.26e30f)) {  // 2^-100, 2^100; a NaN is found by what is done with it
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 r = each(v[i]);
+      root[i] = both(__fsqrt_rn(r.x), __fsqrt_rn(r.y));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 r = each(root[i]);
+    const uint64_t inv = both(inverse(fmaf(r.x, s.root, s.eps)), inverse(fmaf(r.y, s.root, s.eps)));
     const float2 q = each(fma2(both(p[2 * i], p[2 * i + 1]), decay, mul2(mul2(m[i], rate), inv)));
     p[2 * i] = q.x, p[2 * i + 1] = q.y;
   }
@@ -417,7 +441,7 @@ extern "C" NTC_API ntc_status ntc_adamw(const ntc_adamw_desc *desc, const ntc_ad
     return op_fail(NTC_ERR_INVALID_ARG, "workspace must have %u bytes at a multiple of 16", NTC_ADAMW_WORKSPACE);
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const ntc_adamw_desc &d = *desc;
-  Scalars s = {(float)d.beta1, (float)(1.0 - d.beta1), (float)d.beta2, (float)(1.0 - d.beta2), (float)d.eps, 0, 0, 0, 0, nullptr};
+  Scalars s = {(float)d.beta1, (float)(1.0 - d.beta1), (float)d.beta2, (float)(1.0 - d.beta2), (float)d.eps, 1.0f, 0, 0, 0, 0, nullptr};
   if (derived) {
     s.derived = (const float *)workspace;
     const cudaError_t e = launch_pdl(k_adamw_scalars, 1, 32, 0, st, d.lr, d_lr, d.beta1, d.beta2, d.weight_decay, d.step, d_step,

@@ -279,6 +279,37 @@ def test_eight_bits_follow_thirty_two(ntc):
     R.assert_within(runs[1], runs[0], 0.157 * runs[0].abs() + 1e-6)
 
 
+@pytest.mark.parametrize("scale", [1.0, 1e-9, 1e-14, 1e9])
+def test_moments_are_rounded_as_they_are_defined(ntc, scale):
+    """The same operations in torch, each rounded to nearest in fp32: the same moments, codes and scales, bit for bit.  A
+    last digit that is off is a code that is off where codes are far apart."""
+    n, b1, b2 = 256 * 4000, 0.85, 0.98
+    g = torch.Generator(device="cuda").manual_seed(21)
+    size = torch.exp(2 * torch.randn(n, generator=g, device="cuda")) * scale
+    grad = torch.randn(n, generator=g, device="cuda") * size
+    grad[: 256 * 3] = 0.0
+    one = lambda x: torch.tensor(x, dtype=F, device="cuda")  # noqa: E731
+    m32 = torch.randn(n, generator=g, device="cuda") * size
+    (m, a), (r, b) = encode(m32), encode((torch.randn(n, generator=g, device="cuda").abs() + 0.01) * size)
+    s = torch.stack([a, b])
+    m0, r0 = m.float() * a.repeat_interleave(256), r.float() * b.repeat_interleave(256)
+    p = torch.randn(n, generator=g, device="cuda")
+    m1 = m0 * one(b1) + grad * one(1 - b1)
+    v1 = (r0 * r0) * one(b2) + (grad * one(1 - b2)) * grad
+    v32, m_old = r0 * r0, m0.clone()
+    ntc.adamw([p.clone()], [grad], [m_old], [v32], step=5, lr=0.01, beta1=b1, beta2=b2)
+    assert torch.equal(m_old, m1) and torch.equal(v32, v1)
+    ntc.adamw([p], [grad], [m], [r], scales=[s], step=5, lr=0.01, beta1=b1, beta2=b2)
+    for want, code, got_scale, root in ((m1, m, s[0], False), (torch.sqrt(v1), r, s[1], True)):
+        f = want.view(-1, 256)
+        top = f.abs().amax(1, keepdim=True)
+        y = torch.where(top >= 2.0 ** -100, f * torch.div(torch.full_like(top, 448.0), top), torch.zeros_like(f))
+        if root:
+            y = torch.where(y > 0, y.clamp_min(2.0 ** -9), y)
+        assert torch.equal(code.view(torch.uint8), y.to(F8).view(torch.uint8).view(-1))
+        assert torch.equal(got_scale, torch.where(top >= 2.0 ** -100, top * one(1.0 / 448.0), torch.zeros_like(top)).view(-1))
+
+
 def test_past_2_31_elements(ntc):
     """One tensor of 2^31 + 300 elements, most of them zero: offsets past 32 bits."""
     n = 2 ** 31 + 300
