@@ -671,13 +671,14 @@ NTC_API ntc_status ntc_unpack4(const ntc_pack4_desc *desc, const uint8_t *packed
                                uint64_t ld_w, uint64_t stride_w, void *cuda_stream);
 
 /* ntc_linear (without z) with weights in 4 bits (ld_packed and ld_scales below 2^26).
- * desc's ld_w, stride_w and ld_z are
- * not read; its type, in_dim, out_dim and num_experts are those of `weights`.  Calls
- * of few rows per expert (up to 32 on average) multiply the numbers q themselves, exact in 16 bits, and
- * the groups' fp32 sums by their scales; larger ones unpack the weights of experts
- * that have rows into the workspace, rounded to 16 bits, and take ntc_linear's product. */
+ * desc's ld_w, stride_w and ld_z are not read; its type, in_dim, out_dim and
+ * num_experts are those of `weights`.  Calls of few rows per expert multiply the
+ * numbers q themselves, exact in 16 bits, and the groups' fp32 sums by their scales.
+ * Others round scale * q to 16 bits first, as ntc_unpack4 does: on the way to the tensor
+ * cores, or in the workspace where x or packed do not start on 16 bytes, in_dim is not a
+ * multiple of 32, the experts' tiles are few or their rows very many. */
 NTC_API size_t ntc_linear4_workspace(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, const void *x,
-                                     const int32_t *rows);
+                                     const int32_t *rows, const uint8_t *packed);
 NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, const void *x,
                                const int32_t *rows, const int32_t *offsets, const uint8_t *packed,
                                const void *scales, const float *bias, const void *residual, void *y,

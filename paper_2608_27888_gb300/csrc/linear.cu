@@ -34,7 +34,7 @@
 // A weight matrix [N][K] is read as it lies: K-major in the forward product,
 // MN-major (the descriptors' transpose bits) in kDx; kDw takes both operands
 // MN-major.  Nothing is transposed in memory.
-#include "linear.cuh"
+#include "linear4.cuh"
 #include "tcgen05.cuh"
 
 #include <cuda.h>
@@ -1646,6 +1646,7 @@ cudaError_t launch_packs(const Packs &p, cudaStream_t st) {
 
 namespace ntc {
 
+unsigned int *linear_status_word() { return status_word(); }
 ntc_status check_linear(const ntc_linear_desc *d) { return check(d); }
 ntc_status check_linear_rows(const ntc_linear_desc &d, const int32_t *rows, const int32_t *offsets) {
   return check_rows(d, rows, offsets);

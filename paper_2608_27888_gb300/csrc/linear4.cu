@@ -12,9 +12,11 @@
 // rounded.
 // Few (expert, rows) pairs are split along K over the warps of a CTA, whose sums meet
 // in shared memory in a fixed order.
-// Many rows per expert: the weights of experts with rows are unpacked to 16 bits and the
-// product of linear.cu takes them.
-#include "pack4.cuh"
+// More rows per expert, and tiles enough: linear4_mid.cu, whose tcgen05 tiles unpack the
+// weights on their way into shared memory.
+// Many rows per expert, or operands that do not start on 16 bytes: the weights of experts with
+// rows are unpacked to 16 bits in the workspace and the product of linear.cu takes them.
+#include "linear4.cuh"
 
 using namespace ntc;
 
@@ -326,7 +328,24 @@ uint64_t mean_rows(const ntc_linear_desc &d) {
   const uint64_t experts = std::min<uint64_t>(d.num_experts, d.num_rows);
   return (d.num_rows + experts - 1) / experts;
 }
-bool takes_few(const ntc_linear_desc &d) { return d.num_rows == 0 || few_rows(d.num_rows) || mean_rows(d) <= 32; }
+// Whether rows start on as many bytes.
+bool starts_on(const ntc_linear_desc &d, const void *p, uint64_t bytes, uint64_t ld, uint64_t stride) {
+  return (uintptr_t)p % bytes == 0 && ld % bytes == 0 && (d.num_experts == 1 || stride % bytes == 0);
+}
+// Which kernels take the call.  The tcgen05 kernel has one CTA or two an SM, unpacks a tile of weights once for every 128
+// rows and wants tiles enough to fill the GPU (times in us, tcgen05 and the better of the others):
+//   64 tiles or more: 64 experts, 2,048 -> 1,024: 44 and 67 for 16 rows an expert, 52 and 160 for 32,
+//     66 and 117 for 64; 128 rows, 2,048 -> 32,768: 36 and 57; 64 tiles, 32 rows: 20 and 23.5;
+//   fewer: 32 tiles, 4,096 -> 4,096: 29 and 14 for 20 rows, 40 and 26 for 128;
+//   more rows: 256 an expert, 64 experts, 1,024 -> 2,048: 175 and 139.
+enum Path { kFew, kMid, kUnpack };
+Path path_of(const ntc_linear_desc &d, const ntc_pack4_desc &p, const void *x, const uint8_t *packed) {
+  if (d.num_rows == 0 || few_rows(d.num_rows)) return kFew;
+  const uint64_t mean = mean_rows(d), tiles = std::min<uint64_t>(d.num_experts, d.num_rows) * ((d.out_dim + 127ull) / 128);
+  const bool mid = d.in_dim % 32 == 0 && rows_are_vec(x, d.ld_x, 2) && starts_on(d, packed, 16, p.ld_packed, p.stride_packed);
+  if (mid && mean > 8 && mean <= 128 && tiles >= 64) return kMid;
+  return mean <= 32 ? kFew : kUnpack;
+}
 
 uint64_t pitch_of(uint64_t K) { return (K + 63) / 64 * 64; }  // of the unpacked weights: rows of whole 128-byte lines
 uint64_t unpacked_bytes(const ntc_linear_desc &d) {
@@ -352,9 +371,9 @@ ntc_status check(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, ntc
 }  // namespace
 
 extern "C" NTC_API size_t ntc_linear4_workspace(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, const void *x,
-                                                const int32_t *rows) {
+                                                const int32_t *rows, const uint8_t *packed) {
   ntc_linear_desc d;
-  if (check(desc, weights, &d) || takes_few(d)) return 0;
+  if (check(desc, weights, &d) || path_of(d, *weights, x, packed) != kUnpack) return 0;
   // the weights lie at the start of an aligned workspace, whose address has no part in the rest
   return unpacked_bytes(d) + ntc_linear_workspace(&d, x, rows, (const void *)256);
 }
@@ -371,11 +390,12 @@ extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc
   if (((uintptr_t)x | (uintptr_t)scales | (uintptr_t)y | (uintptr_t)residual) & 1)
     return op_fail(NTC_ERR_INVALID_ARG, "a buffer is not aligned to its element (2 bytes)");
   if ((uintptr_t)bias & 3) return op_fail(NTC_ERR_INVALID_ARG, "bias is not aligned to 4 bytes");
-  if (ntc_status s = check_workspace(workspace, workspace_bytes, ntc_linear4_workspace(desc, weights, x, rows))) return s;
+  if (ntc_status s = check_workspace(workspace, workspace_bytes, ntc_linear4_workspace(desc, weights, x, rows, packed))) return s;
   const ntc_pack4_desc &p = *weights;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const bool bf16 = d.type == NTC_TYPE_BF16;
-  if (!takes_few(d)) {
+  const Path path = path_of(d, p, x, packed);
+  if (path == kUnpack) {
     const Unpack u = {packed, (const uint16_t *)scales, (uint16_t *)workspace, offsets, p.ld_packed, p.stride_packed, p.ld_scales,
                       p.stride_scales, d.ld_w, d.stride_w, d.in_dim, d.out_dim, d.num_experts, p.group, (int32_t)d.num_rows};
     if (cudaError_t e = launch_unpack4(u, bf16, st)) return op_cuda(e, "ntc_linear4");
@@ -383,8 +403,7 @@ extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc
     return ntc_linear(&d, x, rows, offsets, workspace, bias, residual, y, nullptr, (uint8_t *)workspace + used,
                       workspace_bytes - used, cuda_stream);
   }
-  FewArgs f{};
-  LinearArgs &a = f.a;
+  LinearArgs a{};
   a.rows = rows;
   a.offsets = offsets;
   a.bias = bias;
@@ -401,6 +420,16 @@ extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc
   a.depth = d.in_dim;
   a.activation = d.activation;
   a.slope = d.leaky_slope;
+  a.bf16 = bf16;
+  if (path == kMid) {
+    a.status = linear_status_word();
+    if (!a.status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
+    const Mid4 m = {a, packed, (const uint16_t *)scales, p.ld_packed, p.stride_packed, p.ld_scales, p.stride_scales,
+                    p.group == 32 ? 5u : p.group == 64 ? 6u : 7u};
+    return op_cuda(launch_linear4_mid(m, mean_rows(d), st), "ntc_linear4");
+  }
+  FewArgs f{};
+  f.a = a;
   f.packed = packed;
   f.scales = (const uint16_t *)scales;
   f.ld_packed = p.ld_packed;
@@ -408,11 +437,8 @@ extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc
   f.ld_scales = p.ld_scales;
   f.stride_scales = p.stride_scales;
   f.groups = (d.in_dim + p.group - 1) / p.group;
-  const auto starts_on = [&](const void *p, uint64_t bytes, uint64_t ld, uint64_t stride) {
-    return (uintptr_t)p % bytes == 0 && ld % bytes == 0 && (d.num_experts == 1 || stride % bytes == 0);
-  };
-  const bool vec = d.in_dim % 32 == 0 && rows_are_vec(x, d.ld_x, 2) && starts_on(packed, p.group / 8, p.ld_packed, p.stride_packed) &&
-                   starts_on(scales, 2 * kChunk / p.group, p.ld_scales * 2, p.stride_scales * 2);
+  const bool vec = d.in_dim % 32 == 0 && rows_are_vec(x, d.ld_x, 2) && starts_on(d, packed, p.group / 8, p.ld_packed, p.stride_packed) &&
+                   starts_on(d, scales, 2 * kChunk / p.group, p.ld_scales * 2, p.stride_scales * 2);
   const uint64_t mean = mean_rows(d), experts = std::min<uint64_t>(d.num_experts, d.num_rows);
   // Rows of x and of weights that a warp takes together: experts of a few rows are left with several turns of eight
   // rows where one has many, which costs less than sixteen columns of MMAs for all.  Two blocks of weights pay where x is

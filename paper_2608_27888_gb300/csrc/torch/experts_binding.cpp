@@ -710,7 +710,7 @@ PyObject *linear4(PyObject *, PyObject *const *a, Py_ssize_t n_args) {
     residual = r.data_ptr();
   }
   Tensor y = fresh({m, N}, x.scalar_type(), x);
-  const size_t size = ntc_linear4_workspace(&d, &p, x.data_ptr(), rows);
+  const size_t size = ntc_linear4_workspace(&d, &p, x.data_ptr(), rows, (const uint8_t *)packed.data_ptr());
   Tensor ws = size ? fresh({(int64_t)size}, at::kByte, x) : Tensor();
   if (!done(ntc_linear4(&d, &p, x.data_ptr(), rows, offsets, (const uint8_t *)packed.data_ptr(), scales.data_ptr(), bias, residual,
                         y.data_ptr(), size ? ws.data_ptr() : nullptr, size, stream_of(x))))

@@ -160,7 +160,7 @@ def _load():
         "ntc_adamw": ([P, P, S, P, P, P, P, S, P], I),
         "ntc_pack4": ([P, P, I, ctypes.c_uint64, ctypes.c_uint64, P, P, P], I),
         "ntc_unpack4": ([P, P, P, P, ctypes.c_uint64, ctypes.c_uint64, P], I),
-        "ntc_linear4_workspace": ([P, P, P, P], S),
+        "ntc_linear4_workspace": ([P, P, P, P, P], S),
         "ntc_linear4": ([P, P, P, P, P, P, P, P, P, P, P, S, P], I),
         "ntc_last_error": ([], ctypes.c_char_p),
         "ntc_status_string": ([I], ctypes.c_char_p),
@@ -334,8 +334,8 @@ def ntc_unpack4(desc, packed, scales, w, ld_w, stride_w, stream):
     _check(_lib.ntc_unpack4(ctypes.byref(desc), packed, scales, w, ld_w, stride_w, stream))
 
 
-def ntc_linear4_workspace(desc, weights, x, rows) -> int:
-    return _lib.ntc_linear4_workspace(ctypes.byref(desc), ctypes.byref(weights), x, rows)
+def ntc_linear4_workspace(desc, weights, x, rows, packed) -> int:
+    return _lib.ntc_linear4_workspace(ctypes.byref(desc), ctypes.byref(weights), x, rows, packed)
 
 
 def ntc_linear4(desc, weights, x, rows, offsets, packed, scales, bias, residual, y, workspace, workspace_bytes, stream):

@@ -143,6 +143,38 @@ def test_many_rows(ntc, T, E, k, N, K, dtype):
     R.assert_within(y, want, bound)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [B, H])
+@pytest.mark.parametrize("T,E,k,N,K", [(40, 1, 1, 8192, 64), (33, 1, 1, 8065, 32), (64, 1, 1, 8300, 96), (100, 1, 1, 8129, 640),
+                                       (128, 1, 1, 8200, 2048), (17, 1, 1, 20000, 160), (300, 24, 2, 400, 160), (150, 16, 2, 520, 512),
+                                       (96, 16, 2, 600, 224), (1500, 33, 2, 257, 128), (700, 256, 8, 129, 96), (3000, 64, 1, 130, 1056),
+                                       (129, 1, 1, 8192, 64), (900, 2, 1, 128, 1056), (300, 4, 2, 200, 160)])
+def test_rows_in_between(ntc, T, E, k, N, K, group, dtype):
+    """Rows of whole 32s that start on 16 bytes: tiles of 32, 64 and 128 rows, experts of several, and, at the end, what
+    unpacking and the product for few rows take."""
+    y, want, bound = product(ntc, T, E, k, N, K, group, dtype, act="gelu", residual=True)
+    R.assert_within(y, want, bound)
+    y, want, bound = product(ntc, T, E, k, N, K, group, dtype, bias=False, seed=2, empty=False)
+    R.assert_within(y, want, bound)
+
+
+@pytest.mark.parametrize("T", [300, 900, 2500])
+def test_every_row_to_one_expert(ntc, T):
+    """The kernels are chosen for experts of as many rows; one that has them all is right too, and so are no rows at all."""
+    E, N, K = 32, 300, 128
+    packed, scales = ntc.pack4(randn(E, N, K, seed=T), group=32, dtype=B)
+    values = S.values(packed, scales, K, 32)
+    x = randn(T, K, seed=T + 1).to(B)
+    for e, live in ((0, T), (17, T), (E - 1, T - 5), (3, 0)):
+        offsets = torch.tensor([0] * (e + 1) + [live] * (E - e), dtype=torch.int32, device="cuda")
+        rows = torch.arange(T, dtype=torch.int32, device="cuda").flip(0).contiguous()
+        y = ntc.linear4(x, packed, scales, group=32, rows=rows, offsets=offsets)
+        want, _, bound, _ = R.linear(x, values, None, rows, offsets)
+        bound[:live] += 1.2 * R.UNIT[B] * (R.gathered(x, rows).abs()[:live] @ values[e].abs().t()) + R.TINY[B] * K
+        R.assert_within(y, want, bound)
+        assert not y[live:].any()
+
+
 @pytest.mark.parametrize("act", ["none", "relu", "leaky", "gelu", "silu"])
 @pytest.mark.parametrize("T", [4, 100])
 def test_activations(ntc, act, T):

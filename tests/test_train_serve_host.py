@@ -161,9 +161,9 @@ def test_pack4_pointer_refusals():
 def test_linear4_refusals():
     f, ws = ntc._lib.ntc_linear4, ntc._lib.ntc_linear4_workspace
     l, p = made(ntc.ntc_linear_desc, LINEAR, {}), made(ntc.ntc_pack4_desc, PACK, {})
-    assert ws(l, p, P, None) == 0 and ws(l, None, P, None) == 0
+    assert ws(l, p, P, None, P) == 0 and ws(l, None, P, None, P) == 0
     big = made(ntc.ntc_linear_desc, LINEAR, dict(num_rows=4000, num_x_rows=500))
-    need = ws(big, p, P, P)
+    need = ws(big, p, P, P, P)
     assert need >= 4 * 32 * 128 * 2  # the weights in 16 bits, rows of whole lines
     assert f(big, p, P, P, P, P, P, P, None, P, P, need - 1, None) == BAD and "workspace" in ntc.ntc_last_error()
     assert f(big, p, P, P, P, P, P, P, None, P, None, need, None) == BAD
