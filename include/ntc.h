@@ -521,7 +521,7 @@ NTC_API ntc_status ntc_linear_backward(const ntc_linear_desc *desc, const void *
                                        void *dw, float *db, void *workspace, size_t workspace_bytes,
                                        void *cuda_stream);
 
-/* Whether a kernel of ntc_linear or ntc_linear_backward gave up one of its
+/* Whether a kernel of ntc_linear, ntc_linear_backward or ntc_linear4 gave up one of its
  * bounded waits (200 ms in which its CTA issued no work) on the current device
  * since the last call of this: NTC_ERR_CUDA then (results since are invalid), and
  * the record is cleared.  Synchronises the stream. */

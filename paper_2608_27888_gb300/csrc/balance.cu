@@ -9,7 +9,12 @@
 // is read once; forward, a lane adds up its experts' p over its tokens in registers.  A
 // CTA's sums go to the workspace and a cluster of eight CTAs adds them in order; few tokens
 // are one CTA's, which ends the sum itself.  Instructions are the bound, a special function
-// or two an element among them.
+// or two an element among them: two experts go through one fp32x2 operation, a masked logit
+// is an exponent of 0 and not a test, and the next token's row is loaded ahead as it lies in
+// memory (65,536 tokens of 256 experts, sigmoid, bf16: 18.4 us, of which the second kernel
+// is 4 to 5; 51.7 without these, 5.2 at the copy's rate).  Above 256 experts a token has
+// several warps, for a lane that holds more than 32 spills (the gradient for 1,000 experts:
+// 29.5 us, 82 by one warp).
 #include "tokens.cuh"
 
 #include <cooperative_groups.h>

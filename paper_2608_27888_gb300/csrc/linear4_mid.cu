@@ -58,16 +58,6 @@ __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a_lo, uint32_t b_lo,
       "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accum)
       : "memory");
 }
-template <typename T>
-__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
-  if constexpr (std::is_same<T, __half>::value) {
-    const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
-  } else {
-    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
-  }
-}
 
 // A bounded wait: false after 200 ms, which sets the CTA's quit flag and the status word, or
 // once another thread's has given up.  The clock is looked at every 64 tries: reading it takes

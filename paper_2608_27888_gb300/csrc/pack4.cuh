@@ -1,4 +1,4 @@
-// Shared by the calls with weights in 4 bits (pack4.cu, linear4.cu).
+// Shared by the calls with weights in 4 bits (pack4.cu, linear4.cu, linear4_mid.cu).
 #pragma once
 
 #include "linear.cuh"
@@ -8,16 +8,16 @@ namespace ntc {
 // Why the descriptor is refused, NTC_OK if it is not.
 ntc_status check_pack4(const ntc_pack4_desc *d);
 
-// Eight weights of a word as pairs (0, 4), (1, 5), (2, 6), (3, 7) of the numbers q.  The
-// halves q + 8 go into the low mantissa bits of 128 (bf16), less 136, or of 1024 (fp16), less
-// 1032; a half four bits up is 16 (q + 8) there, which a sixteenth less 72 makes q: fp16 needs
-// one shift where bf16, with seven mantissa bits, needs three.  All of it is exact.
 // (a & b) | c in one instruction, which takes one constant that is no register.
 __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t v;
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(v) : "r"(a), "r"(b), "r"(c));
   return v;
 }
+// Eight weights of a word as pairs (0, 4), (1, 5), (2, 6), (3, 7) of the numbers q.  The
+// halves q + 8 go into the low mantissa bits of 128 (bf16), less 136, or of 1024 (fp16), less
+// 1032; a half four bits up is 16 (q + 8) there, which a sixteenth less 72 makes q: fp16 needs
+// one shift where bf16, with seven mantissa bits, needs three.  All of it is exact.
 template <typename T>
 __device__ __forceinline__ void numbers4(uint32_t w, uint32_t (&v)[4]) {
   if constexpr (std::is_same<T, __half>::value) {
@@ -38,6 +38,18 @@ __device__ __forceinline__ void numbers4(uint32_t w, uint32_t (&v)[4]) {
           __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&m), __bfloat162bfloat162(__ushort_as_bfloat16(0x4308)));
       v[i] = *reinterpret_cast<const uint32_t *>(&r);
     }
+  }
+}
+
+// Products of two pairs, rounded to 16 bits.
+template <typename T>
+__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
+  if constexpr (std::is_same<T, __half>::value) {
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+  } else {
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
   }
 }
 

@@ -35,6 +35,8 @@ class AdamW:
                        for p in self.params] if bits == 8 else None
         self.steps, self.captured = 0, captured
         if captured:
+            if not self.params:
+                raise ValueError("a captured step needs a parameter")
             dev = self.params[0].device
             self.steps = torch.zeros(1, dtype=torch.int32, device=dev)
             self.lr = torch.empty(1, device=dev)
@@ -52,12 +54,15 @@ class AdamW:
         CUDA tensor of one element)."""
         if self.names is not None:
             grads = [grads[n] for n in self.names]
-        if self.captured:
-            self.steps.add_(1)
-        else:
-            self.steps += 1
-        ntc.adamw(self.masters, grads, self.m, self.v, scales=self.scales, copies=self.copies, step=self.steps, lr=self.lr,
-                  grad_scale=grad_scale, **self.hyper)
+        steps = self.steps.add_(1) if self.captured else self.steps + 1
+        try:
+            ntc.adamw(self.masters, grads, self.m, self.v, scales=self.scales, copies=self.copies, step=steps, lr=self.lr,
+                      grad_scale=grad_scale, **self.hyper)
+        except Exception:
+            if self.captured:
+                self.steps.sub_(1)  # a step that was refused is none
+            raise
+        self.steps = steps
 
     def state(self) -> dict:
         """What a checkpoint holds beside the parameters (references, not copies)."""

@@ -379,3 +379,21 @@ def test_state_of_the_optimizer():
         assert torch.equal(w["a"], one.masters[0].to(B))
         with pytest.raises(ValueError, match="bits"):
             AdamW(w, bits=40 - bits).load(saved)
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_a_refused_step_is_none(captured):
+    """Gradients that do not fit change nothing, and the next step is the first."""
+    from paper_2608_27888_gb300.optim import AdamW
+    w = [torch.ones(40, device="cuda"), torch.ones(3, device="cuda")]
+    opt = AdamW(w, lr=0.1, captured=captured)
+    with pytest.raises(ValueError, match="grads"):
+        opt.step([torch.ones(40, device="cuda"), torch.ones(4, device="cuda")])
+    assert int(opt.steps) == 0 and all(bool((p == 1).all()) for p in w)
+    opt.step([torch.ones(40, device="cuda"), torch.ones(3, device="cuda")])
+    assert int(opt.steps) == 1
+    # the first step's change is the rate whatever the gradient, and the decay its hundredth
+    assert all(bool(((p - (1 - 0.1 * 0.01 - 0.1)).abs() < 1e-6).all()) for p in w)
+    AdamW([], captured=False).step([])
+    with pytest.raises(ValueError, match="captured"):
+        AdamW([], captured=True)

@@ -270,6 +270,44 @@ def test_streams_graphs_and_equal_bits(ntc):
         assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
 
 
+@pytest.mark.parametrize("T,N", [(500, 33), (700, 150), (3000, 120)])
+def test_tiles_in_between_read_nothing_else_and_repeat(ntc, T, N):
+    """64 experts: NaN and 255 around the operands, on both sides of a padded batch; two graphs at once on two streams."""
+    E, K = 64, 224
+    packed, scales = ntc.pack4(randn(E, N, K, seed=T).to(B), group=64)
+    x = torch.full((T + 2, K + 16), math.nan, dtype=B, device="cuda")
+    x[1:-1, 8:8 + K] = randn(T, K, seed=T + 1).to(B)
+    x = x[1:-1, 8:8 + K]
+    p = torch.full((E, N + 1, 112 + 32), 255, dtype=torch.uint8, device="cuda")
+    p[:, :N, 16:128] = packed
+    p = p[:, :N, 16:128]
+    s = torch.full((E, N + 1, scales.shape[-1] + 3), math.nan, dtype=B, device="cuda")
+    s[:, :N, 1:-2] = scales
+    s = s[:, :N, 1:-2]
+    res = torch.full((T, N + 5), math.nan, dtype=B, device="cuda")
+    res[:T - 9, 2:2 + N] = randn(T - 9, N, seed=9).to(B)
+    cuts = torch.sort(torch.randint(0, T - 8, (E + 1,), generator=torch.Generator(device="cuda").manual_seed(N), device="cuda"))[0].int()
+    cuts[0], cuts[-1] = 0, T - 9
+    call = lambda: ntc.linear4(x, p, s, group=64, offsets=cuts, residual=res[:, 2:2 + N], activation="silu")  # noqa: E731
+    y = call()
+    assert torch.equal(y, ntc.linear4(x.contiguous(), packed, scales, group=64, offsets=cuts, residual=res[:, 2:2 + N].contiguous(), activation="silu"))
+    assert bool(torch.isfinite(y).all()) and not y[T - 9:].any()
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for g in graphs:
+        with torch.cuda.graph(g):
+            outs.append(call())
+    x.copy_(randn(T, K, seed=3).to(B))
+    cuts[1:9] = cuts[9].clone()
+    torch.cuda.synchronize()
+    for g in graphs:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            g.replay()
+            g.replay()
+    torch.cuda.synchronize()
+    want = call()
+    assert not torch.equal(want, y) and torch.equal(outs[0], want) and torch.equal(outs[1], want)
+
+
 def test_no_rows(ntc):
     packed, scales = ntc.pack4(randn(2, 8, 64).to(B), group=32)
     y = ntc.linear4(torch.zeros(0, 64, dtype=B, device="cuda"), packed, scales, group=32, offsets=torch.zeros(3, dtype=torch.int32, device="cuda"))
