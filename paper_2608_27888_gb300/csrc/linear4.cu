@@ -332,10 +332,11 @@ uint64_t mean_rows(const ntc_linear_desc &d) {
 bool starts_on(const ntc_linear_desc &d, const void *p, uint64_t bytes, uint64_t ld, uint64_t stride) {
   return (uintptr_t)p % bytes == 0 && ld % bytes == 0 && (d.num_experts == 1 || stride % bytes == 0);
 }
-// Which kernels take the call.  The tcgen05 kernel has one CTA or two an SM, unpacks a tile of weights once for every 128
-// rows and wants tiles enough to fill the GPU (times in us, tcgen05 and the better of the others):
-//   64 tiles or more: 64 experts, 2,048 -> 1,024: 44 and 67 for 16 rows an expert, 52 and 160 for 32,
-//     66 and 117 for 64; 128 rows, 2,048 -> 32,768: 36 and 57; 64 tiles, 32 rows: 20 and 23.5;
+// Which kernels take the call.  The tcgen05 kernel has one CTA or two an SM, unpacks a tile of weights once for up to
+// 192 rows and wants tiles enough to fill the GPU (times in us, tcgen05 and the better of the others):
+//   64 tiles or more: 64 experts, 2,048 -> 1,024: 44 and 67 for 16 rows an expert, 52 and 160 for 32, 66 and 117 for 64;
+//     16 experts, 2,048 -> 2,048: 43 and 72 for 128, 63 and 73 for 192; 192 rows, 2,048 -> 16,384: 23 and 33; 64 tiles
+//     of 32 rows: 20 and 23.5;
 //   fewer: 32 tiles, 4,096 -> 4,096: 29 and 14 for 20 rows, 40 and 26 for 128;
 //   more rows: 256 an expert, 64 experts, 1,024 -> 2,048: 175 and 139.
 enum Path { kFew, kMid, kUnpack };
@@ -343,7 +344,7 @@ Path path_of(const ntc_linear_desc &d, const ntc_pack4_desc &p, const void *x, c
   if (d.num_rows == 0 || few_rows(d.num_rows)) return kFew;
   const uint64_t mean = mean_rows(d), tiles = std::min<uint64_t>(d.num_experts, d.num_rows) * ((d.out_dim + 127ull) / 128);
   const bool mid = d.in_dim % 32 == 0 && rows_are_vec(x, d.ld_x, 2) && starts_on(d, packed, 16, p.ld_packed, p.stride_packed);
-  if (mid && mean > 8 && mean <= 128 && tiles >= 64) return kMid;
+  if (mid && mean > 8 && mean <= 192 && tiles >= 64) return kMid;
   return mean <= 32 ? kFew : kUnpack;
 }
 

@@ -12,17 +12,20 @@
 //   a warp       issues the MMAs into one of two accumulators.  The proxy fence is its own: one
 //                by a copying thread waits for all of its copies in flight (with it, and a
 //                barrier of the CTA for each chunk, a chunk took 1,460 cycles).
-// Unpacked weights never touch HBM.  A chunk is a chain of some 700 cycles (wait, convert, store,
-// arrive, MMA, commit), which is the bound while an SM has too few of them at work: two CTAs an
-// SM fill each other's waits where NT is up to 64, and two sets of 256 threads in one CTA
-// where it is 128 (1,024 tokens of 2 of 16 experts, 2,048 -> 2,048: 50 us; 58 with two
-// CTAs, 72 by way of unpacked weights in HBM).  128 tokens of 4 of 32 experts, 1,024 -> 2,048:
-// 23.5 us, 1.5 TB/s of packed weights, 28 with two sets.  The conversion is done again for
-// every NT rows of an expert.
+// Unpacked weights never touch HBM.  The issuing warp's turn is the bound: a chunk's four MMAs
+// go out as the tensor pipe takes them (300 cycles for NT = 128), and the wait, its vote, the
+// fence and the commit between them take as long again, in which the pipe runs dry; the other
+// warps need about 640 cycles for a chunk.  So two CTAs an SM fill each other's waits where
+// NT is up to 64, and two sets of 256 threads in one CTA where it is more (1,024
+// tokens of 2 of 16 experts, 2,048 -> 2,048: 43 us, 0.4 PFLOP/s; 58 with two CTAs, 72 by way of
+// unpacked weights in HBM; 128 tokens of 4 of 32 experts, 1,024 -> 2,048: 25 us, 1.4 TB/s of
+// packed weights, 32 with two sets).  More stages, a third set, chunks of 128, one arrival a
+// warp and waiting for a chunk between the MMAs of the last one gave nothing or cost time.
 #include "linear4.cuh"
 #include "tcgen05.cuh"
 
 #include <atomic>
+#include <cmath>
 
 using namespace ntc;
 
@@ -36,6 +39,7 @@ constexpr int ctas(int NT) { return 3 - groups(NT); }
 constexpr int kStages = 4, kAhead = 2;  // x is that far ahead, and both the rest of the stages ahead of the MMAs
 constexpr int kDeep = 2;                // a thread's chunks of weights in registers
 constexpr uint32_t kRows = 128, kChunk = 64, kABytes = kRows * 128;
+constexpr uint32_t columns(int NT) { return NT > 128 ? 512 : NT * 2; }  // of TMEM: a power of two
 constexpr uint32_t stage_bytes(int NT) { return kABytes + (uint32_t)NT * 128; }
 
 struct Shared {
@@ -110,7 +114,7 @@ __global__ void __launch_bounds__(threads(NT), ctas(NT)) k_linear4_mid(const Mid
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
   const uint32_t K = a.depth, N = a.width, tiles = (N + kRows - 1) / kRows, chunks = (K + kChunk - 1) / kChunk;
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(saddr(&s.tmem)), "r"((uint32_t)NT * 2) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(saddr(&s.tmem)), "r"(columns(NT)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     fence_before();
   }
@@ -306,7 +310,7 @@ __global__ void __launch_bounds__(threads(NT), ctas(NT)) k_linear4_mid(const Mid
   fence_before();
   __syncthreads();
   fence_after();
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"((uint32_t)NT * 2) : "memory");
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(columns(NT)) : "memory");
 }
 
 template <typename T, int NT>
@@ -332,9 +336,16 @@ cudaError_t launch(const Mid4 &f, cudaStream_t st) {
 namespace ntc {
 
 cudaError_t launch_linear4_mid(const Mid4 &f, uint64_t mean, cudaStream_t st) {
+  // A tile has the rows of most experts, which are about their mean and twice its root where tokens choose by chance: an
+  // expert's next tile unpacks its weights again (2,048 -> 2,048, 16 experts of 128 rows: 43 us by tiles of 192, 51 by
+  // tiles of 128; of 96 rows: 42 and 41).
+  const double rows = f.a.num_experts == 1 ? (double)f.a.num_rows : (double)mean + 2.0 * std::sqrt((double)mean);
   const auto go = [&](auto type) {
     using T = decltype(type);
-    return mean <= 16 ? launch<T, 32>(f, st) : mean <= 32 ? launch<T, 64>(f, st) : launch<T, 128>(f, st);
+    return rows <= 32    ? launch<T, 32>(f, st)
+           : rows <= 64  ? launch<T, 64>(f, st)
+           : rows <= 128 ? launch<T, 128>(f, st)
+                         : launch<T, 192>(f, st);
   };
   return f.a.bf16 ? go(__nv_bfloat16()) : go(__half());
 }

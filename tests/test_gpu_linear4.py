@@ -148,9 +148,9 @@ def test_many_rows(ntc, T, E, k, N, K, dtype):
 @pytest.mark.parametrize("T,E,k,N,K", [(40, 1, 1, 8192, 64), (33, 1, 1, 8065, 32), (64, 1, 1, 8300, 96), (100, 1, 1, 8129, 640),
                                        (128, 1, 1, 8200, 2048), (17, 1, 1, 20000, 160), (300, 24, 2, 400, 160), (150, 16, 2, 520, 512),
                                        (96, 16, 2, 600, 224), (1500, 33, 2, 257, 128), (700, 256, 8, 129, 96), (3000, 64, 1, 130, 1056),
-                                       (129, 1, 1, 8192, 64), (900, 2, 1, 128, 1056), (300, 4, 2, 200, 160)])
+                                       (129, 1, 1, 8192, 64), (192, 1, 1, 8200, 224), (2000, 32, 2, 260, 352), (193, 1, 1, 8192, 64), (900, 2, 1, 128, 1056), (300, 4, 2, 200, 160)])
 def test_rows_in_between(ntc, T, E, k, N, K, group, dtype):
-    """Rows of whole 32s that start on 16 bytes: tiles of 32, 64 and 128 rows, experts of several, and, at the end, what
+    """Rows of whole 32s that start on 16 bytes: tiles of 32, 64, 128 and 192 rows, experts of several, and, at the end, what
     unpacking and the product for few rows take."""
     y, want, bound = product(ntc, T, E, k, N, K, group, dtype, act="gelu", residual=True)
     R.assert_within(y, want, bound)
@@ -158,7 +158,7 @@ def test_rows_in_between(ntc, T, E, k, N, K, group, dtype):
     R.assert_within(y, want, bound)
 
 
-@pytest.mark.parametrize("T", [300, 900, 2500])
+@pytest.mark.parametrize("T", [300, 900, 2500, 5000])
 def test_every_row_to_one_expert(ntc, T):
     """The kernels are chosen for experts of as many rows; one that has them all is right too, and so are no rows at all."""
     E, N, K = 32, 300, 128
@@ -270,7 +270,7 @@ def test_streams_graphs_and_equal_bits(ntc):
         assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
 
 
-@pytest.mark.parametrize("T,N", [(500, 33), (700, 150), (3000, 120)])
+@pytest.mark.parametrize("T,N", [(500, 33), (700, 150), (3000, 120), (9000, 60)])
 def test_tiles_in_between_read_nothing_else_and_repeat(ntc, T, N):
     """64 experts: NaN and 255 around the operands, on both sides of a padded batch; two graphs at once on two streams."""
     E, K = 64, 224
