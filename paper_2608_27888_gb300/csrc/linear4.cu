@@ -334,9 +334,9 @@ bool starts_on(const ntc_linear_desc &d, const void *p, uint64_t bytes, uint64_t
 }
 // Which kernels take the call.  The tcgen05 kernel has one CTA or two an SM, unpacks a tile of weights once for up to
 // 192 rows and wants tiles enough to fill the GPU (times in us, tcgen05 and the better of the others):
-//   64 tiles or more: 64 experts, 2,048 -> 1,024: 44 and 67 for 16 rows an expert, 52 and 160 for 32, 66 and 117 for 64;
+//   64 tiles or more: 64 experts, 2,048 -> 1,024: 43 and 67 for 16 rows an expert, 51 and 160 for 32, 65 and 117 for 64;
 //     16 experts, 2,048 -> 2,048: 43 and 72 for 128, 63 and 73 for 192; 192 rows, 2,048 -> 16,384: 23 and 33; 64 tiles
-//     of 32 rows: 20 and 23.5;
+//     of 32 rows: 16 and 23.5;
 //   fewer: 32 tiles, 4,096 -> 4,096: 29 and 14 for 20 rows, 40 and 26 for 128;
 //   more rows: 256 an expert, 64 experts, 1,024 -> 2,048: 175 and 139.
 enum Path { kFew, kMid, kUnpack };

@@ -16,7 +16,7 @@
 // go out as the tensor pipe takes them (300 cycles for NT = 128), and the wait, its vote, the
 // fence and the commit between them take as long again, in which the pipe runs dry; the other
 // warps need about 640 cycles for a chunk.  So two CTAs an SM fill each other's waits where
-// NT is up to 64, and two sets of 256 threads in one CTA where it is more (1,024
+// NT is up to 64 and tiles are enough, else two sets of 256 threads in one CTA (1,024
 // tokens of 2 of 16 experts, 2,048 -> 2,048: 43 us, 0.4 PFLOP/s; 58 with two CTAs, 72 by way of
 // unpacked weights in HBM; 128 tokens of 4 of 32 experts, 1,024 -> 2,048: 25 us, 1.4 TB/s of
 // packed weights, 32 with two sets).  More stages, a third set, chunks of 128, one arrival a
@@ -31,11 +31,9 @@ using namespace ntc;
 
 namespace {
 
-constexpr int kGroup = 256;                                      // threads that make a chunk
-constexpr int groups(int NT) { return NT >= 128 ? 2 : 1; }       // of them: one of two CTAs an SM, or two of one,
-constexpr int makers(int NT) { return kGroup * groups(NT); }     // which take every other chunk
-constexpr int threads(int NT) { return makers(NT) + 32; }
-constexpr int ctas(int NT) { return 3 - groups(NT); }
+// Threads that make a chunk; SETS of them, which take turns: one in each of two CTAs an SM, or two in one.
+constexpr int kGroup = 256;
+constexpr int threads(int SETS) { return kGroup * SETS + 32; }
 constexpr int kStages = 4, kAhead = 2;  // x is that far ahead, and both the rest of the stages ahead of the MMAs
 constexpr int kDeep = 2;                // a thread's chunks of weights in registers
 constexpr uint32_t kRows = 128, kChunk = 64, kABytes = kRows * 128;
@@ -103,15 +101,15 @@ __device__ __forceinline__ Unit unit_at(const Shared &s, uint32_t u, uint32_t NT
   return {s.which[lo], tile * kRows, (uint32_t)s.begin[lo] + m0, min((uint32_t)s.count[lo] - m0, NT)};
 }
 
-template <typename T, int NT>
-__global__ void __launch_bounds__(threads(NT), ctas(NT)) k_linear4_mid(const Mid4 f) {
-  constexpr int kGroups = groups(NT), kMakers = makers(NT);
+template <typename T, int NT, int SETS>
+__global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const Mid4 f) {
+  constexpr int kMakers = kGroup * SETS;
   constexpr uint32_t kStage = stage_bytes(NT), kPieces = NT * 8 / kGroup;  // of x, a thread's
   extern __shared__ uint8_t dynamic[];
   uint8_t *ring = (uint8_t *)(((uintptr_t)dynamic + 1023) & ~(uintptr_t)1023);
   Shared &s = *reinterpret_cast<Shared *>(ring + kStages * kStage);
   const LinearArgs &a = f.a;
-  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = tid / 32;
+  const uint32_t tid = threadIdx.x, lane = tid & 31, warp = uniform(tid / 32);
   const uint32_t K = a.depth, N = a.width, tiles = (N + kRows - 1) / kRows, chunks = (K + kChunk - 1) / kChunk;
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(saddr(&s.tmem)), "r"(columns(NT)) : "memory");
@@ -159,6 +157,7 @@ __global__ void __launch_bounds__(threads(NT), ctas(NT)) k_linear4_mid(const Mid
     // 128-byte-swizzled K-major operands: 8-row groups 1,024 bytes apart
     constexpr uint32_t kHi = (1024u >> 4) | (1u << 14) | (2u << 29);
     const uint32_t ring_lo = uniform(((base >> 4) & 0x3FFFu) | ((8192u >> 4) << 16));
+    const bool leader = elect_one();
     bool any = false;
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x, ++turn) {
       const uint32_t acc = turn & 1, d = tmem + acc * NT;
@@ -171,7 +170,7 @@ __global__ void __launch_bounds__(threads(NT), ctas(NT)) k_linear4_mid(const Mid
         asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
         any = true;
         const uint32_t alo = ring_lo + st * (kStage >> 4), blo = alo + (kABytes >> 4);
-        if (elect_one()) {
+        if (leader) {
 #pragma unroll
           for (uint32_t k = 0; k < kChunk / 16; ++k) mma_ss(d, alo + k * 2, blo + k * 2, kHi, idesc, (c | k) != 0);
           umma_commit(saddr(&s.empty[st]));
@@ -181,7 +180,7 @@ __global__ void __launch_bounds__(threads(NT), ctas(NT)) k_linear4_mid(const Mid
       }
     }
     if (!ok && any) {
-      if (elect_one()) umma_commit(saddr(&s.drain));
+      if (leader) umma_commit(saddr(&s.drain));
       __syncwarp();
       mbar_wait(saddr(&s.drain), 0);
     }
@@ -203,10 +202,10 @@ __global__ void __launch_bounds__(threads(NT), ctas(NT)) k_linear4_mid(const Mid
           to.scale = scales[k >> f.group_log];
         }
       };
-      const uint32_t c0 = (group + used) % kGroups;  // the group's first chunk: its stages stay the same
+      const uint32_t c0 = (group + used) % SETS;  // the group's first chunk: its stages stay the same
       Ahead next[kDeep];
 #pragma unroll
-      for (int q = 0; q < kDeep; ++q) load(c0 + q * kGroups, next[q]);
+      for (int q = 0; q < kDeep; ++q) load(c0 + q * SETS, next[q]);
       // this thread's pieces of x: rows mine / 8, + 32, ...; bytes (mine & 7) * 16 of a chunk
       const uint8_t *x[kPieces];
       uint32_t there = 0;  // bit i: row i is there
@@ -251,28 +250,27 @@ __global__ void __launch_bounds__(threads(NT), ctas(NT)) k_linear4_mid(const Mid
                        : "memory");
         }
         mbar_arrive(saddr(&s.full[st]));
-        load(c + kDeep * kGroups, now);
+        load(c + kDeep * SETS, now);
       };
 #pragma unroll 1
-      for (uint32_t c = c0; c < c0 + kAhead; c += kGroups) copy(c);
+      for (uint32_t c = c0; c < c0 + kAhead; c += SETS) copy(c);
 #pragma unroll 1
-      for (uint32_t c = c0; ok && c < chunks; c += kDeep * kGroups) {
+      for (uint32_t c = c0; ok && c < chunks; c += kDeep * SETS) {
 #pragma unroll
         for (int q = 0; q < kDeep; ++q)
-          if (c + q * kGroups < chunks) chunk(c + q * kGroups, next[q]);
+          if (c + q * SETS < chunks) chunk(c + q * SETS, next[q]);
       }
       used += chunks;
       const uint32_t acc = turn & 1;
       if (ok) ok = wait(saddr(&s.acc_full[acc]), (turn >> 1) & 1);
       if (!ok) break;
       fence_after();
-      // A thread has a column of the result and kPart of its rows: four warps have the 128 columns
-      constexpr uint32_t kPart = NT / (2 * kGroups);
-      const uint32_t col = o.n0 + (warp & 3) * 32 + lane, part = (warp >> 2) * kPart;
+      // A thread has a column of the result, four warps the 128 of 16 rows at a time
+      const uint32_t col = o.n0 + (warp & 3) * 32 + lane;
       constexpr int kBatch = 16;
       const float bias = a.bias && col < N ? a.bias[(uint64_t)o.e * N + col] : 0.0f;
 #pragma unroll 1
-      for (uint32_t r0 = part; r0 < part + kPart && r0 < o.rows; r0 += kBatch) {
+      for (uint32_t r0 = (warp >> 2) * kBatch; r0 < o.rows; r0 += kMakers / 128 * kBatch) {
         uint32_t r[kBatch];
         tmem_ld16(tmem + acc * NT + (((warp & 3) * 32) << 16) + r0, r);
         T add[kBatch];
@@ -313,22 +311,22 @@ __global__ void __launch_bounds__(threads(NT), ctas(NT)) k_linear4_mid(const Mid
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(columns(NT)) : "memory");
 }
 
-template <typename T, int NT>
+template <typename T, int NT, int SETS>
 cudaError_t launch(const Mid4 &f, cudaStream_t st) {
   static std::atomic<uint64_t> allowed{0};  // devices that know of the kernel's shared memory
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !((allowed.load() >> dev) & 1)) {
-    e = cudaFuncSetAttribute(k_linear4_mid<T, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_bytes(NT));
+    e = cudaFuncSetAttribute(k_linear4_mid<T, NT, SETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_bytes(NT));
     if (e != cudaSuccess) return e;
     if (dev < 64) allowed.fetch_or(1ull << dev);
   }
   // units that there can be: of every expert's last block, a row is enough
   const uint64_t tiles = (f.a.width + kRows - 1) / kRows, experts = std::min<uint64_t>(f.a.num_experts, f.a.num_rows);
   const uint64_t units = tiles * (f.a.num_rows / NT + experts);
-  const unsigned grid = (unsigned)std::min<uint64_t>(units, (uint64_t)sm_count() * ctas(NT));
-  return launch_pdl(k_linear4_mid<T, NT>, grid, threads(NT), shared_bytes(NT), st, f);
+  const unsigned grid = (unsigned)std::min<uint64_t>(units, (uint64_t)sm_count() * (3 - SETS));
+  return launch_pdl(k_linear4_mid<T, NT, SETS>, grid, threads(SETS), shared_bytes(NT), st, f);
 }
 
 }  // namespace
@@ -340,12 +338,15 @@ cudaError_t launch_linear4_mid(const Mid4 &f, uint64_t mean, cudaStream_t st) {
   // expert's next tile unpacks its weights again (2,048 -> 2,048, 16 experts of 128 rows: 43 us by tiles of 192, 51 by
   // tiles of 128; of 96 rows: 42 and 41).
   const double rows = f.a.num_experts == 1 ? (double)f.a.num_rows : (double)mean + 2.0 * std::sqrt((double)mean);
+  // One CTA an SM has two sets of threads to itself; where there are tiles for two CTAs each has one (256 rows of 8
+  // experts, 1,024 -> 2,048, 128 tiles: 11.1 us by two sets, 14.4 by one; 512 rows of 32, 512 tiles: 32.4 and 25.0).
+  const bool two = std::min<uint64_t>(f.a.num_experts, f.a.num_rows) * ((f.a.width + kRows - 1) / kRows) <= (uint64_t)sm_count();
   const auto go = [&](auto type) {
     using T = decltype(type);
-    return rows <= 32    ? launch<T, 32>(f, st)
-           : rows <= 64  ? launch<T, 64>(f, st)
-           : rows <= 128 ? launch<T, 128>(f, st)
-                         : launch<T, 192>(f, st);
+    return rows <= 32    ? (two ? launch<T, 32, 2>(f, st) : launch<T, 32, 1>(f, st))
+           : rows <= 64  ? (two ? launch<T, 64, 2>(f, st) : launch<T, 64, 1>(f, st))
+           : rows <= 128 ? launch<T, 128, 2>(f, st)
+                         : launch<T, 192, 2>(f, st);
   };
   return f.a.bf16 ? go(__nv_bfloat16()) : go(__half());
 }
