@@ -12,6 +12,9 @@
 // rounded.
 // Few (expert, rows) pairs are split along K over the warps of a CTA, whose sums meet
 // in shared memory in a fixed order.
+// Latency of the loads is the bound at four warps a scheduler (64 tokens of 4 of 32 experts,
+// 1,024 -> 2,048, fp16: 25 us, 1.4 TB/s of packed weights; 61 through shared memory), a launch
+// for a token (8 of 64 experts, 2,048 -> 1,024: 8 us).
 // More rows per expert, and tiles enough: linear4_mid.cu, whose tcgen05 tiles unpack the
 // weights on their way into shared memory.
 // Many rows per expert, or operands that do not start on 16 bytes: the weights of experts with
@@ -339,6 +342,8 @@ bool starts_on(const ntc_linear_desc &d, const void *p, uint64_t bytes, uint64_t
 //     of 32 rows: 16 and 23.5;
 //   fewer: 32 tiles, 4,096 -> 4,096: 29 and 14 for 20 rows, 40 and 26 for 128;
 //   more rows: 256 an expert, 64 experts, 1,024 -> 2,048: 175 and 139.
+//   fewer rows: 8 an expert, 2,048 -> 2,048, 32 experts: 43 and 40; 64 experts, 1,024 -> 4,096: 78 and 69 (the other
+//     way only in bf16 with groups of 32, 25 and 36).
 enum Path { kFew, kMid, kUnpack };
 Path path_of(const ntc_linear_desc &d, const ntc_pack4_desc &p, const void *x, const uint8_t *packed) {
   if (d.num_rows == 0 || few_rows(d.num_rows)) return kFew;
@@ -443,7 +448,7 @@ extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc
   const uint64_t mean = mean_rows(d), experts = std::min<uint64_t>(d.num_experts, d.num_rows);
   // Rows of x and of weights that a warp takes together: experts of a few rows are left with several turns of eight
   // rows where one has many, which costs less than sixteen columns of MMAs for all.  Two blocks of weights pay where x is
-  // read for two (128 tokens of 4 of 32 experts, 1,024 -> 2,048: 35 us, 47 with one), and spill registers beside four.
+  // read for two (128 tokens of 4 of 32 experts, 1,024 -> 2,048: 35 us, 47 with one, by this kernel), and spill registers beside four.
   const int nt = d.num_rows <= 8 || mean <= 4 ? 1 : mean <= 16 ? 2 : 4, mt = nt == 2 ? 2 : 1;
   const uint64_t units = experts * ((d.out_dim + 16 * mt - 1) / (16 * mt));
   // Warps along K until the warps that the SMs hold are at work.
