@@ -148,7 +148,7 @@ def test_many_rows(ntc, T, E, k, N, K, dtype):
 @pytest.mark.parametrize("T,E,k,N,K", [(40, 1, 1, 8192, 64), (33, 1, 1, 8065, 32), (64, 1, 1, 8300, 96), (100, 1, 1, 8129, 640),
                                        (128, 1, 1, 8200, 2048), (17, 1, 1, 20000, 160), (300, 24, 2, 400, 160), (150, 16, 2, 520, 512),
                                        (96, 16, 2, 600, 224), (1500, 33, 2, 257, 128), (700, 256, 8, 129, 96), (3000, 64, 1, 130, 1056),
-                                       (900, 64, 3, 330, 160), (129, 1, 1, 8192, 64), (192, 1, 1, 8200, 224), (2000, 32, 2, 260, 352), (193, 1, 1, 8192, 64), (900, 2, 1, 128, 1056), (300, 4, 2, 200, 160)])
+                                       (900, 64, 3, 330, 160), (11000, 1024, 1, 130, 64), (129, 1, 1, 8192, 64), (192, 1, 1, 8200, 224), (2000, 32, 2, 260, 352), (193, 1, 1, 8192, 64), (900, 2, 1, 128, 1056), (300, 4, 2, 200, 160)])
 def test_rows_in_between(ntc, T, E, k, N, K, group, dtype):
     """Rows of whole 32s that start on 16 bytes: tiles of 32, 64, 128 and 192 rows, experts of several, and, at the end, what
     unpacking and the product for few rows take."""
