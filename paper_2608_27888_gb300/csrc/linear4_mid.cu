@@ -124,7 +124,6 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
     s.quit = 0;
   }
   pdl_wait();
-  pdl_trigger();
   if (warp == 0) {
     list_experts(a, lane, s.begin, s.count, s.which, &s.active, &s.live);
     __syncwarp();
@@ -144,6 +143,9 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
     if (lane == 0) s.units = base;
   }
   __syncthreads();
+  // Not before this CTA has its tensor memory: a dependent CTA that took the columns first would wait for this grid's end,
+  // and this grid for the columns.
+  pdl_trigger();
   fence_after();
   const uint32_t tmem = uniform(s.tmem), base = uniform(saddr(ring)), units = uniform(s.units);
   const auto wait = [&](uint32_t bar, uint32_t parity) {  // by a whole warp
