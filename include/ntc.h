@@ -672,11 +672,11 @@ NTC_API ntc_status ntc_unpack4(const ntc_pack4_desc *desc, const uint8_t *packed
 
 /* ntc_linear (without z) with weights in 4 bits (ld_packed and ld_scales below 2^26).
  * desc's ld_w, stride_w and ld_z are not read; its type, in_dim, out_dim and
- * num_experts are those of `weights`.  Calls of few rows per expert multiply the
- * numbers q themselves, exact in 16 bits, and the groups' fp32 sums by their scales.
- * Others round scale * q to 16 bits first, as ntc_unpack4 does: on the way to the tensor
- * cores, or in the workspace where x or packed do not start on 16 bytes, in_dim is not a
- * multiple of 32, the experts' tiles are few or their rows very many. */
+ * num_experts are those of `weights`.  z_i is the sum over the groups of scale * (the
+ * group's sum of q x): the numbers q are exact in 16 bits, both sums and the product with
+ * the scale are fp32, and no scale * q is rounded, however many the rows.  Calls of many rows per expert
+ * copy x or packed to the workspace where their rows do not start on 16 bytes or in_dim is not a
+ * multiple of 32. */
 NTC_API size_t ntc_linear4_workspace(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, const void *x,
                                      const int32_t *rows, const uint8_t *packed);
 NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, const void *x,

@@ -15,10 +15,8 @@
 // Latency of the loads is the bound at four warps a scheduler (64 tokens of 4 of 32 experts,
 // 1,024 -> 2,048, fp16: 25 us, 1.4 TB/s of packed weights; 61 through shared memory), a launch
 // for a token (8 of 64 experts, 2,048 -> 1,024: 8 us).
-// More rows per expert, and tiles enough: linear4_mid.cu, whose tcgen05 tiles unpack the
-// weights on their way into shared memory.
-// Many rows per expert, or operands that do not start on 16 bytes: the weights of experts with
-// rows are unpacked to 16 bits in the workspace and the product of linear.cu takes them.
+// More rows per expert: linear4_mid.cu, whose tcgen05 tiles unpack the weights on their way into
+// shared memory, with the same formula; operands that do not start on 16 bytes are copied for it.
 #include "linear4.cuh"
 
 using namespace ntc;
@@ -326,6 +324,44 @@ cudaError_t launch(const FewArgs &f, uint64_t units, cudaStream_t st) {
   return launch_pdl(k_linear4_few<T, NT, MT, VEC, GROUP>, grid, kThreads, 0, st, f);
 }
 
+// Operands as the tcgen05 kernel takes them: rows that start on 16 bytes and a contraction of whole 32s.  Others are copied
+// to the workspace first, a row in `pitch` bytes of which those past its own are 0.
+struct Copy {
+  const uint8_t *from;
+  uint8_t *to;
+  const int32_t *offsets;  // weights: only those of experts with rows (NULL: all)
+  uint64_t ld, stride;     // bytes from row to row and from matrix to matrix
+  uint64_t pieces;         // 16 bytes of a row in the copy, all rows'; 0: no copy
+  uint32_t rows, bytes, pitch;  // of a matrix; of a row
+  uint32_t odd;            // rows of single bytes, not of 16-bit numbers
+  int32_t num_rows;
+};
+struct Copies {
+  Copy c[2];
+};
+__global__ void __launch_bounds__(kThreads) k_linear4_copy(const Copies all) {
+  const Copy &c = all.c[blockIdx.y];
+  pdl_wait();
+  pdl_trigger();
+  const uint32_t per = c.pitch / 16;
+  for (uint64_t i = (uint64_t)blockIdx.x * kThreads + threadIdx.x; i < c.pieces; i += (uint64_t)gridDim.x * kThreads) {
+    const uint64_t row = i / per, e = row / c.rows;
+    const uint32_t at = (uint32_t)(i - row * per) * 16;
+    if (c.offsets && offset_at(c.offsets, (uint32_t)e, c.num_rows) >= offset_at(c.offsets, (uint32_t)e + 1, c.num_rows)) continue;
+    const uint8_t *p = c.from + e * c.stride + (row - e * c.rows) * c.ld + at;
+    const int32_t have = (int32_t)c.bytes - (int32_t)at;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (have >= 16 && ((uintptr_t)p & 15) == 0) {
+      v = *(const uint4 *)p;
+    } else if (c.odd) {
+      v = make_uint4(load_bytes(p, have), load_bytes(p + 4, have - 4), load_bytes(p + 8, have - 8), load_bytes(p + 12, have - 12));
+    } else if (have > 0) {
+      v = load_x<false>((const uint16_t *)p, 0, (uint32_t)min(have, 16) / 2);
+    }
+    *(uint4 *)(c.to + i * 16) = v;
+  }
+}
+
 // Rows of an expert that has any, on average, where the choices are spread evenly.
 uint64_t mean_rows(const ntc_linear_desc &d) {
   const uint64_t experts = std::min<uint64_t>(d.num_experts, d.num_rows);
@@ -335,33 +371,32 @@ uint64_t mean_rows(const ntc_linear_desc &d) {
 bool starts_on(const ntc_linear_desc &d, const void *p, uint64_t bytes, uint64_t ld, uint64_t stride) {
   return (uintptr_t)p % bytes == 0 && ld % bytes == 0 && (d.num_experts == 1 || stride % bytes == 0);
 }
-// Which kernels take the call.  The tcgen05 kernel has one CTA or two an SM, unpacks a tile of weights once for up to
-// 192 rows and wants tiles enough to fill the GPU (times in us, tcgen05 and the better of the others):
-//   64 tiles or more: 64 experts, 2,048 -> 1,024: 43 and 67 for 16 rows an expert, 51 and 160 for 32, 65 and 117 for 64;
-//     16 experts, 2,048 -> 2,048: 43 and 72 for 128, 63 and 73 for 192; 192 rows, 2,048 -> 16,384: 23 and 33; 64 tiles
-//     of 32 rows: 16 and 23.5;
-//   fewer: 32 tiles, 4,096 -> 4,096: 29 and 14 for 20 rows, 40 and 26 for 128;
-//   more rows: 256 an expert, 64 experts, 1,024 -> 2,048: 175 and 139.
-//   fewer rows: 8 an expert, 2,048 -> 2,048, 32 experts: 43 and 40; 64 experts, 1,024 -> 4,096: 78 and 69 (the other
-//     way only in bf16 with groups of 32, 25 and 36).
-enum Path { kFew, kMid, kUnpack };
-Path path_of(const ntc_linear_desc &d, const ntc_pack4_desc &p, const void *x, const uint8_t *packed) {
-  if (d.num_rows == 0 || few_rows(d.num_rows)) return kFew;
+// Whether the tcgen05 kernel takes x and the packed weights as they are.
+bool x_whole(const ntc_linear_desc &d, const void *x) { return d.in_dim % 32 == 0 && rows_are_vec(x, d.ld_x, 2); }
+bool packed_whole(const ntc_linear_desc &d, const ntc_pack4_desc &p, const uint8_t *packed) {
+  return d.in_dim % 32 == 0 && starts_on(d, packed, 16, p.ld_packed, p.stride_packed);
+}
+// Whether the tcgen05 kernel takes the call.  It unpacks a tile of weights once for up to 192 rows.
+bool by_tiles(const ntc_linear_desc &d, const ntc_pack4_desc &p, const void *x, const uint8_t *packed) {
+  if (d.num_rows == 0 || few_rows(d.num_rows)) return false;
   const uint64_t mean = mean_rows(d), tiles = std::min<uint64_t>(d.num_experts, d.num_rows) * ((d.out_dim + 127ull) / 128);
-  const bool mid = d.in_dim % 32 == 0 && rows_are_vec(x, d.ld_x, 2) && starts_on(d, packed, 16, p.ld_packed, p.stride_packed);
-  if (mid && mean > 8 && mean <= 192 && tiles >= 64) return kMid;
-  return mean <= 32 ? kFew : kUnpack;
+  if (mean > 32) return true;
+  return mean > 8 && tiles >= 64 && x_whole(d, x) && packed_whole(d, p, packed);
 }
 
-uint64_t pitch_of(uint64_t K) { return (K + 63) / 64 * 64; }  // of the unpacked weights: rows of whole 128-byte lines
-uint64_t unpacked_bytes(const ntc_linear_desc &d) {
-  return ((uint64_t)d.num_experts * d.out_dim * pitch_of(d.in_dim) * 2 + 255) / 256 * 256;
+uint32_t whole_32s(uint32_t K) { return (K + 31) / 32 * 32; }
+uint64_t round256(uint64_t n) { return (n + 255) / 256 * 256; }
+uint64_t x_bytes(const ntc_linear_desc &d, const void *x) {
+  return x_whole(d, x) ? 0 : round256(d.num_x_rows * whole_32s(d.in_dim) * 2);
+}
+uint64_t packed_bytes(const ntc_linear_desc &d, const ntc_pack4_desc &p, const uint8_t *packed) {
+  return packed_whole(d, p, packed) ? 0 : round256((uint64_t)d.num_experts * d.out_dim * (whole_32s(d.in_dim) / 2));
 }
 
 ntc_status check(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, ntc_linear_desc *d) {
   if (!desc) return op_fail(NTC_ERR_INVALID_ARG, "null descriptor");
   *d = *desc;
-  d->ld_w = pitch_of(d->in_dim);
+  d->ld_w = d->in_dim;
   d->stride_w = d->ld_w * d->out_dim;
   d->ld_z = d->out_dim;
   if (ntc_status s = check_linear(d)) return s;
@@ -377,11 +412,10 @@ ntc_status check(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, ntc
 }  // namespace
 
 extern "C" NTC_API size_t ntc_linear4_workspace(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, const void *x,
-                                                const int32_t *rows, const uint8_t *packed) {
+                                                const int32_t *, const uint8_t *packed) {
   ntc_linear_desc d;
-  if (check(desc, weights, &d) || path_of(d, *weights, x, packed) != kUnpack) return 0;
-  // the weights lie at the start of an aligned workspace, whose address has no part in the rest
-  return unpacked_bytes(d) + ntc_linear_workspace(&d, x, rows, (const void *)256);
+  if (check(desc, weights, &d) || !by_tiles(d, *weights, x, packed)) return 0;
+  return x_bytes(d, x) + packed_bytes(d, *weights, packed);
 }
 
 extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc_pack4_desc *weights, const void *x,
@@ -400,15 +434,6 @@ extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc
   const ntc_pack4_desc &p = *weights;
   cudaStream_t st = (cudaStream_t)cuda_stream;
   const bool bf16 = d.type == NTC_TYPE_BF16;
-  const Path path = path_of(d, p, x, packed);
-  if (path == kUnpack) {
-    const Unpack u = {packed, (const uint16_t *)scales, (uint16_t *)workspace, offsets, p.ld_packed, p.stride_packed, p.ld_scales,
-                      p.stride_scales, d.ld_w, d.stride_w, d.in_dim, d.out_dim, d.num_experts, p.group, (int32_t)d.num_rows};
-    if (cudaError_t e = launch_unpack4(u, bf16, st)) return op_cuda(e, "ntc_linear4");
-    const size_t used = unpacked_bytes(d);
-    return ntc_linear(&d, x, rows, offsets, workspace, bias, residual, y, nullptr, (uint8_t *)workspace + used,
-                      workspace_bytes - used, cuda_stream);
-  }
   LinearArgs a{};
   a.rows = rows;
   a.offsets = offsets;
@@ -427,11 +452,28 @@ extern "C" NTC_API ntc_status ntc_linear4(const ntc_linear_desc *desc, const ntc
   a.activation = d.activation;
   a.slope = d.leaky_slope;
   a.bf16 = bf16;
-  if (path == kMid) {
+  if (by_tiles(d, p, x, packed)) {
     a.status = linear_status_word();
     if (!a.status) return op_fail(NTC_ERR_CUDA, "no usable current CUDA device");
-    const Mid4 m = {a, packed, (const uint16_t *)scales, p.ld_packed, p.stride_packed, p.ld_scales, p.stride_scales,
-                    p.group == 32 ? 5u : p.group == 64 ? 6u : 7u};
+    Mid4 m = {a, packed, (const uint16_t *)scales, p.ld_packed, p.stride_packed, p.ld_scales, p.stride_scales,
+              p.group == 32 ? 5u : p.group == 64 ? 6u : 7u};
+    Copies all{};
+    uint8_t *ws = (uint8_t *)workspace;
+    const uint32_t K = whole_32s(d.in_dim);
+    m.a.depth = K;
+    if (const uint64_t bytes = x_bytes(d, x)) {
+      all.c[0] = {(const uint8_t *)x, ws, nullptr, d.ld_x * 2, 0, d.num_x_rows * (K / 8), (uint32_t)d.num_x_rows, d.in_dim * 2, K * 2, 0, 0};
+      m.a.x = ws, m.a.ld_x = K, ws += bytes;
+    }
+    if (packed_bytes(d, p, packed)) {
+      all.c[1] = {packed, ws, offsets, p.ld_packed, p.stride_packed, (uint64_t)d.num_experts * d.out_dim * (K / 32), d.out_dim,
+                  (d.in_dim + 1) / 2, K / 2, 1, (int32_t)d.num_rows};
+      m.packed = ws, m.ld_packed = K / 2, m.stride_packed = (uint64_t)d.out_dim * (K / 2);
+    }
+    if (const uint64_t pieces = std::max(all.c[0].pieces, all.c[1].pieces)) {
+      const unsigned ctas = (unsigned)std::min<uint64_t>((pieces + kThreads - 1) / kThreads, (uint64_t)sm_count() * 8);
+      if (cudaError_t e = launch_pdl(k_linear4_copy, dim3(ctas, 2), kThreads, 0, st, all)) return op_cuda(e, "ntc_linear4");
+    }
     return op_cuda(launch_linear4_mid(m, mean_rows(d), st), "ntc_linear4");
   }
   FewArgs f{};

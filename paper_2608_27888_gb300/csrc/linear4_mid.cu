@@ -1,26 +1,22 @@
 // The experts' product with weights in 4 bits, for more rows per expert than registers hold.
 //
+//   y_i = act(sum over groups s_{n,j} (sum over the group q_nk x_{rows[i],k}) + b) + residual
+//
 // A tile is 128 rows of an expert's weights times NT of its rows of x, the weights being the
 // M operand of tcgen05.mma: then few rows of x waste no tensor lanes, and a lane of the
-// accumulator is a column of the result.  Chunks of 64 of the contraction pass through a ring
-// of shared-memory stages:
+// accumulator is a column of the result, whose scales are a thread's own.  The operand is the
+// numbers q, exact in 16 bits; a group's sum leaves tensor memory for fp32 registers times its
+// scale, so that no product of a scale and a weight is rounded (or passes fp16's largest
+// number), as for few rows.  Chunks of 64 of the contraction pass through a ring of
+// shared-memory stages:
 //   256 threads  weights: a thread has half of a row's chunk, 16 bytes, in registers two chunks
-//                ahead; the numbers times the group's scale, rounded to 16 bits as unpack4
-//                does, go to the stage as the swizzle wants them.  x: 16-byte cp.async, rows
-//                gathered by index, two chunks ahead, which arrive at the stage's barrier by
-//                themselves.  At the end the epilogue.
-//   a warp       issues the MMAs into one of two accumulators.  The proxy fence is its own: one
-//                by a copying thread waits for all of its copies in flight (with it, and a
-//                barrier of the CTA for each chunk, a chunk took 1,460 cycles).
-// Unpacked weights never touch HBM.  The issuing warp's turn is the bound: a chunk's four MMAs
-// go out as the tensor pipe takes them (300 cycles for NT = 128), and the wait, its vote, the
-// fence and the commit between them take as long again, in which the pipe runs dry; the other
-// warps need about 640 cycles for a chunk.  So two CTAs an SM fill each other's waits where
-// NT is up to 64 and tiles are enough, else two sets of 256 threads in one CTA (1,024
-// tokens of 2 of 16 experts, 2,048 -> 2,048: 43 us, 0.4 PFLOP/s; 58 with two CTAs, 72 by way of
-// unpacked weights in HBM; 128 tokens of 4 of 32 experts, 1,024 -> 2,048: 25 us, 1.4 TB/s of
-// packed weights, 32 with two sets).  More stages, a third set, chunks of 128, one arrival a
-// warp and waiting for a chunk between the MMAs of the last one gave nothing or cost time.
+//                ahead; the numbers go to the stage as the swizzle wants them.  x: 16-byte
+//                cp.async, rows gathered by index, two chunks ahead, which arrive at the
+//                stage's barrier by themselves.  The sums of the groups that are complete,
+//                three chunks behind.  At the end the epilogue.
+//   a warp       issues the MMAs, a group into one of two or four accumulators.  The proxy
+//                fence is its own: one by a copying thread waits for all of its copies in flight.
+// Unpacked weights never touch HBM.
 #include "linear4.cuh"
 #include "tcgen05.cuh"
 
@@ -36,12 +32,17 @@ constexpr int kGroup = 256;
 constexpr int threads(int SETS) { return kGroup * SETS + 32; }
 constexpr int kStages = 4, kAhead = 2;  // x is that far ahead, and both the rest of the stages ahead of the MMAs
 constexpr int kDeep = 2;                // a thread's chunks of weights in registers
+// Sums are taken that many chunks behind: a set has a chunk's groups added before it waits for the stage of two chunks on,
+// which is free once the MMAs of two chunks before are through.  So the MMAs never wait for an accumulator that is added
+// only after they are: with two accumulators a chunk has at most one group (NT 192 takes no groups of 32).
+constexpr uint32_t kLag = 3;
 constexpr uint32_t kRows = 128, kChunk = 64, kABytes = kRows * 128;
-constexpr uint32_t columns(int NT) { return NT > 128 ? 512 : NT * 2; }  // of TMEM: a power of two
+constexpr uint32_t buffers(int NT) { return NT > 128 ? 2 : 4; }  // accumulators
+constexpr uint32_t columns(int NT) { return NT > 128 ? 512 : NT * buffers(NT); }  // of TMEM: a power of two
 constexpr uint32_t stage_bytes(int NT) { return kABytes + (uint32_t)NT * 128; }
 
 struct Shared {
-  uint64_t full[8], empty[8], acc_full[2], acc_empty[2], drain;
+  uint64_t full[kStages], empty[kStages], acc_full[4], acc_empty[4], drain;
   uint32_t tmem, active, live, units, quit;
   int32_t begin[NTC_MAX_EXPERTS];   // of the experts with rows: first row,
   int32_t count[NTC_MAX_EXPERTS];   // rows,
@@ -80,12 +81,6 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile
   return true;
 }
 
-// What a thread has loaded of a chunk: 32 weights of a row and their scale, twice in a word.
-struct Ahead {
-  uint4 w;
-  uint32_t scale;
-};
-
 // A unit: an expert's tile of weights and a block of its rows.
 struct Unit {
   uint32_t e, n0, from, rows;
@@ -105,12 +100,17 @@ template <typename T, int NT, int SETS>
 __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const Mid4 f) {
   constexpr int kMakers = kGroup * SETS;
   constexpr uint32_t kStage = stage_bytes(NT), kPieces = NT * 8 / kGroup;  // of x, a thread's
+  constexpr uint32_t kAcc = buffers(NT);
+  constexpr int kBatch = 16;                          // rows of x that a thread adds or writes together
+  constexpr uint32_t kApart = kMakers / 128 * kBatch;  // four warps have the 128 columns of the result, the next four the next rows
+  constexpr uint32_t kBatches = (NT + kApart - 1) / kApart;
   extern __shared__ uint8_t dynamic[];
   uint8_t *ring = (uint8_t *)(((uintptr_t)dynamic + 1023) & ~(uintptr_t)1023);
   Shared &s = *reinterpret_cast<Shared *>(ring + kStages * kStage);
   const LinearArgs &a = f.a;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = uniform(tid / 32);
   const uint32_t K = a.depth, N = a.width, tiles = (N + kRows - 1) / kRows, chunks = (K + kChunk - 1) / kChunk;
+  const uint32_t group_mask = (1u << f.group_log) - 1, groups = (K + group_mask) >> f.group_log;
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(saddr(&s.tmem)), "r"(columns(NT)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
   }
   if (tid == 0) {
     for (int i = 0; i < kStages; ++i) mbar_init(saddr(&s.full[i]), 2 * kGroup), mbar_init(saddr(&s.empty[i]), 1);
-    for (int i = 0; i < 2; ++i) mbar_init(saddr(&s.acc_full[i]), 1), mbar_init(saddr(&s.acc_empty[i]), kMakers / 32);
+    for (uint32_t i = 0; i < kAcc; ++i) mbar_init(saddr(&s.acc_full[i]), 1), mbar_init(saddr(&s.acc_empty[i]), kMakers / 32);
     mbar_init(saddr(&s.drain), 1);
     mbar_init_fence();
     s.quit = 0;
@@ -152,32 +152,45 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
     return __all_sync(0xFFFFFFFFu, wait_for(bar, parity, &s.quit, a.status)) != 0;
   };
   bool ok = true;
-  uint32_t used = 0, turn = 0;  // chunks and tiles that this CTA has gone through
+  uint32_t used = 0, summed = 0;  // chunks and groups that this CTA has gone through
   if (warp == kMakers / 32) {
     constexpr uint32_t kBf16 = std::is_same<T, __half>::value ? 0 : 1;
     constexpr uint32_t idesc = (1u << 4) | (kBf16 << 7) | (kBf16 << 10) | ((uint32_t)(NT >> 3) << 17) | ((kRows >> 4) << 24);
     // 128-byte-swizzled K-major operands: 8-row groups 1,024 bytes apart
     constexpr uint32_t kHi = (1024u >> 4) | (1u << 14) | (2u << 29);
     const uint32_t ring_lo = uniform(((base >> 4) & 0x3FFFu) | ((8192u >> 4) << 16));
+    const uint32_t steps = uniform(f.group_log == 5 ? 2 : 4);  // MMAs (16 of the contraction) of a chunk that are of one group
     const bool leader = elect_one();
     bool any = false;
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x, ++turn) {
-      const uint32_t acc = turn & 1, d = tmem + acc * NT;
-      ok = wait(saddr(&s.acc_empty[acc]), ((turn >> 1) & 1) ^ 1);
-      fence_after();
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      uint32_t acc = 0;
       for (uint32_t c = 0; ok && c < chunks; ++c, ++used) {
         const uint32_t st = used % kStages;
         ok = wait(saddr(&s.full[st]), (used / kStages) & 1);
         if (!ok) break;
         asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-        any = true;
         const uint32_t alo = ring_lo + st * (kStage >> 4), blo = alo + (kABytes >> 4);
-        if (leader) {
+        for (uint32_t k0 = 0; k0 < 4 && c * kChunk + k0 * 16 < K; k0 += steps) {
+          const uint32_t at = c * kChunk + k0 * 16;
+          const bool first = (at & group_mask) == 0;
+          if (first) {
+            acc = summed % kAcc;
+            ok = wait(saddr(&s.acc_empty[acc]), ((summed / kAcc) & 1) ^ 1);
+            if (!ok) break;
+            fence_after();
+            ++summed;
+          }
+          any = true;
+          if (leader) {
+            const uint32_t d = tmem + acc * NT;
 #pragma unroll
-          for (uint32_t k = 0; k < kChunk / 16; ++k) mma_ss(d, alo + k * 2, blo + k * 2, kHi, idesc, (c | k) != 0);
-          umma_commit(saddr(&s.empty[st]));
-          if (c + 1 == chunks) umma_commit(saddr(&s.acc_full[acc]));
+            for (uint32_t k = 0; k < 4; ++k)  // past K there is nothing to add
+              if (k < steps && at + k * 16 < K) mma_ss(d, alo + (k0 + k) * 2, blo + (k0 + k) * 2, kHi, idesc, !first || k != 0);
+            if (((at + steps * 16) & group_mask) == 0 || at + steps * 16 >= K) umma_commit(saddr(&s.acc_full[acc]));
+          }
         }
+        if (!ok) break;
+        if (leader) umma_commit(saddr(&s.empty[st]));
         __syncwarp();
       }
     }
@@ -190,35 +203,29 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
     // this thread's weights: row mine / 2, 32 of a chunk's 64; the swizzle moves a 16-byte piece by its row
     const uint32_t mine = tid % kGroup, group = tid / kGroup;
     const uint32_t row = mine >> 1, half = mine & 1, row_at = row * 128, mixed = row & 7;
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x, ++turn) {
+    const uint32_t first_row = (warp >> 2) * kBatch, column = (warp & 3) * 32 + lane, columns_at = ((warp & 3) * 32) << 16;
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
       const Unit o = unit_at(s, u, NT);
       const bool inside = o.n0 + row < N;
       const uint8_t *w = f.packed + o.e * f.stride_packed + (uint64_t)(inside ? o.n0 + row : 0) * f.ld_packed + half * 16;
-      const uint16_t *scales = f.scales + o.e * f.stride_scales + (uint64_t)(inside ? o.n0 + row : 0) * f.ld_scales;
-      const auto load = [&](uint32_t c, Ahead &to) {
-        const uint32_t k = c * kChunk + half * 32;
-        to.w = make_uint4(0, 0, 0, 0);
-        to.scale = 0;
-        if (inside && k < K) {
-          to.w = __ldcs((const uint4 *)(w + c * 32));
-          to.scale = scales[k >> f.group_log];
-        }
+      const auto load = [&](uint32_t c, uint4 &to) {
+        to = make_uint4(0, 0, 0, 0);
+        if (inside && c * kChunk + half * 32 < K) to = __ldcs((const uint4 *)(w + c * 32));
       };
       const uint32_t c0 = (group + used) % SETS;  // the group's first chunk: its stages stay the same
-      Ahead next[kDeep];
+      uint4 next[kDeep];
 #pragma unroll
       for (int q = 0; q < kDeep; ++q) load(c0 + q * SETS, next[q]);
+      // this thread's column of the result, and its scales
+      const uint32_t col = o.n0 + column;
+      const uint16_t *scales = f.scales + o.e * f.stride_scales + (uint64_t)(col < N ? col : 0) * f.ld_scales;
+      uint32_t scale = scales[0];
       // this thread's pieces of x: rows mine / 8, + 32, ...; bytes (mine & 7) * 16 of a chunk
-      const uint8_t *x[kPieces];
-      uint32_t there = 0;  // bit i: row i is there
+      uint32_t x[kPieces];  // rows of x; from x_rows on: none
 #pragma unroll
       for (uint32_t i = 0; i < kPieces; ++i) {
-        const uint32_t r = mine / 8 + 32 * i;
-        uint32_t at = o.from + min(r, o.rows - 1);
-        if (a.rows) at = ld_word((const uint32_t *)a.rows + at);
-        const bool is = r < o.rows && at < a.x_rows;
-        there |= (uint32_t)is << i;
-        x[i] = a.x + (is ? (uint64_t)at * a.ld_x * 2 : 0) + (mine & 7) * 16;
+        const uint32_t r = mine / 8 + 32 * i, at = o.from + min(r, o.rows - 1);
+        x[i] = r >= o.rows ? 0xFFFFFFFFu : a.rows ? ld_word((const uint32_t *)a.rows + at) : at;
       }
       // x of chunk c, whose stage it waits for
       const auto copy = [&](uint32_t c) {
@@ -230,22 +237,21 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
         for (uint32_t i = 0; i < kPieces; ++i) {
           if (32 * i >= o.rows) break;  // nobody looks at the columns of rows that are none
           const uint32_t r = mine / 8 + 32 * i, p = mine & 7;
-          const bool is = (there >> i & 1) && c * kChunk + p * 8 < K;
-          copy16(base + st * kStage + kABytes + r * 128 + ((p ^ (r & 7)) << 4), is ? x[i] + (uint64_t)c * 128 : a.x, is ? 16 : 0);
+          const bool is = x[i] < a.x_rows && c * kChunk + p * 8 < K;
+          copy16(base + st * kStage + kABytes + r * 128 + ((p ^ (r & 7)) << 4),
+                 a.x + (is ? (uint64_t)x[i] * (a.ld_x * 2) + c * 128 + p * 16 : 0), is ? 16 : 0);
         }
         asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(saddr(&s.full[st])) : "memory");
       };
-      const auto chunk = [&](uint32_t c, Ahead &now) {
+      const auto chunk = [&](uint32_t c, uint4 &now) {
         copy(c + kAhead);
         if (!ok) return;
         const uint32_t st = (used + c) % kStages, stage = base + st * kStage + row_at;
-        const uint32_t words[4] = {now.w.x, now.w.y, now.w.z, now.w.w}, scale = now.scale * 0x10001u;
+        const uint32_t words[4] = {now.x, now.y, now.z, now.w};
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q) {
           uint32_t v[4];
           numbers4<T>(words[q], v);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = times<T>(v[i], scale);
           asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + (((half * 4 + q) ^ mixed) << 4)),
                        "r"(__byte_perm(v[0], v[1], 0x5410)), "r"(__byte_perm(v[2], v[3], 0x5410)),
                        "r"(__byte_perm(v[0], v[1], 0x7632)), "r"(__byte_perm(v[2], v[3], 0x7632))
@@ -254,48 +260,79 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
         mbar_arrive(saddr(&s.full[st]));
         load(c + kDeep * SETS, now);
       };
+      // The sums, pairs of rows, and the groups in them
+      uint64_t sum[kBatches][kBatch / 2];
+#pragma unroll
+      for (uint32_t b = 0; b < kBatches; ++b)
+#pragma unroll
+        for (int i = 0; i < kBatch / 2; ++i) sum[b][i] = 0;
+      uint32_t added = 0;
+      const auto add = [&](uint32_t to) {
+#pragma unroll 1
+        for (; ok && added < to; ++added) {
+          const uint32_t acc = (summed + added) % kAcc;
+          const float by = to_f<T>(*reinterpret_cast<const T *>(&scale));
+          if (added + 1 < groups) scale = scales[added + 1];
+          ok = wait(saddr(&s.acc_full[acc]), ((summed + added) / kAcc) & 1);
+          if (!ok) break;
+          fence_after();
+#pragma unroll
+          for (uint32_t b = 0; b < kBatches; ++b) {
+            if (first_row + b * kApart >= o.rows) break;
+            uint32_t r[kBatch];
+            tmem_ld16(tmem + acc * NT + columns_at + first_row + b * kApart, r);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < kBatch / 2; ++i)
+              sum[b][i] = fma2(both(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), both(by, by), sum[b][i]);
+          }
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(saddr(&s.acc_empty[acc]));
+        }
+      };
 #pragma unroll 1
       for (uint32_t c = c0; c < c0 + kAhead; c += SETS) copy(c);
 #pragma unroll 1
       for (uint32_t c = c0; ok && c < chunks; c += kDeep * SETS) {
 #pragma unroll
-        for (int q = 0; q < kDeep; ++q)
-          if (c + q * SETS < chunks) chunk(c + q * SETS, next[q]);
+        for (int q = 0; q < kDeep; ++q) {
+          const uint32_t at = c + q * SETS;
+          if (at < chunks) {
+            if (at >= kLag) add((at - kLag + 1) * kChunk >> f.group_log);
+            chunk(at, next[q]);
+          }
+        }
       }
-      used += chunks;
-      const uint32_t acc = turn & 1;
-      if (ok) ok = wait(saddr(&s.acc_full[acc]), (turn >> 1) & 1);
+      add(groups);
+      used += chunks, summed += groups;
       if (!ok) break;
-      fence_after();
-      // A thread has a column of the result, four warps the 128 of 16 rows at a time
-      const uint32_t col = o.n0 + (warp & 3) * 32 + lane;
-      constexpr int kBatch = 16;
+      // A thread has a column of the result
       const float bias = a.bias && col < N ? a.bias[(uint64_t)o.e * N + col] : 0.0f;
-#pragma unroll 1
-      for (uint32_t r0 = (warp >> 2) * kBatch; r0 < o.rows; r0 += kMakers / 128 * kBatch) {
-        uint32_t r[kBatch];
-        tmem_ld16(tmem + acc * NT + (((warp & 3) * 32) << 16) + r0, r);
-        T add[kBatch];
+#pragma unroll
+      for (uint32_t b = 0; b < kBatches; ++b) {
+        const uint32_t r0 = first_row + b * kApart;
+        if (r0 >= o.rows) break;
+        T residual[kBatch];
         const uint64_t first = o.from + r0;
         if (a.residual && col < N) {
 #pragma unroll
           for (int i = 0; i < kBatch; ++i)
-            if (r0 + i < o.rows) add[i] = ((const T *)a.residual)[(first + i) * a.ld_residual + col];
+            if (r0 + i < o.rows) residual[i] = ((const T *)a.residual)[(first + i) * a.ld_residual + col];
         }
-        tmem_wait_ld();
         float v[kBatch];
 #pragma unroll
-        for (int i = 0; i < kBatch; ++i) v[i] = __uint_as_float(r[i]) + bias;
+        for (int i = 0; i < kBatch / 2; ++i) {
+          const float2 z = each(sum[b][i]);
+          v[2 * i] = z.x + bias, v[2 * i + 1] = z.y + bias;
+        }
         activate(a.activation, a.slope, v);
         if (col < N) {
 #pragma unroll
           for (int i = 0; i < kBatch; ++i)
-            if (r0 + i < o.rows) ((T *)a.out)[(first + i) * a.ld_out + col] = from_f<T>(a.residual ? v[i] + to_f<T>(add[i]) : v[i]);
+            if (r0 + i < o.rows) ((T *)a.out)[(first + i) * a.ld_out + col] = from_f<T>(a.residual ? v[i] + to_f<T>(residual[i]) : v[i]);
         }
       }
-      fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(saddr(&s.acc_empty[acc]));
     }
     if (ok) {
       // rows of no expert
@@ -337,18 +374,30 @@ namespace ntc {
 
 cudaError_t launch_linear4_mid(const Mid4 &f, uint64_t mean, cudaStream_t st) {
   // A tile has the rows of most experts, which are about their mean and twice its root where tokens choose by chance: an
-  // expert's next tile unpacks its weights again (2,048 -> 2,048, 16 experts of 128 rows: 43 us by tiles of 192, 51 by
-  // tiles of 128; of 96 rows: 42 and 41).
+  // expert's next tile unpacks its weights again.
+  const uint64_t experts = std::min<uint64_t>(f.a.num_experts, f.a.num_rows), tiles = experts * ((f.a.width + kRows - 1) / kRows);
   const double rows = f.a.num_experts == 1 ? (double)f.a.num_rows : (double)mean + 2.0 * std::sqrt((double)mean);
-  // One CTA an SM has two sets of threads to itself; where there are tiles for two CTAs each has one (256 rows of 8
-  // experts, 1,024 -> 2,048, 128 tiles: 11.1 us by two sets, 14.4 by one; 512 rows of 32, 512 tiles: 32.4 and 25.0).
-  const bool two = std::min<uint64_t>(f.a.num_experts, f.a.num_rows) * ((f.a.width + kRows - 1) / kRows) <= (uint64_t)sm_count();
+  const auto rounds = [&](int NT, int ctas) {  // of the CTAs that run at once
+    return std::ceil((double)tiles * std::ceil(rows / NT) / ((double)sm_count() * ctas));
+  };
+  struct Choice {
+    int NT, sets;
+    double chunk;  // what a CTA takes for one
+  };
+  constexpr Choice kChoices[] = {{32, 2, 1}, {32, 1, 1.4}, {64, 2, 1.1}, {64, 1, 1.6}, {128, 2, 1.4}, {192, 2, 1.8}};
+  const Choice *best = nullptr;
+  double least = 0;
+  for (const Choice &c : kChoices) {
+    if (c.NT == 192 && f.group_log == 5) continue;
+    const double cost = rounds(c.NT, 3 - c.sets) * c.chunk;
+    if (!best || cost < least) best = &c, least = cost;
+  }
   const auto go = [&](auto type) {
     using T = decltype(type);
-    return rows <= 32    ? (two ? launch<T, 32, 2>(f, st) : launch<T, 32, 1>(f, st))
-           : rows <= 64  ? (two ? launch<T, 64, 2>(f, st) : launch<T, 64, 1>(f, st))
-           : rows <= 128 ? launch<T, 128, 2>(f, st)
-                         : launch<T, 192, 2>(f, st);
+    return best->NT == 32    ? (best->sets == 2 ? launch<T, 32, 2>(f, st) : launch<T, 32, 1>(f, st))
+           : best->NT == 64  ? (best->sets == 2 ? launch<T, 64, 2>(f, st) : launch<T, 64, 1>(f, st))
+           : best->NT == 128 ? launch<T, 128, 2>(f, st)
+                             : launch<T, 192, 2>(f, st);
   };
   return f.a.bf16 ? go(__nv_bfloat16()) : go(__half());
 }

@@ -190,15 +190,32 @@ __global__ void __launch_bounds__(kThreads) k_pack4(const Pack4 a, const Turns t
   }
 }
 
+// Products of two pairs, rounded to 16 bits.
+template <typename T>
+__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
+  if constexpr (std::is_same<T, __half>::value) {
+    const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+  } else {
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+  }
+}
+
+struct Unpack {
+  const uint8_t *packed;
+  const uint16_t *scales;
+  uint16_t *w;
+  uint64_t ld_packed, stride_packed, ld_scales, stride_scales, ld_w, stride_w;
+  uint32_t in_dim, out_dim, num_experts, group;
+};
+
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(kThreads) k_unpack4(const Unpack a, const Turns t) {
   const uint32_t lane = threadIdx.x & 31;
   const uint64_t e = blockIdx.y;
   pdl_wait();
   pdl_trigger();
-  // an offset that falls is taken as the smallest that follows by the product: no expert
-  // has rows there that has none here
-  if (a.offsets && offset_at(a.offsets, e, a.num_rows) >= offset_at(a.offsets, e + 1, a.num_rows)) return;
   for (Walk at(t); at.rows < t.rows; at.next(t)) {
     uint32_t n, k, many;
     at.place(t, lane, n, k, many);
@@ -278,6 +295,14 @@ cudaError_t pack(const Pack4 &a, ntc_type w_type, cudaStream_t st) {
   return w_type == NTC_TYPE_FP32 ? go(float()) : w_type == NTC_TYPE_FP16 ? go(__half()) : go(__nv_bfloat16());
 }
 
+cudaError_t unpack(const Unpack &u, bool bf16, cudaStream_t st) {
+  const Turns t = turns_of(u.in_dim, u.out_dim, u.num_experts, 1);
+  const bool vec = rows_are_vec(u.w, u.ld_w, 2) && (u.num_experts == 1 || u.stride_w % 8 == 0);
+  const auto kernel = bf16 ? (vec ? k_unpack4<__nv_bfloat16, true> : k_unpack4<__nv_bfloat16, false>)
+                           : (vec ? k_unpack4<__half, true> : k_unpack4<__half, false>);
+  return launch_pdl(kernel, grid_of(t, u.num_experts), kThreads, 0, st, u, t);
+}
+
 ntc_status check_matrix(const ntc_pack4_desc *d, const void *w, size_t elem, uint64_t ld_w, uint64_t stride_w,
                         const void *packed, const void *scales) {
   if (ld_w < d->in_dim) return op_fail(NTC_ERR_INVALID_ARG, "ld_w is below in_dim");
@@ -313,14 +338,6 @@ ntc_status check_pack4(const ntc_pack4_desc *d) {
   return NTC_OK;
 }
 
-cudaError_t launch_unpack4(const Unpack &u, bool bf16, cudaStream_t st) {
-  const Turns t = turns_of(u.in_dim, u.out_dim, u.num_experts, 1);
-  const bool vec = rows_are_vec(u.w, u.ld_w, 2) && (u.num_experts == 1 || u.stride_w % 8 == 0);
-  const auto kernel = bf16 ? (vec ? k_unpack4<__nv_bfloat16, true> : k_unpack4<__nv_bfloat16, false>)
-                           : (vec ? k_unpack4<__half, true> : k_unpack4<__half, false>);
-  return launch_pdl(kernel, grid_of(t, u.num_experts), kThreads, 0, st, u, t);
-}
-
 }  // namespace ntc
 
 extern "C" NTC_API ntc_status ntc_pack4(const ntc_pack4_desc *desc, const void *w, ntc_type w_type, uint64_t ld_w,
@@ -341,7 +358,7 @@ extern "C" NTC_API ntc_status ntc_unpack4(const ntc_pack4_desc *desc, const uint
   if (ntc_status s = check_pack4(desc)) return s;
   if (ntc_status s = check_matrix(desc, w, 2, ld_w, stride_w, packed, scales)) return s;
   const ntc_pack4_desc &d = *desc;
-  const Unpack u = {packed, (const uint16_t *)scales, (uint16_t *)w, nullptr, d.ld_packed, d.stride_packed, d.ld_scales,
-                    d.stride_scales, ld_w, stride_w, d.in_dim, d.out_dim, d.num_experts, d.group, 0};
-  return op_cuda(launch_unpack4(u, d.type == NTC_TYPE_BF16, (cudaStream_t)cuda_stream), "ntc_unpack4");
+  const Unpack u = {packed, (const uint16_t *)scales, (uint16_t *)w, d.ld_packed, d.stride_packed, d.ld_scales,
+                    d.stride_scales, ld_w, stride_w, d.in_dim, d.out_dim, d.num_experts, d.group};
+  return op_cuda(unpack(u, d.type == NTC_TYPE_BF16, (cudaStream_t)cuda_stream), "ntc_unpack4");
 }

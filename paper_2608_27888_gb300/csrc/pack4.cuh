@@ -41,27 +41,4 @@ __device__ __forceinline__ void numbers4(uint32_t w, uint32_t (&v)[4]) {
   }
 }
 
-// Products of two pairs, rounded to 16 bits.
-template <typename T>
-__device__ __forceinline__ uint32_t times(uint32_t a, uint32_t b) {
-  if constexpr (std::is_same<T, __half>::value) {
-    const __half2 r = __hmul2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
-  } else {
-    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
-    return *reinterpret_cast<const uint32_t *>(&r);
-  }
-}
-
-struct Unpack {
-  const uint8_t *packed;
-  const uint16_t *scales;
-  uint16_t *w;
-  const int32_t *offsets;  // or NULL: only experts with rows are written
-  uint64_t ld_packed, stride_packed, ld_scales, stride_scales, ld_w, stride_w;
-  uint32_t in_dim, out_dim, num_experts, group;
-  int32_t num_rows;
-};
-cudaError_t launch_unpack4(const Unpack &u, bool bf16, cudaStream_t st);
-
 }  // namespace ntc
