@@ -376,7 +376,11 @@ bool x_whole(const ntc_linear_desc &d, const void *x) { return d.in_dim % 32 == 
 bool packed_whole(const ntc_linear_desc &d, const ntc_pack4_desc &p, const uint8_t *packed) {
   return d.in_dim % 32 == 0 && starts_on(d, packed, 16, p.ld_packed, p.stride_packed);
 }
-// Whether the tcgen05 kernel takes the call.  It unpacks a tile of weights once for up to 192 rows.
+// Whether the tcgen05 kernel takes the call.  It unpacks a tile of weights once for up to 128 rows, the other for every 32.
+// Times in us, tcgen05 and the other:
+//   64 experts, 2,048 -> 1,024, groups of 128: 47 and 67 for 16 rows an expert, 54 and 160 for 32;
+//   32 tiles, 4,096 -> 4,096: 26 and 14 for 20 rows;
+//   8 rows an expert, 2,048 -> 2,048, 32 experts: 43 and 40; 64 experts, 1,024 -> 4,096: 78 and 69.
 bool by_tiles(const ntc_linear_desc &d, const ntc_pack4_desc &p, const void *x, const uint8_t *packed) {
   if (d.num_rows == 0 || few_rows(d.num_rows)) return false;
   const uint64_t mean = mean_rows(d), tiles = std::min<uint64_t>(d.num_experts, d.num_rows) * ((d.out_dim + 127ull) / 128);

@@ -11,12 +11,20 @@
 // shared-memory stages:
 //   256 threads  weights: a thread has half of a row's chunk, 16 bytes, in registers two chunks
 //                ahead; the numbers go to the stage as the swizzle wants them.  x: 16-byte
-//                cp.async, rows gathered by index, two chunks ahead, which arrive at the
-//                stage's barrier by themselves.  The sums of the groups that are complete,
-//                three chunks behind.  At the end the epilogue.
-//   a warp       issues the MMAs, a group into one of two or four accumulators.  The proxy
-//                fence is its own: one by a copying thread waits for all of its copies in flight.
+//                cp.async, rows gathered by index, two chunks ahead.  One lane arrives for its
+//                warp: a barrier takes lanes one by one.
+//   2 or 4 warps issue the MMAs, each a group (or a chunk of two) into accumulators of its own:
+//                one warp's wait, fence, MMAs and commit take 800 to 1,000 cycles for a chunk.
+//                The proxy fence is theirs: one by a copying thread waits for all of its copies
+//                in flight.
+//   4 or 8 warps add the groups, and write the tile while the others are at the next one.
 // Unpacked weights never touch HBM.
+// Bound by instructions (issue slots 67 %): a chunk takes 930 cycles with NT = 128, of which the
+// MMAs are 260 (1,024 tokens of 2 of 16 experts, 2,048 -> 2,048, groups of 128: 53 us; of 64: 70;
+// of 32: 92).  With the products s q rounded to 16 bits and no sums but the accumulator's it
+// was 43 for each.  Tried: sums by the converting threads (66 us, 134 for groups of 32), one set of
+// them with two accumulators of 192 rows (62), fp32x2 sums (57, their pairs are moved together),
+// sleeping waits (no gain; slower for groups of 32), a wait by one lane for its warp (67).
 #include "linear4.cuh"
 #include "tcgen05.cuh"
 
@@ -27,29 +35,35 @@ using namespace ntc;
 
 namespace {
 
-// Threads that make a chunk; SETS of them, which take turns: one in each of two CTAs an SM, or two in one.
-constexpr int kGroup = 256;
-constexpr int threads(int SETS) { return kGroup * SETS + 32; }
-constexpr int kStages = 4, kAhead = 2;  // x is that far ahead, and both the rest of the stages ahead of the MMAs
-constexpr int kDeep = 2;                // a thread's chunks of weights in registers
-// Sums are taken that many chunks behind: a set has a chunk's groups added before it waits for the stage of two chunks on,
-// which is free once the MMAs of two chunks before are through.  So the MMAs never wait for an accumulator that is added
-// only after they are: with two accumulators a chunk has at most one group (NT 192 takes no groups of 32).
-constexpr uint32_t kLag = 3;
 constexpr uint32_t kRows = 128, kChunk = 64, kABytes = kRows * 128;
-constexpr uint32_t buffers(int NT) { return NT > 128 ? 2 : 4; }  // accumulators
-constexpr uint32_t columns(int NT) { return NT > 128 ? 512 : NT * buffers(NT); }  // of TMEM: a power of two
 constexpr uint32_t stage_bytes(int NT) { return kABytes + (uint32_t)NT * 128; }
+// Threads that make a chunk; SETS of them, which take turns: one in each of two CTAs an SM, or two in one.  After them a
+// warpgroup whose warps issue the MMAs, and SETS that add the groups up.
+constexpr int kGroup = 256, kQuad = 128;
+constexpr int threads(int SETS) { return (kGroup + kQuad) * SETS + kQuad; }
+// Registers: at launch as many as the threads leave, and after the start those of each part, which are no more together.
+constexpr int launch_regs(int SETS) { return SETS == 2 ? 72 : 64; }
+constexpr int kMakerRegs = 56, kIssueRegs = 32;
+constexpr int adder_regs(int SETS) { return SETS == 2 ? 120 : 112; }
+constexpr bool registers_suffice(int SETS) {
+  return (kMakerRegs * kGroup + adder_regs(SETS) * kQuad) * SETS + kIssueRegs * kQuad <= launch_regs(SETS) * threads(SETS);
+}
+constexpr int stages(int SETS) { return SETS == 2 ? 6 : 4; }
+constexpr int kAhead = 2;  // x is that far ahead, and both the rest of the stages ahead of the MMAs
+constexpr int kDeep = 2;                            // a thread's chunks of weights in registers
+// Accumulators that there is tensor memory for, and its columns: a power of two.
+constexpr uint32_t accumulators(int NT, int SETS) { return SETS * 256 / NT < 8 ? SETS * 256 / NT : 8; }
+constexpr uint32_t columns(int NT, int SETS) { return NT * accumulators(NT, SETS); }
 
 struct Shared {
-  uint64_t full[kStages], empty[kStages], acc_full[4], acc_empty[4], drain;
+  uint64_t full[6], empty[6], acc_full[4], acc_empty[4], drain[4];
   uint32_t tmem, active, live, units, quit;
   int32_t begin[NTC_MAX_EXPERTS];   // of the experts with rows: first row,
   int32_t count[NTC_MAX_EXPERTS];   // rows,
   uint32_t first[NTC_MAX_EXPERTS];  // first unit,
   uint16_t which[NTC_MAX_EXPERTS];  // and number
 };
-constexpr size_t shared_bytes(int NT) { return 1024 + (size_t)kStages * stage_bytes(NT) + sizeof(Shared); }
+constexpr size_t shared_bytes(int NT, int SETS) { return 1024 + (size_t)stages(SETS) * stage_bytes(NT) + sizeof(Shared); }
 
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, uint32_t bytes) {  // the rest of the 16 are zeros
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -81,6 +95,15 @@ __device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, volatile
   return true;
 }
 
+template <int R>
+__device__ __forceinline__ void take_registers() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(R));
+}
+template <int R>
+__device__ __forceinline__ void leave_registers() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(R));
+}
+
 // A unit: an expert's tile of weights and a block of its rows.
 struct Unit {
   uint32_t e, n0, from, rows;
@@ -98,28 +121,26 @@ __device__ __forceinline__ Unit unit_at(const Shared &s, uint32_t u, uint32_t NT
 
 template <typename T, int NT, int SETS>
 __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const Mid4 f) {
-  constexpr int kMakers = kGroup * SETS;
+  constexpr int kMakers = kGroup * SETS, kStages = stages(SETS);
+  constexpr uint32_t kAcc = accumulators(NT, SETS), kColumns = columns(NT, SETS);
   constexpr uint32_t kStage = stage_bytes(NT), kPieces = NT * 8 / kGroup;  // of x, a thread's
-  constexpr uint32_t kAcc = buffers(NT);
-  constexpr int kBatch = 16;                          // rows of x that a thread adds or writes together
-  constexpr uint32_t kApart = kMakers / 128 * kBatch;  // four warps have the 128 columns of the result, the next four the next rows
-  constexpr uint32_t kBatches = (NT + kApart - 1) / kApart;
+  static_assert(registers_suffice(SETS), "a part would wait for registers that nobody leaves");
   extern __shared__ uint8_t dynamic[];
   uint8_t *ring = (uint8_t *)(((uintptr_t)dynamic + 1023) & ~(uintptr_t)1023);
   Shared &s = *reinterpret_cast<Shared *>(ring + kStages * kStage);
   const LinearArgs &a = f.a;
   const uint32_t tid = threadIdx.x, lane = tid & 31, warp = uniform(tid / 32);
   const uint32_t K = a.depth, N = a.width, tiles = (N + kRows - 1) / kRows, chunks = (K + kChunk - 1) / kChunk;
-  const uint32_t group_mask = (1u << f.group_log) - 1, groups = (K + group_mask) >> f.group_log;
+  const uint32_t groups = (K + (1u << f.group_log) - 1) >> f.group_log;
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(saddr(&s.tmem)), "r"(columns(NT)) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;\n" ::"r"(saddr(&s.tmem)), "r"(kColumns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n" ::: "memory");
     fence_before();
   }
   if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) mbar_init(saddr(&s.full[i]), 2 * kGroup), mbar_init(saddr(&s.empty[i]), 1);
-    for (uint32_t i = 0; i < kAcc; ++i) mbar_init(saddr(&s.acc_full[i]), 1), mbar_init(saddr(&s.acc_empty[i]), kMakers / 32);
-    mbar_init(saddr(&s.drain), 1);
+    for (int i = 0; i < kStages; ++i) mbar_init(saddr(&s.full[i]), kGroup / 32), mbar_init(saddr(&s.empty[i]), 1);
+    for (uint32_t i = 0; i < 4; ++i) mbar_init(saddr(&s.acc_full[i]), 1), mbar_init(saddr(&s.acc_empty[i]), kQuad * SETS / 32);
+    for (int i = 0; i < 4; ++i) mbar_init(saddr(&s.drain[i]), 1);
     mbar_init_fence();
     s.quit = 0;
   }
@@ -153,57 +174,67 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
   };
   bool ok = true;
   uint32_t used = 0, summed = 0;  // chunks and groups that this CTA has gone through
-  if (warp == kMakers / 32) {
+  // A slot is an accumulator for a group, or two for the two groups of 32 of a chunk; as many warps issue as there are slots.
+  const bool halves = f.group_log == 5;
+  const uint32_t slots = uniform(f.group_log == 7 ? 2 : halves ? kAcc / 2 : 4), slot_columns = halves ? 2 * NT : NT;
+  const uint32_t blocks = f.group_log == 7 ? groups : chunks;  // a unit's groups, or chunks of two: what a slot is taken for
+  if (warp >= kMakers / 32 && warp < kMakers / 32 + 4) {
+    leave_registers<kIssueRegs>();
     constexpr uint32_t kBf16 = std::is_same<T, __half>::value ? 0 : 1;
     constexpr uint32_t idesc = (1u << 4) | (kBf16 << 7) | (kBf16 << 10) | ((uint32_t)(NT >> 3) << 17) | ((kRows >> 4) << 24);
     // 128-byte-swizzled K-major operands: 8-row groups 1,024 bytes apart
     constexpr uint32_t kHi = (1024u >> 4) | (1u << 14) | (2u << 29);
-    const uint32_t ring_lo = uniform(((base >> 4) & 0x3FFFu) | ((8192u >> 4) << 16));
-    const uint32_t steps = uniform(f.group_log == 5 ? 2 : 4);  // MMAs (16 of the contraction) of a chunk that are of one group
+    const uint32_t ring_lo = uniform(((base >> 4) & 0x3FFFu) | ((8192u >> 4) << 16)), mine = warp - kMakers / 32;
     const bool leader = elect_one();
     bool any = false;
-    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
-      uint32_t acc = 0;
-      for (uint32_t c = 0; ok && c < chunks; ++c, ++used) {
-        const uint32_t st = used % kStages;
-        ok = wait(saddr(&s.full[st]), (used / kStages) & 1);
-        if (!ok) break;
-        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-        const uint32_t alo = ring_lo + st * (kStage >> 4), blo = alo + (kABytes >> 4);
-        for (uint32_t k0 = 0; k0 < 4 && c * kChunk + k0 * 16 < K; k0 += steps) {
-          const uint32_t at = c * kChunk + k0 * 16;
-          const bool first = (at & group_mask) == 0;
-          if (first) {
-            acc = summed % kAcc;
-            ok = wait(saddr(&s.acc_empty[acc]), ((summed / kAcc) & 1) ^ 1);
+    uint32_t turn = 0;  // whose block it is
+    for (uint32_t u = mine < slots ? blockIdx.x : units; ok && u < units; u += gridDim.x) {
+      for (uint32_t c = 0; ok && c < chunks; ++summed) {
+        const uint32_t many = f.group_log == 7 ? min(2u, chunks - c) : 1;
+        if (turn == mine) {
+          // The slot is waited for before the stages: it is free once the adders, who go in order, are past the block that had
+          // it, so that every chunk up to that one's has been full, and with them the stages' last uses, for the slots' blocks
+          // are no more chunks than there are stages.  Without that a warp that sees only some of a barrier's phases could
+          // take an older one's parity for its own.
+          ok = wait(saddr(&s.acc_empty[mine]), ((summed / slots) & 1) ^ 1);
+          const uint32_t d = uniform(tmem + mine * slot_columns);
+          for (uint32_t i = 0; ok && i < many; ++i) {
+            const uint32_t st = uniform((used + i) % kStages);
+            ok = wait(saddr(&s.full[st]), ((used + i) / kStages) & 1);
             if (!ok) break;
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
             fence_after();
-            ++summed;
-          }
-          any = true;
-          if (leader) {
-            const uint32_t d = tmem + acc * NT;
+            any = true;
+            const uint32_t alo = ring_lo + st * (kStage >> 4), blo = alo + (kABytes >> 4);
+            if (leader) {
+              if (!halves) {
 #pragma unroll
-            for (uint32_t k = 0; k < 4; ++k)  // past K there is nothing to add
-              if (k < steps && at + k * 16 < K) mma_ss(d, alo + (k0 + k) * 2, blo + (k0 + k) * 2, kHi, idesc, !first || k != 0);
-            if (((at + steps * 16) & group_mask) == 0 || at + steps * 16 >= K) umma_commit(saddr(&s.acc_full[acc]));
+                for (uint32_t k = 0; k < kChunk / 16; ++k) mma_ss(d, alo + k * 2, blo + k * 2, kHi, idesc, (i | k) != 0);
+              } else {
+#pragma unroll
+                for (uint32_t k = 0; k < kChunk / 16; ++k) mma_ss(d + k / 2 * NT, alo + k * 2, blo + k * 2, kHi, idesc, k & 1);
+              }
+              umma_commit(saddr(&s.empty[st]));
+              if (i + 1 == many) umma_commit(saddr(&s.acc_full[mine]));
+            }
+            __syncwarp();
           }
         }
-        if (!ok) break;
-        if (leader) umma_commit(saddr(&s.empty[st]));
-        __syncwarp();
+        turn = turn + 1 == slots ? 0 : turn + 1;
+        c += many, used += many;
       }
     }
     if (!ok && any) {
-      if (leader) umma_commit(saddr(&s.drain));
+      if (leader) umma_commit(saddr(&s.drain[mine]));
       __syncwarp();
-      mbar_wait(saddr(&s.drain), 0);
+      mbar_wait(saddr(&s.drain[mine]), 0);
     }
-  } else {
+  } else if (warp < kMakers / 32) {
+    leave_registers<kMakerRegs>();
     // this thread's weights: row mine / 2, 32 of a chunk's 64; the swizzle moves a 16-byte piece by its row
     const uint32_t mine = tid % kGroup, group = tid / kGroup;
-    const uint32_t row = mine >> 1, half = mine & 1, row_at = row * 128, mixed = row & 7;
-    const uint32_t first_row = (warp >> 2) * kBatch, column = (warp & 3) * 32 + lane, columns_at = ((warp & 3) * 32) << 16;
+    const uint32_t row = mine >> 1, half = mine & 1, w_at = row * 128 + ((half * 4 ^ (row & 7)) << 4);
+    const uint32_t x_at = mine / 8 * 128 + (((mine & 7) ^ (mine / 8 & 7)) << 4);  // rows 32 apart have the same swizzle
     for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
       const Unit o = unit_at(s, u, NT);
       const bool inside = o.n0 + row < N;
@@ -216,123 +247,65 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
       uint4 next[kDeep];
 #pragma unroll
       for (int q = 0; q < kDeep; ++q) load(c0 + q * SETS, next[q]);
-      // this thread's column of the result, and its scales
-      const uint32_t col = o.n0 + column;
-      const uint16_t *scales = f.scales + o.e * f.stride_scales + (uint64_t)(col < N ? col : 0) * f.ld_scales;
-      uint32_t scale = scales[0];
       // this thread's pieces of x: rows mine / 8, + 32, ...; bytes (mine & 7) * 16 of a chunk
-      uint32_t x[kPieces];  // rows of x; from x_rows on: none
+      const uint8_t *x[kPieces];
+      uint32_t bytes[kPieces];  // of a piece: 16, or 0 where there is no row
 #pragma unroll
       for (uint32_t i = 0; i < kPieces; ++i) {
-        const uint32_t r = mine / 8 + 32 * i, at = o.from + min(r, o.rows - 1);
-        x[i] = r >= o.rows ? 0xFFFFFFFFu : a.rows ? ld_word((const uint32_t *)a.rows + at) : at;
+        const uint32_t r = mine / 8 + 32 * i;
+        uint32_t at = o.from + min(r, o.rows - 1);
+        if (a.rows) at = ld_word((const uint32_t *)a.rows + at);
+        const bool is = r < o.rows && at < a.x_rows;
+        bytes[i] = is ? 16 : 0;
+        x[i] = a.x + (is ? (uint64_t)at * a.ld_x * 2 : 0) + (mine & 7) * 16;
       }
       // x of chunk c, whose stage it waits for
       const auto copy = [&](uint32_t c) {
-        if (c >= chunks || !ok) return;
+        if (c >= chunks || !ok) {
+          asm volatile("cp.async.commit_group;\n" ::: "memory");  // of nothing
+          return;
+        }
         const uint32_t m = used + c, st = m % kStages;
         ok = wait(saddr(&s.empty[st]), ((m / kStages) & 1) ^ 1);
         if (!ok) return;
+        const uint32_t to = base + st * kStage + kABytes + x_at;
+        const bool in = c * kChunk + (mine & 7) * 8 < K;  // past K: zeros, and the row's first address
+        const int64_t off = in ? (int64_t)(c * 128) : -(int64_t)((mine & 7) * 16);
 #pragma unroll
         for (uint32_t i = 0; i < kPieces; ++i) {
           if (32 * i >= o.rows) break;  // nobody looks at the columns of rows that are none
-          const uint32_t r = mine / 8 + 32 * i, p = mine & 7;
-          const bool is = x[i] < a.x_rows && c * kChunk + p * 8 < K;
-          copy16(base + st * kStage + kABytes + r * 128 + ((p ^ (r & 7)) << 4),
-                 a.x + (is ? (uint64_t)x[i] * (a.ld_x * 2) + c * 128 + p * 16 : 0), is ? 16 : 0);
+          copy16(to + i * 4096, x[i] + off, in ? bytes[i] : 0);
         }
-        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(saddr(&s.full[st])) : "memory");
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
       };
       const auto chunk = [&](uint32_t c, uint4 &now) {
         copy(c + kAhead);
         if (!ok) return;
-        const uint32_t st = (used + c) % kStages, stage = base + st * kStage + row_at;
+        const uint32_t st = (used + c) % kStages, to = base + st * kStage + w_at;
         const uint32_t words[4] = {now.x, now.y, now.z, now.w};
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q) {
           uint32_t v[4];
           numbers4<T>(words[q], v);
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(stage + (((half * 4 + q) ^ mixed) << 4)),
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to ^ (q << 4)),
                        "r"(__byte_perm(v[0], v[1], 0x5410)), "r"(__byte_perm(v[2], v[3], 0x5410)),
                        "r"(__byte_perm(v[0], v[1], 0x7632)), "r"(__byte_perm(v[2], v[3], 0x7632))
                        : "memory");
         }
-        mbar_arrive(saddr(&s.full[st]));
+        asm volatile("cp.async.wait_group %0;\n" ::"n"(kAhead / SETS) : "memory");  // this chunk's x, two chunks later
+        __syncwarp();
+        if (lane == 0) mbar_arrive(saddr(&s.full[st]));
         load(c + kDeep * SETS, now);
-      };
-      // The sums, pairs of rows, and the groups in them
-      uint64_t sum[kBatches][kBatch / 2];
-#pragma unroll
-      for (uint32_t b = 0; b < kBatches; ++b)
-#pragma unroll
-        for (int i = 0; i < kBatch / 2; ++i) sum[b][i] = 0;
-      uint32_t added = 0;
-      const auto add = [&](uint32_t to) {
-#pragma unroll 1
-        for (; ok && added < to; ++added) {
-          const uint32_t acc = (summed + added) % kAcc;
-          const float by = to_f<T>(*reinterpret_cast<const T *>(&scale));
-          if (added + 1 < groups) scale = scales[added + 1];
-          ok = wait(saddr(&s.acc_full[acc]), ((summed + added) / kAcc) & 1);
-          if (!ok) break;
-          fence_after();
-#pragma unroll
-          for (uint32_t b = 0; b < kBatches; ++b) {
-            if (first_row + b * kApart >= o.rows) break;
-            uint32_t r[kBatch];
-            tmem_ld16(tmem + acc * NT + columns_at + first_row + b * kApart, r);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < kBatch / 2; ++i)
-              sum[b][i] = fma2(both(__uint_as_float(r[2 * i]), __uint_as_float(r[2 * i + 1])), both(by, by), sum[b][i]);
-          }
-          fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(saddr(&s.acc_empty[acc]));
-        }
       };
 #pragma unroll 1
       for (uint32_t c = c0; c < c0 + kAhead; c += SETS) copy(c);
 #pragma unroll 1
       for (uint32_t c = c0; ok && c < chunks; c += kDeep * SETS) {
 #pragma unroll
-        for (int q = 0; q < kDeep; ++q) {
-          const uint32_t at = c + q * SETS;
-          if (at < chunks) {
-            if (at >= kLag) add((at - kLag + 1) * kChunk >> f.group_log);
-            chunk(at, next[q]);
-          }
-        }
+        for (int q = 0; q < kDeep; ++q)
+          if (c + q * SETS < chunks) chunk(c + q * SETS, next[q]);
       }
-      add(groups);
-      used += chunks, summed += groups;
-      if (!ok) break;
-      // A thread has a column of the result
-      const float bias = a.bias && col < N ? a.bias[(uint64_t)o.e * N + col] : 0.0f;
-#pragma unroll
-      for (uint32_t b = 0; b < kBatches; ++b) {
-        const uint32_t r0 = first_row + b * kApart;
-        if (r0 >= o.rows) break;
-        T residual[kBatch];
-        const uint64_t first = o.from + r0;
-        if (a.residual && col < N) {
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i)
-            if (r0 + i < o.rows) residual[i] = ((const T *)a.residual)[(first + i) * a.ld_residual + col];
-        }
-        float v[kBatch];
-#pragma unroll
-        for (int i = 0; i < kBatch / 2; ++i) {
-          const float2 z = each(sum[b][i]);
-          v[2 * i] = z.x + bias, v[2 * i + 1] = z.y + bias;
-        }
-        activate(a.activation, a.slope, v);
-        if (col < N) {
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i)
-            if (r0 + i < o.rows) ((T *)a.out)[(first + i) * a.ld_out + col] = from_f<T>(a.residual ? v[i] + to_f<T>(residual[i]) : v[i]);
-        }
-      }
+      used += chunks;
     }
     if (ok) {
       // rows of no expert
@@ -343,11 +316,90 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
       }
     }
     asm volatile("cp.async.wait_all;\n" ::: "memory");  // none lands after the CTA's end
+  } else {
+    take_registers<adder_regs(SETS)>();
+    // A thread has a column of the result, its scales, and every (SETS 2: every second) 16 rows of it.  A group's sums times
+    // its scale are added in pairs of rows; loads of tensor memory are on their way together as registers allow.
+    constexpr int kBatch = 16, kBatches = NT / kBatch / SETS, kFlight = kBatches < 2 ? 1 : 2;
+    const uint32_t column = (warp & 3) * 32 + lane, lanes_at = tmem + (((warp & 3) * 32) << 16);
+    const uint32_t r_first = (warp / 4 - (kMakers + kQuad) / 128) * kBatch;
+    for (uint32_t u = blockIdx.x; ok && u < units; u += gridDim.x) {
+      const Unit o = unit_at(s, u, NT);
+      const uint32_t col = o.n0 + column;
+      const uint16_t *scales = f.scales + o.e * f.stride_scales + (uint64_t)(col < N ? col : 0) * f.ld_scales;
+      uint32_t scale = scales[0];
+      float sum[kBatches][kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatches; ++b)
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) sum[b][i] = 0.0f;
+#pragma unroll 1
+      for (uint32_t j = 0, g = 0; j < blocks; ++j, ++summed) {
+        const uint32_t slot = summed & (slots - 1);
+        ok = wait(saddr(&s.acc_full[slot]), (summed / slots) & 1);
+        if (!ok) break;
+        fence_after();
+        uint32_t from = lanes_at + slot * slot_columns + r_first;
+#pragma unroll 1
+        for (const uint32_t to = min(g + (halves ? 2 : 1), groups); g < to; from += NT) {
+          const float by = unpack2<T>(scale).x;
+          if (++g < groups) scale = scales[g];
+#pragma unroll
+          for (int b0 = 0; b0 < kBatches; b0 += kFlight) {
+            if (r_first + b0 * SETS * kBatch >= o.rows) break;
+            uint32_t r[kFlight][kBatch];
+#pragma unroll
+            for (int b = 0; b < kFlight; ++b) tmem_ld16(from + (b0 + b) * SETS * kBatch, r[b]);
+            tmem_wait_ld();
+#pragma unroll
+            for (int b = 0; b < kFlight; ++b)
+#pragma unroll
+              for (int i = 0; i < kBatch; ++i) sum[b0 + b][i] = fmaf(by, __uint_as_float(r[b][i]), sum[b0 + b][i]);
+          }
+        }
+        fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(saddr(&s.acc_empty[slot]));
+      }
+      if (!ok) break;
+      const float bias = a.bias && col < N ? a.bias[(uint64_t)o.e * N + col] : 0.0f;
+      // one batch's code for all: the others' sums move up
+#pragma unroll 1
+      for (uint32_t r0 = r_first; r0 < o.rows; r0 += SETS * kBatch) {
+        const int left = (int)(o.rows - r0);
+        const uint64_t first = (uint64_t)o.from + r0;
+        T residual[kBatch];
+        if (a.residual && col < N) {
+          const T *p = (const T *)a.residual + first * a.ld_residual + col;
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i, p += a.ld_residual)
+            if (i < left) residual[i] = *p;
+        }
+        float v[kBatch];
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) v[i] = sum[0][i] + bias;
+        activate(a.activation, a.slope, v);
+        if (a.residual) {
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) v[i] += to_f<T>(residual[i]);  // what was not loaded is not stored
+        }
+        if (col < N) {
+          T *p = (T *)a.out + first * a.ld_out + col;
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i, p += a.ld_out)
+            if (i < left) *p = from_f<T>(v[i]);
+        }
+#pragma unroll
+        for (int b = 1; b < kBatches; ++b)
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) sum[b - 1][i] = sum[b][i];
+      }
+    }
   }
   fence_before();
   __syncthreads();
   fence_after();
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(columns(NT)) : "memory");
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;\n" ::"r"(tmem), "r"(kColumns) : "memory");
 }
 
 template <typename T, int NT, int SETS>
@@ -357,7 +409,11 @@ cudaError_t launch(const Mid4 &f, cudaStream_t st) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !((allowed.load() >> dev) & 1)) {
-    e = cudaFuncSetAttribute(k_linear4_mid<T, NT, SETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_bytes(NT));
+    cudaFuncAttributes is;
+    e = cudaFuncGetAttributes(&is, k_linear4_mid<T, NT, SETS>);
+    if (e != cudaSuccess) return e;
+    if (is.numRegs < launch_regs(SETS)) return cudaErrorInvalidConfiguration;  // the parts would wait for what was never there
+    e = cudaFuncSetAttribute(k_linear4_mid<T, NT, SETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared_bytes(NT, SETS));
     if (e != cudaSuccess) return e;
     if (dev < 64) allowed.fetch_or(1ull << dev);
   }
@@ -365,7 +421,7 @@ cudaError_t launch(const Mid4 &f, cudaStream_t st) {
   const uint64_t tiles = (f.a.width + kRows - 1) / kRows, experts = std::min<uint64_t>(f.a.num_experts, f.a.num_rows);
   const uint64_t units = tiles * (f.a.num_rows / NT + experts);
   const unsigned grid = (unsigned)std::min<uint64_t>(units, (uint64_t)sm_count() * (3 - SETS));
-  return launch_pdl(k_linear4_mid<T, NT, SETS>, grid, threads(SETS), shared_bytes(NT), st, f);
+  return launch_pdl(k_linear4_mid<T, NT, SETS>, grid, threads(SETS), shared_bytes(NT, SETS), st, f);
 }
 
 }  // namespace
@@ -373,31 +429,29 @@ cudaError_t launch(const Mid4 &f, cudaStream_t st) {
 namespace ntc {
 
 cudaError_t launch_linear4_mid(const Mid4 &f, uint64_t mean, cudaStream_t st) {
-  // A tile has the rows of most experts, which are about their mean and twice its root where tokens choose by chance: an
-  // expert's next tile unpacks its weights again.
+  // Rows of most experts: about their mean and twice its root where tokens choose by chance.
   const uint64_t experts = std::min<uint64_t>(f.a.num_experts, f.a.num_rows), tiles = experts * ((f.a.width + kRows - 1) / kRows);
   const double rows = f.a.num_experts == 1 ? (double)f.a.num_rows : (double)mean + 2.0 * std::sqrt((double)mean);
-  const auto rounds = [&](int NT, int ctas) {  // of the CTAs that run at once
-    return std::ceil((double)tiles * std::ceil(rows / NT) / ((double)sm_count() * ctas));
-  };
+  // ns that the CTAs which run at once take for a chunk each, by the group's size (2,048 rows of a dense 4,096 -> 4,096 layer,
+  // whole rounds).  High tiles unpack a weight for more rows, low ones are more CTAs; 16 rows of each of 64 experts: 47 us by
+  // the first but one, 51 by the first; 128 rows of a dense layer of 32 tiles: 26 and 34 us for tiles of 32 and of 128 rows.
   struct Choice {
     int NT, sets;
-    double chunk;  // what a CTA takes for one
+    double chunk[3];  // groups of 32, 64, 128
   };
-  constexpr Choice kChoices[] = {{32, 2, 1}, {32, 1, 1.4}, {64, 2, 1.1}, {64, 1, 1.6}, {128, 2, 1.4}, {192, 2, 1.8}};
+  constexpr Choice kChoices[] = {
+      {32, 2, {545, 431, 311}}, {32, 1, {906, 753, 602}}, {64, 2, {663, 553, 367}}, {64, 1, {1042, 790, 672}}, {128, 2, {864, 639, 458}}};
   const Choice *best = nullptr;
   double least = 0;
   for (const Choice &c : kChoices) {
-    if (c.NT == 192 && f.group_log == 5) continue;
-    const double cost = rounds(c.NT, 3 - c.sets) * c.chunk;
+    const double cost = std::ceil((double)tiles * std::ceil(rows / c.NT) / ((double)sm_count() * (3 - c.sets))) * c.chunk[f.group_log - 5];
     if (!best || cost < least) best = &c, least = cost;
   }
   const auto go = [&](auto type) {
     using T = decltype(type);
-    return best->NT == 32    ? (best->sets == 2 ? launch<T, 32, 2>(f, st) : launch<T, 32, 1>(f, st))
-           : best->NT == 64  ? (best->sets == 2 ? launch<T, 64, 2>(f, st) : launch<T, 64, 1>(f, st))
-           : best->NT == 128 ? launch<T, 128, 2>(f, st)
-                             : launch<T, 192, 2>(f, st);
+    return best->NT == 32   ? (best->sets == 2 ? launch<T, 32, 2>(f, st) : launch<T, 32, 1>(f, st))
+           : best->NT == 64 ? (best->sets == 2 ? launch<T, 64, 2>(f, st) : launch<T, 64, 1>(f, st))
+                            : launch<T, 128, 2>(f, st);
   };
   return f.a.bf16 ? go(__nv_bfloat16()) : go(__half());
 }
