@@ -12,7 +12,7 @@ import re
 import pytest
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2608_27888_gb300", "csrc")
-ALLOC = re.compile(r"\b(?:tmem_alloc|tmem_take(?:<\w+>)?)\(saddr|asm volatile\(\"tcgen05\.alloc\b[^\n]*columns")
+ALLOC = re.compile(r"\b(?:tmem_alloc|tmem_take(?:<\w+>)?)\(saddr|asm volatile\(\"tcgen05\.alloc\b[^\n]*olumns")
 BARRIER = re.compile(r"__syncthreads\(\)|\bmake_table\(")  # make_table ends with one
 
 
