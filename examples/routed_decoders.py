@@ -36,7 +36,8 @@ def train(steps=200, experts=8, top_k=2, hidden=128, batch=8192, rate=0.02, seed
     g = torch.Generator(device="cuda").manual_seed(seed)
     x, target = teacher()
     layer = RoutedExperts(x.shape[1], hidden, target.shape[1], experts, top_k, generator=g)
-    adam = AdamW(layer.parameters(), lr=rate, beta2=0.99, weight_decay=0.0, bits=bits)
+    # moments in 8 bits do not follow a decay as fast as 0.99
+    adam = AdamW(layer.parameters(), lr=rate, beta2=0.99 if bits == 32 else 0.999, weight_decay=0.0, bits=bits)
     errors = []
     for step in range(1, steps + 1):
         at = torch.randint(0, x.shape[0], (batch,), generator=g, device="cuda")

@@ -144,7 +144,8 @@ def adamw(params, grads, m, v, *, step, lr, beta1: float = 0.9, beta2: float = 0
 
     params and grads in fp32, fp16 or bf16, each tensor in its own; m and v fp32, or float8_e4m3fn with scales: fp32
     [2, ceil(numel / 256)] for each tensor.  All start at zero.  copies: None, or a list with None or a tensor for each
-    parameter, which receives the parameter in its own type.  step counts from 1.  step (int32), lr and grad_scale
+    parameter, which receives the parameter in its own type.  With moments in float8_e4m3fn use a beta2 of 0.995 or more:
+    ntc_adamw says what smaller ones do.  step counts from 1.  step (int32), lr and grad_scale
     (fp32) may be CUDA tensors of one element: a call captured in a graph reads them at every replay.  optim.AdamW keeps
     the moments and counts the steps."""
     if stream is not None:

