@@ -80,24 +80,32 @@ class AdamW:
                     steps=int(self.steps))
 
     def load(self, state: dict):
-        """Takes over a state(); the parameters become their masters, rounded."""
+        """Takes over a state(), or, where it does not fit, nothing of it; the parameters become their masters, rounded."""
         mine = self.state()
         if (mine["scales"] is None) != (state["scales"] is None):
             raise ValueError("the state's moments have another number of bits")
+        pairs = []  # all of the state is looked at before any of it is taken
+        for k in ("m", "v", "scales", "masters"):
+            if mine[k] is None:
+                continue
+            if len(mine[k]) != len(state[k]):
+                raise ValueError(f"the state has {len(state[k])} {k}, not {len(mine[k])}")
+            for to, of in zip(mine[k], state[k]):
+                if to.shape != of.shape:
+                    raise ValueError(f"{k}: shape {tuple(of.shape)}, not {tuple(to.shape)}")
+                if (to.dtype == torch.float8_e4m3fn) != (of.dtype == torch.float8_e4m3fn):
+                    raise ValueError(f"{k}: {of.dtype}, not {to.dtype}: codes mean nothing without their scales")
+                pairs.append((to, of))
+        steps = int(state["steps"])
+        if steps < 0:
+            raise ValueError(f"steps must not be negative: {steps}")
         with torch.no_grad():
-            for k in ("m", "v", "scales", "masters"):
-                if mine[k] is None:
-                    continue
-                if len(mine[k]) != len(state[k]):
-                    raise ValueError(f"the state has {len(state[k])} {k}, not {len(mine[k])}")
-                for to, of in zip(mine[k], state[k]):
-                    if to.shape != of.shape:
-                        raise ValueError(f"{k}: shape {tuple(of.shape)}, not {tuple(to.shape)}")
-                    to.copy_(of)
+            for to, of in pairs:
+                to.copy_(of)
             for p, c in zip(self.masters, self.copies):
                 if c is not None:
                     c.copy_(p)
         if self.captured:
-            self.steps.fill_(state["steps"])
+            self.steps.fill_(steps)
         else:
-            self.steps = state["steps"]
+            self.steps = steps
