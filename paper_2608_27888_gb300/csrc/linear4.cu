@@ -248,64 +248,64 @@ __global__ void __launch_bounds__(kThreads, kCtas<NT, MT>) k_linear4_few(const F
           for (int r = 0; r < 4; ++r) part[warp][8 * h + 2 * t + (r & 1)][m * 16 + g + 8 * (r >> 1)] = sum[m][h][r];
       team_sync();
       if constexpr (NT == 1) {
-      // 16 threads write 16 columns of a row
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const uint32_t n = m * 16 + (lane & 15), col = n0 + n;
-        if (col >= N) break;
-        const float bias = a.bias ? a.bias[(uint64_t)e * N + col] : 0.0f;
-#pragma unroll 1
-        for (int32_t r = slice * 2 + (lane >> 4); r < rows; r += 2 * split) {
-          const uint64_t row = (uint64_t)(begin[i] + m0) + r;
-          float v[1] = {0.0f};
-          const bool none = a.rows && ld_word((const uint32_t *)a.rows + row) >= a.x_rows;
-          for (uint32_t p = 0; p < split; ++p) v[0] += part[team * split + p][r][n];
-          v[0] = (none ? 0.0f : v[0]) + bias;
-          activate(a.activation, a.slope, v);
-          if (a.residual) v[0] += to_f<T>(((const T *)a.residual)[row * a.ld_residual + col]);
-          ((T *)a.out)[row * a.ld_out + col] = from_f<T>(v[0]);
-        }
-      }
-      } else {
-      // 16 threads write 16 columns of a row; what they read comes for several rows at a time
-      constexpr int kBatch = 4;
-      const uint32_t by = 2 * split;
-#pragma unroll 1
-      for (uint32_t r0 = slice * 2 + (lane >> 4); r0 < (uint32_t)rows; r0 += kBatch * by) {
-        const uint64_t row0 = (uint64_t)(begin[i] + m0) + r0;
-        float add[MT][kBatch], v[MT * kBatch];
-        bool none[kBatch];
-#pragma unroll
-        for (int q = 0; q < kBatch; ++q) {
-          const bool is = r0 + q * by < (uint32_t)rows;
-          none[q] = is && a.rows && ld_word((const uint32_t *)a.rows + row0 + q * by) >= a.x_rows;
-#pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            const uint32_t col = n0 + m * 16 + (lane & 15);
-            add[m][q] = is && a.residual && col < N ? to_f<T>(((const T *)a.residual)[(row0 + q * by) * a.ld_residual + col]) : 0.0f;
-          }
-        }
+        // 16 threads write 16 columns of a row
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           const uint32_t n = m * 16 + (lane & 15), col = n0 + n;
-          const float bias = a.bias && col < N ? a.bias[(uint64_t)e * N + col] : 0.0f;
-#pragma unroll
-          for (int q = 0; q < kBatch; ++q) {
-            float z = 0.0f;
-            if (r0 + q * by < (uint32_t)rows && !none[q])
-              for (uint32_t p = 0; p < split; ++p) z += part[team * split + p][r0 + q * by][n];
-            v[m * kBatch + q] = z + bias;
+          if (col >= N) break;
+          const float bias = a.bias ? a.bias[(uint64_t)e * N + col] : 0.0f;
+#pragma unroll 1
+          for (int32_t r = slice * 2 + (lane >> 4); r < rows; r += 2 * split) {
+            const uint64_t row = (uint64_t)(begin[i] + m0) + r;
+            float v[1] = {0.0f};
+            const bool none = a.rows && ld_word((const uint32_t *)a.rows + row) >= a.x_rows;
+            for (uint32_t p = 0; p < split; ++p) v[0] += part[team * split + p][r][n];
+            v[0] = (none ? 0.0f : v[0]) + bias;
+            activate(a.activation, a.slope, v);
+            if (a.residual) v[0] += to_f<T>(((const T *)a.residual)[row * a.ld_residual + col]);
+            ((T *)a.out)[row * a.ld_out + col] = from_f<T>(v[0]);
           }
         }
-        activate(a.activation, a.slope, v);
+      } else {
+        // 16 threads write 16 columns of a row; what they read comes for several rows at a time
+        constexpr int kBatch = 4;
+        const uint32_t by = 2 * split;
+#pragma unroll 1
+        for (uint32_t r0 = slice * 2 + (lane >> 4); r0 < (uint32_t)rows; r0 += kBatch * by) {
+          const uint64_t row0 = (uint64_t)(begin[i] + m0) + r0;
+          float add[MT][kBatch], v[MT * kBatch];
+          bool none[kBatch];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const uint32_t col = n0 + m * 16 + (lane & 15);
+          for (int q = 0; q < kBatch; ++q) {
+            const bool is = r0 + q * by < (uint32_t)rows;
+            none[q] = is && a.rows && ld_word((const uint32_t *)a.rows + row0 + q * by) >= a.x_rows;
 #pragma unroll
-          for (int q = 0; q < kBatch; ++q)
-            if (r0 + q * by < (uint32_t)rows && col < N) ((T *)a.out)[(row0 + q * by) * a.ld_out + col] = from_f<T>(v[m * kBatch + q] + add[m][q]);
+            for (int m = 0; m < MT; ++m) {
+              const uint32_t col = n0 + m * 16 + (lane & 15);
+              add[m][q] = is && a.residual && col < N ? to_f<T>(((const T *)a.residual)[(row0 + q * by) * a.ld_residual + col]) : 0.0f;
+            }
+          }
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const uint32_t n = m * 16 + (lane & 15), col = n0 + n;
+            const float bias = a.bias && col < N ? a.bias[(uint64_t)e * N + col] : 0.0f;
+#pragma unroll
+            for (int q = 0; q < kBatch; ++q) {
+              float z = 0.0f;
+              if (r0 + q * by < (uint32_t)rows && !none[q])
+                for (uint32_t p = 0; p < split; ++p) z += part[team * split + p][r0 + q * by][n];
+              v[m * kBatch + q] = z + bias;
+            }
+          }
+          activate(a.activation, a.slope, v);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const uint32_t col = n0 + m * 16 + (lane & 15);
+#pragma unroll
+            for (int q = 0; q < kBatch; ++q)
+              if (r0 + q * by < (uint32_t)rows && col < N) ((T *)a.out)[(row0 + q * by) * a.ld_out + col] = from_f<T>(v[m * kBatch + q] + add[m][q]);
+          }
         }
-      }
       }
     }
   }

@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
         c += many, used += many;
       }
     }
-    if (!ok && any) {
+    if (any) {  // none of its MMAs is in flight when the tensor memory goes back, whoever gave up a wait
       if (leader) umma_commit(saddr(&s.drain[mine]));
       __syncwarp();
       mbar_wait(saddr(&s.drain[mine]), 0);
