@@ -615,8 +615,8 @@ NTC_API ntc_status ntc_balance_loss_backward(const ntc_balance_desc *desc, size_
  * part only: (1 - beta2) / 2 of itself a step is less than half of a code's distance, and where the gradients of a
  * block have one size the roots settle too high.  With normally distributed ones and beta1 = 0.9 the median root is,
  * times fp32's, after 1,000 and 4,000 steps
- *   beta2 0.98: 1.52, 1.67   0.99: 1.30, 1.35   0.995: 1.16, 1.16   0.999: 1.08, 1.09
- * and the steps' root mean square is smaller by 31, 37; 21, 25; 11, 11; 1, 1 percent.  Where the sizes in a
+ *   beta2 0.98: 1.56, 1.66   0.99: 1.31, 1.37   0.995: 1.16, 1.17   0.999: 1.09, 1.12
+ * and the steps' root mean square is smaller by 32, 36; 22, 25; 11, 12; 3, 5 percent.  Where the sizes in a
  * block differ by factors of e the root is within 5 percent at each of them.  Use 0.995 or more.  Where a moment's largest is below
  * 2^-100 its block is 0; both moments of a block with an infinity or a NaN read back as
  * NaN. */

@@ -6,9 +6,9 @@ every 256 of a tensor) with ``bits=8``.  Gradients come with the call, as the
 ``*_backward`` functions return them.
 
 Eight bits are too few for a slow decay: where the gradients of a block of 256 have one size,
-the roots of the second moment settle 1.09 times too high with beta2 = 0.999, 1.16 times with
-0.995, 1.35 times with 0.99 and 1.67 times with 0.98 (medians after 4,000 steps of normally
-distributed gradients, beta1 = 0.9), and the steps are 1, 11, 25 and 37 % too small.
+the roots of the second moment settle 1.12 times too high with beta2 = 0.999, 1.17 times with
+0.995, 1.37 times with 0.99 and 1.66 times with 0.98 (medians after 4,000 steps of normally
+distributed gradients, beta1 = 0.9), and the steps are 5, 12, 25 and 36 % too small.
 """
 from __future__ import annotations
 

@@ -1,31 +1,53 @@
-"""Moments in 8 bits over many steps of random gradients, against fp32: the roots settle as high as the header says."""
+"""Moments in 8 bits over many steps of random gradients: the definition's, bit for bit, and as high as the header says."""
 import pytest
 import torch
 
 pytestmark = pytest.mark.gpu
-F8 = torch.float8_e4m3fn
+F, F8 = torch.float32, torch.float8_e4m3fn
 
-# The definition's recurrence on the CPU, gradients of one size (size 0) and of sizes that differ by factors of e, beta1 0.9:
-# median of root / fp32's root after 1,000 steps.  Other gradients and 64 blocks: the median of 16,384 roots has a standard
-# error of 1.25 * spread / 128, below 0.01 for a spread below 1.
-MEDIAN = {(0.98, 0): 1.52, (0.99, 0): 1.30, (0.995, 0): 1.16, (0.999, 0): 1.08, (0.98, 1): 1.00, (0.99, 1): 1.03, (0.999, 1): 1.00}
+# The definition's recurrence on the CPU, gradients of one size (0) and of sizes that differ by factors of e (1), beta1 0.9:
+# median of root / fp32's root after 1,000 steps, 512 blocks (256 for sizes).  A block's roots hang on its largest, so 64
+# blocks are a sample of 64: five seeds of 64 blocks gave 1.54 to 1.58, 1.30 to 1.32, 1.13 to 1.21 and 1.03 to 1.11, standard
+# deviations of 0.017, 0.009, 0.033 and 0.032.  Four times the largest is 0.13.
+MEDIAN = {(0.98, 0): 1.556, (0.99, 0): 1.306, (0.995, 0): 1.162, (0.999, 0): 1.093, (0.98, 1): 1.018, (0.99, 1): 1.041, (0.999, 1): 1.0}
+
+
+def encode(x, root):
+    """e4m3 codes and scales, operation by operation in fp32 as the header has them."""
+    f = x.view(-1, 256)
+    top = f.abs().amax(1, keepdim=True)
+    top = torch.where(top >= 2.0 ** -100, top, torch.zeros_like(top))
+    y = torch.where(top > 0, f * torch.div(torch.full_like(top, 448.0), top), torch.zeros_like(f))
+    if root:
+        y = torch.where(y > 0, y.clamp_min(2.0 ** -9), y)
+    return y.to(F8).view(-1), (top * torch.tensor(1.0 / 448.0, dtype=F, device="cuda")).view(-1)
 
 
 @pytest.mark.parametrize("beta2,size", list(MEDIAN))
 def test_roots_after_a_thousand_steps(beta2, size):
     from paper_2608_27888_gb300 import ntc
-    n = 64 * 256
+    n, beta1 = 64 * 256, 0.9
     g = torch.Generator(device="cuda").manual_seed(7)
     by = torch.exp(size * torch.randn(n, generator=g, device="cuda"))
     runs = []
-    for kind in (torch.float32, F8):
+    for kind in (F, F8):
         m, v = (torch.zeros(n, device="cuda").to(kind) for _ in range(2))
         runs.append((torch.zeros(n, device="cuda"), m, v, [torch.zeros(2, 64, device="cuda")] if kind == F8 else None))
+    one = lambda x: torch.tensor(x, dtype=F, device="cuda")  # noqa: E731
+    b1, c1, b2, c2 = one(beta1), one(1 - beta1), one(beta2), one(1 - beta2)
+    cm, cr = (torch.zeros(n, device="cuda").to(F8) for _ in range(2))
+    sm, sr = (torch.zeros(64, device="cuda") for _ in range(2))
     for t in range(1, 1001):
         grad = torch.randn(n, generator=g, device="cuda") * by
         for p, m, v, s in runs:
             ntc.adamw([p], [grad], [m], [v], scales=s, step=t, lr=1e-3, beta2=beta2, weight_decay=0.0)
+        m0, r0 = cm.float() * sm.repeat_interleave(256), cr.float() * sr.repeat_interleave(256)
+        cm, sm = encode(m0 * b1 + grad * c1, False)
+        cr, sr = encode(torch.sqrt((r0 * r0) * b2 + (grad * c2) * grad), True)
     full, eight = runs
+    for mine, want in ((eight[1], cm), (eight[2], cr)):
+        assert torch.equal(mine.view(torch.uint8), want.view(torch.uint8))
+    assert torch.equal(eight[3][0], torch.stack([sm, sr]))
     root = eight[2].float() * eight[3][0][1].repeat_interleave(256)
     median = float((root / full[2].sqrt()).median())
-    assert abs(median - MEDIAN[beta2, size]) <= 0.03, median
+    assert abs(median - MEDIAN[beta2, size]) <= 0.13, median
