@@ -36,6 +36,9 @@ struct FewArgs {
   uint32_t split;  // warps along K: 1, 2, 4 or 8
 };
 
+// What an index outside x reads: a row of zeros, as long as rows get.
+__device__ uint4 zero_row[(1u << 20) / 8];
+
 template <int NT, int MT>
 constexpr int kCtas = NT * MT == 1 ? 3 : 2;  // on an SM: what registers leave
 
@@ -174,14 +177,13 @@ __global__ void __launch_bounds__(kThreads, kCtas<NT, MT>) k_linear4_few(const F
         }
       };
       if (c_from < c_to) fetch(c_from, std::false_type{});
-      // Columns of the MMAs that are no row read some row: nobody looks at their sums.  A row that is named but not
-      // there is zeros (`none`).
+      // Columns of the MMAs that are no row read some row: nobody looks at their sums
       const uint16_t *x[NT];
 #pragma unroll
       for (int h = 0; h < NT; ++h) {
         const int32_t r = min((int32_t)g + 8 * h, rows - 1) + begin[i] + m0;
         const uint32_t at = a.rows ? ld_word((const uint32_t *)a.rows + r) : (uint32_t)r;
-        x[h] = (const uint16_t *)a.x + (at < a.x_rows ? at * a.ld_x : 0);
+        x[h] = at < a.x_rows ? (const uint16_t *)a.x + at * a.ld_x : (const uint16_t *)zero_row;
       }
       // K of the lane's word j of chunk c
       const auto k_of = [&](uint32_t c, int j) { return c * kChunk + j / kSteps * GROUP + t * (GROUP / 4) + j % kSteps * 8; };
@@ -258,9 +260,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<NT, MT>) k_linear4_few(const F
           for (int32_t r = slice * 2 + (lane >> 4); r < rows; r += 2 * split) {
             const uint64_t row = (uint64_t)(begin[i] + m0) + r;
             float v[1] = {0.0f};
-            const bool none = a.rows && ld_word((const uint32_t *)a.rows + row) >= a.x_rows;
             for (uint32_t p = 0; p < split; ++p) v[0] += part[team * split + p][r][n];
-            v[0] = (none ? 0.0f : v[0]) + bias;
+            v[0] += bias;
             activate(a.activation, a.slope, v);
             if (a.residual) v[0] += to_f<T>(((const T *)a.residual)[row * a.ld_residual + col]);
             ((T *)a.out)[row * a.ld_out + col] = from_f<T>(v[0]);
@@ -274,11 +275,9 @@ __global__ void __launch_bounds__(kThreads, kCtas<NT, MT>) k_linear4_few(const F
         for (uint32_t r0 = slice * 2 + (lane >> 4); r0 < (uint32_t)rows; r0 += kBatch * by) {
           const uint64_t row0 = (uint64_t)(begin[i] + m0) + r0;
           float add[MT][kBatch], v[MT * kBatch];
-          bool none[kBatch];
 #pragma unroll
           for (int q = 0; q < kBatch; ++q) {
             const bool is = r0 + q * by < (uint32_t)rows;
-            none[q] = is && a.rows && ld_word((const uint32_t *)a.rows + row0 + q * by) >= a.x_rows;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
               const uint32_t col = n0 + m * 16 + (lane & 15);
@@ -292,7 +291,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<NT, MT>) k_linear4_few(const F
 #pragma unroll
             for (int q = 0; q < kBatch; ++q) {
               float z = 0.0f;
-              if (r0 + q * by < (uint32_t)rows && !none[q])
+              if (r0 + q * by < (uint32_t)rows)
                 for (uint32_t p = 0; p < split; ++p) z += part[team * split + p][r0 + q * by][n];
               v[m * kBatch + q] = z + bias;
             }

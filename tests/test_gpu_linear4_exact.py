@@ -116,3 +116,24 @@ def test_a_rows_digits_do_not_depend_on_the_batch(ntc, dtype, K):
             y = ntc.linear4(cut(x[:T], dtype, at), packed, scales, group=64)
             off = mag[:T] * (K + 8) * R.F32
             R.assert_within(y, want[:T], off + R.UNIT[dtype] * (want[:T].abs() + off) + R.TINY[dtype], (T, at))
+
+
+@pytest.mark.parametrize("dtype", [B, H])
+@pytest.mark.parametrize("T", [3, 12, 30, 100, 900])
+@pytest.mark.parametrize("K", [128, 100])
+def test_an_index_outside_x_reads_zeros_whatever_the_rows(ntc, T, K, dtype):
+    """Zeros times a scale that is no number are no number, as in the product with 16-bit weights; elsewhere the bias is left."""
+    packed, scales, _, g = whole(1, 70, K, 32, dtype, T)
+    scales[0, 7, 1], scales[0, 68, 2] = math.nan, math.inf
+    x = torch.full((4, K), math.nan, dtype=dtype, device="cuda")
+    x[1:3] = 1.0
+    rows = torch.randint(1, 3, (T,), generator=g, device="cuda", dtype=torch.int32)
+    rows[::3], rows[1::3] = -1, 4
+    bias = torch.randn(70, generator=g, device="cuda")
+    y = ntc.linear4(x, packed[0], scales[0], bias, group=32, rows=rows)
+    z = ntc.linear(x, ntc.unpack4(packed[0], scales[0], K, group=32), bias, rows=rows)
+    bad = torch.zeros(70, dtype=torch.bool, device="cuda")
+    bad[7] = bad[68] = True
+    for out in (y, z):
+        gone = out[(rows < 0) | (rows > 3)]
+        assert bool(torch.isnan(gone[:, bad]).all()) and torch.equal(gone[:, ~bad], bias[~bad].to(dtype).expand(gone.shape[0], -1))
