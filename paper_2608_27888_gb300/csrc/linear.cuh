@@ -91,40 +91,52 @@ __device__ __forceinline__ int32_t offset_before(const int32_t *offsets, uint32_
 }
 
 // A warp lists the experts that have rows (first row, rows, number) in shared memory:
-// *active of them, and *live rows of any.
+// *active of them, and *live rows of any.  The pass for offsets that fall is a loop of its own:
+// inlined into the first one, which loads several experts' offsets together, it cost every call
+// half a microsecond of instruction fetches.
 __device__ __forceinline__ void list_experts(const LinearArgs &a, uint32_t lane, int32_t *begin, int32_t *count, uint16_t *which,
                                              uint32_t *active, uint32_t *live) {
   constexpr uint32_t kAtOnce = 4;
   const uint32_t E = a.num_experts;
+  const int32_t rows = (int32_t)a.num_rows;
   uint32_t many = 0;
   int32_t end = 0;
-  bool falls = false;  // an offset is above the next: once more, with offset_before
-  for (bool again = false;; again = true) {
-    const int32_t rows = (int32_t)a.num_rows;
-    for (uint32_t e0 = 0; e0 < E; e0 += 32 * kAtOnce) {
-      // the offsets of several experts a lane are on their way together
-      int32_t b[kAtOnce], n[kAtOnce];
+  bool falls = false;
+  const auto list = [&](uint32_t e, int32_t b) {  // by the whole warp: the lane's expert from row b to `end`
+    const int32_t n = e < E ? end - b : 0;
+    const uint32_t has = __ballot_sync(0xFFFFFFFFu, n > 0), at = many + __popc(has & ((1u << lane) - 1));
+    falls |= n < 0;
+    if (n > 0) begin[at] = b, count[at] = n, which[at] = (uint16_t)e;
+    many += __popc(has);
+  };
+#pragma unroll 1
+  for (uint32_t e0 = 0; e0 < E; e0 += 32 * kAtOnce) {
+    int32_t from[kAtOnce], to[kAtOnce];  // the offsets of several experts a lane are on their way together
 #pragma unroll
-      for (uint32_t q = 0; q < kAtOnce; ++q) {
-        const uint32_t e = e0 + 32 * q + lane;
-        b[q] = n[q] = 0;
-        if (e < E) {
-          b[q] = !a.offsets ? 0 : again ? offset_before(a.offsets, e, E, rows) : offset_at(a.offsets, e, rows);
-          end = !a.offsets ? rows : again ? offset_before(a.offsets, e + 1, E, rows) : offset_at(a.offsets, e + 1, rows);
-          n[q] = end - b[q];
-        }
-        falls |= n[q] < 0;
-      }
-#pragma unroll
-      for (uint32_t q = 0; q < kAtOnce; ++q) {
-        const uint32_t has = __ballot_sync(0xFFFFFFFFu, n[q] > 0), at = many + __popc(has & ((1u << lane) - 1));
-        if (n[q] > 0) begin[at] = b[q], count[at] = n[q], which[at] = (uint16_t)(e0 + 32 * q + lane);
-        many += __popc(has);
-      }
+    for (uint32_t q = 0; q < kAtOnce; ++q) {
+      const uint32_t e = e0 + 32 * q + lane;
+      from[q] = e < E && a.offsets ? offset_at(a.offsets, e, rows) : 0;
+      to[q] = e < E && a.offsets ? offset_at(a.offsets, e + 1, rows) : rows;
     }
-    if (again || !__any_sync(0xFFFFFFFFu, falls)) break;
+#pragma unroll
+    for (uint32_t q = 0; q < kAtOnce; ++q) {
+      const uint32_t e = e0 + 32 * q + lane;
+      if (e < E) end = to[q];
+      list(e, from[q]);
+    }
+  }
+  if (__any_sync(0xFFFFFFFFu, falls)) {  // an offset is above the next: once more, each as the smallest from there on
     many = 0;
     __syncwarp();
+#pragma unroll 1
+    for (uint32_t e = lane; e - lane < E; e += 32) {
+      int32_t b = 0;
+      if (e < E) {
+        end = offset_before(a.offsets, e + 1, E, rows);
+        b = min(offset_at(a.offsets, e, rows), end);
+      }
+      list(e, b);
+    }
   }
   const int32_t last = __shfl_sync(0xFFFFFFFFu, end, (E - 1) & 31);
   if (lane == 0) *active = many, *live = (uint32_t)last;
