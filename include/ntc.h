@@ -606,8 +606,10 @@ NTC_API ntc_status ntc_balance_loss_backward(const ntc_balance_desc *desc, size_
  * p rounded to its own type (the 16-bit weights of fp32 masters).
  * moment_bits 32: m and v are fp32.  moment_bits 8: m and v hold e4m3 codes of m
  * and of sqrt(v), in blocks of NTC_ADAMW_BLOCK consecutive elements with an fp32
- * scale each, scale_m[i / NTC_ADAMW_BLOCK] and scale_v[...]: value = code * scale,
- * scale = (largest magnitude of the block) / 448, rounded to nearest.  A root that is
+ * scale each, scale_m[i / NTC_ADAMW_BLOCK] and scale_v[...]: value = code * scale.  With top the
+ * largest magnitude of the block, scale = top * fl(1 / 448) and a code is x * fl(448 / top) rounded to the
+ * nearest e4m3 number, fl and the products rounded to fp32 (so the largest reads back within three
+ * roundings of fp32).  A root that is
  * not 0 has at least the least code (2^-9), so that no division loses its denominator.
  * The step itself uses the moments before they are rounded.  A moment that changes by less than
  * half of a code's distance (up to 1/16 of its value) keeps its code, relative to its block's
@@ -665,8 +667,9 @@ typedef struct {
   uint64_t stride_scales;
 } ntc_pack4_desc;
 
-/* scale = max |w| of the group / 7, rounded to `type`; q = w / scale rounded to
- * nearest even and held in -8..7 (0 where the scale is 0).  A group with an infinity
+/* scale = max |w| of the group * fl(1 / 7), fl and the product rounded to fp32, then rounded to
+ * `type` (for fp32 weights a rounding more than max / 7 has: 13.91796875 gives 1.9921875 in bf16, its seventh
+ * 1.984375); q = w / scale rounded to nearest even and held in -8..7 (0 where the scale is 0).  A group with an infinity
  * or a NaN has the scale NaN; one whose scale is above the type's largest number has an
  * infinite scale and reads back as NaN.  Where in_dim is odd the last half byte is q = 0.
  * w[E][N][ld_w] of w_type, stride_w elements from expert to expert. */

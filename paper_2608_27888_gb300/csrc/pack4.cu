@@ -1,6 +1,6 @@
 // Weights to 4 bits with a scale for each group along K, and back.
 //
-//   s = max |w| / 7 of the group, rounded to 16 bits;  q = w / s rounded, held in -8..7;
+//   s = max |w| times 1/7 of the group in fp32, rounded to 16 bits;  q = w / s rounded, held in -8..7;
 //   back: s q, rounded once
 //
 // A lane has eight consecutive weights of a row (16 bytes, of which four bytes remain), a
@@ -54,8 +54,9 @@ struct Pack4 {
   uint32_t in_dim, out_dim, num_experts, group;
 };
 
-// Two quotients w / s, correctly rounded to fp32: the product with an approximate 1 / s,
-// put right by its remainder, which one fused operation gives exactly.
+// Two quotients w / s: the product with an approximate 1 / s, put right by its remainder, which
+// one fused operation gives exactly (Markstein's correction).  Off by an ulp at most, of which
+// `numbers` needs less: see there.
 __device__ __forceinline__ uint64_t quotients(uint64_t w, float s, float inv) {
   const uint64_t i = both(inv, inv), q = mul2(w, i);
   return fma2(fma2(q, both(-s, -s), w), i, q);

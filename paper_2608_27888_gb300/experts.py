@@ -11,8 +11,8 @@ library refuses NtcError.
 
 Autograd does not record these calls: a result has no gradient, and an input that requires
 one draws a warning.  The ``*_backward`` functions compute the gradients.  A call returns
-before its kernels have run; ``ntc.ntc_linear_status`` tells whether one of ``linear`` or
-``linear_backward`` gave up a wait since it was last asked, which makes results invalid
+before its kernels have run; ``ntc.ntc_linear_status`` tells whether one of ``linear``,
+``linear_backward`` or ``linear4`` gave up a wait since it was last asked, which makes results invalid
 (a fault of the machine, for valid calls get on).
 """
 from __future__ import annotations
