@@ -19,9 +19,10 @@
 //                in flight.
 //   4 or 8 warps add the groups, and write the tile while the others are at the next one.
 // Unpacked weights never touch HBM.
-// Bound by instructions (issue slots 67 %): a chunk takes 930 cycles with NT = 128, of which the
-// MMAs are 260 (1,024 tokens of 2 of 16 experts, 2,048 -> 2,048, groups of 128: 53 us; of 64: 70;
-// of 32: 92).  With the products s q rounded to 16 bits and no sums but the accumulator's it
+// Bound by the converting and adding warps' instructions and the hand-overs between them (issue
+// slots busy 50 to 67 %, the tensor pipe 25 %): a chunk takes 900 cycles with NT = 128, of which
+// the MMAs are 260 (1,024 tokens of 2 of 16 experts, 2,048 -> 2,048, groups of 128: 52 us; of 64:
+// 70; of 32: 99).  With the products s q rounded to 16 bits and no sums but the accumulator's it
 // was 43 for each.  Tried: sums by the converting threads (66 us, 134 for groups of 32), one set of
 // them with two accumulators of 192 rows (62), fp32x2 sums (57, their pairs are moved together),
 // sleeping waits (no gain; slower for groups of 32), a wait by one lane for its warp (67).
@@ -328,6 +329,7 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
       const uint32_t col = o.n0 + column;
       const uint16_t *scales = f.scales + o.e * f.stride_scales + (uint64_t)(col < N ? col : 0) * f.ld_scales;
       uint32_t scale = scales[0];
+      const float bias = a.bias && col < N ? a.bias[(uint64_t)o.e * N + col] : 0.0f;
       float sum[kBatches][kBatch];
 #pragma unroll
       for (int b = 0; b < kBatches; ++b)
@@ -362,7 +364,6 @@ __global__ void __launch_bounds__(threads(SETS), 3 - SETS) k_linear4_mid(const M
         if (lane == 0) mbar_arrive(saddr(&s.acc_empty[slot]));
       }
       if (!ok) break;
-      const float bias = a.bias && col < N ? a.bias[(uint64_t)o.e * N + col] : 0.0f;
       // one batch's code for all: the others' sums move up
 #pragma unroll 1
       for (uint32_t r0 = r_first; r0 < o.rows; r0 += SETS * kBatch) {
