@@ -13,7 +13,7 @@
 // Few (expert, rows) pairs are split along K over the warps of a CTA, whose sums meet
 // in shared memory in a fixed order.
 // Latency of the loads is the bound at four warps a scheduler (64 tokens of 4 of 32 experts,
-// 1,024 -> 2,048, fp16: 25 us, 1.4 TB/s of packed weights; 61 through shared memory), a launch
+// 1,024 -> 2,048, fp16: 26 us, 1.3 TB/s of packed weights; 61 through shared memory), a launch
 // for a token (8 of 64 experts, 2,048 -> 1,024: 8 us).
 // More rows per expert: linear4_mid.cu, whose tcgen05 tiles unpack the weights on their way into
 // shared memory, with the same formula; operands that do not start on 16 bytes are copied for it.
