@@ -137,3 +137,46 @@ def test_an_index_outside_x_reads_zeros_whatever_the_rows(ntc, T, K, dtype):
     for out in (y, z):
         gone = out[(rows < 0) | (rows > 3)]
         assert bool(torch.isnan(gone[:, bad]).all()) and torch.equal(gone[:, ~bad], bias[~bad].to(dtype).expand(gone.shape[0], -1))
+
+
+@pytest.mark.parametrize("K", [96, 97])
+def test_copied_operands_with_offsets_that_are_anything(ntc, K):
+    """Operands at odd addresses are copied for the experts that have rows, whatever the offsets: the same bits as in order."""
+    T, E, N = 400, 5, 40
+    packed, scales, _, g = whole(E, N, K, 32, B, K)
+    x = torch.randn(T, K, generator=g, device="cuda").to(B)
+    rows = torch.randint(-1, T + 1, (T,), generator=g, device="cuda", dtype=torch.int32)
+    for o in ([0, 0, 2, 1, 4, T], [-5, 3, 3, 3, 4, 10 * T], [T] * 6, [0] * 6, [2, 1, 0, 3, 2, T // 2], [-2 ** 31, 2 ** 31 - 1, 0, 1, 2, 3],
+              [0, T, 50, 60, 55, T]):
+        offsets = torch.tensor(o, dtype=torch.int32, device="cuda")
+        a = ntc.linear4(cut(x, B, 0), packed, scales, group=32, rows=rows, offsets=offsets)
+        b = ntc.linear4(cut(x, B, 3), shift(packed, 255), shift(scales, math.nan), group=32, rows=rows, offsets=offsets)
+        first = min(max(0, min(v, T)) for v in o)  # rows before the first offset have no result
+        assert torch.equal(a[first:], b[first:]), o
+
+
+def test_copied_operands_in_graphs_and_on_streams(ntc):
+    packed, scales, _, g = whole(3, 70, 101, 32, H, 5)
+    x = [torch.randn(500, 101, generator=g, device="cuda").to(H) for _ in range(3)]
+    offsets = torch.tensor([0, 100, 100, 480], dtype=torch.int32, device="cuda")
+    want = [ntc.linear4(cut(t, H, 1), packed, scales, group=32, offsets=offsets) for t in x]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    live = [cut(x[0], H, 1), cut(x[0], H, 5)]
+    y = ntc.linear4(live[0], packed, scales, group=32, offsets=offsets, stream=side)
+    side.synchronize()
+    assert torch.equal(y, want[0])
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    for t, graph in zip(live, graphs):
+        with torch.cuda.graph(graph):
+            outs.append(ntc.linear4(t, packed, scales, group=32, offsets=offsets))
+    for i in (1, 2):
+        live[0].copy_(x[i])
+        live[1].copy_(x[3 - i])
+        torch.cuda.synchronize()
+        for graph in graphs:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                graph.replay()
+                graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want[i]) and torch.equal(outs[1], want[3 - i])
